@@ -1,0 +1,489 @@
+"""Operators of the end of a network, for classes by the thousand or vocabularies by the hundred thousand, as cases that can be timed:
+
+  score    log probabilities of given tokens, with each row's entropy and its most probable tokens
+  train    the same log probabilities and entropies, and the gradient of a weighted sum of them in the logits
+  quant    microscaled 4-bit floating point: a tensor into codes with a scale for every 32 values, and back into numbers
+  product  FullyConnected on such a filter: the input is quantised within the call, then bias and ReLU
+  adamw    one AdamW step over many tensors, with states of 32 bits or of 8 bits
+
+The plain forms below are elementary torch operations in 32 bits; with `own` the calls of paper_1512_01274_amd.mxc run.
+"""
+import math
+import random
+
+import torch
+
+own = False
+
+DTYPE = {"f32": torch.float32, "bf16": torch.bfloat16}
+CODE = {"f32": 0, "bf16": 1}        # MXC_F32, MXC_BF16
+SIZE = {"f32": 4, "bf16": 2}
+
+
+def _rows(name, kind, N, K, pad, dtype, top, mask, temperature):
+    """pad: columns between a row's last logit and the next row; mask: how forbidden tokens are marked (0: there are none, 1: minus
+    infinity, one row without any allowed token among them, 2: the type's lowest value)."""
+    return {"name": name, "kind": kind, "N": N, "K": K, "pad": pad, "dtype": dtype, "top": top, "mask": mask, "temperature": temperature}
+
+
+def _adamw(name, bits, count, least, most, sizes, grad, copy):
+    """count tensors of least..most values, spread by `sizes`; bits: 32 or 8 for each state; copy: a bf16 copy of the weights too."""
+    return {"name": name, "kind": "adamw", "bits": bits, "count": count, "least": least, "most": most, "sizes": sizes, "grad": grad, "copy": copy}
+
+
+def listed():
+    return [
+        # one token of one sequence has been decoded: its row of a large vocabulary, and the twenty best alternatives: latency
+        _rows("score_token", "score", 1, 131072, 0, "bf16", 20, 0, 1.0),
+        # a prompt of 4096 tokens is scored: an odd vocabulary in rows padded to whole vectors, forbidden tokens at minus infinity
+        _rows("score_prompt", "score", 4096, 50257, 47, "bf16", 8, 1, 0.7),
+        # the classifier's last layer, 1000 classes at batch 128: microseconds of work
+        _rows("train_classes", "train", 128, 1000, 0, "f32", 0, 0, 1.0),
+        # a step of language training: a gigabyte of logits and another of their gradient
+        _rows("train_vocabulary", "train", 4096, 131072, 0, "bf16", 0, 0, 1.0),
+        # a filter of the network's largest FullyConnected layer is brought into 4 bits
+        {"name": "quant_filter", "kind": "quant", "N": 4096, "C": 9216, "dtype": "f32"},
+        # serving one sample: the filter's bytes and latency count
+        {"name": "product_token", "kind": "product", "N": 1, "C": 4096, "K": 4096, "dtype": "bf16", "bias": False, "relu": False},
+        # serving a batch through the network's largest FullyConnected layer
+        {"name": "product_batch", "kind": "product", "N": 128, "C": 9216, "K": 4096, "dtype": "bf16", "bias": True, "relu": True},
+        # a long prompt: the matrix cores' work
+        {"name": "product_prompt", "kind": "product", "N": 8192, "C": 8192, "K": 8192, "dtype": "bf16", "bias": False, "relu": False},
+        # biases and norms: many small tensors, launches and host time count
+        _adamw("adamw_small", 32, 24, 1, 4096, 3, "f32", True),
+        # a convolution stack and its head, 16 tensors of up to 9216 x 4096 values
+        _adamw("adamw_stack", 32, 16, 64, 37748736, 26, "f32", True),
+        # a deep network's 161 tensors with states of 8 bits and gradients in bf16
+        _adamw("adamw8_deep", 8, 161, 64, 2359296, 1, "bf16", True),
+        # large tensors, where states of 8 bits pay: the bytes of the weights and gradients remain
+        _adamw("adamw8_large", 8, 12, 65536, 67108864, 53, "bf16", False),
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    kind = rng.choice(["score", "train", "quant", "product", "product", "adamw"])
+    dtype = rng.choice(["bf16", "bf16", "f32"])
+    if kind in ("score", "train"):
+        K = _log(rng, 2, 131072)
+        N = _log(rng, 1, max(1, min(16384, (4096 * 131072 if kind == "train" else 4096 * 50257) // (K * SIZE[dtype] // 2))))
+        pad = rng.choice([0, 0, -K % 8, rng.randrange(64)])
+        c = _rows("", kind, N, K, pad, dtype, rng.choice([0, 1, 5, 20, 64]) if kind == "score" else 0, rng.randrange(3),
+                  rng.choice([1.0, 1.0, rng.uniform(0.3, 2.0)]))
+    elif kind == "quant":
+        C = _log(rng, 1, 25088)
+        c = {"kind": kind, "N": _log(rng, 1, max(1, 4096 * 9216 // C)), "C": C, "dtype": dtype}
+    elif kind == "product":
+        N, C, K = (_log(rng, *r) for r in ((1, 8192), (1, 16384), (1, 16384)))
+        if rng.random() < 0.5:
+            C, K = max(32, C // 32 * 32), max(1, K // 16) * 16
+        if N * C * K > 8192 ** 3:
+            N = max(1, 8192 ** 3 // (C * K))
+        c = {"kind": kind, "N": N, "C": C, "K": K, "dtype": dtype, "bias": rng.random() < 0.5, "relu": rng.random() < 0.5}
+    else:
+        bits, count = rng.choice([32, 8]), _log(rng, 1, 300)
+        most = _log(rng, 64, 30000000 // count + 64)
+        c = _adamw("", bits, count, _log(rng, 1, most), most, rng.randrange(1 << 20), dtype, rng.random() < 0.5)
+    c.pop("name", None)
+    return c
+
+
+# ---- inputs ----------------------------------------------------------------------------------------------------------------
+
+def _generator(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def _logits(case, gen):
+    N, K, ld, dtype = case["N"], case["K"], case["K"] + case["pad"], DTYPE[case["dtype"]]
+    z = torch.empty(N, ld, dtype=dtype, device="cuda")
+    labels = torch.randint(0, K, (N,), generator=gen, device="cuda", dtype=torch.int32)
+    rows = max(1, (1 << 27) // ld)
+    for a in range(0, N, rows):          # pieces of 128 Mi values
+        part = torch.randn(min(rows, N - a), ld, generator=gen, device="cuda") * 2.5
+        if case["mask"]:
+            forbidden = torch.rand(part.shape, generator=gen, device="cuda") < 0.05
+            part.masked_fill_(forbidden, -math.inf if case["mask"] == 1 else float(torch.finfo(dtype).min))
+        z[a:a + rows] = part
+    at = torch.arange(N, device="cuda")
+    likely = torch.rand(N, generator=gen, device="cuda") < 0.5                  # the model is right about half of them
+    z[at[likely], labels[likely].long()] = 9.0
+    if case["mask"] == 2:               # here the given tokens are allowed ones
+        z[at[~likely], labels[~likely].long()] = 1.0
+    if case["mask"] and N > 1:
+        z[N // 2, :K] = -math.inf if case["mask"] == 1 else float(torch.finfo(dtype).min)
+    if N > 2:
+        labels[torch.rand(N, generator=gen, device="cuda") < 0.05] = -1         # a prompt's own tokens and padding have no label
+    return z, labels
+
+
+def _sizes(case):
+    r = random.Random(case["sizes"])
+    return [_log(r, case["least"], case["most"]) for _ in range(case["count"])]
+
+
+RECORD = 528        # an 8-bit state holds 256 values in 528 bytes: codes of m, codes of r, 8 scales of m, 8 scales of r
+
+
+def prepare(case, seed):
+    gen = _generator(seed)
+    rand = lambda *shape: torch.randn(*shape, generator=gen, device="cuda")  # noqa: E731
+    new = lambda *shape, dtype=torch.float32: torch.empty(*shape, dtype=dtype, device="cuda")  # noqa: E731
+    s = {"case": case}
+    if case["kind"] in ("score", "train"):
+        N, top = case["N"], case["top"]
+        s["z"], s["labels"] = _logits(case, gen)
+        s["scale"] = 1.0 / case["temperature"]
+        s["logp"], s["entropy"], s["stats"] = new(N), new(N), new(N, 2)
+        if case["kind"] == "train":
+            s["dlogp"] = rand(N).abs() * (-1.0 / N)
+            s["dentropy"] = torch.full((N,), -0.01 / N, device="cuda")
+            s["dz"] = torch.zeros_like(s["z"])
+        elif top:
+            s["top_logp"], s["top_index"] = new(N, top), new(N, top, dtype=torch.int32)
+    elif case["kind"] == "quant":
+        N, C = case["N"], case["C"]
+        s["x"] = (rand(N, C) * 0.02 * torch.exp2(torch.randint(-2, 3, (N, 1), generator=gen, device="cuda"))).to(DTYPE[case["dtype"]])
+        s["codes"], s["scales"] = new(N, -(-C // 32) * 16, dtype=torch.uint8), new(N, -(-C // 512) * 16, dtype=torch.uint8)
+        s["y"] = new(N, C, dtype=torch.bfloat16)
+    elif case["kind"] == "product":
+        N, C, K = case["N"], case["C"], case["K"]
+        s["x"] = torch.relu(rand(N, C)).add_(rand(N, C), alpha=0.05).to(DTYPE[case["dtype"]])
+        blocks = -(-C // 32)
+        # a filter in 4 bits: each block's largest code is at least 4 in size, as the scale's rule has it; past the last column zeros
+        lo, hi = (torch.randint(0, 16, (K, blocks, 16), generator=gen, device="cuda", dtype=torch.uint8) for _ in range(2))
+        lo[:, :, 0] |= 6
+        if C % 32:
+            hi[:, -1, C % 32 // 2:] = 0
+            lo[:, -1, (C % 32 + 1) // 2:] = 0
+        s["w_codes"] = (lo | (hi << 4)).view(K, blocks * 16)
+        s["w_scales"] = torch.zeros(K, -(-C // 512) * 16, dtype=torch.uint8, device="cuda")
+        s["w_scales"][:, :blocks] = torch.randint(117, 121, (K, blocks), generator=gen, device="cuda", dtype=torch.uint8)
+        s["bias"] = rand(K) if case["bias"] else None
+        s["y"] = new(N, K, dtype=DTYPE[case["dtype"]])
+    else:
+        sizes = _sizes(case)
+        records = [-(-n // 256) for n in sizes]
+        R = sum(records)
+        # every tensor begins on a whole record of one buffer of each kind; the places between two tensors hold zeros
+        index = torch.cat([torch.arange(r * 256, device="cuda") for r in records])
+        n_of = torch.repeat_interleave(torch.tensor(sizes, device="cuda"), torch.tensor([r * 256 for r in records], device="cuda"))
+        live = index < n_of
+        size = torch.exp2(torch.randint(-14, -7, (R, 1), generator=gen, device="cuda").float())
+        fresh = lambda: (rand(R, 256) * size).view(-1) * live  # noqa: E731
+        w = rand(R * 256) * 0.02 * live
+        g = fresh() * (torch.rand(R * 256, generator=gen, device="cuda") < 0.9)           # units that were off have no gradient
+        m, r = fresh() * 0.3, fresh().abs()
+        s["w"], s["g"] = w, g.to(DTYPE[case["grad"]])
+        s["wb"] = w.to(torch.bfloat16) if case["copy"] else None
+        if case["bits"] == 32:
+            s["m"], s["v"] = m, r * r
+        else:
+            s["state"] = torch.zeros(R, RECORD, dtype=torch.uint8, device="cuda")
+            half = torch.full((R, 256), 0.5, device="cuda")
+            for base, x in ((0, m), (256, r)):
+                codes, scales = _to8(x.view(R, 256), half, base == 256)
+                s["state"][:, base:base + 256], s["state"][:, 512 + base // 32:520 + base // 32] = codes, scales
+            s["index"] = (index & 0xFFFFFFFF).view(R, 256)
+            s["tensor"] = torch.repeat_interleave(torch.arange(len(sizes), device="cuda"), torch.tensor(records, device="cuda")).view(R, 1)
+        starts = [sum(records[:i]) for i in range(len(records))]
+        cut = lambda t: None if t is None else [t[a * 256:a * 256 + n] for a, n in zip(starts, sizes)]  # noqa: E731
+        s["lists"] = {k: cut(s.get(k)) for k in ("w", "g", "wb", "m", "v")}
+        if case["bits"] == 8:
+            s["lists"]["state"] = [s["state"][a:a + r].view(-1) for a, r in zip(starts, records)]
+        s["step"] = 1000
+    return s
+
+
+# ---- the operators ---------------------------------------------------------------------------------------------------------
+
+HYPER = {"lr": 3e-4, "beta1": 0.9, "beta2": 0.999, "eps": 1e-8, "wd": 0.1, "grad_scale": 0.5}
+
+
+def run(state):
+    kind = state["case"]["kind"]
+    if own:
+        return _own(state, kind)
+    return {"score": _plain_rows, "train": _plain_rows, "quant": _plain_quant, "product": _plain_product, "adamw": _plain_adamw}[kind](state)
+
+
+def _own(s, kind):
+    from paper_1512_01274_amd import mxc
+    c = s["case"]
+    if kind in ("score", "train"):
+        N, K, ld, dtype, top = c["N"], c["K"], c["K"] + c["pad"], CODE[c["dtype"]], c["top"]
+        if "workspace" not in s:
+            s["workspace"] = mxc.alloc_workspace(mxc.mxc_logprob_workspace_bytes(N, K, dtype, top))
+        if kind == "train":
+            mxc.mxc_logprob_fwd_bwd(N, K, ld, dtype, s["z"], s["labels"], s["scale"], s["dlogp"], s["dentropy"], s["logp"], s["entropy"], s["dz"],
+                                    s["workspace"])
+            return {"logp": s["logp"], "entropy": s["entropy"], "dz": s["dz"][:, :K]}
+        mxc.mxc_logprob_fwd(N, K, ld, dtype, s["z"], s["labels"], s["scale"], top, s["logp"], s["entropy"], s["stats"], s.get("top_logp"),
+                            s.get("top_index"), s["workspace"])
+        return {"logp": s["logp"], "entropy": s["entropy"], "top_logp": s.get("top_logp"), "top_index": s.get("top_index")}
+    if kind == "quant":
+        mxc.mxc_mxfp4_quantize(c["N"], c["C"], CODE[c["dtype"]], s["x"], s["codes"], s["scales"])
+        mxc.mxc_mxfp4_dequantize(c["N"], c["C"], mxc.MXC_BF16, s["codes"], s["scales"], s["y"])
+        return s["y"]
+    if kind == "product":
+        if "workspace" not in s:
+            s["workspace"] = mxc.alloc_workspace(mxc.mxc_mxfp4_fc_workspace_bytes(c["N"], c["C"], c["K"], CODE[c["dtype"]]))
+        mxc.mxc_mxfp4_fc_fwd(c["N"], c["C"], c["K"], CODE[c["dtype"]], s["x"], s["w_codes"], s["w_scales"], s["bias"], c["relu"], s["y"], s["workspace"])
+        return s["y"]
+    t, h = s["lists"], HYPER
+    s["step"] += 1
+    if c["bits"] == 32:
+        mxc.mxc_adamw_update(t["w"], t["g"], t["m"], t["v"], t["wb"], h["lr"], h["beta1"], h["beta2"], h["eps"], h["wd"], h["grad_scale"], s["step"])
+    else:
+        mxc.mxc_adamw8_update(t["w"], t["g"], t["state"], t["wb"], h["lr"], h["beta1"], h["beta2"], h["eps"], h["wd"], h["grad_scale"], s["step"],
+                              s["step"] * 7919)
+    return _updated(s)
+
+
+def _updated(s):
+    if s["case"]["bits"] == 32:
+        return {"w": s["w"], "wb": s["wb"], "m": s["m"], "v": s["v"]}
+    return {"w": s["w"], "wb": s["wb"], **_halves(s["state"])}
+
+
+def _halves(state):
+    return {"m8": state[:, :256].view(torch.float8_e4m3fn), "r8": state[:, 256:512].view(torch.float8_e4m3fn),
+            "m_scale": state[:, 512:520].view(torch.float8_e8m0fnu), "r_scale": state[:, 520:].view(torch.float8_e8m0fnu)}
+
+
+def _plain_rows(s):
+    """p = exp(scale (z - max)) / sum; an entry at minus infinity has no probability; a row of nothing else has log probabilities of minus
+    infinity, entropy 0 and gradient 0; a label outside the row gives 0 and has no gradient."""
+    c = s["case"]
+    K, dtype = c["K"], DTYPE[c["dtype"]]
+    z = s["z"][:, :K].float()
+    most = z.amax(1, keepdim=True)
+    empty = most == -math.inf
+    d = (z - most.masked_fill(empty, 0.0)) * s["scale"]
+    e = torch.exp(d)
+    total = e.sum(1, keepdim=True).masked_fill_(empty, 1.0)
+    logp = d - torch.log(total)
+    dead = logp == -math.inf
+    e.div_(total)
+    p_logp = (e * logp).masked_fill_(dead, 0.0)
+    entropy = -p_logp.sum(1, keepdim=True)
+    labels = s["labels"].long().unsqueeze(1)
+    given = (labels >= 0) & (labels < K)
+    at = labels.clamp(0, K - 1)
+    out = {"logp": torch.where(given, logp.gather(1, at), 0.0).squeeze(1), "entropy": entropy.squeeze(1)}
+    if c["kind"] == "train":
+        dl, dh = s["dlogp"].unsqueeze(1) * given, s["dentropy"].unsqueeze(1)
+        dz = p_logp.add_(e * entropy).mul_(-dh)
+        dz -= dl * e
+        dz.scatter_add_(1, at, torch.where(empty, 0.0, dl))
+        return {**out, "dz": dz.mul_(s["scale"]).to(dtype)}
+    if c["top"]:
+        bits = (z + 0.0).view(torch.int32)
+        rank = torch.where(bits < 0, bits ^ 0x7FFFFFFF, bits).long() * (1 << 32) + (0xFFFFFFFF - torch.arange(K, device="cuda"))
+        n = min(c["top"], K)
+        index = 0xFFFFFFFF - (torch.topk(rank, n, 1).values & 0xFFFFFFFF)
+        out["top_logp"] = torch.nn.functional.pad(logp.gather(1, index), (0, c["top"] - n), value=-math.inf)
+        out["top_index"] = torch.nn.functional.pad(index.int(), (0, c["top"] - n), value=-1)
+    return {k: out.get(k) for k in ("logp", "entropy", "top_logp", "top_index")}
+
+
+def _mx4(x):
+    """Values of x in 4 bits: in blocks of 32 of a row, scale 2^(floor(log2 of the block's largest) - 2), nearest of 0, .5, 1, 1.5, 2, 3, 4, 6
+    times that, ties to the even code, larger ones 6.  A block with an infinity or a NaN is NaN."""
+    N, C = x.shape
+    blocks = torch.nn.functional.pad(x.float(), (0, -C % 32)).view(N, -1, 32)
+    exponent = (torch.frexp(blocks.abs().amax(2, keepdim=True)).exponent - 3).clamp_(-127)
+    a = blocks * torch.exp2(-exponent.float())
+    quantum = torch.exp2((torch.frexp(a).exponent - 2).clamp_(-1).float())
+    a = torch.round(a / quantum).mul_(quantum).clamp_(-6.0, 6.0).mul_(torch.exp2(exponent.float()))
+    return a.masked_fill_(~blocks.isfinite().all(2, keepdim=True), math.nan).view(N, -1)[:, :C]
+
+
+E2M1 = [0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0, -0.0, -0.5, -1.0, -1.5, -2.0, -3.0, -4.0, -6.0]
+
+
+def _filter(s):
+    """The filter's numbers: value 2j of a row in the low half of byte j, 2j + 1 in the high half; scale bytes b stand for 2^(b - 127)."""
+    codes, C = s["w_codes"], s["case"]["C"]
+    table = torch.tensor(E2M1, device="cuda")
+    blocks = codes.shape[1] // 16
+    w = torch.stack([table[(codes & 15).int()], table[(codes >> 4).int()]], 2).view(codes.shape[0], blocks, 32)
+    return w.mul_(torch.exp2(s["w_scales"][:, :blocks].float() - 127.0).unsqueeze(2)).view(codes.shape[0], -1)[:, :C]
+
+
+def _plain_quant(s):
+    return _mx4(s["x"]).to(torch.bfloat16)
+
+
+def _plain_product(s):
+    y = _mx4(s["x"]) @ _filter(s).t()
+    if s["bias"] is not None:
+        y += s["bias"]
+    return (torch.relu(y) if s["case"]["relu"] else y).to(s["y"].dtype)
+
+
+def _from8(codes, scales):
+    return (codes.view(torch.float8_e4m3fn).float().view(-1, 8, 32) * torch.exp2(scales.float() - 127.0).unsqueeze(2)).view(-1, 256)
+
+
+def _to8(x, u, root):
+    """Codes of x (4 bits of exponent, 3 of mantissa, largest 448) and its scales, one power of two for each 32 values: the smallest that
+    keeps the largest value at 448 or less.  u in [0, 1) decides between a value's two neighbours, so that the code's mean is the value.
+    root: a value that is not 0 does not become 0."""
+    x = x.reshape(-1, 8, 32)
+    f = torch.frexp(x.abs().amax(2, keepdim=True))
+    exponent = (f.exponent - 9 + (f.mantissa > 0.875)).clamp_(-127)
+    y = x.abs() * torch.exp2(-exponent.float())
+    E = (torch.frexp(y).exponent + 6).clamp_(1)
+    k = torch.floor(y * torch.exp2(10.0 - E) + u.view(-1, 8, 32)).int() + (E - 1) * 8
+    if root:
+        k = torch.where((k == 0) & (x > 0), 1, k)
+    return torch.where(x < 0, k | 128, k).to(torch.uint8).view(-1, 256), (exponent + 127).squeeze(2).to(torch.uint8)
+
+
+def _mix(x):
+    """32 bits of x, well mixed."""
+    x = x & 0xFFFFFFFF
+    x = ((x ^ (x >> 16)) * 0xBC0614A5) & 0xFFFFFFFF
+    x = ((x ^ (x >> 15)) * 0xB0D9ED3D) & 0xFFFFFFFF
+    return x ^ (x >> 16)
+
+
+def _plain_adamw(s):
+    c, h = s["case"], HYPER
+    s["step"] += 1
+    t = s["step"]
+    c1, c2 = 1.0 - h["beta1"] ** t, 1.0 - h["beta2"] ** t
+    g = s["g"].float() * h["grad_scale"]
+    if c["bits"] == 32:
+        m, v = s["m"], s["v"]
+    else:
+        g, st = g.view(-1, 256), s["state"]
+        m, r = _from8(st[:, :256], st[:, 512:520]), _from8(st[:, 256:512], st[:, 520:])
+        v = r * r
+    m = m * h["beta1"] + g * (1.0 - h["beta1"])
+    v = v * h["beta2"] + g * g * (1.0 - h["beta2"])
+    r = torch.sqrt(v)
+    move = m / (r * (1.0 / math.sqrt(c2)) + h["eps"]) * (h["lr"] / c1)
+    s["w"].mul_(1.0 - h["lr"] * h["wd"]).sub_(move.view(-1))
+    if s["wb"] is not None:
+        s["wb"].copy_(s["w"])
+    if c["bits"] == 32:
+        s["m"].copy_(m)
+        s["v"].copy_(v)
+    else:
+        # a random number for each value of each tensor and call: its index, the tensor's number and the call's seed, mixed
+        key = _mix(t * 7919 + (s["tensor"] + 1) * 0x9E3779B9)
+        bits = _mix(s["index"] * 0x9E3779B9 + key)
+        for base, x, u in ((0, m, bits & 0xFFFF), (256, r, bits >> 16)):
+            codes, scales = _to8(x, u.float() * 2.0 ** -16, base == 256)
+            st[:, base:base + 256], st[:, 512 + base // 32:520 + base // 32] = codes, scales
+    return _updated(s)
+
+
+# ---- what a pass cannot do without --------------------------------------------------------------------------------------------
+
+def work(case):
+    kind = case["kind"]
+    if kind in ("score", "train"):
+        N, K, size = case["N"], case["K"], SIZE[case["dtype"]]
+        values = N * K
+        if kind == "train":
+            return {"bytes": 2 * values * size + N * 28, "flops": 12 * values}
+        return {"bytes": values * size + N * (20 + 8 * case["top"]), "flops": 5 * values}
+    if kind == "quant":
+        N, C = case["N"], case["C"]
+        return {"bytes": N * (C * (SIZE[case["dtype"]] + 2) + -(-C // 32) * 17), "flops": 4 * N * C}
+    if kind == "product":
+        N, C, K, size = case["N"], case["C"], case["K"], SIZE[case["dtype"]]
+        return {"bytes": (N * C + N * K) * size + K * -(-C // 32) * 17 + (4 * K if case["bias"] else 0), "flops": 2 * N * C * K}
+    values = sum(_sizes(case))
+    state = 16 if case["bits"] == 32 else 4 * (1 + 1 / 32)
+    return {"bytes": values * (8 + SIZE[case["grad"]] + state + (2 if case["copy"] else 0)), "flops": 15 * values}
+
+
+# ---- the definitions in 64 bits ------------------------------------------------------------------------------------------------
+
+def _exact_rows(s):
+    c = s["case"]
+    z = s["z"][:, :c["K"]].double().mul_(s["scale"])
+    empty = (z == -math.inf).all(1)
+    z[empty] = 0.0
+    logp = z.log_softmax(1)
+    del z
+    p = logp.exp()
+    h = -(torch.special.xlogy(p, p).sum(1))
+    h[empty] = 0.0
+    labels = s["labels"].long()
+    given = (labels >= 0) & (labels < c["K"])
+    rows = torch.arange(c["N"], device="cuda")
+    own_logp = logp[rows, labels.clamp(0, c["K"] - 1)]
+    own_logp[empty] = -math.inf
+    own_logp[~given] = 0.0
+    out = {"logp": own_logp, "entropy": h}
+    if c["kind"] == "train":
+        dz = (torch.special.xlogy(p, p) + p * h[:, None]) * -s["dentropy"].double()[:, None]
+        dl = s["dlogp"].double() * given
+        dz -= p * dl[:, None]
+        dz[rows, labels.clamp(0, c["K"] - 1)] += dl
+        dz[empty] = 0.0
+        return {**out, "dz": dz.mul_(s["scale"])}
+    top = None
+    if c["top"]:
+        logp[empty] = -math.inf
+        n = min(c["top"], c["K"])
+        top = torch.full((c["N"], c["top"]), -math.inf, device="cuda", dtype=torch.float64)
+        top[:, :n] = logp.sort(1, descending=True).values[:, :n]
+    return {**out, "top_logp": top, "top_index": None}
+
+
+def _exact_mx4(x):
+    N, C = x.shape
+    b = torch.zeros(N, -(-C // 32) * 32, dtype=torch.float64, device="cuda")
+    b[:, :C] = x
+    b = b.view(N, -1, 32)
+    scale = torch.exp2(torch.floor(torch.log2(b.abs().amax(2, keepdim=True))).sub_(2.0).clamp_(-127.0))
+    a = b.abs() / scale
+    q = torch.zeros_like(a)
+    # half way between two numbers the one with the even code is taken
+    for step, above, with_it in ((0.5, 0.25, False), (0.5, 0.75, True), (0.5, 1.25, False), (0.5, 1.75, True), (1.0, 2.5, False), (1.0, 3.5, True), (2.0, 5.0, False)):
+        q += step * ((a >= above) if with_it else (a > above))
+    return (q * scale * torch.sign(b)).view(N, -1)[:, :C]
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    kind = case["kind"]
+    if kind in ("score", "train"):
+        return _exact_rows(s)
+    if kind == "quant":
+        return _exact_mx4(s["x"])
+    if kind == "product":
+        C, codes = case["C"], s["w_codes"].long()
+        nibbles = torch.stack([codes % 16, codes // 16], 2).flatten(1)[:, :C]
+        size, odd = nibbles % 8 // 2, nibbles % 2
+        w = torch.where(size == 0, odd * 0.5, (1.0 + 0.5 * odd) * torch.exp2(size.double() - 1.0)) * (1 - 2 * (nibbles // 8))
+        w = w * torch.exp2(s["w_scales"].double() - 127.0).repeat_interleave(32, 1)[:, :C]
+        y = _exact_mx4(s["x"]) @ w.t().contiguous()
+        if s["bias"] is not None:
+            y += s["bias"].double()
+        return y.clamp_(0.0) if case["relu"] else y
+    h, t = HYPER, s["step"] + 1
+    g = s["g"].double() * h["grad_scale"]
+    if case["bits"] == 32:
+        m, v = s["m"].double(), s["v"].double()
+    else:
+        parts = {k: x.double() for k, x in _halves(s["state"]).items()}
+        m, r = ((parts[a].view(-1, 32) * parts[b].reshape(-1, 1)).view(-1) for a, b in (("m8", "m_scale"), ("r8", "r_scale")))
+        v = r * r
+    m = h["beta1"] * m + (1 - h["beta1"]) * g
+    v = h["beta2"] * v + (1 - h["beta2"]) * g * g
+    w = s["w"].double()
+    w = w - h["lr"] * (h["wd"] * w + m / (1 - h["beta1"] ** t) / (torch.sqrt(v / (1 - h["beta2"] ** t)) + h["eps"]))
+    out = {"w": w, "wb": w if case["copy"] else None}
+    if case["bits"] == 32:
+        return {**out, "m": m, "v": v}
+    return {**out, "m8": None, "r8": None, "m_scale": None, "r_scale": None}        # codes are choices between two neighbours, not numbers computed
