@@ -337,7 +337,7 @@ def _to8(x, u, root):
     f = torch.frexp(x.abs().amax(2, keepdim=True))
     exponent = (f.exponent - 9 + (f.mantissa > 0.875)).clamp_(-127)
     y = x.abs() * torch.exp2(-exponent.float())
-    E = (torch.frexp(y).exponent + 6).clamp_(1)
+    E = torch.where(y > 0, torch.frexp(y).exponent + 6, 1).clamp_(1)
     k = torch.floor(y * torch.exp2(10.0 - E) + u.view(-1, 8, 32)).int() + (E - 1) * 8
     if root:
         k = torch.where((k == 0) & (x > 0), 1, k)
