@@ -334,8 +334,9 @@ def _to8(x, u, root):
     keeps the largest value at 448 or less.  u in [0, 1) decides between a value's two neighbours, so that the code's mean is the value.
     root: a value that is not 0 does not become 0."""
     x = x.reshape(-1, 8, 32)
-    f = torch.frexp(x.abs().amax(2, keepdim=True))
-    exponent = (f.exponent - 9 + (f.mantissa > 0.875)).clamp_(-127)
+    largest = x.abs().amax(2, keepdim=True)
+    f = torch.frexp(largest)
+    exponent = torch.where(largest > 0, f.exponent - 9 + (f.mantissa > 0.875), -127).clamp_(-127)
     y = x.abs() * torch.exp2(-exponent.float())
     E = torch.where(y > 0, torch.frexp(y).exponent + 6, 1).clamp_(1)
     k = torch.floor(y * torch.exp2(10.0 - E) + u.view(-1, 8, 32)).int() + (E - 1) * 8
