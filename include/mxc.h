@@ -307,6 +307,95 @@ int mxc_sgd_update(size_t n, float *w, const float *g, float *v, void *w_bf16,
                    float lr, float momentum, float wd, void *hip_stream);
 
 /*
+ * Log probabilities of given tokens (or classes) under softmax(scale * z), with the entropy of every row, its most
+ * probable tokens, and the gradient of a weighted sum of the log probabilities and entropies.  z: [N] rows of K
+ * logits of `dtype`, `ld` elements from one row to the next (ld >= K; the ld - K between two rows are neither read
+ * nor written).  With d[k] = scale*(z[n,k] - max_j z[n,j]), S = sum_k exp(d[k]), T = sum_k exp(d[k])*d[k], p = exp(d)/S:
+ *   logp[n]    = d[labels[n]] - log S          entropy[n] = -sum_k p[k]*log p[k] = log S - T/S
+ *   stats[n]   = (max_j z[n,j], log S): two numbers from which any log p[k] = scale*(z[n,k] - stats[0]) - stats[1]
+ *   top_logp[n,i], top_index[n,i], i < top: log probability and index of the i-th most probable token; of equal ones the
+ *                lowest index first; past the K-th token minus infinity and index -1
+ *   dz[n,k]    = scale*( dlogp[n]*((k == labels[n]) - p[k]) - dentropy[n]*p[k]*(log p[k] + entropy[n]) )
+ * labels: device int32; a label outside [0, K) has logp 0 and no gradient of logp.  A logit of minus infinity has
+ * probability 0; a row of nothing else has log probabilities of minus infinity, entropy 0, stats (-inf, 0) and a zero
+ * gradient.  A row that holds a NaN or plus infinity has NaN results.  Arithmetic, logp, entropy, stats and
+ * top_logp are fp32; dz is rounded once to `dtype` and has z's ld.
+ *   mxc_logprob_fwd      any of logp (and with it labels), entropy, stats may be NULL; top in 0..MXC_LOGPROB_MAX_TOP,
+ *                        with top == 0 top_logp and top_index may be NULL
+ *   mxc_logprob_bwd      the gradient from stats and entropy of mxc_logprob_fwd; dlogp or dentropy may be NULL (zeros);
+ *                        labels may be NULL without dlogp, entropy without dentropy
+ *   mxc_logprob_fwd_bwd  both at once, which reads z once: logp or entropy may be NULL
+ * dz may be z itself.  scale must be positive and finite.  Workspace: mxc_logprob_workspace_bytes (top 0 for
+ * mxc_logprob_fwd_bwd, none for mxc_logprob_bwd).  Results are bit-identical from run to run.  Errors: MXC_ERR_SHAPE (non-positive N
+ * or K, ld < K, top out of range), MXC_ERR_UNSUPPORTED (dtype, scale), MXC_ERR_NULL, MXC_ERR_ALIGN (16 bytes for z and dz,
+ * 4 for the others), MXC_ERR_WORKSPACE, MXC_ERR_LAUNCH.
+ */
+enum { MXC_LOGPROB_MAX_TOP = 64 };
+int mxc_logprob_workspace_bytes(int N, int K, int dtype, int top, size_t *out_bytes);
+int mxc_logprob_fwd(int N, int K, int ld, int dtype, const void *z, const int *labels, float scale, int top,
+                    float *logp, float *entropy, float *stats, float *top_logp, int *top_index,
+                    void *workspace, size_t workspace_bytes, void *hip_stream);
+int mxc_logprob_bwd(int N, int K, int ld, int dtype, const void *z, const int *labels, float scale, const float *stats,
+                    const float *entropy, const float *dlogp, const float *dentropy, void *dz, void *hip_stream);
+int mxc_logprob_fwd_bwd(int N, int K, int ld, int dtype, const void *z, const int *labels, float scale,
+                        const float *dlogp, const float *dentropy, float *logp, float *entropy, void *dz,
+                        void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Microscaled 4-bit floating point (the MXFP4 format of the OCP Microscaling Formats specification 1.0).  A row of C values is cut
+ * into blocks of 32; a block has one scale 2^(b - 127), b a byte, and a value is sign * {0, .5, 1, 1.5, 2, 3, 4, 6} times
+ * that.  For N rows of C values:
+ *   codes:  [N][ceil(C/32)*16] bytes; value 2j of a row is the low half of byte j, value 2j+1 the high half; the places past
+ *           column C hold 0
+ *   scales: [N][ceil(C/512)*16] bytes, one for each block; the bytes past the last block hold 0
+ *   mxc_mxfp4_quantize    b = floor(log2(largest |x| of the block)) - 2 + 127, at least 0; values are rounded to the nearest
+ *       representable one, ties to the even code, larger ones than 6 to 6.  A block that holds an infinity or a NaN has b = 255
+ *       and codes 0: all of it reads as NaN.
+ *   mxc_mxfp4_dequantize  the numbers the codes stand for, rounded once to `dtype`
+ * x, y: [N][C] of `dtype`, dense.  No workspace.  Errors: MXC_ERR_SHAPE, MXC_ERR_UNSUPPORTED (dtype), MXC_ERR_NULL, MXC_ERR_ALIGN
+ * (16 bytes), MXC_ERR_LAUNCH.
+ *
+ * FullyConnected on a filter in this form: y[n,k] = act( sum_c q(x)[n,c] * w[k,c] + bias[k] ), x: [N][C] and y: [N][K]
+ * of `dtype`, w_codes and w_scales as above for K rows of C values, q(x) the values of mxc_mxfp4_quantize (the
+ * input is brought into 4 bits within the call), products exact, sums in fp32 (their order depends on the sizes alone), one rounding to `dtype`.  bias
+ * (fp32) may be NULL, relu is 0 or 1 (a NaN stays).  A NaN in q(x) or w makes NaN of the results of its row or column.  Places of w_codes past column C must hold 0
+ * (their scales are read as they are: no infinity arises from them).  Workspace: mxc_mxfp4_fc_workspace_bytes.  Errors as above, and MXC_ERR_WORKSPACE.
+ */
+int mxc_mxfp4_quantize(int N, int C, int dtype, const void *x, void *codes, void *scales, void *hip_stream);
+int mxc_mxfp4_dequantize(int N, int C, int dtype, const void *codes, const void *scales, void *y, void *hip_stream);
+int mxc_mxfp4_fc_workspace_bytes(int N, int C, int K, int dtype, size_t *out_bytes);
+int mxc_mxfp4_fc_fwd(int N, int C, int K, int dtype, const void *x, const void *w_codes, const void *w_scales,
+                     const float *bias, int relu, void *y, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * AdamW step over many tensors in one call (a launch for every MXC_ADAMW_GROUP tensors).  For each value, with
+ * gs = grad_scale*g and t = step (1 for the first):
+ *   m' = beta1*m + (1 - beta1)*gs,   v' = beta2*v + (1 - beta2)*gs*gs
+ *   w' = w*(1 - lr*wd) - lr/(1 - beta1^t) * m' / ( sqrt(v')/sqrt(1 - beta2^t) + eps )
+ * count tensors; sizes, w, g, m, v, w_bf16, state: HOST arrays of `count` element counts and device pointers (read before the
+ * call returns).  w: fp32 master weights, in place; g: gradients of grad_dtype (MXC_F32 or MXC_BF16); m, v: fp32, in place;
+ * w_bf16: NULL, or for each tensor where w' goes rounded to bf16.  A tensor of size 0 is passed over, whatever its pointers.
+ * The factors are computed from the double arguments in 64 bits and used in 32.
+ * mxc_adamw8_update keeps m and r = sqrt(v) in 8 bits: state: mxc_adamw8_state_bytes(n) bytes a tensor, zeros at the start.
+ * 256 values have 528 bytes: 256 codes of m, 256 of r (each sign, 4 bits of exponent, 3 of mantissa, largest 448: e4m3), 8 scales of
+ * m, 8 of r (bytes b for 2^(b - 127), one for every 32 values: the smallest with which the block's largest value is 448 or less;
+ * 0 for a block of zeros).  A value goes to one of its two neighbours at random, so that its mean is the value: up where its place
+ * between them plus u >= 1, u a multiple of 2^-16 taken from a hash of the value's index, the tensor's number and `seed` (16 bits of it for m, 16 for r; the
+ * same call gives the same codes).  An r that is not 0 does not become code 0: a weight's step never divides by eps alone
+ * because of a rounding.  A block of m or r that holds an infinity or a NaN gets scale 255 and reads as NaN.
+ * Errors, found before anything is launched: MXC_ERR_SHAPE (count <= 0, step < 1, a tensor of more than 2^34 values), MXC_ERR_UNSUPPORTED (grad_dtype;
+ * beta1 or beta2 outside [0, 1); negative eps; a factor that is not finite), MXC_ERR_NULL, MXC_ERR_ALIGN (16 bytes), MXC_ERR_LAUNCH.
+ */
+enum { MXC_ADAMW_GROUP = 72 };
+int mxc_adamw_update(int count, const size_t *sizes, void *const *w, const void *const *g, int grad_dtype, void *const *m,
+                     void *const *v, void *const *w_bf16, double lr, double beta1, double beta2, double eps, double wd,
+                     double grad_scale, long long step, void *hip_stream);
+int mxc_adamw8_state_bytes(size_t n, size_t *out_bytes);
+int mxc_adamw8_update(int count, const size_t *sizes, void *const *w, const void *const *g, int grad_dtype, void *const *state,
+                      void *const *w_bf16, double lr, double beta1, double beta2, double eps, double wd,
+                      double grad_scale, long long step, unsigned seed, void *hip_stream);
+
+/*
  * Workspace size in bytes that `pass` (MXC_FWD / MXC_BWD_DATA / MXC_BWD_WEIGHT)
  * needs for these arguments, written to *out_bytes (a HOST pointer).  Touches
  * no GPU state.

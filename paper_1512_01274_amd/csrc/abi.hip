@@ -2,6 +2,7 @@
 // and kernel selection.  See include/mxc.h for the contract of every call.
 #include <string.h>
 
+#include <cmath>
 #include <mutex>
 #include <string>
 
@@ -64,6 +65,7 @@ int validate_shape(int N, int C, int H, int W, int K, int R, int S, int stride, 
 }
 
 bool misaligned(const void *p) { return ((uintptr_t)p & 15u) != 0; }
+bool misaligned4(const void *p) { return ((uintptr_t)p & 3u) != 0; }
 
 #define MXC_TRY(expr)                 \
     do {                              \
@@ -1022,6 +1024,170 @@ int mxc_sgd_update(size_t n, float *w, const float *g, float *v, void *w_bf16, f
     if (!v && momentum != 0.f) return MXC_ERR_NULL;
     if (misaligned(w) || misaligned(g) || misaligned(v) || misaligned(w_bf16)) return MXC_ERR_ALIGN;
     return sgd_update(n, w, g, v, w_bf16, lr, momentum, wd, (hipStream_t)hip_stream);
+}
+
+static int logprob_check(int N, int K, int ld, int dtype, const void *z, float scale)
+{
+    if (N <= 0 || K <= 0 || ld < K) return MXC_ERR_SHAPE;
+    if (dtype != MXC_F32 && dtype != MXC_BF16) return MXC_ERR_UNSUPPORTED;
+    if (!(scale > 0.f) || !std::isfinite(scale)) return MXC_ERR_UNSUPPORTED;
+    return z ? MXC_OK : MXC_ERR_NULL;
+}
+
+int mxc_logprob_workspace_bytes(int N, int K, int dtype, int top, size_t *out_bytes)
+{
+    if (!out_bytes) return MXC_ERR_NULL;
+    if (N <= 0 || K <= 0 || top < 0 || top > MXC_LOGPROB_MAX_TOP) return MXC_ERR_SHAPE;
+    if (dtype != MXC_F32 && dtype != MXC_BF16) return MXC_ERR_UNSUPPORTED;
+    *out_bytes = align_up(logprob_workspace(N, K, dtype, top), 256);
+    return MXC_OK;
+}
+
+int mxc_logprob_fwd(int N, int K, int ld, int dtype, const void *z, const int *labels, float scale, int top,
+                    float *logp, float *entropy, float *stats, float *top_logp, int *top_index,
+                    void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    if (top < 0 || top > MXC_LOGPROB_MAX_TOP) return MXC_ERR_SHAPE;
+    MXC_TRY(logprob_check(N, K, ld, dtype, z, scale));
+    if ((logp && !labels) || (top && (!top_logp || !top_index))) return MXC_ERR_NULL;
+    if (misaligned(z) || misaligned(workspace) || misaligned4(labels) || misaligned4(logp) || misaligned4(entropy) || misaligned4(stats) ||
+        misaligned4(top_logp) || misaligned4(top_index))
+        return MXC_ERR_ALIGN;
+    const size_t need = logprob_workspace(N, K, dtype, top);
+    if (need && (!workspace || workspace_bytes < need)) return MXC_ERR_WORKSPACE;
+    LogprobArgs a = {N, K, ld, dtype, top, z, labels, scale, nullptr, nullptr, logp, entropy, stats, top_logp, top_index, nullptr};
+    return logprob_rows(a, workspace, (hipStream_t)hip_stream);
+}
+
+int mxc_logprob_bwd(int N, int K, int ld, int dtype, const void *z, const int *labels, float scale, const float *stats,
+                    const float *entropy, const float *dlogp, const float *dentropy, void *dz, void *hip_stream)
+{
+    MXC_TRY(logprob_check(N, K, ld, dtype, z, scale));
+    if (!dz || !stats || (dlogp && !labels) || (dentropy && !entropy)) return MXC_ERR_NULL;
+    if (misaligned(z) || misaligned(dz) || misaligned4(labels) || misaligned4(stats) || misaligned4(entropy) || misaligned4(dlogp) ||
+        misaligned4(dentropy))
+        return MXC_ERR_ALIGN;
+    LogprobArgs a = {N, K, ld, dtype, 0, z, labels, scale, dlogp, dentropy, nullptr, nullptr, nullptr, nullptr, nullptr, dz};
+    return logprob_bwd(a, stats, entropy, (hipStream_t)hip_stream);
+}
+
+int mxc_logprob_fwd_bwd(int N, int K, int ld, int dtype, const void *z, const int *labels, float scale,
+                        const float *dlogp, const float *dentropy, float *logp, float *entropy, void *dz,
+                        void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    MXC_TRY(logprob_check(N, K, ld, dtype, z, scale));
+    if (!dz || ((dlogp || logp) && !labels)) return MXC_ERR_NULL;
+    if (misaligned(z) || misaligned(dz) || misaligned(workspace) || misaligned4(labels) || misaligned4(dlogp) || misaligned4(dentropy) ||
+        misaligned4(logp) || misaligned4(entropy))
+        return MXC_ERR_ALIGN;
+    const size_t need = logprob_workspace(N, K, dtype, 0);
+    if (need && (!workspace || workspace_bytes < need)) return MXC_ERR_WORKSPACE;
+    LogprobArgs a = {N, K, ld, dtype, 0, z, labels, scale, dlogp, dentropy, logp, entropy, nullptr, nullptr, nullptr, dz};
+    return logprob_rows(a, workspace, (hipStream_t)hip_stream);
+}
+
+// (N, C, K) of the 4-bit calls: every tensor under 2^40 bytes
+static int mxfp4_check(int N, int C, int K, int dtype)
+{
+    if (N <= 0 || C <= 0 || K <= 0) return MXC_ERR_SHAPE;
+    if ((long double)N * C >= 2.7e11L || (long double)N * K >= 2.7e11L || (long double)K * C >= 2.7e11L) return MXC_ERR_SHAPE;
+    return dtype == MXC_F32 || dtype == MXC_BF16 ? MXC_OK : MXC_ERR_UNSUPPORTED;
+}
+
+int mxc_mxfp4_quantize(int N, int C, int dtype, const void *x, void *codes, void *scales, void *hip_stream)
+{
+    MXC_TRY(mxfp4_check(N, C, 1, dtype));
+    if (!x || !codes || !scales) return MXC_ERR_NULL;
+    if (misaligned(x) || misaligned(codes) || misaligned(scales)) return MXC_ERR_ALIGN;
+    return mxfp4_quantize(N, C, dtype, x, codes, scales, (hipStream_t)hip_stream);
+}
+
+int mxc_mxfp4_dequantize(int N, int C, int dtype, const void *codes, const void *scales, void *y, void *hip_stream)
+{
+    MXC_TRY(mxfp4_check(N, C, 1, dtype));
+    if (!y || !codes || !scales) return MXC_ERR_NULL;
+    if (misaligned(y) || misaligned(codes) || misaligned(scales)) return MXC_ERR_ALIGN;
+    return mxfp4_dequantize(N, C, dtype, codes, scales, y, (hipStream_t)hip_stream);
+}
+
+int mxc_mxfp4_fc_workspace_bytes(int N, int C, int K, int dtype, size_t *out_bytes)
+{
+    if (!out_bytes) return MXC_ERR_NULL;
+    MXC_TRY(mxfp4_check(N, C, K, dtype));
+    *out_bytes = align_up(mxfp4_fc_workspace(N, C, K, dtype), 256);
+    return MXC_OK;
+}
+
+int mxc_mxfp4_fc_fwd(int N, int C, int K, int dtype, const void *x, const void *w_codes, const void *w_scales,
+                     const float *bias, int relu, void *y, void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    MXC_TRY(mxfp4_check(N, C, K, dtype));
+    if (relu != 0 && relu != 1) return MXC_ERR_UNSUPPORTED;
+    if (!x || !w_codes || !w_scales || !y) return MXC_ERR_NULL;
+    if (misaligned(x) || misaligned(w_codes) || misaligned(w_scales) || misaligned(y) || misaligned(workspace) || misaligned4(bias)) return MXC_ERR_ALIGN;
+    const size_t need = mxfp4_fc_workspace(N, C, K, dtype);
+    if (need && (!workspace || workspace_bytes < need)) return MXC_ERR_WORKSPACE;
+    return mxfp4_fc(N, C, K, dtype, x, w_codes, w_scales, bias, relu, y, workspace, (hipStream_t)hip_stream);
+}
+
+// the checks and the factors that both AdamW calls share; tensors: the arrays that may hold no null pointer (w, g, ...)
+static int adamw_check(int count, const size_t *sizes, const void *const *const *tensors, int kinds, void *const *w_bf16, int grad_dtype, double lr,
+                       double beta1, double beta2, double eps, double wd, double grad_scale, long long step, AdamwFactors *f)
+{
+    if (count <= 0 || step < 1) return MXC_ERR_SHAPE;
+    if (grad_dtype != MXC_F32 && grad_dtype != MXC_BF16) return MXC_ERR_UNSUPPORTED;
+    if (!(beta1 >= 0.0 && beta1 < 1.0 && beta2 >= 0.0 && beta2 < 1.0 && eps >= 0.0)) return MXC_ERR_UNSUPPORTED;
+    const double c1 = 1.0 - std::pow(beta1, (double)step), c2 = 1.0 - std::pow(beta2, (double)step);
+    *f = AdamwFactors{(float)beta1, (float)(1.0 - beta1), (float)beta2, (float)(1.0 - beta2), (float)(1.0 / std::sqrt(c2)), (float)eps, (float)(lr / c1),
+                      (float)(1.0 - lr * wd), (float)grad_scale};
+    if (!std::isfinite(f->root_scale) || !std::isfinite(f->eps) || !std::isfinite(f->rate) || !std::isfinite(f->keep) || !std::isfinite(f->grad_scale))
+        return MXC_ERR_UNSUPPORTED;
+    if (!sizes) return MXC_ERR_NULL;
+    for (int k = 0; k < kinds; ++k)
+        if (!tensors[k]) return MXC_ERR_NULL;
+    for (int i = 0; i < count; ++i)
+        if (sizes[i] > (size_t)1 << 34) return MXC_ERR_SHAPE;        // (a group's workgroups are counted in 31 bits)
+    for (int i = 0; i < count; ++i) {
+        if (sizes[i] == 0) continue;
+        for (int k = 0; k < kinds; ++k)
+            if (!tensors[k][i]) return MXC_ERR_NULL;
+        if (w_bf16 && !w_bf16[i]) return MXC_ERR_NULL;
+    }
+    for (int i = 0; i < count; ++i) {
+        if (sizes[i] == 0) continue;
+        for (int k = 0; k < kinds; ++k)
+            if (misaligned(tensors[k][i])) return MXC_ERR_ALIGN;
+        if (w_bf16 && misaligned(w_bf16[i])) return MXC_ERR_ALIGN;
+    }
+    return MXC_OK;
+}
+
+int mxc_adamw_update(int count, const size_t *sizes, void *const *w, const void *const *g, int grad_dtype, void *const *m,
+                     void *const *v, void *const *w_bf16, double lr, double beta1, double beta2, double eps, double wd,
+                     double grad_scale, long long step, void *hip_stream)
+{
+    AdamwFactors f;
+    const void *const *const tensors[] = {w, g, m, v};
+    MXC_TRY(adamw_check(count, sizes, tensors, 4, w_bf16, grad_dtype, lr, beta1, beta2, eps, wd, grad_scale, step, &f));
+    return adamw_update(count, sizes, w, g, grad_dtype, m, v, w_bf16, f, 0, (hipStream_t)hip_stream);
+}
+
+int mxc_adamw8_state_bytes(size_t n, size_t *out_bytes)
+{
+    if (!out_bytes) return MXC_ERR_NULL;
+    if (n > (size_t)1 << 34) return MXC_ERR_SHAPE;
+    *out_bytes = (n + 255) / 256 * ADAMW8_RECORD;
+    return MXC_OK;
+}
+
+int mxc_adamw8_update(int count, const size_t *sizes, void *const *w, const void *const *g, int grad_dtype, void *const *state,
+                      void *const *w_bf16, double lr, double beta1, double beta2, double eps, double wd,
+                      double grad_scale, long long step, unsigned seed, void *hip_stream)
+{
+    AdamwFactors f;
+    const void *const *const tensors[] = {w, g, state};
+    MXC_TRY(adamw_check(count, sizes, tensors, 3, w_bf16, grad_dtype, lr, beta1, beta2, eps, wd, grad_scale, step, &f));
+    return adamw_update(count, sizes, w, g, grad_dtype, state, nullptr, w_bf16, f, seed, (hipStream_t)hip_stream);
 }
 
 int mxc_conv2d_workspace_bytes(int pass, int N, int C, int H, int W, int K, int R, int S, int stride, int pad,

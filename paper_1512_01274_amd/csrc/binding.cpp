@@ -7,6 +7,8 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <vector>
+
 #include "../../include/mxc.h"
 
 namespace {
@@ -81,6 +83,48 @@ bool to_ptr(PyObject *o, void **ptr, size_t *bytes = nullptr)
     }
     *ptr = t.data_ptr();
     if (bytes) *bytes = t.nbytes();
+    return true;
+}
+
+// device pointers of a list (or tuple) of contiguous GPU tensors of one element type; None: an empty vector.  numel: filled by the
+// first list (`first`), and what the others' tensors have to have.  type: the one that they must have, Undefined: that of the first tensor.
+bool to_ptrs(PyObject *o, const char *name, std::vector<void *> *ptrs, std::vector<size_t> *numel, bool first, at::ScalarType *type)
+{
+    ptrs->clear();
+    if (o == nullptr || o == Py_None) return true;
+    if (!PyList_Check(o) && !PyTuple_Check(o)) {
+        PyErr_Format(PyExc_TypeError, "%s: expected a list of tensors, got %s", name, Py_TYPE(o)->tp_name);
+        return false;
+    }
+    const Py_ssize_t n = PySequence_Fast_GET_SIZE(o);
+    if (!first && (size_t)n != numel->size()) {
+        PyErr_Format(PyExc_ValueError, "%s: %zd tensors for %zu weights", name, n, numel->size());
+        return false;
+    }
+    ptrs->reserve((size_t)n);
+    for (Py_ssize_t i = 0; i < n; ++i) {
+        PyObject *item = PySequence_Fast_GET_ITEM(o, i);
+        if (!THPVariable_Check(item)) {
+            PyErr_Format(PyExc_TypeError, "%s[%zd]: expected a torch tensor, got %s", name, i, Py_TYPE(item)->tp_name);
+            return false;
+        }
+        const at::Tensor &t = THPVariable_Unpack(item);
+        if (!t.is_cuda() || !t.is_contiguous()) {
+            PyErr_SetString(PyExc_ValueError, "tensors must be contiguous GPU tensors");
+            return false;
+        }
+        if (*type == at::ScalarType::Undefined) *type = t.scalar_type();
+        if (t.scalar_type() != *type) {
+            PyErr_Format(PyExc_TypeError, "%s[%zd]: expected %s, got %s", name, i, at::toString(*type), at::toString(t.scalar_type()));
+            return false;
+        }
+        if (first) numel->push_back((size_t)t.numel());
+        else if ((size_t)t.numel() != (*numel)[(size_t)i]) {
+            PyErr_Format(PyExc_ValueError, "%s[%zd]: %lld elements, expected %zu", name, i, (long long)t.numel(), (*numel)[(size_t)i]);
+            return false;
+        }
+        ptrs->push_back(t.data_ptr());
+    }
     return true;
 }
 
@@ -212,6 +256,50 @@ WRAP(mxc_sgd_update, 7, N_("w", "g", "v", "w_bf16", "lr", "momentum", "wd", "str
      // the element count is w's, whatever its type
      const size_t count = a.v[0] == Py_None ? 0 : (size_t)THPVariable_Unpack(a.v[0]).numel();
      RUN(mxc_sgd_update(count, (float *)w, (const float *)g, (float *)v, wb, (float)lr, (float)mom, (float)wd, st));)
+WRAP(mxc_logprob_fwd, 13, N_("N", "K", "ld", "dtype", "z", "labels", "scale", "top", "logp", "entropy", "stats", "top_logp", "top_index", "workspace", "stream"),
+     INTS(4); PTR(z, 4); PTR(labels, 5); FLOAT(scale, 6); INT(top, 7); PTR(logp, 8); PTR(entropy, 9); PTR(stats, 10); PTR(tl, 11); PTR(ti, 12); BUF(ws, 13);
+     STREAM(14);
+     RUN(mxc_logprob_fwd(d[0], d[1], d[2], d[3], z, (const int *)labels, (float)scale, top, (float *)logp, (float *)entropy, (float *)stats, (float *)tl,
+                         (int *)ti, ws, ws_n, st));)
+WRAP(mxc_logprob_bwd, 12, N_("N", "K", "ld", "dtype", "z", "labels", "scale", "stats", "entropy", "dlogp", "dentropy", "dz", "stream"),
+     INTS(4); PTR(z, 4); PTR(labels, 5); FLOAT(scale, 6); PTR(stats, 7); PTR(entropy, 8); PTR(dlogp, 9); PTR(dentropy, 10); PTR(dz, 11); STREAM(12);
+     RUN(mxc_logprob_bwd(d[0], d[1], d[2], d[3], z, (const int *)labels, (float)scale, (const float *)stats, (const float *)entropy, (const float *)dlogp,
+                         (const float *)dentropy, dz, st));)
+WRAP(mxc_logprob_fwd_bwd, 12, N_("N", "K", "ld", "dtype", "z", "labels", "scale", "dlogp", "dentropy", "logp", "entropy", "dz", "workspace", "stream"),
+     INTS(4); PTR(z, 4); PTR(labels, 5); FLOAT(scale, 6); PTR(dlogp, 7); PTR(dentropy, 8); PTR(logp, 9); PTR(entropy, 10); PTR(dz, 11); BUF(ws, 12);
+     STREAM(13);
+     RUN(mxc_logprob_fwd_bwd(d[0], d[1], d[2], d[3], z, (const int *)labels, (float)scale, (const float *)dlogp, (const float *)dentropy, (float *)logp,
+                             (float *)entropy, dz, ws, ws_n, st));)
+WRAP(mxc_mxfp4_quantize, 6, N_("N", "C", "dtype", "x", "codes", "scales", "stream"),
+     INTS(3); PTR(x, 3); PTR(codes, 4); PTR(scales, 5); STREAM(6); RUN(mxc_mxfp4_quantize(d[0], d[1], d[2], x, codes, scales, st));)
+WRAP(mxc_mxfp4_dequantize, 6, N_("N", "C", "dtype", "codes", "scales", "y", "stream"),
+     INTS(3); PTR(codes, 3); PTR(scales, 4); PTR(y, 5); STREAM(6); RUN(mxc_mxfp4_dequantize(d[0], d[1], d[2], codes, scales, y, st));)
+WRAP(mxc_mxfp4_fc_fwd, 10, N_("N", "C", "K", "dtype", "x", "w_codes", "w_scales", "bias", "relu", "y", "workspace", "stream"),
+     INTS(4); PTR(x, 4); PTR(wc, 5); PTR(wsc, 6); PTR(bias, 7); BOOL(relu, 8); PTR(y, 9); BUF(ws, 10); STREAM(11);
+     RUN(mxc_mxfp4_fc_fwd(d[0], d[1], d[2], d[3], x, wc, wsc, (const float *)bias, relu, y, ws, ws_n, st));)
+
+// what both AdamW calls read from their lists: element counts and pointers, and the element type of the gradients
+#define PTRS(NAME, AT, TYPE) std::vector<void *> NAME; at::ScalarType NAME##_t = at::ScalarType::TYPE;                          \
+    if (!to_ptrs(a.v[AT], names[AT], &NAME, &numel, (AT) == 0, &NAME##_t)) return nullptr
+#define LIST(NAME) (NAME.empty() ? nullptr : NAME.data())
+#define GRAD_TYPE const int gt = g_t == at::ScalarType::Float ? MXC_F32 : g_t == at::ScalarType::BFloat16 ? MXC_BF16 : g.empty() ? MXC_F32 : -1
+#define LONG(NAME, AT) const long long NAME = PyLong_AsLongLong(a.v[AT]); if (NAME == -1 && PyErr_Occurred()) return nullptr
+WRAP(mxc_adamw_update, 12, N_("w", "g", "m", "v", "w_bf16", "lr", "beta1", "beta2", "eps", "wd", "grad_scale", "step", "stream"),
+     std::vector<size_t> numel; PTRS(w, 0, Float); PTRS(g, 1, Undefined); PTRS(m, 2, Float); PTRS(v, 3, Float); PTRS(wb, 4, BFloat16); GRAD_TYPE;
+     FLOAT(lr, 5); FLOAT(b1, 6); FLOAT(b2, 7); FLOAT(eps, 8); FLOAT(wd, 9); FLOAT(gs, 10); LONG(step, 11); STREAM(12);
+     RUN(mxc_adamw_update((int)numel.size(), numel.data(), LIST(w), LIST(g), gt, LIST(m), LIST(v), LIST(wb), lr, b1, b2, eps, wd, gs, step, st));)
+WRAP(mxc_adamw8_update, 12, N_("w", "g", "state", "w_bf16", "lr", "beta1", "beta2", "eps", "wd", "grad_scale", "step", "seed", "stream"),
+     std::vector<size_t> numel; PTRS(w, 0, Float); PTRS(g, 1, Undefined); PTRS(wb, 3, BFloat16); GRAD_TYPE;
+     std::vector<size_t> bytes(numel.size());
+     for (size_t i = 0; i < numel.size(); ++i)
+         if ((rc = mxc_adamw8_state_bytes(numel[i], &bytes[i])) != MXC_OK) return done(rc);
+     std::vector<void *> state; at::ScalarType byte = at::ScalarType::Byte;
+     if (!to_ptrs(a.v[2], "state", &state, &bytes, false, &byte)) return nullptr;
+     FLOAT(lr, 4); FLOAT(b1, 5); FLOAT(b2, 6); FLOAT(eps, 7); FLOAT(wd, 8); FLOAT(gs, 9); LONG(step, 10);
+     const unsigned long long seed = PyLong_AsUnsignedLongLongMask(a.v[11]);        // its low 32 bits
+     if (PyErr_Occurred()) return nullptr;
+     STREAM(12);
+     RUN(mxc_adamw8_update((int)numel.size(), numel.data(), LIST(w), LIST(g), gt, LIST(state), LIST(wb), lr, b1, b2, eps, wd, gs, step, (unsigned)seed, st));)
 WRAP(mxc_layout_convert, 9, N_("n", "c", "h", "w", "dtype", "src_layout", "dst_layout", "src", "dst", "stream"),
      INTS(7); PTR(src, 7); PTR(dst, 8); STREAM(9);
      RUN(mxc_layout_convert(d[0], d[1], d[2], d[3], d[4], d[5], d[6], src, dst, st));)
@@ -228,6 +316,34 @@ PyObject *py_mxc_conv2d_workspace_bytes(PyObject *, PyObject *const *args, Py_ss
     const int rc = mxc_conv2d_workspace_bytes(d[0], d[1], d[2], d[3], d[4], d[5], d[6], d[7], d[8], d[9], d[10], d[11], &bytes);
     return rc == MXC_OK ? PyLong_FromSize_t(bytes) : done(rc);
     END_HANDLE_TH_ERRORS
+}
+
+// a size query FN(ints..., size_t *out): the ints and the size as a Python integer
+#define SIZE_QUERY(FN, COUNT, CALL, ...)                                                                                \
+    PyObject *py_##FN(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObject *kw)                                \
+    {                                                                                                                   \
+        static const char *const names[] = {__VA_ARGS__};                                                               \
+        Args a(#FN, names, COUNT, COUNT, args, nargs, kw);                                                              \
+        if (!a.ok) return nullptr;                                                                                      \
+        int d[COUNT];                                                                                                   \
+        if (!to_ints(a.v, d, COUNT)) return nullptr;                                                                    \
+        size_t bytes = 0;                                                                                               \
+        const int rc = CALL;                                                                                            \
+        return rc == MXC_OK ? PyLong_FromSize_t(bytes) : done(rc);                                                      \
+    }
+SIZE_QUERY(mxc_logprob_workspace_bytes, 4, mxc_logprob_workspace_bytes(d[0], d[1], d[2], d[3], &bytes), "N", "K", "dtype", "top")
+SIZE_QUERY(mxc_mxfp4_fc_workspace_bytes, 4, mxc_mxfp4_fc_workspace_bytes(d[0], d[1], d[2], d[3], &bytes), "N", "C", "K", "dtype")
+
+PyObject *py_mxc_adamw8_state_bytes(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObject *kw)
+{
+    static const char *const names[] = {"n"};
+    Args a("mxc_adamw8_state_bytes", names, 1, 1, args, nargs, kw);
+    if (!a.ok) return nullptr;
+    const size_t n = PyLong_AsSize_t(a.v[0]);
+    if (n == (size_t)-1 && PyErr_Occurred()) return nullptr;
+    size_t bytes = 0;
+    const int rc = mxc_adamw8_state_bytes(n, &bytes);
+    return rc == MXC_OK ? PyLong_FromSize_t(bytes) : done(rc);
 }
 
 // set_hooks(MxcError, raw_stream, device, slow_stream)
@@ -255,6 +371,9 @@ PyMethodDef methods[] = {
     ENTRY(mxc_conv2d_prepare_input), ENTRY(mxc_conv2d_fwd_prepared_input), ENTRY(mxc_conv2d_bwd_weight_prepared_input),
     ENTRY(mxc_bias_grad), ENTRY(mxc_fc_fwd), ENTRY(mxc_fc_bwd_data), ENTRY(mxc_fc_bwd_weight), ENTRY(mxc_softmax_fwd),
     ENTRY(mxc_softmax_xent_bwd), ENTRY(mxc_sgd_update), ENTRY(mxc_layout_convert), ENTRY(mxc_conv2d_workspace_bytes),
+    ENTRY(mxc_logprob_workspace_bytes), ENTRY(mxc_logprob_fwd), ENTRY(mxc_logprob_bwd), ENTRY(mxc_logprob_fwd_bwd),
+    ENTRY(mxc_mxfp4_quantize), ENTRY(mxc_mxfp4_dequantize), ENTRY(mxc_mxfp4_fc_workspace_bytes), ENTRY(mxc_mxfp4_fc_fwd),
+    ENTRY(mxc_adamw_update), ENTRY(mxc_adamw8_state_bytes), ENTRY(mxc_adamw8_update),
     {"set_hooks", (PyCFunction)(void *)py_set_hooks, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", "Call path of the mxc binding", -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -308,6 +308,39 @@ int sgd_update(size_t n, float *w, const float *g, float *v, void *w_copy, float
 int softmax_fwd(int N, int K, int dtype, const void *z, void *p, hipStream_t st);
 int softmax_xent_bwd(int N, int K, int dtype, const void *p, const int *labels, void *dz, float scale, hipStream_t st);
 
+// ---- logprob.hip: log probabilities, entropies, top tokens and their gradient -------------
+size_t logprob_workspace(int N, int K, int dtype, int top);
+struct LogprobArgs {
+    int N, K, ld, dtype, top;
+    const void *z;
+    const int *labels;
+    float scale;
+    const float *dlogp, *dentropy;              // gradients (dz != nullptr)
+    float *logp, *entropy, *stats, *top_logp;   // each may be nullptr
+    int *top_index;
+    void *dz;
+};
+int logprob_rows(const LogprobArgs &a, void *workspace, hipStream_t st);
+int logprob_bwd(const LogprobArgs &a, const float *stats, const float *entropy, hipStream_t st);
+
+// ---- mxfp4.hip, mxfp4_fc.hip: microscaled 4-bit floating point --------------------------------
+inline size_t mxfp4_code_row(int C) { return ((size_t)C + 31) / 32 * 16; }
+inline size_t mxfp4_scale_row(int C) { return ((size_t)C + 511) / 512 * 16; }
+int mxfp4_quantize(int N, int C, int dtype, const void *x, void *codes, void *scales, hipStream_t st);
+int mxfp4_dequantize(int N, int C, int dtype, const void *codes, const void *scales, void *y, hipStream_t st);
+size_t mxfp4_fc_workspace(int N, int C, int K, int dtype);
+int mxfp4_fc(int N, int C, int K, int dtype, const void *x, const void *w_codes, const void *w_scales, const float *bias, int relu, void *y,
+             void *workspace, hipStream_t st);
+
+// ---- adamw.hip: AdamW over many tensors ---------------------------------------------------------
+struct AdamwFactors {
+    float beta1, one_beta1, beta2, one_beta2, root_scale, eps, rate, keep, grad_scale;      // rate: lr/(1 - beta1^t); keep: 1 - lr*wd
+};
+constexpr size_t ADAMW8_RECORD = 528;      // bytes of the 8-bit state of 256 values
+// v == nullptr: m holds 8-bit states
+int adamw_update(int count, const size_t *sizes, void *const *w, const void *const *g, int grad_dtype, void *const *m, void *const *v,
+                 void *const *w_bf16, const AdamwFactors &f, unsigned seed, hipStream_t st);
+
 // ---- bias.hip: bias gradient ------------------------------------------------------------
 size_t bias_grad_scratch(long long N, int K, long long PQ, int dtype, int layout);      // bytes of partial vectors
 int bias_grad(long long N, int K, long long PQ, int dtype, int layout, const void *dy, float *db, float *partial, hipStream_t st);

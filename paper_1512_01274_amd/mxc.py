@@ -19,6 +19,7 @@ MXC_FWD, MXC_BWD_DATA, MXC_BWD_WEIGHT, MXC_BWD_DATA_RELU, MXC_BIAS_GRAD = 0, 1, 
 MXC_BWD_DATA_FILTER, MXC_BWD_DATA_PREPARED, MXC_BWD_DATA_PREPARED_RELU, MXC_BWD_WEIGHT_BF16 = 5, 6, 7, 8
 MXC_INPUT_PREPARED, MXC_FWD_PREPARED_INPUT, MXC_BWD_WEIGHT_PREPARED_INPUT, MXC_BWD_WEIGHT_PREPARED_INPUT_BF16 = 9, 10, 11, 12
 MXC_FWD_TRANSFORM = 13
+MXC_LOGPROB_MAX_TOP, MXC_ADAMW_GROUP = 64, 72
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libmxc.so")
 if not os.path.exists(LIB_PATH):
@@ -75,6 +76,21 @@ _lib.mxc_softmax_xent_bwd.restype = _I
 _F = ctypes.c_float
 _lib.mxc_sgd_update.argtypes = [_SZ, _VP, _VP, _VP, _VP, _F, _F, _F, _VP]
 _lib.mxc_sgd_update.restype = _I
+_D, _LL, _U, _PSZ, _VPP = ctypes.c_double, ctypes.c_longlong, ctypes.c_uint, ctypes.POINTER(_SZ), ctypes.POINTER(_VP)
+for _name, _args in (
+        ("mxc_logprob_workspace_bytes", [_I] * 4 + [_PSZ]),
+        ("mxc_logprob_fwd", [_I] * 4 + [_VP, _VP, _F, _I] + [_VP] * 6 + [_SZ, _VP]),
+        ("mxc_logprob_bwd", [_I] * 4 + [_VP, _VP, _F] + [_VP] * 6),
+        ("mxc_logprob_fwd_bwd", [_I] * 4 + [_VP, _VP, _F] + [_VP] * 6 + [_SZ, _VP]),
+        ("mxc_mxfp4_quantize", [_I] * 3 + [_VP] * 4),
+        ("mxc_mxfp4_dequantize", [_I] * 3 + [_VP] * 4),
+        ("mxc_mxfp4_fc_workspace_bytes", [_I] * 4 + [_PSZ]),
+        ("mxc_mxfp4_fc_fwd", [_I] * 4 + [_VP] * 4 + [_I, _VP, _VP, _SZ, _VP]),
+        ("mxc_adamw_update", [_I, _PSZ, _VPP, _VPP, _I, _VPP, _VPP, _VPP] + [_D] * 6 + [_LL, _VP]),
+        ("mxc_adamw8_state_bytes", [_SZ, _PSZ]),
+        ("mxc_adamw8_update", [_I, _PSZ, _VPP, _VPP, _I, _VPP, _VPP] + [_D] * 6 + [_LL, _U, _VP])):
+    getattr(_lib, _name).argtypes = _args
+    getattr(_lib, _name).restype = _I
 _lib.mxc_probe_mfma.argtypes = [_I, _I, _VP, _SZ, ctypes.POINTER(ctypes.c_double), _VP]
 _lib.mxc_probe_mfma.restype = _I
 
@@ -179,14 +195,26 @@ def _stream(stream):
 #   mxc_softmax_fwd(N, K, dtype, z, p, stream=None)
 #   mxc_softmax_xent_bwd(N, K, dtype, p, labels, scale, dz, stream=None)
 #   mxc_sgd_update(w, g, v, w_bf16, lr, momentum, wd, stream=None)      in place on w and v (v, w_bf16 may be None)
+#   mxc_logprob_workspace_bytes(N, K, dtype, top) -> int
+#   mxc_logprob_fwd(N, K, ld, dtype, z, labels, scale, top, logp, entropy, stats, top_logp, top_index, workspace=None, stream=None)
+#   mxc_logprob_bwd(N, K, ld, dtype, z, labels, scale, stats, entropy, dlogp, dentropy, dz, stream=None)
+#   mxc_logprob_fwd_bwd(N, K, ld, dtype, z, labels, scale, dlogp, dentropy, logp, entropy, dz, workspace=None, stream=None)
+#   mxc_mxfp4_quantize(N, C, dtype, x, codes, scales, stream=None)
+#   mxc_mxfp4_dequantize(N, C, dtype, codes, scales, y, stream=None)
+#   mxc_mxfp4_fc_workspace_bytes(N, C, K, dtype) -> int
+#   mxc_mxfp4_fc_fwd(N, C, K, dtype, x, w_codes, w_scales, bias, relu, y, workspace=None, stream=None)
+#   mxc_adamw_update(w, g, m, v, w_bf16, lr, beta1, beta2, eps, wd, grad_scale, step, stream=None)      lists of tensors, in place on w, m, v
+#   mxc_adamw8_state_bytes(n) -> int
+#   mxc_adamw8_update(w, g, state, w_bf16, lr, beta1, beta2, eps, wd, grad_scale, step, seed, stream=None)  state: lists of byte tensors
 #   mxc_layout_convert(n, c, h, w, dtype, src_layout, dst_layout, src, dst, stream=None)
 from paper_1512_01274_amd import _native  # noqa: E402
 from paper_1512_01274_amd._native import (  # noqa: E402,F401
-    mxc_bias_grad, mxc_conv2d_bwd_data, mxc_conv2d_bwd_data_prepare_filter, mxc_conv2d_bwd_data_prepared,
+    mxc_adamw8_state_bytes, mxc_adamw8_update, mxc_adamw_update, mxc_bias_grad, mxc_conv2d_bwd_data, mxc_conv2d_bwd_data_prepare_filter, mxc_conv2d_bwd_data_prepared,
     mxc_conv2d_bwd_data_relu, mxc_conv2d_bwd_weight, mxc_conv2d_bwd_weight_bf16, mxc_conv2d_bwd_weight_prepared_input,
     mxc_conv2d_bwd_weight_static, mxc_conv2d_fwd, mxc_conv2d_fwd_bias_act, mxc_conv2d_fwd_prepared_input,
     mxc_conv2d_fwd_transform, mxc_conv2d_prepare_input, mxc_conv2d_workspace_bytes, mxc_fc_bwd_data, mxc_fc_bwd_weight,
-    mxc_fc_fwd, mxc_layout_convert, mxc_sgd_update, mxc_softmax_fwd, mxc_softmax_xent_bwd)
+    mxc_fc_fwd, mxc_layout_convert, mxc_logprob_bwd, mxc_logprob_fwd, mxc_logprob_fwd_bwd, mxc_logprob_workspace_bytes,
+    mxc_mxfp4_dequantize, mxc_mxfp4_fc_fwd, mxc_mxfp4_fc_workspace_bytes, mxc_mxfp4_quantize, mxc_sgd_update, mxc_softmax_fwd, mxc_softmax_xent_bwd)
 
 _native.set_hooks(MxcError, getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None),
                   lambda: torch.cuda.current_stream().cuda_stream)

@@ -1,0 +1,267 @@
+"""Log probabilities, entropies, top tokens and gradients against the definition in 64 bits."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+DTYPES = [torch.float32, torch.bfloat16]
+U = 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def mxc():
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    from paper_1512_01274_amd import mxc as m
+    return m
+
+
+def exact(z, labels, scale, dlogp=None, dentropy=None):
+    """logp, entropy, log p of every entry and dz of rows z (float64), by the definition."""
+    N, K = z.shape
+    most = z.amax(1, keepdim=True)
+    empty = most == -math.inf
+    d = (z - most.masked_fill(empty, 0.0)) * scale
+    e = torch.exp(d)
+    S = e.sum(1, keepdim=True).masked_fill(empty, 1.0)
+    lp, p = d - torch.log(S), e / S
+    plp = torch.where(p > 0, p * lp, p * 0.0)       # (a NaN stays)
+    H = -plp.sum(1)
+    given = (labels >= 0) & (labels < K)
+    at = labels.clamp(0, K - 1).long().unsqueeze(1)
+    logp = torch.where(given, lp.gather(1, at).squeeze(1), 0.0)
+    if dlogp is None:
+        return logp, H, lp, p, d
+    dl, dh = (dlogp.double() * given)[:, None], dentropy.double()[:, None]
+    dz = -dl * p - dh * (plp + p * H[:, None])
+    dz.scatter_add_(1, at, dl)
+    return logp, H, lp, p, d, torch.where(empty, 0.0, dz * scale)
+
+
+def near(got, want, tol):
+    got, want = got.double(), want.double()
+    # (beyond 32 bits a finite value is minus infinity)
+    same = (got == want) | (got.isnan() & want.isnan()) | ((got < -3.0e38) & (want < -3.0e38) & (want > -math.inf))
+    bad = ~(same | ((got - want).abs() <= tol))
+    assert not bool(bad.any()), (int(bad.sum()), got[bad][:4], want[bad][:4])
+
+
+def row_tol(lp, H):
+    """A log probability in 32 bits: d is off by a few roundings of its size; the sum of the exponentials by a rounding for each link of
+    a chain of at most 1000, and by its terms' own errors, which are d's (weighted by p, where d is small)."""
+    return U * (8 * lp.abs() + 1024), U * 1024 * (1 + H)
+
+
+def data(N, K, ld, dtype, seed, masked):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    z = torch.randn(N, ld, generator=g, device="cuda") * 3
+    if masked:
+        z[torch.rand(N, ld, generator=g, device="cuda") < 0.1] = -math.inf if masked == 1 else float(torch.finfo(dtype).min)
+    z = z.to(dtype)
+    if ld > K:
+        z[:, K:] = float("nan")         # between two rows nothing is read
+    labels = torch.randint(0, K, (N,), generator=g, device="cuda", dtype=torch.int32)
+    if N > 3:
+        labels[1], labels[2] = -1, K
+        if masked:
+            z[3, :K] = -math.inf if masked == 1 else float(torch.finfo(dtype).min)
+    return z, labels, torch.randn(N, generator=g, device="cuda"), torch.randn(N, generator=g, device="cuda")
+
+
+def check(mxc, N, K, pad, dtype, masked, scale, top, seed=0, offset=0.0):
+    ld = K + pad
+    z, labels, dlogp, dentropy = data(N, K, ld, dtype, seed + N + K, masked)
+    if offset:
+        z = (z.float() + offset).to(dtype)
+    scale = float(np.float32(scale))
+    code = mxc.dtype_code(dtype)
+    logp, H, lp, p, d, dz = exact(z[:, :K].double(), labels, scale, dlogp, dentropy)
+    tl, th = row_tol(logp, H)
+    new = lambda *s, dtype=torch.float32: torch.full((math.prod(s) + 16,), 77, dtype=dtype, device="cuda")  # noqa: E731
+    got = {"logp": new(N), "entropy": new(N), "stats": new(N, 2), "tl": new(N, top), "ti": new(N, top, dtype=torch.int32)}
+    ws = mxc.alloc_workspace(mxc.mxc_logprob_workspace_bytes(N, K, code, top))
+    if ws is not None:
+        ws.fill_(0xFF)
+    mxc.mxc_logprob_fwd(N, K, ld, code, z, labels, scale, top, got["logp"], got["entropy"], got["stats"], got["tl"] if top else None,
+                        got["ti"] if top else None, ws)
+    for k, n in (("logp", N), ("entropy", N), ("stats", 2 * N), ("tl", N * top), ("ti", N * top)):
+        assert bool((got[k][n:] == 77).all()), k
+    near(got["logp"][:N], logp, tl)
+    near(got["entropy"][:N], H, th)
+    stats = got["stats"][:2 * N].view(N, 2)
+    most = z[:, :K].double().amax(1)
+    assert torch.equal(stats[:, 0].double(), most)
+    empty = most == -math.inf
+    near(stats[:, 1], torch.where(empty, 0.0, torch.log(torch.exp(d).sum(1))), U * 1024)
+    if top:
+        n = min(top, K)
+        ti, tlp = got["ti"][:N * top].view(N, top), got["tl"][:N * top].view(N, top)
+        # a stable sort of what the type holds: of equal values the lowest index first
+        want = torch.sort(z[:, :K].double() + 0.0, dim=1, descending=True, stable=True).indices[:, :n]
+        assert torch.equal(ti[:, :n].long(), want)
+        assert bool((ti[:, n:] == -1).all()) and bool((tlp[:, n:] == -math.inf).all())
+        wl = lp.gather(1, want)
+        over = wl < -3.0e38         # beyond 32 bits: minus infinity or the lowest
+        assert bool((tlp[:, :n][over] < -3.0e38).all())
+        near(torch.where(over, 0.0, tlp[:, :n].double()), torch.where(over, 0.0, wl), torch.where(over, 0.0, U * (8 * wl.abs() + 1024)))
+    # the gradient: a value's own rounding and the errors of its parts
+    grow = 8 * d.clamp(min=-200).abs() + 1024
+    TS = (p * d.clamp(min=-1e30)).sum(1, keepdim=True).abs()
+    dl = dlogp.double()[:, None].abs()
+    onehot = torch.zeros_like(p).scatter_(1, labels.clamp(0, K - 1).long()[:, None], 1.0)
+    tol = U * scale * (dl * (2 * onehot + p * grow) + dentropy.double()[:, None].abs() * p * (d.clamp(min=-200).abs() + TS + 1) * grow)
+    tol = torch.nan_to_num(tol, nan=0.0) + torch.nan_to_num(dz.abs()) * torch.finfo(dtype).eps / 2 + 1e-37
+    out = new(N, ld, dtype=dtype)
+    l2, h2 = new(N), new(N)
+    ws = mxc.alloc_workspace(mxc.mxc_logprob_workspace_bytes(N, K, code, 0))
+    mxc.mxc_logprob_fwd_bwd(N, K, ld, code, z, labels, scale, dlogp, dentropy, l2, h2, out, ws)
+    near(l2[:N], logp, tl)
+    near(h2[:N], H, th)
+    rows = out[:N * ld].view(N, ld)
+    near(rows[:, :K], dz, tol)
+    assert bool((rows[:, K:] == 77).all()) and bool((out[N * ld:] == 77).all())
+    # from the statistics of the forward pass; in place
+    buf = z.clone()
+    mxc.mxc_logprob_bwd(N, K, ld, code, buf, labels, scale, got["stats"], got["entropy"], dlogp, dentropy, buf)
+    near(buf[:, :K], dz, tol)
+    assert bool(buf[:, K:].isnan().all())
+    buf = z.clone()
+    mxc.mxc_logprob_fwd_bwd(N, K, ld, code, buf, labels, scale, dlogp, dentropy, l2, h2, buf, ws)
+    assert torch.equal(buf[:, :K], rows[:, :K])
+
+
+# lengths on both sides of every way of holding a row: one to some values, whole and broken 16-byte pieces, a wave's, a workgroup's, more
+LENGTHS = [1, 2, 3, 7, 8, 9, 31, 64, 65, 127, 255, 256, 257, 511, 512, 513, 1000, 1023, 1025, 2047, 2049, 4095, 4097, 8191, 8193, 16385, 32767, 32769]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("K", LENGTHS)
+def test_lengths(mxc, dtype, K):
+    check(mxc, 6, K, 0, dtype, 0, 1.0, 5)
+    check(mxc, 5, K, 3, dtype, 1, 0.7, 64, seed=1)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("N,K,pad", [(1, 131072, 0), (3, 131071, 1), (2, 131073, 0), (600, 50257, 47), (300, 50257, 0), (2, 300001, 5), (300, 70001, 0),
+                                     (2000, 10, 0), (1500, 129, 7), (4099, 33, 0), (1, 1, 0), (700, 1000, 0), (290, 131072, 0), (260, 140000, 1)])
+def test_rows(mxc, dtype, N, K, pad):
+    if N * K > 2.5e7 and dtype == torch.float32:
+        N = 258
+    check(mxc, N, K, pad, dtype, 0, 1.0, 20)
+    check(mxc, min(N, 280), K, pad, dtype, 2, 1.4, 1, seed=2)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("offset", [1000.0, -30000.0, 1.0e30])
+def test_far_from_zero(mxc, dtype, offset):
+    """Probabilities do not depend on where the logits lie, but for what the type holds of them."""
+    check(mxc, 4, 5000, 3, dtype, 0, 1.0, 8, offset=offset)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("K", [40, 3000, 140001])
+def test_ties_and_peaks(mxc, dtype, K):
+    """Equal logits, all of them or the largest few; descending, ascending and alternating rows; -0 beside 0."""
+    N, top = 7, 64
+    z = torch.zeros(N, K, device="cuda")
+    z[1] = -torch.arange(K, device="cuda") * 0.25
+    z[2] = torch.arange(K, device="cuda") * 0.25
+    z[3, ::2] = -0.0
+    z[4, K // 2:] = 3.0
+    z[5] = -math.inf
+    z[6, ::3] = 50.0
+    z = z.to(dtype)
+    index = torch.empty(N, top, dtype=torch.int32, device="cuda")
+    tl, logp, H = torch.empty(N, top, device="cuda"), torch.empty(N, device="cuda"), torch.empty(N, device="cuda")
+    labels = torch.zeros(N, dtype=torch.int32, device="cuda")
+    code = mxc.dtype_code(dtype)
+    ws = mxc.alloc_workspace(mxc.mxc_logprob_workspace_bytes(N, K, code, top))
+    mxc.mxc_logprob_fwd(N, K, K, code, z, labels, 1.0, top, logp, H, None, tl, index, ws)
+    n = min(K, top)
+    assert torch.equal(index[:, :n].long(), torch.sort(z.double() + 0.0, dim=1, descending=True, stable=True).indices[:, :n])
+    w = exact(z.double(), labels, 1.0)
+    near(H, w[1], row_tol(w[0], w[1])[1])
+    near(logp, w[0], row_tol(w[0], w[1])[0])
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("K", [50, 5000, 140001])
+def test_not_finite(mxc, dtype, K):
+    """A NaN or plus infinity makes its row NaN and no other one."""
+    N = 5
+    z, labels, dlogp, dentropy = data(N, K, K, dtype, 3, 0)
+    labels.fill_(1)
+    z[0, K - 1], z[2, K // 2], z[3, 0] = math.nan, math.inf, -math.nan
+    logp, H, dz = torch.empty(N, device="cuda"), torch.empty(N, device="cuda"), torch.empty_like(z)
+    code = mxc.dtype_code(dtype)
+    mxc.mxc_logprob_fwd_bwd(N, K, K, code, z, labels, 1.0, dlogp, dentropy, logp, H, dz, mxc.alloc_workspace(mxc.mxc_logprob_workspace_bytes(N, K, code, 0)))
+    bad = torch.tensor([True, False, True, True, False], device="cuda")
+    for t in (logp, H, dz):
+        assert bool(t[bad].isnan().all()) and bool(t[~bad].isfinite().all())
+
+
+@pytest.mark.parametrize("K", [6, 700])
+def test_gradient_by_differences(mxc, K):
+    """dz against central differences of the weighted sum of logp and entropy, both in 64 bits but for dz."""
+    z, labels, dlogp, dentropy = data(3, K, K, torch.float32, 9, 0)
+    dz = torch.empty_like(z)
+    mxc.mxc_logprob_fwd_bwd(3, K, K, 0, z, labels, 0.5, dlogp, dentropy, None, None, dz, mxc.alloc_workspace(mxc.mxc_logprob_workspace_bytes(3, K, 0, 0)))
+    h = 2.0 ** -14
+
+    def total(zz):
+        logp, H = exact(zz, labels, 0.5)[:2]
+        return logp * dlogp.double() + H * dentropy.double()
+    for k in list(range(min(K, 6))) + [int(labels[0])]:
+        step = torch.zeros(3, K, device="cuda", dtype=torch.float64)
+        step[:, k] = h
+        slope = (total(z.double() + step) - total(z.double() - step)) / (2 * h)
+        # sums of at most 20 links in 32 bits; the third derivative times h^2/6 and 64-bit rounding over 2h are smaller
+        assert bool(((dz[:, k].double() - slope).abs() <= 64 * U * (dlogp.abs() + 20 * dentropy.abs())).all()), k
+
+
+def test_parts_left_out(mxc):
+    """NULL outputs and gradients."""
+    N, K = 5, 3001
+    z, labels, dlogp, dentropy = data(N, K, K, torch.bfloat16, 4, 1)
+    zero = torch.zeros(N, device="cuda")
+    ws = mxc.alloc_workspace(mxc.mxc_logprob_workspace_bytes(N, K, 1, 64))
+    a, b = torch.empty_like(z), torch.empty_like(z)
+    for dl, dh in ((dlogp, None), (None, dentropy), (None, None)):
+        mxc.mxc_logprob_fwd_bwd(N, K, K, 1, z, labels, 1.0, dl, dh, None, None, a, ws)
+        mxc.mxc_logprob_fwd_bwd(N, K, K, 1, z, labels, 1.0, zero if dl is None else dl, zero if dh is None else dh, None, None, b, ws)
+        assert torch.equal(a, b)
+    full = [torch.empty(N, device="cuda"), torch.empty(N, device="cuda"), torch.empty(N, 2, device="cuda")]
+    mxc.mxc_logprob_fwd(N, K, K, 1, z, labels, 1.0, 0, *full, None, None, ws)
+    for i in range(3):
+        part = [torch.empty_like(t) if i == j else None for j, t in enumerate(full)]
+        mxc.mxc_logprob_fwd(N, K, K, 1, z, labels if i == 0 else None, 1.0, 0, *part, None, None, ws)
+        assert torch.equal(part[i], full[i])
+
+
+def test_graph_and_stream(mxc):
+    """Captured on a stream of its own and replayed on new inputs, with eager work between the replays."""
+    for N, K in ((1, 140000), (300, 6000)):
+        z, labels, dlogp, dentropy = data(N, K, K, torch.bfloat16, 5, 0)
+        logp, H, dz = torch.empty(N, device="cuda"), torch.empty(N, device="cuda"), torch.empty_like(z)
+        tl, ti = torch.empty(N, 9, device="cuda"), torch.empty(N, 9, device="cuda", dtype=torch.int32)
+        ws = mxc.alloc_workspace(mxc.mxc_logprob_workspace_bytes(N, K, 1, 9))
+
+        def both():
+            mxc.mxc_logprob_fwd(N, K, K, 1, z, labels, 1.0, 9, logp, H, None, tl, ti, ws)
+            mxc.mxc_logprob_fwd_bwd(N, K, K, 1, z, labels, 1.0, dlogp, dentropy, logp, H, dz, ws)
+        both()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            both()
+        for i in range(4):
+            z.copy_(data(N, K, K, torch.bfloat16, 50 + i, i % 3)[0])
+            both()
+            torch.cuda.synchronize()
+            want = [t.clone() for t in (logp, H, dz, tl, ti)]
+            for t in (logp, H, dz, tl, ti):
+                t.fill_(1)
+            graph.replay()
+            torch.cuda.synchronize()
+            for t, w in zip((logp, H, dz, tl, ti), want):
+                assert torch.equal(torch.nan_to_num(t.float()), torch.nan_to_num(w.float()))

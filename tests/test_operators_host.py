@@ -1,0 +1,136 @@
+"""Argument checks of the log-probability, 4-bit and AdamW calls: found on the host, before anything is launched (pointers are fake
+and never followed)."""
+import ctypes
+
+import pytest
+
+A, B, C_, D, E, F_, G, H = (4096 * (i + 1) for i in range(8))       # fake device addresses, 16-byte aligned
+NAN, INF = float("nan"), float("inf")
+
+
+@pytest.fixture(scope="module")
+def mxc():
+    from paper_1512_01274_amd import mxc as m
+    return m
+
+
+def test_logprob_refusals(mxc):
+    lib = mxc.raw()
+
+    def fwd(N=4, K=100, ld=104, dtype=1, z=A, labels=B, scale=1.0, top=5, logp=C_, entropy=D, stats=E, tl=F_, ti=G, ws=H, wn=1 << 30):
+        return lib.mxc_logprob_fwd(N, K, ld, dtype, z, labels, scale, top, logp, entropy, stats, tl, ti, ws, wn, None)
+
+    def bwd(N=4, K=100, ld=104, dtype=1, z=A, labels=B, scale=1.0, stats=C_, entropy=D, dlogp=E, dentropy=F_, dz=G):
+        return lib.mxc_logprob_bwd(N, K, ld, dtype, z, labels, scale, stats, entropy, dlogp, dentropy, dz, None)
+
+    def both(N=4, K=100, ld=104, dtype=1, z=A, labels=B, scale=1.0, dlogp=C_, dentropy=D, logp=E, entropy=F_, dz=G, ws=H, wn=1 << 30):
+        return lib.mxc_logprob_fwd_bwd(N, K, ld, dtype, z, labels, scale, dlogp, dentropy, logp, entropy, dz, ws, wn, None)
+
+    for call in (fwd, bwd, both):
+        for bad in (dict(N=0), dict(N=-1), dict(K=0), dict(ld=99), dict(ld=-5)):
+            assert call(**bad) == mxc.MXC_ERR_SHAPE, bad
+        for bad in (dict(dtype=2), dict(dtype=-1), dict(scale=0.0), dict(scale=-1.0), dict(scale=NAN), dict(scale=INF)):
+            assert call(**bad) == mxc.MXC_ERR_UNSUPPORTED, bad
+        assert call(z=None) == mxc.MXC_ERR_NULL and call(labels=None) == mxc.MXC_ERR_NULL
+        assert call(z=A + 8) == mxc.MXC_ERR_ALIGN and call(labels=B + 2) == mxc.MXC_ERR_ALIGN and call(entropy=D + 1) == mxc.MXC_ERR_ALIGN
+    assert fwd(top=65) == mxc.MXC_ERR_SHAPE and fwd(top=-1) == mxc.MXC_ERR_SHAPE
+    assert fwd(tl=None) == mxc.MXC_ERR_NULL and fwd(ti=None) == mxc.MXC_ERR_NULL
+    assert bwd(stats=None) == mxc.MXC_ERR_NULL and bwd(dz=None) == mxc.MXC_ERR_NULL and bwd(entropy=None) == mxc.MXC_ERR_NULL
+    assert both(dz=None) == mxc.MXC_ERR_NULL and both(dz=G + 4) == mxc.MXC_ERR_ALIGN
+    n = ctypes.c_size_t()
+    assert lib.mxc_logprob_workspace_bytes(1, 1, 0, 0, None) == mxc.MXC_ERR_NULL
+    assert lib.mxc_logprob_workspace_bytes(1, 0, 0, 0, ctypes.byref(n)) == mxc.MXC_ERR_SHAPE
+    assert lib.mxc_logprob_workspace_bytes(1, 1, 0, 65, ctypes.byref(n)) == mxc.MXC_ERR_SHAPE
+    assert lib.mxc_logprob_workspace_bytes(1, 1, 7, 0, ctypes.byref(n)) == mxc.MXC_ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("N,K", [(1, 1), (1, 1 << 20), (3, 131072), (4096, 50257), (1 << 20, 7)])
+def test_logprob_workspace(mxc, N, K):
+    """What the size query names is what the call asks for."""
+    lib = mxc.raw()
+    for dtype in (0, 1):
+        for top in (0, 5, 64):
+            need = mxc.mxc_logprob_workspace_bytes(N, K, dtype, top)
+            assert need % 256 == 0
+            if need:
+                assert lib.mxc_logprob_fwd(N, K, K, dtype, A, B, 1.0, top, C_, D, E, F_, G, H, 0, None) == mxc.MXC_ERR_WORKSPACE
+                assert lib.mxc_logprob_fwd(N, K, K, dtype, A, B, 1.0, top, C_, D, E, F_, G, None, need, None) == mxc.MXC_ERR_WORKSPACE
+
+
+def test_mxfp4_refusals(mxc):
+    lib = mxc.raw()
+    for call in (lib.mxc_mxfp4_quantize, lib.mxc_mxfp4_dequantize):
+        assert call(0, 5, 0, A, B, C_, None) == mxc.MXC_ERR_SHAPE and call(5, -1, 0, A, B, C_, None) == mxc.MXC_ERR_SHAPE
+        assert call(1 << 30, 1 << 30, 0, A, B, C_, None) == mxc.MXC_ERR_SHAPE
+        assert call(5, 5, 2, A, B, C_, None) == mxc.MXC_ERR_UNSUPPORTED
+        for i in range(3):
+            null, off = [A, B, C_], [A, B, C_]
+            null[i], off[i] = None, off[i] + 4
+            assert call(5, 5, 1, *null, None) == mxc.MXC_ERR_NULL and call(5, 5, 1, *off, None) == mxc.MXC_ERR_ALIGN
+
+    def fc(N=5, C=70, K=9, dtype=1, x=A, wc=B, ws=C_, bias=D, relu=1, y=E, w=F_, wn=1 << 30):
+        return lib.mxc_mxfp4_fc_fwd(N, C, K, dtype, x, wc, ws, bias, relu, y, w, wn, None)
+
+    for bad in (dict(N=0), dict(C=0), dict(K=-3), dict(C=1 << 30, K=1 << 30)):
+        assert fc(**bad) == mxc.MXC_ERR_SHAPE, bad
+    assert fc(dtype=5) == mxc.MXC_ERR_UNSUPPORTED and fc(relu=2) == mxc.MXC_ERR_UNSUPPORTED
+    for name in ("x", "wc", "ws", "y"):
+        assert fc(**{name: None}) == mxc.MXC_ERR_NULL and fc(**{name: A + 2}) == mxc.MXC_ERR_ALIGN
+    assert fc(bias=D + 2) == mxc.MXC_ERR_ALIGN
+    need = mxc.mxc_mxfp4_fc_workspace_bytes(300, 5000, 70, 1)
+    assert need and fc(N=300, C=5000, K=70, wn=need - 256) == mxc.MXC_ERR_WORKSPACE and fc(N=300, C=5000, K=70, w=None) == mxc.MXC_ERR_WORKSPACE
+
+
+def arrays(*addresses):
+    return (ctypes.c_void_p * len(addresses))(*addresses)
+
+
+def test_adamw_refusals(mxc):
+    lib = mxc.raw()
+    two = (ctypes.c_size_t * 2)
+
+    def call(count=2, sizes=two(3, 5), w=arrays(A, B), g=arrays(C_, D), gt=0, m=arrays(E, F_), v=arrays(G, H), wb=None, lr=1e-3, b1=0.9, b2=0.999,
+             eps=1e-8, wd=0.1, gs=1.0, step=1, bits=32):
+        if bits == 32:
+            return lib.mxc_adamw_update(count, sizes, w, g, gt, m, v, wb, lr, b1, b2, eps, wd, gs, step, None)
+        return lib.mxc_adamw8_update(count, sizes, w, g, gt, m, wb, lr, b1, b2, eps, wd, gs, step, 1, None)
+
+    for bits in (32, 8):
+        for bad in (dict(count=0), dict(count=-1), dict(step=0), dict(sizes=two(3, (1 << 34) + 1))):
+            assert call(bits=bits, **bad) == mxc.MXC_ERR_SHAPE, bad
+        for bad in (dict(gt=2), dict(b1=1.0), dict(b2=1.0), dict(b1=-0.1), dict(b2=NAN), dict(eps=-1e-8), dict(eps=NAN), dict(lr=INF), dict(lr=NAN),
+                    dict(wd=NAN), dict(gs=INF)):
+            assert call(bits=bits, **bad) == mxc.MXC_ERR_UNSUPPORTED, bad
+        for bad in (dict(sizes=None), dict(w=None), dict(g=None), dict(m=None), dict(w=arrays(A, None)), dict(wb=arrays(A, None))):
+            assert call(bits=bits, **bad) == mxc.MXC_ERR_NULL, bad
+        for bad in (dict(w=arrays(A, B + 4)), dict(g=arrays(C_ + 2, D)), dict(m=arrays(E, F_ + 8)), dict(wb=arrays(A + 2, B))):
+            assert call(bits=bits, **bad) == mxc.MXC_ERR_ALIGN, bad
+        # tensors of no values are passed over, whatever their pointers: here there is nothing else
+        nothing = arrays(None, None)
+        assert call(bits=bits, sizes=two(0, 0), w=nothing, g=nothing, m=nothing, v=nothing, wb=nothing) == mxc.MXC_OK
+    assert call(v=None) == mxc.MXC_ERR_NULL and call(v=arrays(G, H + 1)) == mxc.MXC_ERR_ALIGN
+    assert mxc.mxc_adamw8_state_bytes(0) == 0 and mxc.mxc_adamw8_state_bytes(1) == 528 and mxc.mxc_adamw8_state_bytes(257) == 1056
+    with pytest.raises(mxc.MxcError):
+        mxc.mxc_adamw8_state_bytes((1 << 34) + 1)
+
+
+def test_binding_lists(mxc):
+    """Lists that do not fit each other are refused by the binding (fake device tensors: nothing is launched)."""
+    import torch
+    from torch._subclasses.fake_tensor import FakeTensorMode
+    args = (1e-3, 0.9, 0.999, 1e-8, 0.1, 1.0, 1)
+    with FakeTensorMode():
+        w, g, h = (torch.empty(4, device="cuda") for _ in range(3))
+        b = torch.empty(4, device="cuda", dtype=torch.bfloat16)
+        for lists, error in [((w, [g], [g], [g], None), TypeError), (([w], [3], [g], [g], None), TypeError), (([b], [g], [g], [g], None), TypeError),
+                             (([w], [g], [b], [g], None), TypeError), (([w], [g], [g], [g], [g]), TypeError)]:
+            with pytest.raises(error):
+                mxc.mxc_adamw_update(*lists, *args, 0)
+    cpu = torch.empty(4)
+    with pytest.raises(ValueError):
+        mxc.mxc_adamw_update([cpu], [cpu], [cpu], [cpu], None, *args, 0)
+    with pytest.raises(ValueError):
+        mxc.mxc_adamw8_update([cpu], [cpu], [cpu], None, *args, 1, 0)
+    with pytest.raises(mxc.MxcError) as e:
+        mxc.mxc_adamw_update([], [], [], [], None, *args, 0)
+    assert e.value.status == mxc.MXC_ERR_SHAPE
