@@ -37,34 +37,53 @@ __device__ __forceinline__ float step_one(float &w, float g, float &m, float &v,
     return r;
 }
 
-// the tensor of this workgroup
+// the tensor of this workgroup: the last one that begins at or before it (tensors of no values begin where the next one does).  Every lane
+// looks at one place of the table, which is one access to the kernel's arguments where a binary search is seven in a row.
 __device__ __forceinline__ int find_tensor(const Group &q)
 {
-    int lo = 0, hi = q.count - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (q.first[mid] <= blockIdx.x) lo = mid;
-        else hi = mid - 1;
-    }
-    return lo;
+    const int lane = threadIdx.x & 63;
+    int n = __popcll(__ballot(lane < q.count && q.first[lane] <= blockIdx.x));
+    if (q.count > 64) n += __popcll(__ballot(64 + lane < q.count && q.first[min(64 + lane, MXC_ADAMW_GROUP)] <= blockIdx.x));
+    return __builtin_amdgcn_readfirstlane(n - 1);
 }
 
-constexpr int CHUNK = 1024;     // values a workgroup
+constexpr int CHUNK = 1024;     // values a workgroup: four a thread, a record of 256 a wave
+
+__device__ __forceinline__ float4 load4(const float *p) { return *reinterpret_cast<const float4 *>(p); }
+__device__ __forceinline__ float4 load4(const bf16_t *p)
+{
+    const uint2 u = *reinterpret_cast<const uint2 *>(p);
+    return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xFFFF0000u), __uint_as_float(u.y << 16), __uint_as_float(u.y & 0xFFFF0000u));
+}
+__device__ __forceinline__ void store_copy(bf16_t *p, const float *w) { *reinterpret_cast<uint2 *>(p) = make_uint2(pack_bf16x2(w[0], w[1]), pack_bf16x2(w[2], w[3])); }
 
 template <typename G>
 __global__ __launch_bounds__(256) void adamw_kernel(Group q)
 {
     const int i = find_tensor(q);
     const Tensor &t = q.t[i];
-    const size_t at = (size_t)(blockIdx.x - q.first[i]) * CHUNK;
-    for (int k = threadIdx.x; k < CHUNK && at + k < t.n; k += 256) {
-        const size_t j = at + k;
-        float w = t.w[j], m = ((float *)t.m)[j], v = t.v[j];
-        step_one(w, load_f32((const G *)t.g + j), m, v, q.f);
-        t.w[j] = w;
-        ((float *)t.m)[j] = m;
-        t.v[j] = v;
-        if (t.copy) t.copy[j] = (bf16_t)pack_bf16x2(w, w);
+    const size_t j = (size_t)(blockIdx.x - q.first[i]) * CHUNK + threadIdx.x * 4;
+    float *tm = (float *)t.m;
+    const G *tg = (const G *)t.g;
+    if (j + 4 <= t.n) {
+        const float4 w4 = load4(t.w + j), m4 = load4(tm + j), v4 = load4(t.v + j), g4 = load4(tg + j);
+        float w[4] = {w4.x, w4.y, w4.z, w4.w}, m[4] = {m4.x, m4.y, m4.z, m4.w}, v[4] = {v4.x, v4.y, v4.z, v4.w};
+        const float g[4] = {g4.x, g4.y, g4.z, g4.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) step_one(w[k], g[k], m[k], v[k], q.f);
+        *reinterpret_cast<float4 *>(t.w + j) = make_float4(w[0], w[1], w[2], w[3]);
+        *reinterpret_cast<float4 *>(tm + j) = make_float4(m[0], m[1], m[2], m[3]);
+        *reinterpret_cast<float4 *>(t.v + j) = make_float4(v[0], v[1], v[2], v[3]);
+        if (t.copy) store_copy(t.copy + j, w);
+        return;
+    }
+    for (size_t k = j; k < t.n; ++k) {
+        float w = t.w[k], m = tm[k], v = t.v[k];
+        step_one(w, load_f32(tg + k), m, v, q.f);
+        t.w[k] = w;
+        tm[k] = m;
+        t.v[k] = v;
+        if (t.copy) t.copy[k] = (bf16_t)pack_bf16x2(w, w);
     }
 }
 
@@ -76,21 +95,24 @@ __device__ __forceinline__ unsigned mix(unsigned x)
     return x ^ (x >> 16);
 }
 
-__device__ __forceinline__ float scale_value(unsigned b) { return b == 255u ? __uint_as_float(0x7FC00000u) : b ? __uint_as_float(b << 23) : __uint_as_float(1u << 22); }
-
-__device__ __forceinline__ float e4m3_value(unsigned c)
+// values of four codes (no code is the format's NaN) times the block's scale
+__device__ __forceinline__ void decode4(unsigned codes, float scale, float *x)
 {
-    const unsigned e = (c >> 3) & 15u, m = c & 7u;
-    float v = e ? __uint_as_float(((e + 120u) << 23) | (m << 20)) : (float)m * 0x1p-9f;
-    if ((c & 127u) == 127u) v = __uint_as_float(0x7FC00000u);
-    return c & 128u ? -v : v;
+    typedef float f32x2_t __attribute__((ext_vector_type(2)));
+    const f32x2_t lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, true);
+    x[0] = lo.x * scale;
+    x[1] = lo.y * scale;
+    x[2] = hi.x * scale;
+    x[3] = hi.y * scale;
 }
 
 // largest |x| of the block's eight lanes, as bits
 __device__ __forceinline__ unsigned block_largest(const float *x)
 {
     unsigned b = 0;
+#pragma unroll
     for (int k = 0; k < 4; ++k) b = max(b, __float_as_uint(x[k]) & 0x7FFFFFFFu);
+#pragma unroll
     for (int d = 1; d < 8; d <<= 1) b = max(b, (unsigned)__shfl_xor((int)b, d));
     return b;
 }
@@ -103,14 +125,16 @@ __device__ __forceinline__ unsigned scale_byte(unsigned largest)
     return (unsigned)max(field - 8 + ((largest & 0x7FFFFFu) > 0x600000u ? 1 : 0), 0);
 }
 
-__device__ __forceinline__ unsigned e4m3_code(float x, unsigned byte, float u, bool root)
+// Code of x by a random choice u = u16*2^-16 between its neighbours: floor(y*2^(10-E) + u) + 8*(E - 1), y = |x|/scale in [0, 448], E its
+// exponent's field in the code, at least 1.  From y = 2^-6 on the sum has no more than the 24 bits of a float's mantissa, and the
+// whole is one addition to the float's bits (a carry moves on to the next exponent by itself); below, E = 1 and the sum is a float's.
+__device__ __forceinline__ unsigned e4m3_code(float x, float up, unsigned u16, bool root)
 {
-    if (byte == 255u) return 0u;
-    const float y = fabsf(x) * __uint_as_float((254u - byte) << 23);
-    const int E = max((int)(__float_as_uint(y) >> 23) - 120, 1);
-    int k = (int)floorf(y * __uint_as_float((unsigned)(137 - E) << 23) + u) + (E - 1) * 8;
-    if (root && k == 0 && x > 0.f) k = 1;
-    return (unsigned)k | (x < 0.f ? 128u : 0u);
+    const float y = fabsf(x) * up;
+    const unsigned normal = ((__float_as_uint(y) + (u16 << 4)) >> 20) - 960u;
+    unsigned k = y < 0x1p-6f ? (unsigned)(y * 512.f + (float)u16 * 0x1p-16f) : normal;
+    if (root) k = max(k, x > 0.f ? 1u : 0u);
+    return k | (x < 0.f ? 128u : 0u);
 }
 
 // a wave holds one record of 256 values, four a lane, eight lanes a block
@@ -123,31 +147,54 @@ __global__ __launch_bounds__(256) void adamw8_kernel(Group q)
     const size_t record = (size_t)(blockIdx.x - q.first[i]) * (CHUNK / 256) + (threadIdx.x >> 6);
     if (record * 256 >= t.n) return;
     unsigned char *state = (unsigned char *)t.m + record * ADAMW8_RECORD;
-    const unsigned key = mix(q.seed + (unsigned)(q.base + i + 1) * 0x9E3779B9u);
+    const size_t j = record * 256 + lane * 4;
     const unsigned mc = *(const unsigned *)(state + lane * 4), rc = *(const unsigned *)(state + 256 + lane * 4);
-    const float ms = scale_value(state[512 + lane / 8]), rs = scale_value(state[520 + lane / 8]);
-    float m[4], r[4];
+    const unsigned msb = state[512 + lane / 8], rsb = state[520 + lane / 8];
+    const G *tg = (const G *)t.g;
+    const bool whole = j + 4 <= t.n;
+    float w[4] = {0.f, 0.f, 0.f, 0.f}, g[4] = {0.f, 0.f, 0.f, 0.f}, m[4], r[4];
+    if (whole) {
+        const float4 w4 = load4(t.w + j), g4 = load4(tg + j);
+        w[0] = w4.x; w[1] = w4.y; w[2] = w4.z; w[3] = w4.w;
+        g[0] = g4.x; g[1] = g4.y; g[2] = g4.z; g[3] = g4.w;
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (j + k < t.n) {
+                w[k] = t.w[j + k];
+                g[k] = load_f32(tg + j + k);
+            }
+    }
+    decode4(mc, e8m0_value(msb), m);
+    decode4(rc, e8m0_value(rsb), r);
+#pragma unroll
     for (int k = 0; k < 4; ++k) {
-        const size_t j = record * 256 + lane * 4 + k;
-        const bool in = j < t.n;
-        m[k] = e4m3_value((mc >> (8 * k)) & 255u) * ms;
-        r[k] = e4m3_value((rc >> (8 * k)) & 255u) * rs;
-        float w = in ? t.w[j] : 0.f, v = r[k] * r[k];
-        r[k] = step_one(w, in ? load_f32((const G *)t.g + j) : 0.f, m[k], v, q.f);
-        if (in) {
-            t.w[j] = w;
-            if (t.copy) t.copy[j] = (bf16_t)pack_bf16x2(w, w);
-        }
+        float v = r[k] * r[k];
+        r[k] = step_one(w[k], g[k], m[k], v, q.f);
+    }
+    if (whole) {
+        *reinterpret_cast<float4 *>(t.w + j) = make_float4(w[0], w[1], w[2], w[3]);
+        if (t.copy) store_copy(t.copy + j, w);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (j + k < t.n) {
+                t.w[j + k] = w[k];
+                if (t.copy) t.copy[j + k] = (bf16_t)pack_bf16x2(w[k], w[k]);
+            }
     }
     const unsigned mb = scale_byte(block_largest(m)), rb = scale_byte(block_largest(r));
-    unsigned mo = 0, ro = 0;
-    for (int k = 0; k < 4; ++k) {
-        const unsigned bits = mix((unsigned)(record * 256 + lane * 4 + k) * 0x9E3779B9u + key);
-        mo |= e4m3_code(m[k], mb, (float)(bits & 0xFFFFu) * 0x1p-16f, false) << (8 * k);
-        ro |= e4m3_code(r[k], rb, (float)(bits >> 16) * 0x1p-16f, true) << (8 * k);
+    const float mup = __uint_as_float((254u - mb) << 23), rup = __uint_as_float((254u - rb) << 23);       // 1/scale (at 255 nothing is read)
+    const unsigned key = mix(q.seed + (unsigned)(q.base + i + 1) * 0x9E3779B9u);
+    unsigned mo = 0, ro = 0, at = (unsigned)j * 0x9E3779B9u + key;
+#pragma unroll
+    for (int k = 0; k < 4; ++k, at += 0x9E3779B9u) {
+        const unsigned bits = mix(at);
+        mo |= e4m3_code(m[k], mup, bits & 0xFFFFu, false) << (8 * k);
+        ro |= e4m3_code(r[k], rup, bits >> 16, true) << (8 * k);
     }
-    *(unsigned *)(state + lane * 4) = mo;
-    *(unsigned *)(state + 256 + lane * 4) = ro;
+    *(unsigned *)(state + lane * 4) = mb == 255u ? 0u : mo;
+    *(unsigned *)(state + 256 + lane * 4) = rb == 255u ? 0u : ro;
     if (lane % 8 == 0) {
         state[512 + lane / 8] = (unsigned char)mb;
         state[520 + lane / 8] = (unsigned char)rb;

@@ -53,6 +53,9 @@ __device__ __forceinline__ float load_f32(const bf16_t *p) { return bf16_to_f32(
 __device__ __forceinline__ void store_f32(float *p, float v) { *p = v; }
 __device__ __forceinline__ void store_f32(bf16_t *p, float v) { *p = f32_to_bf16(v); }
 
+// the power of two that a scale byte stands for; 255 is NaN
+__device__ __forceinline__ float e8m0_value(unsigned b) { return __uint_as_float(b == 255u ? 0x7FC00000u : b ? b << 23 : 1u << 22); }
+
 // Order of a launch's tiles.  Each XCD, whose L2 is its own, gets `share` tiles that follow each other: what they read between
 // them is least when the tiles that share the larger operand's rows are neighbours.  bm, bn: what a tile reads of either operand.  True:
 // the row tiles of a column follow each other, which has to save a quarter (5850 pixels, 112 columns, 5x5 on 176 channels, near the
