@@ -2,126 +2,742 @@
 // sum of log probabilities and entropies.  With d = scale*(z - max), S = sum exp(d), T = sum exp(d)*d:
 //     logp = d[label] - log S,    entropy = log S - T/S,    dz = e*(A + B*d) + [k == label]*scale*dlogp,
 //     e = exp(d), A = scale/S*(dentropy*T/S - dlogp), B = -scale/S*dentropy.
-// fp32 arithmetic whatever the storage type.
+// fp32 arithmetic whatever the storage type, in powers of two: d2 = d/ln 2, so that an exponential is one instruction.
+//
+// A row is read once.  Workgroups of 64 to 1024 threads hold it in registers as 16-byte pieces (up to 256 KB: half of a compute
+// unit's registers), meet for the maximum and for the sums, and write the gradient from what they hold.  Few rows, and rows that
+// are longer, are cut into chunks, each with its own maximum and sums, which a second launch joins (and reads again for the gradient).
+#include <type_traits>
+
 #include "mxc_internal.h"
 
 namespace mxc {
 namespace {
 
-constexpr float LOWEST = -3.402823466e38f;
+constexpr float LOWEST = -3.402823466e38f, LN2 = 0.693147182464599609f, LOG2E = 1.442695021629333496f;
+constexpr float NO_WEIGHT = -300.f;     // exp2 of this is 0: a term exp2(d)*d is 0 there, also at d = minus infinity
+constexpr unsigned long long NO_KEY = 0;
 
-// where exp(d) is 0 the product exp(d)*d is 0, also at d = minus infinity
-constexpr float NO_WEIGHT = -200.f;
-
-// a larger key is a larger value, of equal ones the one of the lower index; 0 is no entry.  -0 counts as 0.
-__device__ __forceinline__ unsigned long long rank_key(float z, unsigned index)
+// ordered as the values are; -0 and 0 are one value
+__device__ __forceinline__ unsigned order(float z)
 {
     const int b = __float_as_int(z + 0.f);
-    const unsigned o = (unsigned)(b < 0 ? b ^ 0x7FFFFFFF : b) ^ 0x80000000u;
-    return ((unsigned long long)o << 32) | (0xFFFFFFFFu - index);
+    return (unsigned)(b ^ ((b >> 31) & 0x7FFFFFFF)) ^ 0x80000000u;
 }
-
-constexpr int THREADS = 256;
-
-template <class T, class F>
-__device__ __forceinline__ T block_join(T v, T *red, F f)
+__device__ __forceinline__ float unorder(unsigned o)
 {
-    red[threadIdx.x] = v;
-    __syncthreads();
-    for (int half = THREADS / 2; half > 0; half >>= 1) {
-        if ((int)threadIdx.x < half) red[threadIdx.x] = f(red[threadIdx.x], red[threadIdx.x + half]);
-        __syncthreads();
-    }
-    const T r = red[0];
-    __syncthreads();
+    const int b = (int)(o ^ 0x80000000u);
+    return __int_as_float(b ^ ((b >> 31) & 0x7FFFFFFF));
+}
+// a larger key is a larger value, of equal ones the one of the lower index; NO_KEY is less than any
+__device__ __forceinline__ unsigned long long key_of(unsigned o, unsigned index) { return ((unsigned long long)o << 32) | (0xFFFFFFFFu - index); }
+__device__ __forceinline__ unsigned key_index(unsigned long long key) { return 0xFFFFFFFFu - (unsigned)key; }
+
+// fmaxf takes an instruction more, for the sake of signalling NaNs
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
     return r;
 }
 
 template <typename T>
-__device__ void write_gradient(const LogprobArgs &a, const T *z, T *dz, size_t row, float m, float S, float TS, bool empty)
+struct Piece {      // 16 bytes of a row
+    static constexpr int V = 16 / (int)sizeof(T);
+    uint32_t w[4];
+    __device__ __forceinline__ float at(int k) const
+    {
+        if constexpr (V == 8) return __uint_as_float(k & 1 ? w[k / 2] & 0xFFFF0000u : w[k / 2] << 16);
+        else return __uint_as_float(w[k]);
+    }
+    // The same for passes after the first: the compiler would keep both halves of each word as floats, or what the first pass made of
+    // them, in twice the registers.
+    __device__ __forceinline__ float again(int k) const
+    {
+        if constexpr (V == 8) {
+            float r;
+            if (k & 1) asm volatile("v_and_b32 %0, %1, %2" : "=v"(r) : "s"(0xFFFF0000u), "v"(w[k / 2]));
+            else asm volatile("v_lshlrev_b32 %0, 16, %1" : "=v"(r) : "v"(w[k / 2]));
+            return r;
+        } else {
+            uint32_t r;
+            asm volatile("" : "=v"(r) : "0"(w[k]));
+            return __uint_as_float(r);
+        }
+    }
+    template <bool AGAIN>
+    __device__ __forceinline__ float largest() const
+    {
+        auto v = [&](int k) { return AGAIN ? again(k) : at(k); };
+        float m = v(0);
+#pragma unroll
+        for (int k = 1; k + 1 < V; k += 2) m = max3(m, v(k), v(k + 1));
+        const float last = v(V - 1);
+        return max3(m, last, last);
+    }
+    __device__ __forceinline__ void nothing()      // minus infinities: no weight in any sum
+    {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[k] = V == 8 ? 0xFF80FF80u : 0xFF800000u;
+    }
+};
+
+// A row as pieces at 16-byte boundaries: the first and the last may be shared with what lies before and behind the row, which is
+// neither read nor written.
+template <typename T>
+struct Row {
+    static constexpr int V = Piece<T>::V;
+    const T *z;         // element `head` elements before the row's first
+    T *dz;
+    int head, K, pieces;
+    __device__ __forceinline__ Row(const LogprobArgs &a, size_t row)
+    {
+        const size_t first = row * a.ld;
+        head = (int)(first % V);
+        K = a.K;
+        pieces = (a.K + head + V - 1) / V;
+        z = (const T *)a.z + first - head;
+        dz = a.dz ? (T *)a.dz + first - head : nullptr;
+    }
+    __device__ __forceinline__ bool whole(int piece) const { return piece * V >= head && (piece + 1) * V <= K + head; }
+    __device__ __forceinline__ Piece<T> load(int piece) const
+    {
+        Piece<T> p;
+        if (whole(piece)) {
+            const uint4 u = reinterpret_cast<const uint4 *>(z)[(unsigned)piece];
+            p.w[0] = u.x; p.w[1] = u.y; p.w[2] = u.z; p.w[3] = u.w;
+        } else {
+            p.nothing();
+            if (piece < pieces) {
+#pragma unroll
+                for (int k = 0; k < V; ++k) {
+                    const int i = piece * V + k;
+                    if (i < head || i >= K + head) continue;
+                    if constexpr (V == 8) {
+                        const uint32_t v = z[i];
+                        p.w[k / 2] = k & 1 ? (p.w[k / 2] & 0xFFFFu) | (v << 16) : (p.w[k / 2] & 0xFFFF0000u) | v;
+                    } else
+                        p.w[k] = __float_as_uint(z[i]);
+                }
+            }
+        }
+        return p;
+    }
+    __device__ __forceinline__ void store(int piece, const float *g) const
+    {
+        if (whole(piece)) {
+            uint4 u;
+            if constexpr (V == 8) u = make_uint4(pack_bf16x2(g[0], g[1]), pack_bf16x2(g[2], g[3]), pack_bf16x2(g[4], g[5]), pack_bf16x2(g[6], g[7]));
+            else u = make_uint4(__float_as_uint(g[0]), __float_as_uint(g[1]), __float_as_uint(g[2]), __float_as_uint(g[3]));
+            reinterpret_cast<uint4 *>(dz)[(unsigned)piece] = u;
+        } else if (piece < pieces) {
+#pragma unroll
+            for (int k = 0; k < V; ++k) {
+                const int i = piece * V + k;
+                if (i < head || i >= K + head) continue;
+                if constexpr (V == 8) dz[i] = (bf16_t)pack_bf16x2(g[k], g[k]);
+                else dz[i] = g[k];
+            }
+        }
+    }
+};
+
+// d2 of a logit.  Near: one fma, z*k2 + c with c = -max*k2 rounded once: the same for the whole row, so that it moves the
+// reference point of d2 a little (by less than 2^-8) and cancels in every result.  Far from zero, where it would move it by more, and where the products
+// overflow: the difference first.
+struct Scale {
+    float k2, m, c;
+    bool near;
+    __device__ __forceinline__ Scale(float scale, float most)
+    {
+        k2 = scale * LOG2E;
+        m = most;
+        c = -(most * k2);
+        near = fabsf(c) < 65536.f;
+    }
+    template <bool NEAR>
+    __device__ __forceinline__ float d2(float z) const { return NEAR ? fmaf(z, k2, c) : (z - m) * k2; }
+    __device__ __forceinline__ float any(float z) const { return near ? d2<true>(z) : d2<false>(z); }
+};
+
+// lanes of a group of G (a power of two up to a wave) meet
+template <int G, class F>
+__device__ __forceinline__ float meet(float x, F f)
 {
-    const int label = a.labels ? a.labels[row] : -1;
-    const float dl = a.dlogp && (unsigned)label < (unsigned)a.K ? a.dlogp[row] : 0.f, dh = a.dentropy ? a.dentropy[row] : 0.f;
-    const float A = a.scale / S * (dh * TS - dl), B = -a.scale / S * dh;
-    for (int k = threadIdx.x; k < a.K; k += THREADS) {
-        const float d = (load_f32(z + k) - m) * a.scale;
-        const float g = expf(d) * (A + B * fmaxf(d, NO_WEIGHT)) + (k == label ? a.scale * dl : 0.f);
-        store_f32(dz + k, empty ? 0.f : g);
+#pragma unroll
+    for (int d = G / 2; d > 0; d >>= 1) x = f(x, __shfl_xor(x, d));
+    return x;
+}
+__device__ __forceinline__ float larger(float a, float b) { return fmaxf(a, b); }
+__device__ __forceinline__ float sum(float a, float b) { return a + b; }
+
+// ---- the most probable tokens ---------------------------------------------------------------------------------------------
+// Cells are sets of a wave's values, 64 or more of them, of which each lane knows the largest.  The top-th largest of these is a bound that
+// `top` values reach at least; so is the largest of the waves' bounds.  What reaches it is collected in LDS and ranked by
+// counting, which makes the order that of the keys whatever order they were collected in.
+constexpr int CAP = 1024;
+struct TopShared {
+    unsigned long long list[CAP];
+    unsigned bound[16], tie[16];
+    int count;
+};
+
+// the largest t that at least n of the wave's cells reach (t's lowest LOW bits are 0)
+template <int S, int LOW>
+__device__ __forceinline__ unsigned wave_bound(const unsigned *cell, int n)
+{
+    unsigned t = 0;
+    for (int b = 31; b >= LOW; --b) {
+        const unsigned trial = t | (1u << b);
+        int c = 0;
+#pragma unroll
+        for (int s = 0; s < S; ++s) c += __popcll(__ballot(cell[s] >= trial));
+        if (c >= n) t = trial;
+    }
+    return t;
+}
+
+// Hands the i-th largest key of the row to emit(i, key); places past the last value get NO_KEY.  Called by a whole workgroup of W waves;
+// cell: this lane's S cells.  each(from, f) calls f(order, index) for each of the thread's values that reaches `from`.
+template <int W, int S, int LOW, class Each, class Emit>
+__device__ __forceinline__ void select_top(TopShared &sh, const unsigned *cell, int top, Each each, Emit emit)
+{
+    const int wave = threadIdx.x >> 6;
+    const unsigned mine = wave_bound<S, LOW>(cell, top);
+    if (threadIdx.x == 0) sh.count = 0;
+    unsigned bound = mine;
+    if constexpr (W > 1) {
+        if ((threadIdx.x & 63) == 0) sh.bound[wave] = mine;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < W; ++w) bound = max(bound, sh.bound[w]);
+    } else
+        __syncthreads();
+    auto collect = [&](unsigned from, unsigned tie) {       // values above `from`, and equal ones up to index `tie`
+        each(from, [&](unsigned o, unsigned index) {
+            if (o >> LOW > from >> LOW || index <= tie) {
+                const int at = atomicAdd(&sh.count, 1);
+                if (at < CAP) sh.list[at] = key_of(o, index);
+            }
+        });
+        __syncthreads();
+    };
+    collect(bound, 0xFFFFFFFFu);
+    int n = sh.count;
+    if (n > CAP) {
+        // Many equal values (rows of one value, rows where few tokens are allowed): of those at the bound only the lowest
+        // indices count.  Each lane's first one is a cell again.
+        __syncthreads();
+        if (threadIdx.x == 0) sh.count = 0;
+        unsigned first = 0xFFFFFFFFu;
+        each(bound, [&](unsigned o, unsigned index) { if (o >> LOW == bound >> LOW) first = min(first, index); });
+        const unsigned cells[1] = {~first};
+        const unsigned t = ~wave_bound<1, 0>(cells, top);       // (no less than top: those above the bound may be none)
+        unsigned tie = t;
+        if constexpr (W > 1) {
+            if ((threadIdx.x & 63) == 0) sh.tie[wave] = t;
+            __syncthreads();
+#pragma unroll
+            for (int w = 0; w < W; ++w) tie = min(tie, sh.tie[w]);
+        } else
+            __syncthreads();
+        collect(bound, tie);
+        n = sh.count;
+    }
+    if (n <= CAP) {
+        for (int i = threadIdx.x; i < n; i += 64 * W) {
+            const unsigned long long key = sh.list[i];
+            int rank = 0;
+            for (int j = 0; j < n; ++j) rank += sh.list[j] > key ? 1 : 0;
+            if (rank < top) emit(rank, key);
+        }
+        for (int i = n + (int)threadIdx.x; i < top; i += 64 * W) emit(i, NO_KEY);
+        return;
+    }
+    // the largest values crowd in a few threads' pieces: one after the other
+    unsigned long long last = ~0ull;
+    for (int i = 0; i < top; ++i) {
+        unsigned long long best = NO_KEY;
+        each(0, [&](unsigned o, unsigned index) {
+            const unsigned long long key = key_of(o, index);
+            if (key < last && key > best) best = key;
+        });
+#pragma unroll
+        for (int d = 32; d > 0; d >>= 1) {
+            const unsigned long long other = __shfl_xor(best, d);
+            best = other > best ? other : best;
+        }
+        if constexpr (W > 1) {
+            __syncthreads();
+            if ((threadIdx.x & 63) == 0) sh.list[wave] = best;
+            __syncthreads();
+            for (int w = 0; w < W; ++w) best = sh.list[w] > best ? sh.list[w] : best;
+        }
+        last = best;
+        if (threadIdx.x == 0) emit(i, best);
     }
 }
 
-template <typename T>
-__global__ __launch_bounds__(THREADS) void logprob_kernel(LogprobArgs a)
+// the values of a thread's pieces that reach `from`, and the row's index of each: f(order, index); first: the index of value 0 of piece 0
+template <typename T, int P, class F>
+__device__ __forceinline__ void each_value(const Piece<T> (&p)[P], int first, int stride, int K, unsigned from, F f)
 {
-    __shared__ float red[THREADS];
-    __shared__ unsigned long long redk[THREADS];
-    const size_t row = blockIdx.x;
-    const T *z = (const T *)a.z + row * a.ld;
-    auto max2 = [](float x, float y) { return fmaxf(x, y); };
-    auto add2 = [](float x, float y) { return x + y; };
-    float m = LOWEST;
-    for (int k = threadIdx.x; k < a.K; k += THREADS) m = fmaxf(m, load_f32(z + k));
-    m = block_join(m, red, max2);
-    float s = 0.f, t = 0.f;
-    for (int k = threadIdx.x; k < a.K; k += THREADS) {
-        const float d = (load_f32(z + k) - m) * a.scale, e = expf(d);
-        s += e;
-        t += e * fmaxf(d, NO_WEIGHT);
+    const float limit = unorder(from);
+    unsigned mask = 0;
+#pragma unroll
+    for (int q = 0; q < P; ++q) mask |= p[q].template largest<true>() < limit ? 0u : 1u << q;       // (all of them for the lowest bounds, which are NaN)
+    while (mask) {
+        const int q = __ffs(mask) - 1;
+        mask &= mask - 1;
+        Piece<T> c = p[0];
+#pragma unroll
+        for (int i = 1; i < P; ++i)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) c.w[k] = q == i ? p[i].w[k] : c.w[k];
+#pragma unroll
+        for (int k = 0; k < Piece<T>::V; ++k) {
+            const int i = first + q * stride + k;
+            const unsigned o = order(c.at(k));
+            if (o >= from && (unsigned)i < (unsigned)K) f(o, (unsigned)i);
+        }
     }
-    s = block_join(s, red, add2);
-    t = block_join(t, red, add2);
+}
+
+// ---- rows in registers ----------------------------------------------------------------------------------------------------
+
+// G threads a row, P pieces a thread; rows of fewer than a wave's lanes share one.  TOP: with the most probable tokens, else
+// the gradient where dz is given.
+template <typename T, int G, int P, bool TOP>
+__global__ __launch_bounds__(G < 64 ? 256 : G) void logprob_row_kernel(LogprobArgs a)
+{
+    constexpr int W = G / 64;       // waves a row; 0: several rows a wave
+    __shared__ float red[3][W > 1 ? W : 1];
+    const int lane = G < 64 ? threadIdx.x % G : threadIdx.x;
+    const size_t row = G < 64 ? (size_t)blockIdx.x * (256 / G) + threadIdx.x / G : (size_t)blockIdx.x;
+    if (G < 64 && row >= (size_t)a.N) return;
+    const Row<T> r(a, row);
+    Piece<T> p[P];
+#pragma unroll
+    for (int q = 0; q < P; ++q) p[q] = r.load(q * G + lane);
+    const int label = a.labels ? a.labels[row] : -1;
+    const bool given = (unsigned)label < (unsigned)a.K;
+    const float zl = given ? load_f32(r.z + r.head + label) : 0.f;      // (before the gradient is written: dz may be z)
+    auto meet_row = [&](float x, int slot, auto f) {
+        x = meet<(G < 64 ? G : 64)>(x, f);
+        if constexpr (W > 1) {
+            if ((threadIdx.x & 63) == 0) red[slot][threadIdx.x >> 6] = x;
+        }
+        return x;
+    };
+    auto joined = [&](float x, int slot, auto f) {
+        if constexpr (W > 1) {
+            x = red[slot][0];
+#pragma unroll
+            for (int w = 1; w < W; ++w) x = f(x, red[slot][w]);
+        }
+        return x;
+    };
+    constexpr int S = P < 4 ? P : 4;
+    float m = LOWEST;
+    unsigned cell[S];
+    if constexpr (TOP) {
+        float top_of[S];
+#pragma unroll
+        for (int q = 0; q < P; ++q) {
+            const float x = p[q].template largest<false>();
+            top_of[q % S] = q < S ? x : max3(top_of[q % S], x, x);
+        }
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+            cell[s] = order(top_of[s]);
+            m = fmaxf(m, top_of[s]);
+        }
+    } else {
+#pragma unroll
+        for (int q = 0; q < P; ++q) m = max3(m, p[q].template largest<false>(), m);
+    }
+    m = meet_row(m, 0, larger);
+    if constexpr (W > 1) __syncthreads();
+    m = joined(m, 0, larger);
+    const Scale sc(a.scale, m);
+    float s = 0.f, t = 0.f;
+    auto sums = [&](auto near) {
+#pragma unroll
+        for (int q = 0; q < P; ++q) {
+#pragma unroll
+            for (int k = 0; k < Piece<T>::V; ++k) {
+                const float d = sc.d2<decltype(near)::value>(p[q].again(k)), e = __builtin_amdgcn_exp2f(d);
+                s += e;
+                t = fmaf(e, fmaxf(d, NO_WEIGHT), t);
+            }
+        }
+    };
+    if (sc.near) sums(std::true_type());
+    else sums(std::false_type());
+    s = meet_row(s, 1, sum);
+    t = meet_row(t, 2, sum);
+    if constexpr (W > 1) __syncthreads();
+    s = joined(s, 1, sum);
+    t = joined(t, 2, sum);
     const bool empty = s == 0.f;
-    const float ls = empty ? 0.f : logf(s);
-    if (threadIdx.x == 0) {
-        const int label = a.labels ? a.labels[row] : -1;
-        if (a.logp) a.logp[row] = (unsigned)label >= (unsigned)a.K ? 0.f : empty ? -INFINITY : (load_f32(z + label) - m) * a.scale - ls;
-        if (a.entropy) a.entropy[row] = empty ? 0.f : ls - t / s;
+    const float ls = empty ? 0.f : log2f(s), mean = t / s;
+    if (lane == 0) {
+        if (a.logp) a.logp[row] = !given ? 0.f : empty ? -INFINITY : (sc.any(zl) - ls) * LN2;
+        if (a.entropy) a.entropy[row] = empty ? 0.f : (ls - mean) * LN2;
         if (a.stats) {
             a.stats[2 * row] = empty ? -INFINITY : m;
-            a.stats[2 * row + 1] = ls;
+            a.stats[2 * row + 1] = empty ? 0.f : (ls - sc.any(m)) * LN2;
         }
     }
-    unsigned long long last = ~0ull;
-    for (int i = 0; i < a.top; ++i) {
-        unsigned long long best = 0;
-        for (int k = threadIdx.x; k < a.K; k += THREADS) {
-            const unsigned long long key = rank_key(load_f32(z + k), (unsigned)k);
-            if (key < last && key > best) best = key;
-        }
-        last = block_join(best, redk, [](unsigned long long x, unsigned long long y) { return x > y ? x : y; });
-        if (threadIdx.x == 0) {
-            const int k = last ? (int)(0xFFFFFFFFu - (unsigned)last) : -1;
-            a.top_index[row * a.top + i] = k;
-            a.top_logp[row * a.top + i] = k < 0 || empty ? -INFINITY : (load_f32(z + k) - m) * a.scale - ls;
+    if constexpr (TOP) {
+        __shared__ TopShared sh;
+        select_top<W, S, sizeof(T) == 2 ? 16 : 0>(
+            sh, cell, a.top,
+            [&](unsigned from, auto f) { each_value<T, P>(p, lane * Piece<T>::V - r.head, G * Piece<T>::V, a.K, from, f); },
+            [&](int i, unsigned long long key) {
+                a.top_index[row * a.top + i] = key == NO_KEY ? -1 : (int)key_index(key);
+                a.top_logp[row * a.top + i] = key == NO_KEY || empty ? -INFINITY : (sc.any(unorder((unsigned)(key >> 32))) - ls) * LN2;
+            });
+    } else if (a.dz) {
+        const float dl = a.dlogp && given ? a.dlogp[row] : 0.f, dh = a.dentropy ? a.dentropy[row] : 0.f;
+        const float per = a.scale / s, A = per * (dh * (mean * LN2) - dl), B = -per * dh * LN2;
+        const int place = given ? label + r.head : -1;
+        auto gradient = [&](auto near) {
+#pragma unroll
+            for (int q = 0; q < P; ++q) {
+                float g[Piece<T>::V];
+#pragma unroll
+                for (int k = 0; k < Piece<T>::V; ++k) {
+                    const float d = sc.d2<decltype(near)::value>(p[q].again(k));
+                    g[k] = __builtin_amdgcn_exp2f(d) * fmaf(fmaxf(d, NO_WEIGHT), B, A);
+                }
+                const int at = place - (q * G + lane) * Piece<T>::V;
+                if ((unsigned)at < (unsigned)Piece<T>::V) {
+#pragma unroll
+                    for (int k = 0; k < Piece<T>::V; ++k)
+                        if (k == at) g[k] += a.scale * dl;
+                }
+                if (empty) {
+#pragma unroll
+                    for (int k = 0; k < Piece<T>::V; ++k) g[k] = 0.f;
+                }
+                r.store(q * G + lane, g);
+            }
+        };
+        if (sc.near) gradient(std::true_type());
+        else gradient(std::false_type());
+    }
+}
+
+// ---- rows in chunks -------------------------------------------------------------------------------------------------------
+
+constexpr int CHUNK_THREADS = 256;
+
+struct Part {       // of a chunk: its largest value, its sums, and the label's logit where it lies there
+    float m, s, t, zl;
+};
+
+template <typename T, int P, bool TOP>
+__global__ __launch_bounds__(CHUNK_THREADS) void logprob_chunk_kernel(LogprobArgs a, int chunks, Part *parts, unsigned long long *keys)
+{
+    constexpr int G = CHUNK_THREADS, V = Piece<T>::V, S = P < 4 ? P : 4;
+    __shared__ float red[3][4];
+    const size_t row = blockIdx.x / (unsigned)chunks;
+    const int chunk = blockIdx.x % (unsigned)chunks;
+    const Row<T> r(a, row);
+    const int piece0 = chunk * (G * P);
+    Piece<T> p[P];
+#pragma unroll
+    for (int q = 0; q < P; ++q) p[q] = r.load(piece0 + q * G + (int)threadIdx.x);
+    float top_of[S], m = LOWEST;
+    unsigned cell[S];
+#pragma unroll
+    for (int q = 0; q < P; ++q) {
+        const float x = p[q].template largest<false>();
+        top_of[q % S] = q < S ? x : max3(top_of[q % S], x, x);
+    }
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+        cell[s] = order(top_of[s]);
+        m = fmaxf(m, top_of[s]);
+    }
+    const int wave = threadIdx.x >> 6;
+    m = meet<64>(m, larger);
+    if ((threadIdx.x & 63) == 0) red[0][wave] = m;
+    __syncthreads();
+    m = max3(max3(red[0][0], red[0][1], red[0][2]), red[0][3], LOWEST);
+    const Scale sc(a.scale, m);
+    float s = 0.f, t = 0.f;
+#pragma unroll
+    for (int q = 0; q < P; ++q) {
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            const float d = sc.d2<false>(p[q].again(k)), e = __builtin_amdgcn_exp2f(d);
+            s += e;
+            t = fmaf(e, fmaxf(d, NO_WEIGHT), t);
         }
     }
-    if (a.dz) write_gradient(a, z, (T *)a.dz + row * a.ld, row, m, s, t / s, empty);
+    s = meet<64>(s, sum);
+    t = meet<64>(t, sum);
+    if ((threadIdx.x & 63) == 0) {
+        red[1][wave] = s;
+        red[2][wave] = t;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        const int label = a.labels ? a.labels[row] : -1, at = label + r.head - piece0 * V;
+        const bool here = (unsigned)label < (unsigned)a.K && (unsigned)at < (unsigned)(G * P * V);
+        parts[blockIdx.x] = Part{m, red[1][0] + red[1][1] + red[1][2] + red[1][3], red[2][0] + red[2][1] + red[2][2] + red[2][3],
+                                 here ? load_f32(r.z + r.head + label) : 0.f};
+    }
+    if constexpr (TOP) {
+        __shared__ TopShared sh;
+        select_top<4, S, sizeof(T) == 2 ? 16 : 0>(
+            sh, cell, a.top,
+            [&](unsigned from, auto f) { each_value<T, P>(p, (piece0 + (int)threadIdx.x) * V - r.head, G * V, a.K, from, f); },
+            [&](int i, unsigned long long key) { keys[(size_t)blockIdx.x * a.top + i] = key; });
+    }
+}
+
+// the chunks' sums at the row's maximum, in the chunks' order within each thread and the threads' in a fixed one
+struct Joined {
+    float m, s, t;
+};
+template <int W>
+__device__ __forceinline__ Joined join_parts(const Part *parts, int chunks, float scale, float (*red)[W])
+{
+    const int wave = threadIdx.x >> 6;
+    float m = LOWEST;
+    for (int c = threadIdx.x; c < chunks; c += 64 * W) m = fmaxf(m, parts[c].m);
+    m = meet<64>(m, larger);
+    if ((threadIdx.x & 63) == 0) red[0][wave] = m;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < W; ++w) m = fmaxf(m, red[0][w]);
+    const Scale sc(scale, m);
+    float s = 0.f, t = 0.f;
+    for (int c = threadIdx.x; c < chunks; c += 64 * W) {
+        const Part q = parts[c];
+        const float d = sc.d2<false>(q.m), e = __builtin_amdgcn_exp2f(d);
+        s = fmaf(q.s, e, s);
+        t = fmaf(fmaf(fmaxf(d, NO_WEIGHT), q.s, q.t), e, t);
+    }
+    s = meet<64>(s, sum);
+    t = meet<64>(t, sum);
+    if ((threadIdx.x & 63) == 0) {
+        red[1][wave] = s;
+        red[2][wave] = t;
+    }
+    __syncthreads();
+    Joined j{m, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+        j.s += red[1][w];
+        j.t += red[2][w];
+    }
+    return j;
 }
 
 template <typename T>
-__global__ __launch_bounds__(THREADS) void logprob_bwd_kernel(LogprobArgs a, const float *stats, const float *entropy)
+__device__ __forceinline__ void write_row_results(const LogprobArgs &a, size_t row, const Part *parts, int span, const Joined &j)
 {
+    const int label = a.labels ? a.labels[row] : -1;
+    const bool given = (unsigned)label < (unsigned)a.K, empty = j.s == 0.f;
+    const float ls = empty ? 0.f : log2f(j.s);
+    const Scale sc(a.scale, j.m);
+    if (a.logp) {
+        const float zl = given ? parts[(label + Row<T>(a, row).head) / span].zl : 0.f;
+        a.logp[row] = !given ? 0.f : empty ? -INFINITY : (sc.d2<false>(zl) - ls) * LN2;
+    }
+    if (a.entropy) a.entropy[row] = empty ? 0.f : (ls - j.t / j.s) * LN2;
+    if (a.stats) {
+        a.stats[2 * row] = empty ? -INFINITY : j.m;
+        a.stats[2 * row + 1] = ls * LN2;
+    }
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void logprob_join_kernel(LogprobArgs a, int chunks, int span, const Part *parts, const unsigned long long *keys)
+{
+    __shared__ float red[3][4];
     const size_t row = blockIdx.x;
+    parts += row * chunks;
+    const Joined j = join_parts<4>(parts, chunks, a.scale, red);
+    if (threadIdx.x == 0) write_row_results<T>(a, row, parts, span, j);
+    if (a.top == 0) return;
+    __shared__ TopShared sh;
+    keys += row * chunks * a.top;
+    const int n = chunks * a.top;       // (fewer than 2^31: logprob_rows)
+    unsigned cell[4] = {0, 0, 0, 0};
+    for (int i = threadIdx.x, s = 0; i < n; i += 256, s = (s + 1) & 3) {
+        const unsigned o = (unsigned)(keys[i] >> 32);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) cell[c] = c == s ? max(cell[c], o) : cell[c];
+    }
+    const bool empty = j.s == 0.f;
+    const float ls = empty ? 0.f : log2f(j.s);
+    const Scale sc(a.scale, j.m);
+    select_top<4, 4, sizeof(T) == 2 ? 16 : 0>(
+        sh, cell, a.top,
+        [&](unsigned from, auto f) {
+            if (max(max(cell[0], cell[1]), max(cell[2], cell[3])) < from) return;
+            for (int i = threadIdx.x; i < n; i += 256) {
+                const unsigned long long key = keys[i];
+                if (key != NO_KEY && (unsigned)(key >> 32) >= from) f((unsigned)(key >> 32), key_index(key));
+            }
+        },
+        [&](int i, unsigned long long key) {
+            a.top_index[row * a.top + i] = key == NO_KEY ? -1 : (int)key_index(key);
+            a.top_logp[row * a.top + i] = key == NO_KEY || empty ? -INFINITY : (sc.d2<false>(unorder((unsigned)(key >> 32))) - ls) * LN2;
+        });
+}
+
+// the gradient of a chunk's values: e2 = log2 of the probability up to ls, mean: T/S in d2's units
+template <typename T, int P>
+__device__ __forceinline__ void chunk_gradient(const LogprobArgs &a, size_t row, int chunk, float m, float s, float mean, bool empty)
+{
+    constexpr int V = Piece<T>::V;
+    const Row<T> r(a, row);
+    const Scale sc(a.scale, m);
+    const int label = a.labels ? a.labels[row] : -1;
+    const bool given = (unsigned)label < (unsigned)a.K;
+    const float dl = a.dlogp && given ? a.dlogp[row] : 0.f, dh = a.dentropy ? a.dentropy[row] : 0.f;
+    const float per = a.scale / s, A = per * (dh * (mean * LN2) - dl), B = -per * dh * LN2;
+    const int place = given ? label + r.head : -1;
+    const int piece0 = chunk * (CHUNK_THREADS * P) + (int)threadIdx.x;
+    Piece<T> p[P];
+#pragma unroll
+    for (int q = 0; q < P; ++q) p[q] = r.load(piece0 + q * CHUNK_THREADS);
+#pragma unroll
+    for (int q = 0; q < P; ++q) {
+        const int piece = piece0 + q * CHUNK_THREADS;
+        float g[V];
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            const float d = sc.d2<false>(p[q].at(k));
+            g[k] = __builtin_amdgcn_exp2f(d) * fmaf(fmaxf(d, NO_WEIGHT), B, A) + (place == piece * V + k ? a.scale * dl : 0.f);
+            if (empty) g[k] = 0.f;
+        }
+        r.store(piece, g);
+    }
+}
+
+template <typename T, int P>
+__global__ __launch_bounds__(CHUNK_THREADS) void logprob_gradient_kernel(LogprobArgs a, int chunks, int span, const Part *parts)
+{
+    __shared__ float red[3][4];
+    const size_t row = blockIdx.x / (unsigned)chunks;
+    const int chunk = blockIdx.x % (unsigned)chunks;
+    parts += row * chunks;
+    const Joined j = join_parts<4>(parts, chunks, a.scale, red);
+    if (chunk == 0 && threadIdx.x == 0) write_row_results<T>(a, row, parts, span, j);
+    chunk_gradient<T, P>(a, row, chunk, j.m, j.s, j.t / j.s, j.s == 0.f);
+}
+
+template <typename T, int P>
+__global__ __launch_bounds__(CHUNK_THREADS) void logprob_bwd_kernel(LogprobArgs a, int chunks, const float *stats, const float *entropy)
+{
+    const size_t row = blockIdx.x / (unsigned)chunks;
     const float m = stats[2 * row], ls = stats[2 * row + 1];
-    write_gradient(a, (const T *)a.z + row * a.ld, (T *)a.dz + row * a.ld, row, m, expf(ls), entropy ? ls - entropy[row] : 0.f, m == -INFINITY);
+    chunk_gradient<T, P>(a, row, blockIdx.x % (unsigned)chunks, m, expf(ls), entropy ? (ls - entropy[row]) * LOG2E : 0.f, m == -INFINITY);
+}
+
+// ---- host -----------------------------------------------------------------------------------------------------------------
+
+// pieces that a row of K values can have
+int row_pieces(int K, int dtype)
+{
+    const int V = 16 / (int)elem_size(dtype);
+    return (int)(((long long)K + 2 * V - 2) / V);
+}
+
+constexpr int ROW_PIECES = 16384;       // in registers: 16 of each of 1024 threads
+
+// chunks of a row (0: rows in registers).  Pieces a thread of a chunk: 1 or 8.
+int chunk_pieces(int N, int K, int dtype)
+{
+    const int pieces = row_pieces(K, dtype);
+    if (pieces > ROW_PIECES) return N < 64 ? 1 : 8;
+    if (pieces > 1024 && N < 64) return 1;
+    return 0;
+}
+int chunk_count(int K, int dtype, int per_thread) { return (int)(((long long)row_pieces(K, dtype) + CHUNK_THREADS * per_thread - 1) / (CHUNK_THREADS * per_thread)); }
+
+template <typename T, bool TOP>
+void launch_row(const LogprobArgs &a, hipStream_t st)
+{
+    const int pieces = row_pieces(a.K, a.dtype);
+    const dim3 rows((unsigned)a.N);
+    if (!TOP && pieces <= 8) {
+        hipLaunchKernelGGL((logprob_row_kernel<T, 8, 1, false>), dim3((unsigned)((a.N + 31ll) / 32)), dim3(256), 0, st, a);
+        return;
+    }
+    if (pieces <= 64) hipLaunchKernelGGL((logprob_row_kernel<T, 64, 1, TOP>), rows, dim3(64), 0, st, a);
+    else if (pieces <= 256) hipLaunchKernelGGL((logprob_row_kernel<T, 64, 4, TOP>), rows, dim3(64), 0, st, a);
+    else if (pieces <= 512) hipLaunchKernelGGL((logprob_row_kernel<T, 256, 2, TOP>), rows, dim3(256), 0, st, a);
+    else if (pieces <= 1024) hipLaunchKernelGGL((logprob_row_kernel<T, 256, 4, TOP>), rows, dim3(256), 0, st, a);
+    else if (pieces <= 2048) hipLaunchKernelGGL((logprob_row_kernel<T, 256, 8, TOP>), rows, dim3(256), 0, st, a);
+    else if (pieces <= 4096) hipLaunchKernelGGL((logprob_row_kernel<T, 512, 8, TOP>), rows, dim3(512), 0, st, a);
+    else if (pieces <= 8192) hipLaunchKernelGGL((logprob_row_kernel<T, 512, 16, TOP>), rows, dim3(512), 0, st, a);
+    else hipLaunchKernelGGL((logprob_row_kernel<T, 1024, 16, TOP>), rows, dim3(1024), 0, st, a);
+}
+
+template <typename T>
+int launch(const LogprobArgs &a, void *workspace, hipStream_t st)
+{
+    const int per = chunk_pieces(a.N, a.K, a.dtype);
+    if (per == 0) {
+        if (a.top) launch_row<T, true>(a, st);
+        else launch_row<T, false>(a, st);
+        return hipGetLastError() == hipSuccess ? MXC_OK : MXC_ERR_LAUNCH;
+    }
+    const int chunks = chunk_count(a.K, a.dtype, per), span = CHUNK_THREADS * per * Piece<T>::V;
+    const size_t grid = (size_t)a.N * chunks;
+    if (grid > 0x7FFFFFFFu || (size_t)chunks * (a.top ? a.top : 1) > 0x7FFFFFFFu) return MXC_ERR_SHAPE;
+    Part *parts = (Part *)workspace;
+    unsigned long long *keys = (unsigned long long *)((char *)workspace + align_up(grid * sizeof(Part), 256));
+    const dim3 g((unsigned)grid), b(CHUNK_THREADS);
+    if (a.top && per == 1) hipLaunchKernelGGL((logprob_chunk_kernel<T, 1, true>), g, b, 0, st, a, chunks, parts, keys);
+    else if (a.top) hipLaunchKernelGGL((logprob_chunk_kernel<T, 8, true>), g, b, 0, st, a, chunks, parts, keys);
+    else if (per == 1) hipLaunchKernelGGL((logprob_chunk_kernel<T, 1, false>), g, b, 0, st, a, chunks, parts, keys);
+    else hipLaunchKernelGGL((logprob_chunk_kernel<T, 8, false>), g, b, 0, st, a, chunks, parts, keys);
+    if (hipGetLastError() != hipSuccess) return MXC_ERR_LAUNCH;
+    if (!a.dz) hipLaunchKernelGGL(logprob_join_kernel<T>, dim3((unsigned)a.N), dim3(256), 0, st, a, chunks, span, parts, keys);
+    else if (per == 1) hipLaunchKernelGGL((logprob_gradient_kernel<T, 1>), g, b, 0, st, a, chunks, span, parts);
+    else hipLaunchKernelGGL((logprob_gradient_kernel<T, 8>), g, b, 0, st, a, chunks, span, parts);
+    return hipGetLastError() == hipSuccess ? MXC_OK : MXC_ERR_LAUNCH;
+}
+
+template <typename T>
+int launch_bwd(const LogprobArgs &a, const float *stats, const float *entropy, hipStream_t st)
+{
+    const int per = row_pieces(a.K, a.dtype) <= CHUNK_THREADS ? 1 : 4, chunks = chunk_count(a.K, a.dtype, per);
+    const size_t grid = (size_t)a.N * chunks;
+    if (grid > 0x7FFFFFFFu) return MXC_ERR_SHAPE;
+    const dim3 g((unsigned)grid), b(CHUNK_THREADS);
+    if (per == 1) hipLaunchKernelGGL((logprob_bwd_kernel<T, 1>), g, b, 0, st, a, chunks, stats, entropy);
+    else hipLaunchKernelGGL((logprob_bwd_kernel<T, 4>), g, b, 0, st, a, chunks, stats, entropy);
+    return hipGetLastError() == hipSuccess ? MXC_OK : MXC_ERR_LAUNCH;
 }
 
 }  // namespace
 
-size_t logprob_workspace(int N, int K, int dtype, int top) { return 0; }
+size_t logprob_workspace(int N, int K, int dtype, int top)
+{
+    const int per = chunk_pieces(N, K, dtype);
+    if (per == 0) return 0;
+    const size_t grid = (size_t)N * chunk_count(K, dtype, per);
+    return align_up(grid * sizeof(Part), 256) + grid * top * sizeof(unsigned long long);
+}
 
 int logprob_rows(const LogprobArgs &a, void *workspace, hipStream_t st)
 {
-    if (a.dtype == MXC_BF16) hipLaunchKernelGGL(logprob_kernel<bf16_t>, dim3((unsigned)a.N), dim3(THREADS), 0, st, a);
-    else hipLaunchKernelGGL(logprob_kernel<float>, dim3((unsigned)a.N), dim3(THREADS), 0, st, a);
-    return hipGetLastError() == hipSuccess ? MXC_OK : MXC_ERR_LAUNCH;
+    return a.dtype == MXC_BF16 ? launch<bf16_t>(a, workspace, st) : launch<float>(a, workspace, st);
 }
 
 int logprob_bwd(const LogprobArgs &a, const float *stats, const float *entropy, hipStream_t st)
 {
-    if (a.dtype == MXC_BF16) hipLaunchKernelGGL(logprob_bwd_kernel<bf16_t>, dim3((unsigned)a.N), dim3(THREADS), 0, st, a, stats, entropy);
-    else hipLaunchKernelGGL(logprob_bwd_kernel<float>, dim3((unsigned)a.N), dim3(THREADS), 0, st, a, stats, entropy);
-    return hipGetLastError() == hipSuccess ? MXC_OK : MXC_ERR_LAUNCH;
+    return a.dtype == MXC_BF16 ? launch_bwd<bf16_t>(a, stats, entropy, st) : launch_bwd<float>(a, stats, entropy, st);
 }
 
 }  // namespace mxc
