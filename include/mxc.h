@@ -359,8 +359,10 @@ int mxc_logprob_fwd_bwd(int N, int K, int ld, int dtype, const void *z, const in
  * of `dtype`, w_codes and w_scales as above for K rows of C values, q(x) the values of mxc_mxfp4_quantize (the
  * input is brought into 4 bits within the call), products exact, sums in fp32 (their order depends on the sizes alone), one rounding to `dtype`.  bias
  * (fp32) may be NULL, relu is 0 or 1 (a NaN stays).  A NaN in q(x) or w makes NaN of the results of its row or column.  Places of w_codes past column C must hold 0
- * (their scales are read as they are: no infinity arises from them).  Workspace: mxc_mxfp4_fc_workspace_bytes.  Errors as above, and MXC_ERR_WORKSPACE.
+ * (their scales are read as they are: no infinity arises from them).  Workspace: mxc_mxfp4_fc_workspace_bytes.  Errors as above (MXC_ERR_SHAPE also for C above
+ * MXC_MXFP4_FC_MAX_C), and MXC_ERR_WORKSPACE.
  */
+enum { MXC_MXFP4_FC_MAX_C = 1 << 23 };
 int mxc_mxfp4_quantize(int N, int C, int dtype, const void *x, void *codes, void *scales, void *hip_stream);
 int mxc_mxfp4_dequantize(int N, int C, int dtype, const void *codes, const void *scales, void *y, void *hip_stream);
 int mxc_mxfp4_fc_workspace_bytes(int N, int C, int K, int dtype, size_t *out_bytes);

@@ -1114,6 +1114,7 @@ int mxc_mxfp4_fc_workspace_bytes(int N, int C, int K, int dtype, size_t *out_byt
 {
     if (!out_bytes) return MXC_ERR_NULL;
     MXC_TRY(mxfp4_check(N, C, K, dtype));
+    if (C > MXC_MXFP4_FC_MAX_C) return MXC_ERR_SHAPE;
     *out_bytes = align_up(mxfp4_fc_workspace(N, C, K, dtype), 256);
     return MXC_OK;
 }
@@ -1122,6 +1123,7 @@ int mxc_mxfp4_fc_fwd(int N, int C, int K, int dtype, const void *x, const void *
                      const float *bias, int relu, void *y, void *workspace, size_t workspace_bytes, void *hip_stream)
 {
     MXC_TRY(mxfp4_check(N, C, K, dtype));
+    if (C > MXC_MXFP4_FC_MAX_C) return MXC_ERR_SHAPE;
     if (relu != 0 && relu != 1) return MXC_ERR_UNSUPPORTED;
     if (!x || !w_codes || !w_scales || !y) return MXC_ERR_NULL;
     if (misaligned(x) || misaligned(w_codes) || misaligned(w_scales) || misaligned(y) || misaligned(workspace) || misaligned4(bias)) return MXC_ERR_ALIGN;

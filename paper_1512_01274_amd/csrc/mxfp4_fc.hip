@@ -1,74 +1,505 @@
-// FullyConnected on a filter in microscaled 4-bit floating point.
+// FullyConnected on a filter in microscaled 4-bit floating point: y[n][k] = act( sum_c q(x)[n][c]*w[k][c] + bias[k] ).
+// The matrix instructions take 4-bit operands as they are, 32 values of a row and their scale byte in each lane, multiply and add
+// them in fp32.  The product is formed transposed (filter rows first), so that a lane holds four neighbouring columns of y.
+// Which columns meet in one instruction is free as long as both operands agree; every kernel below uses this to let a lane
+// read neighbouring bytes.
+//   token:  N <= 16.  One launch: every wave quantises the part of x that it multiplies.
+//   skinny: x is quantised once, then workgroups of eight waves that share out the columns.
+//   tiled:  x quantised, both operands' scales brought into the order of the tiles, and tiles of LDS that a ring of loads fills.
+#include <type_traits>
+
 #include "mxfp4.h"
 
 namespace mxc {
 namespace {
 
-__device__ __forceinline__ float e2m1_value(unsigned code)
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+__device__ __forceinline__ i32x8 operand(uint4 u) { return i32x8{(int)u.x, (int)u.y, (int)u.z, (int)u.w, 0, 0, 0, 0}; }
+constexpr int FP4 = 4;      // the instructions' code for the operands' format
+
+// byte J of the scale words belongs to these operands
+template <int J, int L>
+__device__ __forceinline__ f32x4 mfma16(uint4 a, uint4 b, f32x4 c, int sa, int sb)
 {
-    const unsigned m = code & 1u, e = (code >> 1) & 3u;
-    const float v = e ? __uint_as_float(((e + 126u) << 23) | (m << 22)) : 0.5f * (float)m;
-    return code & 8u ? -v : v;
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(a), operand(b), c, FP4, FP4, J, sa, L, sb);
+}
+template <int J>
+__device__ __forceinline__ f32x16 mfma32(uint4 a, uint4 b, f32x16 c, int sa, int sb)
+{
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(a), operand(b), c, FP4, FP4, J, sa, J, sb);
 }
 
-// simplest product: 16x16 outputs a workgroup, one block of 32 columns decoded into LDS at a time
 template <typename T>
-__global__ __launch_bounds__(256) void mxfp4_fc_kernel(int N, int C, int K, int blocks, int scale_row, const unsigned char *xc, const unsigned char *xs,
-                                                       const unsigned char *wc, const unsigned char *ws, const float *bias, int relu, T *y)
+__device__ __forceinline__ void store_one(T *y, float v)
 {
-    __shared__ float a[16][33], b[16][33];
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    const long long n0 = (long long)blockIdx.y * 16, k0 = (long long)blockIdx.x * 16;
-    float sum = 0.f;
-    for (int blk = 0; blk < blocks; ++blk) {
-        __syncthreads();
-        // thread (ty, tx): row ty of either tile, byte tx of the block
-        for (int side = 0; side < 2; ++side) {
-            const long long row = (side ? k0 : n0) + ty;
-            float lo = 0.f, hi = 0.f;
-            if (row < (side ? K : N)) {
-                const unsigned char c = (side ? wc : xc)[((size_t)row * blocks + blk) * 16 + tx];
-                const float sc = e8m0_value((side ? ws : xs)[(size_t)row * scale_row + blk]);
-                lo = e2m1_value(c & 15u) * sc;
-                hi = e2m1_value(c >> 4) * sc;
-            }
-            (side ? b : a)[ty][2 * tx] = lo;
-            (side ? b : a)[ty][2 * tx + 1] = hi;
+    if constexpr (sizeof(T) == 2) *y = (bf16_t)pack_bf16x2(v, v);
+    else *y = v;
+}
+__device__ __forceinline__ float activated(float v, const float *bias, long long k, int relu)
+{
+    if (bias) v += bias[k];
+    return relu && v < 0.f ? 0.f : v;
+}
+
+// ---- up to 16 rows of x ---------------------------------------------------------------------------------------------------
+// 16 filter rows a workgroup; its eight waves take every eighth group of 512 columns, a lane 128 neighbouring ones of them: 64 bytes of
+// codes, a word of scales.  Lane l holds filter row l%16 and row l%16 of x, which it quantises itself.
+constexpr int TOKEN_WAVES = 8;
+
+struct TokenGroup {
+    uint4 w[4];
+    int scale;
+};
+__device__ __forceinline__ TokenGroup load_filter(const unsigned char *wc, const unsigned char *ws, int group, int quarter, int blocks)
+{
+    TokenGroup g;
+    const int b = group * 16 + quarter * 4;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) g.w[j] = b + j < blocks ? *reinterpret_cast<const uint4 *>(wc + (size_t)(b + j) * 16) : make_uint4(0, 0, 0, 0);
+    g.scale = *reinterpret_cast<const int *>(ws + b);
+    return g;
+}
+
+template <int J, typename T>
+__device__ __forceinline__ f32x4 token_step(const T *x, int column, int C, bool live, const TokenGroup &g, f32x4 acc)
+{
+    uint4 codes = make_uint4(0, 0, 0, 0);
+    unsigned byte = 0;
+    const int left = C - column - J * 32;
+    if (live && left > 0) {
+        float v[4][8];
+        unsigned most = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            load8_edge(x + column + J * 32 + k * 8, left - k * 8, v[k]);
+            most = max(most, largest8(v[k]));
         }
-        __syncthreads();
-        for (int c = 0; c < 32; ++c) sum += a[ty][c] * b[tx][c];
+        byte = mxfp4_scale_byte(most);
+        codes = make_uint4(mxfp4_codes8(v[0], byte), mxfp4_codes8(v[1], byte), mxfp4_codes8(v[2], byte), mxfp4_codes8(v[3], byte));
     }
-    const long long n = n0 + ty, k = k0 + tx;
-    if (n >= N || k >= K) return;
-    if (bias) sum += bias[k];
-    if (relu && sum < 0.f) sum = 0.f;
-    if constexpr (sizeof(T) == 2) y[(size_t)n * K + k] = (bf16_t)pack_bf16x2(sum, sum);
-    else y[(size_t)n * K + k] = sum;
+    return mfma16<J, 0>(g.w[J], codes, acc, g.scale, (int)byte);
+}
+
+template <typename T>
+__global__ __launch_bounds__(64 * TOKEN_WAVES) void mxfp4_token_kernel(int N, int C, int K, int blocks, int scale_row, const T *x, const unsigned char *wc,
+                                                                       const unsigned char *ws, const float *bias, int relu, T *y)
+{
+    __shared__ f32x4 part[TOKEN_WAVES][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, quarter = lane >> 4;
+    const long long k0 = (long long)blockIdx.x * 16;
+    const long long k = k0 + r < K ? k0 + r : K - 1;
+    wc += (size_t)k * blocks * 16;
+    ws += (size_t)k * scale_row;
+    const bool live = r < N;
+    x += (size_t)(live ? r : 0) * C;
+    const int groups = scale_row / 16;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    TokenGroup next;
+    if (wave < groups) next = load_filter(wc, ws, wave, quarter, blocks);
+    for (int group = wave; group < groups; group += TOKEN_WAVES) {
+        const TokenGroup g = next;
+        if (group + TOKEN_WAVES < groups) next = load_filter(wc, ws, group + TOKEN_WAVES, quarter, blocks);
+        const int column = group * 512 + quarter * 128;
+        acc = token_step<0>(x, column, C, live, g, acc);
+        acc = token_step<1>(x, column, C, live, g, acc);
+        acc = token_step<2>(x, column, C, live, g, acc);
+        acc = token_step<3>(x, column, C, live, g, acc);
+    }
+    part[wave][lane] = acc;
+    __syncthreads();
+    // thread t: column t/16 of the tile's sixteen, row t%16 of x
+    const int t = threadIdx.x;
+    const int n = t & 15, kk = t >> 4;
+    if (t >= 256 || n >= N || k0 + kk >= K) return;
+    const float *p = reinterpret_cast<const float *>(&part[0][(kk >> 2) * 16 + n]) + (kk & 3);
+    float sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < TOKEN_WAVES; ++w) sum += p[w * 256];
+    store_one(y + (size_t)n * K + k0 + kk, activated(sum, bias, k0 + kk, relu));
+}
+
+// ---- some rows of x -------------------------------------------------------------------------------------------------------
+// 16*WF filter rows and 16*NF rows of x a workgroup, both straight from the caches into registers; the waves' sums meet in LDS.
+template <int WF, int NF>
+struct SkinnyStep {
+    uint4 w[WF], x[NF];
+};
+
+template <typename T, int WF, int NF>
+__global__ __launch_bounds__(512) void mxfp4_skinny_kernel(int N, int K, int blocks, int scale_row, const unsigned char *xc, const unsigned char *xs,
+                                                           const unsigned char *wc, const unsigned char *ws, const float *bias, int relu, T *y)
+{
+    constexpr int WAVES = 8, BM = 16 * WF, BN = 16 * NF;
+    __shared__ f32x4 part[WAVES][WF * NF][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, quarter = lane >> 4;
+    const long long k0 = (long long)blockIdx.x * BM, n0 = (long long)blockIdx.y * BN;
+    // offsets from the tiles' first rows, which are less than 2 GB (C <= MXC_MXFP4_FC_MAX_C, at most 128 rows)
+    const unsigned code_row = (unsigned)blocks * 16u;
+    wc += (size_t)k0 * code_row;
+    ws += (size_t)k0 * scale_row;
+    xc += (size_t)n0 * code_row;
+    xs += (size_t)n0 * scale_row;
+    unsigned w_row[WF], x_row[NF];
+#pragma unroll
+    for (int i = 0; i < WF; ++i) w_row[i] = (unsigned)(k0 + i * 16 + r < K ? i * 16 + r : K - 1 - k0);
+#pragma unroll
+    for (int i = 0; i < NF; ++i) x_row[i] = (unsigned)(n0 + i * 16 + r < N ? i * 16 + r : N - 1 - n0);
+    f32x4 acc[WF][NF] = {};
+    auto load = [&](int group, int j) {
+        SkinnyStep<WF, NF> s;
+        const int b = group * 16 + quarter * 4 + j;
+        const bool in = b < blocks;
+        const unsigned at = (unsigned)b * 16u;
+#pragma unroll
+        for (int i = 0; i < WF; ++i) s.w[i] = in ? *reinterpret_cast<const uint4 *>(wc + (w_row[i] * code_row + at)) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < NF; ++i) s.x[i] = in ? *reinterpret_cast<const uint4 *>(xc + (x_row[i] * code_row + at)) : make_uint4(0, 0, 0, 0);
+        return s;
+    };
+    int sw[WF], sx[NF];
+    auto multiply = [&](auto j, const SkinnyStep<WF, NF> &s) {
+#pragma unroll
+        for (int i = 0; i < WF; ++i)
+#pragma unroll
+            for (int q = 0; q < NF; ++q) acc[i][q] = mfma16<decltype(j)::value, decltype(j)::value>(s.w[i], s.x[q], acc[i][q], sw[i], sx[q]);
+    };
+    const int groups = scale_row / 16;
+    if (wave < groups) {
+        SkinnyStep<WF, NF> a = load(wave, 0), b;
+        for (int group = wave; group < groups; group += WAVES) {
+#pragma unroll
+            for (int i = 0; i < WF; ++i) sw[i] = *reinterpret_cast<const int *>(ws + (w_row[i] * (unsigned)scale_row + (unsigned)(group * 16 + quarter * 4)));
+#pragma unroll
+            for (int i = 0; i < NF; ++i) sx[i] = *reinterpret_cast<const int *>(xs + (x_row[i] * (unsigned)scale_row + (unsigned)(group * 16 + quarter * 4)));
+            b = load(group, 1);
+            multiply(std::integral_constant<int, 0>(), a);
+            a = load(group, 2);
+            multiply(std::integral_constant<int, 1>(), b);
+            b = load(group, 3);
+            multiply(std::integral_constant<int, 2>(), a);
+            const int next = group + WAVES < groups ? group + WAVES : group;
+            a = load(next, 0);
+            multiply(std::integral_constant<int, 3>(), b);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < WF; ++i)
+#pragma unroll
+        for (int q = 0; q < NF; ++q) part[wave][i * NF + q][lane] = acc[i][q];
+    __syncthreads();
+    // a thread: four neighbouring columns of a row, in ascending order of waves
+    for (int u = threadIdx.x; u < WF * NF * 64; u += 512) {
+        const int f = u >> 6, l = u & 63;
+        f32x4 v = part[0][f][l];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) v += part[w][f][l];
+        const long long k = k0 + (f / NF) * 16 + (l >> 4) * 4, n = n0 + (f % NF) * 16 + (l & 15);
+        if (n >= N) continue;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (k + e < K) store_one(y + (size_t)n * K + k + e, activated(v[e], bias, k + e, relu));
+    }
+}
+
+// ---- many rows of x -------------------------------------------------------------------------------------------------------
+// Scales in the tiles' order: for 32 rows and 256 columns one word a lane, lane l: row l%32 and of the 8 blocks those of l/32's parity.
+// [group of 256 columns][32 rows][64 lanes] words.
+__device__ __forceinline__ unsigned pick_scales(uint2 s, int odd)
+{
+    return odd ? (s.x >> 8 & 255u) | (s.x >> 24) << 8 | (s.y >> 8 & 255u) << 16 | (s.y >> 24) << 24
+               : (s.x & 255u) | (s.x >> 16 & 255u) << 8 | (s.y & 255u) << 16 | (s.y >> 16 & 255u) << 24;
+}
+
+// Prepares both operands in one launch.  Workgroups up to `x_groups`: x, 32 rows and 256 columns each, a block of 32 values a thread;
+// the others: the filter's scales, 32 rows and 8 groups.
+template <typename T>
+__global__ __launch_bounds__(256) void mxfp4_prepare_kernel(int N, int C, int K, int blocks, int scale_row, int groups, unsigned x_groups, const T *x,
+                                                            unsigned char *xc, unsigned *xs, const unsigned char *ws, unsigned *wt)
+{
+    const int row = threadIdx.x >> 3, at = threadIdx.x & 7;
+    if (blockIdx.x >= x_groups) {
+        const unsigned i = blockIdx.x - x_groups, eights = (unsigned)(groups + 7) / 8;
+        const int group = (int)(i % eights) * 8 + at;
+        const long long tile = i / eights, k = tile * 32 + row, tiles = (K + 31ll) / 32;
+        if (group >= groups) return;
+        uint2 s = make_uint2(0, 0);
+        if (k < K) s = *reinterpret_cast<const uint2 *>(ws + (size_t)k * scale_row + group * 8);
+        unsigned *out = wt + ((size_t)group * tiles + tile) * 64 + row;
+        out[0] = pick_scales(s, 0);
+        out[32] = pick_scales(s, 1);
+        return;
+    }
+    __shared__ unsigned char bytes[32][8];
+    const int group = (int)(blockIdx.x % (unsigned)groups);
+    const long long tile = blockIdx.x / (unsigned)groups, n = tile * 32 + row, tiles = (N + 31ll) / 32;
+    const int b = group * 8 + at, left = C - b * 32;
+    unsigned byte = 0;
+    if (n < N && b < blocks) {
+        float v[4][8];
+        unsigned most = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            load8_edge(x + (size_t)n * C + b * 32 + k * 8, left - k * 8, v[k]);
+            most = max(most, largest8(v[k]));
+        }
+        byte = mxfp4_scale_byte(most);
+        *reinterpret_cast<uint4 *>(xc + ((size_t)n * blocks + b) * 16) =
+            make_uint4(mxfp4_codes8(v[0], byte), mxfp4_codes8(v[1], byte), mxfp4_codes8(v[2], byte), mxfp4_codes8(v[3], byte));
+    }
+    bytes[row][at] = (unsigned char)byte;
+    __syncthreads();
+    if (threadIdx.x < 64) {
+        const uint2 s = *reinterpret_cast<const uint2 *>(bytes[threadIdx.x & 31]);
+        xs[((size_t)group * tiles + tile) * 64 + threadIdx.x] = pick_scales(s, threadIdx.x >> 5);
+    }
+}
+
+// Tile of 64*FM filter rows and 64*FN rows of x; four waves, two by two, of 32*FM x 32*FN.  A stage is 128 columns, 64 bytes of codes a
+// row, brought into a ring of four stages by direct loads; scales come a word for two stages.  Row r's 16-byte chunk c lies at place
+// c ^ (r/4)%4, so that the 16 rows that one phase of a 16-byte read covers lie in all 64 banks once.
+// One barrier a stage, between the last operand fetch of the stage and its last product: the fetches of the next stage and the
+// loads of the one after three more go between the products.
+template <int FM, int FN>
+struct Tile {
+    static constexpr int BM = 64 * FM, BN = 64 * FN;
+    static constexpr int STAGE = (BM + BN) * 64, RING = 4;
+    static constexpr int SCALES = (BM + BN) * 8 < 4096 ? 4096 : (BM + BN) * 8;      // bytes of scales of two stages (room for a kilobyte of each wave)
+    static constexpr int LDS = RING * STAGE + 4 * SCALES;
+    static constexpr int LOADS = FM + FN;       // of 1 KB, each wave's, a stage
+};
+
+template <typename T, int FM, int FN>
+__global__ __launch_bounds__(256, 1) void mxfp4_tile_kernel(int N, int K, int code_row, int groups, const unsigned char *xc, const unsigned *xs,
+                                                            const unsigned char *wc, const unsigned *wt, const float *bias, int relu, T *y, int k_tiles, int n_tiles)
+{
+    typedef Tile<FM, FN> G;
+    __shared__ __align__(16) unsigned char lds[G::LDS];
+    unsigned char *ring = lds, *scales = lds + G::RING * G::STAGE;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave & 1, wn = wave >> 1, half = lane >> 5;
+
+    // Each XCD works on neighbouring tiles: groups of 8 filter tiles by all tiles of x, the filter's fastest.
+    const unsigned total = (unsigned)k_tiles * (unsigned)n_tiles, per = total / 8, rest = total % 8, xcd = blockIdx.x % 8, in_xcd = blockIdx.x / 8;
+    const unsigned id = xcd * per + (xcd < rest ? xcd : rest) + in_xcd;
+    const unsigned band = id / (8u * (unsigned)n_tiles), first = band * 8u, width = min(8u, (unsigned)k_tiles - first), in_band = id - band * 8u * (unsigned)n_tiles;
+    const long long k0 = (long long)(first + in_band % width) * G::BM, n0 = (long long)(in_band / width) * G::BN;
+
+    // sources: this tile's rows (what lies outside reads as zeros)
+    const int k_rows = (int)(K - k0 < G::BM ? K - k0 : G::BM), n_rows = (int)(N - n0 < G::BN ? N - n0 : G::BN);
+    const buf_rsrc_t rs_w = make_buf_rsrc(wc + (size_t)k0 * code_row, (unsigned)k_rows * (unsigned)code_row);
+    const buf_rsrc_t rs_x = make_buf_rsrc(xc + (size_t)n0 * code_row, (unsigned)n_rows * (unsigned)code_row);
+    // a kilobyte of scales is 128 rows: wave w brings part w of the filter's, then of x's
+    constexpr int WS = G::BM / 128, XS = G::BN / 128;
+    const long long w32 = (K + 31ll) / 32, x32 = (N + 31ll) / 32;
+    const bool of_w = wave < WS, of_any = wave < WS + XS;
+    const unsigned *s_base = of_w ? wt + (k0 / 32 + wave * 4) * 64 : xs + (n0 / 32 + (wave - WS) * 4) * 64;
+    const long long s_tiles = of_w ? w32 - (k0 / 32 + wave * 4) : x32 - (n0 / 32 + (wave - WS) * 4);        // that are left
+    const unsigned s_pitch = (unsigned)(of_w ? w32 : x32) * 256u;
+    const unsigned s_bytes = !of_any || s_tiles <= 0 ? 0u : (unsigned)min(s_tiles, 4ll) * 256u;
+
+    const int stages = (code_row + 63) / 64;
+    const int chunk = (lane & 3) ^ ((lane >> 4) & 3);
+    unsigned src[G::LOADS];
+#pragma unroll
+    for (int i = 0; i < G::LOADS; ++i) {
+        const int row = (i < FM ? wave * FM + i : wave * FN + i - FM) * 16 + (lane >> 2);
+        src[i] = (unsigned)row * (unsigned)code_row + chunk * 16;
+    }
+    auto issue_codes = [&](int stage, int i) {       // load i of a stage: FM of filter rows, then FN of rows of x
+        const unsigned column = (unsigned)stage * 64u;
+        const unsigned off = (int)(column + chunk * 16) < code_row ? src[i] + column : 0x80000000u;
+        unsigned char *to = ring + (stage & 3) * G::STAGE;
+        if (i < FM) lds_dma16(rs_w, off, to + (wave * FM + i) * 1024);
+        else lds_dma16(rs_x, off, to + G::BM * 64 + (wave * FN + i - FM) * 1024);
+    };
+    auto issue_scales = [&](int stage) {             // of stages `stage` (even) and the next
+        const int group = stage >> 1;
+        const buf_rsrc_t rs = make_buf_rsrc((const unsigned char *)s_base + (size_t)(group < groups ? group : 0) * s_pitch, group < groups ? s_bytes : 0u);
+        lds_dma16(rs, (unsigned)lane * 16u, scales + (group & 3) * G::SCALES + wave * 1024);
+    };
+
+    f32x16 acc[FM][FN] = {};
+    uint4 w[2][FM], x[2][FN];
+    int sw[FM], sx[FN];
+    // operand addresses of the first half of a stage; the second's are 32 bytes away, one way or the other
+    const int swz = (lane >> 2) & 3;
+    const int w_at = (wm * 32 * FM + (lane & 31)) * 64, x_at = (G::BM + wn * 32 * FN + (lane & 31)) * 64;
+    auto fetch_w = [&](int stage, int s, int i) { return *reinterpret_cast<const uint4 *>(ring + (stage & 3) * G::STAGE + w_at + i * 2048 + ((2 * s + half) ^ swz) * 16); };
+    auto fetch_x = [&](int stage, int s, int i) { return *reinterpret_cast<const uint4 *>(ring + (stage & 3) * G::STAGE + x_at + i * 2048 + ((2 * s + half) ^ swz) * 16); };
+    auto fetch_sw = [&](int group, int i) { return *reinterpret_cast<const int *>(scales + (group & 3) * G::SCALES + (wm * FM + i) * 256 + lane * 4); };
+    auto fetch_sx = [&](int group, int i) { return *reinterpret_cast<const int *>(scales + (group & 3) * G::SCALES + G::BM * 8 + (wn * FN + i) * 256 + lane * 4); };
+
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        if (t % 2 == 0) issue_scales(t);
+#pragma unroll
+        for (int i = 0; i < G::LOADS; ++i) issue_codes(t, i);
+    }
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" : : "n"(3 * G::LOADS + 1) : "memory");
+#pragma unroll
+    for (int i = 0; i < FM; ++i) { w[0][i] = fetch_w(0, 0, i); sw[i] = fetch_sw(0, i); }
+#pragma unroll
+    for (int i = 0; i < FN; ++i) { x[0][i] = fetch_x(0, 0, i); sx[i] = fetch_sx(0, i); }
+
+    // products of half S of a stage (byte B of the scales), and between them fetch(i), i < FM*FN
+    auto products = [&](auto B, int s, auto fetch) {
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j) {
+                acc[i][j] = mfma32<decltype(B)::value>(w[s][i], x[s][j], acc[i][j], sw[i], sx[j]);
+                fetch(i * FN + j);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+    };
+    int nsw[FM], nsx[FN];
+    auto stage_of = [&](int t, auto odd) {
+        constexpr int ODD = decltype(odd)::value;
+        products(std::integral_constant<int, 2 * ODD>(), 0, [&](int u) {
+            if (u < FM) w[1][u < FM ? u : 0] = fetch_w(t, 1, u);
+            else if (u < FM + FN) x[1][u < FM ? 0 : u - FM < FN ? u - FM : 0] = fetch_x(t, 1, u - FM);
+        });
+        // the next stage has landed (those after it, two of codes and one of scales, may be under way), and no wave reads this one any more
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(2 * G::LOADS + 1) : "memory");
+        products(std::integral_constant<int, 2 * ODD + 1>(), 1, [&](int u) {
+            if (u < FM) w[0][u < FM ? u : 0] = fetch_w(t + 1, 0, u);
+            else if (u < FM + FN) x[0][u < FM ? 0 : u - FM < FN ? u - FM : 0] = fetch_x(t + 1, 0, u - FM);
+            if (ODD) {
+                if (u < FM) nsw[u < FM ? u : 0] = fetch_sw((t + 1) >> 1, u);
+                else if (u < FM + FN) nsx[u < FM ? 0 : u - FM < FN ? u - FM : 0] = fetch_sx((t + 1) >> 1, u - FM);
+            }
+            if (u < G::LOADS) {
+                if (u == 0 && !ODD) issue_scales(t + 4);
+                issue_codes(t + 4, u);
+            }
+        });
+    };
+    static_assert(FM + FN <= FM * FN && G::LOADS <= FM * FN, "room between the products");
+    for (int t = 0; t < stages; t += 2) {
+        stage_of(t, std::integral_constant<int, 0>());
+        stage_of(t + 1, std::integral_constant<int, 1>());
+#pragma unroll
+        for (int i = 0; i < FM; ++i) sw[i] = nsw[i];
+#pragma unroll
+        for (int i = 0; i < FN; ++i) sx[i] = nsx[i];
+    }
+    asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const long long k = k0 + wm * 32 * FM + i * 32 + g * 8 + half * 4;
+            f32x4 b = {0.f, 0.f, 0.f, 0.f};
+            if (bias) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (k + e < K) b[e] = bias[k + e];
+            }
+#pragma unroll
+            for (int j = 0; j < FN; ++j) {
+                const long long n = n0 + wn * 32 * FN + j * 32 + (lane & 31);
+                if (n >= N) continue;
+                T *to = y + (size_t)n * K + k;
+                float v[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    v[e] = acc[i][j][g * 4 + e] + b[e];
+                    if (relu && v[e] < 0.f) v[e] = 0.f;
+                }
+                if (K % 4 == 0) {
+                    if (k >= K) continue;
+                    if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2 *>(to) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+                    else *reinterpret_cast<float4 *>(to) = make_float4(v[0], v[1], v[2], v[3]);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (k + e < K) store_one(to + e, v[e]);
+                }
+            }
+        }
+}
+
+// ---- host -----------------------------------------------------------------------------------------------------------------
+
+enum Path { TOKEN, SKINNY, TILED };
+Path path_of(int N, int C, int K)
+{
+    if (N <= 16) return TOKEN;
+    return N <= 128 ? SKINNY : TILED;
+}
+
+struct Buffers {        // of the workspace
+    size_t codes = 0, scales = 0, filter_scales = 0, total = 0;     // offsets of the last two, and the whole
+};
+Buffers buffers(int N, int C, int K)
+{
+    Buffers b;
+    const Path path = path_of(N, C, K);
+    if (path == TOKEN) return b;
+    const size_t groups = ((size_t)C + 255) / 256;
+    b.scales = align_up((size_t)N * mxfp4_code_row(C), 256);
+    b.filter_scales = b.scales + (path == SKINNY ? align_up((size_t)N * mxfp4_scale_row(C), 256) : ((size_t)N + 31) / 32 * groups * 256);
+    b.total = b.filter_scales + (path == SKINNY ? 0 : ((size_t)K + 31) / 32 * groups * 256);
+    return b;
+}
+
+template <typename T, int FM, int FN>
+int launch_tiles(int N, int C, int K, const unsigned char *xc, const unsigned *xs, const unsigned char *wc, const unsigned *wt, const float *bias, int relu, T *y,
+                 hipStream_t st)
+{
+    typedef Tile<FM, FN> G;
+    const long long kt = (K + G::BM - 1ll) / G::BM, nt = (N + G::BN - 1ll) / G::BN;
+    if (kt * nt > 0x7FFFFFFFll / 8) return MXC_ERR_SHAPE;
+    hipLaunchKernelGGL((mxfp4_tile_kernel<T, FM, FN>), dim3((unsigned)(kt * nt)), dim3(256), 0, st, N, K, (int)mxfp4_code_row(C), (int)(((long long)C + 255) / 256), xc, xs,
+                       wc, wt, bias, relu, y, (int)kt, (int)nt);
+    return MXC_OK;
+}
+
+template <typename T>
+int fc(int N, int C, int K, const T *x, const unsigned char *wc, const unsigned char *ws, const float *bias, int relu, T *y, void *workspace, hipStream_t st)
+{
+    const int blocks = (int)(mxfp4_code_row(C) / 16), scale_row = (int)mxfp4_scale_row(C);
+    const Path path = path_of(N, C, K);
+    if (path == TOKEN) {
+        hipLaunchKernelGGL(mxfp4_token_kernel<T>, dim3((unsigned)((K + 15ll) / 16)), dim3(64 * TOKEN_WAVES), 0, st, N, C, K, blocks, scale_row, x, wc, ws, bias, relu, y);
+        return hipGetLastError() == hipSuccess ? MXC_OK : MXC_ERR_LAUNCH;
+    }
+    const Buffers b = buffers(N, C, K);
+    unsigned char *xc = (unsigned char *)workspace, *xs = xc + b.scales;
+    if (path == SKINNY) {
+        const int rc = mxfp4_quantize(N, C, sizeof(T) == 2 ? MXC_BF16 : MXC_F32, x, xc, xs, st);
+        if (rc != MXC_OK) return rc;
+        const dim3 block(512);
+        if (N <= 32) hipLaunchKernelGGL((mxfp4_skinny_kernel<T, 1, 2>), dim3((unsigned)((K + 15ll) / 16)), block, 0, st, N, K, blocks, scale_row, xc, xs, wc, ws, bias, relu, y);
+        else if (N <= 64) hipLaunchKernelGGL((mxfp4_skinny_kernel<T, 1, 4>), dim3((unsigned)((K + 15ll) / 16)), block, 0, st, N, K, blocks, scale_row, xc, xs, wc, ws, bias, relu, y);
+        else hipLaunchKernelGGL((mxfp4_skinny_kernel<T, 1, 8>), dim3((unsigned)((K + 15ll) / 16)), block, 0, st, N, K, blocks, scale_row, xc, xs, wc, ws, bias, relu, y);
+        return hipGetLastError() == hipSuccess ? MXC_OK : MXC_ERR_LAUNCH;
+    }
+    const int groups = (int)(((long long)C + 255) / 256);
+    unsigned *xt = (unsigned *)xs, *wt = (unsigned *)((unsigned char *)workspace + b.filter_scales);
+    const size_t x_groups = ((size_t)N + 31) / 32 * groups, w_groups = ((size_t)K + 31) / 32 * ((groups + 7) / 8);
+    if (x_groups + w_groups > 0x7FFFFFFFu) return MXC_ERR_SHAPE;
+    hipLaunchKernelGGL(mxfp4_prepare_kernel<T>, dim3((unsigned)(x_groups + w_groups)), dim3(256), 0, st, N, C, K, blocks, scale_row, groups, (unsigned)x_groups, x, xc, xt, ws, wt);
+    if (hipGetLastError() != hipSuccess) return MXC_ERR_LAUNCH;
+    const long long big = ((K + 255ll) / 256) * ((N + 255ll) / 256);
+    const int rc = big >= 192 ? launch_tiles<T, 4, 4>(N, C, K, xc, xt, wc, wt, bias, relu, y, st) : launch_tiles<T, 2, 2>(N, C, K, xc, xt, wc, wt, bias, relu, y, st);
+    if (rc != MXC_OK) return rc;
+    return hipGetLastError() == hipSuccess ? MXC_OK : MXC_ERR_LAUNCH;
 }
 
 }  // namespace
 
-size_t mxfp4_fc_workspace(int N, int C, int K, int dtype)
-{
-    return align_up((size_t)N * mxfp4_code_row(C), 256) + align_up((size_t)N * mxfp4_scale_row(C), 256);
-}
+size_t mxfp4_fc_workspace(int N, int C, int K, int dtype) { return buffers(N, C, K).total; }
 
 int mxfp4_fc(int N, int C, int K, int dtype, const void *x, const void *w_codes, const void *w_scales, const float *bias, int relu, void *y,
              void *workspace, hipStream_t st)
 {
-    const int blocks = (int)(mxfp4_code_row(C) / 16), scale_row = (int)mxfp4_scale_row(C);
-    unsigned char *xc = (unsigned char *)workspace, *xs = xc + align_up((size_t)N * mxfp4_code_row(C), 256);
-    const int rc = mxfp4_quantize(N, C, dtype, x, xc, xs, st);
-    if (rc != MXC_OK) return rc;
-    const unsigned gx = (unsigned)((K + 15ll) / 16), gy = (unsigned)((N + 15ll) / 16);
-    if (gy > 65535u) return MXC_ERR_SHAPE;
-    if (dtype == MXC_BF16)
-        hipLaunchKernelGGL(mxfp4_fc_kernel<bf16_t>, dim3(gx, gy), dim3(256), 0, st, N, C, K, blocks, scale_row, xc, xs, (const unsigned char *)w_codes,
-                           (const unsigned char *)w_scales, bias, relu, (bf16_t *)y);
-    else
-        hipLaunchKernelGGL(mxfp4_fc_kernel<float>, dim3(gx, gy), dim3(256), 0, st, N, C, K, blocks, scale_row, xc, xs, (const unsigned char *)w_codes,
-                           (const unsigned char *)w_scales, bias, relu, (float *)y);
-    return hipGetLastError() == hipSuccess ? MXC_OK : MXC_ERR_LAUNCH;
+    const unsigned char *wc = (const unsigned char *)w_codes, *ws = (const unsigned char *)w_scales;
+    return dtype == MXC_BF16 ? fc<bf16_t>(N, C, K, (const bf16_t *)x, wc, ws, bias, relu, (bf16_t *)y, workspace, st)
+                             : fc<float>(N, C, K, (const float *)x, wc, ws, bias, relu, (float *)y, workspace, st);
 }
 
 }  // namespace mxc
