@@ -41,6 +41,13 @@ __device__ __forceinline__ float max3(float a, float b, float c)
     return r;
 }
 
+__device__ __forceinline__ float min3(float a, float b, float c)
+{
+    float r;
+    asm("v_min3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+
 template <typename T>
 struct Piece {      // 16 bytes of a row
     static constexpr int V = 16 / (int)sizeof(T);
@@ -75,11 +82,92 @@ struct Piece {      // 16 bytes of a row
         const float last = v(V - 1);
         return max3(m, last, last);
     }
+    // minus infinities become `value`
+    __device__ __forceinline__ void refill(float value)
+    {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if constexpr (V == 8) {
+                const uint32_t v = __float_as_uint(value) >> 16;
+                if ((w[k] & 0xFFFFu) == 0xFF80u) w[k] = (w[k] & 0xFFFF0000u) | v;
+                if (w[k] >> 16 == 0xFF80u) w[k] = (w[k] & 0xFFFFu) | (v << 16);
+            } else if (w[k] == 0xFF800000u)
+                w[k] = __float_as_uint(value);
+        }
+    }
     __device__ __forceinline__ void nothing()      // minus infinities: no weight in any sum
     {
 #pragma unroll
         for (int k = 0; k < 4; ++k) w[k] = V == 8 ? 0xFF80FF80u : 0xFF800000u;
     }
+};
+
+// What the first look at a row finds: its largest and its lowest value.  bf16 words are looked at as
+// pairs of 16-bit integers, two values an instruction: of signed ones the largest is the largest value unless all are negative (then it
+// is some value; `sure` is false), of unsigned ones the largest is the most negative value where there is one.  fp32 values are looked at as they are.
+template <typename T>
+struct Extent;
+template <>
+struct Extent<bf16_t> {
+    typedef short i16x2 __attribute__((ext_vector_type(2)));
+    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+    i16x2 hi = {(short)0x8000, (short)0x8000};
+    u16x2 lo = {0, 0};
+    __device__ __forceinline__ void look(const Piece<bf16_t> &p, bool whole)
+    {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) hi = __builtin_elementwise_max(hi, __builtin_bit_cast(i16x2, p.w[k]));
+        if (whole) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) lo = __builtin_elementwise_max(lo, __builtin_bit_cast(u16x2, p.w[k]));
+        }
+    }
+    __device__ __forceinline__ void look(float low)
+    {
+        const unsigned short u = (unsigned short)(__float_as_uint(low) >> 16);
+        lo.x = lo.x > u ? lo.x : u;
+    }
+    __device__ __forceinline__ void look(const Extent &e)
+    {
+        hi = __builtin_elementwise_max(hi, e.hi);
+        lo = __builtin_elementwise_max(lo, e.lo);
+    }
+    __device__ __forceinline__ float largest() const { return __uint_as_float((unsigned)(uint16_t)(hi.x > hi.y ? hi.x : hi.y) << 16); }
+    // one word for the lanes and waves to meet with: both maxima as signed numbers
+    typedef i16x2 Word;
+    __device__ __forceinline__ Word word() const
+    {
+        const unsigned short u = lo.x > lo.y ? lo.x : lo.y;
+        return Word{hi.x > hi.y ? hi.x : hi.y, (short)(u ^ 0x8000u)};
+    }
+    static __device__ __forceinline__ Word join(Word a, Word b) { return __builtin_elementwise_max(a, b); }
+    static __device__ __forceinline__ Word from_lane(Word a, int mask) { return __builtin_bit_cast(Word, __shfl_xor(__builtin_bit_cast(int, a), mask)); }
+    static __device__ __forceinline__ float most(Word a) { return __uint_as_float((unsigned)(uint16_t)a.x << 16); }
+    static __device__ __forceinline__ bool sure(Word a) { return a.x >= 0; }
+    static __device__ __forceinline__ float lowest(Word a) { return __uint_as_float(((uint16_t)a.y ^ 0x8000u) << 16); }
+};
+template <>
+struct Extent<float> {
+    float hi = -INFINITY, lo = INFINITY;
+    __device__ __forceinline__ void look(const Piece<float> &p, bool whole)
+    {
+        hi = max3(max3(hi, p.at(0), p.at(1)), p.at(2), p.at(3));
+        if (whole) lo = min3(min3(lo, p.at(0), p.at(1)), p.at(2), p.at(3));
+    }
+    __device__ __forceinline__ void look(float low) { lo = fminf(lo, low); }
+    __device__ __forceinline__ void look(const Extent &e)
+    {
+        hi = fmaxf(hi, e.hi);
+        lo = fminf(lo, e.lo);
+    }
+    __device__ __forceinline__ float largest() const { return hi; }
+    typedef float2 Word;
+    __device__ __forceinline__ Word word() const { return make_float2(hi, lo); }
+    static __device__ __forceinline__ Word join(Word a, Word b) { return make_float2(fmaxf(a.x, b.x), fminf(a.y, b.y)); }
+    static __device__ __forceinline__ Word from_lane(Word a, int mask) { return make_float2(__shfl_xor(a.x, mask), __shfl_xor(a.y, mask)); }
+    static __device__ __forceinline__ float most(Word a) { return fmaxf(a.x, LOWEST); }
+    static __device__ __forceinline__ bool sure(Word) { return true; }
+    static __device__ __forceinline__ float lowest(Word a) { return a.y; }
 };
 
 // A row as pieces at 16-byte boundaries: the first and the last may be shared with what lies before and behind the row, which is
@@ -99,8 +187,11 @@ struct Row {
         z = (const T *)a.z + first - head;
         dz = a.dz ? (T *)a.dz + first - head : nullptr;
     }
-    __device__ __forceinline__ bool whole(int piece) const { return piece * V >= head && (piece + 1) * V <= K + head; }
-    __device__ __forceinline__ Piece<T> load(int piece) const
+    __device__ __forceinline__ bool whole(int piece) const { return whole(piece, 1); }
+    // all pieces of [piece, piece + n) lie wholly in the row
+    __device__ __forceinline__ bool whole(int piece, int n) const { return piece * V >= head && (piece + n) * V <= K + head; }
+    // Places outside the row get minus infinity; low: the lowest value of pieces that are not whole.
+    __device__ __forceinline__ Piece<T> load(int piece, float &low) const
     {
         Piece<T> p;
         if (whole(piece)) {
@@ -113,6 +204,7 @@ struct Row {
                 for (int k = 0; k < V; ++k) {
                     const int i = piece * V + k;
                     if (i < head || i >= K + head) continue;
+                    low = fminf(low, load_f32(z + i));
                     if constexpr (V == 8) {
                         const uint32_t v = z[i];
                         p.w[k / 2] = k & 1 ? (p.w[k / 2] & 0xFFFFu) | (v << 16) : (p.w[k / 2] & 0xFFFF0000u) | v;
@@ -160,6 +252,9 @@ struct Scale {
     __device__ __forceinline__ float any(float z) const { return near ? d2<true>(z) : d2<false>(z); }
 };
 
+template <bool CLAMP>
+__device__ __forceinline__ float weight(float d) { return CLAMP ? fmaxf(d, NO_WEIGHT) : d; }
+
 // lanes of a group of G (a power of two up to a wave) meet
 template <int G, class F>
 __device__ __forceinline__ float meet(float x, F f)
@@ -172,9 +267,9 @@ __device__ __forceinline__ float larger(float a, float b) { return fmaxf(a, b); 
 __device__ __forceinline__ float sum(float a, float b) { return a + b; }
 
 // ---- the most probable tokens ---------------------------------------------------------------------------------------------
-// Cells are sets of a wave's values, 64 or more of them, of which each lane knows the largest.  The top-th largest of these is a bound that
-// `top` values reach at least; so is the largest of the waves' bounds.  What reaches it is collected in LDS and ranked by
-// counting, which makes the order that of the keys whatever order they were collected in.
+// Cells are sets of a wave's values, 64 or more of them, of which each lane knows one of the largest.  Where each of W waves has top/W cells that
+// reach a bound, `top` values reach it; so they do where one wave has `top` cells that reach it.  What reaches the bound is collected in
+// LDS and ranked by counting, which makes the order that of the keys whatever order they were collected in.
 constexpr int CAP = 1024;
 struct TopShared {
     unsigned long long list[CAP];
@@ -203,14 +298,21 @@ template <int W, int S, int LOW, class Each, class Emit>
 __device__ __forceinline__ void select_top(TopShared &sh, const unsigned *cell, int top, Each each, Emit emit)
 {
     const int wave = threadIdx.x >> 6;
-    const unsigned mine = wave_bound<S, LOW>(cell, top);
+    unsigned bound = wave_bound<S, LOW>(cell, (top + W - 1) / W);
     if (threadIdx.x == 0) sh.count = 0;
-    unsigned bound = mine;
     if constexpr (W > 1) {
-        if ((threadIdx.x & 63) == 0) sh.bound[wave] = mine;
+        if ((threadIdx.x & 63) == 0) sh.bound[wave] = bound;
         __syncthreads();
 #pragma unroll
-        for (int w = 0; w < W; ++w) bound = max(bound, sh.bound[w]);
+        for (int w = 0; w < W; ++w) bound = min(bound, sh.bound[w]);
+        if (bound <= order(-INFINITY)) {        // a wave has less than its share: what one wave holds alone
+            __syncthreads();
+            bound = wave_bound<S, LOW>(cell, top);
+            if ((threadIdx.x & 63) == 0) sh.bound[wave] = bound;
+            __syncthreads();
+#pragma unroll
+            for (int w = 0; w < W; ++w) bound = max(bound, sh.bound[w]);
+        }
     } else
         __syncthreads();
     auto collect = [&](unsigned from, unsigned tie) {       // values above `from`, and equal ones up to index `tie`
@@ -295,6 +397,8 @@ __device__ __forceinline__ void each_value(const Piece<T> (&p)[P], int first, in
 #pragma unroll
             for (int k = 0; k < 4; ++k) c.w[k] = q == i ? p[i].w[k] : c.w[k];
 #pragma unroll
+        for (int k = 0; k < 4; ++k) asm volatile("" : "+v"(c.w[k]));        // (else every piece is unpacked before the choice, and held)
+#pragma unroll
         for (int k = 0; k < Piece<T>::V; ++k) {
             const int i = first + q * stride + k;
             const unsigned o = order(c.at(k));
@@ -308,17 +412,19 @@ __device__ __forceinline__ void each_value(const Piece<T> (&p)[P], int first, in
 // G threads a row, P pieces a thread; rows of fewer than a wave's lanes share one.  TOP: with the most probable tokens, else
 // the gradient where dz is given.
 template <typename T, int G, int P, bool TOP>
-__global__ __launch_bounds__(G < 64 ? 256 : G) void logprob_row_kernel(LogprobArgs a)
+__global__ __launch_bounds__(G < 64 ? 256 : G, G == 512 && P == 16 ? 4 : 1) void logprob_row_kernel(LogprobArgs a)
 {
     constexpr int W = G / 64;       // waves a row; 0: several rows a wave
-    __shared__ float red[3][W > 1 ? W : 1];
+    __shared__ float red[2][W > 1 ? W : 1];
+    __shared__ typename Extent<T>::Word ext[W > 1 ? W : 1];
     const int lane = G < 64 ? threadIdx.x % G : threadIdx.x;
     const size_t row = G < 64 ? (size_t)blockIdx.x * (256 / G) + threadIdx.x / G : (size_t)blockIdx.x;
     if (G < 64 && row >= (size_t)a.N) return;
     const Row<T> r(a, row);
     Piece<T> p[P];
+    float low = 0.f;        // (above nothing that matters)
 #pragma unroll
-    for (int q = 0; q < P; ++q) p[q] = r.load(q * G + lane);
+    for (int q = 0; q < P; ++q) p[q] = r.load(q * G + lane, low);
     const int label = a.labels ? a.labels[row] : -1;
     const bool given = (unsigned)label < (unsigned)a.K;
     const float zl = given ? load_f32(r.z + r.head + label) : 0.f;      // (before the gradient is written: dz may be z)
@@ -338,47 +444,85 @@ __global__ __launch_bounds__(G < 64 ? 256 : G) void logprob_row_kernel(LogprobAr
         return x;
     };
     constexpr int S = P < 4 ? P : 4;
-    float m = LOWEST;
+    Extent<T> part[S];
+#pragma unroll
+    for (int q = 0; q < P; ++q) {
+        if (r.whole(q * G, G)) part[q % S].look(p[q], true);        // (the same for all of the row's lanes)
+        else part[q % S].look(p[q], r.whole(q * G + lane));
+    }
+    part[0].look(low);
     unsigned cell[S];
     if constexpr (TOP) {
-        float top_of[S];
+#pragma unroll
+        for (int s = 0; s < S; ++s) cell[s] = order(part[s].largest());
+    }
+#pragma unroll
+    for (int s = 1; s < S; ++s) part[0].look(part[s]);
+    typename Extent<T>::Word e = part[0].word();
+#pragma unroll
+    for (int d = (G < 64 ? G : 64) / 2; d > 0; d >>= 1) e = Extent<T>::join(e, Extent<T>::from_lane(e, d));
+    if constexpr (W > 1) {
+        if ((threadIdx.x & 63) == 0) ext[threadIdx.x >> 6] = e;
+        __syncthreads();
+        e = ext[0];
+#pragma unroll
+        for (int w = 1; w < W; ++w) e = Extent<T>::join(e, ext[w]);
+    }
+    float m = Extent<T>::most(e);
+    if (!Extent<T>::sure(e)) {      // all are negative
+        m = LOWEST;
+        float of[S];
 #pragma unroll
         for (int q = 0; q < P; ++q) {
-            const float x = p[q].template largest<false>();
-            top_of[q % S] = q < S ? x : max3(top_of[q % S], x, x);
+            const float x = p[q].template largest<true>();
+            of[q % S] = q < S ? x : fmaxf(of[q % S], x);
         }
 #pragma unroll
         for (int s = 0; s < S; ++s) {
-            cell[s] = order(top_of[s]);
-            m = fmaxf(m, top_of[s]);
+            if constexpr (TOP) cell[s] = order(of[s]);
+            m = fmaxf(m, of[s]);
         }
-    } else {
-#pragma unroll
-        for (int q = 0; q < P; ++q) m = max3(m, p[q].template largest<false>(), m);
+        m = meet_row(m, 0, larger);
+        if constexpr (W > 1) __syncthreads();
+        m = joined(m, 0, larger);
+        if constexpr (W > 1) __syncthreads();
     }
-    m = meet_row(m, 0, larger);
-    if constexpr (W > 1) __syncthreads();
-    m = joined(m, 0, larger);
     const Scale sc(a.scale, m);
-    float s = 0.f, t = 0.f;
-    auto sums = [&](auto near) {
+    // Some d2 may be minus infinity (a NaN comes here too).  Where none is, the places outside the row get a number that has no weight
+    // either, and no product needs care.
+    const bool masked = !(Extent<T>::lowest(e) * sc.k2 > -3.0e38f);
+    const float fill = sc.near && !masked ? -0x1p20f / sc.k2 : -INFINITY;
 #pragma unroll
-        for (int q = 0; q < P; ++q) {
+    for (int q = 0; q < P; ++q)
+        if (!r.whole(q * G, G)) p[q].refill(fill);
+    float s = 0.f, t = 0.f;
+    auto sums = [&](auto clamp) {
+#pragma unroll
+        for (int q = 0; q < P; ++q)
 #pragma unroll
             for (int k = 0; k < Piece<T>::V; ++k) {
-                const float d = sc.d2<decltype(near)::value>(p[q].again(k)), e = __builtin_amdgcn_exp2f(d);
+                const float d = sc.d2<true>(p[q].again(k)), e = __builtin_amdgcn_exp2f(d);
                 s += e;
-                t = fmaf(e, fmaxf(d, NO_WEIGHT), t);
+                t = fmaf(e, weight<decltype(clamp)::value>(d), t);
+            }
+    };
+    if (!sc.near) {     // rare: the pieces once more from memory, one after the other
+        for (int piece = lane; piece < r.pieces; piece += G) {
+            const Piece<T> c = r.load(piece, low);
+#pragma unroll
+            for (int k = 0; k < Piece<T>::V; ++k) {
+                const float d = sc.d2<false>(c.at(k)), e = __builtin_amdgcn_exp2f(d);
+                s += e;
+                t = fmaf(e, weight<true>(d), t);
             }
         }
-    };
-    if (sc.near) sums(std::true_type());
+    } else if (masked) sums(std::true_type());
     else sums(std::false_type());
-    s = meet_row(s, 1, sum);
-    t = meet_row(t, 2, sum);
+    s = meet_row(s, 0, sum);
+    t = meet_row(t, 1, sum);
     if constexpr (W > 1) __syncthreads();
-    s = joined(s, 1, sum);
-    t = joined(t, 2, sum);
+    s = joined(s, 0, sum);
+    t = joined(t, 1, sum);
     const bool empty = s == 0.f;
     const float ls = empty ? 0.f : log2f(s), mean = t / s;
     if (lane == 0) {
@@ -400,32 +544,37 @@ __global__ __launch_bounds__(G < 64 ? 256 : G) void logprob_row_kernel(LogprobAr
             });
     } else if (a.dz) {
         const float dl = a.dlogp && given ? a.dlogp[row] : 0.f, dh = a.dentropy ? a.dentropy[row] : 0.f;
-        const float per = a.scale / s, A = per * (dh * (mean * LN2) - dl), B = -per * dh * LN2;
-        const int place = given ? label + r.head : -1;
-        auto gradient = [&](auto near) {
+        const float per = empty ? 0.f : a.scale / s, A = empty ? 0.f : per * (dh * (mean * LN2) - dl), B = -per * dh * LN2;
+        const int place = given && !empty ? label + r.head : -1;
+        auto gradient = [&](int piece, auto near, auto clamp, auto value) {
+            float g[Piece<T>::V];
 #pragma unroll
-            for (int q = 0; q < P; ++q) {
-                float g[Piece<T>::V];
-#pragma unroll
-                for (int k = 0; k < Piece<T>::V; ++k) {
-                    const float d = sc.d2<decltype(near)::value>(p[q].again(k));
-                    g[k] = __builtin_amdgcn_exp2f(d) * fmaf(fmaxf(d, NO_WEIGHT), B, A);
-                }
-                const int at = place - (q * G + lane) * Piece<T>::V;
-                if ((unsigned)at < (unsigned)Piece<T>::V) {
-#pragma unroll
-                    for (int k = 0; k < Piece<T>::V; ++k)
-                        if (k == at) g[k] += a.scale * dl;
-                }
-                if (empty) {
-#pragma unroll
-                    for (int k = 0; k < Piece<T>::V; ++k) g[k] = 0.f;
-                }
-                r.store(q * G + lane, g);
+            for (int k = 0; k < Piece<T>::V; ++k) {
+                const float d = sc.d2<decltype(near)::value>(value(k));
+                g[k] = __builtin_amdgcn_exp2f(d) * fmaf(weight<decltype(clamp)::value>(d), B, A);
             }
+            const int at = place - piece * Piece<T>::V;
+            if ((unsigned)at < (unsigned)Piece<T>::V) {
+#pragma unroll
+                for (int k = 0; k < Piece<T>::V; ++k)
+                    if (k == at) g[k] += a.scale * dl;
+            }
+            r.store(piece, g);
+            __builtin_amdgcn_sched_barrier(0);      // one piece at a time: several would cost the registers that hold the row
         };
-        if (sc.near) gradient(std::true_type());
-        else gradient(std::false_type());
+        int again = lane;       // (else the places of all pieces are kept from the loads on, in registers)
+        asm volatile("" : "+v"(again));
+        auto held = [&](auto clamp) {
+#pragma unroll
+            for (int q = 0; q < P; ++q) gradient(q * G + again, std::true_type(), clamp, [&](int k) { return p[q].again(k); });
+        };
+        if (!sc.near) {
+            for (int piece = lane; piece < r.pieces; piece += G) {
+                const Piece<T> c = r.load(piece, low);
+                gradient(piece, std::false_type(), std::true_type(), [&](int k) { return empty ? -INFINITY : c.at(k); });
+            }
+        } else if (masked) held(std::true_type());
+        else held(std::false_type());
     }
 }
 
@@ -447,8 +596,9 @@ __global__ __launch_bounds__(CHUNK_THREADS) void logprob_chunk_kernel(LogprobArg
     const Row<T> r(a, row);
     const int piece0 = chunk * (G * P);
     Piece<T> p[P];
+    float low = 0.f;        // (above nothing that matters)
 #pragma unroll
-    for (int q = 0; q < P; ++q) p[q] = r.load(piece0 + q * G + (int)threadIdx.x);
+    for (int q = 0; q < P; ++q) p[q] = r.load(piece0 + q * G + (int)threadIdx.x, low);
     float top_of[S], m = LOWEST;
     unsigned cell[S];
 #pragma unroll
@@ -606,8 +756,9 @@ __device__ __forceinline__ void chunk_gradient(const LogprobArgs &a, size_t row,
     const int place = given ? label + r.head : -1;
     const int piece0 = chunk * (CHUNK_THREADS * P) + (int)threadIdx.x;
     Piece<T> p[P];
+    float low = 0.f;        // (above nothing that matters)
 #pragma unroll
-    for (int q = 0; q < P; ++q) p[q] = r.load(piece0 + q * CHUNK_THREADS);
+    for (int q = 0; q < P; ++q) p[q] = r.load(piece0 + q * CHUNK_THREADS, low);
 #pragma unroll
     for (int q = 0; q < P; ++q) {
         const int piece = piece0 + q * CHUNK_THREADS;
@@ -644,29 +795,29 @@ __global__ __launch_bounds__(CHUNK_THREADS) void logprob_bwd_kernel(LogprobArgs 
 
 // ---- host -----------------------------------------------------------------------------------------------------------------
 
-// pieces that a row of K values can have
-int row_pieces(int K, int dtype)
+// 16-byte pieces that a row of K values has where all rows begin on one (ld a multiple of a piece), or may have
+int row_pieces(int K, int dtype, int ld)
 {
     const int V = 16 / (int)elem_size(dtype);
-    return (int)(((long long)K + 2 * V - 2) / V);
+    return (int)(((long long)K + (ld % V == 0 ? V - 1 : 2 * V - 2)) / V);
 }
+constexpr int ANY_LD = 1;
 
 constexpr int ROW_PIECES = 16384;       // in registers: 16 of each of 1024 threads
 
 // chunks of a row (0: rows in registers).  Pieces a thread of a chunk: 1 or 8.
-int chunk_pieces(int N, int K, int dtype)
+int chunk_pieces(int N, int pieces)
 {
-    const int pieces = row_pieces(K, dtype);
     if (pieces > ROW_PIECES) return N < 64 ? 1 : 8;
     if (pieces > 1024 && N < 64) return 1;
     return 0;
 }
-int chunk_count(int K, int dtype, int per_thread) { return (int)(((long long)row_pieces(K, dtype) + CHUNK_THREADS * per_thread - 1) / (CHUNK_THREADS * per_thread)); }
+int chunk_count(int pieces, int per_thread) { return (int)((pieces + (long long)CHUNK_THREADS * per_thread - 1) / (CHUNK_THREADS * per_thread)); }
 
 template <typename T, bool TOP>
 void launch_row(const LogprobArgs &a, hipStream_t st)
 {
-    const int pieces = row_pieces(a.K, a.dtype);
+    const int pieces = row_pieces(a.K, a.dtype, a.ld);
     const dim3 rows((unsigned)a.N);
     if (!TOP && pieces <= 8) {
         hipLaunchKernelGGL((logprob_row_kernel<T, 8, 1, false>), dim3((unsigned)((a.N + 31ll) / 32)), dim3(256), 0, st, a);
@@ -685,13 +836,13 @@ void launch_row(const LogprobArgs &a, hipStream_t st)
 template <typename T>
 int launch(const LogprobArgs &a, void *workspace, hipStream_t st)
 {
-    const int per = chunk_pieces(a.N, a.K, a.dtype);
+    const int pieces = row_pieces(a.K, a.dtype, a.ld), per = chunk_pieces(a.N, pieces);
     if (per == 0) {
         if (a.top) launch_row<T, true>(a, st);
         else launch_row<T, false>(a, st);
         return hipGetLastError() == hipSuccess ? MXC_OK : MXC_ERR_LAUNCH;
     }
-    const int chunks = chunk_count(a.K, a.dtype, per), span = CHUNK_THREADS * per * Piece<T>::V;
+    const int chunks = chunk_count(pieces, per), span = CHUNK_THREADS * per * Piece<T>::V;
     const size_t grid = (size_t)a.N * chunks;
     if (grid > 0x7FFFFFFFu || (size_t)chunks * (a.top ? a.top : 1) > 0x7FFFFFFFu) return MXC_ERR_SHAPE;
     Part *parts = (Part *)workspace;
@@ -711,7 +862,7 @@ int launch(const LogprobArgs &a, void *workspace, hipStream_t st)
 template <typename T>
 int launch_bwd(const LogprobArgs &a, const float *stats, const float *entropy, hipStream_t st)
 {
-    const int per = row_pieces(a.K, a.dtype) <= CHUNK_THREADS ? 1 : 4, chunks = chunk_count(a.K, a.dtype, per);
+    const int pieces = row_pieces(a.K, a.dtype, a.ld), per = pieces <= CHUNK_THREADS ? 1 : 4, chunks = chunk_count(pieces, per);
     const size_t grid = (size_t)a.N * chunks;
     if (grid > 0x7FFFFFFFu) return MXC_ERR_SHAPE;
     const dim3 g((unsigned)grid), b(CHUNK_THREADS);
@@ -724,9 +875,9 @@ int launch_bwd(const LogprobArgs &a, const float *stats, const float *entropy, h
 
 size_t logprob_workspace(int N, int K, int dtype, int top)
 {
-    const int per = chunk_pieces(N, K, dtype);
+    const int pieces = row_pieces(K, dtype, ANY_LD), per = chunk_pieces(N, pieces);
     if (per == 0) return 0;
-    const size_t grid = (size_t)N * chunk_count(K, dtype, per);
+    const size_t grid = (size_t)N * chunk_count(pieces, per);
     return align_up(grid * sizeof(Part), 256) + grid * top * sizeof(unsigned long long);
 }
 

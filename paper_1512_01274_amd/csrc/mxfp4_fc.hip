@@ -1,8 +1,6 @@
 // FullyConnected on a filter in microscaled 4-bit floating point: y[n][k] = act( sum_c q(x)[n][c]*w[k][c] + bias[k] ).
 // The matrix instructions take 4-bit operands as they are, 32 values of a row and their scale byte in each lane, multiply and add
 // them in fp32.  The product is formed transposed (filter rows first), so that a lane holds four neighbouring columns of y.
-// Which columns meet in one instruction is free as long as both operands agree; every kernel below uses this to let a lane
-// read neighbouring bytes.
 //   token:  N <= 16.  One launch: every wave quantises the part of x that it multiplies.
 //   skinny: x is quantised once, then workgroups of eight waves that share out the columns.
 //   tiled:  x quantised, both operands' scales brought into the order of the tiles, and tiles of LDS that a ring of loads fills.
@@ -45,42 +43,41 @@ __device__ __forceinline__ float activated(float v, const float *bias, long long
 }
 
 // ---- up to 16 rows of x ---------------------------------------------------------------------------------------------------
-// 16 filter rows a workgroup; its eight waves take every eighth group of 512 columns, a lane 128 neighbouring ones of them: 64 bytes of
-// codes, a word of scales.  Lane l holds filter row l%16 and row l%16 of x, which it quantises itself.
+// 16 filter rows a workgroup; its eight waves take every eighth group of 512 columns in four steps of 128.  Lane l holds a block of filter row
+// l%16 and one of row l%16 of x, which it quantises itself: the four lanes of a row read 64 bytes of codes that follow each other.
 constexpr int TOKEN_WAVES = 8;
 
 struct TokenGroup {
-    uint4 w[4];
-    int scale;
+    uint4 w[4], scale;      // scale: the 16 bytes of the group's blocks
 };
 __device__ __forceinline__ TokenGroup load_filter(const unsigned char *wc, const unsigned char *ws, int group, int quarter, int blocks)
 {
     TokenGroup g;
-    const int b = group * 16 + quarter * 4;
+    const int b = group * 16 + quarter;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) g.w[j] = b + j < blocks ? *reinterpret_cast<const uint4 *>(wc + (size_t)(b + j) * 16) : make_uint4(0, 0, 0, 0);
-    g.scale = *reinterpret_cast<const int *>(ws + b);
+    for (int j = 0; j < 4; ++j) g.w[j] = b + 4 * j < blocks ? *reinterpret_cast<const uint4 *>(wc + (size_t)(b + 4 * j) * 16) : make_uint4(0, 0, 0, 0);
+    g.scale = *reinterpret_cast<const uint4 *>(ws + (size_t)group * 16);
     return g;
 }
 
-template <int J, typename T>
-__device__ __forceinline__ f32x4 token_step(const T *x, int column, int C, bool live, const TokenGroup &g, f32x4 acc)
+template <typename T>
+__device__ __forceinline__ f32x4 token_step(const T *x, int column, int C, bool live, uint4 w, unsigned scales, int quarter, f32x4 acc)
 {
     uint4 codes = make_uint4(0, 0, 0, 0);
     unsigned byte = 0;
-    const int left = C - column - J * 32;
+    const int left = C - column;
     if (live && left > 0) {
         float v[4][8];
         unsigned most = 0;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            load8_edge(x + column + J * 32 + k * 8, left - k * 8, v[k]);
+            load8_edge(x + column + k * 8, left - k * 8, v[k]);
             most = max(most, largest8(v[k]));
         }
         byte = mxfp4_scale_byte(most);
         codes = make_uint4(mxfp4_codes8(v[0], byte), mxfp4_codes8(v[1], byte), mxfp4_codes8(v[2], byte), mxfp4_codes8(v[3], byte));
     }
-    return mfma16<J, 0>(g.w[J], codes, acc, g.scale, (int)byte);
+    return mfma16<0, 0>(w, codes, acc, (int)(scales >> (8 * quarter)), (int)byte);
 }
 
 template <typename T>
@@ -102,11 +99,11 @@ __global__ __launch_bounds__(64 * TOKEN_WAVES) void mxfp4_token_kernel(int N, in
     for (int group = wave; group < groups; group += TOKEN_WAVES) {
         const TokenGroup g = next;
         if (group + TOKEN_WAVES < groups) next = load_filter(wc, ws, group + TOKEN_WAVES, quarter, blocks);
-        const int column = group * 512 + quarter * 128;
-        acc = token_step<0>(x, column, C, live, g, acc);
-        acc = token_step<1>(x, column, C, live, g, acc);
-        acc = token_step<2>(x, column, C, live, g, acc);
-        acc = token_step<3>(x, column, C, live, g, acc);
+        const int column = group * 512 + quarter * 32;
+        acc = token_step(x, column, C, live, g.w[0], g.scale.x, quarter, acc);
+        acc = token_step(x, column + 128, C, live, g.w[1], g.scale.y, quarter, acc);
+        acc = token_step(x, column + 256, C, live, g.w[2], g.scale.z, quarter, acc);
+        acc = token_step(x, column + 384, C, live, g.w[3], g.scale.w, quarter, acc);
     }
     part[wave][lane] = acc;
     __syncthreads();
@@ -122,81 +119,95 @@ __global__ __launch_bounds__(64 * TOKEN_WAVES) void mxfp4_token_kernel(int N, in
 }
 
 // ---- some rows of x -------------------------------------------------------------------------------------------------------
-// 16*WF filter rows and 16*NF rows of x a workgroup, both straight from the caches into registers; the waves' sums meet in LDS.
-template <int WF, int NF>
-struct SkinnyStep {
-    uint4 w[WF], x[NF];
-};
-
-template <typename T, int WF, int NF>
-__global__ __launch_bounds__(512) void mxfp4_skinny_kernel(int N, int K, int blocks, int scale_row, const unsigned char *xc, const unsigned char *xs,
-                                                           const unsigned char *wc, const unsigned char *ws, const float *bias, int relu, T *y)
+// x in the order in which the waves read it: [16 rows][step of 128 columns][lane] of 16 bytes, lane l: row l%16, block l/16 of the step, and
+// [16 rows][group of 512 columns][lane] words of scales, byte j: step j of the group.  Rows past N are zeros.
+template <typename T>
+__global__ __launch_bounds__(256) void mxfp4_order_kernel(int N, int C, int groups, const T *x, unsigned *xc, unsigned *xs)
 {
-    constexpr int WAVES = 8, BM = 16 * WF, BN = 16 * NF;
-    __shared__ f32x4 part[WAVES][WF * NF][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, quarter = lane >> 4;
-    const long long k0 = (long long)blockIdx.x * BM, n0 = (long long)blockIdx.y * BN;
-    // offsets from the tiles' first rows, which are less than 2 GB (C <= MXC_MXFP4_FC_MAX_C, at most 128 rows)
-    const unsigned code_row = (unsigned)blocks * 16u;
-    wc += (size_t)k0 * code_row;
-    ws += (size_t)k0 * scale_row;
-    xc += (size_t)n0 * code_row;
-    xs += (size_t)n0 * scale_row;
-    unsigned w_row[WF], x_row[NF];
+    __shared__ unsigned words[64];
+    const int group = (int)(blockIdx.x % (unsigned)groups), tile = (int)(blockIdx.x / (unsigned)groups);
+    const int quarter = threadIdx.x & 3, row = threadIdx.x >> 4, at = (threadIdx.x >> 2) & 3;       // four lanes a block, the step's block `at`
+    const int n = tile * 16 + row, lane = row + 16 * at;
+    float v[4][8];
 #pragma unroll
-    for (int i = 0; i < WF; ++i) w_row[i] = (unsigned)(k0 + i * 16 + r < K ? i * 16 + r : K - 1 - k0);
+    for (int j = 0; j < 4; ++j) {
+        const int column = group * 512 + j * 128 + at * 32 + quarter * 8;
+        load8_edge(x + (n < N ? (size_t)n * C + column : 0), n < N ? C - column : 0, v[j]);
+    }
+    unsigned bytes = 0;
 #pragma unroll
-    for (int i = 0; i < NF; ++i) x_row[i] = (unsigned)(n0 + i * 16 + r < N ? i * 16 + r : N - 1 - n0);
-    f32x4 acc[WF][NF] = {};
+    for (int j = 0; j < 4; ++j) {
+        const unsigned byte = mxfp4_scale_byte(max_quad(largest8(v[j])));
+        bytes |= byte << (8 * j);
+        xc[(((size_t)blockIdx.x * 4 + j) * 64 + lane) * 4 + quarter] = mxfp4_codes8(v[j], byte);
+    }
+    if (quarter == 0) words[lane] = bytes;
+    __syncthreads();
+    if (threadIdx.x < 64) xs[(size_t)blockIdx.x * 64 + threadIdx.x] = words[threadIdx.x];
+}
+
+// 16 filter rows and 16*NF rows of x a workgroup, both straight from the caches into registers; its eight waves take every eighth group of
+// 512 columns, and their sums meet in LDS.
+template <typename T, int NF>
+__global__ __launch_bounds__(512) void mxfp4_skinny_kernel(int N, int K, int blocks, int scale_row, const uint4 *xc, const unsigned *xs, const unsigned char *wc,
+                                                           const unsigned char *ws, const float *bias, int relu, T *y)
+{
+    constexpr int WAVES = 8;
+    __shared__ f32x4 part[WAVES][NF][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quarter = lane >> 4;
+    const int groups = scale_row / 16, tiles = (N + 15) / 16, tile0 = blockIdx.y * NF;
+    const long long k0 = (long long)blockIdx.x * 16, row = k0 + (lane & 15) < K ? k0 + (lane & 15) : K - 1;
+    wc += (size_t)row * blocks * 16;
+    ws += (size_t)row * scale_row;
+    int tile[NF];       // (the last one again where there are fewer)
+#pragma unroll
+    for (int i = 0; i < NF; ++i) tile[i] = min(tile0 + i, tiles - 1);
+    f32x4 acc[NF] = {};
+    struct Step {
+        uint4 w, x[NF];
+    };
     auto load = [&](int group, int j) {
-        SkinnyStep<WF, NF> s;
-        const int b = group * 16 + quarter * 4 + j;
-        const bool in = b < blocks;
-        const unsigned at = (unsigned)b * 16u;
+        Step s;
+        const int b = group * 16 + j * 4 + quarter;
+        s.w = b < blocks ? *reinterpret_cast<const uint4 *>(wc + (size_t)b * 16) : make_uint4(0, 0, 0, 0);
 #pragma unroll
-        for (int i = 0; i < WF; ++i) s.w[i] = in ? *reinterpret_cast<const uint4 *>(wc + (w_row[i] * code_row + at)) : make_uint4(0, 0, 0, 0);
-#pragma unroll
-        for (int i = 0; i < NF; ++i) s.x[i] = in ? *reinterpret_cast<const uint4 *>(xc + (x_row[i] * code_row + at)) : make_uint4(0, 0, 0, 0);
+        for (int i = 0; i < NF; ++i) s.x[i] = xc[(((size_t)tile[i] * groups + group) * 4 + j) * 64 + lane];
         return s;
     };
-    int sw[WF], sx[NF];
-    auto multiply = [&](auto j, const SkinnyStep<WF, NF> &s) {
+    uint4 sw = make_uint4(0, 0, 0, 0);      // 16 scale bytes of the filter's row: this lane's of step j is byte `quarter` of word j
+    int sx[NF] = {};
+    auto multiply = [&](auto j, const Step &s) {
+        constexpr int J = decltype(j)::value;
+        const int mine = (int)((J == 0 ? sw.x : J == 1 ? sw.y : J == 2 ? sw.z : sw.w) >> (8 * quarter));
 #pragma unroll
-        for (int i = 0; i < WF; ++i)
-#pragma unroll
-            for (int q = 0; q < NF; ++q) acc[i][q] = mfma16<decltype(j)::value, decltype(j)::value>(s.w[i], s.x[q], acc[i][q], sw[i], sx[q]);
+        for (int i = 0; i < NF; ++i) acc[i] = mfma16<0, J>(s.w, s.x[i], acc[i], mine, sx[i]);
     };
-    const int groups = scale_row / 16;
     if (wave < groups) {
-        SkinnyStep<WF, NF> a = load(wave, 0), b;
+        Step a = load(wave, 0), b;
         for (int group = wave; group < groups; group += WAVES) {
+            sw = *reinterpret_cast<const uint4 *>(ws + (size_t)group * 16);
 #pragma unroll
-            for (int i = 0; i < WF; ++i) sw[i] = *reinterpret_cast<const int *>(ws + (w_row[i] * (unsigned)scale_row + (unsigned)(group * 16 + quarter * 4)));
-#pragma unroll
-            for (int i = 0; i < NF; ++i) sx[i] = *reinterpret_cast<const int *>(xs + (x_row[i] * (unsigned)scale_row + (unsigned)(group * 16 + quarter * 4)));
+            for (int i = 0; i < NF; ++i) sx[i] = (int)xs[((size_t)tile[i] * groups + group) * 64 + lane];
             b = load(group, 1);
             multiply(std::integral_constant<int, 0>(), a);
             a = load(group, 2);
             multiply(std::integral_constant<int, 1>(), b);
             b = load(group, 3);
             multiply(std::integral_constant<int, 2>(), a);
-            const int next = group + WAVES < groups ? group + WAVES : group;
-            a = load(next, 0);
+            a = load(group + WAVES < groups ? group + WAVES : group, 0);
             multiply(std::integral_constant<int, 3>(), b);
         }
     }
 #pragma unroll
-    for (int i = 0; i < WF; ++i)
-#pragma unroll
-        for (int q = 0; q < NF; ++q) part[wave][i * NF + q][lane] = acc[i][q];
+    for (int i = 0; i < NF; ++i) part[wave][i][lane] = acc[i];
     __syncthreads();
     // a thread: four neighbouring columns of a row, in ascending order of waves
-    for (int u = threadIdx.x; u < WF * NF * 64; u += 512) {
+    for (int u = threadIdx.x; u < NF * 64; u += 512) {
         const int f = u >> 6, l = u & 63;
         f32x4 v = part[0][f][l];
 #pragma unroll
         for (int w = 1; w < WAVES; ++w) v += part[w][f][l];
-        const long long k = k0 + (f / NF) * 16 + (l >> 4) * 4, n = n0 + (f % NF) * 16 + (l & 15);
+        const long long k = k0 + (l >> 4) * 4, n = (tile0 + f) * 16ll + (l & 15);
         if (n >= N) continue;
 #pragma unroll
         for (int e = 0; e < 4; ++e)
@@ -213,14 +224,14 @@ __device__ __forceinline__ unsigned pick_scales(uint2 s, int odd)
                : (s.x & 255u) | (s.x >> 16 & 255u) << 8 | (s.y & 255u) << 16 | (s.y >> 16 & 255u) << 24;
 }
 
-// Prepares both operands in one launch.  Workgroups up to `x_groups`: x, 32 rows and 256 columns each, a block of 32 values a thread;
-// the others: the filter's scales, 32 rows and 8 groups.
+// Prepares both operands in one launch.  Workgroups up to `x_groups`: x, 32 rows and 256 columns each, four lanes a block as in
+// mxfp4_quantize; the others: the filter's scales, 32 rows and 8 groups.
 template <typename T>
 __global__ __launch_bounds__(256) void mxfp4_prepare_kernel(int N, int C, int K, int blocks, int scale_row, int groups, unsigned x_groups, const T *x,
-                                                            unsigned char *xc, unsigned *xs, const unsigned char *ws, unsigned *wt)
+                                                            unsigned *xc, unsigned *xs, const unsigned char *ws, unsigned *wt)
 {
-    const int row = threadIdx.x >> 3, at = threadIdx.x & 7;
     if (blockIdx.x >= x_groups) {
+        const int row = threadIdx.x >> 3, at = threadIdx.x & 7;
         const unsigned i = blockIdx.x - x_groups, eights = (unsigned)(groups + 7) / 8;
         const int group = (int)(i % eights) * 8 + at;
         const long long tile = i / eights, k = tile * 32 + row, tiles = (K + 31ll) / 32;
@@ -233,23 +244,23 @@ __global__ __launch_bounds__(256) void mxfp4_prepare_kernel(int N, int C, int K,
         return;
     }
     __shared__ unsigned char bytes[32][8];
-    const int group = (int)(blockIdx.x % (unsigned)groups);
-    const long long tile = blockIdx.x / (unsigned)groups, n = tile * 32 + row, tiles = (N + 31ll) / 32;
-    const int b = group * 8 + at, left = C - b * 32;
-    unsigned byte = 0;
-    if (n < N && b < blocks) {
-        float v[4][8];
-        unsigned most = 0;
+    const int group = (int)(blockIdx.x % (unsigned)groups), quarter = threadIdx.x & 3, at = (threadIdx.x >> 2) & 7, b = group * 8 + at;
+    const long long tile = blockIdx.x / (unsigned)groups, tiles = (N + 31ll) / 32;
+    const int column = b * 32 + quarter * 8;
+    float v[4][8];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            load8_edge(x + (size_t)n * C + b * 32 + k * 8, left - k * 8, v[k]);
-            most = max(most, largest8(v[k]));
-        }
-        byte = mxfp4_scale_byte(most);
-        *reinterpret_cast<uint4 *>(xc + ((size_t)n * blocks + b) * 16) =
-            make_uint4(mxfp4_codes8(v[0], byte), mxfp4_codes8(v[1], byte), mxfp4_codes8(v[2], byte), mxfp4_codes8(v[3], byte));
+    for (int i = 0; i < 4; ++i) {       // rows threadIdx.x/32 + 8*i
+        const long long n = tile * 32 + i * 8 + (threadIdx.x >> 5);
+        load8_edge(x + (n < N ? (size_t)n * C + column : 0), n < N ? C - column : 0, v[i]);
     }
-    bytes[row][at] = (unsigned char)byte;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int row = i * 8 + (threadIdx.x >> 5);
+        const long long n = tile * 32 + row;
+        const unsigned byte = mxfp4_scale_byte(max_quad(largest8(v[i])));
+        if (n < N && b < blocks) xc[((size_t)n * blocks + b) * 4 + quarter] = mxfp4_codes8(v[i], byte);
+        if (quarter == 0) bytes[row][at] = (unsigned char)byte;
+    }
     __syncthreads();
     if (threadIdx.x < 64) {
         const uint2 s = *reinterpret_cast<const uint2 *>(bytes[threadIdx.x & 31]);
@@ -257,28 +268,29 @@ __global__ __launch_bounds__(256) void mxfp4_prepare_kernel(int N, int C, int K,
     }
 }
 
-// Tile of 64*FM filter rows and 64*FN rows of x; four waves, two by two, of 32*FM x 32*FN.  A stage is 128 columns, 64 bytes of codes a
-// row, brought into a ring of four stages by direct loads; scales come a word for two stages.  Row r's 16-byte chunk c lies at place
-// c ^ (r/4)%4, so that the 16 rows that one phase of a 16-byte read covers lie in all 64 banks once.
-// One barrier a stage, between the last operand fetch of the stage and its last product: the fetches of the next stage and the
+// GM x GN waves of 32*FM filter rows by 32*FN rows of x each.  A stage is 128 columns, 64 bytes of codes a row, brought into a ring of four
+// stages by direct loads; scales come a word for two stages.  Row r's 16-byte chunk c lies at place c ^ (r/4)%4, so that the 16 rows
+// that one phase of a 16-byte read covers lie in all 64 banks once.
+// One barrier a stage, between the last operand fetch of the stage and its last products: the fetches of the next stage and the
 // loads of the one after three more go between the products.
-template <int FM, int FN>
+template <int FM, int FN, int GM, int GN>
 struct Tile {
-    static constexpr int BM = 64 * FM, BN = 64 * FN;
+    static constexpr int WAVES = GM * GN, BM = 32 * FM * GM, BN = 32 * FN * GN;
     static constexpr int STAGE = (BM + BN) * 64, RING = 4;
-    static constexpr int SCALES = (BM + BN) * 8 < 4096 ? 4096 : (BM + BN) * 8;      // bytes of scales of two stages (room for a kilobyte of each wave)
-    static constexpr int LDS = RING * STAGE + 4 * SCALES;
-    static constexpr int LOADS = FM + FN;       // of 1 KB, each wave's, a stage
+    static constexpr int KB = (BM + BN) / 128;      // kilobytes of scales of two stages
+    static constexpr int LW = BM / 16 / WAVES, LX = BN / 16 / WAVES, LOADS = LW + LX;       // of 1 KB, each wave's, a stage
+    static_assert(BM % 128 == 0 && BN % 128 == 0 && LW * WAVES * 16 == BM && LX * WAVES * 16 == BN && KB <= WAVES, "whole loads");
+    static_assert(FM + FN <= FM * FN && LOADS <= FM * FN, "room between the products");
 };
 
-template <typename T, int FM, int FN>
-__global__ __launch_bounds__(256, 1) void mxfp4_tile_kernel(int N, int K, int code_row, int groups, const unsigned char *xc, const unsigned *xs,
-                                                            const unsigned char *wc, const unsigned *wt, const float *bias, int relu, T *y, int k_tiles, int n_tiles)
+template <typename T, int FM, int FN, int GM, int GN>
+__global__ __launch_bounds__(64 * GM * GN, 1) void mxfp4_tile_kernel(int N, int K, int code_row, int groups, const unsigned char *xc, const unsigned *xs,
+                                                                     const unsigned char *wc, const unsigned *wt, const float *bias, int relu, T *y, int k_tiles,
+                                                                     int n_tiles)
 {
-    typedef Tile<FM, FN> G;
-    __shared__ __align__(16) unsigned char lds[G::LDS];
-    unsigned char *ring = lds, *scales = lds + G::RING * G::STAGE;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave & 1, wn = wave >> 1, half = lane >> 5;
+    typedef Tile<FM, FN, GM, GN> G;
+    __shared__ __align__(16) unsigned char ring[G::RING * G::STAGE], scales[4 * G::KB * 1024];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave % GM, wn = wave / GM, half = lane >> 5;
 
     // Each XCD works on neighbouring tiles: groups of 8 filter tiles by all tiles of x, the filter's fastest.
     const unsigned total = (unsigned)k_tiles * (unsigned)n_tiles, per = total / 8, rest = total % 8, xcd = blockIdx.x % 8, in_xcd = blockIdx.x / 8;
@@ -290,34 +302,35 @@ __global__ __launch_bounds__(256, 1) void mxfp4_tile_kernel(int N, int K, int co
     const int k_rows = (int)(K - k0 < G::BM ? K - k0 : G::BM), n_rows = (int)(N - n0 < G::BN ? N - n0 : G::BN);
     const buf_rsrc_t rs_w = make_buf_rsrc(wc + (size_t)k0 * code_row, (unsigned)k_rows * (unsigned)code_row);
     const buf_rsrc_t rs_x = make_buf_rsrc(xc + (size_t)n0 * code_row, (unsigned)n_rows * (unsigned)code_row);
-    // a kilobyte of scales is 128 rows: wave w brings part w of the filter's, then of x's
-    constexpr int WS = G::BM / 128, XS = G::BN / 128;
-    const long long w32 = (K + 31ll) / 32, x32 = (N + 31ll) / 32;
-    const bool of_w = wave < WS, of_any = wave < WS + XS;
-    const unsigned *s_base = of_w ? wt + (k0 / 32 + wave * 4) * 64 : xs + (n0 / 32 + (wave - WS) * 4) * 64;
-    const long long s_tiles = of_w ? w32 - (k0 / 32 + wave * 4) : x32 - (n0 / 32 + (wave - WS) * 4);        // that are left
-    const unsigned s_pitch = (unsigned)(of_w ? w32 : x32) * 256u;
-    const unsigned s_bytes = !of_any || s_tiles <= 0 ? 0u : (unsigned)min(s_tiles, 4ll) * 256u;
+    // A kilobyte of scales is 128 rows: wave w brings part w of the filter's, then of x's; waves past the last part bring one of these once more
+    // (the same bytes to the same place), so that every wave has as many loads under way.
+    constexpr int WS = G::BM / 128;
+    const int s_part = wave % G::KB;
+    const bool of_w = s_part < WS;
+    const long long s_tile = of_w ? k0 / 32 + s_part * 4 : n0 / 32 + (s_part - WS) * 4, s_tiles = of_w ? (K + 31ll) / 32 : (N + 31ll) / 32;
+    const unsigned *s_base = (of_w ? wt : xs) + s_tile * 64;
+    const size_t s_pitch = (size_t)s_tiles * 256;
+    const unsigned s_bytes = s_tile >= s_tiles ? 0u : (unsigned)min(s_tiles - s_tile, 4ll) * 256u;
 
     const int stages = (code_row + 63) / 64;
     const int chunk = (lane & 3) ^ ((lane >> 4) & 3);
     unsigned src[G::LOADS];
 #pragma unroll
     for (int i = 0; i < G::LOADS; ++i) {
-        const int row = (i < FM ? wave * FM + i : wave * FN + i - FM) * 16 + (lane >> 2);
+        const int row = (i < G::LW ? wave * G::LW + i : wave * G::LX + i - G::LW) * 16 + (lane >> 2);
         src[i] = (unsigned)row * (unsigned)code_row + chunk * 16;
     }
-    auto issue_codes = [&](int stage, int i) {       // load i of a stage: FM of filter rows, then FN of rows of x
+    auto issue_codes = [&](int stage, int i) {       // load i of a stage: LW of filter rows, then LX of rows of x
         const unsigned column = (unsigned)stage * 64u;
         const unsigned off = (int)(column + chunk * 16) < code_row ? src[i] + column : 0x80000000u;
         unsigned char *to = ring + (stage & 3) * G::STAGE;
-        if (i < FM) lds_dma16(rs_w, off, to + (wave * FM + i) * 1024);
-        else lds_dma16(rs_x, off, to + G::BM * 64 + (wave * FN + i - FM) * 1024);
+        if (i < G::LW) lds_dma16(rs_w, off, to + (wave * G::LW + i) * 1024);
+        else lds_dma16(rs_x, off, to + G::BM * 64 + (wave * G::LX + i - G::LW) * 1024);
     };
     auto issue_scales = [&](int stage) {             // of stages `stage` (even) and the next
         const int group = stage >> 1;
         const buf_rsrc_t rs = make_buf_rsrc((const unsigned char *)s_base + (size_t)(group < groups ? group : 0) * s_pitch, group < groups ? s_bytes : 0u);
-        lds_dma16(rs, (unsigned)lane * 16u, scales + (group & 3) * G::SCALES + wave * 1024);
+        lds_dma16(rs, (unsigned)lane * 16u, scales + ((group & 3) * G::KB + s_part) * 1024);
     };
 
     f32x16 acc[FM][FN] = {};
@@ -328,8 +341,8 @@ __global__ __launch_bounds__(256, 1) void mxfp4_tile_kernel(int N, int K, int co
     const int w_at = (wm * 32 * FM + (lane & 31)) * 64, x_at = (G::BM + wn * 32 * FN + (lane & 31)) * 64;
     auto fetch_w = [&](int stage, int s, int i) { return *reinterpret_cast<const uint4 *>(ring + (stage & 3) * G::STAGE + w_at + i * 2048 + ((2 * s + half) ^ swz) * 16); };
     auto fetch_x = [&](int stage, int s, int i) { return *reinterpret_cast<const uint4 *>(ring + (stage & 3) * G::STAGE + x_at + i * 2048 + ((2 * s + half) ^ swz) * 16); };
-    auto fetch_sw = [&](int group, int i) { return *reinterpret_cast<const int *>(scales + (group & 3) * G::SCALES + (wm * FM + i) * 256 + lane * 4); };
-    auto fetch_sx = [&](int group, int i) { return *reinterpret_cast<const int *>(scales + (group & 3) * G::SCALES + G::BM * 8 + (wn * FN + i) * 256 + lane * 4); };
+    auto fetch_sw = [&](int group, int i) { return *reinterpret_cast<const int *>(scales + (group & 3) * G::KB * 1024 + (wm * FM + i) * 256 + lane * 4); };
+    auto fetch_sx = [&](int group, int i) { return *reinterpret_cast<const int *>(scales + (group & 3) * G::KB * 1024 + G::BM * 8 + (wn * FN + i) * 256 + lane * 4); };
 
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
@@ -376,7 +389,6 @@ __global__ __launch_bounds__(256, 1) void mxfp4_tile_kernel(int N, int K, int co
             }
         });
     };
-    static_assert(FM + FN <= FM * FN && G::LOADS <= FM * FN, "room between the products");
     for (int t = 0; t < stages; t += 2) {
         stage_of(t, std::integral_constant<int, 0>());
         stage_of(t + 1, std::integral_constant<int, 1>());
@@ -439,21 +451,27 @@ Buffers buffers(int N, int C, int K)
     Buffers b;
     const Path path = path_of(N, C, K);
     if (path == TOKEN) return b;
+    if (path == SKINNY) {
+        const size_t units = ((size_t)N + 15) / 16 * (((size_t)C + 511) / 512);     // of 16 rows and 512 columns
+        b.scales = units * 4096;
+        b.filter_scales = b.total = b.scales + units * 256;
+        return b;
+    }
     const size_t groups = ((size_t)C + 255) / 256;
     b.scales = align_up((size_t)N * mxfp4_code_row(C), 256);
-    b.filter_scales = b.scales + (path == SKINNY ? align_up((size_t)N * mxfp4_scale_row(C), 256) : ((size_t)N + 31) / 32 * groups * 256);
-    b.total = b.filter_scales + (path == SKINNY ? 0 : ((size_t)K + 31) / 32 * groups * 256);
+    b.filter_scales = b.scales + ((size_t)N + 31) / 32 * groups * 256;
+    b.total = b.filter_scales + ((size_t)K + 31) / 32 * groups * 256;
     return b;
 }
 
-template <typename T, int FM, int FN>
+template <typename T, int FM, int FN, int GM, int GN>
 int launch_tiles(int N, int C, int K, const unsigned char *xc, const unsigned *xs, const unsigned char *wc, const unsigned *wt, const float *bias, int relu, T *y,
                  hipStream_t st)
 {
-    typedef Tile<FM, FN> G;
+    typedef Tile<FM, FN, GM, GN> G;
     const long long kt = (K + G::BM - 1ll) / G::BM, nt = (N + G::BN - 1ll) / G::BN;
     if (kt * nt > 0x7FFFFFFFll / 8) return MXC_ERR_SHAPE;
-    hipLaunchKernelGGL((mxfp4_tile_kernel<T, FM, FN>), dim3((unsigned)(kt * nt)), dim3(256), 0, st, N, K, (int)mxfp4_code_row(C), (int)(((long long)C + 255) / 256), xc, xs,
+    hipLaunchKernelGGL((mxfp4_tile_kernel<T, FM, FN, GM, GN>), dim3((unsigned)(kt * nt)), dim3(64 * G::WAVES), 0, st, N, K, (int)mxfp4_code_row(C), (int)(((long long)C + 255) / 256), xc, xs,
                        wc, wt, bias, relu, y, (int)kt, (int)nt);
     return MXC_OK;
 }
@@ -470,22 +488,26 @@ int fc(int N, int C, int K, const T *x, const unsigned char *wc, const unsigned 
     const Buffers b = buffers(N, C, K);
     unsigned char *xc = (unsigned char *)workspace, *xs = xc + b.scales;
     if (path == SKINNY) {
-        const int rc = mxfp4_quantize(N, C, sizeof(T) == 2 ? MXC_BF16 : MXC_F32, x, xc, xs, st);
-        if (rc != MXC_OK) return rc;
-        const dim3 block(512);
-        if (N <= 32) hipLaunchKernelGGL((mxfp4_skinny_kernel<T, 1, 2>), dim3((unsigned)((K + 15ll) / 16)), block, 0, st, N, K, blocks, scale_row, xc, xs, wc, ws, bias, relu, y);
-        else if (N <= 64) hipLaunchKernelGGL((mxfp4_skinny_kernel<T, 1, 4>), dim3((unsigned)((K + 15ll) / 16)), block, 0, st, N, K, blocks, scale_row, xc, xs, wc, ws, bias, relu, y);
-        else hipLaunchKernelGGL((mxfp4_skinny_kernel<T, 1, 8>), dim3((unsigned)((K + 15ll) / 16)), block, 0, st, N, K, blocks, scale_row, xc, xs, wc, ws, bias, relu, y);
+        const int groups = scale_row / 16, tiles = (N + 15) / 16;
+        if ((long long)groups * tiles > 0x7FFFFFFFll) return MXC_ERR_SHAPE;
+        hipLaunchKernelGGL(mxfp4_order_kernel<T>, dim3((unsigned)(groups * tiles)), dim3(256), 0, st, N, C, groups, x, (unsigned *)xc, (unsigned *)xs);
+        if (hipGetLastError() != hipSuccess) return MXC_ERR_LAUNCH;
+        const dim3 grid((unsigned)((K + 15ll) / 16)), block(512);
+        const uint4 *codes = (const uint4 *)xc;
+        const unsigned *scales = (const unsigned *)xs;
+        if (N <= 32) hipLaunchKernelGGL((mxfp4_skinny_kernel<T, 2>), grid, block, 0, st, N, K, blocks, scale_row, codes, scales, wc, ws, bias, relu, y);
+        else if (N <= 64) hipLaunchKernelGGL((mxfp4_skinny_kernel<T, 4>), grid, block, 0, st, N, K, blocks, scale_row, codes, scales, wc, ws, bias, relu, y);
+        else hipLaunchKernelGGL((mxfp4_skinny_kernel<T, 8>), grid, block, 0, st, N, K, blocks, scale_row, codes, scales, wc, ws, bias, relu, y);
         return hipGetLastError() == hipSuccess ? MXC_OK : MXC_ERR_LAUNCH;
     }
     const int groups = (int)(((long long)C + 255) / 256);
     unsigned *xt = (unsigned *)xs, *wt = (unsigned *)((unsigned char *)workspace + b.filter_scales);
     const size_t x_groups = ((size_t)N + 31) / 32 * groups, w_groups = ((size_t)K + 31) / 32 * ((groups + 7) / 8);
     if (x_groups + w_groups > 0x7FFFFFFFu) return MXC_ERR_SHAPE;
-    hipLaunchKernelGGL(mxfp4_prepare_kernel<T>, dim3((unsigned)(x_groups + w_groups)), dim3(256), 0, st, N, C, K, blocks, scale_row, groups, (unsigned)x_groups, x, xc, xt, ws, wt);
+    hipLaunchKernelGGL(mxfp4_prepare_kernel<T>, dim3((unsigned)(x_groups + w_groups)), dim3(256), 0, st, N, C, K, blocks, scale_row, groups, (unsigned)x_groups, x, (unsigned *)xc, xt, ws, wt);
     if (hipGetLastError() != hipSuccess) return MXC_ERR_LAUNCH;
     const long long big = ((K + 255ll) / 256) * ((N + 255ll) / 256);
-    const int rc = big >= 192 ? launch_tiles<T, 4, 4>(N, C, K, xc, xt, wc, wt, bias, relu, y, st) : launch_tiles<T, 2, 2>(N, C, K, xc, xt, wc, wt, bias, relu, y, st);
+    const int rc = big >= 192 ? launch_tiles<T, 4, 2, 2, 4>(N, C, K, xc, xt, wc, wt, bias, relu, y, st) : launch_tiles<T, 2, 2, 2, 2>(N, C, K, xc, xt, wc, wt, bias, relu, y, st);
     if (rc != MXC_OK) return rc;
     return hipGetLastError() == hipSuccess ? MXC_OK : MXC_ERR_LAUNCH;
 }
