@@ -273,7 +273,7 @@ __device__ __forceinline__ float sum(float a, float b) { return a + b; }
 constexpr int CAP = 1024;
 struct TopShared {
     unsigned long long list[CAP];
-    unsigned bound[16], tie[16];
+    unsigned bound[16];
     int count;
 };
 
@@ -315,36 +315,33 @@ __device__ __forceinline__ void select_top(TopShared &sh, const unsigned *cell, 
         }
     } else
         __syncthreads();
-    auto collect = [&](unsigned from, unsigned tie) {       // values above `from`, and equal ones up to index `tie`
-        each(from, [&](unsigned o, unsigned index) {
-            if (o >> LOW > from >> LOW || index <= tie) {
+    // Values above the bound, and equal ones up to index `tie`.  Where there are many equal ones (rows of one value, rows where few tokens are
+    // allowed) a second turn takes only the lowest indices of those at the bound: each lane's first one is a cell again.
+    unsigned tie = 0xFFFFFFFFu, first = 0xFFFFFFFFu;
+    int n;
+    for (int turn = 0;; ++turn) {
+        each(bound, [&](unsigned o, unsigned index) {
+            const bool at_bound = o >> LOW == bound >> LOW;
+            if (!at_bound || index <= tie) {
                 const int at = atomicAdd(&sh.count, 1);
                 if (at < CAP) sh.list[at] = key_of(o, index);
             }
+            if (at_bound) first = min(first, index);
         });
         __syncthreads();
-    };
-    collect(bound, 0xFFFFFFFFu);
-    int n = sh.count;
-    if (n > CAP) {
-        // Many equal values (rows of one value, rows where few tokens are allowed): of those at the bound only the lowest
-        // indices count.  Each lane's first one is a cell again.
+        n = sh.count;
+        if (n <= CAP || turn == 1) break;
+        const unsigned cells[1] = {~first};
+        tie = ~wave_bound<1, 0>(cells, top);        // (no less than top of them: those above the bound may be none)
         __syncthreads();
         if (threadIdx.x == 0) sh.count = 0;
-        unsigned first = 0xFFFFFFFFu;
-        each(bound, [&](unsigned o, unsigned index) { if (o >> LOW == bound >> LOW) first = min(first, index); });
-        const unsigned cells[1] = {~first};
-        const unsigned t = ~wave_bound<1, 0>(cells, top);       // (no less than top: those above the bound may be none)
-        unsigned tie = t;
         if constexpr (W > 1) {
-            if ((threadIdx.x & 63) == 0) sh.tie[wave] = t;
+            if ((threadIdx.x & 63) == 0) sh.bound[wave] = tie;
             __syncthreads();
 #pragma unroll
-            for (int w = 0; w < W; ++w) tie = min(tie, sh.tie[w]);
+            for (int w = 0; w < W; ++w) tie = min(tie, sh.bound[w]);
         } else
             __syncthreads();
-        collect(bound, tie);
-        n = sh.count;
     }
     if (n <= CAP) {
         for (int i = threadIdx.x; i < n; i += 64 * W) {
@@ -380,34 +377,28 @@ __device__ __forceinline__ void select_top(TopShared &sh, const unsigned *cell, 
     }
 }
 
-// the values of a thread's pieces that reach `from`, and the row's index of each: f(order, index); first: the index of value 0 of piece 0
+// The values of a thread's pieces that reach `from`, and the row's index of each: f(order, index).  first: the index of value 0 of piece 0;
+// held: pieces that any thread holds.  A whole wave goes on where no lane has a piece that may reach it.
 template <typename T, int P, class F>
-__device__ __forceinline__ void each_value(const Piece<T> (&p)[P], int first, int stride, int K, unsigned from, F f)
+__device__ __forceinline__ void each_value(const Piece<T> (&p)[P], int held, int first, int stride, int K, unsigned from, F f)
 {
-    const float limit = unorder(from);
-    unsigned mask = 0;
+    const float limit = unorder(from);      // (NaN for the lowest bounds: then every value is looked at)
 #pragma unroll
-    for (int q = 0; q < P; ++q) mask |= p[q].template largest<true>() < limit ? 0u : 1u << q;       // (all of them for the lowest bounds, which are NaN)
-    while (mask) {
-        const int q = __ffs(mask) - 1;
-        mask &= mask - 1;
-        Piece<T> c = p[0];
-#pragma unroll
-        for (int i = 1; i < P; ++i)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) c.w[k] = q == i ? p[i].w[k] : c.w[k];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) asm volatile("" : "+v"(c.w[k]));        // (else every piece is unpacked before the choice, and held)
+    for (int q = 0; q < P; ++q) {
+        if (q >= held) continue;
+        if (__ballot(!(p[q].template largest<true>() < limit)) == 0) continue;
+        int index = first + q * stride;
+        asm volatile("" : "+v"(index));     // (else the indices of all values are worked out ahead, and held)
 #pragma unroll
         for (int k = 0; k < Piece<T>::V; ++k) {
-            const int i = first + q * stride + k;
-            const unsigned o = order(c.at(k));
+            const float v = p[q].again(k);
+            if (v < limit) continue;
+            const int i = index + k;
+            const unsigned o = order(v);
             if (o >= from && (unsigned)i < (unsigned)K) f(o, (unsigned)i);
         }
     }
 }
-
-// ---- rows in registers ----------------------------------------------------------------------------------------------------
 
 // G threads a row, P pieces a thread; rows of fewer than a wave's lanes share one.  TOP: with the most probable tokens, else
 // the gradient where dz is given.
@@ -422,6 +413,7 @@ __global__ __launch_bounds__(G < 64 ? 256 : G, G == 512 && P == 16 ? 4 : 1) void
     if (G < 64 && row >= (size_t)a.N) return;
     const Row<T> r(a, row);
     Piece<T> p[P];
+    const int held = (r.pieces + G - 1) / G;        // pieces that any thread holds: what follows passes over the others
     float low = 0.f;        // (above nothing that matters)
 #pragma unroll
     for (int q = 0; q < P; ++q) p[q] = r.load(q * G + lane, low);
@@ -447,6 +439,7 @@ __global__ __launch_bounds__(G < 64 ? 256 : G, G == 512 && P == 16 ? 4 : 1) void
     Extent<T> part[S];
 #pragma unroll
     for (int q = 0; q < P; ++q) {
+        if (q >= held) continue;
         if (r.whole(q * G, G)) part[q % S].look(p[q], true);        // (the same for all of the row's lanes)
         else part[q % S].look(p[q], r.whole(q * G + lane));
     }
@@ -474,7 +467,7 @@ __global__ __launch_bounds__(G < 64 ? 256 : G, G == 512 && P == 16 ? 4 : 1) void
         float of[S];
 #pragma unroll
         for (int q = 0; q < P; ++q) {
-            const float x = p[q].template largest<true>();
+            const float x = q < held ? p[q].template largest<true>() : -INFINITY;
             of[q % S] = q < S ? x : fmaxf(of[q % S], x);
         }
 #pragma unroll
@@ -494,17 +487,19 @@ __global__ __launch_bounds__(G < 64 ? 256 : G, G == 512 && P == 16 ? 4 : 1) void
     const float fill = sc.near && !masked ? -0x1p20f / sc.k2 : -INFINITY;
 #pragma unroll
     for (int q = 0; q < P; ++q)
-        if (!r.whole(q * G, G)) p[q].refill(fill);
+        if (q < held && !r.whole(q * G, G)) p[q].refill(fill);
     float s = 0.f, t = 0.f;
     auto sums = [&](auto clamp) {
 #pragma unroll
-        for (int q = 0; q < P; ++q)
+        for (int q = 0; q < P; ++q) {
+            if (q >= held) continue;
 #pragma unroll
             for (int k = 0; k < Piece<T>::V; ++k) {
                 const float d = sc.d2<true>(p[q].again(k)), e = __builtin_amdgcn_exp2f(d);
                 s += e;
                 t = fmaf(e, weight<decltype(clamp)::value>(d), t);
             }
+        }
     };
     if (!sc.near) {     // rare: the pieces once more from memory, one after the other
         for (int piece = lane; piece < r.pieces; piece += G) {
@@ -537,7 +532,7 @@ __global__ __launch_bounds__(G < 64 ? 256 : G, G == 512 && P == 16 ? 4 : 1) void
         __shared__ TopShared sh;
         select_top<W, S, sizeof(T) == 2 ? 16 : 0>(
             sh, cell, a.top,
-            [&](unsigned from, auto f) { each_value<T, P>(p, lane * Piece<T>::V - r.head, G * Piece<T>::V, a.K, from, f); },
+            [&](unsigned from, auto f) { each_value<T, P>(p, held, lane * Piece<T>::V - r.head, G * Piece<T>::V, a.K, from, f); },
             [&](int i, unsigned long long key) {
                 a.top_index[row * a.top + i] = key == NO_KEY ? -1 : (int)key_index(key);
                 a.top_logp[row * a.top + i] = key == NO_KEY || empty ? -INFINITY : (sc.any(unorder((unsigned)(key >> 32))) - ls) * LN2;
@@ -564,17 +559,18 @@ __global__ __launch_bounds__(G < 64 ? 256 : G, G == 512 && P == 16 ? 4 : 1) void
         };
         int again = lane;       // (else the places of all pieces are kept from the loads on, in registers)
         asm volatile("" : "+v"(again));
-        auto held = [&](auto clamp) {
+        auto all = [&](auto clamp) {
 #pragma unroll
-            for (int q = 0; q < P; ++q) gradient(q * G + again, std::true_type(), clamp, [&](int k) { return p[q].again(k); });
+            for (int q = 0; q < P; ++q)
+                if (q < held) gradient(q * G + again, std::true_type(), clamp, [&](int k) { return p[q].again(k); });
         };
         if (!sc.near) {
             for (int piece = lane; piece < r.pieces; piece += G) {
                 const Piece<T> c = r.load(piece, low);
                 gradient(piece, std::false_type(), std::true_type(), [&](int k) { return empty ? -INFINITY : c.at(k); });
             }
-        } else if (masked) held(std::true_type());
-        else held(std::false_type());
+        } else if (masked) all(std::true_type());
+        else all(std::false_type());
     }
 }
 
@@ -594,7 +590,7 @@ __global__ __launch_bounds__(CHUNK_THREADS) void logprob_chunk_kernel(LogprobArg
     const size_t row = blockIdx.x / (unsigned)chunks;
     const int chunk = blockIdx.x % (unsigned)chunks;
     const Row<T> r(a, row);
-    const int piece0 = chunk * (G * P);
+    const int piece0 = chunk * (G * P), held = min(P, (r.pieces - piece0 + G - 1) / G);
     Piece<T> p[P];
     float low = 0.f;        // (above nothing that matters)
 #pragma unroll
@@ -644,7 +640,7 @@ __global__ __launch_bounds__(CHUNK_THREADS) void logprob_chunk_kernel(LogprobArg
         __shared__ TopShared sh;
         select_top<4, S, sizeof(T) == 2 ? 16 : 0>(
             sh, cell, a.top,
-            [&](unsigned from, auto f) { each_value<T, P>(p, (piece0 + (int)threadIdx.x) * V - r.head, G * V, a.K, from, f); },
+            [&](unsigned from, auto f) { each_value<T, P>(p, held, (piece0 + (int)threadIdx.x) * V - r.head, G * V, a.K, from, f); },
             [&](int i, unsigned long long key) { keys[(size_t)blockIdx.x * a.top + i] = key; });
     }
 }

@@ -289,7 +289,8 @@ __global__ __launch_bounds__(64 * GM * GN, 1) void mxfp4_tile_kernel(int N, int 
                                                                      int n_tiles)
 {
     typedef Tile<FM, FN, GM, GN> G;
-    __shared__ __align__(16) unsigned char ring[G::RING * G::STAGE], scales[4 * G::KB * 1024];
+    __shared__ __align__(16) unsigned char lds[G::RING * G::STAGE + 4 * G::KB * 1024];
+    unsigned char *ring = lds, *scales = lds + G::RING * G::STAGE;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave % GM, wn = wave / GM, half = lane >> 5;
 
     // Each XCD works on neighbouring tiles: groups of 8 filter tiles by all tiles of x, the filter's fastest.
@@ -397,41 +398,59 @@ __global__ __launch_bounds__(64 * GM * GN, 1) void mxfp4_tile_kernel(int N, int 
 #pragma unroll
         for (int i = 0; i < FN; ++i) sx[i] = nsx[i];
     }
-    asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
-
+    // Results through LDS, 32*GN rows of y at a time, so that they leave as whole lines: written from the registers, eight bytes of each
+    // of 32 rows an instruction, they took 10 us a tile.  A row's pitch of 16 bytes more spreads rows over the banks.
+    constexpr int PIECE = 16 / (int)sizeof(T), PITCH = G::BM * (int)sizeof(T) + 16, ROWS = 32 * GN, PIECES = G::BM / PIECE;
+    static_assert(ROWS * PITCH <= (int)sizeof(lds), "room for the results");
+    f32x4 b[FM][4] = {};
+    if (bias) {
 #pragma unroll
-    for (int i = 0; i < FM; ++i)
+        for (int i = 0; i < FM; ++i)
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const long long k = k0 + wm * 32 * FM + i * 32 + g * 8 + half * 4;
-            f32x4 b = {0.f, 0.f, 0.f, 0.f};
-            if (bias) {
+            for (int g = 0; g < 4; ++g)
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (k + e < K) b[e] = bias[k + e];
-            }
+                for (int e = 0; e < 4; ++e) {
+                    const long long k = k0 + wm * 32 * FM + i * 32 + g * 8 + half * 4 + e;
+                    if (k < K) b[i][g][e] = bias[k];
+                }
+    }
 #pragma unroll
-            for (int j = 0; j < FN; ++j) {
-                const long long n = n0 + wn * 32 * FN + j * 32 + (lane & 31);
-                if (n >= N) continue;
-                T *to = y + (size_t)n * K + k;
+    for (int j = 0; j < FN; ++j) {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" : : : "memory");       // nothing under way into, or read from, what is written now
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
                 float v[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    v[e] = acc[i][j][g * 4 + e] + b[e];
+                    v[e] = acc[i][j][g * 4 + e] + b[i][g][e];
                     if (relu && v[e] < 0.f) v[e] = 0.f;
                 }
-                if (K % 4 == 0) {
-                    if (k >= K) continue;
-                    if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2 *>(to) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
-                    else *reinterpret_cast<float4 *>(to) = make_float4(v[0], v[1], v[2], v[3]);
-                } else {
+                unsigned char *to = lds + (wn * 32 + (lane & 31)) * PITCH + (wm * 32 * FM + i * 32 + g * 8 + half * 4) * (int)sizeof(T);
+                if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2 *>(to) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+                else *reinterpret_cast<float4 *>(to) = make_float4(v[0], v[1], v[2], v[3]);
+            }
+        __syncthreads();
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (k + e < K) store_one(to + e, v[e]);
-                }
+        for (int u = 0; u < ROWS * PIECES / (64 * G::WAVES); ++u) {
+            const int at = u * 64 * G::WAVES + (int)threadIdx.x, row = at / PIECES, piece = at % PIECES;
+            const long long n = n0 + (row >> 5) * 32 * FN + j * 32 + (row & 31), k = k0 + piece * PIECE;
+            const uint4 q = *reinterpret_cast<const uint4 *>(lds + row * PITCH + piece * 16);
+            const u32x4_any v = {q.x, q.y, q.z, q.w};
+            if (n >= N || k >= K) continue;
+            T *to = y + (size_t)n * K + k;
+            if (k + PIECE <= K) *reinterpret_cast<u32x4_any *>(to) = v;
+            else {
+#pragma unroll
+                for (int e = 0; e < PIECE; ++e)
+                    if (k + e < K) {
+                        if constexpr (sizeof(T) == 2) to[e] = (bf16_t)(v[e / 2] >> (16 * (e & 1)));
+                        else to[e] = __uint_as_float(v[e]);
+                    }
             }
         }
+    }
 }
 
 // ---- host -----------------------------------------------------------------------------------------------------------------
