@@ -191,15 +191,17 @@ struct Row {
     // all pieces of [piece, piece + n) lie wholly in the row
     __device__ __forceinline__ bool whole(int piece, int n) const { return piece * V >= head && (piece + n) * V <= K + head; }
     // Places outside the row get minus infinity; low: the lowest value of pieces that are not whole.
-    __device__ __forceinline__ Piece<T> load(int piece, float &low) const
+    __device__ __forceinline__ Piece<T> load(int piece, float &low) const { return load(piece, low, pieces); }
+    // as if the row ended before piece `end`
+    __device__ __forceinline__ Piece<T> load(int piece, float &low, int end) const
     {
         Piece<T> p;
-        if (whole(piece)) {
+        if (whole(piece) && piece < end) {
             const uint4 u = reinterpret_cast<const uint4 *>(z)[(unsigned)piece];
             p.w[0] = u.x; p.w[1] = u.y; p.w[2] = u.z; p.w[3] = u.w;
         } else {
             p.nothing();
-            if (piece < pieces) {
+            if (piece < end) {
 #pragma unroll
                 for (int k = 0; k < V; ++k) {
                     const int i = piece * V + k;
@@ -292,6 +294,19 @@ __device__ __forceinline__ unsigned wave_bound(const unsigned *cell, int n)
     return t;
 }
 
+template <int W, class Emit>
+__device__ __forceinline__ void rank_candidates(const TopShared &sh, int n, int top, Emit emit)
+{
+    for (int i = threadIdx.x; i < n; i += 64 * W) {
+        const unsigned long long key = sh.list[i];
+        int rank = 0;
+#pragma unroll 4
+        for (int j = 0; j < n; ++j) rank += sh.list[j] > key ? 1 : 0;
+        if (rank < top) emit(rank, key);
+    }
+    for (int i = n + (int)threadIdx.x; i < top; i += 64 * W) emit(i, NO_KEY);
+}
+
 // Hands the i-th largest key of the row to emit(i, key); places past the last value get NO_KEY.  Called by a whole workgroup of W waves;
 // cell: this lane's S cells.  each(from, f) calls f(order, index) for each of the thread's values that reaches `from`.
 template <int W, int S, int LOW, class Each, class Emit>
@@ -318,19 +333,22 @@ __device__ __forceinline__ void select_top(TopShared &sh, const unsigned *cell, 
     // Values above the bound, and equal ones up to index `tie`.  Where there are many equal ones (rows of one value, rows where few tokens are
     // allowed) a second turn takes only the lowest indices of those at the bound: each lane's first one is a cell again.
     unsigned tie = 0xFFFFFFFFu, first = 0xFFFFFFFFu;
+    bool full = false;      // the list was, when this lane last had something for it
     int n;
     for (int turn = 0;; ++turn) {
         each(bound, [&](unsigned o, unsigned index) {
             const bool at_bound = o >> LOW == bound >> LOW;
-            if (!at_bound || index <= tie) {
+            if (!full && (!at_bound || index <= tie)) {
                 const int at = atomicAdd(&sh.count, 1);
                 if (at < CAP) sh.list[at] = key_of(o, index);
+                full = at >= CAP;
             }
             if (at_bound) first = min(first, index);
         });
         __syncthreads();
         n = sh.count;
         if (n <= CAP || turn == 1) break;
+        full = false;
         const unsigned cells[1] = {~first};
         tie = ~wave_bound<1, 0>(cells, top);        // (no less than top of them: those above the bound may be none)
         __syncthreads();
@@ -344,13 +362,7 @@ __device__ __forceinline__ void select_top(TopShared &sh, const unsigned *cell, 
             __syncthreads();
     }
     if (n <= CAP) {
-        for (int i = threadIdx.x; i < n; i += 64 * W) {
-            const unsigned long long key = sh.list[i];
-            int rank = 0;
-            for (int j = 0; j < n; ++j) rank += sh.list[j] > key ? 1 : 0;
-            if (rank < top) emit(rank, key);
-        }
-        for (int i = n + (int)threadIdx.x; i < top; i += 64 * W) emit(i, NO_KEY);
+        rank_candidates<W>(sh, n, top, emit);
         return;
     }
     // the largest values crowd in a few threads' pieces: one after the other
@@ -574,81 +586,265 @@ __global__ __launch_bounds__(G < 64 ? 256 : G, G == 512 && P == 16 ? 4 : 1) void
     }
 }
 
-// ---- rows in chunks -------------------------------------------------------------------------------------------------------
+// what a row's sums say
+struct Joined {
+    float m, s, t;
+};
+template <typename T>
+__device__ __forceinline__ void write_row_results(const LogprobArgs &a, size_t row, float zl, const Joined &j)
+{
+    const int label = a.labels ? a.labels[row] : -1;
+    const bool given = (unsigned)label < (unsigned)a.K, empty = j.s == 0.f;
+    const float ls = empty ? 0.f : log2f(j.s);
+    const Scale sc(a.scale, j.m);
+    if (a.logp) a.logp[row] = !given ? 0.f : empty ? -INFINITY : (sc.d2<false>(zl) - ls) * LN2;
+    if (a.entropy) a.entropy[row] = empty ? 0.f : (ls - j.t / j.s) * LN2;
+    if (a.stats) {
+        a.stats[2 * row] = empty ? -INFINITY : j.m;
+        a.stats[2 * row + 1] = ls * LN2;
+    }
+}
+__device__ __forceinline__ void write_top(const LogprobArgs &a, size_t row, const Joined &j, int i, unsigned long long key)
+{
+    const bool none = key == NO_KEY;
+    a.top_index[row * a.top + i] = none ? -1 : (int)key_index(key);
+    a.top_logp[row * a.top + i] = none || j.s == 0.f ? -INFINITY : (Scale(a.scale, j.m).d2<false>(unorder((unsigned)(key >> 32))) - log2f(j.s)) * LN2;
+}
 
-constexpr int CHUNK_THREADS = 256;
+// ---- rows that stream by --------------------------------------------------------------------------------------------------
+// Without a gradient nothing has to be held: a thread keeps a maximum, and the sums at it, as its pieces pass; four pieces at a time, whose
+// values are unpacked once for the maximum and the sums.  Few registers, so that a compute unit has eight workgroups at different places
+// of their rows, where rows held in registers leave it two that wait for each other's barriers (4096 rows of 50257: 134 us so).
+// A row is one chunk, or several where there are few rows: chunks leave a Part each, which a second launch joins.
+
+constexpr int CHUNK_THREADS = 256, UNROLL = 4;
 
 struct Part {       // of a chunk: its largest value, its sums, and the label's logit where it lies there
     float m, s, t, zl;
 };
 
-template <typename T, int P, bool TOP>
-__global__ __launch_bounds__(CHUNK_THREADS) void logprob_chunk_kernel(LogprobArgs a, int chunks, Part *parts, unsigned long long *keys)
+// The values of a chunk once more, from memory, for the rare rows whose candidates do not fit their list: cells are every fourth of a
+// thread's pieces.
+template <typename T>
+struct Streamed {
+    const Row<T> &r;
+    int begin, end, K;
+    const unsigned *cell;
+    template <class F>
+    __device__ __forceinline__ void operator()(unsigned from, F f) const
+    {
+        constexpr int AHEAD = 4, STEP = UNROLL * CHUNK_THREADS;
+        const float limit = unorder(from);      // (NaN for the lowest bounds: then every value is looked at)
+        float low = 0.f;
+        unsigned hits = 0;
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) hits |= cell[u] >= from ? 1u << u : 0u;
+        for (; hits; hits &= hits - 1)
+            for (int at = begin + (__ffs(hits) - 1) * CHUNK_THREADS + (int)threadIdx.x; at < end; at += AHEAD * STEP) {
+                Piece<T> p[AHEAD];
+#pragma unroll
+                for (int i = 0; i < AHEAD; ++i) p[i] = r.load(at + i * STEP, low, end);
+#pragma unroll
+                for (int i = 0; i < AHEAD; ++i) {
+                    if (at + i * STEP >= end || p[i].template largest<true>() < limit) continue;
+                    int first = (at + i * STEP) * Piece<T>::V - r.head;
+                    asm volatile("" : "+v"(first));
+#pragma unroll
+                    for (int k = 0; k < Piece<T>::V; ++k) {
+                        const unsigned o = order(p[i].again(k));
+                        if (o >= from && (unsigned)(first + k) < (unsigned)K) f(o, (unsigned)(first + k));
+                    }
+                }
+            }
+    }
+};
+
+constexpr int HELD = 384;        // pieces that a workgroup sets aside for the most probable tokens
+struct Aside {
+    uint4 piece[HELD];
+    int place[HELD], count;
+    unsigned said[4];
+};
+
+template <typename T, bool TOP>
+__global__ __launch_bounds__(CHUNK_THREADS) void logprob_stream_kernel(LogprobArgs a, int chunks, int chunk_pieces, Part *parts, unsigned long long *keys)
 {
-    constexpr int G = CHUNK_THREADS, V = Piece<T>::V, S = P < 4 ? P : 4;
+    constexpr int V = Piece<T>::V, LOW = sizeof(T) == 2 ? 16 : 0;
     __shared__ float red[3][4];
     const size_t row = blockIdx.x / (unsigned)chunks;
-    const int chunk = blockIdx.x % (unsigned)chunks;
+    const int chunk = blockIdx.x % (unsigned)chunks, wave = threadIdx.x >> 6;
     const Row<T> r(a, row);
-    const int piece0 = chunk * (G * P), held = min(P, (r.pieces - piece0 + G - 1) / G);
-    Piece<T> p[P];
-    float low = 0.f;        // (above nothing that matters)
+    const int begin = chunk * chunk_pieces, end = min(begin + chunk_pieces, r.pieces);
+    const float k2 = a.scale * LOG2E;
+    // the sums are those of exp2((z - m)*k2 + shift): shift is what the rounding of m*k2 moves them by (see Scale)
+    float m = LOWEST, shift = 0.f, s = 0.f, t = 0.f, low = 0.f;
+
+    // Candidates for the most probable tokens: pieces with a value that reaches a bound which `top` values have reached so far are set aside as they
+    // pass.  The bound comes from what each wave says of its lanes' maxima (top/4 lanes have reached it), before the first turn and
+    // after 1, 2, 4, ...; a wave may read an older word of another one, which is a bound too.  Minus infinities are never set aside.
+    __shared__ Aside aside;
+    float limit = LOWEST, seen = -INFINITY, of[UNROLL];
+    int turn = 0;
+    bool bounded = true;
+    auto say = [&]() {
+        const unsigned cells[1] = {order(seen)};
+        const unsigned b = wave_bound<1, LOW>(cells, (a.top + 3) / 4);
+        if ((threadIdx.x & 63) == 0) *(volatile unsigned *)&aside.said[wave] = b;
+    };
+    auto hear = [&]() {
+        const volatile unsigned *said = aside.said;
+        const unsigned b = min(min(said[0], said[1]), min(said[2], said[3]));
+        bounded = b >> LOW > order(-INFINITY) >> LOW;
+        limit = bounded ? unorder(b) : LOWEST;
+        return b;
+    };
+    if constexpr (TOP) {
+        if (threadIdx.x == 0) aside.count = 0;
 #pragma unroll
-    for (int q = 0; q < P; ++q) p[q] = r.load(piece0 + q * G + (int)threadIdx.x, low);
-    float top_of[S], m = LOWEST;
-    unsigned cell[S];
-#pragma unroll
-    for (int q = 0; q < P; ++q) {
-        const float x = p[q].template largest<false>();
-        top_of[q % S] = q < S ? x : max3(top_of[q % S], x, x);
+        for (int u = 0; u < UNROLL; ++u) of[u] = -INFINITY;
     }
+    Piece<T> p[UNROLL];
 #pragma unroll
-    for (int s = 0; s < S; ++s) {
-        cell[s] = order(top_of[s]);
-        m = fmaxf(m, top_of[s]);
+    for (int u = 0; u < UNROLL; ++u) p[u] = r.load(begin + u * CHUNK_THREADS + (int)threadIdx.x, low, end);
+    if constexpr (TOP) {
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) seen = fmaxf(seen, p[u].template largest<true>());
+        say();
+        __syncthreads();
+        hear();
     }
-    const int wave = threadIdx.x >> 6;
-    m = meet<64>(m, larger);
-    if ((threadIdx.x & 63) == 0) red[0][wave] = m;
-    __syncthreads();
-    m = max3(max3(red[0][0], red[0][1], red[0][2]), red[0][3], LOWEST);
-    const Scale sc(a.scale, m);
-    float s = 0.f, t = 0.f;
+    for (int base = begin; base < end; base += UNROLL * CHUNK_THREADS) {
+        Piece<T> c[UNROLL];
+        const int next = base + UNROLL * CHUNK_THREADS;
 #pragma unroll
-    for (int q = 0; q < P; ++q) {
+        for (int u = 0; u < UNROLL; ++u) {
+            c[u] = p[u];
+            if (next < end) p[u] = r.load(next + u * CHUNK_THREADS + (int)threadIdx.x, low, end);
+        }
+        float z[UNROLL][V], most = m;
 #pragma unroll
-        for (int k = 0; k < V; ++k) {
-            const float d = sc.d2<false>(p[q].again(k)), e = __builtin_amdgcn_exp2f(d);
-            s += e;
-            t = fmaf(e, fmaxf(d, NO_WEIGHT), t);
+        for (int u = 0; u < UNROLL; ++u) {
+#pragma unroll
+            for (int k = 0; k < V; ++k) z[u][k] = c[u].at(k);
+            float x = z[u][0];
+#pragma unroll
+            for (int k = 1; k + 1 < V; k += 2) x = max3(x, z[u][k], z[u][k + 1]);
+            x = max3(x, z[u][V - 1], z[u][V - 1]);
+            most = fmaxf(most, x);
+            if constexpr (TOP) {
+                of[u] = fmaxf(of[u], x);
+                if (x >= limit) {
+                    const int at = atomicAdd(&aside.count, 1);
+                    if (at < HELD) {
+                        aside.piece[at] = make_uint4(c[u].w[0], c[u].w[1], c[u].w[2], c[u].w[3]);
+                        aside.place[at] = base + u * CHUNK_THREADS + (int)threadIdx.x;
+                    } else
+                        limit = INFINITY;       // too many: they are looked for once more below
+                }
+            }
+        }
+        // the sums so far at the new maximum
+        const Scale sc(a.scale, most);
+        const bool near = __ballot(!sc.near) == 0;
+        const float to = near ? fmaf(most, k2, sc.c) : 0.f;
+        const float down = fmaxf(fmaf(m - most, k2, to - shift), NO_WEIGHT), by = __builtin_amdgcn_exp2f(down);
+        t = fmaf(down, s, t) * by;
+        s *= by;
+        m = most;
+        shift = to;
+        auto sums = [&](auto near) {
+#pragma unroll
+            for (int u = 0; u < UNROLL; ++u)
+#pragma unroll
+                for (int k = 0; k < V; ++k) {
+                    const float d = sc.d2<decltype(near)::value>(z[u][k]), e = __builtin_amdgcn_exp2f(d);
+                    s += e;
+                    t = fmaf(e, weight<true>(d), t);
+                }
+        };
+        if (near) sums(std::true_type());
+        else sums(std::false_type());
+        if constexpr (TOP) {
+            ++turn;
+            if ((turn & (turn - 1)) == 0 && next < end && limit < INFINITY) {
+                seen = max3(max3(of[0], of[1], of[2]), of[3], seen);
+                say();
+                hear();
+            }
         }
     }
-    s = meet<64>(s, sum);
-    t = meet<64>(t, sum);
+    if constexpr (TOP) {
+        seen = max3(max3(of[0], of[1], of[2]), of[3], seen);
+        say();
+    }
+    float most = meet<64>(m, larger);
+    if ((threadIdx.x & 63) == 0) red[0][wave] = most;
+    __syncthreads();
+    most = max3(max3(red[0][0], red[0][1], red[0][2]), red[0][3], LOWEST);
+    const float down = fmaxf(fmaf(m - most, k2, -shift), NO_WEIGHT), by = __builtin_amdgcn_exp2f(down);
+    t = meet<64>(fmaf(down, s, t) * by, sum);
+    s = meet<64>(s * by, sum);
     if ((threadIdx.x & 63) == 0) {
         red[1][wave] = s;
         red[2][wave] = t;
     }
+    __shared__ TopShared sh;
+    if (TOP && threadIdx.x == 0) sh.count = 0;
     __syncthreads();
+    const Joined j{most, red[1][0] + red[1][1] + red[1][2] + red[1][3], red[2][0] + red[2][1] + red[2][2] + red[2][3]};
     if (threadIdx.x == 0) {
-        const int label = a.labels ? a.labels[row] : -1, at = label + r.head - piece0 * V;
-        const bool here = (unsigned)label < (unsigned)a.K && (unsigned)at < (unsigned)(G * P * V);
-        parts[blockIdx.x] = Part{m, red[1][0] + red[1][1] + red[1][2] + red[1][3], red[2][0] + red[2][1] + red[2][2] + red[2][3],
-                                 here ? load_f32(r.z + r.head + label) : 0.f};
+        const int label = a.labels ? a.labels[row] : -1, at = (label + r.head) / V;
+        const bool here = (unsigned)label < (unsigned)a.K && at >= begin && at < end;
+        const float zl = here ? load_f32(r.z + r.head + label) : 0.f;
+        if (parts) parts[blockIdx.x] = Part{j.m, j.s, j.t, zl};
+        else write_row_results<T>(a, row, zl, j);
     }
     if constexpr (TOP) {
-        __shared__ TopShared sh;
-        select_top<4, S, sizeof(T) == 2 ? 16 : 0>(
-            sh, cell, a.top,
-            [&](unsigned from, auto f) { each_value<T, P>(p, held, (piece0 + (int)threadIdx.x) * V - r.head, G * V, a.K, from, f); },
-            [&](int i, unsigned long long key) { keys[(size_t)blockIdx.x * a.top + i] = key; });
+        auto emit = [&](int i, unsigned long long key) {
+            if (parts) keys[(size_t)blockIdx.x * a.top + i] = key;
+            else write_top(a, row, j, i, key);
+        };
+        const int first = max(begin * V - r.head, 0), values = min(end * V - r.head, a.K) - first;
+        if (j.s == 0.f) {       // minus infinities alone
+            if ((int)threadIdx.x < a.top) emit(threadIdx.x, (int)threadIdx.x < values ? key_of(order(-INFINITY), (unsigned)(first + (int)threadIdx.x)) : NO_KEY);
+            return;
+        }
+        // what reaches the bound of the whole
+        const unsigned bound = hear();
+        const int pieces = aside.count;
+        if (pieces <= HELD) {
+            for (int i = threadIdx.x; i < pieces; i += CHUNK_THREADS) {
+                const uint4 u = aside.piece[i];
+                const Piece<T> q = {{u.x, u.y, u.z, u.w}};
+                const int at = aside.place[i] * V - r.head;
+#pragma unroll
+                for (int k = 0; k < V; ++k) {
+                    const unsigned o = order(q.at(k));
+                    if (q.at(k) >= limit && o >= bound && (unsigned)(at + k) < (unsigned)a.K) {
+                        const int to = atomicAdd(&sh.count, 1);
+                        if (to < CAP) sh.list[to] = key_of(o, (unsigned)(at + k));
+                    }
+                }
+            }
+            __syncthreads();
+            const int n = sh.count;
+            if (n <= CAP && (bounded || n >= a.top || n >= values)) {
+                rank_candidates<4>(sh, n, a.top, emit);
+                return;
+            }
+        }
+        // too many of them, or minus infinities are among the most probable
+        __syncthreads();
+        unsigned cell[UNROLL];
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) cell[u] = begin + u * CHUNK_THREADS + (int)threadIdx.x < end ? order(of[u]) : 0u;
+        select_top<4, UNROLL, LOW>(sh, cell, a.top, Streamed<T>{r, begin, end, a.K, cell}, emit);
     }
 }
 
+// ---- chunks ---------------------------------------------------------------------------------------------------------------
+
 // the chunks' sums at the row's maximum, in the chunks' order within each thread and the threads' in a fixed one
-struct Joined {
-    float m, s, t;
-};
 template <int W>
 __device__ __forceinline__ Joined join_parts(const Part *parts, int chunks, float scale, float (*red)[W])
 {
@@ -684,32 +880,22 @@ __device__ __forceinline__ Joined join_parts(const Part *parts, int chunks, floa
     return j;
 }
 
+// the label's logit as its chunk found it
 template <typename T>
-__device__ __forceinline__ void write_row_results(const LogprobArgs &a, size_t row, const Part *parts, int span, const Joined &j)
+__device__ __forceinline__ float label_logit(const LogprobArgs &a, size_t row, const Part *parts, int chunk_pieces)
 {
     const int label = a.labels ? a.labels[row] : -1;
-    const bool given = (unsigned)label < (unsigned)a.K, empty = j.s == 0.f;
-    const float ls = empty ? 0.f : log2f(j.s);
-    const Scale sc(a.scale, j.m);
-    if (a.logp) {
-        const float zl = given ? parts[(label + Row<T>(a, row).head) / span].zl : 0.f;
-        a.logp[row] = !given ? 0.f : empty ? -INFINITY : (sc.d2<false>(zl) - ls) * LN2;
-    }
-    if (a.entropy) a.entropy[row] = empty ? 0.f : (ls - j.t / j.s) * LN2;
-    if (a.stats) {
-        a.stats[2 * row] = empty ? -INFINITY : j.m;
-        a.stats[2 * row + 1] = ls * LN2;
-    }
+    return (unsigned)label < (unsigned)a.K ? parts[(label + Row<T>(a, row).head) / Piece<T>::V / chunk_pieces].zl : 0.f;
 }
 
 template <typename T>
-__global__ __launch_bounds__(256) void logprob_join_kernel(LogprobArgs a, int chunks, int span, const Part *parts, const unsigned long long *keys)
+__global__ __launch_bounds__(256) void logprob_join_kernel(LogprobArgs a, int chunks, int chunk_pieces, const Part *parts, const unsigned long long *keys)
 {
     __shared__ float red[3][4];
     const size_t row = blockIdx.x;
     parts += row * chunks;
     const Joined j = join_parts<4>(parts, chunks, a.scale, red);
-    if (threadIdx.x == 0) write_row_results<T>(a, row, parts, span, j);
+    if (threadIdx.x == 0) write_row_results<T>(a, row, label_logit<T>(a, row, parts, chunk_pieces), j);
     if (a.top == 0) return;
     __shared__ TopShared sh;
     keys += row * chunks * a.top;
@@ -720,9 +906,6 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(LogprobArgs a, int ch
 #pragma unroll
         for (int c = 0; c < 4; ++c) cell[c] = c == s ? max(cell[c], o) : cell[c];
     }
-    const bool empty = j.s == 0.f;
-    const float ls = empty ? 0.f : log2f(j.s);
-    const Scale sc(a.scale, j.m);
     select_top<4, 4, sizeof(T) == 2 ? 16 : 0>(
         sh, cell, a.top,
         [&](unsigned from, auto f) {
@@ -732,15 +915,12 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(LogprobArgs a, int ch
                 if (key != NO_KEY && (unsigned)(key >> 32) >= from) f((unsigned)(key >> 32), key_index(key));
             }
         },
-        [&](int i, unsigned long long key) {
-            a.top_index[row * a.top + i] = key == NO_KEY ? -1 : (int)key_index(key);
-            a.top_logp[row * a.top + i] = key == NO_KEY || empty ? -INFINITY : (sc.d2<false>(unorder((unsigned)(key >> 32))) - ls) * LN2;
-        });
+        [&](int i, unsigned long long key) { write_top(a, row, j, i, key); });
 }
 
-// the gradient of a chunk's values: e2 = log2 of the probability up to ls, mean: T/S in d2's units
+// the gradient of a workgroup's 256*P pieces; mean: T/S in d2's units
 template <typename T, int P>
-__device__ __forceinline__ void chunk_gradient(const LogprobArgs &a, size_t row, int chunk, float m, float s, float mean, bool empty)
+__device__ __forceinline__ void block_gradient(const LogprobArgs &a, size_t row, int block, float m, float s, float mean, bool empty)
 {
     constexpr int V = Piece<T>::V;
     const Row<T> r(a, row);
@@ -750,7 +930,7 @@ __device__ __forceinline__ void chunk_gradient(const LogprobArgs &a, size_t row,
     const float dl = a.dlogp && given ? a.dlogp[row] : 0.f, dh = a.dentropy ? a.dentropy[row] : 0.f;
     const float per = a.scale / s, A = per * (dh * (mean * LN2) - dl), B = -per * dh * LN2;
     const int place = given ? label + r.head : -1;
-    const int piece0 = chunk * (CHUNK_THREADS * P) + (int)threadIdx.x;
+    const int piece0 = block * (CHUNK_THREADS * P) + (int)threadIdx.x;
     Piece<T> p[P];
     float low = 0.f;        // (above nothing that matters)
 #pragma unroll
@@ -770,23 +950,23 @@ __device__ __forceinline__ void chunk_gradient(const LogprobArgs &a, size_t row,
 }
 
 template <typename T, int P>
-__global__ __launch_bounds__(CHUNK_THREADS) void logprob_gradient_kernel(LogprobArgs a, int chunks, int span, const Part *parts)
+__global__ __launch_bounds__(CHUNK_THREADS) void logprob_gradient_kernel(LogprobArgs a, int blocks, int chunks, int chunk_pieces, const Part *parts)
 {
     __shared__ float red[3][4];
-    const size_t row = blockIdx.x / (unsigned)chunks;
-    const int chunk = blockIdx.x % (unsigned)chunks;
+    const size_t row = blockIdx.x / (unsigned)blocks;
+    const int block = blockIdx.x % (unsigned)blocks;
     parts += row * chunks;
     const Joined j = join_parts<4>(parts, chunks, a.scale, red);
-    if (chunk == 0 && threadIdx.x == 0) write_row_results<T>(a, row, parts, span, j);
-    chunk_gradient<T, P>(a, row, chunk, j.m, j.s, j.t / j.s, j.s == 0.f);
+    if (block == 0 && threadIdx.x == 0) write_row_results<T>(a, row, label_logit<T>(a, row, parts, chunk_pieces), j);
+    block_gradient<T, P>(a, row, block, j.m, j.s, j.t / j.s, j.s == 0.f);
 }
 
 template <typename T, int P>
-__global__ __launch_bounds__(CHUNK_THREADS) void logprob_bwd_kernel(LogprobArgs a, int chunks, const float *stats, const float *entropy)
+__global__ __launch_bounds__(CHUNK_THREADS) void logprob_bwd_kernel(LogprobArgs a, int blocks, const float *stats, const float *entropy)
 {
-    const size_t row = blockIdx.x / (unsigned)chunks;
+    const size_t row = blockIdx.x / (unsigned)blocks;
     const float m = stats[2 * row], ls = stats[2 * row + 1];
-    chunk_gradient<T, P>(a, row, blockIdx.x % (unsigned)chunks, m, expf(ls), entropy ? (ls - entropy[row]) * LOG2E : 0.f, m == -INFINITY);
+    block_gradient<T, P>(a, row, blockIdx.x % (unsigned)blocks, m, expf(ls), entropy ? (ls - entropy[row]) * LOG2E : 0.f, m == -INFINITY);
 }
 
 // ---- host -----------------------------------------------------------------------------------------------------------------
@@ -800,15 +980,23 @@ int row_pieces(int K, int dtype, int ld)
 constexpr int ANY_LD = 1;
 
 constexpr int ROW_PIECES = 16384;       // in registers: 16 of each of 1024 threads
+constexpr int SHORT_PIECES = 1024;      // rows that are held in registers without a gradient too
 
-// chunks of a row (0: rows in registers).  Pieces a thread of a chunk: 1 or 8.
-int chunk_pieces(int N, int pieces)
+// How a row is cut where it is not held: chunks, and pieces of each.
+struct Cut {
+    int chunks, pieces;     // chunks 0: rows are held
+};
+Cut cut_rows(int N, int pieces, bool gradient)
 {
-    if (pieces > ROW_PIECES) return N < 64 ? 1 : 8;
-    if (pieces > 1024 && N < 64) return 1;
-    return 0;
+    if (pieces <= SHORT_PIECES || (gradient && pieces <= ROW_PIECES && N >= 64)) return Cut{0, 0};
+    int chunks = N >= 256 ? 1 : (1024 + N - 1) / N;
+    chunks = chunks < (pieces + CHUNK_THREADS - 1) / CHUNK_THREADS ? chunks : (pieces + CHUNK_THREADS - 1) / CHUNK_THREADS;
+    Cut c;
+    c.pieces = ((pieces + chunks - 1) / chunks + CHUNK_THREADS - 1) / CHUNK_THREADS * CHUNK_THREADS;
+    c.chunks = (pieces + c.pieces - 1) / c.pieces;
+    return c;
 }
-int chunk_count(int pieces, int per_thread) { return (int)((pieces + (long long)CHUNK_THREADS * per_thread - 1) / (CHUNK_THREADS * per_thread)); }
+int block_count(int pieces, int per_thread) { return (int)((pieces + (long long)CHUNK_THREADS * per_thread - 1) / (CHUNK_THREADS * per_thread)); }
 
 template <typename T, bool TOP>
 void launch_row(const LogprobArgs &a, hipStream_t st)
@@ -822,48 +1010,50 @@ void launch_row(const LogprobArgs &a, hipStream_t st)
     if (pieces <= 64) hipLaunchKernelGGL((logprob_row_kernel<T, 64, 1, TOP>), rows, dim3(64), 0, st, a);
     else if (pieces <= 256) hipLaunchKernelGGL((logprob_row_kernel<T, 64, 4, TOP>), rows, dim3(64), 0, st, a);
     else if (pieces <= 512) hipLaunchKernelGGL((logprob_row_kernel<T, 256, 2, TOP>), rows, dim3(256), 0, st, a);
-    else if (pieces <= 1024) hipLaunchKernelGGL((logprob_row_kernel<T, 256, 4, TOP>), rows, dim3(256), 0, st, a);
-    else if (pieces <= 2048) hipLaunchKernelGGL((logprob_row_kernel<T, 256, 8, TOP>), rows, dim3(256), 0, st, a);
-    else if (pieces <= 4096) hipLaunchKernelGGL((logprob_row_kernel<T, 512, 8, TOP>), rows, dim3(512), 0, st, a);
-    else if (pieces <= 8192) hipLaunchKernelGGL((logprob_row_kernel<T, 512, 16, TOP>), rows, dim3(512), 0, st, a);
-    else hipLaunchKernelGGL((logprob_row_kernel<T, 1024, 16, TOP>), rows, dim3(1024), 0, st, a);
+    else if (TOP || pieces <= 1024) hipLaunchKernelGGL((logprob_row_kernel<T, 256, 4, TOP>), rows, dim3(256), 0, st, a);
+    else if (pieces <= 2048) hipLaunchKernelGGL((logprob_row_kernel<T, 256, 8, false>), rows, dim3(256), 0, st, a);
+    else if (pieces <= 4096) hipLaunchKernelGGL((logprob_row_kernel<T, 512, 8, false>), rows, dim3(512), 0, st, a);
+    else if (pieces <= 8192) hipLaunchKernelGGL((logprob_row_kernel<T, 512, 16, false>), rows, dim3(512), 0, st, a);
+    else hipLaunchKernelGGL((logprob_row_kernel<T, 1024, 16, false>), rows, dim3(1024), 0, st, a);
 }
 
 template <typename T>
 int launch(const LogprobArgs &a, void *workspace, hipStream_t st)
 {
-    const int pieces = row_pieces(a.K, a.dtype, a.ld), per = chunk_pieces(a.N, pieces);
-    if (per == 0) {
+    const int pieces = row_pieces(a.K, a.dtype, a.ld);
+    const Cut cut = cut_rows(a.N, pieces, a.dz != nullptr);
+    if (cut.chunks == 0) {
         if (a.top) launch_row<T, true>(a, st);
         else launch_row<T, false>(a, st);
         return hipGetLastError() == hipSuccess ? MXC_OK : MXC_ERR_LAUNCH;
     }
-    const int chunks = chunk_count(pieces, per), span = CHUNK_THREADS * per * Piece<T>::V;
-    const size_t grid = (size_t)a.N * chunks;
-    if (grid > 0x7FFFFFFFu || (size_t)chunks * (a.top ? a.top : 1) > 0x7FFFFFFFu) return MXC_ERR_SHAPE;
-    Part *parts = (Part *)workspace;
+    const size_t grid = (size_t)a.N * cut.chunks;
+    const int per = pieces <= 2048 || a.N < 64 ? 1 : 4, blocks = block_count(pieces, per);
+    if (grid > 0x7FFFFFFFu || (size_t)cut.chunks * (a.top ? a.top : 1) > 0x7FFFFFFFu || (a.dz && (size_t)a.N * blocks > 0x7FFFFFFFu)) return MXC_ERR_SHAPE;
+    const bool alone = cut.chunks == 1 && !a.dz;
+    Part *parts = alone ? nullptr : (Part *)workspace;
     unsigned long long *keys = (unsigned long long *)((char *)workspace + align_up(grid * sizeof(Part), 256));
     const dim3 g((unsigned)grid), b(CHUNK_THREADS);
-    if (a.top && per == 1) hipLaunchKernelGGL((logprob_chunk_kernel<T, 1, true>), g, b, 0, st, a, chunks, parts, keys);
-    else if (a.top) hipLaunchKernelGGL((logprob_chunk_kernel<T, 8, true>), g, b, 0, st, a, chunks, parts, keys);
-    else if (per == 1) hipLaunchKernelGGL((logprob_chunk_kernel<T, 1, false>), g, b, 0, st, a, chunks, parts, keys);
-    else hipLaunchKernelGGL((logprob_chunk_kernel<T, 8, false>), g, b, 0, st, a, chunks, parts, keys);
+    if (a.top) hipLaunchKernelGGL((logprob_stream_kernel<T, true>), g, b, 0, st, a, cut.chunks, cut.pieces, parts, keys);
+    else hipLaunchKernelGGL((logprob_stream_kernel<T, false>), g, b, 0, st, a, cut.chunks, cut.pieces, parts, keys);
     if (hipGetLastError() != hipSuccess) return MXC_ERR_LAUNCH;
-    if (!a.dz) hipLaunchKernelGGL(logprob_join_kernel<T>, dim3((unsigned)a.N), dim3(256), 0, st, a, chunks, span, parts, keys);
-    else if (per == 1) hipLaunchKernelGGL((logprob_gradient_kernel<T, 1>), g, b, 0, st, a, chunks, span, parts);
-    else hipLaunchKernelGGL((logprob_gradient_kernel<T, 8>), g, b, 0, st, a, chunks, span, parts);
+    if (alone) return MXC_OK;
+    const dim3 gg((unsigned)((size_t)a.N * blocks));
+    if (!a.dz) hipLaunchKernelGGL(logprob_join_kernel<T>, dim3((unsigned)a.N), dim3(256), 0, st, a, cut.chunks, cut.pieces, parts, keys);
+    else if (per == 1) hipLaunchKernelGGL((logprob_gradient_kernel<T, 1>), gg, b, 0, st, a, blocks, cut.chunks, cut.pieces, parts);
+    else hipLaunchKernelGGL((logprob_gradient_kernel<T, 4>), gg, b, 0, st, a, blocks, cut.chunks, cut.pieces, parts);
     return hipGetLastError() == hipSuccess ? MXC_OK : MXC_ERR_LAUNCH;
 }
 
 template <typename T>
 int launch_bwd(const LogprobArgs &a, const float *stats, const float *entropy, hipStream_t st)
 {
-    const int pieces = row_pieces(a.K, a.dtype, a.ld), per = pieces <= CHUNK_THREADS ? 1 : 4, chunks = chunk_count(pieces, per);
-    const size_t grid = (size_t)a.N * chunks;
+    const int pieces = row_pieces(a.K, a.dtype, a.ld), per = pieces <= CHUNK_THREADS ? 1 : 4, blocks = block_count(pieces, per);
+    const size_t grid = (size_t)a.N * blocks;
     if (grid > 0x7FFFFFFFu) return MXC_ERR_SHAPE;
     const dim3 g((unsigned)grid), b(CHUNK_THREADS);
-    if (per == 1) hipLaunchKernelGGL((logprob_bwd_kernel<T, 1>), g, b, 0, st, a, chunks, stats, entropy);
-    else hipLaunchKernelGGL((logprob_bwd_kernel<T, 4>), g, b, 0, st, a, chunks, stats, entropy);
+    if (per == 1) hipLaunchKernelGGL((logprob_bwd_kernel<T, 1>), g, b, 0, st, a, blocks, stats, entropy);
+    else hipLaunchKernelGGL((logprob_bwd_kernel<T, 4>), g, b, 0, st, a, blocks, stats, entropy);
     return hipGetLastError() == hipSuccess ? MXC_OK : MXC_ERR_LAUNCH;
 }
 
@@ -871,10 +1061,14 @@ int launch_bwd(const LogprobArgs &a, const float *stats, const float *entropy, h
 
 size_t logprob_workspace(int N, int K, int dtype, int top)
 {
-    const int pieces = row_pieces(K, dtype, ANY_LD), per = chunk_pieces(N, pieces);
-    if (per == 0) return 0;
-    const size_t grid = (size_t)N * chunk_count(pieces, per);
-    return align_up(grid * sizeof(Part), 256) + grid * top * sizeof(unsigned long long);
+    size_t need = 0;
+    for (int ld : {0, ANY_LD})      // whatever ld the call has
+        for (bool gradient : {false, true}) {
+            const Cut c = cut_rows(N, row_pieces(K, dtype, ld), gradient);
+            const size_t grid = (size_t)N * c.chunks, bytes = c.chunks == 0 || (c.chunks == 1 && !gradient) ? 0 : align_up(grid * sizeof(Part), 256) + grid * top * sizeof(unsigned long long);
+            need = bytes > need ? bytes : need;
+        }
+    return need;
 }
 
 int logprob_rows(const LogprobArgs &a, void *workspace, hipStream_t st)
