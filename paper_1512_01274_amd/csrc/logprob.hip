@@ -102,6 +102,24 @@ struct Piece {      // 16 bytes of a row
     }
 };
 
+// Lanes of a group of G (8 or a whole wave) meet: exchanges within rows of 16 lanes are part of an instruction (a shuffle through LDS has ten times the
+// latency, and a row of few values is latency), the four rows meet as scalars.  The same order everywhere.
+template <int CONTROL>
+__device__ __forceinline__ float exchanged(float x) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CONTROL, 0xF, 0xF, true)); }
+template <int G, class F>
+__device__ __forceinline__ float meet(float x, F f)
+{
+    x = f(x, exchanged<0xB1>(x));       // lanes 1 0 3 2
+    x = f(x, exchanged<0x4E>(x));       // lanes 2 3 0 1
+    x = f(x, exchanged<0x141>(x));      // the other half of eight
+    if constexpr (G == 8) return x;
+    x = f(x, exchanged<0x140>(x));      // the other half of sixteen
+    auto of_row = [&](int lane) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), lane)); };
+    return f(f(of_row(0), of_row(16)), f(of_row(32), of_row(48)));
+}
+__device__ __forceinline__ float larger(float a, float b) { return fmaxf(a, b); }
+__device__ __forceinline__ float sum(float a, float b) { return a + b; }
+
 // What the first look at a row finds: its largest and its lowest value.  bf16 words are looked at as
 // pairs of 16-bit integers, two values an instruction: of signed ones the largest is the largest value unless all are negative (then it
 // is some value; `sure` is false), of unsigned ones the largest is the most negative value where there is one.  fp32 values are looked at as they are.
@@ -141,7 +159,13 @@ struct Extent<bf16_t> {
         return Word{hi.x > hi.y ? hi.x : hi.y, (short)(u ^ 0x8000u)};
     }
     static __device__ __forceinline__ Word join(Word a, Word b) { return __builtin_elementwise_max(a, b); }
-    static __device__ __forceinline__ Word from_lane(Word a, int mask) { return __builtin_bit_cast(Word, __shfl_xor(__builtin_bit_cast(int, a), mask)); }
+    template <int G>
+    static __device__ __forceinline__ Word meet_lanes(Word a)
+    {
+        return __builtin_bit_cast(Word, meet<G>(__builtin_bit_cast(float, a), [](float x, float y) {
+            return __builtin_bit_cast(float, join(__builtin_bit_cast(Word, x), __builtin_bit_cast(Word, y)));
+        }));
+    }
     static __device__ __forceinline__ float most(Word a) { return __uint_as_float((unsigned)(uint16_t)a.x << 16); }
     static __device__ __forceinline__ bool sure(Word a) { return a.x >= 0; }
     static __device__ __forceinline__ float lowest(Word a) { return __uint_as_float(((uint16_t)a.y ^ 0x8000u) << 16); }
@@ -164,7 +188,11 @@ struct Extent<float> {
     typedef float2 Word;
     __device__ __forceinline__ Word word() const { return make_float2(hi, lo); }
     static __device__ __forceinline__ Word join(Word a, Word b) { return make_float2(fmaxf(a.x, b.x), fminf(a.y, b.y)); }
-    static __device__ __forceinline__ Word from_lane(Word a, int mask) { return make_float2(__shfl_xor(a.x, mask), __shfl_xor(a.y, mask)); }
+    template <int G>
+    static __device__ __forceinline__ Word meet_lanes(Word a)
+    {
+        return make_float2(meet<G>(a.x, [](float x, float y) { return fmaxf(x, y); }), meet<G>(a.y, [](float x, float y) { return fminf(x, y); }));
+    }
     static __device__ __forceinline__ float most(Word a) { return fmaxf(a.x, LOWEST); }
     static __device__ __forceinline__ bool sure(Word) { return true; }
     static __device__ __forceinline__ float lowest(Word a) { return a.y; }
@@ -256,17 +284,6 @@ struct Scale {
 
 template <bool CLAMP>
 __device__ __forceinline__ float weight(float d) { return CLAMP ? fmaxf(d, NO_WEIGHT) : d; }
-
-// lanes of a group of G (a power of two up to a wave) meet
-template <int G, class F>
-__device__ __forceinline__ float meet(float x, F f)
-{
-#pragma unroll
-    for (int d = G / 2; d > 0; d >>= 1) x = f(x, __shfl_xor(x, d));
-    return x;
-}
-__device__ __forceinline__ float larger(float a, float b) { return fmaxf(a, b); }
-__device__ __forceinline__ float sum(float a, float b) { return a + b; }
 
 // ---- the most probable tokens ---------------------------------------------------------------------------------------------
 // Cells are sets of a wave's values, 64 or more of them, of which each lane knows one of the largest.  Where each of W waves has top/W cells that
@@ -464,8 +481,7 @@ __global__ __launch_bounds__(G < 64 ? 256 : G, G == 512 && P == 16 ? 4 : 1) void
 #pragma unroll
     for (int s = 1; s < S; ++s) part[0].look(part[s]);
     typename Extent<T>::Word e = part[0].word();
-#pragma unroll
-    for (int d = (G < 64 ? G : 64) / 2; d > 0; d >>= 1) e = Extent<T>::join(e, Extent<T>::from_lane(e, d));
+    e = Extent<T>::template meet_lanes<(G < 64 ? G : 64)>(e);
     if constexpr (W > 1) {
         if ((threadIdx.x & 63) == 0) ext[threadIdx.x >> 6] = e;
         __syncthreads();
@@ -590,10 +606,8 @@ __global__ __launch_bounds__(G < 64 ? 256 : G, G == 512 && P == 16 ? 4 : 1) void
 struct Joined {
     float m, s, t;
 };
-template <typename T>
-__device__ __forceinline__ void write_row_results(const LogprobArgs &a, size_t row, float zl, const Joined &j)
+__device__ __forceinline__ void write_row_results(const LogprobArgs &a, size_t row, int label, float zl, const Joined &j)
 {
-    const int label = a.labels ? a.labels[row] : -1;
     const bool given = (unsigned)label < (unsigned)a.K, empty = j.s == 0.f;
     const float ls = empty ? 0.f : log2f(j.s);
     const Scale sc(a.scale, j.m);
@@ -619,7 +633,7 @@ __device__ __forceinline__ void write_top(const LogprobArgs &a, size_t row, cons
 
 constexpr int CHUNK_THREADS = 256, UNROLL = 4;
 
-struct Part {       // of a chunk: its largest value, its sums, and the label's logit where it lies there
+struct Part {       // of a chunk: its largest value, its sums, and the label's logit
     float m, s, t, zl;
 };
 
@@ -676,6 +690,9 @@ __global__ __launch_bounds__(CHUNK_THREADS) void logprob_stream_kernel(LogprobAr
     const Row<T> r(a, row);
     const int begin = chunk * chunk_pieces, end = min(begin + chunk_pieces, r.pieces);
     const float k2 = a.scale * LOG2E;
+    // (read first: two accesses that wait for each other)
+    const int label = a.labels ? a.labels[row] : -1;
+    const float zl = (unsigned)label < (unsigned)a.K ? load_f32(r.z + r.head + label) : 0.f;
     // the sums are those of exp2((z - m)*k2 + shift): shift is what the rounding of m*k2 moves them by (see Scale)
     float m = LOWEST, shift = 0.f, s = 0.f, t = 0.f, low = 0.f;
 
@@ -793,11 +810,8 @@ __global__ __launch_bounds__(CHUNK_THREADS) void logprob_stream_kernel(LogprobAr
     __syncthreads();
     const Joined j{most, red[1][0] + red[1][1] + red[1][2] + red[1][3], red[2][0] + red[2][1] + red[2][2] + red[2][3]};
     if (threadIdx.x == 0) {
-        const int label = a.labels ? a.labels[row] : -1, at = (label + r.head) / V;
-        const bool here = (unsigned)label < (unsigned)a.K && at >= begin && at < end;
-        const float zl = here ? load_f32(r.z + r.head + label) : 0.f;
         if (parts) parts[blockIdx.x] = Part{j.m, j.s, j.t, zl};
-        else write_row_results<T>(a, row, zl, j);
+        else write_row_results(a, row, label, zl, j);
     }
     if constexpr (TOP) {
         auto emit = [&](int i, unsigned long long key) {
@@ -880,42 +894,44 @@ __device__ __forceinline__ Joined join_parts(const Part *parts, int chunks, floa
     return j;
 }
 
-// the label's logit as its chunk found it
-template <typename T>
-__device__ __forceinline__ float label_logit(const LogprobArgs &a, size_t row, const Part *parts, int chunk_pieces)
+// What chunks found out about a row.  Their keys are read before their sums are joined; HELD_KEYS of each thread are held, more are read again.
+template <typename T, bool TOP>
+__global__ __launch_bounds__(256) void logprob_join_kernel(LogprobArgs a, int chunks, const Part *parts, const unsigned long long *keys)
 {
-    const int label = a.labels ? a.labels[row] : -1;
-    return (unsigned)label < (unsigned)a.K ? parts[(label + Row<T>(a, row).head) / Piece<T>::V / chunk_pieces].zl : 0.f;
-}
-
-template <typename T>
-__global__ __launch_bounds__(256) void logprob_join_kernel(LogprobArgs a, int chunks, int chunk_pieces, const Part *parts, const unsigned long long *keys)
-{
+    constexpr int HELD_KEYS = 8;
     __shared__ float red[3][4];
     const size_t row = blockIdx.x;
     parts += row * chunks;
-    const Joined j = join_parts<4>(parts, chunks, a.scale, red);
-    if (threadIdx.x == 0) write_row_results<T>(a, row, label_logit<T>(a, row, parts, chunk_pieces), j);
-    if (a.top == 0) return;
-    __shared__ TopShared sh;
-    keys += row * chunks * a.top;
-    const int n = chunks * a.top;       // (fewer than 2^31: logprob_rows)
-    unsigned cell[4] = {0, 0, 0, 0};
-    for (int i = threadIdx.x, s = 0; i < n; i += 256, s = (s + 1) & 3) {
-        const unsigned o = (unsigned)(keys[i] >> 32);
+    const int label = a.labels ? a.labels[row] : -1;
+    const float zl = parts[0].zl;       // (every chunk has it)
+    const int n = chunks * a.top;       // (fewer than 2^31: launch)
+    unsigned long long held[HELD_KEYS];
+    if constexpr (TOP) {
+        keys += row * chunks * a.top;
 #pragma unroll
-        for (int c = 0; c < 4; ++c) cell[c] = c == s ? max(cell[c], o) : cell[c];
+        for (int i = 0; i < HELD_KEYS; ++i) held[i] = i * 256 + (int)threadIdx.x < n ? keys[i * 256 + (int)threadIdx.x] : NO_KEY;
     }
-    select_top<4, 4, sizeof(T) == 2 ? 16 : 0>(
-        sh, cell, a.top,
-        [&](unsigned from, auto f) {
-            if (max(max(cell[0], cell[1]), max(cell[2], cell[3])) < from) return;
-            for (int i = threadIdx.x; i < n; i += 256) {
-                const unsigned long long key = keys[i];
-                if (key != NO_KEY && (unsigned)(key >> 32) >= from) f((unsigned)(key >> 32), key_index(key));
-            }
-        },
-        [&](int i, unsigned long long key) { write_top(a, row, j, i, key); });
+    const Joined j = join_parts<4>(parts, chunks, a.scale, red);
+    if (threadIdx.x == 0) write_row_results(a, row, label, zl, j);
+    if constexpr (TOP) {
+        __shared__ TopShared sh;
+        unsigned cell[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < HELD_KEYS; ++i) cell[i & 3] = max(cell[i & 3], (unsigned)(held[i] >> 32));
+        for (int i = HELD_KEYS * 256 + (int)threadIdx.x; i < n; i += 256) cell[0] = max(cell[0], (unsigned)(keys[i] >> 32));
+        select_top<4, 4, sizeof(T) == 2 ? 16 : 0>(
+            sh, cell, a.top,
+            [&](unsigned from, auto f) {
+                auto look = [&](unsigned long long key) {
+                    if (key != NO_KEY && (unsigned)(key >> 32) >= from) f((unsigned)(key >> 32), key_index(key));
+                };
+                if (__ballot(max(max(cell[0], cell[1]), max(cell[2], cell[3])) >= from) == 0) return;
+#pragma unroll
+                for (int i = 0; i < HELD_KEYS; ++i) look(held[i]);
+                for (int i = HELD_KEYS * 256 + (int)threadIdx.x; i < n; i += 256) look(keys[i]);
+            },
+            [&](int i, unsigned long long key) { write_top(a, row, j, i, key); });
+    }
 }
 
 // the gradient of a workgroup's 256*P pieces; mean: T/S in d2's units
@@ -950,14 +966,16 @@ __device__ __forceinline__ void block_gradient(const LogprobArgs &a, size_t row,
 }
 
 template <typename T, int P>
-__global__ __launch_bounds__(CHUNK_THREADS) void logprob_gradient_kernel(LogprobArgs a, int blocks, int chunks, int chunk_pieces, const Part *parts)
+__global__ __launch_bounds__(CHUNK_THREADS) void logprob_gradient_kernel(LogprobArgs a, int blocks, int chunks, const Part *parts)
 {
     __shared__ float red[3][4];
     const size_t row = blockIdx.x / (unsigned)blocks;
     const int block = blockIdx.x % (unsigned)blocks;
     parts += row * chunks;
+    const int label = a.labels ? a.labels[row] : -1;
+    const float zl = parts[0].zl;       // (the gradient may take z's place)
     const Joined j = join_parts<4>(parts, chunks, a.scale, red);
-    if (block == 0 && threadIdx.x == 0) write_row_results<T>(a, row, label_logit<T>(a, row, parts, chunk_pieces), j);
+    if (block == 0 && threadIdx.x == 0) write_row_results(a, row, label, zl, j);
     block_gradient<T, P>(a, row, block, j.m, j.s, j.t / j.s, j.s == 0.f);
 }
 
@@ -1039,9 +1057,10 @@ int launch(const LogprobArgs &a, void *workspace, hipStream_t st)
     if (hipGetLastError() != hipSuccess) return MXC_ERR_LAUNCH;
     if (alone) return MXC_OK;
     const dim3 gg((unsigned)((size_t)a.N * blocks));
-    if (!a.dz) hipLaunchKernelGGL(logprob_join_kernel<T>, dim3((unsigned)a.N), dim3(256), 0, st, a, cut.chunks, cut.pieces, parts, keys);
-    else if (per == 1) hipLaunchKernelGGL((logprob_gradient_kernel<T, 1>), gg, b, 0, st, a, blocks, cut.chunks, cut.pieces, parts);
-    else hipLaunchKernelGGL((logprob_gradient_kernel<T, 4>), gg, b, 0, st, a, blocks, cut.chunks, cut.pieces, parts);
+    if (!a.dz && a.top) hipLaunchKernelGGL((logprob_join_kernel<T, true>), dim3((unsigned)a.N), dim3(256), 0, st, a, cut.chunks, parts, keys);
+    else if (!a.dz) hipLaunchKernelGGL((logprob_join_kernel<T, false>), dim3((unsigned)a.N), dim3(256), 0, st, a, cut.chunks, parts, keys);
+    else if (per == 1) hipLaunchKernelGGL((logprob_gradient_kernel<T, 1>), gg, b, 0, st, a, blocks, cut.chunks, parts);
+    else hipLaunchKernelGGL((logprob_gradient_kernel<T, 4>), gg, b, 0, st, a, blocks, cut.chunks, parts);
     return hipGetLastError() == hipSuccess ? MXC_OK : MXC_ERR_LAUNCH;
 }
 
