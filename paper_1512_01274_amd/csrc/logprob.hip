@@ -406,6 +406,57 @@ __device__ __forceinline__ void select_top(TopShared &sh, const unsigned *cell, 
     }
 }
 
+// Pieces with a value that may be among the most probable, set aside in LDS.  Minus infinities are left out: limit is LOWEST at least.  From there
+// each thread looks at one value of one piece: short code counts here, for a kernel of few rows is mostly latency, that of fetching its code included.
+constexpr int HELD = 640;
+template <typename T>
+struct Aside {
+    static constexpr int V = Piece<T>::V;
+    T value[HELD][V];
+    int place[HELD], count;
+    unsigned said[16];      // bounds of the waves
+
+    __device__ __forceinline__ bool put(const Piece<T> &p, int piece)
+    {
+        const int at = atomicAdd(&count, 1);
+        if (at >= HELD) return false;
+        *reinterpret_cast<uint4 *>(value[at]) = make_uint4(p.w[0], p.w[1], p.w[2], p.w[3]);
+        place[at] = piece;
+        return true;
+    }
+    // the bound that all of W waves have reached
+    template <int W>
+    __device__ __forceinline__ unsigned hear() const
+    {
+        const volatile unsigned *w = said;
+        unsigned b = w[0];
+#pragma unroll
+        for (int i = 1; i < W; ++i) b = min(b, w[i]);
+        return b;
+    }
+    // Ranks what reaches the bound; false where that is not to be had: too many of them, or minus infinities are among the most probable ones of
+    // `values`.  sh.count is 0.
+    template <int W, int LOW, class Emit>
+    __device__ __forceinline__ bool rank(TopShared &sh, unsigned bound, int head, int K, int top, int values, Emit emit) const
+    {
+        const int pieces = count;
+        if (pieces > HELD) return false;
+        const bool bounded = bound >> LOW > order(-INFINITY) >> LOW;
+        for (int i = threadIdx.x; i < pieces * V; i += 64 * W) {
+            const float z = load_f32(&value[0][0] + i);
+            const int index = place[i / V] * V + i % V - head;
+            if (!(z >= LOWEST) || order(z) < bound || (unsigned)index >= (unsigned)K) continue;
+            const int at = atomicAdd(&sh.count, 1);
+            if (at < CAP) sh.list[at] = key_of(order(z), (unsigned)index);
+        }
+        __syncthreads();
+        const int n = sh.count;
+        if (n > CAP || !(bounded || n >= top || n >= values)) return false;
+        rank_candidates<W>(sh, n, top, emit);
+        return true;
+    }
+};
+
 // The values of a thread's pieces that reach `from`, and the row's index of each: f(order, index).  first: the index of value 0 of piece 0;
 // held: pieces that any thread holds.  A whole wave goes on where no lane has a piece that may reach it.
 template <typename T, int P, class F>
@@ -558,13 +609,29 @@ __global__ __launch_bounds__(G < 64 ? 256 : G, G == 512 && P == 16 ? 4 : 1) void
     }
     if constexpr (TOP) {
         __shared__ TopShared sh;
-        select_top<W, S, sizeof(T) == 2 ? 16 : 0>(
-            sh, cell, a.top,
-            [&](unsigned from, auto f) { each_value<T, P>(p, held, lane * Piece<T>::V - r.head, G * Piece<T>::V, a.K, from, f); },
-            [&](int i, unsigned long long key) {
-                a.top_index[row * a.top + i] = key == NO_KEY ? -1 : (int)key_index(key);
-                a.top_logp[row * a.top + i] = key == NO_KEY || empty ? -INFINITY : (sc.any(unorder((unsigned)(key >> 32))) - ls) * LN2;
-            });
+        __shared__ Aside<T> aside;
+        constexpr int LOW = sizeof(T) == 2 ? 16 : 0;
+        auto emit = [&](int i, unsigned long long key) {
+            a.top_index[row * a.top + i] = key == NO_KEY ? -1 : (int)key_index(key);
+            a.top_logp[row * a.top + i] = key == NO_KEY || empty ? -INFINITY : (sc.any(unorder((unsigned)(key >> 32))) - ls) * LN2;
+        };
+        if (empty) {        // minus infinities alone
+            if (lane < a.top) emit(lane, lane < a.K ? key_of(order(-INFINITY), (unsigned)lane) : NO_KEY);
+            return;
+        }
+        const unsigned mine = wave_bound<S, LOW>(cell, (a.top + W - 1) / W);
+        if ((lane & 63) == 0) aside.said[lane >> 6] = mine;
+        if (lane == 0) aside.count = sh.count = 0;
+        __syncthreads();
+        const unsigned bound = aside.template hear<W>();
+        const float limit = bound >> LOW > order(-INFINITY) >> LOW ? unorder(bound) : LOWEST;
+#pragma unroll
+        for (int q = 0; q < P; ++q)
+            if (q < held && p[q].template largest<true>() >= limit) aside.put(p[q], q * G + lane);
+        __syncthreads();
+        if (aside.template rank<W, LOW>(sh, bound, r.head, a.K, a.top, a.K, emit)) return;
+        __syncthreads();
+        select_top<W, S, LOW>(sh, cell, a.top, [&](unsigned from, auto f) { each_value<T, P>(p, held, lane * Piece<T>::V - r.head, G * Piece<T>::V, a.K, from, f); }, emit);
     } else if (a.dz) {
         const float dl = a.dlogp && given ? a.dlogp[row] : 0.f, dh = a.dentropy ? a.dentropy[row] : 0.f;
         const float per = empty ? 0.f : a.scale / s, A = empty ? 0.f : per * (dh * (mean * LN2) - dl), B = -per * dh * LN2;
@@ -631,7 +698,7 @@ __device__ __forceinline__ void write_top(const LogprobArgs &a, size_t row, cons
 // of their rows, where rows held in registers leave it two that wait for each other's barriers (4096 rows of 50257: 134 us so).
 // A row is one chunk, or several where there are few rows: chunks leave a Part each, which a second launch joins.
 
-constexpr int CHUNK_THREADS = 256, UNROLL = 4;
+constexpr int CHUNK_THREADS = 256;
 
 struct Part {       // of a chunk: its largest value, its sums, and the label's logit
     float m, s, t, zl;
@@ -639,7 +706,7 @@ struct Part {       // of a chunk: its largest value, its sums, and the label's 
 
 // The values of a chunk once more, from memory, for the rare rows whose candidates do not fit their list: cells are every fourth of a
 // thread's pieces.
-template <typename T>
+template <typename T, int UNROLL>
 struct Streamed {
     const Row<T> &r;
     int begin, end, K;
@@ -673,14 +740,7 @@ struct Streamed {
     }
 };
 
-constexpr int HELD = 384;        // pieces that a workgroup sets aside for the most probable tokens
-struct Aside {
-    uint4 piece[HELD];
-    int place[HELD], count;
-    unsigned said[4];
-};
-
-template <typename T, bool TOP>
+template <typename T, bool TOP, int UNROLL>
 __global__ __launch_bounds__(CHUNK_THREADS) void logprob_stream_kernel(LogprobArgs a, int chunks, int chunk_pieces, Part *parts, unsigned long long *keys)
 {
     constexpr int V = Piece<T>::V, LOW = sizeof(T) == 2 ? 16 : 0;
@@ -699,21 +759,17 @@ __global__ __launch_bounds__(CHUNK_THREADS) void logprob_stream_kernel(LogprobAr
     // Candidates for the most probable tokens: pieces with a value that reaches a bound which `top` values have reached so far are set aside as they
     // pass.  The bound comes from what each wave says of its lanes' maxima (top/4 lanes have reached it), before the first turn and
     // after 1, 2, 4, ...; a wave may read an older word of another one, which is a bound too.  Minus infinities are never set aside.
-    __shared__ Aside aside;
+    __shared__ Aside<T> aside;
     float limit = LOWEST, seen = -INFINITY, of[UNROLL];
     int turn = 0;
-    bool bounded = true;
     auto say = [&]() {
         const unsigned cells[1] = {order(seen)};
         const unsigned b = wave_bound<1, LOW>(cells, (a.top + 3) / 4);
         if ((threadIdx.x & 63) == 0) *(volatile unsigned *)&aside.said[wave] = b;
     };
     auto hear = [&]() {
-        const volatile unsigned *said = aside.said;
-        const unsigned b = min(min(said[0], said[1]), min(said[2], said[3]));
-        bounded = b >> LOW > order(-INFINITY) >> LOW;
-        limit = bounded ? unorder(b) : LOWEST;
-        return b;
+        const unsigned b = aside.template hear<4>();
+        limit = b >> LOW > order(-INFINITY) >> LOW ? unorder(b) : LOWEST;
     };
     if constexpr (TOP) {
         if (threadIdx.x == 0) aside.count = 0;
@@ -750,14 +806,7 @@ __global__ __launch_bounds__(CHUNK_THREADS) void logprob_stream_kernel(LogprobAr
             most = fmaxf(most, x);
             if constexpr (TOP) {
                 of[u] = fmaxf(of[u], x);
-                if (x >= limit) {
-                    const int at = atomicAdd(&aside.count, 1);
-                    if (at < HELD) {
-                        aside.piece[at] = make_uint4(c[u].w[0], c[u].w[1], c[u].w[2], c[u].w[3]);
-                        aside.place[at] = base + u * CHUNK_THREADS + (int)threadIdx.x;
-                    } else
-                        limit = INFINITY;       // too many: they are looked for once more below
-                }
+                if (x >= limit && !aside.put(c[u], base + u * CHUNK_THREADS + (int)threadIdx.x)) limit = INFINITY;     // too many: they are looked for once more below
             }
         }
         // the sums so far at the new maximum
@@ -771,27 +820,30 @@ __global__ __launch_bounds__(CHUNK_THREADS) void logprob_stream_kernel(LogprobAr
         shift = to;
         auto sums = [&](auto near) {
 #pragma unroll
-            for (int u = 0; u < UNROLL; ++u)
+            for (int u = 0; u < UNROLL; ++u) {
 #pragma unroll
                 for (int k = 0; k < V; ++k) {
                     const float d = sc.d2<decltype(near)::value>(z[u][k]), e = __builtin_amdgcn_exp2f(d);
                     s += e;
                     t = fmaf(e, weight<true>(d), t);
                 }
+            }
         };
         if (near) sums(std::true_type());
         else sums(std::false_type());
         if constexpr (TOP) {
             ++turn;
             if ((turn & (turn - 1)) == 0 && next < end && limit < INFINITY) {
-                seen = max3(max3(of[0], of[1], of[2]), of[3], seen);
+#pragma unroll
+                for (int u = 0; u < UNROLL; ++u) seen = fmaxf(seen, of[u]);
                 say();
                 hear();
             }
         }
     }
     if constexpr (TOP) {
-        seen = max3(max3(of[0], of[1], of[2]), of[3], seen);
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) seen = fmaxf(seen, of[u]);
         say();
     }
     float most = meet<64>(m, larger);
@@ -823,36 +875,12 @@ __global__ __launch_bounds__(CHUNK_THREADS) void logprob_stream_kernel(LogprobAr
             if ((int)threadIdx.x < a.top) emit(threadIdx.x, (int)threadIdx.x < values ? key_of(order(-INFINITY), (unsigned)(first + (int)threadIdx.x)) : NO_KEY);
             return;
         }
-        // what reaches the bound of the whole
-        const unsigned bound = hear();
-        const int pieces = aside.count;
-        if (pieces <= HELD) {
-            for (int i = threadIdx.x; i < pieces; i += CHUNK_THREADS) {
-                const uint4 u = aside.piece[i];
-                const Piece<T> q = {{u.x, u.y, u.z, u.w}};
-                const int at = aside.place[i] * V - r.head;
-#pragma unroll
-                for (int k = 0; k < V; ++k) {
-                    const unsigned o = order(q.at(k));
-                    if (q.at(k) >= limit && o >= bound && (unsigned)(at + k) < (unsigned)a.K) {
-                        const int to = atomicAdd(&sh.count, 1);
-                        if (to < CAP) sh.list[to] = key_of(o, (unsigned)(at + k));
-                    }
-                }
-            }
-            __syncthreads();
-            const int n = sh.count;
-            if (n <= CAP && (bounded || n >= a.top || n >= values)) {
-                rank_candidates<4>(sh, n, a.top, emit);
-                return;
-            }
-        }
-        // too many of them, or minus infinities are among the most probable
+        if (aside.template rank<4, LOW>(sh, aside.template hear<4>(), r.head, a.K, a.top, values, emit)) return;
         __syncthreads();
         unsigned cell[UNROLL];
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) cell[u] = begin + u * CHUNK_THREADS + (int)threadIdx.x < end ? order(of[u]) : 0u;
-        select_top<4, UNROLL, LOW>(sh, cell, a.top, Streamed<T>{r, begin, end, a.K, cell}, emit);
+        select_top<4, UNROLL, LOW>(sh, cell, a.top, Streamed<T, UNROLL>{r, begin, end, a.K, cell}, emit);
     }
 }
 
@@ -894,43 +922,59 @@ __device__ __forceinline__ Joined join_parts(const Part *parts, int chunks, floa
     return j;
 }
 
-// What chunks found out about a row.  Their keys are read before their sums are joined; HELD_KEYS of each thread are held, more are read again.
+// What chunks found out about a row, joined by one wave.  A chunk's keys are in descending order: the first DEPTH of each give the bound, and a lane goes
+// down its chunks' lists as far as that.
 template <typename T, bool TOP>
-__global__ __launch_bounds__(256) void logprob_join_kernel(LogprobArgs a, int chunks, const Part *parts, const unsigned long long *keys)
+__global__ __launch_bounds__(64) void logprob_join_kernel(LogprobArgs a, int chunks, const Part *parts, const unsigned long long *keys)
 {
-    constexpr int HELD_KEYS = 8;
-    __shared__ float red[3][4];
+    constexpr int DEPTH = 4, LOW = sizeof(T) == 2 ? 16 : 0;
+    __shared__ float red[3][1];
     const size_t row = blockIdx.x;
+    const int lane = threadIdx.x, top = a.top;
     parts += row * chunks;
     const int label = a.labels ? a.labels[row] : -1;
     const float zl = parts[0].zl;       // (every chunk has it)
-    const int n = chunks * a.top;       // (fewer than 2^31: launch)
-    unsigned long long held[HELD_KEYS];
+    unsigned cell[DEPTH] = {};
     if constexpr (TOP) {
-        keys += row * chunks * a.top;
+        keys += row * chunks * top;
+        for (int c = lane; c < chunks; c += 64)
 #pragma unroll
-        for (int i = 0; i < HELD_KEYS; ++i) held[i] = i * 256 + (int)threadIdx.x < n ? keys[i * 256 + (int)threadIdx.x] : NO_KEY;
+            for (int d = 0; d < DEPTH; ++d) cell[d] = max(cell[d], d < top ? (unsigned)(keys[(size_t)c * top + d] >> 32) : 0u);
     }
-    const Joined j = join_parts<4>(parts, chunks, a.scale, red);
-    if (threadIdx.x == 0) write_row_results(a, row, label, zl, j);
+    const Joined j = join_parts<1>(parts, chunks, a.scale, red);
+    if (lane == 0) write_row_results(a, row, label, zl, j);
     if constexpr (TOP) {
         __shared__ TopShared sh;
-        unsigned cell[4] = {0, 0, 0, 0};
-#pragma unroll
-        for (int i = 0; i < HELD_KEYS; ++i) cell[i & 3] = max(cell[i & 3], (unsigned)(held[i] >> 32));
-        for (int i = HELD_KEYS * 256 + (int)threadIdx.x; i < n; i += 256) cell[0] = max(cell[0], (unsigned)(keys[i] >> 32));
-        select_top<4, 4, sizeof(T) == 2 ? 16 : 0>(
-            sh, cell, a.top,
+        if (lane == 0) sh.count = 0;
+        __syncthreads();
+        const unsigned bound = wave_bound<DEPTH, LOW>(cell, top);
+        auto emit = [&](int i, unsigned long long key) { write_top(a, row, j, i, key); };
+        for (int c = lane; c < chunks; c += 64)
+            for (int i = 0; i < top; ++i) {
+                const unsigned long long key = keys[(size_t)c * top + i];
+                if (key == NO_KEY || (unsigned)(key >> 32) < bound) break;
+                const int at = atomicAdd(&sh.count, 1);
+                if (at < CAP) sh.list[at] = key;
+                else break;
+            }
+        __syncthreads();
+        const int n = sh.count;
+        if (n <= CAP) {
+            rank_candidates<1>(sh, n, top, emit);
+            return;
+        }
+        __syncthreads();
+        select_top<1, DEPTH, LOW>(
+            sh, cell, top,
             [&](unsigned from, auto f) {
-                auto look = [&](unsigned long long key) {
-                    if (key != NO_KEY && (unsigned)(key >> 32) >= from) f((unsigned)(key >> 32), key_index(key));
-                };
-                if (__ballot(max(max(cell[0], cell[1]), max(cell[2], cell[3])) >= from) == 0) return;
-#pragma unroll
-                for (int i = 0; i < HELD_KEYS; ++i) look(held[i]);
-                for (int i = HELD_KEYS * 256 + (int)threadIdx.x; i < n; i += 256) look(keys[i]);
+                for (int c = lane; c < chunks; c += 64)
+                    for (int i = 0; i < top; ++i) {
+                        const unsigned long long key = keys[(size_t)c * top + i];
+                        if (key == NO_KEY || (unsigned)(key >> 32) < from) break;
+                        f((unsigned)(key >> 32), key_index(key));
+                    }
             },
-            [&](int i, unsigned long long key) { write_top(a, row, j, i, key); });
+            emit);
     }
 }
 
@@ -1052,13 +1096,17 @@ int launch(const LogprobArgs &a, void *workspace, hipStream_t st)
     Part *parts = alone ? nullptr : (Part *)workspace;
     unsigned long long *keys = (unsigned long long *)((char *)workspace + align_up(grid * sizeof(Part), 256));
     const dim3 g((unsigned)grid), b(CHUNK_THREADS);
-    if (a.top) hipLaunchKernelGGL((logprob_stream_kernel<T, true>), g, b, 0, st, a, cut.chunks, cut.pieces, parts, keys);
-    else hipLaunchKernelGGL((logprob_stream_kernel<T, false>), g, b, 0, st, a, cut.chunks, cut.pieces, parts, keys);
+    // a piece a thread: short code, whose fetching counts
+    const bool once = cut.pieces <= CHUNK_THREADS;
+    if (a.top && once) hipLaunchKernelGGL((logprob_stream_kernel<T, true, 1>), g, b, 0, st, a, cut.chunks, cut.pieces, parts, keys);
+    else if (a.top) hipLaunchKernelGGL((logprob_stream_kernel<T, true, 4>), g, b, 0, st, a, cut.chunks, cut.pieces, parts, keys);
+    else if (once) hipLaunchKernelGGL((logprob_stream_kernel<T, false, 1>), g, b, 0, st, a, cut.chunks, cut.pieces, parts, keys);
+    else hipLaunchKernelGGL((logprob_stream_kernel<T, false, 4>), g, b, 0, st, a, cut.chunks, cut.pieces, parts, keys);
     if (hipGetLastError() != hipSuccess) return MXC_ERR_LAUNCH;
     if (alone) return MXC_OK;
     const dim3 gg((unsigned)((size_t)a.N * blocks));
-    if (!a.dz && a.top) hipLaunchKernelGGL((logprob_join_kernel<T, true>), dim3((unsigned)a.N), dim3(256), 0, st, a, cut.chunks, parts, keys);
-    else if (!a.dz) hipLaunchKernelGGL((logprob_join_kernel<T, false>), dim3((unsigned)a.N), dim3(256), 0, st, a, cut.chunks, parts, keys);
+    if (!a.dz && a.top) hipLaunchKernelGGL((logprob_join_kernel<T, true>), dim3((unsigned)a.N), dim3(64), 0, st, a, cut.chunks, parts, keys);
+    else if (!a.dz) hipLaunchKernelGGL((logprob_join_kernel<T, false>), dim3((unsigned)a.N), dim3(64), 0, st, a, cut.chunks, parts, keys);
     else if (per == 1) hipLaunchKernelGGL((logprob_gradient_kernel<T, 1>), gg, b, 0, st, a, blocks, cut.chunks, parts);
     else hipLaunchKernelGGL((logprob_gradient_kernel<T, 4>), gg, b, 0, st, a, blocks, cut.chunks, parts);
     return hipGetLastError() == hipSuccess ? MXC_OK : MXC_ERR_LAUNCH;
