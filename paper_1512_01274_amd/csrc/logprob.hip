@@ -289,8 +289,9 @@ __device__ __forceinline__ float weight(float d) { return CLAMP ? fmaxf(d, NO_WE
 // Cells are sets of a wave's values, 64 or more of them, of which each lane knows one of the largest.  Where each of W waves has top/W cells that
 // reach a bound, `top` values reach it; so they do where one wave has `top` cells that reach it.  What reaches the bound is collected in
 // LDS and ranked by counting, which makes the order that of the keys whatever order they were collected in.
-constexpr int CAP = 1024;
+template <int CAP_>
 struct TopShared {
+    static constexpr int CAP = CAP_;
     unsigned long long list[CAP];
     unsigned bound[16];
     int count;
@@ -311,8 +312,8 @@ __device__ __forceinline__ unsigned wave_bound(const unsigned *cell, int n)
     return t;
 }
 
-template <int W, class Emit>
-__device__ __forceinline__ void rank_candidates(const TopShared &sh, int n, int top, Emit emit)
+template <int W, int CAP, class Emit>
+__device__ __forceinline__ void rank_candidates(const TopShared<CAP> &sh, int n, int top, Emit emit)
 {
     for (int i = threadIdx.x; i < n; i += 64 * W) {
         const unsigned long long key = sh.list[i];
@@ -326,8 +327,8 @@ __device__ __forceinline__ void rank_candidates(const TopShared &sh, int n, int 
 
 // Hands the i-th largest key of the row to emit(i, key); places past the last value get NO_KEY.  Called by a whole workgroup of W waves;
 // cell: this lane's S cells.  each(from, f) calls f(order, index) for each of the thread's values that reaches `from`.
-template <int W, int S, int LOW, class Each, class Emit>
-__device__ __forceinline__ void select_top(TopShared &sh, const unsigned *cell, int top, Each each, Emit emit)
+template <int W, int S, int LOW, int CAP, class Each, class Emit>
+__device__ __forceinline__ void select_top(TopShared<CAP> &sh, const unsigned *cell, int top, Each each, Emit emit)
 {
     const int wave = threadIdx.x >> 6;
     unsigned bound = wave_bound<S, LOW>(cell, (top + W - 1) / W);
@@ -408,8 +409,7 @@ __device__ __forceinline__ void select_top(TopShared &sh, const unsigned *cell, 
 
 // Pieces with a value that may be among the most probable, set aside in LDS.  Minus infinities are left out: limit is LOWEST at least.  From there
 // each thread looks at one value of one piece: short code counts here, for a kernel of few rows is mostly latency, that of fetching its code included.
-constexpr int HELD = 640;
-template <typename T>
+template <typename T, int HELD>
 struct Aside {
     static constexpr int V = Piece<T>::V;
     T value[HELD][V];
@@ -436,8 +436,8 @@ struct Aside {
     }
     // Ranks what reaches the bound; false where that is not to be had: too many of them, or minus infinities are among the most probable ones of
     // `values`.  sh.count is 0.
-    template <int W, int LOW, class Emit>
-    __device__ __forceinline__ bool rank(TopShared &sh, unsigned bound, int head, int K, int top, int values, Emit emit) const
+    template <int W, int LOW, int CAP, class Emit>
+    __device__ __forceinline__ bool rank(TopShared<CAP> &sh, unsigned bound, int head, int K, int top, int values, Emit emit) const
     {
         const int pieces = count;
         if (pieces > HELD) return false;
@@ -608,8 +608,10 @@ __global__ __launch_bounds__(G < 64 ? 256 : G, G == 512 && P == 16 ? 4 : 1) void
         }
     }
     if constexpr (TOP) {
-        __shared__ TopShared sh;
-        __shared__ Aside<T> aside;
+        // (small where a workgroup is a wave: what a compute unit holds of them goes by their LDS)
+        constexpr int CAP = W == 1 ? 256 : 512, HELD = W == 1 ? 32 + 32 * P : 256;
+        __shared__ TopShared<CAP> sh;
+        __shared__ Aside<T, HELD> aside;
         constexpr int LOW = sizeof(T) == 2 ? 16 : 0;
         auto emit = [&](int i, unsigned long long key) {
             a.top_index[row * a.top + i] = key == NO_KEY ? -1 : (int)key_index(key);
@@ -759,7 +761,8 @@ __global__ __launch_bounds__(CHUNK_THREADS) void logprob_stream_kernel(LogprobAr
     // Candidates for the most probable tokens: pieces with a value that reaches a bound which `top` values have reached so far are set aside as they
     // pass.  The bound comes from what each wave says of its lanes' maxima (top/4 lanes have reached it), before the first turn and
     // after 1, 2, 4, ...; a wave may read an older word of another one, which is a bound too.  Minus infinities are never set aside.
-    __shared__ Aside<T> aside;
+    constexpr int CAP = 1024;
+    __shared__ Aside<T, TOP ? 640 : 1> aside;
     float limit = LOWEST, seen = -INFINITY, of[UNROLL];
     int turn = 0;
     auto say = [&]() {
@@ -857,7 +860,7 @@ __global__ __launch_bounds__(CHUNK_THREADS) void logprob_stream_kernel(LogprobAr
         red[1][wave] = s;
         red[2][wave] = t;
     }
-    __shared__ TopShared sh;
+    __shared__ TopShared<TOP ? CAP : 1> sh;
     if (TOP && threadIdx.x == 0) sh.count = 0;
     __syncthreads();
     const Joined j{most, red[1][0] + red[1][1] + red[1][2] + red[1][3], red[2][0] + red[2][1] + red[2][2] + red[2][3]};
@@ -944,7 +947,8 @@ __global__ __launch_bounds__(64) void logprob_join_kernel(LogprobArgs a, int chu
     const Joined j = join_parts<1>(parts, chunks, a.scale, red);
     if (lane == 0) write_row_results(a, row, label, zl, j);
     if constexpr (TOP) {
-        __shared__ TopShared sh;
+        constexpr int CAP = 1024;
+        __shared__ TopShared<CAP> sh;
         if (lane == 0) sh.count = 0;
         __syncthreads();
         const unsigned bound = wave_bound<DEPTH, LOW>(cell, top);
@@ -1050,7 +1054,9 @@ struct Cut {
 };
 Cut cut_rows(int N, int pieces, bool gradient)
 {
-    if (pieces <= SHORT_PIECES || (gradient && pieces <= ROW_PIECES && N >= 64)) return Cut{0, 0};
+    // A gradient's rows are held, but for the longest ones where there are few: 131072 of bf16 took 20.4 us held and 13.9 in chunks at 64 rows, 23.3
+    // and 21.2 at 128, 29.4 and 31.5 at 192; 50304 of them 10.5 and 10.9 at 64.
+    if (pieces <= SHORT_PIECES || (gradient && (pieces <= ROW_PIECES / 2 || (pieces <= ROW_PIECES && N >= 160)))) return Cut{0, 0};
     int chunks = N >= 256 ? 1 : (1024 + N - 1) / N;
     chunks = chunks < (pieces + CHUNK_THREADS - 1) / CHUNK_THREADS ? chunks : (pieces + CHUNK_THREADS - 1) / CHUNK_THREADS;
     Cut c;
@@ -1090,7 +1096,7 @@ int launch(const LogprobArgs &a, void *workspace, hipStream_t st)
         return hipGetLastError() == hipSuccess ? MXC_OK : MXC_ERR_LAUNCH;
     }
     const size_t grid = (size_t)a.N * cut.chunks;
-    const int per = pieces <= 2048 || a.N < 64 ? 1 : 4, blocks = block_count(pieces, per);
+    const int per = pieces <= 2048 || a.N < 160 ? 1 : 4, blocks = block_count(pieces, per);
     if (grid > 0x7FFFFFFFu || (size_t)cut.chunks * (a.top ? a.top : 1) > 0x7FFFFFFFu || (a.dz && (size_t)a.N * blocks > 0x7FFFFFFFu)) return MXC_ERR_SHAPE;
     const bool alone = cut.chunks == 1 && !a.dz;
     Part *parts = alone ? nullptr : (Part *)workspace;

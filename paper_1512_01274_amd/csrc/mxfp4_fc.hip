@@ -5,6 +5,7 @@
 //   skinny: x is quantised once, then workgroups of eight waves that share out the columns.
 //   tiled:  x quantised, both operands' scales brought into the order of the tiles, and tiles of LDS that a ring of loads fills.
 #include <type_traits>
+#include <utility>
 
 #include "mxfp4.h"
 
@@ -42,68 +43,112 @@ __device__ __forceinline__ float activated(float v, const float *bias, long long
     return relu && v < 0.f ? 0.f : v;
 }
 
+// ---- 16 rows of the filter straight from memory -----------------------------------------------------------------------------
+// The instruction wants block l/16 of row l%16 in lane l.  Read so, neighbouring lanes are rows apart, and the 64 lanes' 16 bytes take 64 turns of the
+// address unit; read as block l%4 of row l/4, four lanes a 64-byte piece, they take 16, and each word changes its lane through LDS.
+__device__ __forceinline__ uint4 to_operand(uint4 v, int lane)
+{
+    const int from = (((lane & 15) << 2) | (lane >> 4)) << 2;       // byte address of the lane that has it
+    return make_uint4((unsigned)__builtin_amdgcn_ds_bpermute(from, (int)v.x), (unsigned)__builtin_amdgcn_ds_bpermute(from, (int)v.y),
+                      (unsigned)__builtin_amdgcn_ds_bpermute(from, (int)v.z), (unsigned)__builtin_amdgcn_ds_bpermute(from, (int)v.w));
+}
+// scale byte of this lane's block in step j: lane 4*row + j holds the four bytes of the step
+__device__ __forceinline__ int to_scale(unsigned word, int lane, int j)
+{
+    return (int)((unsigned)__builtin_amdgcn_ds_bpermute((((lane & 15) << 2) | j) << 2, (int)word) >> (8 * (lane >> 4)));
+}
+
+struct FilterRows {
+    const unsigned char *codes, *scales;        // of row l/4 of the 16
+    int blocks, part;                           // part: l%4
+    __device__ __forceinline__ FilterRows(const unsigned char *wc, const unsigned char *ws, int K, int blocks_, int scale_row, int lane) : blocks(blocks_), part(lane & 3)
+    {
+        const long long k = (long long)blockIdx.x * 16 + (lane >> 2), row = k < K ? k : K - 1;
+        codes = wc + (size_t)row * blocks * 16;
+        scales = ws + (size_t)row * scale_row;
+    }
+    // step j of a group of 512 columns
+    __device__ __forceinline__ uint4 load(int group, int j) const
+    {
+        const int b = group * 16 + j * 4 + part;
+        return b < blocks ? *reinterpret_cast<const uint4 *>(codes + (size_t)b * 16) : make_uint4(0, 0, 0, 0);
+    }
+    __device__ __forceinline__ unsigned load_scales(int group) const { return *reinterpret_cast<const unsigned *>(scales + (size_t)group * 16 + part * 4); }
+};
+
 // ---- up to 16 rows of x ---------------------------------------------------------------------------------------------------
-// 16 filter rows a workgroup; its eight waves take every eighth group of 512 columns in four steps of 128.  Lane l holds a block of filter row
-// l%16 and one of row l%16 of x, which it quantises itself: the four lanes of a row read 64 bytes of codes that follow each other.
+// 16 filter rows a workgroup; its eight waves take every eighth group of 512 columns in four steps of 128.  A wave brings its columns of x into
+// 4 bits by itself, eight values a lane, and passes the codes through LDS to the lanes that multiply them: lane l holds a block of
+// filter row l%16 and one of row l%16 of x.
 constexpr int TOKEN_WAVES = 8;
 
-struct TokenGroup {
-    uint4 w[4], scale;      // scale: the 16 bytes of the group's blocks
+struct TokenRow {       // of x: the codes and scales of a group, and room that spreads rows over the banks
+    unsigned codes[64];
+    unsigned char scales[16];
 };
-__device__ __forceinline__ TokenGroup load_filter(const unsigned char *wc, const unsigned char *ws, int group, int quarter, int blocks)
-{
-    TokenGroup g;
-    const int b = group * 16 + quarter;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) g.w[j] = b + 4 * j < blocks ? *reinterpret_cast<const uint4 *>(wc + (size_t)(b + 4 * j) * 16) : make_uint4(0, 0, 0, 0);
-    g.scale = *reinterpret_cast<const uint4 *>(ws + (size_t)group * 16);
-    return g;
-}
-
-template <typename T>
-__device__ __forceinline__ f32x4 token_step(const T *x, int column, int C, bool live, uint4 w, unsigned scales, int quarter, f32x4 acc)
-{
-    uint4 codes = make_uint4(0, 0, 0, 0);
-    unsigned byte = 0;
-    const int left = C - column;
-    if (live && left > 0) {
-        float v[4][8];
-        unsigned most = 0;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            load8_edge(x + column + k * 8, left - k * 8, v[k]);
-            most = max(most, largest8(v[k]));
-        }
-        byte = mxfp4_scale_byte(most);
-        codes = make_uint4(mxfp4_codes8(v[0], byte), mxfp4_codes8(v[1], byte), mxfp4_codes8(v[2], byte), mxfp4_codes8(v[3], byte));
-    }
-    return mfma16<0, 0>(w, codes, acc, (int)(scales >> (8 * quarter)), (int)byte);
-}
 
 template <typename T>
 __global__ __launch_bounds__(64 * TOKEN_WAVES) void mxfp4_token_kernel(int N, int C, int K, int blocks, int scale_row, const T *x, const unsigned char *wc,
                                                                        const unsigned char *ws, const float *bias, int relu, T *y)
 {
+    constexpr int BATCH = 4;        // rows of x whose loads are under way together
     __shared__ f32x4 part[TOKEN_WAVES][64];
+    __shared__ __align__(16) TokenRow rows[TOKEN_WAVES][16];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, quarter = lane >> 4;
     const long long k0 = (long long)blockIdx.x * 16;
-    const long long k = k0 + r < K ? k0 + r : K - 1;
-    wc += (size_t)k * blocks * 16;
-    ws += (size_t)k * scale_row;
-    const bool live = r < N;
-    x += (size_t)(live ? r : 0) * C;
+    const FilterRows filter(wc, ws, K, blocks, scale_row, lane);
     const int groups = scale_row / 16;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    TokenGroup next;
-    if (wave < groups) next = load_filter(wc, ws, wave, quarter, blocks);
+    uint4 next[4];
+    unsigned next_scales = 0;
+    auto ahead = [&](int group) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) next[j] = filter.load(group, j);
+        next_scales = filter.load_scales(group);
+    };
+    if (wave < groups) ahead(wave);
     for (int group = wave; group < groups; group += TOKEN_WAVES) {
-        const TokenGroup g = next;
-        if (group + TOKEN_WAVES < groups) next = load_filter(wc, ws, group + TOKEN_WAVES, quarter, blocks);
-        const int column = group * 512 + quarter * 32;
-        acc = token_step(x, column, C, live, g.w[0], g.scale.x, quarter, acc);
-        acc = token_step(x, column + 128, C, live, g.w[1], g.scale.y, quarter, acc);
-        acc = token_step(x, column + 256, C, live, g.w[2], g.scale.z, quarter, acc);
-        acc = token_step(x, column + 384, C, live, g.w[3], g.scale.w, quarter, acc);
+        uint4 w[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = next[j];
+        const unsigned sw = next_scales;
+        if (group + TOKEN_WAVES < groups) ahead(group + TOKEN_WAVES);
+        const int column = group * 512 + lane * 8;
+#pragma unroll 1
+        for (int n0 = 0; n0 < N; n0 += BATCH) {
+            float v[BATCH][8];
+#pragma unroll
+            for (int i = 0; i < BATCH; ++i) {
+                const int n = n0 + i;
+                load8_edge(x + (n < N ? (size_t)n * C + column : 0), n < N ? C - column : 0, v[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < BATCH; ++i) {
+                if (n0 + i >= N) break;
+                const unsigned byte = mxfp4_scale_byte(max_quad(largest8(v[i])));
+                TokenRow &to = rows[wave][n0 + i];
+                to.codes[lane] = mxfp4_codes8(v[i], byte);
+                if ((lane & 3) == 0) to.scales[lane >> 2] = (unsigned char)byte;
+            }
+        }
+        // (a wave's own accesses to LDS keep their order)
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        const TokenRow &from = rows[wave][r];
+        const bool live = r < N;
+        const uint4 scales = *reinterpret_cast<const uint4 *>(from.scales);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            uint4 c = *reinterpret_cast<const uint4 *>(from.codes + (4 * j + quarter) * 4);
+            unsigned sx = j == 0 ? scales.x : j == 1 ? scales.y : j == 2 ? scales.z : scales.w;
+            if (!live) {
+                c = make_uint4(0, 0, 0, 0);
+                sx = 0;
+            }
+            acc = mfma16<0, 0>(to_operand(w[j], lane), c, acc, to_scale(sw, lane, j), (int)(sx >> (8 * quarter)));
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
     }
     part[wave][lane] = acc;
     __syncthreads();
@@ -146,6 +191,11 @@ __global__ __launch_bounds__(256) void mxfp4_order_kernel(int N, int C, int grou
     if (threadIdx.x < 64) xs[(size_t)blockIdx.x * 64 + threadIdx.x] = words[threadIdx.x];
 }
 
+template <int N, class F, int... U>
+__device__ __forceinline__ void each_number(F f, std::integer_sequence<int, U...>) { (f(std::integral_constant<int, U>()), ...); }
+template <int N, class F>
+__device__ __forceinline__ void each_number(F f) { each_number<N>(f, std::make_integer_sequence<int, N>()); }
+
 // 16 filter rows and 16*NF rows of x a workgroup, both straight from the caches into registers; its eight waves take every eighth group of
 // 512 columns, and their sums meet in LDS.
 template <typename T, int NF>
@@ -154,48 +204,58 @@ __global__ __launch_bounds__(512) void mxfp4_skinny_kernel(int N, int K, int blo
 {
     constexpr int WAVES = 8;
     __shared__ f32x4 part[WAVES][NF][64];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quarter = lane >> 4;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int groups = scale_row / 16, tiles = (N + 15) / 16, tile0 = blockIdx.y * NF;
-    const long long k0 = (long long)blockIdx.x * 16, row = k0 + (lane & 15) < K ? k0 + (lane & 15) : K - 1;
-    wc += (size_t)row * blocks * 16;
-    ws += (size_t)row * scale_row;
-    int tile[NF];       // (the last one again where there are fewer)
+    const long long k0 = (long long)blockIdx.x * 16;
+    const FilterRows filter(wc, ws, K, blocks, scale_row, lane);
+    // byte offsets of this lane's part of each tile of x (the last tile again where there are fewer): less than 4 GB for at most 128 rows
+    unsigned at[NF], scale_at[NF];
 #pragma unroll
-    for (int i = 0; i < NF; ++i) tile[i] = min(tile0 + i, tiles - 1);
+    for (int i = 0; i < NF; ++i) {
+        const unsigned unit = (unsigned)min(tile0 + i, tiles - 1) * (unsigned)groups;
+        at[i] = unit * 4096u + (unsigned)lane * 16u;
+        scale_at[i] = unit * 256u + (unsigned)lane * 4u;
+    }
+    const char *codes = (const char *)xc, *scales = (const char *)xs;
     f32x4 acc[NF] = {};
+    // A wave's steps of 128 columns, four a group, follow each other over its groups; three places for them: two steps are under way while
+    // one is multiplied (a fourth place would not fit the registers).
     struct Step {
         uint4 w, x[NF];
-    };
-    auto load = [&](int group, int j) {
-        Step s;
-        const int b = group * 16 + j * 4 + quarter;
-        s.w = b < blocks ? *reinterpret_cast<const uint4 *>(wc + (size_t)b * 16) : make_uint4(0, 0, 0, 0);
+    } place[3];
+    unsigned scales_w[2];
+    int scales_x[2][NF];
+    const int steps = wave < groups ? ((groups - 1 - wave) / WAVES + 1) * 4 : 0;
+    auto load = [&](Step &s, int step) {
+        const int group = wave + (step >> 2) * WAVES, j = step & 3;
+        s.w = filter.load(group, j);
 #pragma unroll
-        for (int i = 0; i < NF; ++i) s.x[i] = xc[(((size_t)tile[i] * groups + group) * 4 + j) * 64 + lane];
-        return s;
+        for (int i = 0; i < NF; ++i) s.x[i] = *reinterpret_cast<const uint4 *>(codes + (at[i] + (unsigned)(group * 4 + j) * 1024u));
     };
-    uint4 sw = make_uint4(0, 0, 0, 0);      // 16 scale bytes of the filter's row: this lane's of step j is byte `quarter` of word j
-    int sx[NF] = {};
-    auto multiply = [&](auto j, const Step &s) {
-        constexpr int J = decltype(j)::value;
-        const int mine = (int)((J == 0 ? sw.x : J == 1 ? sw.y : J == 2 ? sw.z : sw.w) >> (8 * quarter));
+    auto load_scales = [&](int which, int step) {
+        const int group = wave + (step >> 2) * WAVES;
+        scales_w[which] = filter.load_scales(group);
 #pragma unroll
-        for (int i = 0; i < NF; ++i) acc[i] = mfma16<0, J>(s.w, s.x[i], acc[i], mine, sx[i]);
+        for (int i = 0; i < NF; ++i) scales_x[which][i] = *reinterpret_cast<const int *>(scales + (scale_at[i] + (unsigned)group * 256u));
     };
-    if (wave < groups) {
-        Step a = load(wave, 0), b;
-        for (int group = wave; group < groups; group += WAVES) {
-            sw = *reinterpret_cast<const uint4 *>(ws + (size_t)group * 16);
+    if (steps > 0) {
+        load(place[0], 0);
+        load_scales(0, 0);
+        load(place[1], 1);
+        for (int base = 0; base < steps; base += 24) {      // 24 steps: whole turns of the places, the groups and their two sets of scales
+            auto one = [&](auto number) {
+                constexpr int U = decltype(number)::value, J = U & 3, SET = (U >> 2) & 1;
+                const int step = base + U;
+                if (step >= steps) return;
+                if (step + 2 < steps) load(place[(U + 2) % 3], step + 2);
+                if (J == 2 && step + 2 < steps) load_scales(SET ^ 1, step + 2);
+                const Step &s = place[U % 3];
+                const uint4 w = to_operand(s.w, lane);
+                const int mine = to_scale(scales_w[SET], lane, J);
 #pragma unroll
-            for (int i = 0; i < NF; ++i) sx[i] = (int)xs[((size_t)tile[i] * groups + group) * 64 + lane];
-            b = load(group, 1);
-            multiply(std::integral_constant<int, 0>(), a);
-            a = load(group, 2);
-            multiply(std::integral_constant<int, 1>(), b);
-            b = load(group, 3);
-            multiply(std::integral_constant<int, 2>(), a);
-            a = load(group + WAVES < groups ? group + WAVES : group, 0);
-            multiply(std::integral_constant<int, 3>(), b);
+                for (int i = 0; i < NF; ++i) acc[i] = mfma16<0, J>(w, s.x[i], acc[i], mine, scales_x[SET][i]);
+            };
+            each_number<24>(one);
         }
     }
 #pragma unroll
