@@ -5,7 +5,6 @@
 //   skinny: x is quantised once, then workgroups of eight waves that share out the columns.
 //   tiled:  x quantised, both operands' scales brought into the order of the tiles, and tiles of LDS that a ring of loads fills.
 #include <type_traits>
-#include <utility>
 
 #include "mxfp4.h"
 
@@ -52,28 +51,26 @@ __device__ __forceinline__ uint4 to_operand(uint4 v, int lane)
     return make_uint4((unsigned)__builtin_amdgcn_ds_bpermute(from, (int)v.x), (unsigned)__builtin_amdgcn_ds_bpermute(from, (int)v.y),
                       (unsigned)__builtin_amdgcn_ds_bpermute(from, (int)v.z), (unsigned)__builtin_amdgcn_ds_bpermute(from, (int)v.w));
 }
-// scale byte of this lane's block in step j: lane 4*row + j holds the four bytes of the step
-__device__ __forceinline__ int to_scale(unsigned word, int lane, int j)
-{
-    return (int)((unsigned)__builtin_amdgcn_ds_bpermute((((lane & 15) << 2) | j) << 2, (int)word) >> (8 * (lane >> 4)));
-}
+__device__ __forceinline__ int to_operand(unsigned v, int lane) { return __builtin_amdgcn_ds_bpermute((((lane & 15) << 2) | (lane >> 4)) << 2, (int)v); }
 
 struct FilterRows {
     const unsigned char *codes, *scales;        // of row l/4 of the 16
     int blocks, part;                           // part: l%4
-    __device__ __forceinline__ FilterRows(const unsigned char *wc, const unsigned char *ws, int K, int blocks_, int scale_row, int lane) : blocks(blocks_), part(lane & 3)
+    __device__ __forceinline__ FilterRows() {}
+    __device__ __forceinline__ FilterRows(const unsigned char *wc, const unsigned char *ws, long long k0, int K, int blocks_, int scale_row, int lane)
+        : blocks(blocks_), part(lane & 3)
     {
-        const long long k = (long long)blockIdx.x * 16 + (lane >> 2), row = k < K ? k : K - 1;
+        const long long k = k0 + (lane >> 2), row = k < K ? k : K - 1;
         codes = wc + (size_t)row * blocks * 16;
         scales = ws + (size_t)row * scale_row;
     }
-    // step j of a group of 512 columns
-    __device__ __forceinline__ uint4 load(int group, int j) const
+    // codes and scale of a step of 128 columns
+    __device__ __forceinline__ uint4 load(int step) const
     {
-        const int b = group * 16 + j * 4 + part;
+        const int b = step * 4 + part;
         return b < blocks ? *reinterpret_cast<const uint4 *>(codes + (size_t)b * 16) : make_uint4(0, 0, 0, 0);
     }
-    __device__ __forceinline__ unsigned load_scales(int group) const { return *reinterpret_cast<const unsigned *>(scales + (size_t)group * 16 + part * 4); }
+    __device__ __forceinline__ unsigned load_scale(int step) const { return scales[step * 4 + part]; }
 };
 
 // ---- up to 16 rows of x ---------------------------------------------------------------------------------------------------
@@ -96,22 +93,27 @@ __global__ __launch_bounds__(64 * TOKEN_WAVES) void mxfp4_token_kernel(int N, in
     __shared__ __align__(16) TokenRow rows[TOKEN_WAVES][16];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, quarter = lane >> 4;
     const long long k0 = (long long)blockIdx.x * 16;
-    const FilterRows filter(wc, ws, K, blocks, scale_row, lane);
+    const FilterRows filter(wc, ws, k0, K, blocks, scale_row, lane);
     const int groups = scale_row / 16;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
     uint4 next[4];
-    unsigned next_scales = 0;
+    unsigned next_scale[4];
     auto ahead = [&](int group) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) next[j] = filter.load(group, j);
-        next_scales = filter.load_scales(group);
+        for (int j = 0; j < 4; ++j) {
+            next[j] = filter.load(group * 4 + j);
+            next_scale[j] = filter.load_scale(group * 4 + j);
+        }
     };
     if (wave < groups) ahead(wave);
     for (int group = wave; group < groups; group += TOKEN_WAVES) {
         uint4 w[4];
+        unsigned sw[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) w[j] = next[j];
-        const unsigned sw = next_scales;
+        for (int j = 0; j < 4; ++j) {
+            w[j] = next[j];
+            sw[j] = next_scale[j];
+        }
         if (group + TOKEN_WAVES < groups) ahead(group + TOKEN_WAVES);
         const int column = group * 512 + lane * 8;
 #pragma unroll 1
@@ -145,7 +147,7 @@ __global__ __launch_bounds__(64 * TOKEN_WAVES) void mxfp4_token_kernel(int N, in
                 c = make_uint4(0, 0, 0, 0);
                 sx = 0;
             }
-            acc = mfma16<0, 0>(to_operand(w[j], lane), c, acc, to_scale(sw, lane, j), (int)(sx >> (8 * quarter)));
+            acc = mfma16<0, 0>(to_operand(w[j], lane), c, acc, to_operand(sw[j], lane), (int)(sx >> (8 * quarter)));
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
@@ -164,12 +166,12 @@ __global__ __launch_bounds__(64 * TOKEN_WAVES) void mxfp4_token_kernel(int N, in
 }
 
 // ---- some rows of x -------------------------------------------------------------------------------------------------------
-// x in the order in which the waves read it: [16 rows][step of 128 columns][lane] of 16 bytes, lane l: row l%16, block l/16 of the step, and
-// [16 rows][group of 512 columns][lane] words of scales, byte j: step j of the group.  Rows past N are zeros.
+// x in the order in which the waves read it: [16 rows][step of 128 columns][lane] of 16 bytes of codes, lane l: row l%16, block l/16 of the step, and
+// the same of bytes of scales.  Rows past N are zeros.
 template <typename T>
 __global__ __launch_bounds__(256) void mxfp4_order_kernel(int N, int C, int groups, const T *x, unsigned *xc, unsigned *xs)
 {
-    __shared__ unsigned words[64];
+    __shared__ unsigned char bytes[4][64];
     const int group = (int)(blockIdx.x % (unsigned)groups), tile = (int)(blockIdx.x / (unsigned)groups);
     const int quarter = threadIdx.x & 3, row = threadIdx.x >> 4, at = (threadIdx.x >> 2) & 3;       // four lanes a block, the step's block `at`
     const int n = tile * 16 + row, lane = row + 16 * at;
@@ -179,95 +181,85 @@ __global__ __launch_bounds__(256) void mxfp4_order_kernel(int N, int C, int grou
         const int column = group * 512 + j * 128 + at * 32 + quarter * 8;
         load8_edge(x + (n < N ? (size_t)n * C + column : 0), n < N ? C - column : 0, v[j]);
     }
-    unsigned bytes = 0;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const unsigned byte = mxfp4_scale_byte(max_quad(largest8(v[j])));
-        bytes |= byte << (8 * j);
+        if (quarter == 0) bytes[j][lane] = (unsigned char)byte;
         xc[(((size_t)blockIdx.x * 4 + j) * 64 + lane) * 4 + quarter] = mxfp4_codes8(v[j], byte);
     }
-    if (quarter == 0) words[lane] = bytes;
     __syncthreads();
-    if (threadIdx.x < 64) xs[(size_t)blockIdx.x * 64 + threadIdx.x] = words[threadIdx.x];
+    if (threadIdx.x < 64) xs[(size_t)blockIdx.x * 64 + threadIdx.x] = reinterpret_cast<const unsigned *>(bytes)[threadIdx.x];
 }
 
-template <int N, class F, int... U>
-__device__ __forceinline__ void each_number(F f, std::integer_sequence<int, U...>) { (f(std::integral_constant<int, U>()), ...); }
-template <int N, class F>
-__device__ __forceinline__ void each_number(F f) { each_number<N>(f, std::make_integer_sequence<int, N>()); }
-
-// 16 filter rows and 16*NF rows of x a workgroup, both straight from the caches into registers; its eight waves take every eighth group of
-// 512 columns, and their sums meet in LDS.
-template <typename T, int NF>
-__global__ __launch_bounds__(512) void mxfp4_skinny_kernel(int N, int K, int blocks, int scale_row, const uint4 *xc, const unsigned *xs, const unsigned char *wc,
-                                                           const unsigned char *ws, const float *bias, int relu, T *y)
+// 16*WF filter rows and 16*NF rows of x a workgroup, both straight from the caches into registers; its eight waves take every eighth step of
+// 128 columns, and their sums meet in LDS.  Two steps are under way while one is multiplied.
+template <typename T, int WF, int NF>
+__global__ __launch_bounds__(512) void mxfp4_skinny_kernel(int N, int K, int blocks, int scale_row, const unsigned char *xc, const unsigned char *xs,
+                                                           const unsigned char *wc, const unsigned char *ws, const float *bias, int relu, T *y)
 {
-    constexpr int WAVES = 8;
-    __shared__ f32x4 part[WAVES][NF][64];
+    constexpr int WAVES = 8, PLACES = 3;
+    __shared__ f32x4 part[WAVES][WF * NF][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int groups = scale_row / 16, tiles = (N + 15) / 16, tile0 = blockIdx.y * NF;
-    const long long k0 = (long long)blockIdx.x * 16;
-    const FilterRows filter(wc, ws, K, blocks, scale_row, lane);
-    // byte offsets of this lane's part of each tile of x (the last tile again where there are fewer): less than 4 GB for at most 128 rows
-    unsigned at[NF], scale_at[NF];
+    const int groups = scale_row / 16, tiles = (N + 15) / 16, tile0 = blockIdx.y * NF, all = (blocks + 3) / 4;
+    const long long k0 = (long long)blockIdx.x * (16 * WF);
+    FilterRows filter[WF];
 #pragma unroll
-    for (int i = 0; i < NF; ++i) {
-        const unsigned unit = (unsigned)min(tile0 + i, tiles - 1) * (unsigned)groups;
-        at[i] = unit * 4096u + (unsigned)lane * 16u;
-        scale_at[i] = unit * 256u + (unsigned)lane * 4u;
-    }
-    const char *codes = (const char *)xc, *scales = (const char *)xs;
-    f32x4 acc[NF] = {};
-    // A wave's steps of 128 columns, four a group, follow each other over its groups; three places for them: two steps are under way while
-    // one is multiplied (a fourth place would not fit the registers).
+    for (int i = 0; i < WF; ++i) filter[i] = FilterRows(wc, ws, k0 + 16 * i, K, blocks, scale_row, lane);
+    // first steps of each tile of x (the last tile again where there are fewer): offsets are less than 4 GB for at most 128 rows
+    unsigned first[NF];
+#pragma unroll
+    for (int i = 0; i < NF; ++i) first[i] = (unsigned)min(tile0 + i, tiles - 1) * (unsigned)groups * 4u;
+    f32x4 acc[WF][NF] = {};
     struct Step {
-        uint4 w, x[NF];
-    } place[3];
-    unsigned scales_w[2];
-    int scales_x[2][NF];
-    const int steps = wave < groups ? ((groups - 1 - wave) / WAVES + 1) * 4 : 0;
+        uint4 w[WF], x[NF];
+        unsigned sw[WF];
+        int sx[NF];
+    } place[PLACES];
     auto load = [&](Step &s, int step) {
-        const int group = wave + (step >> 2) * WAVES, j = step & 3;
-        s.w = filter.load(group, j);
 #pragma unroll
-        for (int i = 0; i < NF; ++i) s.x[i] = *reinterpret_cast<const uint4 *>(codes + (at[i] + (unsigned)(group * 4 + j) * 1024u));
+        for (int i = 0; i < WF; ++i) {
+            s.w[i] = filter[i].load(step);
+            s.sw[i] = filter[i].load_scale(step);
+        }
+#pragma unroll
+        for (int i = 0; i < NF; ++i) {
+            const unsigned at = (first[i] + (unsigned)step) * 64u + (unsigned)lane;
+            s.x[i] = reinterpret_cast<const uint4 *>(xc)[at];
+            s.sx[i] = xs[at];
+        }
     };
-    auto load_scales = [&](int which, int step) {
-        const int group = wave + (step >> 2) * WAVES;
-        scales_w[which] = filter.load_scales(group);
+    auto multiply = [&](const Step &s) {
 #pragma unroll
-        for (int i = 0; i < NF; ++i) scales_x[which][i] = *reinterpret_cast<const int *>(scales + (scale_at[i] + (unsigned)group * 256u));
+        for (int i = 0; i < WF; ++i) {
+            const uint4 w = to_operand(s.w[i], lane);
+            const int sw = to_operand(s.sw[i], lane);
+#pragma unroll
+            for (int q = 0; q < NF; ++q) acc[i][q] = mfma16<0, 0>(w, s.x[q], acc[i][q], sw, s.sx[q]);
+        }
     };
-    if (steps > 0) {
-        load(place[0], 0);
-        load_scales(0, 0);
-        load(place[1], 1);
-        for (int base = 0; base < steps; base += 24) {      // 24 steps: whole turns of the places, the groups and their two sets of scales
-            auto one = [&](auto number) {
-                constexpr int U = decltype(number)::value, J = U & 3, SET = (U >> 2) & 1;
-                const int step = base + U;
-                if (step >= steps) return;
-                if (step + 2 < steps) load(place[(U + 2) % 3], step + 2);
-                if (J == 2 && step + 2 < steps) load_scales(SET ^ 1, step + 2);
-                const Step &s = place[U % 3];
-                const uint4 w = to_operand(s.w, lane);
-                const int mine = to_scale(scales_w[SET], lane, J);
+    if (wave < all) load(place[0], wave);
+    if (wave + WAVES < all) load(place[1], wave + WAVES);
+    for (int step = wave; step < all; step += PLACES * WAVES) {
 #pragma unroll
-                for (int i = 0; i < NF; ++i) acc[i] = mfma16<0, J>(w, s.x[i], acc[i], mine, scales_x[SET][i]);
-            };
-            each_number<24>(one);
+        for (int u = 0; u < PLACES; ++u) {
+            const int now = step + u * WAVES;
+            if (now >= all) break;
+            if (now + 2 * WAVES < all) load(place[(u + 2) % PLACES], now + 2 * WAVES);
+            multiply(place[u]);
         }
     }
 #pragma unroll
-    for (int i = 0; i < NF; ++i) part[wave][i][lane] = acc[i];
+    for (int i = 0; i < WF; ++i)
+#pragma unroll
+        for (int q = 0; q < NF; ++q) part[wave][i * NF + q][lane] = acc[i][q];
     __syncthreads();
     // a thread: four neighbouring columns of a row, in ascending order of waves
-    for (int u = threadIdx.x; u < NF * 64; u += 512) {
+    for (int u = threadIdx.x; u < WF * NF * 64; u += 512) {
         const int f = u >> 6, l = u & 63;
         f32x4 v = part[0][f][l];
 #pragma unroll
         for (int w = 1; w < WAVES; ++w) v += part[w][f][l];
-        const long long k = k0 + (l >> 4) * 4, n = (tile0 + f) * 16ll + (l & 15);
+        const long long k = k0 + (f / NF) * 16 + (l >> 4) * 4, n = (tile0 + f % NF) * 16ll + (l & 15);
         if (n >= N) continue;
 #pragma unroll
         for (int e = 0; e < 4; ++e)
@@ -515,6 +507,8 @@ __global__ __launch_bounds__(64 * GM * GN, 1) void mxfp4_tile_kernel(int N, int 
 
 // ---- host -----------------------------------------------------------------------------------------------------------------
 
+constexpr int WIDE_K = 8192;
+
 enum Path { TOKEN, SKINNY, TILED };
 Path path_of(int N, int C, int K)
 {
@@ -571,12 +565,13 @@ int fc(int N, int C, int K, const T *x, const unsigned char *wc, const unsigned 
         if ((long long)groups * tiles > 0x7FFFFFFFll) return MXC_ERR_SHAPE;
         hipLaunchKernelGGL(mxfp4_order_kernel<T>, dim3((unsigned)(groups * tiles)), dim3(256), 0, st, N, C, groups, x, (unsigned *)xc, (unsigned *)xs);
         if (hipGetLastError() != hipSuccess) return MXC_ERR_LAUNCH;
-        const dim3 grid((unsigned)((K + 15ll) / 16)), block(512);
-        const uint4 *codes = (const uint4 *)xc;
-        const unsigned *scales = (const unsigned *)xs;
-        if (N <= 32) hipLaunchKernelGGL((mxfp4_skinny_kernel<T, 2>), grid, block, 0, st, N, K, blocks, scale_row, codes, scales, wc, ws, bias, relu, y);
-        else if (N <= 64) hipLaunchKernelGGL((mxfp4_skinny_kernel<T, 4>), grid, block, 0, st, N, K, blocks, scale_row, codes, scales, wc, ws, bias, relu, y);
-        else hipLaunchKernelGGL((mxfp4_skinny_kernel<T, 8>), grid, block, 0, st, N, K, blocks, scale_row, codes, scales, wc, ws, bias, relu, y);
+        void (*kernel)(int, int, int, int, const unsigned char *, const unsigned char *, const unsigned char *, const unsigned char *, const float *, int, T *);
+        const bool wide = K >= WIDE_K;
+        if (N <= 32) kernel = wide ? mxfp4_skinny_kernel<T, 2, 2> : mxfp4_skinny_kernel<T, 1, 2>;
+        else if (N <= 64) kernel = wide ? mxfp4_skinny_kernel<T, 2, 4> : mxfp4_skinny_kernel<T, 1, 4>;
+        else kernel = wide ? mxfp4_skinny_kernel<T, 2, 8> : mxfp4_skinny_kernel<T, 1, 8>;
+        const int rows = wide ? 32 : 16;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)((K + rows - 1ll) / rows)), dim3(512), 0, st, N, K, blocks, scale_row, xc, xs, wc, ws, bias, relu, y);
         return hipGetLastError() == hipSuccess ? MXC_OK : MXC_ERR_LAUNCH;
     }
     const int groups = (int)(((long long)C + 255) / 256);
