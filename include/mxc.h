@@ -370,7 +370,7 @@ int mxc_mxfp4_fc_fwd(int N, int C, int K, int dtype, const void *x, const void *
                      const float *bias, int relu, void *y, void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /*
- * AdamW step over many tensors in one call (a launch for every MXC_ADAMW_GROUP tensors).  For each value, with
+ * AdamW step over many tensors in one call (a launch for every MXC_ADAMW_GROUP tensors, or MXC_ADAMW8_GROUP).  For each value, with
  * gs = grad_scale*g and t = step (1 for the first):
  *   m' = beta1*m + (1 - beta1)*gs,   v' = beta2*v + (1 - beta2)*gs*gs
  *   w' = w*(1 - lr*wd) - lr/(1 - beta1^t) * m' / ( sqrt(v')/sqrt(1 - beta2^t) + eps )
@@ -388,7 +388,7 @@ int mxc_mxfp4_fc_fwd(int N, int C, int K, int dtype, const void *x, const void *
  * Errors, found before anything is launched: MXC_ERR_SHAPE (count <= 0, step < 1, a tensor of more than 2^34 values), MXC_ERR_UNSUPPORTED (grad_dtype;
  * beta1 or beta2 outside [0, 1); negative eps; a factor that is not finite), MXC_ERR_NULL, MXC_ERR_ALIGN (16 bytes), MXC_ERR_LAUNCH.
  */
-enum { MXC_ADAMW_GROUP = 72 };
+enum { MXC_ADAMW_GROUP = 72, MXC_ADAMW8_GROUP = 88 };
 int mxc_adamw_update(int count, const size_t *sizes, void *const *w, const void *const *g, int grad_dtype, void *const *m,
                      void *const *v, void *const *w_bf16, double lr, double beta1, double beta2, double eps, double wd,
                      double grad_scale, long long step, void *hip_stream);

@@ -1,7 +1,7 @@
 // AdamW over many tensors: m' = beta1*m + (1 - beta1)*g, v' = beta2*v + (1 - beta2)*g*g,
 // w' = keep*w - rate*m'/(sqrt(v')*root_scale + eps), with states in fp32, or m and r = sqrt(v) in 8 bits with a scale for
-// every 32 values.  The tensors' pointers and sizes travel in the kernel's arguments, MXC_ADAMW_GROUP tensors a launch, so that
-// nothing is copied to the device and a captured launch holds all that it needs.
+// every 32 values.  The tensors' pointers and sizes travel in the kernel's arguments, MXC_ADAMW_GROUP tensors a launch (with 8-bit states
+// MXC_ADAMW8_GROUP), so that nothing is copied to the device and a captured launch holds all that it needs.
 #include "mxc_internal.h"
 
 // every operation rounds by itself: where a code of 8 bits is decided, no product is kept unrounded in one place and not in another
@@ -13,19 +13,29 @@ namespace {
 struct Tensor {
     float *w;
     const void *g;
-    void *m;            // fp32, or the 8-bit states
-    float *v;
+    float *m, *v;
     bf16_t *copy;
     size_t n;
 };
+struct Tensor8 {
+    float *w;
+    const void *g;
+    unsigned char *state;
+    bf16_t *copy;
+    size_t n;
+};
+template <class TENSOR, int N>
 struct Group {
-    Tensor t[MXC_ADAMW_GROUP];
-    unsigned first[MXC_ADAMW_GROUP + 1];        // workgroups before tensor i's
-    int count, base;                            // base: tensors in the call before this group's
+    static constexpr int MOST = N;
+    TENSOR t[N];
+    unsigned first[N + 1];      // workgroups before tensor i's
+    int count, base;            // base: tensors in the call before this group's
     AdamwFactors f;
     unsigned seed;
 };
-static_assert(sizeof(Group) <= 4096, "kernel arguments");
+typedef Group<Tensor, MXC_ADAMW_GROUP> Group32;
+typedef Group<Tensor8, MXC_ADAMW8_GROUP> Group8;
+static_assert(sizeof(Group32) <= 4096 && sizeof(Group8) <= 4096, "kernel arguments");
 
 __device__ __forceinline__ float step_one(float &w, float g, float &m, float &v, const AdamwFactors &f)
 {
@@ -39,11 +49,12 @@ __device__ __forceinline__ float step_one(float &w, float g, float &m, float &v,
 
 // the tensor of this workgroup: the last one that begins at or before it (tensors of no values begin where the next one does).  Every lane
 // looks at one place of the table, which is one access to the kernel's arguments where a binary search is seven in a row.
-__device__ __forceinline__ int find_tensor(const Group &q)
+template <class GROUP>
+__device__ __forceinline__ int find_tensor(const GROUP &q)
 {
     const int lane = threadIdx.x & 63;
     int n = __popcll(__ballot(lane < q.count && q.first[lane] <= blockIdx.x));
-    if (q.count > 64) n += __popcll(__ballot(64 + lane < q.count && q.first[min(64 + lane, MXC_ADAMW_GROUP)] <= blockIdx.x));
+    if (q.count > 64) n += __popcll(__ballot(64 + lane < q.count && q.first[min(64 + lane, GROUP::MOST)] <= blockIdx.x));
     return __builtin_amdgcn_readfirstlane(n - 1);
 }
 
@@ -80,12 +91,12 @@ template <bool NT>
 __device__ __forceinline__ void store4(bf16_t *p, const float *v) { store<NT>(p, u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])}); }
 
 template <typename G, bool NT>
-__global__ __launch_bounds__(256) void adamw_kernel(Group q)
+__global__ __launch_bounds__(256) void adamw_kernel(Group32 q)
 {
     const int i = find_tensor(q);
     const Tensor &t = q.t[i];
     const size_t j = (size_t)(blockIdx.x - q.first[i]) * CHUNK + threadIdx.x * 4;
-    float *tm = (float *)t.m;
+    float *const tm = t.m;
     const G *tg = (const G *)t.g;
     if (j + 4 <= t.n) {
         const f32x4 w4 = load4<NT>(t.w + j), m4 = load4<NT>(tm + j), v4 = load4<NT>(t.v + j), g4 = load4<NT>(tg + j);
@@ -134,9 +145,9 @@ __device__ __forceinline__ unsigned block_largest(const float *x)
     unsigned b = 0;
 #pragma unroll
     for (int k = 0; k < 4; ++k) b = max(b, __float_as_uint(x[k]) & 0x7FFFFFFFu);
-#pragma unroll
-    for (int d = 1; d < 8; d <<= 1) b = max(b, (unsigned)__shfl_xor((int)b, d));
-    return b;
+    b = max(b, (unsigned)__builtin_amdgcn_update_dpp(0, (int)b, 0xB1, 0xF, 0xF, true));      // lanes 1 0 3 2
+    b = max(b, (unsigned)__builtin_amdgcn_update_dpp(0, (int)b, 0x4E, 0xF, 0xF, true));      // lanes 2 3 0 1
+    return max(b, (unsigned)__builtin_amdgcn_update_dpp(0, (int)b, 0x141, 0xF, 0xF, true));  // the other half of eight
 }
 
 // scale byte of a block: the smallest power of two with which its largest value is at most 448 = 1.75*2^8
@@ -161,14 +172,14 @@ __device__ __forceinline__ unsigned e4m3_code(float x, float up, unsigned u16, b
 
 // a wave holds one record of 256 values, four a lane, eight lanes a block
 template <typename G, bool NT>
-__global__ __launch_bounds__(256) void adamw8_kernel(Group q)
+__global__ __launch_bounds__(256) void adamw8_kernel(Group8 q)
 {
     const int i = find_tensor(q);
-    const Tensor &t = q.t[i];
+    const Tensor8 &t = q.t[i];
     const int lane = threadIdx.x & 63;
     const size_t record = (size_t)(blockIdx.x - q.first[i]) * (CHUNK / 256) + (threadIdx.x >> 6);
     if (record * 256 >= t.n) return;
-    unsigned char *state = (unsigned char *)t.m + record * ADAMW8_RECORD;
+    unsigned char *state = t.state + record * ADAMW8_RECORD;
     const size_t j = record * 256 + lane * 4;
     const unsigned mc = load<NT, unsigned>(state + lane * 4), rc = load<NT, unsigned>(state + 256 + lane * 4);
     const unsigned msb = state[512 + lane / 8], rsb = state[520 + lane / 8];
@@ -223,6 +234,30 @@ __global__ __launch_bounds__(256) void adamw8_kernel(Group q)
     }
 }
 
+// one launch for every GROUP::MOST tensors; tensor(k): the k-th one's entry
+template <class GROUP, class F>
+int launch_groups(void (*kernel)(GROUP), int count, const AdamwFactors &f, unsigned seed, hipStream_t st, F tensor)
+{
+    for (int base = 0; base < count; base += GROUP::MOST) {
+        GROUP q;
+        q.count = count - base < GROUP::MOST ? count - base : GROUP::MOST;
+        q.base = base;
+        q.f = f;
+        q.seed = seed;
+        size_t blocks = 0;      // (fewer than 2^31: a tensor has no more than 2^34 values)
+        for (int i = 0; i < q.count; ++i) {
+            q.t[i] = tensor(base + i);
+            q.first[i] = (unsigned)blocks;
+            blocks += (q.t[i].n + CHUNK - 1) / CHUNK;
+        }
+        q.first[q.count] = (unsigned)blocks;
+        if (blocks == 0) continue;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, st, q);
+        if (hipGetLastError() != hipSuccess) return MXC_ERR_LAUNCH;
+    }
+    return MXC_OK;
+}
+
 }  // namespace
 
 int adamw_update(int count, const size_t *sizes, void *const *w, const void *const *g, int grad_dtype, void *const *m, void *const *v,
@@ -230,32 +265,14 @@ int adamw_update(int count, const size_t *sizes, void *const *w, const void *con
 {
     size_t values = 0;
     for (int i = 0; i < count; ++i) values += sizes[i];
-    // what the call touches, against the 256 MB of the last cache
-    const bool past = values * (8 + elem_size(grad_dtype) + (v ? 16 : 4) + (w_bf16 ? 2 : 0)) > (size_t)256 << 20;
-    for (int base = 0; base < count; base += MXC_ADAMW_GROUP) {
-        Group q;
-        q.count = count - base < MXC_ADAMW_GROUP ? count - base : MXC_ADAMW_GROUP;
-        q.base = base;
-        q.f = f;
-        q.seed = seed;
-        size_t blocks = 0;
-        for (int i = 0; i < q.count; ++i) {
-            const int k = base + i;
-            q.t[i] = Tensor{(float *)w[k], g[k], m[k], v ? (float *)v[k] : nullptr, w_bf16 ? (bf16_t *)w_bf16[k] : nullptr, sizes[k]};
-            q.first[i] = (unsigned)blocks;
-            blocks += (sizes[k] + CHUNK - 1) / CHUNK;
-            if (blocks > 0x7FFFFFFFu) return MXC_ERR_SHAPE;
-        }
-        q.first[q.count] = (unsigned)blocks;
-        if (blocks == 0) continue;
-        const dim3 grid((unsigned)blocks), block(256);
-        void (*kernel)(Group);
-        if (v) kernel = grad_dtype == MXC_BF16 ? (past ? adamw_kernel<bf16_t, true> : adamw_kernel<bf16_t, false>) : (past ? adamw_kernel<float, true> : adamw_kernel<float, false>);
-        else kernel = grad_dtype == MXC_BF16 ? (past ? adamw8_kernel<bf16_t, true> : adamw8_kernel<bf16_t, false>) : (past ? adamw8_kernel<float, true> : adamw8_kernel<float, false>);
-        hipLaunchKernelGGL(kernel, grid, block, 0, st, q);
-        if (hipGetLastError() != hipSuccess) return MXC_ERR_LAUNCH;
-    }
-    return MXC_OK;
+    // what the call reads and writes, against the 256 MB of the last cache
+    const bool bf16 = grad_dtype == MXC_BF16, past = values * (4 + elem_size(grad_dtype) + (v ? 8 : 2) + (w_bf16 ? 2 : 0)) > (size_t)256 << 20;
+    auto copy = [&](int k) { return w_bf16 ? (bf16_t *)w_bf16[k] : nullptr; };
+    if (v)
+        return launch_groups<Group32>(bf16 ? (past ? adamw_kernel<bf16_t, true> : adamw_kernel<bf16_t, false>) : (past ? adamw_kernel<float, true> : adamw_kernel<float, false>),
+                                      count, f, seed, st, [&](int k) { return Tensor{(float *)w[k], g[k], (float *)m[k], (float *)v[k], copy(k), sizes[k]}; });
+    return launch_groups<Group8>(bf16 ? (past ? adamw8_kernel<bf16_t, true> : adamw8_kernel<bf16_t, false>) : (past ? adamw8_kernel<float, true> : adamw8_kernel<float, false>), count,
+                                 f, seed, st, [&](int k) { return Tensor8{(float *)w[k], g[k], (unsigned char *)m[k], copy(k), sizes[k]}; });
 }
 
 }  // namespace mxc

@@ -133,8 +133,9 @@ def test_adamw8_mean_and_seed(mxc):
         state = [torch.zeros(bytes_, dtype=torch.uint8, device="cuda") for _ in range(tensors)]
         mxc.mxc_adamw8_update([w.clone() for _ in state], [g] * tensors, state, None, **H, step=1, seed=seed)
         return state
-    a, b = run(7, 75), run(7, 75)
+    a, b = run(7, 95), run(7, 95)       # more than one launch
     assert all(torch.equal(x, y) for x, y in zip(a, b))
+    assert len({bytes(x.cpu().numpy().tobytes()) for x in a}) == 95
     assert not torch.equal(a[0], a[1]) and not torch.equal(a[0], a[72]) and not torch.equal(a[1], a[73]) and not torch.equal(a[0], run(8)[0])
     _, m, v, _, _, _ = exact_step(w, g, torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda"), 1)
     total_m, total_r, rounds = 0.0, 0.0, 400
