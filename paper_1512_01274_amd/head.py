@@ -1,0 +1,133 @@
+"""A classifier's head, trained and then served in 4 bits: the library's layers and the operators at the end of a network together.
+
+A training step is two FullyConnected layers forward (bias and ReLU in the first), the log probabilities of the labels
+with the gradient of their mean, the layers' gradients, and one AdamW call over all four tensors, with states in 32 bits
+or in 8.  Serving brings the filters into microscaled 4-bit floating point once; a request runs the layers on them and
+asks for the most probable classes with their log probabilities.
+
+Usage: python -m paper_1512_01274_amd.head [--bits 8] [--steps 200]
+"""
+import argparse
+
+import torch
+
+from paper_1512_01274_amd import mxc
+
+BF16 = mxc.MXC_BF16
+
+
+class Head:
+    """y = w2 relu(w1 x + b1) + b2 for rows x of `features` values, `classes` logits; master weights in fp32, copies in bf16."""
+
+    def __init__(self, features, hidden, classes, bits=32, seed=0, device="cuda"):
+        gen = torch.Generator(device=device).manual_seed(seed)
+        shapes = [(hidden, features), (hidden,), (classes, hidden), (classes,)]
+        self.dims, self.bits, self.step = (features, hidden, classes), bits, 0
+        self.w = [torch.randn(s, generator=gen, device=device) * (2.0 / s[1]) ** 0.5 if len(s) == 2 else torch.zeros(s, device=device) for s in shapes]
+        self.copy = [w.bfloat16() for w in self.w]
+        self.grad = [torch.zeros_like(w) for w in self.w]
+        if bits == 32:
+            self.m, self.v = [torch.zeros_like(w) for w in self.w], [torch.zeros_like(w) for w in self.w]
+        else:
+            self.state = [torch.zeros(mxc.mxc_adamw8_state_bytes(w.numel()), dtype=torch.uint8, device=device) for w in self.w]
+        self._buffers = {}
+
+    def _of_batch(self, N):
+        """Activations, gradients and workspace for batches of N, made once."""
+        if N not in self._buffers:
+            C, H, K = self.dims
+            new = lambda *s, dtype=torch.bfloat16: torch.empty(*s, dtype=dtype, device=self.w[0].device)  # noqa: E731
+            need = [mxc.mxc_conv2d_workspace_bytes(op, N, c, 1, 1, k, 1, 1, 1, 0, BF16, mxc.MXC_NHWC)
+                    for c, k in ((C, H), (H, K)) for op in (mxc.MXC_FWD, mxc.MXC_BWD_DATA_RELU, mxc.MXC_BWD_WEIGHT, mxc.MXC_BIAS_GRAD)]
+            need.append(mxc.mxc_logprob_workspace_bytes(N, K, BF16, 0))
+            self._buffers[N] = {"h": new(N, H), "z": new(N, K), "dh": new(N, H), "logp": new(N, dtype=torch.float32),
+                                "weight": torch.full((N,), -1.0 / N, device=self.w[0].device), "workspace": mxc.alloc_workspace(max(need))}
+        return self._buffers[N]
+
+    def train_step(self, x, labels, lr=1e-3, wd=0.01):
+        """One step on bf16 rows x and int32 labels; returns the log probabilities of the labels (before the step)."""
+        N, (C, H, K) = x.shape[0], self.dims
+        b = self._of_batch(N)
+        ws = b["workspace"]
+        mxc.mxc_fc_fwd(N, C, H, BF16, x, self.copy[0], self.w[1], True, b["h"], ws)
+        mxc.mxc_fc_fwd(N, H, K, BF16, b["h"], self.copy[2], self.w[3], False, b["z"], ws)
+        # the loss is the mean of -logp: its gradient in logp is -1/N; dz takes the logits' place
+        mxc.mxc_logprob_fwd_bwd(N, K, K, BF16, b["z"], labels, 1.0, b["weight"], None, b["logp"], None, b["z"], ws)
+        mxc.mxc_fc_bwd_weight(N, H, K, BF16, b["h"], b["z"], self.grad[2], ws)
+        mxc.mxc_bias_grad(N, K, 1, 1, BF16, mxc.MXC_NHWC, b["z"], self.grad[3], ws)
+        mxc.mxc_fc_bwd_data(N, H, K, BF16, b["z"], self.copy[2], b["h"], b["dh"], ws)
+        mxc.mxc_fc_bwd_weight(N, C, H, BF16, x, b["dh"], self.grad[0], ws)
+        mxc.mxc_bias_grad(N, H, 1, 1, BF16, mxc.MXC_NHWC, b["dh"], self.grad[1], ws)
+        self.step += 1
+        rest = (lr, 0.9, 0.999, 1e-8, wd, 1.0, self.step)
+        if self.bits == 32:
+            mxc.mxc_adamw_update(self.w, self.grad, self.m, self.v, self.copy, *rest)
+        else:
+            mxc.mxc_adamw8_update(self.w, self.grad, self.state, self.copy, *rest, self.step)
+        return b["logp"]
+
+    def served(self):
+        return Served(self)
+
+
+class Served:
+    """A head whose filters are held in 4 bits: 17 bytes for 32 weights."""
+
+    def __init__(self, head):
+        self.dims, self.bias, self.filters = head.dims, (head.w[1].clone(), head.w[3].clone()), []
+        for w in (head.w[0], head.w[2]):
+            K, C = w.shape
+            codes = torch.empty(K, -(-C // 32) * 16, dtype=torch.uint8, device=w.device)
+            scales = torch.empty(K, -(-C // 512) * 16, dtype=torch.uint8, device=w.device)
+            mxc.mxc_mxfp4_quantize(K, C, mxc.MXC_F32, w, codes, scales)
+            self.filters.append((codes, scales))
+
+    def score(self, x, labels=None, top=5):
+        """(log probabilities of the labels or None, entropy, the `top` most probable classes' log probabilities and indices) of bf16 rows x."""
+        N, (C, H, K) = x.shape[0], self.dims
+        new = lambda *s, dtype=torch.float32: torch.empty(*s, dtype=dtype, device=x.device)  # noqa: E731
+        h, z = new(N, H, dtype=torch.bfloat16), new(N, K, dtype=torch.bfloat16)
+        need = [mxc.mxc_mxfp4_fc_workspace_bytes(N, C, H, BF16), mxc.mxc_mxfp4_fc_workspace_bytes(N, H, K, BF16), mxc.mxc_logprob_workspace_bytes(N, K, BF16, top)]
+        ws = mxc.alloc_workspace(max(need), device=x.device)
+        mxc.mxc_mxfp4_fc_fwd(N, C, H, BF16, x, *self.filters[0], self.bias[0], True, h, ws)
+        mxc.mxc_mxfp4_fc_fwd(N, H, K, BF16, h, *self.filters[1], self.bias[1], False, z, ws)
+        logp, entropy = None if labels is None else new(N), new(N)
+        top_logp, top_index = new(N, top), new(N, top, dtype=torch.int32)
+        mxc.mxc_logprob_fwd(N, K, K, BF16, z, labels, 1.0, top, logp, entropy, None, top_logp, top_index, ws)
+        return logp, entropy, top_logp, top_index
+
+
+def clusters(features, classes, seed=1, device="cuda"):
+    """Synthetic data: a direction for each class, and batches of noisy samples of them."""
+    gen = torch.Generator(device=device).manual_seed(seed)
+    centre = torch.randn(classes, features, generator=gen, device=device)
+
+    def batch(N):
+        labels = torch.randint(0, classes, (N,), generator=gen, device=device, dtype=torch.int32)
+        return (centre[labels.long()] + 1.5 * torch.randn(N, features, generator=gen, device=device)).bfloat16(), labels
+    return batch
+
+
+def main(argv=None):
+    ap = argparse.ArgumentParser(description=__doc__.splitlines()[0])
+    ap.add_argument("--features", type=int, default=512)
+    ap.add_argument("--hidden", type=int, default=1024)
+    ap.add_argument("--classes", type=int, default=1000)
+    ap.add_argument("--batch", type=int, default=256)
+    ap.add_argument("--steps", type=int, default=200)
+    ap.add_argument("--bits", type=int, choices=(8, 32), default=32, help="of the optimiser's states")
+    a = ap.parse_args(argv)
+    head, batch = Head(a.features, a.hidden, a.classes, a.bits), clusters(a.features, a.classes)
+    for i in range(a.steps):
+        loss = -head.train_step(*batch(a.batch))
+        if i % 50 == 0 or i == a.steps - 1:
+            print(f"step {i:4d}  loss {float(loss.mean()):.4f}", flush=True)
+    x, labels = batch(a.batch)
+    logp, entropy, _, top = head.served().score(x, labels)
+    right = top == labels[:, None]
+    print(f"served in 4 bits: loss {-float(logp.mean()):.4f}, entropy {float(entropy.mean()):.4f}, "
+          f"first {float(right[:, 0].float().mean()):.3f}, first five {float(right.any(1).float().mean()):.3f}")
+
+
+if __name__ == "__main__":
+    main()
