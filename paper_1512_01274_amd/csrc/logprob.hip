@@ -199,8 +199,8 @@ struct Extent<float> {
 };
 
 // A row as pieces at 16-byte boundaries: the first and the last may be shared with what lies before and behind the row, which is
-// neither read nor written.
-template <typename T>
+// neither read nor written.  NT: past the caches, for calls of more than they hold.
+template <typename T, bool NT = false>
 struct Row {
     static constexpr int V = Piece<T>::V;
     const T *z;         // element `head` elements before the row's first
@@ -225,7 +225,9 @@ struct Row {
     {
         Piece<T> p;
         if (whole(piece) && piece < end) {
-            const uint4 u = reinterpret_cast<const uint4 *>(z)[(unsigned)piece];
+            typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+            const u32x4 *from = reinterpret_cast<const u32x4 *>(z) + (unsigned)piece;
+            const u32x4 u = NT ? __builtin_nontemporal_load(from) : *from;
             p.w[0] = u.x; p.w[1] = u.y; p.w[2] = u.z; p.w[3] = u.w;
         } else {
             p.nothing();
@@ -248,10 +250,13 @@ struct Row {
     __device__ __forceinline__ void store(int piece, const float *g) const
     {
         if (whole(piece)) {
-            uint4 u;
-            if constexpr (V == 8) u = make_uint4(pack_bf16x2(g[0], g[1]), pack_bf16x2(g[2], g[3]), pack_bf16x2(g[4], g[5]), pack_bf16x2(g[6], g[7]));
-            else u = make_uint4(__float_as_uint(g[0]), __float_as_uint(g[1]), __float_as_uint(g[2]), __float_as_uint(g[3]));
-            reinterpret_cast<uint4 *>(dz)[(unsigned)piece] = u;
+            typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+            u32x4 u;
+            if constexpr (V == 8) u = u32x4{pack_bf16x2(g[0], g[1]), pack_bf16x2(g[2], g[3]), pack_bf16x2(g[4], g[5]), pack_bf16x2(g[6], g[7])};
+            else u = u32x4{__float_as_uint(g[0]), __float_as_uint(g[1]), __float_as_uint(g[2]), __float_as_uint(g[3])};
+            u32x4 *to = reinterpret_cast<u32x4 *>(dz) + (unsigned)piece;
+            if (NT) __builtin_nontemporal_store(u, to);
+            else *to = u;
         } else if (piece < pieces) {
 #pragma unroll
             for (int k = 0; k < V; ++k) {
@@ -482,7 +487,7 @@ __device__ __forceinline__ void each_value(const Piece<T> (&p)[P], int held, int
 
 // G threads a row, P pieces a thread; rows of fewer than a wave's lanes share one.  TOP: with the most probable tokens, else
 // the gradient where dz is given.
-template <typename T, int G, int P, bool TOP>
+template <typename T, int G, int P, bool TOP, bool NT = false>
 __global__ __launch_bounds__(G < 64 ? 256 : G, G == 512 && P == 16 ? 4 : 1) void logprob_row_kernel(LogprobArgs a)
 {
     constexpr int W = G / 64;       // waves a row; 0: several rows a wave
@@ -491,7 +496,7 @@ __global__ __launch_bounds__(G < 64 ? 256 : G, G == 512 && P == 16 ? 4 : 1) void
     const int lane = G < 64 ? threadIdx.x % G : threadIdx.x;
     const size_t row = G < 64 ? (size_t)blockIdx.x * (256 / G) + threadIdx.x / G : (size_t)blockIdx.x;
     if (G < 64 && row >= (size_t)a.N) return;
-    const Row<T> r(a, row);
+    const Row<T, NT> r(a, row);
     Piece<T> p[P];
     const int held = (r.pieces + G - 1) / G;        // pieces that any thread holds: what follows passes over the others
     float low = 0.f;        // (above nothing that matters)
@@ -708,9 +713,9 @@ struct Part {       // of a chunk: its largest value, its sums, and the label's 
 
 // The values of a chunk once more, from memory, for the rare rows whose candidates do not fit their list: cells are every fourth of a
 // thread's pieces.
-template <typename T, int UNROLL>
+template <typename T, int UNROLL, bool NT>
 struct Streamed {
-    const Row<T> &r;
+    const Row<T, NT> &r;
     int begin, end, K;
     const unsigned *cell;
     template <class F>
@@ -742,14 +747,14 @@ struct Streamed {
     }
 };
 
-template <typename T, bool TOP, int UNROLL>
+template <typename T, bool TOP, int UNROLL, bool NT>
 __global__ __launch_bounds__(CHUNK_THREADS) void logprob_stream_kernel(LogprobArgs a, int chunks, int chunk_pieces, Part *parts, unsigned long long *keys)
 {
     constexpr int V = Piece<T>::V, LOW = sizeof(T) == 2 ? 16 : 0;
     __shared__ float red[3][4];
     const size_t row = blockIdx.x / (unsigned)chunks;
     const int chunk = blockIdx.x % (unsigned)chunks, wave = threadIdx.x >> 6;
-    const Row<T> r(a, row);
+    const Row<T, NT> r(a, row);
     const int begin = chunk * chunk_pieces, end = min(begin + chunk_pieces, r.pieces);
     const float k2 = a.scale * LOG2E;
     // (read first: two accesses that wait for each other)
@@ -759,15 +764,16 @@ __global__ __launch_bounds__(CHUNK_THREADS) void logprob_stream_kernel(LogprobAr
     float m = LOWEST, shift = 0.f, s = 0.f, t = 0.f, low = 0.f;
 
     // Candidates for the most probable tokens: pieces with a value that reaches a bound which `top` values have reached so far are set aside as they
-    // pass.  The bound comes from what each wave says of its lanes' maxima (top/4 lanes have reached it), before the first turn and
-    // after 1, 2, 4, ...; a wave may read an older word of another one, which is a bound too.  Minus infinities are never set aside.
+    // pass.  The bound comes from what each wave says of its lanes' maxima: its share of `top` lanes have reached it, a quarter, or less of a wave that
+    // has fewer lanes with a value, and more of the others.  They say so before the first turn and after 1, 2, 4, ...; a wave may read
+    // an older word of another one, which is a bound too.  Minus infinities are never set aside.
     constexpr int CAP = 1024;
     __shared__ Aside<T, TOP ? 640 : 1> aside;
     float limit = LOWEST, seen = -INFINITY, of[UNROLL];
-    int turn = 0;
+    int turn = 0, share = 0;        // share: less than 0 where there are not `top` lanes
     auto say = [&]() {
         const unsigned cells[1] = {order(seen)};
-        const unsigned b = wave_bound<1, LOW>(cells, (a.top + 3) / 4);
+        const unsigned b = share > 0 ? wave_bound<1, LOW>(cells, share) : share == 0 ? 0xFFFFFFFFu : 0u;
         if ((threadIdx.x & 63) == 0) *(volatile unsigned *)&aside.said[wave] = b;
     };
     auto hear = [&]() {
@@ -785,6 +791,17 @@ __global__ __launch_bounds__(CHUNK_THREADS) void logprob_stream_kernel(LogprobAr
     if constexpr (TOP) {
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) seen = fmaxf(seen, p[u].template largest<true>());
+        const unsigned lanes = (unsigned)__popcll(__ballot(seen > -INFINITY));
+        if ((threadIdx.x & 63) == 0) aside.said[4 + wave] = lanes;
+        __syncthreads();
+        unsigned most = (unsigned)(a.top + 3) / 4, total = 0;
+        for (; most <= 64u; ++most) {
+            total = 0;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) total += min(aside.said[4 + w], most);
+            if (total >= (unsigned)a.top) break;
+        }
+        share = total >= (unsigned)a.top ? (int)min(lanes, most) : -1;
         say();
         __syncthreads();
         hear();
@@ -845,9 +862,11 @@ __global__ __launch_bounds__(CHUNK_THREADS) void logprob_stream_kernel(LogprobAr
         }
     }
     if constexpr (TOP) {
+        if (end - begin > UNROLL * CHUNK_THREADS) {     // (else it has been said)
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u) seen = fmaxf(seen, of[u]);
-        say();
+            for (int u = 0; u < UNROLL; ++u) seen = fmaxf(seen, of[u]);
+            say();
+        }
     }
     float most = meet<64>(m, larger);
     if ((threadIdx.x & 63) == 0) red[0][wave] = most;
@@ -883,7 +902,7 @@ __global__ __launch_bounds__(CHUNK_THREADS) void logprob_stream_kernel(LogprobAr
         unsigned cell[UNROLL];
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) cell[u] = begin + u * CHUNK_THREADS + (int)threadIdx.x < end ? order(of[u]) : 0u;
-        select_top<4, UNROLL, LOW>(sh, cell, a.top, Streamed<T, UNROLL>{r, begin, end, a.K, cell}, emit);
+        select_top<4, UNROLL, LOW>(sh, cell, a.top, Streamed<T, UNROLL, NT>{r, begin, end, a.K, cell}, emit);
     }
 }
 
@@ -925,8 +944,9 @@ __device__ __forceinline__ Joined join_parts(const Part *parts, int chunks, floa
     return j;
 }
 
-// What chunks found out about a row, joined by one wave.  A chunk's keys are in descending order: the first DEPTH of each give the bound, and a lane goes
-// down its chunks' lists as far as that.
+// What chunks found out about a row, joined by one wave.  A chunk's keys are in descending order: the first ones of each give the bound, and a lane goes
+// down its chunks' lists as far as that.  Up to 64 chunks: the lanes hold the first 256 keys counted across the lists, which holds all that matters but for
+// rare rows; more: the first four of each.
 template <typename T, bool TOP>
 __global__ __launch_bounds__(64) void logprob_join_kernel(LogprobArgs a, int chunks, const Part *parts, const unsigned long long *keys)
 {
@@ -938,29 +958,67 @@ __global__ __launch_bounds__(64) void logprob_join_kernel(LogprobArgs a, int chu
     const int label = a.labels ? a.labels[row] : -1;
     const float zl = parts[0].zl;       // (every chunk has it)
     unsigned cell[DEPTH] = {};
+    unsigned long long own[DEPTH] = {};
+    const bool across = chunks <= 64;
     if constexpr (TOP) {
         keys += row * chunks * top;
-        for (int c = lane; c < chunks; c += 64)
+#pragma unroll
+        for (int d = 0; d < DEPTH; ++d) {
+            const int e = lane + 64 * d, c = across ? e % chunks : lane, at = across ? e / chunks : d;
+            own[d] = at < top ? keys[(size_t)c * top + at] : NO_KEY;
+        }
+#pragma unroll
+        for (int d = 0; d < DEPTH; ++d) cell[d] = (unsigned)(own[d] >> 32);
+        for (int c = lane + 64; c < chunks; c += 64)
 #pragma unroll
             for (int d = 0; d < DEPTH; ++d) cell[d] = max(cell[d], d < top ? (unsigned)(keys[(size_t)c * top + d] >> 32) : 0u);
     }
     const Joined j = join_parts<1>(parts, chunks, a.scale, red);
     if (lane == 0) write_row_results(a, row, label, zl, j);
     if constexpr (TOP) {
+        auto emit = [&](int i, unsigned long long key) { write_top(a, row, j, i, key); };
+        if (j.s == 0.f) {       // minus infinities alone
+            if (lane < top) emit(lane, lane < a.K ? key_of(order(-INFINITY), (unsigned)lane) : NO_KEY);
+            return;
+        }
         constexpr int CAP = 1024;
         __shared__ TopShared<CAP> sh;
         if (lane == 0) sh.count = 0;
         __syncthreads();
         const unsigned bound = wave_bound<DEPTH, LOW>(cell, top);
-        auto emit = [&](int i, unsigned long long key) { write_top(a, row, j, i, key); };
-        for (int c = lane; c < chunks; c += 64)
-            for (int i = 0; i < top; ++i) {
-                const unsigned long long key = keys[(size_t)c * top + i];
-                if (key == NO_KEY || (unsigned)(key >> 32) < bound) break;
-                const int at = atomicAdd(&sh.count, 1);
-                if (at < CAP) sh.list[at] = key;
-                else break;
-            }
+        // Many equal values: the index decides among those at the bound as well.
+        unsigned long long least = (unsigned long long)bound << 32;
+        int above = 0, reach = 0;
+        unsigned low[DEPTH];
+#pragma unroll
+        for (int d = 0; d < DEPTH; ++d) {
+            const bool equal = cell[d] >> LOW == bound >> LOW;
+            above += __popcll(__ballot(cell[d] >= bound && !equal));
+            reach += __popcll(__ballot(cell[d] >= bound));
+            low[d] = equal ? (unsigned)own[d] : 0u;
+        }
+        if (across && reach > top + 32) {
+            const unsigned index = wave_bound<DEPTH, 0>(low, top - above);
+            least = (unsigned long long)(bound | (LOW ? (1u << LOW) - 1u : 0u)) << 32 | index;
+        }
+        auto take = [&](unsigned long long key) {       // whether to go on down the list
+            // (keys at the bound differ in what lies below LOW only by their sign's fill: there all of them count as the largest)
+            const unsigned o = (unsigned)(key >> 32);
+            const unsigned long long as = o >> LOW == bound >> LOW ? (key | (unsigned long long)(LOW ? (1u << LOW) - 1u : 0u) << 32) : key;
+            if (key == NO_KEY || as < least) return false;
+            const int at = atomicAdd(&sh.count, 1);
+            if (at < CAP) sh.list[at] = key;
+            return at < CAP;
+        };
+        bool on = true;
+#pragma unroll
+        for (int d = 0; d < DEPTH; ++d) on = (across || on) && take(own[d]);
+        if (across) {       // what lies below the keys that were held
+            if (lane < chunks)
+                for (int i = (64 * DEPTH - lane + chunks - 1) / chunks; i < top && take(keys[(size_t)lane * top + i]); ++i) {}
+        } else
+            for (int c = lane, i = DEPTH; c < chunks; c += 64, i = 0, on = true)
+                for (; on && i < top; ++i) on = take(keys[(size_t)c * top + i]);
         __syncthreads();
         const int n = sh.count;
         if (n <= CAP) {
@@ -1060,11 +1118,15 @@ Cut cut_rows(int N, int pieces, bool gradient)
     int chunks = N >= 256 ? 1 : (1024 + N - 1) / N;
     chunks = chunks < (pieces + CHUNK_THREADS - 1) / CHUNK_THREADS ? chunks : (pieces + CHUNK_THREADS - 1) / CHUNK_THREADS;
     Cut c;
-    c.pieces = ((pieces + chunks - 1) / chunks + CHUNK_THREADS - 1) / CHUNK_THREADS * CHUNK_THREADS;
+    c.pieces = (pieces + chunks - 1) / chunks;
     c.chunks = (pieces + c.pieces - 1) / c.pieces;
     return c;
 }
 int block_count(int pieces, int per_thread) { return (int)((pieces + (long long)CHUNK_THREADS * per_thread - 1) / (CHUNK_THREADS * per_thread)); }
+
+// Whether the logits alone fill the 256 MB of the last cache: then accesses go past the caches.  4096 rows of 50257 bf16: 90 -> 86 us with the top
+// tokens, 161 -> 152 with the gradient; the gradient of 131072 does not gain.
+bool past_caches(const LogprobArgs &a) { return (size_t)a.N * a.ld * elem_size(a.dtype) > (size_t)256 << 20; }
 
 template <typename T, bool TOP>
 void launch_row(const LogprobArgs &a, hipStream_t st)
@@ -1080,9 +1142,12 @@ void launch_row(const LogprobArgs &a, hipStream_t st)
     else if (pieces <= 512) hipLaunchKernelGGL((logprob_row_kernel<T, 256, 2, TOP>), rows, dim3(256), 0, st, a);
     else if (TOP || pieces <= 1024) hipLaunchKernelGGL((logprob_row_kernel<T, 256, 4, TOP>), rows, dim3(256), 0, st, a);
     else if (pieces <= 2048) hipLaunchKernelGGL((logprob_row_kernel<T, 256, 8, false>), rows, dim3(256), 0, st, a);
-    else if (pieces <= 4096) hipLaunchKernelGGL((logprob_row_kernel<T, 512, 8, false>), rows, dim3(512), 0, st, a);
-    else if (pieces <= 8192) hipLaunchKernelGGL((logprob_row_kernel<T, 512, 16, false>), rows, dim3(512), 0, st, a);
-    else hipLaunchKernelGGL((logprob_row_kernel<T, 1024, 16, false>), rows, dim3(1024), 0, st, a);
+    else {
+        const bool past = past_caches(a);
+        if (pieces <= 4096) hipLaunchKernelGGL((past ? logprob_row_kernel<T, 512, 8, false, true> : logprob_row_kernel<T, 512, 8, false>), rows, dim3(512), 0, st, a);
+        else if (pieces <= 8192) hipLaunchKernelGGL((past ? logprob_row_kernel<T, 512, 16, false, true> : logprob_row_kernel<T, 512, 16, false>), rows, dim3(512), 0, st, a);
+        else hipLaunchKernelGGL((logprob_row_kernel<T, 1024, 16, false>), rows, dim3(1024), 0, st, a);
+    }
 }
 
 template <typename T>
@@ -1102,12 +1167,15 @@ int launch(const LogprobArgs &a, void *workspace, hipStream_t st)
     Part *parts = alone ? nullptr : (Part *)workspace;
     unsigned long long *keys = (unsigned long long *)((char *)workspace + align_up(grid * sizeof(Part), 256));
     const dim3 g((unsigned)grid), b(CHUNK_THREADS);
+    const bool past = !a.dz && past_caches(a);      // (what a gradient reads once more should stay)
     // a piece a thread: short code, whose fetching counts
     const bool once = cut.pieces <= CHUNK_THREADS;
-    if (a.top && once) hipLaunchKernelGGL((logprob_stream_kernel<T, true, 1>), g, b, 0, st, a, cut.chunks, cut.pieces, parts, keys);
-    else if (a.top) hipLaunchKernelGGL((logprob_stream_kernel<T, true, 4>), g, b, 0, st, a, cut.chunks, cut.pieces, parts, keys);
-    else if (once) hipLaunchKernelGGL((logprob_stream_kernel<T, false, 1>), g, b, 0, st, a, cut.chunks, cut.pieces, parts, keys);
-    else hipLaunchKernelGGL((logprob_stream_kernel<T, false, 4>), g, b, 0, st, a, cut.chunks, cut.pieces, parts, keys);
+    if (a.top && once) hipLaunchKernelGGL((logprob_stream_kernel<T, true, 1, false>), g, b, 0, st, a, cut.chunks, cut.pieces, parts, keys);
+    else if (a.top && past) hipLaunchKernelGGL((logprob_stream_kernel<T, true, 4, true>), g, b, 0, st, a, cut.chunks, cut.pieces, parts, keys);
+    else if (a.top) hipLaunchKernelGGL((logprob_stream_kernel<T, true, 4, false>), g, b, 0, st, a, cut.chunks, cut.pieces, parts, keys);
+    else if (once) hipLaunchKernelGGL((logprob_stream_kernel<T, false, 1, false>), g, b, 0, st, a, cut.chunks, cut.pieces, parts, keys);
+    else if (past) hipLaunchKernelGGL((logprob_stream_kernel<T, false, 4, true>), g, b, 0, st, a, cut.chunks, cut.pieces, parts, keys);
+    else hipLaunchKernelGGL((logprob_stream_kernel<T, false, 4, false>), g, b, 0, st, a, cut.chunks, cut.pieces, parts, keys);
     if (hipGetLastError() != hipSuccess) return MXC_ERR_LAUNCH;
     if (alone) return MXC_OK;
     const dim3 gg((unsigned)((size_t)a.N * blocks));
