@@ -327,10 +327,10 @@ int mxc_sgd_update(size_t n, float *w, const float *g, float *v, void *w_bf16,
  *   mxc_logprob_fwd_bwd  both at once, which reads z once: logp or entropy may be NULL
  * dz may be z itself.  scale must be positive and finite.  Workspace: mxc_logprob_workspace_bytes (top 0 for
  * mxc_logprob_fwd_bwd, none for mxc_logprob_bwd).  Results are bit-identical from run to run.  Errors: MXC_ERR_SHAPE (non-positive N
- * or K, ld < K, top out of range), MXC_ERR_UNSUPPORTED (dtype, scale), MXC_ERR_NULL, MXC_ERR_ALIGN (16 bytes for z and dz,
+ * or K, K above MXC_LOGPROB_MAX_K, ld < K, top out of range, more rows than one launch holds), MXC_ERR_UNSUPPORTED (dtype, scale), MXC_ERR_NULL, MXC_ERR_ALIGN (16 bytes for z and dz,
  * 4 for the others), MXC_ERR_WORKSPACE, MXC_ERR_LAUNCH.
  */
-enum { MXC_LOGPROB_MAX_TOP = 64 };
+enum { MXC_LOGPROB_MAX_TOP = 64, MXC_LOGPROB_MAX_K = 1 << 30 };
 int mxc_logprob_workspace_bytes(int N, int K, int dtype, int top, size_t *out_bytes);
 int mxc_logprob_fwd(int N, int K, int ld, int dtype, const void *z, const int *labels, float scale, int top,
                     float *logp, float *entropy, float *stats, float *top_logp, int *top_index,
@@ -352,8 +352,8 @@ int mxc_logprob_fwd_bwd(int N, int K, int ld, int dtype, const void *z, const in
  *       representable one, ties to the even code, larger ones than 6 to 6.  A block that holds an infinity or a NaN has b = 255
  *       and codes 0: all of it reads as NaN.
  *   mxc_mxfp4_dequantize  the numbers the codes stand for, rounded once to `dtype`
- * x, y: [N][C] of `dtype`, dense.  No workspace.  Errors: MXC_ERR_SHAPE, MXC_ERR_UNSUPPORTED (dtype), MXC_ERR_NULL, MXC_ERR_ALIGN
- * (16 bytes), MXC_ERR_LAUNCH.
+ * x, y: [N][C] of `dtype`, dense.  No workspace.  Errors: MXC_ERR_SHAPE (also for more values than one launch holds: about 2^35 in a call, 2^27 filter rows), MXC_ERR_UNSUPPORTED (dtype),
+ * MXC_ERR_NULL, MXC_ERR_ALIGN (16 bytes), MXC_ERR_LAUNCH.
  *
  * FullyConnected on a filter in this form: y[n,k] = act( sum_c q(x)[n,c] * w[k,c] + bias[k] ), x: [N][C] and y: [N][K]
  * of `dtype`, w_codes and w_scales as above for K rows of C values, q(x) the values of mxc_mxfp4_quantize (the
@@ -370,7 +370,8 @@ int mxc_mxfp4_fc_fwd(int N, int C, int K, int dtype, const void *x, const void *
                      const float *bias, int relu, void *y, void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /*
- * AdamW step over many tensors in one call (a launch for every MXC_ADAMW_GROUP tensors, or MXC_ADAMW8_GROUP).  For each value, with
+ * AdamW step over many tensors in one call (a launch for every MXC_ADAMW_GROUP tensors, or MXC_ADAMW8_GROUP,
+ * and 2^34 values).  For each value, with
  * gs = grad_scale*g and t = step (1 for the first):
  *   m' = beta1*m + (1 - beta1)*gs,   v' = beta2*v + (1 - beta2)*gs*gs
  *   w' = w*(1 - lr*wd) - lr/(1 - beta1^t) * m' / ( sqrt(v')/sqrt(1 - beta2^t) + eps )
@@ -385,7 +386,7 @@ int mxc_mxfp4_fc_fwd(int N, int C, int K, int dtype, const void *x, const void *
  * between them plus u >= 1, u a multiple of 2^-16 taken from a hash of the value's index, the tensor's number and `seed` (16 bits of it for m, 16 for r; the
  * same call gives the same codes).  An r that is not 0 does not become code 0: a weight's step never divides by eps alone
  * because of a rounding.  A block of m or r that holds an infinity or a NaN gets scale 255 and reads as NaN.
- * Errors, found before anything is launched: MXC_ERR_SHAPE (count <= 0, step < 1, a tensor of more than 2^34 values), MXC_ERR_UNSUPPORTED (grad_dtype;
+ * Errors, found before anything is launched: MXC_ERR_SHAPE (count <= 0, step < 1, a tensor of more than 2^33 values), MXC_ERR_UNSUPPORTED (grad_dtype;
  * beta1 or beta2 outside [0, 1); negative eps; a factor that is not finite), MXC_ERR_NULL, MXC_ERR_ALIGN (16 bytes), MXC_ERR_LAUNCH.
  */
 enum { MXC_ADAMW_GROUP = 72, MXC_ADAMW8_GROUP = 88 };

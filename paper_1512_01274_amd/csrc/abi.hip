@@ -1028,7 +1028,7 @@ int mxc_sgd_update(size_t n, float *w, const float *g, float *v, void *w_bf16, f
 
 static int logprob_check(int N, int K, int ld, int dtype, const void *z, float scale)
 {
-    if (N <= 0 || K <= 0 || ld < K) return MXC_ERR_SHAPE;
+    if (N <= 0 || K <= 0 || K > MXC_LOGPROB_MAX_K || ld < K) return MXC_ERR_SHAPE;
     if (dtype != MXC_F32 && dtype != MXC_BF16) return MXC_ERR_UNSUPPORTED;
     if (!(scale > 0.f) || !std::isfinite(scale)) return MXC_ERR_UNSUPPORTED;
     return z ? MXC_OK : MXC_ERR_NULL;
@@ -1037,7 +1037,7 @@ static int logprob_check(int N, int K, int ld, int dtype, const void *z, float s
 int mxc_logprob_workspace_bytes(int N, int K, int dtype, int top, size_t *out_bytes)
 {
     if (!out_bytes) return MXC_ERR_NULL;
-    if (N <= 0 || K <= 0 || top < 0 || top > MXC_LOGPROB_MAX_TOP) return MXC_ERR_SHAPE;
+    if (N <= 0 || K <= 0 || K > MXC_LOGPROB_MAX_K || top < 0 || top > MXC_LOGPROB_MAX_TOP) return MXC_ERR_SHAPE;
     if (dtype != MXC_F32 && dtype != MXC_BF16) return MXC_ERR_UNSUPPORTED;
     *out_bytes = align_up(logprob_workspace(N, K, dtype, top), 256);
     return MXC_OK;
@@ -1148,7 +1148,7 @@ static int adamw_check(int count, const size_t *sizes, const void *const *const 
     for (int k = 0; k < kinds; ++k)
         if (!tensors[k]) return MXC_ERR_NULL;
     for (int i = 0; i < count; ++i)
-        if (sizes[i] > (size_t)1 << 34) return MXC_ERR_SHAPE;        // (a group's workgroups are counted in 31 bits)
+        if (sizes[i] > (size_t)1 << 33) return MXC_ERR_SHAPE;        // (one launch holds its workgroups)
     for (int i = 0; i < count; ++i) {
         if (sizes[i] == 0) continue;
         for (int k = 0; k < kinds; ++k)
@@ -1177,7 +1177,7 @@ int mxc_adamw_update(int count, const size_t *sizes, void *const *w, const void 
 int mxc_adamw8_state_bytes(size_t n, size_t *out_bytes)
 {
     if (!out_bytes) return MXC_ERR_NULL;
-    if (n > (size_t)1 << 34) return MXC_ERR_SHAPE;
+    if (n > (size_t)1 << 33) return MXC_ERR_SHAPE;
     *out_bytes = (n + 255) / 256 * ADAMW8_RECORD;
     return MXC_OK;
 }

@@ -234,23 +234,27 @@ __global__ __launch_bounds__(256) void adamw8_kernel(Group8 q)
     }
 }
 
-// one launch for every GROUP::MOST tensors; tensor(k): the k-th one's entry
+// one launch for every GROUP::MOST tensors, or for fewer where one launch does not hold these; tensor(k): the k-th one's entry
 template <class GROUP, class F>
 int launch_groups(void (*kernel)(GROUP), int count, const AdamwFactors &f, unsigned seed, hipStream_t st, F tensor)
 {
-    for (int base = 0; base < count; base += GROUP::MOST) {
+    for (int base = 0; base < count;) {
         GROUP q;
-        q.count = count - base < GROUP::MOST ? count - base : GROUP::MOST;
         q.base = base;
         q.f = f;
         q.seed = seed;
-        size_t blocks = 0;      // (fewer than 2^31: a tensor has no more than 2^34 values)
-        for (int i = 0; i < q.count; ++i) {
+        size_t blocks = 0;
+        int i = 0;
+        for (; i < GROUP::MOST && base + i < count; ++i) {
             q.t[i] = tensor(base + i);
+            const size_t more = (q.t[i].n + CHUNK - 1) / CHUNK;
+            if (!one_launch(blocks + more, 256)) break;        // (the first one fits: it has 2^33 values at most)
             q.first[i] = (unsigned)blocks;
-            blocks += (q.t[i].n + CHUNK - 1) / CHUNK;
+            blocks += more;
         }
-        q.first[q.count] = (unsigned)blocks;
+        q.count = i;
+        q.first[i] = (unsigned)blocks;
+        base += i;
         if (blocks == 0) continue;
         hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, st, q);
         if (hipGetLastError() != hipSuccess) return MXC_ERR_LAUNCH;

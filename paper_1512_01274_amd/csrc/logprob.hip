@@ -1156,13 +1156,14 @@ int launch(const LogprobArgs &a, void *workspace, hipStream_t st)
     const int pieces = row_pieces(a.K, a.dtype, a.ld);
     const Cut cut = cut_rows(a.N, pieces, a.dz != nullptr);
     if (cut.chunks == 0) {
+        if (!one_launch(a.N + 31ll, !a.top && pieces <= 8 ? 8 : pieces <= 256 ? 64 : pieces <= 2048 ? 256 : pieces <= 8192 ? 512 : 1024)) return MXC_ERR_SHAPE;
         if (a.top) launch_row<T, true>(a, st);
         else launch_row<T, false>(a, st);
         return hipGetLastError() == hipSuccess ? MXC_OK : MXC_ERR_LAUNCH;
     }
     const size_t grid = (size_t)a.N * cut.chunks;
     const int per = pieces <= 2048 || a.N < 160 ? 1 : 4, blocks = block_count(pieces, per);
-    if (grid > 0x7FFFFFFFu || (size_t)cut.chunks * (a.top ? a.top : 1) > 0x7FFFFFFFu || (a.dz && (size_t)a.N * blocks > 0x7FFFFFFFu)) return MXC_ERR_SHAPE;
+    if (!one_launch(grid, CHUNK_THREADS) || (a.dz && !one_launch((size_t)a.N * blocks, CHUNK_THREADS))) return MXC_ERR_SHAPE;
     const bool alone = cut.chunks == 1 && !a.dz;
     Part *parts = alone ? nullptr : (Part *)workspace;
     unsigned long long *keys = (unsigned long long *)((char *)workspace + align_up(grid * sizeof(Part), 256));
@@ -1191,7 +1192,7 @@ int launch_bwd(const LogprobArgs &a, const float *stats, const float *entropy, h
 {
     const int pieces = row_pieces(a.K, a.dtype, a.ld), per = pieces <= CHUNK_THREADS ? 1 : 4, blocks = block_count(pieces, per);
     const size_t grid = (size_t)a.N * blocks;
-    if (grid > 0x7FFFFFFFu) return MXC_ERR_SHAPE;
+    if (!one_launch(grid, CHUNK_THREADS)) return MXC_ERR_SHAPE;
     const dim3 g((unsigned)grid), b(CHUNK_THREADS);
     if (per == 1) hipLaunchKernelGGL((logprob_bwd_kernel<T, 1>), g, b, 0, st, a, blocks, stats, entropy);
     else hipLaunchKernelGGL((logprob_bwd_kernel<T, 4>), g, b, 0, st, a, blocks, stats, entropy);

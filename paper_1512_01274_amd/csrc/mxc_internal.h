@@ -311,6 +311,9 @@ int sgd_update(size_t n, float *w, const float *g, float *v, void *w_copy, float
 int softmax_fwd(int N, int K, int dtype, const void *z, void *p, hipStream_t st);
 int softmax_xent_bwd(int N, int K, int dtype, const void *p, const int *labels, void *dz, float scale, hipStream_t st);
 
+// one launch holds fewer than 2^32 threads
+inline bool one_launch(unsigned long long workgroups, int threads) { return workgroups * threads <= 0xFFFFFFFFull; }
+
 // ---- logprob.hip: log probabilities, entropies, top tokens and their gradient -------------
 size_t logprob_workspace(int N, int K, int dtype, int top);
 struct LogprobArgs {

@@ -80,7 +80,7 @@ int quantize(int N, int C, const void *x, void *codes, void *scales, hipStream_t
 {
     const FastDiv blocks((int)(mxfp4_code_row(C) / 16));
     const size_t grid = ((size_t)N * blocks.d + 63) / 64;
-    if (grid > 0x7FFFFFFFu) return MXC_ERR_SHAPE;
+    if (!one_launch(grid, 256)) return MXC_ERR_SHAPE;
     hipLaunchKernelGGL(mxfp4_quantize_kernel<T>, dim3((unsigned)grid), dim3(256), 0, st, N, C, blocks, (int)mxfp4_scale_row(C), (const T *)x, (unsigned *)codes,
                        (unsigned char *)scales);
     return hipGetLastError() == hipSuccess ? MXC_OK : MXC_ERR_LAUNCH;
@@ -91,7 +91,7 @@ int dequantize(int N, int C, const void *codes, const void *scales, void *y, hip
 {
     const FastDiv blocks((int)(mxfp4_code_row(C) / 16));
     const size_t grid = ((size_t)N * blocks.d + 63) / 64;
-    if (grid > 0x7FFFFFFFu) return MXC_ERR_SHAPE;
+    if (!one_launch(grid, 256)) return MXC_ERR_SHAPE;
     hipLaunchKernelGGL(mxfp4_dequantize_kernel<T>, dim3((unsigned)grid), dim3(256), 0, st, N, C, blocks, (int)mxfp4_scale_row(C), (const unsigned *)codes,
                        (const unsigned char *)scales, (T *)y);
     return hipGetLastError() == hipSuccess ? MXC_OK : MXC_ERR_LAUNCH;

@@ -543,7 +543,7 @@ int launch_tiles(int N, int C, int K, const unsigned char *xc, const unsigned *x
 {
     typedef Tile<FM, FN, GM, GN> G;
     const long long kt = (K + G::BM - 1ll) / G::BM, nt = (N + G::BN - 1ll) / G::BN;
-    if (kt * nt > 0x7FFFFFFFll / 8) return MXC_ERR_SHAPE;
+    if (!one_launch(kt * nt, 64 * G::WAVES)) return MXC_ERR_SHAPE;
     hipLaunchKernelGGL((mxfp4_tile_kernel<T, FM, FN, GM, GN>), dim3((unsigned)(kt * nt)), dim3(64 * G::WAVES), 0, st, N, K, (int)mxfp4_code_row(C), (int)(((long long)C + 255) / 256), xc, xs,
                        wc, wt, bias, relu, y, (int)kt, (int)nt);
     return MXC_OK;
@@ -555,6 +555,7 @@ int fc(int N, int C, int K, const T *x, const unsigned char *wc, const unsigned 
     const int blocks = (int)(mxfp4_code_row(C) / 16), scale_row = (int)mxfp4_scale_row(C);
     const Path path = path_of(N, C, K);
     if (path == TOKEN) {
+        if (!one_launch((K + 15ll) / 16, 64 * TOKEN_WAVES)) return MXC_ERR_SHAPE;
         hipLaunchKernelGGL(mxfp4_token_kernel<T>, dim3((unsigned)((K + 15ll) / 16)), dim3(64 * TOKEN_WAVES), 0, st, N, C, K, blocks, scale_row, x, wc, ws, bias, relu, y);
         return hipGetLastError() == hipSuccess ? MXC_OK : MXC_ERR_LAUNCH;
     }
@@ -562,7 +563,7 @@ int fc(int N, int C, int K, const T *x, const unsigned char *wc, const unsigned 
     unsigned char *xc = (unsigned char *)workspace, *xs = xc + b.scales;
     if (path == SKINNY) {
         const int groups = scale_row / 16, tiles = (N + 15) / 16;
-        if ((long long)groups * tiles > 0x7FFFFFFFll) return MXC_ERR_SHAPE;
+        if (!one_launch((unsigned long long)groups * tiles, 256) || !one_launch((K + 15ll) / 16, 512)) return MXC_ERR_SHAPE;
         hipLaunchKernelGGL(mxfp4_order_kernel<T>, dim3((unsigned)(groups * tiles)), dim3(256), 0, st, N, C, groups, x, (unsigned *)xc, (unsigned *)xs);
         if (hipGetLastError() != hipSuccess) return MXC_ERR_LAUNCH;
         void (*kernel)(int, int, int, int, const unsigned char *, const unsigned char *, const unsigned char *, const unsigned char *, const float *, int, T *);
@@ -577,7 +578,7 @@ int fc(int N, int C, int K, const T *x, const unsigned char *wc, const unsigned 
     const int groups = (int)(((long long)C + 255) / 256);
     unsigned *xt = (unsigned *)xs, *wt = (unsigned *)((unsigned char *)workspace + b.filter_scales);
     const size_t x_groups = ((size_t)N + 31) / 32 * groups, w_groups = ((size_t)K + 31) / 32 * ((groups + 7) / 8);
-    if (x_groups + w_groups > 0x7FFFFFFFu) return MXC_ERR_SHAPE;
+    if (!one_launch(x_groups + w_groups, 256)) return MXC_ERR_SHAPE;
     hipLaunchKernelGGL(mxfp4_prepare_kernel<T>, dim3((unsigned)(x_groups + w_groups)), dim3(256), 0, st, N, C, K, blocks, scale_row, groups, (unsigned)x_groups, x, (unsigned *)xc, xt, ws, wt);
     if (hipGetLastError() != hipSuccess) return MXC_ERR_LAUNCH;
     const long long big = ((K + 255ll) / 256) * ((N + 255ll) / 256);

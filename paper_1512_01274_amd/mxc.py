@@ -19,7 +19,7 @@ MXC_FWD, MXC_BWD_DATA, MXC_BWD_WEIGHT, MXC_BWD_DATA_RELU, MXC_BIAS_GRAD = 0, 1, 
 MXC_BWD_DATA_FILTER, MXC_BWD_DATA_PREPARED, MXC_BWD_DATA_PREPARED_RELU, MXC_BWD_WEIGHT_BF16 = 5, 6, 7, 8
 MXC_INPUT_PREPARED, MXC_FWD_PREPARED_INPUT, MXC_BWD_WEIGHT_PREPARED_INPUT, MXC_BWD_WEIGHT_PREPARED_INPUT_BF16 = 9, 10, 11, 12
 MXC_FWD_TRANSFORM = 13
-MXC_LOGPROB_MAX_TOP, MXC_MXFP4_FC_MAX_C, MXC_ADAMW_GROUP, MXC_ADAMW8_GROUP = 64, 1 << 23, 72, 88
+MXC_LOGPROB_MAX_TOP, MXC_LOGPROB_MAX_K, MXC_MXFP4_FC_MAX_C, MXC_ADAMW_GROUP, MXC_ADAMW8_GROUP = 64, 1 << 30, 1 << 23, 72, 88
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libmxc.so")
 if not os.path.exists(LIB_PATH):

@@ -134,3 +134,27 @@ def test_binding_lists(mxc):
     with pytest.raises(mxc.MxcError) as e:
         mxc.mxc_adamw_update([], [], [], [], None, *args, 0)
     assert e.value.status == mxc.MXC_ERR_SHAPE
+
+
+def test_sizes_past_a_launch(mxc):
+    """More threads than one launch holds, or indexes past 31 bits, are refused before a launch."""
+    lib, n, most = mxc.raw(), ctypes.c_size_t(), (1 << 31) - 1
+    K = mxc.MXC_LOGPROB_MAX_K
+    assert lib.mxc_logprob_workspace_bytes(1, K + 1, 0, 0, ctypes.byref(n)) == mxc.MXC_ERR_SHAPE
+    assert lib.mxc_logprob_workspace_bytes(1, K, 0, 64, ctypes.byref(n)) == mxc.MXC_OK
+    assert lib.mxc_logprob_fwd(1, K + 1, K + 1, 1, A, B, 1.0, 0, C_, D, E, None, None, H, 1 << 40, None) == mxc.MXC_ERR_SHAPE
+    assert lib.mxc_logprob_bwd(1, K + 1, K + 1, 1, A, B, 1.0, C_, D, E, F_, G, None) == mxc.MXC_ERR_SHAPE
+    assert lib.mxc_logprob_fwd_bwd(1, K + 1, K + 1, 1, A, B, 1.0, C_, D, E, F_, G, H, 1 << 40, None) == mxc.MXC_ERR_SHAPE
+    for top, k in ((0, 1), (0, 100), (5, 1), (0, 5000), (0, 20000)):
+        assert lib.mxc_logprob_fwd(most, k, k, 1, A, B, 1.0, top, C_, D, E, F_, G, H, 1 << 60, None) == mxc.MXC_ERR_SHAPE, (top, k)
+        assert lib.mxc_logprob_fwd_bwd(most, k, k, 1, A, B, 1.0, C_, D, E, F_, G, H, 1 << 60, None) == mxc.MXC_ERR_SHAPE, k
+        assert lib.mxc_logprob_bwd(most, k, k, 1, A, B, 1.0, C_, D, E, F_, G, None) == mxc.MXC_ERR_SHAPE, k
+    for call in (lib.mxc_mxfp4_quantize, lib.mxc_mxfp4_dequantize):
+        assert call(most, 1, 1, A, B, C_, None) == mxc.MXC_ERR_SHAPE
+    for N, k in ((1, most), (20, most), (129, most - 70000000)):
+        assert lib.mxc_mxfp4_fc_fwd(N, 1, k, 1, A, B, C_, D, 0, E, F_, 1 << 60, None) == mxc.MXC_ERR_SHAPE
+    assert lib.mxc_mxfp4_fc_fwd(4, mxc.MXC_MXFP4_FC_MAX_C + 1, 8, 1, A, B, C_, D, 0, E, F_, 1 << 60, None) == mxc.MXC_ERR_SHAPE
+    with pytest.raises(mxc.MxcError):
+        mxc.mxc_mxfp4_fc_workspace_bytes(4, mxc.MXC_MXFP4_FC_MAX_C + 1, 8, 1)
+    with pytest.raises(mxc.MxcError):
+        mxc.mxc_adamw8_state_bytes((1 << 33) + 1)
