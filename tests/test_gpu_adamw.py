@@ -197,3 +197,38 @@ def test_graph(mxc):
         assert all(torch.equal(a, b) for a, b in zip(everything, want))
         for t in g:
             t.copy_(torch.randn(t.numel(), device="cuda"))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("bits", [32, 8])
+def test_more_than_the_caches(mxc, dtype, bits):
+    """More than 256 MB, which pass the caches by."""
+    sizes = [34000003, 5, 2999]
+    if bits == 32:
+        test_adamw(mxc, dtype, True, sizes)
+    else:
+        test_adamw8(mxc, dtype, sizes)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_past_32_bits(mxc, bits):
+    """A tensor of more than 2^31 values: its last ones are those of a tensor of these alone (8 bits: the weights, after one step)."""
+    n, last = (1 << 31) + 256 * 4 + 77, 256 * 3 + 77
+    w, g = torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda", dtype=torch.bfloat16)
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    w[n - last:], g[n - last:] = torch.randn(last, generator=gen, device="cuda"), torch.randn(last, generator=gen, device="cuda").bfloat16()
+    small = w[n - last:].clone(), g[n - last:].clone()
+    copy = torch.empty(n, device="cuda", dtype=torch.bfloat16)
+    if bits == 32:
+        m, v = torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda")
+        sm, sv = torch.zeros(last, device="cuda"), torch.zeros(last, device="cuda")
+        mxc.mxc_adamw_update([w], [g], [m], [v], [copy], **H, step=1)
+        mxc.mxc_adamw_update([small[0]], [small[1]], [sm], [sv], None, **H, step=1)
+        assert torch.equal(m[n - last:], sm) and torch.equal(v[n - last:], sv)
+    else:
+        state = torch.zeros(mxc.mxc_adamw8_state_bytes(n), dtype=torch.uint8, device="cuda")
+        ss = torch.zeros(mxc.mxc_adamw8_state_bytes(last), dtype=torch.uint8, device="cuda")
+        mxc.mxc_adamw8_update([w], [g], [state], [copy], **H, step=1, seed=1)
+        mxc.mxc_adamw8_update([small[0]], [small[1]], [ss], None, **H, step=1, seed=1)
+        assert torch.equal(state.view(-1, 528)[-4:, 512:], ss.view(-1, 528)[:, 512:])
+    assert torch.equal(w[n - last:], small[0]) and torch.equal(copy[n - last:], small[0].bfloat16()) and not bool(w[:n - last].any())

@@ -265,3 +265,69 @@ def test_graph_and_stream(mxc):
             torch.cuda.synchronize()
             for t, w in zip((logp, H, dz, tl, ti), want):
                 assert torch.equal(torch.nan_to_num(t.float()), torch.nan_to_num(w.float()))
+
+
+@pytest.mark.parametrize("N,K,pad,dtype", [(2700, 50257, 0, torch.bfloat16), (5000, 30000, 0, torch.bfloat16), (2300, 30001, 2, torch.float32), (5000, 14000, 0, torch.float32),
+                                           (1100, 131072, 0, torch.bfloat16)])
+def test_more_than_the_caches(mxc, N, K, pad, dtype):
+    """More than 256 MB of logits, which pass the caches by; with top tokens and without."""
+    check(mxc, N, K, pad, dtype, 0, 1.0, 20)
+    check(mxc, N, K, pad, dtype, 2, 1.4, 0, seed=2)
+
+
+# rows of 8192, 8193, 16384 and 16385 pieces of 16 bytes; fewer and more than 160 rows; rows that begin at any value
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("pieces", [8192, 8193, 16384, 16385])
+@pytest.mark.parametrize("N", [159, 160])
+def test_borders_of_the_cuts(mxc, dtype, pieces, N):
+    V = 16 // dtype.itemsize
+    check(mxc, N, pieces * V, 0, dtype, 1, 0.8, 7)
+    check(mxc, N, pieces * V - 2 * V + 2, 1, dtype, 0, 1.0, 64, seed=3)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("N,K,pad", [(200, 20000, 3), (300, 20000, 0), (20, 70001, 1)])
+def test_rows_of_one_value(mxc, dtype, N, K, pad):
+    """Rows whose values are all the same, or all but few: the first indices; few chunks, one, many."""
+    top = 64
+    z = torch.full((N, K + pad), float("nan"), device="cuda")
+    z[:, :K] = torch.arange(N, device="cuda")[:, None] % 9 - 4.0
+    z[1::4, K - 3:K] = 9.0
+    z[2::4, :K] = -math.inf
+    z[2::4, K // 2:K // 2 + 2] = 1.0
+    z = z.to(dtype)
+    code = mxc.dtype_code(dtype)
+    ws = mxc.alloc_workspace(mxc.mxc_logprob_workspace_bytes(N, K, code, top))
+    logp, index = torch.empty(N, top, device="cuda"), torch.empty(N, top, dtype=torch.int32, device="cuda")
+    mxc.mxc_logprob_fwd(N, K, K + pad, code, z, None, 1.0, top, None, None, None, logp, index, ws)
+    want = torch.sort(z[:, :K].double(), dim=1, descending=True, stable=True).indices[:, :top]
+    assert torch.equal(index.long(), want)
+    _, _, lp, _, _ = exact(z[:, :K].double(), torch.zeros(N, dtype=torch.int32, device="cuda"), 1.0)
+    lp = lp.gather(1, want)
+    near(logp, lp, torch.where(lp == -math.inf, 0.0, U * (8 * lp.abs() + 1024)))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_past_32_bits(mxc, dtype):
+    """More than 2^32 bytes and 2^31 values of logits: the last rows are the ones that a call of these alone gives."""
+    N, K, ld, top, last = 43000, 50257, 50261, 9, 5
+    z = torch.empty(N, ld, dtype=dtype, device="cuda")
+    z[:N - last] = 0
+    rows, labels, dlogp, dentropy = data(last, K, ld, dtype, 3, 0)
+    z[N - last:] = rows
+    wide = lambda t: torch.cat([torch.zeros(N - last, dtype=t.dtype, device="cuda"), t])  # noqa: E731
+    code = mxc.dtype_code(dtype)
+    got = []
+    for n, x, lab, dl, dh in ((N, z, wide(labels), wide(dlogp), wide(dentropy)), (last, rows, labels, dlogp, dentropy)):
+        logp, H, stats = torch.empty(n, device="cuda"), torch.empty(n, device="cuda"), torch.empty(n, 2, device="cuda")
+        tl, ti = torch.empty(n, top, device="cuda"), torch.empty(n, top, dtype=torch.int32, device="cuda")
+        mxc.mxc_logprob_fwd(n, K, ld, code, x, lab, 1.0, top, logp, H, stats, tl, ti, mxc.alloc_workspace(mxc.mxc_logprob_workspace_bytes(n, K, code, top)))
+        dz = torch.empty(n, ld, dtype=dtype, device="cuda")
+        mxc.mxc_logprob_bwd(n, K, ld, code, x, lab, 1.0, stats, H, dl, dh, dz)
+        mxc.mxc_logprob_fwd_bwd(n, K, ld, code, x, lab, 1.0, dl, dh, None, None, x, mxc.alloc_workspace(mxc.mxc_logprob_workspace_bytes(n, K, code, 0)))
+        got.append([t[-last:] for t in (logp, H, stats, tl, ti, dz[:, :K], x[:, :K])])
+    for a, b in zip(*got):
+        if a.dtype == torch.int32:
+            assert torch.equal(a, b)
+        else:       # two ways of summing: twice the bound of one, of values of at most some tens
+            near(a, b, 2 * U * 1024 * (1 + b.double().abs()) + torch.finfo(a.dtype).eps * b.double().abs())

@@ -226,3 +226,41 @@ def test_graph(mxc):
             graph.replay()
             torch.cuda.synchronize()
             assert torch.equal(y, want)
+
+
+# wide filters' workgroups from 8192 rows; 128 rows of x and more; the sizes of tiles on both sides of 192 of the larger ones
+@pytest.mark.parametrize("N,C,K", [(17, 300, 8192), (100, 1000, 8191), (128, 512, 8192), (128, 640, 9001), (129, 512, 8192), (33, 4097, 8200), (64, 96, 16400),
+                                   (6144, 256, 2048), (6143, 288, 2047), (6144, 256, 1792), (5000, 100, 2500)])
+def test_borders_of_the_paths(mxc, N, C, K):
+    for dtype in DTYPES:
+        check_product(mxc, N, C, K, dtype, True, True)
+
+
+@pytest.mark.parametrize("N,C,K,last", [(1, 65504, 140001, 40), (30, 65504, 140001, 40), (200, 65504, 140001, 40), (50000, 64, 50001, 5)])
+def test_past_32_bits(mxc, N, C, K, last):
+    """A filter of more than 2^32 bytes; more than 2^31 results: the last ones are those of a call of the last filter rows or rows of x."""
+    gen = torch.Generator(device="cuda").manual_seed(N)
+    x = torch.randn(N, C, generator=gen, device="cuda").bfloat16()
+    codes, scales = filter4(K, C, gen, 117, 123)
+    y = torch.empty(N, K, dtype=torch.bfloat16, device="cuda")
+    ws = lambda n, k: mxc.alloc_workspace(mxc.mxc_mxfp4_fc_workspace_bytes(n, C, k, 1))  # noqa: E731
+    mxc.mxc_mxfp4_fc_fwd(N, C, K, 1, x, codes, scales, None, 0, y, ws(N, K))
+    rows = N if N <= 200 else last
+    xc, xs = run_quantize(mxc, x[N - rows:].contiguous())
+    q, w = decode(xc, xs, C).cuda(), decode(codes[K - last:], scales[K - last:], C).cuda()
+    want, D = q @ w.t().contiguous(), q.abs() @ w.t().contiguous().abs()
+    # (sums: a chain of C/64 partial sums at most)
+    assert bool(((y[N - rows:, K - last:].double() - want).abs() <= (C / 64 + 64) * U * D + 2.0 ** -8 * want.abs() + 1e-37).all())
+
+
+def test_quantize_past_32_bits(mxc):
+    """More than 2^31 values, there and back."""
+    N, C, last = 70000, 32800, 3
+    x = torch.zeros(N, C, dtype=torch.bfloat16, device="cuda")
+    x[N - last:] = torch.randn(last, C, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").bfloat16()
+    codes, scales = run_quantize(mxc, x)
+    small = run_quantize(mxc, x[N - last:].contiguous())
+    assert torch.equal(codes[N - last:], small[0]) and torch.equal(scales[N - last:], small[1]) and not bool(codes[:N - last].any())
+    y = torch.empty_like(x)
+    mxc.mxc_mxfp4_dequantize(N, C, 1, codes, scales, y)
+    assert torch.equal(y[N - last:].cpu().double(), decode(*small, C)) and not bool(y[:N - last].any())
