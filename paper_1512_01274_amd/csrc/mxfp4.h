@@ -6,6 +6,7 @@ namespace mxc {
 
 // V values of 16 bytes (or 2 x 16), from memory of the element's own alignment: rows of any length begin anywhere, and the machine
 // reads 16 bytes from there at once
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
 typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 

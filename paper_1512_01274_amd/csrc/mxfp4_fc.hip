@@ -1,8 +1,8 @@
 // FullyConnected on a filter in microscaled 4-bit floating point: y[n][k] = act( sum_c q(x)[n][c]*w[k][c] + bias[k] ).
 // The matrix instructions take 4-bit operands as they are, 32 values of a row and their scale byte in each lane, multiply and add
 // them in fp32.  The product is formed transposed (filter rows first), so that a lane holds four neighbouring columns of y.
-//   token:  N <= 16.  One launch: every wave quantises the part of x that it multiplies.
-//   skinny: x is quantised once, then workgroups of eight waves that share out the columns.
+//   token:  up to 16 rows of x.  One launch: every wave quantises the part of x that it multiplies.
+//   skinny: some rows, or few filter rows: x is quantised once, then workgroups of eight waves that share out the columns.
 //   tiled:  x quantised, both operands' scales brought into the order of the tiles, and tiles of LDS that a ring of loads fills.
 #include <type_traits>
 
@@ -192,12 +192,12 @@ __global__ __launch_bounds__(256) void mxfp4_order_kernel(int N, int C, int grou
 }
 
 // 16*WF filter rows and 16*NF rows of x a workgroup, both straight from the caches into registers; its eight waves take every eighth step of
-// 128 columns, and their sums meet in LDS.  Two steps are under way while one is multiplied.
+// 128 columns, and their sums meet in LDS.  A step is under way while one is multiplied.
 template <typename T, int WF, int NF>
 __global__ __launch_bounds__(512) void mxfp4_skinny_kernel(int N, int K, int blocks, int scale_row, const unsigned char *xc, const unsigned char *xs,
                                                            const unsigned char *wc, const unsigned char *ws, const float *bias, int relu, T *y)
 {
-    constexpr int WAVES = 8, PLACES = 3;
+    constexpr int WAVES = 8;
     __shared__ f32x4 part[WAVES][WF * NF][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int groups = scale_row / 16, tiles = (N + 15) / 16, tile0 = blockIdx.y * NF, all = (blocks + 3) / 4;
@@ -205,7 +205,8 @@ __global__ __launch_bounds__(512) void mxfp4_skinny_kernel(int N, int K, int blo
     FilterRows filter[WF];
 #pragma unroll
     for (int i = 0; i < WF; ++i) filter[i] = FilterRows(wc, ws, k0 + 16 * i, K, blocks, scale_row, lane);
-    // first steps of each tile of x (the last tile again where there are fewer): offsets are less than 4 GB for at most 128 rows
+    // first steps of each tile of x (the last tile again where there are fewer); places are counted in 32 bits: at most 2^14 rows of 2^23 columns
+    // are 2^32 lanes' pieces
     unsigned first[NF];
 #pragma unroll
     for (int i = 0; i < NF; ++i) first[i] = (unsigned)min(tile0 + i, tiles - 1) * (unsigned)groups * 4u;
@@ -214,7 +215,7 @@ __global__ __launch_bounds__(512) void mxfp4_skinny_kernel(int N, int K, int blo
         uint4 w[WF], x[NF];
         unsigned sw[WF];
         int sx[NF];
-    } place[PLACES];
+    } place[2];
     auto load = [&](Step &s, int step) {
 #pragma unroll
         for (int i = 0; i < WF; ++i) {
@@ -238,13 +239,12 @@ __global__ __launch_bounds__(512) void mxfp4_skinny_kernel(int N, int K, int blo
         }
     };
     if (wave < all) load(place[0], wave);
-    if (wave + WAVES < all) load(place[1], wave + WAVES);
-    for (int step = wave; step < all; step += PLACES * WAVES) {
+    for (int step = wave; step < all; step += 2 * WAVES) {
 #pragma unroll
-        for (int u = 0; u < PLACES; ++u) {
+        for (int u = 0; u < 2; ++u) {
             const int now = step + u * WAVES;
             if (now >= all) break;
-            if (now + 2 * WAVES < all) load(place[(u + 2) % PLACES], now + 2 * WAVES);
+            if (now + WAVES < all) load(place[1 - u], now + WAVES);
             multiply(place[u]);
         }
     }
@@ -261,9 +261,14 @@ __global__ __launch_bounds__(512) void mxfp4_skinny_kernel(int N, int K, int blo
         for (int w = 1; w < WAVES; ++w) v += part[w][f][l];
         const long long k = k0 + (f / NF) * 16 + (l >> 4) * 4, n = (tile0 + f % NF) * 16ll + (l & 15);
         if (n >= N) continue;
+        T *to = y + (size_t)n * K + k;
+        if (k + 4 <= K) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (k + e < K) store_one(y + (size_t)n * K + k + e, activated(v[e], bias, k + e, relu));
+            for (int e = 0; e < 4; ++e) v[e] = activated(v[e], bias, k + e, relu);
+            if constexpr (sizeof(T) == 2) *reinterpret_cast<u32x2_any *>(to) = u32x2_any{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+            else *reinterpret_cast<f32x4_any *>(to) = f32x4_any{v[0], v[1], v[2], v[3]};
+        } else
+            for (int e = 0; k + e < K; ++e) store_one(to + e, activated(v[e], bias, k + e, relu));
     }
 }
 
@@ -507,13 +512,16 @@ __global__ __launch_bounds__(64 * GM * GN, 1) void mxfp4_tile_kernel(int N, int 
 
 // ---- host -----------------------------------------------------------------------------------------------------------------
 
-constexpr int WIDE_K = 8192;
 
 enum Path { TOKEN, SKINNY, TILED };
 Path path_of(int N, int C, int K)
 {
+    // One launch where it serves: 4096 x 4096, one row, 4.5 us, the ordering launch alone is 3.  The skinny workgroups read their operands once for 16
+    // or 32 filter rows, the tiles once for 128 or 256, but need one for each compute unit: 512 rows of 9216 by 2048 (64 small tiles)
+    // 18 us skinny and 30 tiled, 256 by 6144 (96) 30 and 32, 512 by 4096 (128) 31 and 31, 80 by 32768 (256) 74 and 51.  Up to 32 rows a tile is mostly
+    // zeros: 32 by 131072, 76 and 92.
     if (N <= 16) return TOKEN;
-    return N <= 128 ? SKINNY : TILED;
+    return N <= 32 || ((N + 127ll) / 128) * ((K + 127ll) / 128) <= 128 ? SKINNY : TILED;
 }
 
 struct Buffers {        // of the workspace
@@ -566,13 +574,20 @@ int fc(int N, int C, int K, const T *x, const unsigned char *wc, const unsigned 
         if (!one_launch((unsigned long long)groups * tiles, 256) || !one_launch((K + 15ll) / 16, 512)) return MXC_ERR_SHAPE;
         hipLaunchKernelGGL(mxfp4_order_kernel<T>, dim3((unsigned)(groups * tiles)), dim3(256), 0, st, N, C, groups, x, (unsigned *)xc, (unsigned *)xs);
         if (hipGetLastError() != hipSuccess) return MXC_ERR_LAUNCH;
-        void (*kernel)(int, int, int, int, const unsigned char *, const unsigned char *, const unsigned char *, const unsigned char *, const float *, int, T *);
-        const bool wide = K >= WIDE_K;
-        if (N <= 32) kernel = wide ? mxfp4_skinny_kernel<T, 2, 2> : mxfp4_skinny_kernel<T, 1, 2>;
-        else if (N <= 64) kernel = wide ? mxfp4_skinny_kernel<T, 2, 4> : mxfp4_skinny_kernel<T, 1, 4>;
-        else kernel = wide ? mxfp4_skinny_kernel<T, 2, 8> : mxfp4_skinny_kernel<T, 1, 8>;
-        const int rows = wide ? 32 : 16;
-        hipLaunchKernelGGL(kernel, dim3((unsigned)((K + rows - 1ll) / rows)), dim3(512), 0, st, N, K, blocks, scale_row, xc, xs, wc, ws, bias, relu, y);
+        // The largest workgroups of which there are enough.  128 rows of 9216, us with workgroups of 32 filter rows by 128 rows of x, 32 by 64, 16 by 64, 16 by 32:
+        // 1000 filter rows 18, 13, 11.1, 10.7; 2048: 18, 13.0, 11.2, 12.1; 4096: 18, 13.3, 15, 16; 6000: 18.4, 21.6, 24.7, 28; 8192: 18.8, 20.9, 27, 35.
+        auto launch = [&](auto wf, auto nf, bool last) {
+            constexpr int WF = decltype(wf)::value, NF = decltype(nf)::value;
+            const long long k_parts = (K + 16 * WF - 1ll) / (16 * WF), n_parts = (tiles + NF - 1) / NF;
+            if (!last && (tiles <= NF / 2 || k_parts * n_parts < 160)) return false;
+            hipLaunchKernelGGL((mxfp4_skinny_kernel<T, WF, NF>), dim3((unsigned)k_parts, (unsigned)n_parts), dim3(512), 0, st, N, K, blocks, scale_row, xc, xs, wc, ws, bias, relu, y);
+            return true;
+        };
+        const std::integral_constant<int, 1> one;
+        const std::integral_constant<int, 2> two;
+        const std::integral_constant<int, 4> four;
+        const std::integral_constant<int, 8> eight;
+        launch(two, eight, false) || launch(two, four, false) || launch(one, four, false) || (tiles <= 2 && launch(two, two, false)) || launch(one, two, true);
         return hipGetLastError() == hipSuccess ? MXC_OK : MXC_ERR_LAUNCH;
     }
     const int groups = (int)(((long long)C + 255) / 256);
@@ -581,6 +596,8 @@ int fc(int N, int C, int K, const T *x, const unsigned char *wc, const unsigned 
     if (!one_launch(x_groups + w_groups, 256)) return MXC_ERR_SHAPE;
     hipLaunchKernelGGL(mxfp4_prepare_kernel<T>, dim3((unsigned)(x_groups + w_groups)), dim3(256), 0, st, N, C, K, blocks, scale_row, groups, (unsigned)x_groups, x, (unsigned *)xc, xt, ws, wt);
     if (hipGetLastError() != hipSuccess) return MXC_ERR_LAUNCH;
+    // Tiles of 256 x 256 need half the reads from LDS that tiles of 128 x 128 do, but have to fill 256 compute units: 2048 rows by 4096 of 4096 (128 large ones)
+    // 34.1 us large and 31.0 small, 3000 x 8192 by 4096 (192) 70.9 and 78.9, 4096 x 4096 by 4096 (256) 46.6 and 54.3.
     const long long big = ((K + 255ll) / 256) * ((N + 255ll) / 256);
     const int rc = big >= 192 ? launch_tiles<T, 4, 2, 2, 4>(N, C, K, xc, xt, wc, wt, bias, relu, y, st) : launch_tiles<T, 2, 2, 2, 2>(N, C, K, xc, xt, wc, wt, bias, relu, y, st);
     if (rc != MXC_OK) return rc;

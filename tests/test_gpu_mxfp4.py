@@ -264,3 +264,11 @@ def test_quantize_past_32_bits(mxc):
     y = torch.empty_like(x)
     mxc.mxc_mxfp4_dequantize(N, C, 1, codes, scales, y)
     assert torch.equal(y[N - last:].cpu().double(), decode(*small, C)) and not bool(y[:N - last].any())
+
+
+# some rows or few filter rows on one side, tiles on the other; each size of workgroup
+@pytest.mark.parametrize("N,C,K", [(300, 640, 4096), (512, 200, 4096), (513, 512, 4096), (1000, 1056, 500), (4000, 130, 65), (9000, 288, 17), (64, 256, 16384), (64, 256, 16400),
+                                   (33, 100, 20000), (32, 700, 40000), (128, 1024, 1000), (128, 1024, 2050), (96, 1024, 4100), (128, 1024, 6001), (40, 2048, 8193), (24, 544, 3001)])
+def test_shapes_of_workgroups(mxc, N, C, K):
+    for dtype in DTYPES:
+        check_product(mxc, N, C, K, dtype, True, True)
