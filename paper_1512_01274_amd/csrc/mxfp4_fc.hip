@@ -74,23 +74,22 @@ struct FilterRows {
 };
 
 // ---- up to 16 rows of x ---------------------------------------------------------------------------------------------------
-// 16 filter rows a workgroup; its eight waves take every eighth group of 512 columns in four steps of 128.  A wave brings its columns of x into
+// 16 filter rows a workgroup; its WAVES waves take every WAVES-th group of 512 columns in four steps of 128.  A wave brings its columns of x into
 // 4 bits by itself, eight values a lane, and passes the codes through LDS to the lanes that multiply them: lane l holds a block of
 // filter row l%16 and one of row l%16 of x.
-constexpr int TOKEN_WAVES = 8;
 
 struct TokenRow {       // of x: the codes and scales of a group, and room that spreads rows over the banks
     unsigned codes[64];
     unsigned char scales[16];
 };
 
-template <typename T>
-__global__ __launch_bounds__(64 * TOKEN_WAVES) void mxfp4_token_kernel(int N, int C, int K, int blocks, int scale_row, const T *x, const unsigned char *wc,
+template <typename T, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void mxfp4_token_kernel(int N, int C, int K, int blocks, int scale_row, const T *x, const unsigned char *wc,
                                                                        const unsigned char *ws, const float *bias, int relu, T *y)
 {
     constexpr int BATCH = 4;        // rows of x whose loads are under way together
-    __shared__ f32x4 part[TOKEN_WAVES][64];
-    __shared__ __align__(16) TokenRow rows[TOKEN_WAVES][16];
+    __shared__ f32x4 part[WAVES][64];
+    __shared__ __align__(16) TokenRow rows[WAVES][16];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, quarter = lane >> 4;
     const long long k0 = (long long)blockIdx.x * 16;
     const FilterRows filter(wc, ws, k0, K, blocks, scale_row, lane);
@@ -106,7 +105,7 @@ __global__ __launch_bounds__(64 * TOKEN_WAVES) void mxfp4_token_kernel(int N, in
         }
     };
     if (wave < groups) ahead(wave);
-    for (int group = wave; group < groups; group += TOKEN_WAVES) {
+    for (int group = wave; group < groups; group += WAVES) {
         uint4 w[4];
         unsigned sw[4];
 #pragma unroll
@@ -114,7 +113,6 @@ __global__ __launch_bounds__(64 * TOKEN_WAVES) void mxfp4_token_kernel(int N, in
             w[j] = next[j];
             sw[j] = next_scale[j];
         }
-        if (group + TOKEN_WAVES < groups) ahead(group + TOKEN_WAVES);
         const int column = group * 512 + lane * 8;
 #pragma unroll 1
         for (int n0 = 0; n0 < N; n0 += BATCH) {
@@ -133,6 +131,7 @@ __global__ __launch_bounds__(64 * TOKEN_WAVES) void mxfp4_token_kernel(int N, in
                 if ((lane & 3) == 0) to.scales[lane >> 2] = (unsigned char)byte;
             }
         }
+        if (group + WAVES < groups) ahead(group + WAVES);       // (after x, whose arrival would be waited for behind it)
         // (a wave's own accesses to LDS keep their order)
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
@@ -161,7 +160,7 @@ __global__ __launch_bounds__(64 * TOKEN_WAVES) void mxfp4_token_kernel(int N, in
     const float *p = reinterpret_cast<const float *>(&part[0][(kk >> 2) * 16 + n]) + (kk & 3);
     float sum = 0.f;
 #pragma unroll
-    for (int w = 0; w < TOKEN_WAVES; ++w) sum += p[w * 256];
+    for (int w = 0; w < WAVES; ++w) sum += p[w * 256];
     store_one(y + (size_t)n * K + k0 + kk, activated(sum, bias, k0 + kk, relu));
 }
 
@@ -513,14 +512,21 @@ __global__ __launch_bounds__(64 * GM * GN, 1) void mxfp4_tile_kernel(int N, int 
 // ---- host -----------------------------------------------------------------------------------------------------------------
 
 
+// Waves of a token workgroup: 16 where there is one for a compute unit at most and each has some columns.  1 row of 16384 by 4096 13.4 -> 11.1 us, 8 of
+// 8192 13.2 -> 9.4; by 16384, where workgroups share a compute unit, 1 row of 9216 22 -> 28.
+int token_waves(int C, int K) { return C > 4096 && K <= 4096 ? 16 : 8; }
+
 enum Path { TOKEN, SKINNY, TILED };
 Path path_of(int N, int C, int K)
 {
-    // One launch where it serves: 4096 x 4096, one row, 4.5 us, the ordering launch alone is 3.  The skinny workgroups read their operands once for 16
-    // or 32 filter rows, the tiles once for 128 or 256, but need one for each compute unit: 512 rows of 9216 by 2048 (64 small tiles)
-    // 18 us skinny and 30 tiled, 256 by 6144 (96) 30 and 32, 512 by 4096 (128) 31 and 31, 80 by 32768 (256) 74 and 51.  Up to 32 rows a tile is mostly
-    // zeros: 32 by 131072, 76 and 92.
-    if (N <= 16) return TOKEN;
+    // One launch where it serves: every workgroup brings x into 4 bits once more, rows of groups of 512 columns, and a compute unit does it for each
+    // of its workgroups.  Token and skinny, us: 1 row of 4096 by 4096 (8 such rows for each compute unit) 7.9 and 11, 16 rows (128) 8.2 and 10.5; 8 of 8192 by 4096 (128)
+    // 9.4 and 11, of 9216 (144) 12.4 and 10.8; 16 of 9216 (288) 17 and 10.7; 8 of 4096 by 8192 (128) 9.1 and 10.8; 1 of 16384 by 16384 (128) 37 and 44, of
+    // 4096 by 32768 (64) 20 and 17.
+    if (N <= 16 && N * ((C + 511ll) / 512) * ((K + 4095ll) / 4096) <= 128) return TOKEN;
+    // The skinny workgroups read their operands once for 16 or 32 filter rows, the tiles once for 128 or 256, but need one for each compute unit: 512
+    // rows of 9216 by 2048 (64 small tiles) 18 us skinny and 30 tiled, 256 by 6144 (96) 30 and 32, 512 by 4096 (128) 31 and 31, 80 by 32768 (256) 74
+    // and 51.  Up to 32 rows a tile is mostly zeros: 32 by 131072, 76 and 92.
     return N <= 32 || ((N + 127ll) / 128) * ((K + 127ll) / 128) <= 128 ? SKINNY : TILED;
 }
 
@@ -563,8 +569,10 @@ int fc(int N, int C, int K, const T *x, const unsigned char *wc, const unsigned 
     const int blocks = (int)(mxfp4_code_row(C) / 16), scale_row = (int)mxfp4_scale_row(C);
     const Path path = path_of(N, C, K);
     if (path == TOKEN) {
-        if (!one_launch((K + 15ll) / 16, 64 * TOKEN_WAVES)) return MXC_ERR_SHAPE;
-        hipLaunchKernelGGL(mxfp4_token_kernel<T>, dim3((unsigned)((K + 15ll) / 16)), dim3(64 * TOKEN_WAVES), 0, st, N, C, K, blocks, scale_row, x, wc, ws, bias, relu, y);
+        const int waves = token_waves(C, K);
+        if (!one_launch((K + 15ll) / 16, 64 * waves)) return MXC_ERR_SHAPE;
+        hipLaunchKernelGGL((waves == 8 ? mxfp4_token_kernel<T, 8> : mxfp4_token_kernel<T, 16>), dim3((unsigned)((K + 15ll) / 16)), dim3(64 * waves), 0, st, N, C, K, blocks, scale_row,
+                           x, wc, ws, bias, relu, y);
         return hipGetLastError() == hipSuccess ? MXC_OK : MXC_ERR_LAUNCH;
     }
     const Buffers b = buffers(N, C, K);

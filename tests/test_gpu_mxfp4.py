@@ -268,7 +268,8 @@ def test_quantize_past_32_bits(mxc):
 
 # some rows or few filter rows on one side, tiles on the other; each size of workgroup
 @pytest.mark.parametrize("N,C,K", [(300, 640, 4096), (512, 200, 4096), (513, 512, 4096), (1000, 1056, 500), (4000, 130, 65), (9000, 288, 17), (64, 256, 16384), (64, 256, 16400),
-                                   (33, 100, 20000), (32, 700, 40000), (128, 1024, 1000), (128, 1024, 2050), (96, 1024, 4100), (128, 1024, 6001), (40, 2048, 8193), (24, 544, 3001)])
+                                   (33, 100, 20000), (32, 700, 40000), (128, 1024, 1000), (128, 1024, 2050), (96, 1024, 4100), (128, 1024, 6001), (40, 2048, 8193), (24, 544, 3001), (16, 4096, 4096), (16, 4097, 300), (8, 8192, 1000), (9, 8200, 100), (1, 25088, 1000), (3, 16384, 50),
+                                   (1, 2048, 70000), (2, 500, 40000), (16, 700, 4097), (17, 8192, 33), (4, 9216, 5000)])
 def test_shapes_of_workgroups(mxc, N, C, K):
     for dtype in DTYPES:
         check_product(mxc, N, C, K, dtype, True, True)
