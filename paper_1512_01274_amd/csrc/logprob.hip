@@ -338,21 +338,18 @@ __device__ __forceinline__ void select_top(TopShared<CAP> &sh, const unsigned *c
     const int wave = threadIdx.x >> 6;
     unsigned bound = wave_bound<S, LOW>(cell, (top + W - 1) / W);
     if (threadIdx.x == 0) sh.count = 0;
-    if constexpr (W > 1) {
+    if ((threadIdx.x & 63) == 0) sh.bound[wave] = bound;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < W; ++w) bound = min(bound, sh.bound[w]);
+    if (bound <= order(-INFINITY)) {        // a wave has less than its share: what one wave holds alone
+        __syncthreads();
+        bound = wave_bound<S, LOW>(cell, top);
         if ((threadIdx.x & 63) == 0) sh.bound[wave] = bound;
         __syncthreads();
 #pragma unroll
-        for (int w = 0; w < W; ++w) bound = min(bound, sh.bound[w]);
-        if (bound <= order(-INFINITY)) {        // a wave has less than its share: what one wave holds alone
-            __syncthreads();
-            bound = wave_bound<S, LOW>(cell, top);
-            if ((threadIdx.x & 63) == 0) sh.bound[wave] = bound;
-            __syncthreads();
-#pragma unroll
-            for (int w = 0; w < W; ++w) bound = max(bound, sh.bound[w]);
-        }
-    } else
-        __syncthreads();
+        for (int w = 0; w < W; ++w) bound = max(bound, sh.bound[w]);
+    }
     // Values above the bound, and equal ones up to index `tie`.  Where there are many equal ones (rows of one value, rows where few tokens are
     // allowed) a second turn takes only the lowest indices of those at the bound: each lane's first one is a cell again.
     unsigned tie = 0xFFFFFFFFu, first = 0xFFFFFFFFu;
@@ -376,13 +373,10 @@ __device__ __forceinline__ void select_top(TopShared<CAP> &sh, const unsigned *c
         tie = ~wave_bound<1, 0>(cells, top);        // (no less than top of them: those above the bound may be none)
         __syncthreads();
         if (threadIdx.x == 0) sh.count = 0;
-        if constexpr (W > 1) {
-            if ((threadIdx.x & 63) == 0) sh.bound[wave] = tie;
-            __syncthreads();
+        if ((threadIdx.x & 63) == 0) sh.bound[wave] = tie;
+        __syncthreads();
 #pragma unroll
-            for (int w = 0; w < W; ++w) tie = min(tie, sh.bound[w]);
-        } else
-            __syncthreads();
+        for (int w = 0; w < W; ++w) tie = min(tie, sh.bound[w]);
     }
     if (n <= CAP) {
         rank_candidates<W>(sh, n, top, emit);
@@ -401,12 +395,10 @@ __device__ __forceinline__ void select_top(TopShared<CAP> &sh, const unsigned *c
             const unsigned long long other = __shfl_xor(best, d);
             best = other > best ? other : best;
         }
-        if constexpr (W > 1) {
-            __syncthreads();
-            if ((threadIdx.x & 63) == 0) sh.list[wave] = best;
-            __syncthreads();
-            for (int w = 0; w < W; ++w) best = sh.list[w] > best ? sh.list[w] : best;
-        }
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) sh.list[wave] = best;
+        __syncthreads();
+        for (int w = 0; w < W; ++w) best = sh.list[w] > best ? sh.list[w] : best;
         last = best;
         if (threadIdx.x == 0) emit(i, best);
     }
@@ -485,6 +477,73 @@ __device__ __forceinline__ void each_value(const Piece<T> (&p)[P], int held, int
     }
 }
 
+// The most probable tokens of a row that one wave holds; cell: the largest value of each of the lane's P pieces, first: the index of value 0 of piece 0.
+// The bound is the largest value that `top` pieces reach; what reaches it is collected and ranked.  Where that is many values (equal ones: rows in which few
+// tokens are allowed), the second way: fewer than `top` pieces have values above the bound, all of which go on the list, and of those at the bound
+// as many of the lowest indices as are missing.  Indices ascend with the piece, the lane and the place, so that their order is a count over ballots.
+template <typename T, int P, int CAP, class Emit>
+__device__ __forceinline__ void wave_top(TopShared<CAP> &sh, const Piece<T> (&p)[P], const unsigned (&cell)[P], int held, int first, int K, int top, Emit emit)
+{
+    constexpr int V = Piece<T>::V, LOW = sizeof(T) == 2 ? 16 : 0, FEW = 160;
+    static_assert(CAP >= (MXC_LOGPROB_MAX_TOP - 1) * V, "room for all values of the pieces above the bound");
+    const unsigned bound = wave_bound<P, LOW>(cell, top);
+    const float limit = bound >> LOW <= order(-INFINITY) >> LOW ? -INFINITY : __uint_as_float(__float_as_uint(unorder(bound)) >> LOW << LOW);
+    // f(index, value, in the row) for the places of piece q
+    auto places = [&](int q, auto f) {
+        int index = first + q * 64 * V;
+        asm volatile("" : "+v"(index));
+#pragma unroll
+        for (int k = 0; k < V; ++k) f(index + k, p[q].again(k), (unsigned)(index + k) < (unsigned)K);
+    };
+    auto put = [&](float v, int index) {
+        const int at = atomicAdd(&sh.count, 1);
+        if (at < CAP) sh.list[at] = key_of(order(v), (unsigned)index);
+    };
+    if (threadIdx.x == 0) sh.count = 0;
+    __syncthreads();
+    if (limit > -INFINITY) {
+#pragma unroll
+        for (int q = 0; q < P; ++q)
+            if (q < held && cell[q] >= bound)
+                places(q, [&](int index, float v, bool in) {
+                    if (v >= limit && in) put(v, index);
+                });
+        __syncthreads();
+        const int n = sh.count;
+        if (n <= FEW) {
+            rank_candidates<1>(sh, n, top, emit);
+            return;
+        }
+        __syncthreads();
+        if (threadIdx.x == 0) sh.count = 0;
+    }
+    int above = 0;
+#pragma unroll
+    for (int q = 0; q < P; ++q)
+        if (q < held && __ballot(cell[q] >> LOW > bound >> LOW)) places(q, [&](int, float v, bool in) { above += __popcll(__ballot(in && v > limit)); });
+    int need = top - above;
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < P; ++q) {
+        if (q >= held || !__ballot(cell[q] >= bound)) continue;
+        int before = 0, all = 0;        // values at the bound in earlier lanes, in all
+        if (need > 0)
+            places(q, [&](int, float v, bool in) {
+                const unsigned long long b = __ballot(in && v == limit);
+                before = __builtin_amdgcn_mbcnt_hi((unsigned)(b >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)b, before));
+                all += __popcll(b);
+            });
+        places(q, [&](int index, float v, bool in) {
+            const bool equal = in && v == limit;
+            if ((in && v > limit) || (equal && before < need)) put(v, index);
+            if (equal) ++before;
+        });
+        need -= all;
+    }
+    __syncthreads();
+    rank_candidates<1>(sh, min(sh.count, CAP), top, emit);
+}
+
 // G threads a row, P pieces a thread; rows of fewer than a wave's lanes share one.  TOP: with the most probable tokens, else
 // the gradient where dz is given.
 template <typename T, int G, int P, bool TOP, bool NT = false>
@@ -530,7 +589,7 @@ __global__ __launch_bounds__(G < 64 ? 256 : G, G == 512 && P == 16 ? 4 : 1) void
     }
     part[0].look(low);
     unsigned cell[S];
-    if constexpr (TOP) {
+    if constexpr (TOP && W > 1) {
 #pragma unroll
         for (int s = 0; s < S; ++s) cell[s] = order(part[s].largest());
     }
@@ -545,6 +604,12 @@ __global__ __launch_bounds__(G < 64 ? 256 : G, G == 512 && P == 16 ? 4 : 1) void
 #pragma unroll
         for (int w = 1; w < W; ++w) e = Extent<T>::join(e, ext[w]);
     }
+    // (where one wave selects, each piece's largest value, before the places outside the row get a number)
+    unsigned most[TOP && W == 1 ? P : 1];
+    if constexpr (TOP && W == 1) {
+#pragma unroll
+        for (int q = 0; q < P; ++q) most[q] = order(p[q].template largest<true>());
+    }
     float m = Extent<T>::most(e);
     if (!Extent<T>::sure(e)) {      // all are negative
         m = LOWEST;
@@ -556,7 +621,7 @@ __global__ __launch_bounds__(G < 64 ? 256 : G, G == 512 && P == 16 ? 4 : 1) void
         }
 #pragma unroll
         for (int s = 0; s < S; ++s) {
-            if constexpr (TOP) cell[s] = order(of[s]);
+            if constexpr (TOP && W > 1) cell[s] = order(of[s]);
             m = fmaxf(m, of[s]);
         }
         m = meet_row(m, 0, larger);
@@ -613,11 +678,8 @@ __global__ __launch_bounds__(G < 64 ? 256 : G, G == 512 && P == 16 ? 4 : 1) void
         }
     }
     if constexpr (TOP) {
-        // (small where a workgroup is a wave: what a compute unit holds of them goes by their LDS)
-        constexpr int CAP = W == 1 ? 256 : 512, HELD = W == 1 ? 32 + 32 * P : 256;
+        constexpr int CAP = 512, HELD = 256, LOW = sizeof(T) == 2 ? 16 : 0;
         __shared__ TopShared<CAP> sh;
-        __shared__ Aside<T, HELD> aside;
-        constexpr int LOW = sizeof(T) == 2 ? 16 : 0;
         auto emit = [&](int i, unsigned long long key) {
             a.top_index[row * a.top + i] = key == NO_KEY ? -1 : (int)key_index(key);
             a.top_logp[row * a.top + i] = key == NO_KEY || empty ? -INFINITY : (sc.any(unorder((unsigned)(key >> 32))) - ls) * LN2;
@@ -626,19 +688,25 @@ __global__ __launch_bounds__(G < 64 ? 256 : G, G == 512 && P == 16 ? 4 : 1) void
             if (lane < a.top) emit(lane, lane < a.K ? key_of(order(-INFINITY), (unsigned)lane) : NO_KEY);
             return;
         }
-        const unsigned mine = wave_bound<S, LOW>(cell, (a.top + W - 1) / W);
-        if ((lane & 63) == 0) aside.said[lane >> 6] = mine;
-        if (lane == 0) aside.count = sh.count = 0;
-        __syncthreads();
-        const unsigned bound = aside.template hear<W>();
-        const float limit = bound >> LOW > order(-INFINITY) >> LOW ? unorder(bound) : LOWEST;
+        if constexpr (W == 1) {
+            wave_top<T, P>(sh, p, most, held, lane * Piece<T>::V - r.head, a.K, a.top, emit);
+            return;
+        } else {
+            __shared__ Aside<T, HELD> aside;
+            const unsigned mine = wave_bound<S, LOW>(cell, (a.top + W - 1) / W);
+            if ((lane & 63) == 0) aside.said[lane >> 6] = mine;
+            if (lane == 0) aside.count = sh.count = 0;
+            __syncthreads();
+            const unsigned bound = aside.template hear<W>();
+            const float limit = bound >> LOW > order(-INFINITY) >> LOW ? unorder(bound) : LOWEST;
 #pragma unroll
-        for (int q = 0; q < P; ++q)
-            if (q < held && p[q].template largest<true>() >= limit) aside.put(p[q], q * G + lane);
-        __syncthreads();
-        if (aside.template rank<W, LOW>(sh, bound, r.head, a.K, a.top, a.K, emit)) return;
-        __syncthreads();
-        select_top<W, S, LOW>(sh, cell, a.top, [&](unsigned from, auto f) { each_value<T, P>(p, held, lane * Piece<T>::V - r.head, G * Piece<T>::V, a.K, from, f); }, emit);
+            for (int q = 0; q < P; ++q)
+                if (q < held && p[q].template largest<true>() >= limit) aside.put(p[q], q * G + lane);
+            __syncthreads();
+            if (aside.template rank<W, LOW>(sh, bound, r.head, a.K, a.top, a.K, emit)) return;
+            __syncthreads();
+            select_top<W, S, LOW>(sh, cell, a.top, [&](unsigned from, auto f) { each_value<T, P>(p, held, lane * Piece<T>::V - r.head, G * Piece<T>::V, a.K, from, f); }, emit);
+        }
     } else if (a.dz) {
         const float dl = a.dlogp && given ? a.dlogp[row] : 0.f, dh = a.dentropy ? a.dentropy[row] : 0.f;
         const float per = empty ? 0.f : a.scale / s, A = empty ? 0.f : per * (dh * (mean * LN2) - dl), B = -per * dh * LN2;

@@ -331,3 +331,32 @@ def test_past_32_bits(mxc, dtype):
             assert torch.equal(a, b)
         else:       # two ways of summing: twice the bound of one, of values of at most some tens
             near(a, b, 2 * U * 1024 * (1 + b.double().abs()) + torch.finfo(a.dtype).eps * b.double().abs())
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("K", [3, 70, 250, 511, 700, 1000, 2040])
+def test_few_allowed(mxc, dtype, K):
+    """Rows in which a few tokens are allowed and the others share one value, the type's lowest or another; crowded and scattered; top of 1 to 64."""
+    N = 60
+    g = torch.Generator(device="cuda").manual_seed(K)
+    z = torch.full((N, K), float(torch.finfo(dtype).min), device="cuda")
+    z[1::4] = -2.0
+    z[2::4] = 1.5
+    for n in range(N):
+        many = n * K // N
+        at = torch.randperm(K, generator=g, device="cuda")[:many] if n % 3 else torch.arange(K - many, K, device="cuda")
+        z[n, at] = (torch.randint(-3, 3, (many,), generator=g, device="cuda") if n % 5 else torch.randn(many, generator=g, device="cuda")).float() - (4.0 if n % 7 == 0 else 0.0)
+    z = z.to(dtype)
+    code = mxc.dtype_code(dtype)
+    order = torch.sort(z.double(), dim=1, descending=True, stable=True).indices
+    _, _, lp, _, _ = exact(z.double(), torch.zeros(N, dtype=torch.int32, device="cuda"), 1.0)
+    for top in (1, 7, 20, 64):
+        ws = mxc.alloc_workspace(mxc.mxc_logprob_workspace_bytes(N, K, code, top))
+        logp, index = torch.empty(N, top, device="cuda"), torch.empty(N, top, dtype=torch.int32, device="cuda")
+        mxc.mxc_logprob_fwd(N, K, K, code, z, None, 1.0, top, None, None, None, logp, index, ws)
+        n = min(top, K)
+        assert torch.equal(index[:, :n].long(), order[:, :n]) and bool((index[:, n:] == -1).all())
+        want = lp.gather(1, order[:, :n])
+        over = want < -3.0e38
+        assert bool((logp[:, :n][over] < -3.0e38).all())
+        near(torch.where(over, 0.0, logp[:, :n].double()), torch.where(over, 0.0, want), torch.where(over, 0.0, U * (8 * want.abs() + 1024)))
