@@ -275,10 +275,11 @@ struct Row {
 // reference point of d2 a little (by less than 2^-8) and cancels in every result.  Far from zero, where it would move it by more, and where the products
 // overflow: the difference first.
 struct Scale {
-    float k2, m, c;
+    float k, k2, m, c;
     bool near;
     __device__ __forceinline__ Scale(float scale, float most)
     {
+        k = scale;
         k2 = scale * LOG2E;
         m = most;
         c = -(most * k2);
@@ -287,6 +288,9 @@ struct Scale {
     template <bool NEAR>
     __device__ __forceinline__ float d2(float z) const { return NEAR ? fmaf(z, k2, c) : (z - m) * k2; }
     __device__ __forceinline__ float any(float z) const { return near ? d2<true>(z) : d2<false>(z); }
+    // the log probability of a logit whose d2 this is.  Very far from the maximum (a masked token) the product in powers of two may overflow where
+    // the result does not, and ls is nothing (or NaN).
+    __device__ __forceinline__ float log_prob(float d2, float z, float ls) const { return d2 > -0x1p100f ? (d2 - ls) * LN2 : (0.5f * z - 0.5f * m) * k * 2.f - ls; }
 };
 
 template <bool CLAMP>
@@ -488,8 +492,9 @@ __device__ __forceinline__ void wave_top(TopShared<CAP> &sh, const Piece<T> (&p)
 {
     constexpr int V = Piece<T>::V, LOW = sizeof(T) == 2 ? 16 : 0, FEW = 160;
     static_assert(CAP >= (MXC_LOGPROB_MAX_TOP - 1) * V, "room for all values of the pieces above the bound");
-    const unsigned bound = wave_bound<P, LOW>(cell, top);
-    const float limit = bound >> LOW <= order(-INFINITY) >> LOW ? -INFINITY : __uint_as_float(__float_as_uint(unorder(bound)) >> LOW << LOW);
+    auto value_of = [](unsigned o) { return o >> LOW <= order(-INFINITY) >> LOW ? -INFINITY : __uint_as_float(__float_as_uint(unorder(o)) >> LOW << LOW); };
+    unsigned bound = wave_bound<P, LOW>(cell, top);
+    float limit = value_of(bound);
     // f(index, value, in the row) for the places of piece q
     auto places = [&](int q, auto f) {
         int index = first + q * 64 * V;
@@ -518,6 +523,19 @@ __device__ __forceinline__ void wave_top(TopShared<CAP> &sh, const Piece<T> (&p)
         }
         __syncthreads();
         if (threadIdx.x == 0) sh.count = 0;
+    } else if (K > 128) {       // fewer pieces than `top` have a value: the bound that as many values reach (of fewer values all are ranked)
+        bound = 0;
+#pragma unroll 1
+        for (int b = 31; b >= LOW; --b) {
+            const unsigned trial = bound | (1u << b);
+            const float t = unorder(trial);     // (NaN below minus infinity)
+            int c = 0;
+#pragma unroll
+            for (int q = 0; q < P; ++q)
+                if (q < held) places(q, [&](int, float v, bool in) { c += __popcll(__ballot(in && v >= t)); });
+            if (c >= top) bound = trial;
+        }
+        limit = value_of(bound);
     }
     int above = 0;
 #pragma unroll
@@ -672,7 +690,7 @@ __global__ __launch_bounds__(G < 64 ? 256 : G, G == 512 && P == 16 ? 4 : 1) void
     const bool empty = s == 0.f;
     const float ls = empty ? 0.f : log2f(s), mean = t / s;
     if (lane == 0) {
-        if (a.logp) a.logp[row] = !given ? 0.f : empty ? -INFINITY : (sc.any(zl) - ls) * LN2;
+        if (a.logp) a.logp[row] = !given ? 0.f : empty ? -INFINITY : sc.log_prob(sc.any(zl), zl, ls);
         if (a.entropy) a.entropy[row] = empty ? 0.f : (ls - mean) * LN2;
         if (a.stats) {
             a.stats[2 * row] = empty ? -INFINITY : m;
@@ -684,7 +702,10 @@ __global__ __launch_bounds__(G < 64 ? 256 : G, G == 512 && P == 16 ? 4 : 1) void
         __shared__ TopShared<CAP> sh;
         auto emit = [&](int i, unsigned long long key) {
             a.top_index[row * a.top + i] = key == NO_KEY ? -1 : (int)key_index(key);
-            a.top_logp[row * a.top + i] = key == NO_KEY || empty ? -INFINITY : (sc.any(unorder((unsigned)(key >> 32))) - ls) * LN2;
+            a.top_logp[row * a.top + i] = -INFINITY;
+            if (key == NO_KEY || empty) return;
+            const float z = unorder((unsigned)(key >> 32));
+            a.top_logp[row * a.top + i] = sc.log_prob(sc.any(z), z, ls);
         };
         if (empty) {        // minus infinities alone
             if (lane < a.top) emit(lane, lane < a.K ? key_of(order(-INFINITY), (unsigned)lane) : NO_KEY);
@@ -755,7 +776,7 @@ __device__ __forceinline__ void write_row_results(const LogprobArgs &a, size_t r
     const bool given = (unsigned)label < (unsigned)a.K, empty = j.s == 0.f;
     const float ls = empty ? 0.f : log2f(j.s);
     const Scale sc(a.scale, j.m);
-    if (a.logp) a.logp[row] = !given ? 0.f : empty ? -INFINITY : (sc.d2<false>(zl) - ls) * LN2;
+    if (a.logp) a.logp[row] = !given ? 0.f : empty ? -INFINITY : sc.log_prob(sc.d2<false>(zl), zl, ls);
     if (a.entropy) a.entropy[row] = empty ? 0.f : (ls - j.t / j.s) * LN2;
     if (a.stats) {
         a.stats[2 * row] = empty ? -INFINITY : j.m;
@@ -766,7 +787,9 @@ __device__ __forceinline__ void write_top(const LogprobArgs &a, size_t row, cons
 {
     const bool none = key == NO_KEY;
     a.top_index[row * a.top + i] = none ? -1 : (int)key_index(key);
-    a.top_logp[row * a.top + i] = none || j.s == 0.f ? -INFINITY : (Scale(a.scale, j.m).d2<false>(unorder((unsigned)(key >> 32))) - log2f(j.s)) * LN2;
+    const Scale sc(a.scale, j.m);
+    const float z = unorder((unsigned)(key >> 32));
+    a.top_logp[row * a.top + i] = none || j.s == 0.f ? -INFINITY : sc.log_prob(sc.d2<false>(z), z, log2f(j.s));
 }
 
 // ---- rows that stream by --------------------------------------------------------------------------------------------------
@@ -1182,9 +1205,9 @@ struct Cut {
 };
 Cut cut_rows(int N, int pieces, bool gradient)
 {
-    // A gradient's rows are held, but for the longest ones where there are few: 131072 of bf16 took 20.4 us held and 13.9 in chunks at 64 rows, 23.3
-    // and 21.2 at 128, 29.4 and 31.5 at 192; 50304 of them 10.5 and 10.9 at 64.
-    if (pieces <= SHORT_PIECES || (gradient && (pieces <= ROW_PIECES / 2 || (pieces <= ROW_PIECES && N >= 160)))) return Cut{0, 0};
+    // A gradient's rows are held, but for long ones where there are few: 131072 of bf16 took 20.4 us held and 13.9 in chunks at 64 rows, 23.3 and 21.2 at 128,
+    // 29.4 and 31.5 at 192; 58262 of them 11.5 and 6.9 at 2, 12.7 and 12.6 at 64; 30000 7.4 and 6.2 at 2, 8.0 and 8.2 at 64.
+    if (pieces <= SHORT_PIECES || (gradient && (pieces <= 2 * SHORT_PIECES || (pieces <= ROW_PIECES / 2 && N >= 64) || (pieces <= ROW_PIECES && N >= 160)))) return Cut{0, 0};
     int chunks = N >= 256 ? 1 : (1024 + N - 1) / N;
     chunks = chunks < (pieces + CHUNK_THREADS - 1) / CHUNK_THREADS ? chunks : (pieces + CHUNK_THREADS - 1) / CHUNK_THREADS;
     Cut c;

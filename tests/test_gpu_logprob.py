@@ -360,3 +360,43 @@ def test_few_allowed(mxc, dtype, K):
         over = want < -3.0e38
         assert bool((logp[:, :n][over] < -3.0e38).all())
         near(torch.where(over, 0.0, logp[:, :n].double()), torch.where(over, 0.0, want), torch.where(over, 0.0, U * (8 * want.abs() + 1024)))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("K", [129, 204, 378, 511, 900])
+def test_fewer_pieces_than_top(mxc, dtype, K):
+    """More best tokens than the row has 16-byte pieces, or pieces with a value."""
+    check(mxc, 9, K, 1, dtype, 0, 1.0, 64, seed=7)
+    check(mxc, 9, K, 0, dtype, 1, 1.0, 64, seed=8)
+    check(mxc, 9, K, 5, dtype, 2, 0.6, 63, seed=9)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("N,pieces", [(1, 2048), (1, 2049), (63, 2049), (64, 2049), (63, 8192), (64, 8192), (64, 8193), (2, 7283)])
+def test_gradient_of_few_long_rows(mxc, dtype, N, pieces):
+    V = 16 // dtype.itemsize
+    check(mxc, N, pieces * V, 0, dtype, 2, 0.8, 3)
+    check(mxc, N, (pieces - 2) * V + 2, 1, dtype, 1, 1.0, 0, seed=3)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("N,K", [(5, 6), (5, 300), (5, 3000), (1, 70000), (300, 20000)])
+def test_far_masked_tokens(mxc, dtype, N, K):
+    """The log probability of a masked token is scale times its logit as long as 32 bits hold that: scales around log 2, masks of the lowest value."""
+    for scale in (0.25, 0.7, 0.75, 0.95, 1.0):
+        z = torch.randn(N, K, generator=torch.Generator(device="cuda").manual_seed(K), device="cuda") + 3
+        z[:, K // 2:] = float(torch.finfo(dtype).min) * 0.875
+        z[0, 0] = 1e30
+        z = z.to(dtype)
+        labels = torch.full((N,), K - 1, dtype=torch.int32, device="cuda")
+        top = min(64, K)
+        code, s = mxc.dtype_code(dtype), float(np.float32(scale))
+        want, _, lp, _, _ = exact(z.double(), labels, s)
+        logp, tl, ti = torch.empty(N, device="cuda"), torch.empty(N, top, device="cuda"), torch.empty(N, top, dtype=torch.int32, device="cuda")
+        mxc.mxc_logprob_fwd(N, K, K, code, z, labels, s, top, logp, None, None, tl, ti, mxc.alloc_workspace(mxc.mxc_logprob_workspace_bytes(N, K, code, top)))
+        near(logp, want, U * (8 * want.abs() + 1024))
+        lp = lp.gather(1, ti.long())
+        near(tl, lp, U * (8 * lp.abs() + 1024))
+        z[0, 1] = math.nan
+        mxc.mxc_logprob_fwd(N, K, K, code, z, labels, s, 0, logp, None, None, None, None, mxc.alloc_workspace(mxc.mxc_logprob_workspace_bytes(N, K, code, top)))
+        assert bool(logp[0].isnan()) and bool(logp[1:].isfinite().all())
