@@ -1,7 +1,7 @@
 // FullyConnected on a filter in microscaled 4-bit floating point: y[n][k] = act( sum_c q(x)[n][c]*w[k][c] + bias[k] ).
 // The matrix instructions take 4-bit operands as they are, 32 values of a row and their scale byte in each lane, multiply and add
 // them in fp32.  The product is formed transposed (filter rows first), so that a lane holds four neighbouring columns of y.
-//   token:  up to 16 rows of x.  One launch: every wave quantises the part of x that it multiplies.
+//   token:  up to 8 rows of x.  One launch: every wave quantises the part of x that it multiplies.
 //   skinny: some rows, or few filter rows: x is quantised once, then workgroups of eight waves that share out the columns.
 //   tiled:  x quantised, both operands' scales brought into the order of the tiles, and tiles of LDS that a ring of loads fills.
 #include <type_traits>
@@ -73,11 +73,13 @@ struct FilterRows {
     __device__ __forceinline__ unsigned load_scale(int step) const { return scales[step * 4 + part]; }
 };
 
-// ---- up to 16 rows of x ---------------------------------------------------------------------------------------------------
+// ---- up to 8 rows of x ----------------------------------------------------------------------------------------------------
 // 16 filter rows a workgroup; its WAVES waves take every WAVES-th group of 512 columns in four steps of 128.  A wave brings its columns of x into
 // 4 bits by itself, eight values a lane, and passes the codes through LDS to the lanes that multiply them: lane l holds a block of
 // filter row l%16 and one of row l%16 of x.  1 row of 4096 by 4096 4.2 us, of which most is a launch and one chain of load, quantise, multiply, join;
-// of 16384 by 16384 37 us, 3.9 TB/s.
+// of 16384 by 16384 30 us, 4.7 TB/s.
+
+constexpr int TOKEN_ROWS = 8;
 
 struct TokenRow {       // of x: the codes and scales of a group, and room that spreads rows over the banks
     unsigned codes[64];
@@ -90,7 +92,7 @@ __global__ __launch_bounds__(64 * WAVES) void mxfp4_token_kernel(int N, int C, i
 {
     constexpr int BATCH = 4;        // rows of x whose loads are under way together
     __shared__ f32x4 part[WAVES][64];
-    __shared__ __align__(16) TokenRow rows[WAVES][16];
+    __shared__ __align__(16) TokenRow rows[WAVES][TOKEN_ROWS];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, quarter = lane >> 4;
     const long long k0 = (long long)blockIdx.x * 16;
     const FilterRows filter(wc, ws, k0, K, blocks, scale_row, lane);
@@ -120,8 +122,8 @@ __global__ __launch_bounds__(64 * WAVES) void mxfp4_token_kernel(int N, int C, i
             float v[BATCH][8];
 #pragma unroll
             for (int i = 0; i < BATCH; ++i) {
-                const int n = n0 + i;
-                load8_edge(x + (n < N ? (size_t)n * C + column : 0), n < N ? C - column : 0, v[i]);
+                if (n0 + i >= N) break;
+                load8_edge(x + (size_t)(n0 + i) * C + column, C - column, v[i]);
             }
 #pragma unroll
             for (int i = 0; i < BATCH; ++i) {
@@ -136,7 +138,7 @@ __global__ __launch_bounds__(64 * WAVES) void mxfp4_token_kernel(int N, int C, i
         // (a wave's own accesses to LDS keep their order)
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
-        const TokenRow &from = rows[wave][r];
+        const TokenRow &from = rows[wave][r % TOKEN_ROWS];
         const bool live = r < N;
         const uint4 scales = *reinterpret_cast<const uint4 *>(from.scales);
 #pragma unroll
@@ -523,11 +525,11 @@ int token_waves(int C, int K) { return C > 4096 && K <= 4096 ? 16 : 8; }
 enum Path { TOKEN, SKINNY, TILED };
 Path path_of(int N, int C, int K)
 {
-    // One launch where it serves: every workgroup brings x into 4 bits once more, rows of groups of 512 columns, and a compute unit does it for each
-    // of its workgroups.  Token and skinny, us: 1 row of 4096 by 4096 (8 such rows for each compute unit) 7.9 and 11, 16 rows (128) 8.2 and 10.5; 8 of 8192 by 4096 (128)
-    // 9.4 and 11, of 9216 (144) 12.4 and 10.8; 16 of 9216 (288) 17 and 10.7; 8 of 4096 by 8192 (128) 9.1 and 10.8; 1 of 16384 by 16384 (128) 37 and 44, of
-    // 4096 by 32768 (64) 20 and 17.
-    if (N <= 16 && N * ((C + 511ll) / 512) * ((K + 4095ll) / 4096) <= 128) return TOKEN;
+    // One launch where it serves: every workgroup brings x into 4 bits once more, which costs for each row and round of workgroups, against one launch more and
+    // x read from the caches.  Token and skinny, us: 4096 by 4096, 1 row 4.6 and 7.7, 8 rows 6.5 and 7.4, 12 rows 7.7 and 7.4; 9216 by 4096, 4 rows 9.9 and 10.6,
+    // 8 rows 12.8 and 10.7; 4096 by 16384, 2 rows 12.4 and 13.0, 4 rows 14.0 and 12.5; 512 by 65536, 1 row 20.7 and 12.3.  Long rows
+    // read the filter at memory's rate: 16384 by 65536, 1 row 114 and 160, 3 rows 134 and 161; 16384 by 16384, 2 rows 34 and 40, 4 rows 41 and 40.
+    if (N * ((K + 4095ll) / 4096) <= TOKEN_ROWS || (N <= 3 && C > 12288)) return TOKEN;
     // The skinny workgroups read their operands once for 16 or 32 filter rows, the tiles once for 128 or 256, but need one for each compute unit: 512
     // rows of 9216 by 2048 (64 small tiles) 18 us skinny and 30 tiled, 256 by 6144 (96) 30 and 32, 512 by 4096 (128) 31 and 31, 80 by 32768 (256) 74
     // and 51.  Up to 32 rows a tile is mostly zeros: 32 by 131072, 76 and 92.

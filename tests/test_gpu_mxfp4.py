@@ -273,3 +273,11 @@ def test_quantize_past_32_bits(mxc):
 def test_shapes_of_workgroups(mxc, N, C, K):
     for dtype in DTYPES:
         check_product(mxc, N, C, K, dtype, True, True)
+
+
+# the single launch and two on both sides of each of its limits
+@pytest.mark.parametrize("N,C,K", [(8, 640, 4096), (9, 640, 4096), (8, 640, 4097), (4, 640, 8192), (5, 640, 8192), (4, 640, 8193), (1, 100, 32768), (1, 100, 32769), (2, 100, 20000),
+                                   (3, 12320, 33000), (3, 12288, 33000), (4, 12320, 33000), (2, 12289, 40001), (8, 12320, 1000)])
+def test_borders_of_the_single_launch(mxc, N, C, K):
+    for dtype in DTYPES:
+        check_product(mxc, N, C, K, dtype, True, True)
