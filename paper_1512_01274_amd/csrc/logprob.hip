@@ -8,7 +8,7 @@
 // unit's registers), meet for the maximum and for the sums, and write the gradient from what they hold.  Without a gradient, rows of more than
 // 1024 pieces stream by.  Few rows, and rows that are longer than registers, are cut into chunks, each with its own maximum and sums, which a second
 // launch joins (and reads again for the gradient).  Memory bounds it: 4096 rows of 131072 bf16 with the gradient 434 us, 4.95 TB/s; 4096 of
-// 50257 with the 8 best tokens 87 us, 4.7 TB/s; one row of 131072 with the 20 best is latency, 11.3 us in two launches.
+// 50257 with the 8 best tokens 85 us, 4.8 TB/s; one row of 131072 with the 20 best is latency, 11.3 us in two launches.
 #include <type_traits>
 
 #include "mxc_internal.h"

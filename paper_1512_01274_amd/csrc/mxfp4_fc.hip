@@ -517,7 +517,6 @@ __global__ __launch_bounds__(64 * GM * GN, 1) void mxfp4_tile_kernel(int N, int 
 
 // ---- host -----------------------------------------------------------------------------------------------------------------
 
-
 // Waves of a token workgroup: 16 where there is one for a compute unit at most and each has some columns.  1 row of 16384 by 4096 13.4 -> 11.1 us, 8 of
 // 8192 13.2 -> 9.4; by 16384, where workgroups share a compute unit, 1 row of 9216 22 -> 28.
 int token_waves(int C, int K) { return C > 4096 && K <= 4096 ? 16 : 8; }
