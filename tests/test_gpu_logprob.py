@@ -400,3 +400,51 @@ def test_far_masked_tokens(mxc, dtype, N, K):
         z[0, 1] = math.nan
         mxc.mxc_logprob_fwd(N, K, K, code, z, labels, s, 0, logp, None, None, None, None, mxc.alloc_workspace(mxc.mxc_logprob_workspace_bytes(N, K, code, top)))
         assert bool(logp[0].isnan()) and bool(logp[1:].isfinite().all())
+
+
+def gradient_tol(z, labels, scale, dlogp, dentropy, dtype):
+    """The definition's logp, H, dz, and how far a gradient may be off: its own rounding and the errors of its parts (as in check);
+    exponentials below 2^-126 of the largest are nothing."""
+    logp, H, lp, p, d, dz = exact(z.double(), labels, scale, dlogp, dentropy)
+    grow = 8 * d.clamp(min=-200).abs() + 1024
+    TS = (p * d.clamp(min=-1e30)).sum(1, keepdim=True).abs()
+    onehot = torch.zeros_like(p).scatter_(1, labels.clamp(0, z.shape[1] - 1).long()[:, None], 1.0)
+    part = U * p * grow + torch.where(p > 0, 2.0 ** -126, 0.0)
+    tol = scale * (dlogp.double()[:, None].abs() * (2 * U * onehot + part) + dentropy.double()[:, None].abs() * part * (d.clamp(min=-200).abs() + TS + 1))
+    return logp, H, dz, tol + dz.abs() * torch.finfo(dtype).eps / 2 + 1e-37
+
+
+# rows of eight lanes, of a wave with one and four pieces a lane, of 256, 512 and 1024 threads, in chunks
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("N,bytes_", [(40, 80), (40, 600), (40, 3000), (40, 7000), (40, 14000), (40, 30000), (200, 60000), (200, 120000), (200, 250000), (3, 120000), (40, 300000)])
+def test_gradient_of_masked_tokens(mxc, dtype, N, bytes_):
+    """Tokens masked by numbers whose product with a strong weight of the entropy leaves 32 bits: they have no gradient, the others theirs."""
+    K = bytes_ // dtype.itemsize - 3
+    gen = torch.Generator(device="cuda").manual_seed(K)
+    code, lowest = mxc.dtype_code(dtype), float(torch.finfo(dtype).min)
+    ws = mxc.alloc_workspace(mxc.mxc_logprob_workspace_bytes(N, K, code, 0))
+    for scale, mask, weight in ((0.5, lowest, 8.0), (0.6, lowest, -3.0), (0.25, lowest, 1e5), (1.0, -2e38, 3.0), (10.0, -2e37, 0.5), (1.0, lowest, -1e5), (1.0, -math.inf, 1e36),
+                                (0.5, lowest, -1e36), (0.5, -1e4, 1e36)):
+        z = torch.rand(N, K, generator=gen, device="cuda") * 6 - 3
+        z[:, ::2] = mask
+        z[:, 2] = 9.0           # most of the probability, or (rows below) one allowed token alone
+        z[1, 3:] = mask
+        z[2, :] = mask
+        z[2, K - 1] = -1.5
+        z = z.to(dtype)
+        labels = torch.randint(0, K, (N,), generator=gen, device="cuda", dtype=torch.int32)
+        labels[0] = 2
+        s = float(np.float32(scale))
+        dlogp = torch.randn(N, generator=gen, device="cuda")
+        dentropy = (torch.rand(N, generator=gen, device="cuda") + 0.5) * weight
+        logp, H, dz, tol = gradient_tol(z, labels, s, dlogp, dentropy, dtype)
+        l, h, out = torch.empty(N, device="cuda"), torch.empty(N, device="cuda"), torch.empty_like(z)
+        mxc.mxc_logprob_fwd_bwd(N, K, K, code, z, labels, s, dlogp, dentropy, l, h, out, ws)
+        tl, th = row_tol(logp, H)
+        near(l, logp, tl)
+        near(h, H, th)
+        near(out, dz, tol)
+        stats = torch.empty(N, 2, device="cuda")
+        mxc.mxc_logprob_fwd(N, K, K, code, z, None, s, 0, None, h, stats, None, None, ws)
+        mxc.mxc_logprob_bwd(N, K, K, code, z, labels, s, stats, h, dlogp, dentropy, out)
+        near(out, dz, tol)
