@@ -661,8 +661,8 @@ __global__ __launch_bounds__(G < 64 ? 256 : G, G == 512 && P == 16 ? 4 : 1) void
     }
     const Scale sc(a.scale, m);
     // Some d2 may be minus infinity (a NaN comes here too).  Where none is, the places outside the row get a number that has no weight
-    // either, and no product needs care.
-    const bool masked = !(Extent<T>::lowest(e) * sc.k2 > -3.0e38f);
+    // either, and no product needs care.  (Under a scale so small that there is no such number they stay minus infinities.)
+    const bool masked = !(Extent<T>::lowest(e) * sc.k2 > -3.0e38f) || sc.k2 < 0x1p-100f;
     const float fill = sc.near && !masked ? -0x1p20f / sc.k2 : -INFINITY;
 #pragma unroll
     for (int q = 0; q < P; ++q)

@@ -448,3 +448,12 @@ def test_gradient_of_masked_tokens(mxc, dtype, N, bytes_):
         mxc.mxc_logprob_fwd(N, K, K, code, z, None, s, 0, None, h, stats, None, None, ws)
         mxc.mxc_logprob_bwd(N, K, K, code, z, labels, s, stats, h, dlogp, dentropy, out)
         near(out, dz, tol)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("N,K,pad", [(5, 13, 0), (5, 300, 5), (6, 5001, 3), (200, 9001, 0), (2, 70001, 1)])
+def test_scales_at_the_ends(mxc, dtype, N, K, pad):
+    """Temperatures near the ends of what 32 bits hold, with broken 16-byte pieces."""
+    for scale in (1e-30, 1.7e-33, 1e-36, 1e-38, 1e-42, 1e37):
+        for masked in (0, 1, 2):
+            check(mxc, N, K, pad, dtype, masked, scale, 7, seed=masked)
