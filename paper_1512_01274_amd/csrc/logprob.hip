@@ -764,12 +764,15 @@ __global__ __launch_bounds__(G < 64 ? 256 : G, G == 512 && P == 16 ? 4 : 1) void
             for (int q = 0; q < P; ++q)
                 if (q < held) gradient(q * G + again, how, [&](int k) { return sc.d2<true>(p[q].again(k)); });
         };
-        if (!sc.near || !moderate(A, B)) {
+        auto reread = [&](auto near) {      // rare: the pieces once more from memory, as for the sums
             for (int piece = lane; piece < r.pieces; piece += G) {
                 const Piece<T> c = r.load(piece, low);
-                gradient(piece, std::integral_constant<int, ANY>(), [&](int k) { return empty ? -INFINITY : sc.any(c.at(k)); });
+                gradient(piece, std::integral_constant<int, ANY>(), [&](int k) { return sc.d2<decltype(near)::value>(empty ? -INFINITY : c.at(k)); });
             }
-        } else if (masked || fabsf(B) > 1.f) all(std::integral_constant<int, CLAMPED>());
+        };
+        if (!sc.near) reread(std::false_type());
+        else if (!moderate(A, B)) reread(std::true_type());
+        else if (masked || fabsf(B) > 1.f) all(std::integral_constant<int, CLAMPED>());
         else all(std::integral_constant<int, PLAIN>());
     }
 }
