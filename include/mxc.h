@@ -325,7 +325,7 @@ int mxc_sgd_update(size_t n, float *w, const float *g, float *v, void *w_bf16,
  *   mxc_logprob_bwd      the gradient from stats and entropy of mxc_logprob_fwd; dlogp or dentropy may be NULL (zeros);
  *                        labels may be NULL without dlogp, entropy without dentropy
  *   mxc_logprob_fwd_bwd  both at once, which reads z once: logp or entropy may be NULL
- * dz may be z itself.  scale must be positive and finite.  Workspace: mxc_logprob_workspace_bytes (top 0 for
+ * dz may be z itself.  scale must be positive, and finite times log2(e) (2.358e38 at most).  Workspace: mxc_logprob_workspace_bytes (top 0 for
  * mxc_logprob_fwd_bwd, none for mxc_logprob_bwd).  Results are bit-identical from run to run.  Errors: MXC_ERR_SHAPE (non-positive N
  * or K, K above MXC_LOGPROB_MAX_K, ld < K, top out of range, more rows than one launch holds), MXC_ERR_UNSUPPORTED (dtype, scale), MXC_ERR_NULL, MXC_ERR_ALIGN (16 bytes for z and dz,
  * 4 for the others), MXC_ERR_WORKSPACE, MXC_ERR_LAUNCH.

@@ -1030,7 +1030,7 @@ static int logprob_check(int N, int K, int ld, int dtype, const void *z, float s
 {
     if (N <= 0 || K <= 0 || K > MXC_LOGPROB_MAX_K || ld < K) return MXC_ERR_SHAPE;
     if (dtype != MXC_F32 && dtype != MXC_BF16) return MXC_ERR_UNSUPPORTED;
-    if (!(scale > 0.f) || !std::isfinite(scale)) return MXC_ERR_UNSUPPORTED;
+    if (!(scale > 0.f) || !std::isfinite(scale * 1.442695041f)) return MXC_ERR_UNSUPPORTED;      // (the kernels take exponentials in powers of two)
     return z ? MXC_OK : MXC_ERR_NULL;
 }
 

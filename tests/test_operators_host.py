@@ -158,3 +158,13 @@ def test_sizes_past_a_launch(mxc):
         mxc.mxc_mxfp4_fc_workspace_bytes(4, mxc.MXC_MXFP4_FC_MAX_C + 1, 8, 1)
     with pytest.raises(mxc.MxcError):
         mxc.mxc_adamw8_state_bytes((1 << 33) + 1)
+
+
+def test_logprob_scales(mxc):
+    """Any positive scale whose product with log2(e) 32 bits hold; the kernels count in powers of two."""
+    lib = mxc.raw()
+    off = A + 4         # a misaligned z: the checks before that one have passed
+    for scale, want in ((1e-45, mxc.MXC_ERR_ALIGN), (1e-30, mxc.MXC_ERR_ALIGN), (2.35e38, mxc.MXC_ERR_ALIGN), (2.37e38, mxc.MXC_ERR_UNSUPPORTED), (3.4e38, mxc.MXC_ERR_UNSUPPORTED)):
+        assert lib.mxc_logprob_fwd(4, 100, 104, 1, off, B, scale, 5, C_, D, E, F_, G, H, 1 << 30, None) == want, scale
+        assert lib.mxc_logprob_bwd(4, 100, 104, 1, off, B, scale, C_, D, E, F_, G, None) == want, scale
+        assert lib.mxc_logprob_fwd_bwd(4, 100, 104, 1, off, B, scale, C_, D, E, F_, G, H, 1 << 30, None) == want, scale
