@@ -318,7 +318,8 @@ int mxc_sgd_update(size_t n, float *w, const float *g, float *v, void *w_bf16,
  *   dz[n,k]    = scale*( dlogp[n]*((k == labels[n]) - p[k]) - dentropy[n]*p[k]*(log p[k] + entropy[n]) )
  * labels: device int32; a label outside [0, K) has logp 0 and no gradient of logp.  A logit of minus infinity has
  * probability 0; a row of nothing else has log probabilities of minus infinity, entropy 0, stats (-inf, 0) and a zero
- * gradient.  A row that holds a NaN or plus infinity has NaN results.  Arithmetic, logp, entropy, stats and
+ * gradient.  A row that holds a NaN or plus infinity has NaN results; its top_index names tokens of the row in the order of the logits, where a NaN
+ * comes before plus infinity, one whose sign bit is set after minus infinity, and top_logp is NaN beside each.  Arithmetic, logp, entropy, stats and
  * top_logp are fp32; dz is rounded once to `dtype` and has z's ld.
  *   mxc_logprob_fwd      any of logp (and with it labels), entropy, stats may be NULL; top in 0..MXC_LOGPROB_MAX_TOP,
  *                        with top == 0 top_logp and top_index may be NULL

@@ -703,7 +703,7 @@ __global__ __launch_bounds__(G < 64 ? 256 : G, G == 512 && P == 16 ? 4 : 1) void
         if (a.logp) a.logp[row] = !given ? 0.f : empty ? -INFINITY : sc.log_prob(sc.any(zl), zl, ls);
         if (a.entropy) a.entropy[row] = empty ? 0.f : (ls - mean) * LN2;
         if (a.stats) {
-            a.stats[2 * row] = empty ? -INFINITY : m;
+            a.stats[2 * row] = empty ? -INFINITY : s == s ? m : s;
             a.stats[2 * row + 1] = empty ? 0.f : (ls - sc.any(m)) * LN2;
         }
     }
@@ -721,24 +721,34 @@ __global__ __launch_bounds__(G < 64 ? 256 : G, G == 512 && P == 16 ? 4 : 1) void
             if (lane < a.top) emit(lane, lane < a.K ? key_of(order(-INFINITY), (unsigned)lane) : NO_KEY);
             return;
         }
+        // A row with a NaN or plus infinity, whose log probabilities are all NaN: bounds and limits are no numbers there.  Cells that say nothing make
+        // select_top look at every value.
+        const bool ordered = s == s;
+        auto each = [&](unsigned from, auto f) { each_value<T, P>(p, held, lane * Piece<T>::V - r.head, G * Piece<T>::V, a.K, from, f); };
         if constexpr (W == 1) {
-            wave_top<T, P>(sh, p, most, held, lane * Piece<T>::V - r.head, a.K, a.top, emit);
-            return;
+            const unsigned nothing[1] = {0u};
+            if (ordered) wave_top<T, P>(sh, p, most, held, lane * Piece<T>::V - r.head, a.K, a.top, emit);
+            else select_top<1, 1, LOW>(sh, nothing, a.top, each, emit);
         } else {
             __shared__ Aside<T, HELD> aside;
-            const unsigned mine = wave_bound<S, LOW>(cell, (a.top + W - 1) / W);
-            if ((lane & 63) == 0) aside.said[lane >> 6] = mine;
-            if (lane == 0) aside.count = sh.count = 0;
-            __syncthreads();
-            const unsigned bound = aside.template hear<W>();
-            const float limit = bound >> LOW > order(-INFINITY) >> LOW ? unorder(bound) : LOWEST;
+            if (ordered) {
+                const unsigned mine = wave_bound<S, LOW>(cell, (a.top + W - 1) / W);
+                if ((lane & 63) == 0) aside.said[lane >> 6] = mine;
+                if (lane == 0) aside.count = sh.count = 0;
+                __syncthreads();
+                const unsigned bound = aside.template hear<W>();
+                const float limit = bound >> LOW > order(-INFINITY) >> LOW ? unorder(bound) : LOWEST;
 #pragma unroll
-            for (int q = 0; q < P; ++q)
-                if (q < held && p[q].template largest<true>() >= limit) aside.put(p[q], q * G + lane);
-            __syncthreads();
-            if (aside.template rank<W, LOW>(sh, bound, r.head, a.K, a.top, a.K, emit)) return;
-            __syncthreads();
-            select_top<W, S, LOW>(sh, cell, a.top, [&](unsigned from, auto f) { each_value<T, P>(p, held, lane * Piece<T>::V - r.head, G * Piece<T>::V, a.K, from, f); }, emit);
+                for (int q = 0; q < P; ++q)
+                    if (q < held && p[q].template largest<true>() >= limit) aside.put(p[q], q * G + lane);
+                __syncthreads();
+                if (aside.template rank<W, LOW>(sh, bound, r.head, a.K, a.top, a.K, emit)) return;
+                __syncthreads();
+            } else {
+#pragma unroll
+                for (int c = 0; c < S; ++c) cell[c] = 0;
+            }
+            select_top<W, S, LOW>(sh, cell, a.top, each, emit);
         }
     } else if (a.dz) {
         const float dl = a.dlogp && given ? a.dlogp[row] : 0.f, dh = a.dentropy ? a.dentropy[row] : 0.f;
@@ -789,7 +799,7 @@ __device__ __forceinline__ void write_row_results(const LogprobArgs &a, size_t r
     if (a.logp) a.logp[row] = !given ? 0.f : empty ? -INFINITY : sc.log_prob(sc.d2<false>(zl), zl, ls);
     if (a.entropy) a.entropy[row] = empty ? 0.f : (ls - j.t / j.s) * LN2;
     if (a.stats) {
-        a.stats[2 * row] = empty ? -INFINITY : j.m;
+        a.stats[2 * row] = empty ? -INFINITY : j.s == j.s ? j.m : j.s;
         a.stats[2 * row + 1] = ls * LN2;
     }
 }
@@ -1000,11 +1010,12 @@ __global__ __launch_bounds__(CHUNK_THREADS) void logprob_stream_kernel(LogprobAr
             if ((int)threadIdx.x < a.top) emit(threadIdx.x, (int)threadIdx.x < values ? key_of(order(-INFINITY), (unsigned)(first + (int)threadIdx.x)) : NO_KEY);
             return;
         }
-        if (aside.template rank<4, LOW>(sh, aside.template hear<4>(), r.head, a.K, a.top, values, emit)) return;
+        const bool ordered = j.s == j.s;        // (else cells say nothing, and every value is looked at: maxima pass over NaNs)
+        if (ordered && aside.template rank<4, LOW>(sh, aside.template hear<4>(), r.head, a.K, a.top, values, emit)) return;
         __syncthreads();
         unsigned cell[UNROLL];
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u) cell[u] = begin + u * CHUNK_THREADS + (int)threadIdx.x < end ? order(of[u]) : 0u;
+        for (int u = 0; u < UNROLL; ++u) cell[u] = ordered && begin + u * CHUNK_THREADS + (int)threadIdx.x < end ? order(of[u]) : 0u;
         select_top<4, UNROLL, LOW>(sh, cell, a.top, Streamed<T, UNROLL, NT>{r, begin, end, a.K, cell}, emit);
     }
 }

@@ -457,3 +457,45 @@ def test_scales_at_the_ends(mxc, dtype, N, K, pad):
     for scale in (1e-30, 1.7e-33, 1e-36, 1e-38, 1e-42, 1e37):
         for masked in (0, 1, 2):
             check(mxc, N, K, pad, dtype, masked, scale, 7, seed=masked)
+
+
+def set_bits(z, row, places, kind):
+    """NaN of either sign or plus infinity at places of a row, as bits."""
+    bits = {"nan": 0x7FC0, "-nan": 0xFFC0, "inf": 0x7F80}[kind]
+    if z.dtype == torch.float32:
+        z.view(torch.int32)[row, places] = bits << 16 if bits < 0x8000 else (bits << 16) - (1 << 32)
+    else:
+        z.view(torch.int16)[row, places] = bits if bits < 0x8000 else bits - (1 << 16)
+
+
+# rows of a wave, of a workgroup, streamed whole and in chunks
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("N,K", [(12, 3), (12, 100), (12, 500), (12, 1500), (12, 2900), (12, 7000), (300, 20000), (12, 20000), (12, 140001)])
+def test_top_of_rows_that_are_not_finite(mxc, dtype, N, K):
+    """Log probabilities are NaN, tokens in the order of their logits, with a NaN past the infinity of its sign; other rows are as ever."""
+    z = data(N, K, K, dtype, K, 0)[0]
+    gen = torch.Generator(device="cuda").manual_seed(K)
+    z[4, 1:] = -math.inf
+    for row, share, kind in ((0, 1.0, "nan"), (1, 1.0, "-nan"), (2, 1.0, "inf"), (5, 0.1, "nan"), (6, 0.1, "-nan"), (7, 0.1, "inf"), (10, 0.5, "nan"), (10, 0.5, "-nan")):
+        set_bits(z, row, torch.rand(K, generator=gen, device="cuda") < share, kind)
+    for row, kind in ((4, "nan"), (5, "nan"), (6, "-nan"), (7, "inf"), (9, "nan"), (9, "inf"), (10, "-nan")):
+        set_bits(z, row, torch.randint(0, K, (1,), generator=gen, device="cuda"), kind)
+    bad = ~(z.isfinite() | (z == -math.inf)).all(1)
+    # the values' bits as whole numbers in the order of the values
+    wide = z.view(torch.int32) if dtype == torch.float32 else z.view(torch.int16).int() << 16
+    rank = torch.where(wide < 0, wide ^ 0x7FFFFFFF, wide).long()
+    order = torch.sort(rank, dim=1, descending=True, stable=True).indices
+    code = mxc.dtype_code(dtype)
+    _, _, lp, _, _ = exact(z.double(), torch.zeros(N, dtype=torch.int32, device="cuda"), 1.0)
+    for top in (1, 20, 64):
+        ws = mxc.alloc_workspace(mxc.mxc_logprob_workspace_bytes(N, K, code, top))
+        H, stats = torch.empty(N, device="cuda"), torch.empty(N, 2, device="cuda")
+        tl, ti = torch.empty(N, top, device="cuda"), torch.empty(N, top, dtype=torch.int32, device="cuda")
+        mxc.mxc_logprob_fwd(N, K, K, code, z, None, 1.0, top, None, H, stats, tl, ti, ws)
+        n = min(top, K)
+        assert torch.equal(ti[:, :n].long(), order[:, :n])
+        assert bool(tl[bad][:, :n].isnan().all())
+        assert bool((ti[:, n:] == -1).all()) and bool((tl[:, n:] == -math.inf).all())
+        want = lp.gather(1, order[:, :n])[~bad]
+        near(tl[~bad][:, :n], want, torch.where(want == -math.inf, 0.0, U * (8 * want.abs() + 1024)))
+        assert bool(H[bad].isnan().all()) and bool(stats[bad].isnan().all()) and bool(H[~bad].isfinite().all()) and bool(stats[~bad].isfinite().all())
