@@ -86,6 +86,28 @@ bool to_ptr(PyObject *o, void **ptr, size_t *bytes = nullptr)
     return true;
 }
 
+// The same of a tensor that has to have at least `least` elements (0: any number) of `type` (Undefined: any; then `least` counts bytes).
+bool to_ptr_of(PyObject *o, const char *name, at::ScalarType type, size_t least, void **ptr)
+{
+    if (o != nullptr && THPVariable_Check(o)) {
+        const at::Tensor &t = THPVariable_Unpack(o);
+        if (type != at::ScalarType::Undefined && t.scalar_type() != type) {
+            PyErr_Format(PyExc_TypeError, "%s: expected %s, got %s", name, at::toString(type), at::toString(t.scalar_type()));
+            return false;
+        }
+        const size_t has = type == at::ScalarType::Undefined ? (size_t)t.nbytes() : (size_t)t.numel();
+        if (has < least) {
+            PyErr_Format(PyExc_ValueError, "%s: %zu %s, the call needs %zu", name, has, type == at::ScalarType::Undefined ? "bytes" : "elements", least);
+            return false;
+        }
+    }
+    return to_ptr(o, ptr);
+}
+
+// element type of a dtype argument, and products of sizes; what is not valid asks for nothing here: the library refuses it
+at::ScalarType type_of(int dtype) { return dtype == MXC_F32 ? at::ScalarType::Float : dtype == MXC_BF16 ? at::ScalarType::BFloat16 : at::ScalarType::Undefined; }
+size_t count(long long a, long long b = 1) { return a > 0 && b > 0 ? (size_t)a * (size_t)b : 0; }
+
 // device pointers of a list (or tuple) of contiguous GPU tensors of one element type; None: an empty vector.  numel: filled by the
 // first list (`first`), and what the others' tensors have to have.  type: the one that they must have, Undefined: that of the first tensor.
 bool to_ptrs(PyObject *o, const char *name, std::vector<void *> *ptrs, std::vector<size_t> *numel, bool first, at::ScalarType *type)
@@ -195,6 +217,10 @@ PyObject *done(int rc)
 #define RUN(EXPR) do { WithoutGil off; rc = EXPR; } while (0)
 #define INTS(COUNT) int d[COUNT]; if (!to_ints(a.v, d, COUNT)) return nullptr
 #define PTR(NAME, AT) void *NAME; if (!to_ptr(a.v[AT], &NAME)) return nullptr
+// a tensor of LEAST elements of TYPE; of the call's dtype DT (bytes where that is none: a call that the library refuses); bytes of any type
+#define PTR_OF(NAME, AT, TYPE, LEAST) void *NAME; if (!to_ptr_of(a.v[AT], names[AT], at::ScalarType::TYPE, LEAST, &NAME)) return nullptr
+#define PTR_IN(NAME, AT, DT, LEAST) void *NAME; if (!to_ptr_of(a.v[AT], names[AT], type_of(DT), type_of(DT) == at::ScalarType::Undefined ? 0 : (LEAST), &NAME)) return nullptr
+#define BYTES(NAME, AT, LEAST) PTR_OF(NAME, AT, Undefined, LEAST)
 #define BUF(NAME, AT) void *NAME; size_t NAME##_n; if (!to_ptr(a.v[AT], &NAME, &NAME##_n)) return nullptr
 #define STREAM(AT) void *st; if (!to_stream(a.v[AT], &st)) return nullptr
 #define INT(NAME, AT) int NAME; if (!to_int(a.v[AT], &NAME)) return nullptr
@@ -256,26 +282,34 @@ WRAP(mxc_sgd_update, 7, N_("w", "g", "v", "w_bf16", "lr", "momentum", "wd", "str
      // the element count is w's, whatever its type
      const size_t count = a.v[0] == Py_None ? 0 : (size_t)THPVariable_Unpack(a.v[0]).numel();
      RUN(mxc_sgd_update(count, (float *)w, (const float *)g, (float *)v, wb, (float)lr, (float)mom, (float)wd, st));)
+// N, K, ld, dtype of the log-probability calls: elements of the logits, from the first row's first to the last row's last
+#define LOGITS const size_t rows = count(d[0]), logits = d[0] > 0 && d[1] > 0 && d[2] >= d[1] ? (rows - 1) * (size_t)d[2] + (size_t)d[1] : 0
 WRAP(mxc_logprob_fwd, 13, N_("N", "K", "ld", "dtype", "z", "labels", "scale", "top", "logp", "entropy", "stats", "top_logp", "top_index", "workspace", "stream"),
-     INTS(4); PTR(z, 4); PTR(labels, 5); FLOAT(scale, 6); INT(top, 7); PTR(logp, 8); PTR(entropy, 9); PTR(stats, 10); PTR(tl, 11); PTR(ti, 12); BUF(ws, 13);
-     STREAM(14);
+     INTS(4); LOGITS; INT(top, 7); PTR_IN(z, 4, d[3], logits); PTR_OF(labels, 5, Int, rows); FLOAT(scale, 6); PTR_OF(logp, 8, Float, rows); PTR_OF(entropy, 9, Float, rows);
+     PTR_OF(stats, 10, Float, 2 * rows); PTR_OF(tl, 11, Float, count(d[0], top)); PTR_OF(ti, 12, Int, count(d[0], top)); BUF(ws, 13); STREAM(14);
      RUN(mxc_logprob_fwd(d[0], d[1], d[2], d[3], z, (const int *)labels, (float)scale, top, (float *)logp, (float *)entropy, (float *)stats, (float *)tl,
                          (int *)ti, ws, ws_n, st));)
 WRAP(mxc_logprob_bwd, 12, N_("N", "K", "ld", "dtype", "z", "labels", "scale", "stats", "entropy", "dlogp", "dentropy", "dz", "stream"),
-     INTS(4); PTR(z, 4); PTR(labels, 5); FLOAT(scale, 6); PTR(stats, 7); PTR(entropy, 8); PTR(dlogp, 9); PTR(dentropy, 10); PTR(dz, 11); STREAM(12);
+     INTS(4); LOGITS; PTR_IN(z, 4, d[3], logits); PTR_OF(labels, 5, Int, rows); FLOAT(scale, 6); PTR_OF(stats, 7, Float, 2 * rows); PTR_OF(entropy, 8, Float, rows);
+     PTR_OF(dlogp, 9, Float, rows); PTR_OF(dentropy, 10, Float, rows); PTR_IN(dz, 11, d[3], logits); STREAM(12);
      RUN(mxc_logprob_bwd(d[0], d[1], d[2], d[3], z, (const int *)labels, (float)scale, (const float *)stats, (const float *)entropy, (const float *)dlogp,
                          (const float *)dentropy, dz, st));)
 WRAP(mxc_logprob_fwd_bwd, 12, N_("N", "K", "ld", "dtype", "z", "labels", "scale", "dlogp", "dentropy", "logp", "entropy", "dz", "workspace", "stream"),
-     INTS(4); PTR(z, 4); PTR(labels, 5); FLOAT(scale, 6); PTR(dlogp, 7); PTR(dentropy, 8); PTR(logp, 9); PTR(entropy, 10); PTR(dz, 11); BUF(ws, 12);
-     STREAM(13);
+     INTS(4); LOGITS; PTR_IN(z, 4, d[3], logits); PTR_OF(labels, 5, Int, rows); FLOAT(scale, 6); PTR_OF(dlogp, 7, Float, rows); PTR_OF(dentropy, 8, Float, rows);
+     PTR_OF(logp, 9, Float, rows); PTR_OF(entropy, 10, Float, rows); PTR_IN(dz, 11, d[3], logits); BUF(ws, 12); STREAM(13);
      RUN(mxc_logprob_fwd_bwd(d[0], d[1], d[2], d[3], z, (const int *)labels, (float)scale, (const float *)dlogp, (const float *)dentropy, (float *)logp,
                              (float *)entropy, dz, ws, ws_n, st));)
+#define CODE_BYTES(ROWS, C) count(ROWS, ((C) + 31ll) / 32 * 16)
+#define SCALE_BYTES(ROWS, C) count(ROWS, ((C) + 511ll) / 512 * 16)
 WRAP(mxc_mxfp4_quantize, 6, N_("N", "C", "dtype", "x", "codes", "scales", "stream"),
-     INTS(3); PTR(x, 3); PTR(codes, 4); PTR(scales, 5); STREAM(6); RUN(mxc_mxfp4_quantize(d[0], d[1], d[2], x, codes, scales, st));)
+     INTS(3); PTR_IN(x, 3, d[2], count(d[0], d[1])); BYTES(codes, 4, CODE_BYTES(d[0], d[1])); BYTES(scales, 5, SCALE_BYTES(d[0], d[1])); STREAM(6);
+     RUN(mxc_mxfp4_quantize(d[0], d[1], d[2], x, codes, scales, st));)
 WRAP(mxc_mxfp4_dequantize, 6, N_("N", "C", "dtype", "codes", "scales", "y", "stream"),
-     INTS(3); PTR(codes, 3); PTR(scales, 4); PTR(y, 5); STREAM(6); RUN(mxc_mxfp4_dequantize(d[0], d[1], d[2], codes, scales, y, st));)
+     INTS(3); BYTES(codes, 3, CODE_BYTES(d[0], d[1])); BYTES(scales, 4, SCALE_BYTES(d[0], d[1])); PTR_IN(y, 5, d[2], count(d[0], d[1])); STREAM(6);
+     RUN(mxc_mxfp4_dequantize(d[0], d[1], d[2], codes, scales, y, st));)
 WRAP(mxc_mxfp4_fc_fwd, 10, N_("N", "C", "K", "dtype", "x", "w_codes", "w_scales", "bias", "relu", "y", "workspace", "stream"),
-     INTS(4); PTR(x, 4); PTR(wc, 5); PTR(wsc, 6); PTR(bias, 7); BOOL(relu, 8); PTR(y, 9); BUF(ws, 10); STREAM(11);
+     INTS(4); PTR_IN(x, 4, d[3], count(d[0], d[1])); BYTES(wc, 5, CODE_BYTES(d[2], d[1])); BYTES(wsc, 6, SCALE_BYTES(d[2], d[1])); PTR_OF(bias, 7, Float, count(d[2]));
+     BOOL(relu, 8); PTR_IN(y, 9, d[3], count(d[0], d[2])); BUF(ws, 10); STREAM(11);
      RUN(mxc_mxfp4_fc_fwd(d[0], d[1], d[2], d[3], x, wc, wsc, (const float *)bias, relu, y, ws, ws_n, st));)
 
 // what both AdamW calls read from their lists: element counts and pointers, and the element type of the gradients

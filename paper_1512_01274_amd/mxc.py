@@ -173,7 +173,8 @@ def _stream(stream):
 
 
 # The entry points, with these arguments (workspace and stream may be left out; tensors may be None where the header
-# allows it).  They are built-in functions of the extension module (csrc/binding.cpp) and raise MxcError on a status.
+# allows it).  They are built-in functions of the extension module (csrc/binding.cpp) and raise MxcError on a status.  The
+# log-probability, 4-bit and AdamW calls raise TypeError or ValueError for tensors of another element type or too few elements.
 #
 #   mxc_conv2d_workspace_bytes(op, N, C, H, W, K, R, S, stride, pad, dtype, layout) -> int
 #   mxc_conv2d_fwd(N, C, H, W, K, R, S, stride, pad, dtype, layout, x, w, y, workspace=None, stream=None)

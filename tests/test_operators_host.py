@@ -168,3 +168,48 @@ def test_logprob_scales(mxc):
         assert lib.mxc_logprob_fwd(4, 100, 104, 1, off, B, scale, 5, C_, D, E, F_, G, H, 1 << 30, None) == want, scale
         assert lib.mxc_logprob_bwd(4, 100, 104, 1, off, B, scale, C_, D, E, F_, G, None) == want, scale
         assert lib.mxc_logprob_fwd_bwd(4, 100, 104, 1, off, B, scale, C_, D, E, F_, G, H, 1 << 30, None) == want, scale
+
+
+def test_binding_types_and_sizes(mxc):
+    """Tensors of another element type than the call reads, or with fewer elements, are refused by the binding (fake device tensors: nothing is
+    launched, the library finds null pointers in a call that the binding lets through)."""
+    import torch
+    from torch._subclasses.fake_tensor import FakeTensorMode
+    N, K, ld, top, C = 4, 100, 104, 5, 70
+    with FakeTensorMode():
+        new = lambda n, dtype=torch.float32: torch.empty(n, dtype=dtype, device="cuda")  # noqa: E731
+        bf, i32, u8 = torch.bfloat16, torch.int32, torch.uint8
+        # name: (elements, type, another type that is refused); bytes may be of any type that holds them
+        z, row, ints = ((N - 1) * ld + K, bf, torch.float32), (N, torch.float32, torch.float64), (N, i32, torch.int64)
+        codes, scales, wc, ws = (N * 48, u8, None), (N * 16, u8, None), (K * 48, u8, None), (K * 16, u8, None)
+        calls = [
+            (mxc.mxc_logprob_fwd, dict(N=N, K=K, ld=ld, dtype=1, scale=1.0, top=top, stream=0),
+             dict(z=z, labels=ints, logp=row, entropy=row, stats=(2 * N, torch.float32, bf), top_logp=(N * top, torch.float32, bf), top_index=(N * top, i32, torch.int64))),
+            (mxc.mxc_logprob_bwd, dict(N=N, K=K, ld=ld, dtype=1, scale=1.0, stream=0),
+             dict(z=z, labels=ints, stats=(2 * N, torch.float32, torch.float64), entropy=row, dlogp=row, dentropy=row, dz=z)),
+            (mxc.mxc_logprob_fwd_bwd, dict(N=N, K=K, ld=ld, dtype=1, scale=1.0, stream=0),
+             dict(z=z, labels=ints, dlogp=row, dentropy=row, logp=row, entropy=row, dz=z)),
+            (mxc.mxc_mxfp4_quantize, dict(N=N, C=C, dtype=0, stream=0), dict(x=(N * C, torch.float32, bf), codes=codes, scales=scales)),
+            (mxc.mxc_mxfp4_dequantize, dict(N=N, C=C, dtype=1, stream=0), dict(y=(N * C, bf, torch.float16), codes=codes, scales=scales)),
+            (mxc.mxc_mxfp4_fc_fwd, dict(N=N, C=C, K=K, dtype=1, relu=1, stream=0),
+             dict(x=(N * C, bf, torch.float32), w_codes=wc, w_scales=ws, bias=(K, torch.float32, bf), y=(N * K, bf, torch.float32))),
+        ]
+        for call, plain, tensors in calls:
+            good = {k: new(n, t) for k, (n, t, _) in tensors.items()}
+            with pytest.raises(mxc.MxcError) as e:
+                call(**plain, **good)
+            assert e.value.status == mxc.MXC_ERR_NULL
+            for k, (n, t, other) in tensors.items():
+                with pytest.raises(ValueError, match=k):
+                    call(**plain, **{**good, k: new(n - 1, t)})
+                if other is not None:
+                    with pytest.raises(TypeError, match=k):
+                        call(**plain, **{**good, k: new(n, other)})
+            # bad sizes and types of the call itself are the library's to refuse
+            for bad in (dict(N=0), dict(N=-1), dict(dtype=9)):
+                with pytest.raises(mxc.MxcError):
+                    call(**{**plain, **bad}, **good)
+        # a NULL where one may be
+        with pytest.raises(mxc.MxcError) as e:
+            mxc.mxc_logprob_fwd(N, K, ld, 1, new(z[0], bf), None, 1.0, 0, None, new(N), None, None, None, None, 0)
+        assert e.value.status == mxc.MXC_ERR_NULL
