@@ -40,19 +40,19 @@ class Head:
             need = [mxc.mxc_conv2d_workspace_bytes(op, N, c, 1, 1, k, 1, 1, 1, 0, BF16, mxc.MXC_NHWC)
                     for c, k in ((C, H), (H, K)) for op in (mxc.MXC_FWD, mxc.MXC_BWD_DATA_RELU, mxc.MXC_BWD_WEIGHT, mxc.MXC_BIAS_GRAD)]
             need.append(mxc.mxc_logprob_workspace_bytes(N, K, BF16, 0))
-            self._buffers[N] = {"h": new(N, H), "z": new(N, K), "dh": new(N, H), "logp": new(N, dtype=torch.float32),
+            self._buffers[N] = {"h": new(N, H), "z": new(N, K), "dh": new(N, H),
                                 "weight": torch.full((N,), -1.0 / N, device=self.w[0].device), "workspace": mxc.alloc_workspace(max(need))}
         return self._buffers[N]
 
     def train_step(self, x, labels, lr=1e-3, wd=0.01):
-        """One step on bf16 rows x and int32 labels; returns the log probabilities of the labels (before the step)."""
+        """One step on bf16 rows x and int32 labels; returns the log probabilities of the labels (before the step), a new tensor."""
         N, (C, H, K) = x.shape[0], self.dims
         b = self._of_batch(N)
-        ws = b["workspace"]
+        ws, logp = b["workspace"], torch.empty(N, dtype=torch.float32, device=x.device)
         mxc.mxc_fc_fwd(N, C, H, BF16, x, self.copy[0], self.w[1], True, b["h"], ws)
         mxc.mxc_fc_fwd(N, H, K, BF16, b["h"], self.copy[2], self.w[3], False, b["z"], ws)
         # the loss is the mean of -logp: its gradient in logp is -1/N; dz takes the logits' place
-        mxc.mxc_logprob_fwd_bwd(N, K, K, BF16, b["z"], labels, 1.0, b["weight"], None, b["logp"], None, b["z"], ws)
+        mxc.mxc_logprob_fwd_bwd(N, K, K, BF16, b["z"], labels, 1.0, b["weight"], None, logp, None, b["z"], ws)
         mxc.mxc_fc_bwd_weight(N, H, K, BF16, b["h"], b["z"], self.grad[2], ws)
         mxc.mxc_bias_grad(N, K, 1, 1, BF16, mxc.MXC_NHWC, b["z"], self.grad[3], ws)
         mxc.mxc_fc_bwd_data(N, H, K, BF16, b["z"], self.copy[2], b["h"], b["dh"], ws)
@@ -64,7 +64,7 @@ class Head:
             mxc.mxc_adamw_update(self.w, self.grad, self.m, self.v, self.copy, *rest)
         else:
             mxc.mxc_adamw8_update(self.w, self.grad, self.state, self.copy, *rest, self.step)
-        return b["logp"]
+        return logp
 
     def served(self):
         return Served(self)

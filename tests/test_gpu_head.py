@@ -62,3 +62,13 @@ def test_first_gradients(head):
     torch.nn.functional.cross_entropy(logits, labels.long()).backward()
     for ours, theirs in zip(net.grad, w):
         assert float((ours - theirs.grad).abs().max()) <= 2.0 ** -5 * float(theirs.grad.abs().max())
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_results_of_a_step_stay(head, bits):
+    """A step's log probabilities are the caller's: the next steps of the same batch size leave them as they are."""
+    net, batch = head.Head(64, 96, 37, bits), head.clusters(64, 37)
+    kept = [net.train_step(*batch(48)) for _ in range(3)]
+    first = [k.clone() for k in kept]
+    net.train_step(*batch(48))
+    assert all(torch.equal(a, b) for a, b in zip(kept, first)) and not torch.equal(kept[0], kept[1]) and not torch.equal(kept[1], kept[2])
