@@ -41,7 +41,7 @@ class Head:
                     for c, k in ((C, H), (H, K)) for op in (mxc.MXC_FWD, mxc.MXC_BWD_DATA_RELU, mxc.MXC_BWD_WEIGHT, mxc.MXC_BIAS_GRAD)]
             need.append(mxc.mxc_logprob_workspace_bytes(N, K, BF16, 0))
             self._buffers[N] = {"h": new(N, H), "z": new(N, K), "dh": new(N, H),
-                                "weight": torch.full((N,), -1.0 / N, device=self.w[0].device), "workspace": mxc.alloc_workspace(max(need))}
+                                "weight": torch.full((N,), -1.0 / N, device=self.w[0].device), "workspace": mxc.alloc_workspace(max(need), device=self.w[0].device)}
         return self._buffers[N]
 
     def train_step(self, x, labels, lr=1e-3, wd=0.01):
