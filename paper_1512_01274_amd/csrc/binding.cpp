@@ -55,6 +55,10 @@ bool to_int(PyObject *o, int *out)
 {
     const long v = PyLong_AsLong(o);
     if (v == -1 && PyErr_Occurred()) return false;
+    if (v != (int)v) {
+        PyErr_Format(PyExc_OverflowError, "%ld does not fit an int", v);
+        return false;
+    }
     *out = (int)v;
     return true;
 }

@@ -221,3 +221,15 @@ def test_head_on_its_device():
     held = Head(64, 96, 37, device="cpu")._of_batch(48)
     assert held["workspace"] is not None
     assert all(t.device.type == "cpu" for t in held.values())
+
+
+def test_binding_sizes_past_32_bits(mxc):
+    """Sizes that an int does not hold are refused, not cut."""
+    for big in (1 << 32, (1 << 32) + 5, 1 << 31, -(1 << 31) - 1):
+        for call, args in ((mxc.mxc_logprob_workspace_bytes, [5, 100, 1, 3]), (mxc.mxc_mxfp4_fc_workspace_bytes, [5, 100, 70, 1]),
+                           (mxc.mxc_mxfp4_quantize, [5, 100, 1, None, None, None]), (mxc.mxc_logprob_fwd, [5, 100, 104, 1, None, None, 1.0, 3] + [None] * 5),
+                           (mxc.mxc_mxfp4_fc_fwd, [5, 100, 70, 1, None, None, None, None, 0, None])):
+            for i, a in enumerate(args):
+                if isinstance(a, int):
+                    with pytest.raises(OverflowError):
+                        call(*args[:i], big, *args[i + 1:])
