@@ -16,6 +16,13 @@ from paper_1512_01274_amd import mxc
 BF16 = mxc.MXC_BF16
 
 
+def _rows(x, features):
+    """How many rows x has, which are bf16 and of this many features."""
+    if x.dim() != 2 or x.shape[1] != features or x.dtype != torch.bfloat16:
+        raise ValueError(f"expected bf16 rows of {features} features, got {x.dtype} of shape {tuple(x.shape)}")
+    return x.shape[0]
+
+
 class Head:
     """y = w2 relu(w1 x + b1) + b2 for rows x of `features` values, `classes` logits; master weights in fp32, copies in bf16."""
 
@@ -46,7 +53,8 @@ class Head:
 
     def train_step(self, x, labels, lr=1e-3, wd=0.01):
         """One step on bf16 rows x and int32 labels; returns the log probabilities of the labels (before the step), a new tensor."""
-        N, (C, H, K) = x.shape[0], self.dims
+        C, H, K = self.dims
+        N = _rows(x, C)
         b = self._of_batch(N)
         ws, logp = b["workspace"], torch.empty(N, dtype=torch.float32, device=x.device)
         mxc.mxc_fc_fwd(N, C, H, BF16, x, self.copy[0], self.w[1], True, b["h"], ws)
@@ -84,7 +92,8 @@ class Served:
 
     def score(self, x, labels=None, top=5):
         """(log probabilities of the labels or None, entropy, the `top` most probable classes' log probabilities and indices) of bf16 rows x."""
-        N, (C, H, K) = x.shape[0], self.dims
+        C, H, K = self.dims
+        N = _rows(x, C)
         new = lambda *s, dtype=torch.float32: torch.empty(*s, dtype=dtype, device=x.device)  # noqa: E731
         h, z = new(N, H, dtype=torch.bfloat16), new(N, K, dtype=torch.bfloat16)
         need = [mxc.mxc_mxfp4_fc_workspace_bytes(N, C, H, BF16), mxc.mxc_mxfp4_fc_workspace_bytes(N, H, K, BF16), mxc.mxc_logprob_workspace_bytes(N, K, BF16, top)]

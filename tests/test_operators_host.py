@@ -233,3 +233,19 @@ def test_binding_sizes_past_32_bits(mxc):
                 if isinstance(a, int):
                     with pytest.raises(OverflowError):
                         call(*args[:i], big, *args[i + 1:])
+
+
+def test_head_refuses_other_rows():
+    """Rows of another length or type than the head's first layer reads are refused before anything runs."""
+    import torch
+    from paper_1512_01274_amd.head import Head, Served
+    net = Head(64, 96, 37, device="cpu")
+    served = Served.__new__(Served)
+    served.dims = net.dims
+    labels = torch.zeros(4, dtype=torch.int32)
+    for x in (torch.zeros(4, 63), torch.zeros(4, 64), torch.zeros(64).bfloat16(), torch.zeros(4, 63).bfloat16(), torch.zeros(4, 65).bfloat16(), torch.zeros(2, 4, 64).bfloat16()):
+        with pytest.raises(ValueError, match="rows"):
+            net.train_step(x, labels)
+        with pytest.raises(ValueError, match="rows"):
+            served.score(x)
+    assert net.step == 0
