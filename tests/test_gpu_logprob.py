@@ -499,3 +499,42 @@ def test_top_of_rows_that_are_not_finite(mxc, dtype, N, K):
         want = lp.gather(1, order[:, :n])[~bad]
         near(tl[~bad][:, :n], want, torch.where(want == -math.inf, 0.0, U * (8 * want.abs() + 1024)))
         assert bool(H[bad].isnan().all()) and bool(stats[bad].isnan().all()) and bool(H[~bad].isfinite().all()) and bool(stats[~bad].isfinite().all())
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("K", [2, 7, 9, 33, 64, 100, 257, 500, 1000, 1500, 2047, 4000, 8100])
+@pytest.mark.parametrize("masked,scale", [(0, 1.0), (2, 0.7), (1, 1.3)])
+def test_close(mxc, dtype, K, masked, scale):
+    """The bounds of `check` with the chain that a row of K values really has: a thread adds 128 values of its row at most, lanes and waves 22 more.
+    Errors of d are 2.5 roundings of its size (of the scale's product, the factor and the difference), an exponential's is two and d's, a sum's one a link
+    and the terms' own; twice that, for what is divided, multiplied and put together from them."""
+    N = 9
+    z, labels, dlogp, dentropy = data(N, K, K, dtype, K + masked, masked)
+    s = float(np.float32(scale))
+    logp, H, lp, p, d, dz = exact(z.double(), labels, s, dlogp, dentropy)
+    a = torch.where(p > 0, d.abs(), 0.0)        # (a token without probability has no part in any sum)
+    n = 2 * (min(K, 128) + 22) + 16
+    m1, m2 = (p * a).sum(1), (p * a * a).sum(1)
+    logS = torch.where(H > 0, H, 0.0) + m1
+    tl = U * (n + 8 * torch.where(logp > -math.inf, logp.abs(), 0.0) + 8 * m1 + 8 * logS)
+    th = U * (n * (1 + m1) + 8 * m2 + 8 * (logS + m1))
+    m1, m2 = m1[:, None], m2[:, None]
+    dl, dh = dlogp.double()[:, None].abs(), dentropy.double()[:, None].abs()
+    onehot = torch.zeros_like(p).scatter_(1, labels.clamp(0, K - 1).long()[:, None], 1.0)
+    tz = U * s * (2 * dl * onehot + p * (dl * (n + 8 * a + 8 * m1) + dh * (n * (1 + a + m1) + 8 * (a * a + a * m1 + m2)))) + dz.abs() * torch.finfo(dtype).eps / 2 + 1e-37
+    code, top = mxc.dtype_code(dtype), min(K, 20)
+    ws = mxc.alloc_workspace(mxc.mxc_logprob_workspace_bytes(N, K, code, top))
+    l, h, stats, out = torch.empty(N, device="cuda"), torch.empty(N, device="cuda"), torch.empty(N, 2, device="cuda"), torch.empty_like(z)
+    t, ti = torch.empty(N, top, device="cuda"), torch.empty(N, top, dtype=torch.int32, device="cuda")
+    mxc.mxc_logprob_fwd_bwd(N, K, K, code, z, labels, s, dlogp, dentropy, l, h, out, ws)
+    near(l, logp, tl)
+    near(h, H, th)
+    near(out, dz, tz)
+    mxc.mxc_logprob_fwd(N, K, K, code, z, labels, s, top, l, h, stats, t, ti, ws)
+    near(l, logp, tl)
+    near(h, H, th)
+    want = lp.gather(1, ti.long())
+    size = torch.where(want > -3e38, want.abs(), 0.0)
+    near(torch.where(want > -3e38, t.double(), 0.0), torch.where(want > -3e38, want, 0.0), U * (n + 8 * size + 8 * (m1 + logS[:, None])))
+    mxc.mxc_logprob_bwd(N, K, K, code, z, labels, s, stats, h, dlogp, dentropy, out)
+    near(out, dz, tz)
