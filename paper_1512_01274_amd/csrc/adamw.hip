@@ -3,7 +3,7 @@
 // every 32 values.  The tensors' pointers and sizes travel in the kernel's arguments, MXC_ADAMW_GROUP tensors a launch (with 8-bit states
 // MXC_ADAMW8_GROUP), so that nothing is copied to the device and a captured launch holds all that it needs.  Memory bounds it, with every byte moved once:
 // 65 million values, fp32 states, gradients and a bf16 copy, 30 bytes a value, 331 us, 5.9 TB/s; 204 million with 8-bit states and bf16 gradients, 14.1
-// bytes, 520 us, 5.6 TB/s; 24 tensors of up to 4096 values are one launch, 5.7 us.
+// bytes, 522 us, 5.5 TB/s, where the vector units are busy throughout, too; 24 tensors of up to 4096 values are one launch, 5.7 us.
 #include "mxc_internal.h"
 
 // every operation rounds by itself: where a code of 8 bits is decided, no product is kept unrounded in one place and not in another

@@ -7,8 +7,10 @@
 // A row is read once.  Workgroups of 64 to 1024 threads hold it in registers as 16-byte pieces (up to 256 KB: half of a compute
 // unit's registers), meet for the maximum and for the sums, and write the gradient from what they hold.  Without a gradient, rows of more than
 // 1024 pieces stream by.  Few rows, and rows that are longer than registers, are cut into chunks, each with its own maximum and sums, which a second
-// launch joins (and reads again for the gradient).  Memory bounds it: 4096 rows of 131072 bf16 with the gradient 434 us, 4.95 TB/s; 4096 of
-// 50257 with the 8 best tokens 85 us, 4.8 TB/s; one row of 131072 with the 20 best is latency, 11.3 us in two launches.
+// launch joins (and reads again for the gradient).  4096 rows of 131072 bf16 with the gradient 433 us, 4.95 TB/s: one workgroup a compute unit, which loads nothing
+// while it reduces and writes its row; the gradient from statistics, eight workgroups a unit, moves the same bytes in 367 us, 5.85 TB/s.  4096 of 50257 with the 8 best
+// tokens 86 us, 4.8 TB/s: the vector units issue without a pause, 14.4 instructions a value (75 us and 11.3 without the best tokens; of fp32 151 us, 5.4 TB/s).
+// One row of 131072 with the 20 best is latency, 11.3 us in two launches.
 #include <type_traits>
 
 #include "mxc_internal.h"
@@ -1232,6 +1234,9 @@ Cut cut_rows(int N, int pieces, bool gradient)
     // A gradient's rows are held, but for long ones where there are few: 131072 of bf16 took 20.4 us held and 13.9 in chunks at 64 rows, 23.3 and 21.2 at 128,
     // 29.4 and 31.5 at 192; 58262 of them 11.5 and 6.9 at 2, 12.7 and 12.6 at 64; 30000 7.4 and 6.2 at 2, 8.0 and 8.2 at 64.
     if (pieces <= SHORT_PIECES || (gradient && (pieces <= 2 * SHORT_PIECES || (pieces <= ROW_PIECES / 2 && N >= 64) || (pieces <= ROW_PIECES && N >= 160)))) return Cut{0, 0};
+    // Without one, from 256 rows on a row is one workgroup and one launch: 4 (512 rows and more: 2) chunks each, 131072 of bf16 with 20 best tokens, 28.9 and 26.0 in
+    // chunks at 256 rows, 35.1 and 36.9 at 400, 54.8 and 63.1 at 1000; without best tokens 16.8 and 16.7, 23.3 and 26.0, 49.1 and 55.2; 50257 18.0 and 19.8,
+    // 20.6 and 24.9, 29.5 and 39.8; 20000 11.4 and 14.7, 13.3 and 16.6, 17.8 and 28.1.
     int chunks = N >= 256 ? 1 : (1024 + N - 1) / N;
     chunks = chunks < (pieces + CHUNK_THREADS - 1) / CHUNK_THREADS ? chunks : (pieces + CHUNK_THREADS - 1) / CHUNK_THREADS;
     Cut c;

@@ -194,8 +194,9 @@ __global__ __launch_bounds__(256) void mxfp4_order_kernel(int N, int C, int grou
 }
 
 // 16*WF filter rows and 16*NF rows of x a workgroup, both straight from the caches into registers; its eight waves take every eighth step of
-// 128 columns, and their sums meet in LDS.  A step is under way while one is multiplied (two were no faster, in half as many workgroups a compute unit).
-// What it reads through the L2s bounds it: 128 rows of 9216 by 4096 10.4 us (and 3.1 to order x) for 0.45 MB in each of 256 workgroups.
+// 128 columns, and their sums meet in LDS.  A step is under way while one is multiplied (two were no faster).
+// What a compute unit reads through its L2 bounds the steps: 128 rows by 4096 take 6.6, 10.6 and 17.1 us for 4608, 9216 and 18432 columns, so 0.7 to 0.9 us for each
+// step of 52 KB a workgroup, and 3 us to begin and to join; with steps of 26 KB (32 rows of x) 9216 columns take 6.5 us.  Ordering x is another 3 to 4 us.
 template <typename T, int WF, int NF>
 __global__ __launch_bounds__(512) void mxfp4_skinny_kernel(int N, int K, int blocks, int scale_row, const unsigned char *xc, const unsigned char *xs,
                                                            const unsigned char *wc, const unsigned char *ws, const float *bias, int relu, T *y)
@@ -331,8 +332,8 @@ __global__ __launch_bounds__(256) void mxfp4_prepare_kernel(int N, int C, int K,
 // GM x GN waves of 32*FM filter rows by 32*FN rows of x each.  A stage is 128 columns, 64 bytes of codes a row, brought into a ring of four
 // stages by direct loads; scales come a word for two stages.  Row r's 16-byte chunk c lies at place c ^ (r/4)%4, so that the 16 rows
 // that one phase of a 16-byte read covers lie in all 64 banks once.
-// 8192 x 8192 by 8192: 260 us, 4.2 PFLOP/s, the matrix pipe busy 0.62 of the time at 1.75 GHz: a stage's reads from LDS and fills of it take as many
-// cycles as its products.  Preparing the operands takes 39 us more.
+// 8192 x 8192 by 8192: 260 us, 4.2 PFLOP/s (in single calls 293), the matrix pipe busy 0.62 of the time at 1.75 GHz: a stage's reads from LDS and fills of it take as many
+// cycles as its products.  Preparing the operands takes 38 us more, from fp32 66.
 // One barrier a stage, between the last operand fetch of the stage and its last products: the fetches of the next stage and the
 // loads of the one after three more go between the products.
 template <int FM, int FN, int GM, int GN>
