@@ -473,15 +473,16 @@ struct Aside {
 };
 
 // The values of a thread's pieces that reach `from`, and the row's index of each: f(order, index).  first: the index of value 0 of piece 0;
-// held: pieces that any thread holds.  A whole wave goes on where no lane has a piece that may reach it.
+// held: pieces that any thread holds.  A whole wave goes on where no lane has a piece that may reach it (ordered: none of them is a NaN, which a piece's
+// largest value passes over).
 template <typename T, int P, class F>
-__device__ __forceinline__ void each_value(const Piece<T> (&p)[P], int held, int first, int stride, int K, unsigned from, F f)
+__device__ __forceinline__ void each_value(const Piece<T> (&p)[P], int held, int first, int stride, int K, bool ordered, unsigned from, F f)
 {
     const float limit = unorder(from);      // (NaN for the lowest bounds: then every value is looked at)
 #pragma unroll
     for (int q = 0; q < P; ++q) {
         if (q >= held) continue;
-        if (__ballot(!(p[q].template largest<true>() < limit)) == 0) continue;
+        if (ordered && __ballot(!(p[q].template largest<true>() < limit)) == 0) continue;
         int index = first + q * stride;
         asm volatile("" : "+v"(index));     // (else the indices of all values are worked out ahead, and held)
 #pragma unroll
@@ -723,14 +724,21 @@ __global__ __launch_bounds__(G < 64 ? 256 : G, G == 512 && P == 16 ? 4 : 1) void
             if (lane < a.top) emit(lane, lane < a.K ? key_of(order(-INFINITY), (unsigned)lane) : NO_KEY);
             return;
         }
-        // A row with a NaN or plus infinity, whose log probabilities are all NaN: bounds and limits are no numbers there.  Cells that say nothing make
-        // select_top look at every value.
+        // Not ordered: a row with a NaN or plus infinity, whose log probabilities are all NaN.  Maxima pass over NaNs and limits may be none; there the cells come from
+        // the values' order as whole numbers, in which a NaN has its place.
         const bool ordered = s == s;
-        auto each = [&](unsigned from, auto f) { each_value<T, P>(p, held, lane * Piece<T>::V - r.head, G * Piece<T>::V, a.K, from, f); };
+        auto each = [&](unsigned from, auto f) { each_value<T, P>(p, held, lane * Piece<T>::V - r.head, G * Piece<T>::V, a.K, ordered, from, f); };
+        auto largest_order = [&]() {
+            unsigned m = 0;
+            each(0, [&](unsigned o, unsigned) { m = max(m, o); });
+            return m;
+        };
         if constexpr (W == 1) {
-            const unsigned nothing[1] = {0u};
             if (ordered) wave_top<T, P>(sh, p, most, held, lane * Piece<T>::V - r.head, a.K, a.top, emit);
-            else select_top<1, 1, LOW>(sh, nothing, a.top, each, emit);
+            else {
+                const unsigned own[1] = {largest_order()};
+                select_top<1, 1, LOW>(sh, own, a.top, each, emit);
+            }
         } else {
             __shared__ Aside<T, HELD> aside;
             if (ordered) {
@@ -748,7 +756,8 @@ __global__ __launch_bounds__(G < 64 ? 256 : G, G == 512 && P == 16 ? 4 : 1) void
                 __syncthreads();
             } else {
 #pragma unroll
-                for (int c = 0; c < S; ++c) cell[c] = 0;
+                for (int c = 1; c < S; ++c) cell[c] = 0;
+                cell[0] = largest_order();
             }
             select_top<W, S, LOW>(sh, cell, a.top, each, emit);
         }
@@ -833,6 +842,7 @@ struct Streamed {
     const Row<T, NT> &r;
     int begin, end, K;
     const unsigned *cell;
+    bool ordered;       // as in each_value
     template <class F>
     __device__ __forceinline__ void operator()(unsigned from, F f) const
     {
@@ -849,7 +859,7 @@ struct Streamed {
                 for (int i = 0; i < AHEAD; ++i) p[i] = r.load(at + i * STEP, low, end);
 #pragma unroll
                 for (int i = 0; i < AHEAD; ++i) {
-                    if (at + i * STEP >= end || p[i].template largest<true>() < limit) continue;
+                    if (at + i * STEP >= end || (ordered && p[i].template largest<true>() < limit)) continue;
                     int first = (at + i * STEP) * Piece<T>::V - r.head;
                     asm volatile("" : "+v"(first));
 #pragma unroll
@@ -1012,13 +1022,25 @@ __global__ __launch_bounds__(CHUNK_THREADS) void logprob_stream_kernel(LogprobAr
             if ((int)threadIdx.x < a.top) emit(threadIdx.x, (int)threadIdx.x < values ? key_of(order(-INFINITY), (unsigned)(first + (int)threadIdx.x)) : NO_KEY);
             return;
         }
-        const bool ordered = j.s == j.s;        // (else cells say nothing, and every value is looked at: maxima pass over NaNs)
+        const bool ordered = j.s == j.s;        // (as in logprob_row_kernel)
         if (ordered && aside.template rank<4, LOW>(sh, aside.template hear<4>(), r.head, a.K, a.top, values, emit)) return;
         __syncthreads();
         unsigned cell[UNROLL];
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) cell[u] = ordered && begin + u * CHUNK_THREADS + (int)threadIdx.x < end ? order(of[u]) : 0u;
-        select_top<4, UNROLL, LOW>(sh, cell, a.top, Streamed<T, UNROLL, NT>{r, begin, end, a.K, cell}, emit);
+        const Streamed<T, UNROLL, NT> each{r, begin, end, a.K, cell, ordered};
+        if (!ordered) {
+            unsigned largest[UNROLL] = {};
+            each(0, [&](unsigned o, unsigned index) {
+                const int turn = ((int)index + r.head) / V - begin;     // of pieces, in which u comes round
+#pragma unroll
+                for (int u = 0; u < UNROLL; ++u)
+                    if (turn / CHUNK_THREADS % UNROLL == u) largest[u] = max(largest[u], o);
+            });
+#pragma unroll
+            for (int u = 0; u < UNROLL; ++u) cell[u] = largest[u];
+        }
+        select_top<4, UNROLL, LOW>(sh, cell, a.top, each, emit);
     }
 }
 
