@@ -624,7 +624,7 @@ __global__ __launch_bounds__(G < 64 ? 256 : G, G == 512 && P == 16 ? 4 : 1) void
     unsigned cell[S];
     if constexpr (TOP && W > 1) {
 #pragma unroll
-        for (int s = 0; s < S; ++s) cell[s] = order(part[s].largest());
+        for (int s = 0; s < S; ++s) cell[s] = s < held ? order(part[s].largest()) : 0u;     // (a part that has seen nothing has a value all the same)
     }
 #pragma unroll
     for (int s = 1; s < S; ++s) part[0].look(part[s]);

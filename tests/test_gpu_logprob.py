@@ -538,3 +538,28 @@ def test_close(mxc, dtype, K, masked, scale):
     near(torch.where(want > -3e38, t.double(), 0.0), torch.where(want > -3e38, want, 0.0), U * (n + 8 * size + 8 * (m1 + logS[:, None])))
     mxc.mxc_logprob_bwd(N, K, K, code, z, labels, s, stats, h, dlogp, dentropy, out)
     near(out, dz, tz)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("pieces", [257, 300, 400, 511, 513, 554, 640, 767, 768, 769, 900, 1023])
+@pytest.mark.parametrize("top", [1, 20, 64])
+def test_few_tokens_of_no_less_than_zero(mxc, dtype, pieces, top):
+    """Rows of which fewer logits than `top` are 0 or more, or one is: the others are negative, or one masked value; of lengths that fill some of a
+    thread's pieces."""
+    N, K = 24, pieces * 16 // dtype.itemsize - 3
+    gen = torch.Generator(device="cuda").manual_seed(pieces)
+    z = -torch.rand(N, K, generator=gen, device="cuda") * 5 - 0.5
+    z[1::3] = torch.where(torch.rand(N, K, generator=gen, device="cuda") < 0.03, z, torch.tensor(-1e4, device="cuda"))[1::3]
+    z[2::3] = -1e20
+    for n in range(N):
+        at = torch.randperm(K, generator=gen, device="cuda")[:n * top // N + 1]
+        z[n, at] = torch.randint(0, 4, (len(at),), generator=gen, device="cuda").float()
+    z = z.to(dtype)
+    code = mxc.dtype_code(dtype)
+    ws = mxc.alloc_workspace(mxc.mxc_logprob_workspace_bytes(N, K, code, top))
+    logp, index = torch.empty(N, top, device="cuda"), torch.empty(N, top, dtype=torch.int32, device="cuda")
+    mxc.mxc_logprob_fwd(N, K, K, code, z, None, 1.0, top, None, None, None, logp, index, ws)
+    order = torch.sort(z.double(), dim=1, descending=True, stable=True).indices[:, :top]
+    assert torch.equal(index.long(), order)
+    want = exact(z.double(), torch.zeros(N, dtype=torch.int32, device="cuda"), 1.0)[2].gather(1, order)
+    near(logp, want, U * (8 * want.abs() + 1024))
