@@ -763,7 +763,8 @@ __global__ __launch_bounds__(G < 64 ? 256 : G, G == 512 && P == 16 ? 4 : 1) void
         }
     } else if (a.dz) {
         const float dl = a.dlogp && given ? a.dlogp[row] : 0.f, dh = a.dentropy ? a.dentropy[row] : 0.f;
-        const float per = empty ? 0.f : a.scale / s, A = empty ? 0.f : per * (dh * (mean * LN2) - dl), B = -per * dh * LN2;
+        // (the scale meets the weights first: divided by the sum it might be too small for a normal number where the product is not)
+        const float part = empty ? 0.f : 1.f / s, A = empty ? 0.f : a.scale * (dh * (mean * LN2) - dl) * part, B = -(a.scale * dh) * LN2 * part;
         const int place = given && !empty ? label + r.head : -1;
         auto gradient = [&](int piece, auto how, auto d2_of) {
             float g[Piece<T>::V];
@@ -1188,7 +1189,7 @@ __device__ __forceinline__ void block_gradient(const LogprobArgs &a, size_t row,
     const int label = a.labels ? a.labels[row] : -1;
     const bool given = (unsigned)label < (unsigned)a.K;
     const float dl = a.dlogp && given ? a.dlogp[row] : 0.f, dh = a.dentropy ? a.dentropy[row] : 0.f;
-    const float per = a.scale / s, A = per * (dh * (mean * LN2) - dl), B = -per * dh * LN2;
+    const float part = 1.f / s, A = a.scale * (dh * (mean * LN2) - dl) * part, B = -(a.scale * dh) * LN2 * part;        // (as in logprob_row_kernel)
     const int place = given ? label + r.head : -1;
     const int piece0 = block * (CHUNK_THREADS * P) + (int)threadIdx.x;
     Piece<T> p[P];

@@ -563,3 +563,24 @@ def test_few_tokens_of_no_less_than_zero(mxc, dtype, pieces, top):
     assert torch.equal(index.long(), order)
     want = exact(z.double(), torch.zeros(N, dtype=torch.int32, device="cuda"), 1.0)[2].gather(1, order)
     near(logp, want, U * (8 * want.abs() + 1024))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("N,K", [(5, 30), (9, 3001), (70, 27974), (3, 70001)])
+def test_small_scales_with_large_weights(mxc, dtype, N, K):
+    """A scale that is hardly a normal number, divided by a large sum, under weights that bring the gradient back into range."""
+    for scale, weight in ((2.5e-38, 1e13), (1e-36, 1e30), (3e36, 1e-30)):
+        s = float(np.float32(scale))
+        z, labels, dlogp, dentropy = data(N, K, K, dtype, K, 0)
+        z[1] *= 2.0 / s if s < 1 else 1.0       # (within what either type holds)
+        z[1].clamp_(-1e38, 1e38)
+        dlogp, dentropy = dlogp * weight, dentropy * weight
+        logp, H, dz, tol = gradient_tol(z, labels, s, dlogp, dentropy, dtype)
+        code = mxc.dtype_code(dtype)
+        ws = mxc.alloc_workspace(mxc.mxc_logprob_workspace_bytes(N, K, code, 0))
+        out, h, stats = torch.empty_like(z), torch.empty(N, device="cuda"), torch.empty(N, 2, device="cuda")
+        mxc.mxc_logprob_fwd_bwd(N, K, K, code, z, labels, s, dlogp, dentropy, None, None, out, ws)
+        near(out, dz, tol)
+        mxc.mxc_logprob_fwd(N, K, K, code, z, None, s, 0, None, h, stats, None, None, ws)
+        mxc.mxc_logprob_bwd(N, K, K, code, z, labels, s, stats, h, dlogp, dentropy, out)
+        near(out, dz, tol)
