@@ -332,7 +332,7 @@ __global__ __launch_bounds__(256) void mxfp4_prepare_kernel(int N, int C, int K,
 // GM x GN waves of 32*FM filter rows by 32*FN rows of x each.  A stage is 128 columns, 64 bytes of codes a row, brought into a ring of four
 // stages by direct loads; scales come a word for two stages.  Row r's 16-byte chunk c lies at place c ^ (r/4)%4, so that the 16 rows
 // that one phase of a 16-byte read covers lie in all 64 banks once.
-// 8192 x 8192 by 8192: 260 us, 4.2 PFLOP/s (in single calls 293), the matrix pipe busy 0.62 of the time at 1.75 GHz: a stage's reads from LDS and fills of it take as many
+// 8192 x 8192 by 8192: 260 us, 4.2 PFLOP/s (in single calls some 300), the matrix pipe busy 0.62 of the time at 1.75 GHz: a stage's reads from LDS and fills of it take as many
 // cycles as its products.  Preparing the operands takes 38 us more, from fp32 66.
 // One barrier a stage, between the last operand fetch of the stage and its last products: the fetches of the next stage and the
 // loads of the one after three more go between the products.
