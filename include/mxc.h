@@ -400,6 +400,70 @@ int mxc_adamw8_update(int count, const size_t *sizes, void *const *w, const void
                       double grad_scale, long long step, unsigned seed, void *hip_stream);
 
 /*
+ * Embedding: rows of a table for given tokens, and the table's gradient.  tokens: [N] device int32; w: [V][C] and y, dy: [N][C] of `dtype`; dw: [V][C]
+ * fp32 for both dtypes.  A token outside [0, V) (padding) has a row of zeros and no gradient.
+ *   mxc_embedding_fwd:  y[n,c] = scale * w[tokens[n],c], rounded once to `dtype`
+ *   mxc_embedding_bwd:  dw[v,c] = scale * sum over n with tokens[n] == v of dy[n,c], zeros for a token that stands nowhere; with accumulate == 1 this
+ *                       is added to the dw that is there, and rows of tokens that stand nowhere are neither read nor written (a table whose product
+ *                       with the last layer's input has left its gradient there)
+ * Sums in fp32 in an order that depends on the tokens alone (bit-identical from run to run).  Workspace: mxc_embedding_workspace_bytes, for the
+ * gradient.  Errors: MXC_ERR_SHAPE (non-positive sizes, N, V or C above the limits below), MXC_ERR_UNSUPPORTED (dtype, scale that is not finite,
+ * accumulate), MXC_ERR_NULL, MXC_ERR_ALIGN (16 bytes, 4 for tokens), MXC_ERR_WORKSPACE, MXC_ERR_LAUNCH.
+ */
+enum { MXC_EMBEDDING_MAX_N = 1 << 23, MXC_EMBEDDING_MAX_V = 1 << 23, MXC_EMBEDDING_MAX_C = 1 << 20 };
+int mxc_embedding_fwd(int N, int V, int C, int dtype, const int *tokens, const void *w, float scale, void *y, void *hip_stream);
+int mxc_embedding_workspace_bytes(int N, int V, int C, int dtype, size_t *out_bytes);
+int mxc_embedding_bwd(int N, int V, int C, int dtype, const int *tokens, const void *dy, float scale, int accumulate, float *dw,
+                      void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Layer norm over the rows of x: [N][C] of `dtype`, dense; gamma, beta: C fp32 values.
+ *   mxc_layernorm_fwd:  mean = sum_c x / C,  rstd = 1 / sqrt(sum_c (x - mean)^2 / C + eps),  z = (x - mean) * rstd
+ *                       y = z * gamma + beta,  stats[n] = (mean, rstd);  gamma (ones), beta (zeros) and stats may each be NULL; y may be x
+ *   mxc_layernorm_bwd:  from x and the stats of the forward call, with g = dy * gamma:
+ *                       dx = rstd * (g - sum_c g / C - z * sum_c g * z / C),  dgamma[c] = sum_n dy * z,  dbeta[c] = sum_n dy
+ *                       gamma (ones), dgamma and dbeta may each be NULL; dx may be dy or x
+ * Arithmetic, stats, dgamma and dbeta are fp32 (the squares are those of the differences from the mean: a large mean costs no digits), y and dx are rounded
+ * once to `dtype`; an infinity or a NaN makes NaN of its row's results and of the gradients that it enters.  dgamma and dbeta are added in a fixed order.
+ * Workspace: mxc_layernorm_workspace_bytes, for the gradient.  Errors: MXC_ERR_SHAPE (non-positive sizes, C above MXC_LAYERNORM_MAX_C), MXC_ERR_UNSUPPORTED
+ * (dtype; eps that is not a normal positive number), MXC_ERR_NULL, MXC_ERR_ALIGN (16 bytes, 4 for stats), MXC_ERR_WORKSPACE, MXC_ERR_LAUNCH.
+ */
+enum { MXC_LAYERNORM_MAX_C = 1 << 20 };
+int mxc_layernorm_fwd(int N, int C, int dtype, const void *x, const float *gamma, const float *beta, float eps, void *y, float *stats, void *hip_stream);
+int mxc_layernorm_workspace_bytes(int N, int C, int dtype, size_t *out_bytes);
+int mxc_layernorm_bwd(int N, int C, int dtype, const void *x, const float *gamma, const float *stats, const void *dy, void *dx, float *dgamma, float *dbeta,
+                      void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Orthogonal update directions by Newton-Schulz steps, and the optimiser's step that uses them (Muon).  count matrices of rows[i] x cols[i] values,
+ * dense; rows, cols and the lists of device pointers are HOST arrays, read before the call returns.
+ *   mxc_orthogonalize:  X = x / |x|, |x| the root of the sum of squares;  `steps` times  X <- a X + (b A + c A A) X,  A = X X^T,  with a = 3.4445,
+ *                       b = -4.7750, c = 2.0315 and X turned so that its rows are not longer than its columns;  y = X, bf16.  x is of `dtype`.  Singular values of x
+ *                       above 0.0025 |x| come out between 0.68 and 1.21 after 5 steps; their directions stay.  A matrix of
+ *                       zeros gives zeros; an infinity or a NaN in x makes NaN of the whole of y.
+ *   mxc_muon_update:    with gs = grad_scale*g:  m' = momentum*m + gs,  u = gs + momentum*m' (nesterov == 1) or m' (0),
+ *                       w' = w*(1 - lr*wd) - lr*f*O,  O = u made orthogonal as above, not rounded between;  f = rms*sqrt(max(rows, cols)), with which
+ *                       the step's values have a root mean square of about lr*rms (0.2 is usual beside AdamW's learning rates), or with rms == 0
+ *                       f = sqrt(max(1, rows/cols)).  w: fp32 master weights, in place; m: fp32, in place, zeros at the start; g of grad_dtype;
+ *                       w_bf16: NULL, or for each matrix where w' goes rounded to bf16.
+ * Arithmetic: the products multiply values of 11 bits (fp16 at fixed powers of two, which no entry of X, A or b A + c A A leaves, their singular values being
+ * bounded) with fp32 sums; the diagonals of A and of b A + c A A are kept apart in fp32, and X is carried with 22 bits.  O's error is about 1e-3 of its
+ * norm after 5 steps, in directions of any singular value.  |x| is summed in 64 bits.  Results are bit-identical from run to run and do not depend on the
+ * other matrices of a call.  No tensor may overlap another of the call.
+ * Workspace: mxc_orthogonalize_workspace_bytes, for both.  Errors, found before anything is launched: MXC_ERR_SHAPE (non-positive count or sides, more
+ * than MXC_ORTHOGONALIZE_MAX_COUNT matrices, sides above MXC_ORTHOGONALIZE_MAX_SIDE), MXC_ERR_UNSUPPORTED (dtype; steps outside 1..MXC_ORTHOGONALIZE_MAX_STEPS, past which the
+ * rounding of small directions grows; momentum outside [0, 1), negative rms, nesterov, factors that are not finite), MXC_ERR_NULL, MXC_ERR_ALIGN (16 bytes),
+ * MXC_ERR_WORKSPACE, MXC_ERR_LAUNCH.
+ */
+enum { MXC_ORTHOGONALIZE_MAX_SIDE = 32768, MXC_ORTHOGONALIZE_MAX_STEPS = 6, MXC_ORTHOGONALIZE_MAX_COUNT = 4096 };
+int mxc_orthogonalize_workspace_bytes(int count, const int *rows, const int *cols, size_t *out_bytes);
+int mxc_orthogonalize(int count, const int *rows, const int *cols, const void *const *x, int dtype, int steps, void *const *y,
+                      void *workspace, size_t workspace_bytes, void *hip_stream);
+int mxc_muon_update(int count, const int *rows, const int *cols, float *const *w, const void *const *g, int grad_dtype, float *const *m,
+                    void *const *w_bf16, double lr, double momentum, int nesterov, double wd, double rms, double grad_scale, int steps,
+                    void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
  * Workspace size in bytes that `pass` (MXC_FWD / MXC_BWD_DATA / MXC_BWD_WEIGHT)
  * needs for these arguments, written to *out_bytes (a HOST pointer).  Touches
  * no GPU state.

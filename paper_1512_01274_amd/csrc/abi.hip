@@ -1192,6 +1192,139 @@ int mxc_adamw8_update(int count, const size_t *sizes, void *const *w, const void
     return adamw_update(count, sizes, w, g, grad_dtype, state, nullptr, w_bf16, f, seed, (hipStream_t)hip_stream);
 }
 
+static int embedding_check(int N, int V, int C, int dtype)
+{
+    if (N <= 0 || V <= 0 || C <= 0 || N > MXC_EMBEDDING_MAX_N || V > MXC_EMBEDDING_MAX_V || C > MXC_EMBEDDING_MAX_C) return MXC_ERR_SHAPE;
+    return dtype != MXC_F32 && dtype != MXC_BF16 ? MXC_ERR_UNSUPPORTED : MXC_OK;
+}
+
+int mxc_embedding_fwd(int N, int V, int C, int dtype, const int *tokens, const void *w, float scale, void *y, void *hip_stream)
+{
+    MXC_TRY(embedding_check(N, V, C, dtype));
+    if (!std::isfinite(scale)) return MXC_ERR_UNSUPPORTED;
+    if (!tokens || !w || !y) return MXC_ERR_NULL;
+    if (misaligned4(tokens) || misaligned(w) || misaligned(y)) return MXC_ERR_ALIGN;
+    return embedding_fwd(N, V, C, dtype, tokens, w, scale, y, (hipStream_t)hip_stream);
+}
+
+int mxc_embedding_workspace_bytes(int N, int V, int C, int dtype, size_t *out_bytes)
+{
+    if (!out_bytes) return MXC_ERR_NULL;
+    MXC_TRY(embedding_check(N, V, C, dtype));
+    *out_bytes = embedding_workspace(N, V, C);
+    return MXC_OK;
+}
+
+int mxc_embedding_bwd(int N, int V, int C, int dtype, const int *tokens, const void *dy, float scale, int accumulate, float *dw,
+                      void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    MXC_TRY(embedding_check(N, V, C, dtype));
+    if (!std::isfinite(scale) || (accumulate != 0 && accumulate != 1)) return MXC_ERR_UNSUPPORTED;
+    if (!tokens || !dy || !dw) return MXC_ERR_NULL;
+    if (misaligned4(tokens) || misaligned(dy) || misaligned(dw) || misaligned(workspace)) return MXC_ERR_ALIGN;
+    const size_t need = embedding_workspace(N, V, C);
+    if (need && (!workspace || workspace_bytes < need)) return MXC_ERR_WORKSPACE;
+    return embedding_bwd(N, V, C, dtype, tokens, dy, scale, accumulate, dw, workspace, (hipStream_t)hip_stream);
+}
+
+static int layernorm_check(int N, int C, int dtype)
+{
+    if (N <= 0 || C <= 0 || C > MXC_LAYERNORM_MAX_C) return MXC_ERR_SHAPE;
+    return dtype != MXC_F32 && dtype != MXC_BF16 ? MXC_ERR_UNSUPPORTED : MXC_OK;
+}
+
+int mxc_layernorm_fwd(int N, int C, int dtype, const void *x, const float *gamma, const float *beta, float eps, void *y, float *stats, void *hip_stream)
+{
+    MXC_TRY(layernorm_check(N, C, dtype));
+    if (!(eps >= 1.17549435e-38f && std::isfinite(eps))) return MXC_ERR_UNSUPPORTED;
+    if (!x || !y) return MXC_ERR_NULL;
+    if (misaligned(x) || misaligned(y) || misaligned(gamma) || misaligned(beta) || misaligned4(stats)) return MXC_ERR_ALIGN;
+    return layernorm_fwd(N, C, dtype, x, gamma, beta, eps, y, stats, (hipStream_t)hip_stream);
+}
+
+int mxc_layernorm_workspace_bytes(int N, int C, int dtype, size_t *out_bytes)
+{
+    if (!out_bytes) return MXC_ERR_NULL;
+    MXC_TRY(layernorm_check(N, C, dtype));
+    *out_bytes = layernorm_workspace(N, C, dtype);
+    return MXC_OK;
+}
+
+int mxc_layernorm_bwd(int N, int C, int dtype, const void *x, const float *gamma, const float *stats, const void *dy, void *dx, float *dgamma, float *dbeta,
+                      void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    MXC_TRY(layernorm_check(N, C, dtype));
+    if (!x || !stats || !dy || !dx) return MXC_ERR_NULL;
+    if (misaligned(x) || misaligned(gamma) || misaligned4(stats) || misaligned(dy) || misaligned(dx) || misaligned(dgamma) || misaligned(dbeta) || misaligned(workspace))
+        return MXC_ERR_ALIGN;
+    const size_t need = layernorm_workspace(N, C, dtype);
+    if (need && (!workspace || workspace_bytes < need)) return MXC_ERR_WORKSPACE;
+    return layernorm_bwd(N, C, dtype, x, gamma, stats, dy, dx, dgamma, dbeta, workspace, (hipStream_t)hip_stream);
+}
+
+// sizes of the matrices; pointers: the arrays that may hold no null pointer for a matrix of any values
+static int matrices_check(int count, const int *rows, const int *cols)
+{
+    if (count <= 0 || count > MXC_ORTHOGONALIZE_MAX_COUNT) return MXC_ERR_SHAPE;
+    if (!rows || !cols) return MXC_ERR_NULL;
+    for (int i = 0; i < count; ++i)
+        if (rows[i] <= 0 || cols[i] <= 0 || rows[i] > MXC_ORTHOGONALIZE_MAX_SIDE || cols[i] > MXC_ORTHOGONALIZE_MAX_SIDE) return MXC_ERR_SHAPE;
+    return MXC_OK;
+}
+static int pointers_check(int count, const void *const *const *tensors, int kinds)
+{
+    for (int k = 0; k < kinds; ++k)
+        if (!tensors[k]) return MXC_ERR_NULL;
+    for (int k = 0; k < kinds; ++k)
+        for (int i = 0; i < count; ++i)
+            if (!tensors[k][i]) return MXC_ERR_NULL;
+    for (int k = 0; k < kinds; ++k)
+        for (int i = 0; i < count; ++i)
+            if (misaligned(tensors[k][i])) return MXC_ERR_ALIGN;
+    return MXC_OK;
+}
+
+int mxc_orthogonalize_workspace_bytes(int count, const int *rows, const int *cols, size_t *out_bytes)
+{
+    if (!out_bytes) return MXC_ERR_NULL;
+    MXC_TRY(matrices_check(count, rows, cols));
+    *out_bytes = muon_workspace(count, rows, cols);
+    return MXC_OK;
+}
+
+int mxc_orthogonalize(int count, const int *rows, const int *cols, const void *const *x, int dtype, int steps, void *const *y, void *workspace, size_t workspace_bytes,
+                      void *hip_stream)
+{
+    MXC_TRY(matrices_check(count, rows, cols));
+    if ((dtype != MXC_F32 && dtype != MXC_BF16) || steps < 1 || steps > MXC_ORTHOGONALIZE_MAX_STEPS) return MXC_ERR_UNSUPPORTED;
+    const void *const *const tensors[] = {x, y};
+    MXC_TRY(pointers_check(count, tensors, 2));
+    if (misaligned(workspace)) return MXC_ERR_ALIGN;
+    if (!workspace || workspace_bytes < muon_workspace(count, rows, cols)) return MXC_ERR_WORKSPACE;
+    MuonArgs a = {};
+    a.count = count; a.rows = rows; a.cols = cols; a.u = x; a.dtype = dtype; a.y = y; a.steps = steps;
+    return muon_run(a, workspace, (hipStream_t)hip_stream);
+}
+
+int mxc_muon_update(int count, const int *rows, const int *cols, float *const *w, const void *const *g, int grad_dtype, float *const *m, void *const *w_bf16,
+                    double lr, double momentum, int nesterov, double wd, double rms, double grad_scale, int steps, void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    MXC_TRY(matrices_check(count, rows, cols));
+    if ((grad_dtype != MXC_F32 && grad_dtype != MXC_BF16) || steps < 1 || steps > MXC_ORTHOGONALIZE_MAX_STEPS || (nesterov != 0 && nesterov != 1)) return MXC_ERR_UNSUPPORTED;
+    if (!(momentum >= 0.0 && momentum < 1.0 && rms >= 0.0)) return MXC_ERR_UNSUPPORTED;
+    // (the largest factor that a matrix's sides give is 256 * rms, or 182 where rms is 0)
+    if (!std::isfinite((float)momentum) || !std::isfinite((float)grad_scale) || !std::isfinite((float)(1.0 - lr * wd)) || !std::isfinite((float)(lr * (rms + 1.0) * 256.0)))
+        return MXC_ERR_UNSUPPORTED;
+    const void *const *const tensors[] = {(const void *const *)w, g, (const void *const *)m, (const void *const *)w_bf16};
+    MXC_TRY(pointers_check(count, tensors, w_bf16 ? 4 : 3));
+    if (misaligned(workspace)) return MXC_ERR_ALIGN;
+    if (!workspace || workspace_bytes < muon_workspace(count, rows, cols)) return MXC_ERR_WORKSPACE;
+    MuonArgs a = {};
+    a.count = count; a.rows = rows; a.cols = cols; a.u = g; a.dtype = grad_dtype; a.w = w; a.m = m; a.w_bf16 = w_bf16;
+    a.steps = steps; a.nesterov = nesterov; a.momentum = (float)momentum; a.grad_scale = (float)grad_scale; a.keep = (float)(1.0 - lr * wd); a.lr = lr; a.rms = rms;
+    return muon_run(a, workspace, (hipStream_t)hip_stream);
+}
+
 int mxc_conv2d_workspace_bytes(int pass, int N, int C, int H, int W, int K, int R, int S, int stride, int pad,
                                int dtype, int layout, size_t *out_bytes)
 {

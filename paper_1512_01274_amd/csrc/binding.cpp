@@ -7,6 +7,7 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <climits>
 #include <vector>
 
 #include "../../include/mxc.h"
@@ -338,6 +339,51 @@ WRAP(mxc_adamw8_update, 12, N_("w", "g", "state", "w_bf16", "lr", "beta1", "beta
      if (PyErr_Occurred()) return nullptr;
      STREAM(12);
      RUN(mxc_adamw8_update((int)numel.size(), numel.data(), LIST(w), LIST(g), gt, LIST(state), LIST(wb), lr, b1, b2, eps, wd, gs, step, (unsigned)seed, st));)
+WRAP(mxc_embedding_fwd, 8, N_("N", "V", "C", "dtype", "tokens", "w", "scale", "y", "stream"),
+     INTS(4); PTR_OF(tokens, 4, Int, count(d[0])); PTR_IN(w, 5, d[3], count(d[1], d[2])); FLOAT(scale, 6); PTR_IN(y, 7, d[3], count(d[0], d[2])); STREAM(8);
+     RUN(mxc_embedding_fwd(d[0], d[1], d[2], d[3], (const int *)tokens, w, (float)scale, y, st));)
+WRAP(mxc_embedding_bwd, 9, N_("N", "V", "C", "dtype", "tokens", "dy", "scale", "accumulate", "dw", "workspace", "stream"),
+     INTS(4); PTR_OF(tokens, 4, Int, count(d[0])); PTR_IN(dy, 5, d[3], count(d[0], d[2])); FLOAT(scale, 6); BOOL(accumulate, 7); PTR_OF(dw, 8, Float, count(d[1], d[2])); BUF(ws, 9);
+     STREAM(10); RUN(mxc_embedding_bwd(d[0], d[1], d[2], d[3], (const int *)tokens, dy, (float)scale, accumulate, (float *)dw, ws, ws_n, st));)
+WRAP(mxc_layernorm_fwd, 9, N_("N", "C", "dtype", "x", "gamma", "beta", "eps", "y", "stats", "stream"),
+     INTS(3); PTR_IN(x, 3, d[2], count(d[0], d[1])); PTR_OF(gamma, 4, Float, count(d[1])); PTR_OF(beta, 5, Float, count(d[1])); FLOAT(eps, 6); PTR_IN(y, 7, d[2], count(d[0], d[1]));
+     PTR_OF(stats, 8, Float, 2 * count(d[0])); STREAM(9);
+     RUN(mxc_layernorm_fwd(d[0], d[1], d[2], x, (const float *)gamma, (const float *)beta, (float)eps, y, (float *)stats, st));)
+WRAP(mxc_layernorm_bwd, 10, N_("N", "C", "dtype", "x", "gamma", "stats", "dy", "dx", "dgamma", "dbeta", "workspace", "stream"),
+     INTS(3); PTR_IN(x, 3, d[2], count(d[0], d[1])); PTR_OF(gamma, 4, Float, count(d[1])); PTR_OF(stats, 5, Float, 2 * count(d[0])); PTR_IN(dy, 6, d[2], count(d[0], d[1]));
+     PTR_IN(dx, 7, d[2], count(d[0], d[1])); PTR_OF(dgamma, 8, Float, count(d[1])); PTR_OF(dbeta, 9, Float, count(d[1])); BUF(ws, 10); STREAM(11);
+     RUN(mxc_layernorm_bwd(d[0], d[1], d[2], x, (const float *)gamma, (const float *)stats, dy, dx, (float *)dgamma, (float *)dbeta, ws, ws_n, st));)
+
+// rows and columns of the matrices in argument 0: a tensor of more dimensions is the matrix of its first by the rest (a filter's outputs by its taps)
+bool to_sides(PyObject *o, std::vector<int> *rows, std::vector<int> *cols)
+{
+    const Py_ssize_t n = o && (PyList_Check(o) || PyTuple_Check(o)) ? PySequence_Fast_GET_SIZE(o) : 0;
+    for (Py_ssize_t i = 0; i < n; ++i) {
+        const at::Tensor &t = THPVariable_Unpack(PySequence_Fast_GET_ITEM(o, i));        // (to_ptrs has seen that it is one)
+        if (t.dim() < 2) {
+            PyErr_Format(PyExc_ValueError, "[%zd]: a matrix has two dimensions or more, got %d", i, (int)t.dim());
+            return false;
+        }
+        long long r = t.size(0), c = 1;
+        for (int64_t k = 1; k < t.dim(); ++k) c *= t.size(k);
+        if (r > INT_MAX || c > INT_MAX) {
+            PyErr_Format(PyExc_OverflowError, "[%zd]: %lld x %lld does not fit an int", i, r, c);
+            return false;
+        }
+        rows->push_back((int)r);
+        cols->push_back((int)c);
+    }
+    return true;
+}
+#define SIDES std::vector<int> rows, cols; if (!to_sides(a.v[0], &rows, &cols)) return nullptr
+WRAP(mxc_orthogonalize, 3, N_("x", "steps", "y", "workspace", "stream"),
+     std::vector<size_t> numel; PTRS(g, 0, Undefined); SIDES; INT(steps, 1); PTRS(y, 2, BFloat16); GRAD_TYPE; BUF(ws, 3); STREAM(4);
+     RUN(mxc_orthogonalize((int)rows.size(), rows.data(), cols.data(), LIST(g), gt, steps, LIST(y), ws, ws_n, st));)
+WRAP(mxc_muon_update, 11, N_("w", "g", "m", "w_bf16", "lr", "momentum", "nesterov", "wd", "rms", "grad_scale", "steps", "workspace", "stream"),
+     std::vector<size_t> numel; PTRS(w, 0, Float); SIDES; PTRS(g, 1, Undefined); PTRS(m, 2, Float); PTRS(wb, 3, BFloat16); GRAD_TYPE;
+     FLOAT(lr, 4); FLOAT(mom, 5); BOOL(nesterov, 6); FLOAT(wd, 7); FLOAT(rms, 8); FLOAT(gs, 9); INT(steps, 10); BUF(ws, 11); STREAM(12);
+     RUN(mxc_muon_update((int)rows.size(), rows.data(), cols.data(), (float *const *)LIST(w), LIST(g), gt, (float *const *)LIST(m), LIST(wb), lr, mom, nesterov, wd, rms, gs, steps,
+                         ws, ws_n, st));)
 WRAP(mxc_layout_convert, 9, N_("n", "c", "h", "w", "dtype", "src_layout", "dst_layout", "src", "dst", "stream"),
      INTS(7); PTR(src, 7); PTR(dst, 8); STREAM(9);
      RUN(mxc_layout_convert(d[0], d[1], d[2], d[3], d[4], d[5], d[6], src, dst, st));)
@@ -370,6 +416,37 @@ PyObject *py_mxc_conv2d_workspace_bytes(PyObject *, PyObject *const *args, Py_ss
         return rc == MXC_OK ? PyLong_FromSize_t(bytes) : done(rc);                                                      \
     }
 SIZE_QUERY(mxc_logprob_workspace_bytes, 4, mxc_logprob_workspace_bytes(d[0], d[1], d[2], d[3], &bytes), "N", "K", "dtype", "top")
+SIZE_QUERY(mxc_embedding_workspace_bytes, 4, mxc_embedding_workspace_bytes(d[0], d[1], d[2], d[3], &bytes), "N", "V", "C", "dtype")
+SIZE_QUERY(mxc_layernorm_workspace_bytes, 3, mxc_layernorm_workspace_bytes(d[0], d[1], d[2], &bytes), "N", "C", "dtype")
+
+// a list (or tuple) of integers
+bool to_int_list(PyObject *o, const char *name, std::vector<int> *out)
+{
+    if (!PyList_Check(o) && !PyTuple_Check(o)) {
+        PyErr_Format(PyExc_TypeError, "%s: expected a list of integers, got %s", name, Py_TYPE(o)->tp_name);
+        return false;
+    }
+    out->resize((size_t)PySequence_Fast_GET_SIZE(o));
+    for (size_t i = 0; i < out->size(); ++i)
+        if (!to_int(PySequence_Fast_GET_ITEM(o, (Py_ssize_t)i), &(*out)[i])) return false;
+    return true;
+}
+PyObject *py_mxc_orthogonalize_workspace_bytes(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObject *kw)
+{
+    HANDLE_TH_ERRORS
+    static const char *const names[] = {"rows", "cols"};
+    Args a("mxc_orthogonalize_workspace_bytes", names, 2, 2, args, nargs, kw);
+    std::vector<int> rows, cols;
+    if (!a.ok || !to_int_list(a.v[0], names[0], &rows) || !to_int_list(a.v[1], names[1], &cols)) return nullptr;
+    if (rows.size() != cols.size()) {
+        PyErr_Format(PyExc_ValueError, "%zu rows and %zu cols", rows.size(), cols.size());
+        return nullptr;
+    }
+    size_t bytes = 0;
+    const int rc = mxc_orthogonalize_workspace_bytes((int)rows.size(), rows.data(), cols.data(), &bytes);
+    return rc == MXC_OK ? PyLong_FromSize_t(bytes) : done(rc);
+    END_HANDLE_TH_ERRORS
+}
 SIZE_QUERY(mxc_mxfp4_fc_workspace_bytes, 4, mxc_mxfp4_fc_workspace_bytes(d[0], d[1], d[2], d[3], &bytes), "N", "C", "K", "dtype")
 
 PyObject *py_mxc_adamw8_state_bytes(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObject *kw)
@@ -412,6 +489,8 @@ PyMethodDef methods[] = {
     ENTRY(mxc_logprob_workspace_bytes), ENTRY(mxc_logprob_fwd), ENTRY(mxc_logprob_bwd), ENTRY(mxc_logprob_fwd_bwd),
     ENTRY(mxc_mxfp4_quantize), ENTRY(mxc_mxfp4_dequantize), ENTRY(mxc_mxfp4_fc_workspace_bytes), ENTRY(mxc_mxfp4_fc_fwd),
     ENTRY(mxc_adamw_update), ENTRY(mxc_adamw8_state_bytes), ENTRY(mxc_adamw8_update),
+    ENTRY(mxc_embedding_fwd), ENTRY(mxc_embedding_workspace_bytes), ENTRY(mxc_embedding_bwd), ENTRY(mxc_layernorm_fwd), ENTRY(mxc_layernorm_workspace_bytes),
+    ENTRY(mxc_layernorm_bwd), ENTRY(mxc_orthogonalize_workspace_bytes), ENTRY(mxc_orthogonalize), ENTRY(mxc_muon_update),
     {"set_hooks", (PyCFunction)(void *)py_set_hooks, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", "Call path of the mxc binding", -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -314,6 +314,30 @@ int softmax_xent_bwd(int N, int K, int dtype, const void *p, const int *labels, 
 // one launch holds fewer than 2^32 threads
 inline bool one_launch(unsigned long long workgroups, int threads) { return workgroups * threads <= 0xFFFFFFFFull; }
 
+// ---- embedding.hip, layernorm.hip, muon.hip: the layers around a model's products and the update of its matrices (see there) ----
+int embedding_fwd(int N, int V, int C, int dtype, const int *tokens, const void *w, float scale, void *y, hipStream_t st);
+size_t embedding_workspace(int N, int V, int C);
+int embedding_bwd(int N, int V, int C, int dtype, const int *tokens, const void *dy, float scale, int add, float *dw, void *ws, hipStream_t st);
+int layernorm_fwd(int N, int C, int dtype, const void *x, const float *gamma, const float *beta, float eps, void *y, float *stats, hipStream_t st);
+size_t layernorm_workspace(int N, int C, int dtype);
+int layernorm_bwd(int N, int C, int dtype, const void *x, const float *gamma, const float *stats, const void *dy, void *dx, float *dgamma, float *dbeta, void *ws,
+                  hipStream_t st);
+// What becomes of a matrix made orthogonal: y = O, or with w a step of the update (u: the gradients; m, w in place)
+struct MuonArgs {
+    int count;
+    const int *rows, *cols;
+    const void *const *u;
+    int dtype;                      // of u
+    void *const *y;                 // bf16
+    float *const *w, *const *m;
+    void *const *w_bf16;
+    int steps, nesterov;
+    float momentum, grad_scale, keep;
+    double lr, rms;
+};
+size_t muon_workspace(int count, const int *rows, const int *cols);
+int muon_run(const MuonArgs &a, void *ws, hipStream_t st);
+
 // ---- logprob.hip: log probabilities, entropies, top tokens and their gradient -------------
 size_t logprob_workspace(int N, int K, int dtype, int top);
 struct LogprobArgs {

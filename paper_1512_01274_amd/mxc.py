@@ -20,6 +20,8 @@ MXC_BWD_DATA_FILTER, MXC_BWD_DATA_PREPARED, MXC_BWD_DATA_PREPARED_RELU, MXC_BWD_
 MXC_INPUT_PREPARED, MXC_FWD_PREPARED_INPUT, MXC_BWD_WEIGHT_PREPARED_INPUT, MXC_BWD_WEIGHT_PREPARED_INPUT_BF16 = 9, 10, 11, 12
 MXC_FWD_TRANSFORM = 13
 MXC_LOGPROB_MAX_TOP, MXC_LOGPROB_MAX_K, MXC_MXFP4_FC_MAX_C, MXC_ADAMW_GROUP, MXC_ADAMW8_GROUP = 64, 1 << 30, 1 << 23, 72, 88
+MXC_EMBEDDING_MAX_N, MXC_EMBEDDING_MAX_V, MXC_EMBEDDING_MAX_C, MXC_LAYERNORM_MAX_C = 1 << 23, 1 << 23, 1 << 20, 1 << 20
+MXC_ORTHOGONALIZE_MAX_SIDE, MXC_ORTHOGONALIZE_MAX_STEPS, MXC_ORTHOGONALIZE_MAX_COUNT = 32768, 6, 4096
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libmxc.so")
 if not os.path.exists(LIB_PATH):
@@ -76,6 +78,7 @@ _lib.mxc_softmax_xent_bwd.restype = _I
 _F = ctypes.c_float
 _lib.mxc_sgd_update.argtypes = [_SZ, _VP, _VP, _VP, _VP, _F, _F, _F, _VP]
 _lib.mxc_sgd_update.restype = _I
+_PI = ctypes.POINTER(_I)
 _D, _LL, _U, _PSZ, _VPP = ctypes.c_double, ctypes.c_longlong, ctypes.c_uint, ctypes.POINTER(_SZ), ctypes.POINTER(_VP)
 for _name, _args in (
         ("mxc_logprob_workspace_bytes", [_I] * 4 + [_PSZ]),
@@ -88,7 +91,16 @@ for _name, _args in (
         ("mxc_mxfp4_fc_fwd", [_I] * 4 + [_VP] * 4 + [_I, _VP, _VP, _SZ, _VP]),
         ("mxc_adamw_update", [_I, _PSZ, _VPP, _VPP, _I, _VPP, _VPP, _VPP] + [_D] * 6 + [_LL, _VP]),
         ("mxc_adamw8_state_bytes", [_SZ, _PSZ]),
-        ("mxc_adamw8_update", [_I, _PSZ, _VPP, _VPP, _I, _VPP, _VPP] + [_D] * 6 + [_LL, _U, _VP])):
+        ("mxc_adamw8_update", [_I, _PSZ, _VPP, _VPP, _I, _VPP, _VPP] + [_D] * 6 + [_LL, _U, _VP]),
+        ("mxc_embedding_fwd", [_I] * 4 + [_VP, _VP, _F, _VP, _VP]),
+        ("mxc_embedding_workspace_bytes", [_I] * 4 + [_PSZ]),
+        ("mxc_embedding_bwd", [_I] * 4 + [_VP, _VP, _F, _I, _VP, _VP, _SZ, _VP]),
+        ("mxc_layernorm_fwd", [_I] * 3 + [_VP] * 3 + [_F] + [_VP] * 3),
+        ("mxc_layernorm_workspace_bytes", [_I] * 3 + [_PSZ]),
+        ("mxc_layernorm_bwd", [_I] * 3 + [_VP] * 8 + [_SZ, _VP]),
+        ("mxc_orthogonalize_workspace_bytes", [_I, _PI, _PI, _PSZ]),
+        ("mxc_orthogonalize", [_I, _PI, _PI, _VPP, _I, _I, _VPP, _VP, _SZ, _VP]),
+        ("mxc_muon_update", [_I, _PI, _PI, _VPP, _VPP, _I, _VPP, _VPP, _D, _D, _I] + [_D] * 3 + [_I, _VP, _SZ, _VP])):
     getattr(_lib, _name).argtypes = _args
     getattr(_lib, _name).restype = _I
 _lib.mxc_probe_mfma.argtypes = [_I, _I, _VP, _SZ, ctypes.POINTER(ctypes.c_double), _VP]
@@ -174,7 +186,7 @@ def _stream(stream):
 
 # The entry points, with these arguments (workspace and stream may be left out; tensors may be None where the header
 # allows it).  They are built-in functions of the extension module (csrc/binding.cpp) and raise MxcError on a status.  The
-# log-probability, 4-bit and AdamW calls raise TypeError or ValueError for tensors of another element type or too few elements.
+# log-probability, 4-bit, AdamW, embedding, layer norm, orthogonalise and Muon calls raise TypeError or ValueError for tensors of another element type or too few elements.
 #
 #   mxc_conv2d_workspace_bytes(op, N, C, H, W, K, R, S, stride, pad, dtype, layout) -> int
 #   mxc_conv2d_fwd(N, C, H, W, K, R, S, stride, pad, dtype, layout, x, w, y, workspace=None, stream=None)
@@ -207,15 +219,26 @@ def _stream(stream):
 #   mxc_adamw_update(w, g, m, v, w_bf16, lr, beta1, beta2, eps, wd, grad_scale, step, stream=None)      lists of tensors, in place on w, m, v
 #   mxc_adamw8_state_bytes(n) -> int
 #   mxc_adamw8_update(w, g, state, w_bf16, lr, beta1, beta2, eps, wd, grad_scale, step, seed, stream=None)  state: lists of byte tensors
+#   mxc_embedding_fwd(N, V, C, dtype, tokens, w, scale, y, stream=None)
+#   mxc_embedding_workspace_bytes(N, V, C, dtype) -> int
+#   mxc_embedding_bwd(N, V, C, dtype, tokens, dy, scale, accumulate, dw, workspace=None, stream=None)
+#   mxc_layernorm_fwd(N, C, dtype, x, gamma, beta, eps, y, stats, stream=None)
+#   mxc_layernorm_workspace_bytes(N, C, dtype) -> int
+#   mxc_layernorm_bwd(N, C, dtype, x, gamma, stats, dy, dx, dgamma, dbeta, workspace=None, stream=None)
+#   mxc_orthogonalize_workspace_bytes(rows, cols) -> int            lists of integers
+#   mxc_orthogonalize(x, steps, y, workspace=None, stream=None)     lists of matrices; more dimensions than two: the first by the rest
+#   mxc_muon_update(w, g, m, w_bf16, lr, momentum, nesterov, wd, rms, grad_scale, steps, workspace=None, stream=None)    lists, in place on w, m
 #   mxc_layout_convert(n, c, h, w, dtype, src_layout, dst_layout, src, dst, stream=None)
 from paper_1512_01274_amd import _native  # noqa: E402
 from paper_1512_01274_amd._native import (  # noqa: E402,F401
-    mxc_adamw8_state_bytes, mxc_adamw8_update, mxc_adamw_update, mxc_bias_grad, mxc_conv2d_bwd_data, mxc_conv2d_bwd_data_prepare_filter, mxc_conv2d_bwd_data_prepared,
-    mxc_conv2d_bwd_data_relu, mxc_conv2d_bwd_weight, mxc_conv2d_bwd_weight_bf16, mxc_conv2d_bwd_weight_prepared_input,
-    mxc_conv2d_bwd_weight_static, mxc_conv2d_fwd, mxc_conv2d_fwd_bias_act, mxc_conv2d_fwd_prepared_input,
-    mxc_conv2d_fwd_transform, mxc_conv2d_prepare_input, mxc_conv2d_workspace_bytes, mxc_fc_bwd_data, mxc_fc_bwd_weight,
-    mxc_fc_fwd, mxc_layout_convert, mxc_logprob_bwd, mxc_logprob_fwd, mxc_logprob_fwd_bwd, mxc_logprob_workspace_bytes,
-    mxc_mxfp4_dequantize, mxc_mxfp4_fc_fwd, mxc_mxfp4_fc_workspace_bytes, mxc_mxfp4_quantize, mxc_sgd_update, mxc_softmax_fwd, mxc_softmax_xent_bwd)
+    mxc_adamw8_state_bytes, mxc_adamw8_update, mxc_adamw_update, mxc_bias_grad, mxc_conv2d_bwd_data, mxc_conv2d_bwd_data_prepare_filter,
+    mxc_conv2d_bwd_data_prepared, mxc_conv2d_bwd_data_relu, mxc_conv2d_bwd_weight, mxc_conv2d_bwd_weight_bf16, mxc_conv2d_bwd_weight_prepared_input,
+    mxc_conv2d_bwd_weight_static, mxc_conv2d_fwd, mxc_conv2d_fwd_bias_act, mxc_conv2d_fwd_prepared_input, mxc_conv2d_fwd_transform,
+    mxc_conv2d_prepare_input, mxc_conv2d_workspace_bytes, mxc_embedding_bwd, mxc_embedding_fwd, mxc_embedding_workspace_bytes, mxc_fc_bwd_data,
+    mxc_fc_bwd_weight, mxc_fc_fwd, mxc_layernorm_bwd, mxc_layernorm_fwd, mxc_layernorm_workspace_bytes, mxc_layout_convert, mxc_logprob_bwd,
+    mxc_logprob_fwd, mxc_logprob_fwd_bwd, mxc_logprob_workspace_bytes, mxc_muon_update, mxc_mxfp4_dequantize, mxc_mxfp4_fc_fwd,
+    mxc_mxfp4_fc_workspace_bytes, mxc_mxfp4_quantize, mxc_orthogonalize, mxc_orthogonalize_workspace_bytes, mxc_sgd_update, mxc_softmax_fwd,
+    mxc_softmax_xent_bwd)
 
 _native.set_hooks(MxcError, getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None),
                   lambda: torch.cuda.current_stream().cuda_stream)
