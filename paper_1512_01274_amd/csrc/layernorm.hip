@@ -1,7 +1,12 @@
 // Layer norm: y = (x - mean) * rstd * gamma + beta over rows of C values, rstd = 1 / sqrt(var + eps), and its gradient: with z = (x - mean) * rstd
 // and g = dy * gamma,
 //     dx = rstd * (g - sum(g) / C - z * sum(g * z) / C),   dgamma[c] = sum_n dy * z,   dbeta[c] = sum_n dy.
-// Memory bounds both: a row is read once (x, and dy), held in registers over its sums, and written once.
+// Memory bounds both: a row is read once (x, and dy), held in registers over its sums, and written once; rows that registers do not hold are read again.
+// Sums are fp32: a thread's values one after the other, then lanes and waves as a tree; squares are of differences from the mean.  16384 x 4096 bf16: forward 50 us,
+// 5.4 TB/s, gradient 78, 5.2 TB/s with the shares of dgamma and dbeta; rows of 4097 values, which begin at any element, 64.5 and 95.7; 128 x 1000 fp32 4.4 and 7.5, one launch
+// and two.
+#include <type_traits>
+
 #include "pieces.h"
 
 namespace mxc {
@@ -126,73 +131,380 @@ __global__ __launch_bounds__(256) void bwd_columns_kernel(int N, int C, int rows
         }
 }
 
-// dgamma and dbeta from the ranges' shares, added in their order: 64 columns by 16 lanes of ranges
-__global__ __launch_bounds__(1024) void bwd_join_kernel(int C, int ranges, const float *part, int pitch, float *dgamma, float *dbeta)
+// dgamma and dbeta from the ranges' shares: 32 columns by LANES lanes of ranges
+template <int LANES>
+__global__ __launch_bounds__(32 * LANES) void bwd_join_kernel(int C, int ranges, const float *part, int pitch, float *dgamma, float *dbeta)
 {
-    __shared__ float sum[16][64];
-    const int c = blockIdx.x * 64 + (threadIdx.x & 63), lane = threadIdx.x >> 6;
-    const float *from = part + (size_t)blockIdx.y * pitch + c;
+    __shared__ float sum[LANES][33];
+    const int col = threadIdx.x & 31, lane = threadIdx.x >> 5, c = blockIdx.x * 32 + col;
+    const float *from = part + (size_t)blockIdx.y * pitch + (c < C ? c : 0);
     float s = 0.f;
-    if (c < C)
-        for (int r = lane; r < ranges; r += 16) s += from[(size_t)r * 2 * pitch];
-    sum[lane][threadIdx.x & 63] = s;
+#pragma unroll 8
+    for (int r = lane; r < ranges; r += LANES) s += from[(size_t)r * 2 * pitch];
+    sum[lane][col] = s;
     __syncthreads();
     float *out = blockIdx.y ? dbeta : dgamma;
     if (lane || c >= C || !out) return;
-    s = sum[0][threadIdx.x];
-    for (int r = 1; r < 16; ++r) s += sum[r][threadIdx.x];
+    s = 0.f;
+#pragma unroll
+    for (int r = 0; r < LANES; ++r) s += sum[r][col];
     out[c] = s;
 }
 
+// ---- rows that a workgroup's registers hold ---------------------------------------------------------------------------------------
+//
+// A row is shared by TPR lanes of a wave (4 to 64), or with TPR = 0 by the workgroup's waves, PC pieces a lane; workgroups walk over the rows with the next
+// row's loads under way, the weights (and the sums of their gradients) staying in registers.
+
+struct __attribute__((packed, aligned(4))) Two { float x, y; };         // stats may begin at any float
+
+constexpr int ROW_NT = 256;                // workgroup of rows that lanes share
+template <int TPR> __device__ __forceinline__ int groups() { return TPR ? ROW_NT / (TPR ? TPR : 1) : 1; }
+
+// sums over a row's lanes; `part` alternates between calls, so that one barrier keeps them apart
+template <int TPR, int K>
+__device__ __forceinline__ void row_sums(float (&v)[K], float (*part)[16])
+{
+    if constexpr (TPR) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) v[k] = lane_sum<TPR>(v[k]);
+    } else {
+        const int waves = blockDim.x / 64;
+#pragma unroll
+        for (int k = 0; k < K; ++k) v[k] = lane_sum<64>(v[k]);
+        if ((threadIdx.x & 63) == 0)
+#pragma unroll
+            for (int k = 0; k < K; ++k) part[k][threadIdx.x >> 6] = v[k];
+        __syncthreads();
+        const int at = threadIdx.x & 15;
+#pragma unroll
+        for (int k = 0; k < K; ++k) v[k] = lane_sum<16>(at < waves ? part[k][at] : 0.f);
+    }
+}
+
+template <class T, int TPR, int PC, bool PAST>
+struct Lane {       // which pieces of a row are this lane's
+    static constexpr int VE = Piece<T>::VE, V = PC * VE;
+    int group, first, step;
+    __device__ __forceinline__ Lane()
+    {
+        const int lanes = TPR ? TPR : blockDim.x;
+        group = TPR ? threadIdx.x / lanes : 0;
+        first = (TPR ? threadIdx.x % lanes : threadIdx.x) * VE;
+        step = lanes * VE;
+    }
+    __device__ __forceinline__ int at(int k) const { return first + k * step; }
+    __device__ __forceinline__ void load(Piece<T> (&p)[PC], const T *row, int C) const
+    {
+#pragma unroll
+        for (int k = 0; k < PC; ++k) p[k] = begin_piece<PAST>(row, at(k), C);
+    }
+    __device__ __forceinline__ void settle(Piece<T> (&p)[PC], int C) const
+    {
+#pragma unroll
+        for (int k = 0; k < PC; ++k) settle_piece(p[k], at(k), C);
+    }
+    __device__ __forceinline__ void weights(float (&g)[V], const float *from, float without, int C) const
+    {
+#pragma unroll
+        for (int k = 0; k < PC; ++k)
+#pragma unroll
+            for (int i = 0; i < VE; i += 4) {
+                if (from) {
+                    const Piece<float> q = load_piece(from, at(k) + i, C);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) g[k * VE + i + j] = q.get(j);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) g[k * VE + i + j] = without;
+                }
+            }
+    }
+};
+
+template <class T, int TPR, int PC, bool PAST>
+__global__ __launch_bounds__(TPR ? ROW_NT : 1024) void fwd_rows_kernel(int N, int C, const T *x, const float *gamma, const float *beta, float eps, T *y, float *stats)
+{
+    constexpr int VE = Piece<T>::VE, V = PC * VE;
+    __shared__ float part[2][1][16];
+    const Lane<T, TPR, PC, PAST> l;
+    const int G = groups<TPR>();
+    float gm[V], bt[V];
+    l.weights(gm, gamma, 1.f, C);
+    l.weights(bt, beta, 0.f, C);
+    const float by = 1.f / (float)C;
+    long long n = (long long)blockIdx.x * G + l.group;
+    const long long step = (long long)gridDim.x * G, turns = (N - (long long)blockIdx.x * G + step - 1) / step;
+    Piece<T> p[PC], next[PC];
+    l.load(p, x + (size_t)(n < N ? n : 0) * C, C);
+    for (long long turn = 0; turn < turns; ++turn, n += step) {
+        const bool in = n < N;
+        if (turn + 1 < turns) l.load(next, x + (size_t)(n + step < N ? n + step : 0) * C, C);
+        l.settle(p, C);
+        float s[1] = {0.f};
+#pragma unroll
+        for (int k = 0; k < PC; ++k)
+#pragma unroll
+            for (int i = 0; i < VE; ++i) s[0] += p[k].get(i);       // (zeros past the row)
+        row_sums<TPR>(s, part[0]);
+        const float mean = s[0] * by;
+        s[0] = 0.f;
+#pragma unroll
+        for (int k = 0; k < PC; ++k)
+#pragma unroll
+            for (int i = 0; i < VE; ++i) {
+                const float d = p[k].get(i) - mean;
+                s[0] += l.at(k) + i < C ? d * d : 0.f;
+            }
+        row_sums<TPR>(s, part[1]);
+        const float rstd = 1.f / sqrtf(s[0] * by + eps);
+#pragma unroll
+        for (int k = 0; k < PC; ++k) held(p[k].raw);
+        if (in) {
+            if (stats && l.first == 0) *reinterpret_cast<Two *>(stats + 2 * n) = Two{mean, rstd};
+#pragma unroll
+            for (int k = 0; k < PC; ++k) {
+                float v[VE];
+#pragma unroll
+                for (int i = 0; i < VE; ++i) v[i] = (p[k].get(i) - mean) * rstd * gm[k * VE + i] + bt[k * VE + i];
+                Piece<T> r;
+                r.set(v);
+                store_piece<PAST>(y + (size_t)n * C, l.at(k), C, r);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < PC; ++k) p[k] = next[k];
+    }
+}
+
+// AHEAD: with the next row's loads under way; rows of more than 8 waves have no registers for it
+template <class T, int TPR, int PC, bool AHEAD, bool PAST>
+__global__ __launch_bounds__(TPR ? ROW_NT : AHEAD && PC > 1 ? 512 : 1024) void bwd_rows_kernel(int N, int C, const T *x, const float *gamma, const float *stats, const T *dy, T *dx, float *parts, int pitch)
+{
+    constexpr int VE = Piece<T>::VE, V = PC * VE;
+    __shared__ float part[2][2][16];
+    __shared__ float4 meet[TPR ? ROW_NT : 1];
+    const Lane<T, TPR, PC, PAST> l;
+    const int G = groups<TPR>();
+    float gm[V], ag[V], ab[V];
+    if (AHEAD) l.weights(gm, gamma, 1.f, C);
+#pragma unroll
+    for (int i = 0; i < V; ++i) ag[i] = ab[i] = 0.f;
+    const float by = 1.f / (float)C;
+    long long n = (long long)blockIdx.x * G + l.group;
+    const long long step = (long long)gridDim.x * G, turns = (N - (long long)blockIdx.x * G + step - 1) / step;
+    Piece<T> p[PC], q[PC], p1[PC], q1[PC];
+    auto fetch = [&](Piece<T> (&a)[PC], Piece<T> (&b)[PC], long long row) __attribute__((always_inline)) {
+        l.load(a, x + (size_t)row * C, C);
+        l.load(b, dy + (size_t)row * C, C);
+    };
+    fetch(p, q, n < N ? n : 0);
+    Two st = *reinterpret_cast<const Two *>(stats + 2 * (n < N ? n : 0)), st1 = st;
+    for (long long turn = 0; turn < turns; ++turn, n += step) {
+        const bool in = n < N;
+        const long long m = n + step < N ? n + step : 0;
+        if (AHEAD && turn + 1 < turns) {
+            fetch(p1, q1, m);
+            st1 = *reinterpret_cast<const Two *>(stats + 2 * m);
+        }
+        if (!AHEAD) l.weights(gm, gamma, 1.f, C);
+        l.settle(p, C);
+        l.settle(q, C);
+        const float mean = st.x, rstd = st.y;
+        float s[2] = {0.f, 0.f};
+        // (past the row g is zero, and z a number or what makes NaN of the row anyway)
+#pragma unroll
+        for (int k = 0; k < PC; ++k)
+#pragma unroll
+            for (int i = 0; i < VE; ++i) {
+                const float g = q[k].get(i) * gm[k * VE + i];
+                s[0] += g;
+                s[1] += g * ((p[k].get(i) - mean) * rstd);
+            }
+        row_sums<TPR>(s, part[turn & 1]);
+#pragma unroll
+        for (int k = 0; k < PC; ++k) {
+            held(p[k].raw);
+            held(q[k].raw);
+        }
+        const float s1 = s[0] * by, s2 = s[1] * by;
+        if (in) {
+#pragma unroll
+            for (int k = 0; k < PC; ++k) {
+                float v[VE];
+#pragma unroll
+                for (int i = 0; i < VE; ++i) {
+                    const float d = q[k].get(i), z = (p[k].get(i) - mean) * rstd;
+                    v[i] = (d * gm[k * VE + i] - s1 - z * s2) * rstd;
+                    ag[k * VE + i] += d * z;
+                    ab[k * VE + i] += d;
+                }
+                Piece<T> r;
+                r.set(v);
+                store_piece<PAST>(dx + (size_t)n * C, l.at(k), C, r);
+            }
+        }
+        if (AHEAD) {
+#pragma unroll
+            for (int k = 0; k < PC; ++k) {
+                p[k] = p1[k];
+                q[k] = q1[k];
+            }
+            st = st1;
+        } else if (turn + 1 < turns) {
+            fetch(p, q, m);
+            st = *reinterpret_cast<const Two *>(stats + 2 * m);
+        }
+    }
+    float *to = parts + (size_t)blockIdx.x * 2 * pitch;
+#pragma unroll
+    for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int k = 0; k < V; k += 4) {
+            const float *a = half ? ab + k : ag + k;
+            float4 f = make_float4(a[0], a[1], a[2], a[3]);
+            if constexpr (TPR != 0) {          // the rows that share the workgroup meet
+                __syncthreads();
+                meet[threadIdx.x] = f;
+                __syncthreads();
+                for (int r = 1; r < G; ++r) {
+                    const float4 o = meet[(threadIdx.x + r * TPR) % ROW_NT];
+                    f.x += o.x; f.y += o.y; f.z += o.z; f.w += o.w;
+                }
+            }
+            const int c = l.at(k / VE) + k % VE;
+            if (l.group == 0 && c < C) *reinterpret_cast<float4 *>(to + (size_t)half * pitch + c) = f;      // (pitch is a multiple of 4)
+        }
+}
+
+int launched() { return hipGetLastError() == hipSuccess ? MXC_OK : MXC_ERR_LAUNCH; }
+// whether a call moves what the 256 MB of the last cache do not hold: then its rows go past the caches.  us, us past them: forward 16384 x 4096 bf16 52.8, 49.6; 4096 x 2048 fp32
+// 12.7, 14.2; gradient 16384 x 4096 bf16 81.0, 77.8; 1024 x 4096 13.2, 14.5
+bool past_caches(int N, int C, int tensors, int dtype) { return (unsigned long long)N * C * tensors * elem_size(dtype) >= 256ull << 20; }
+
+// How a row is shared: TPR lanes of PC pieces (TPR = 0: `waves` waves); PC = 0: a row that registers do not hold.  More pieces a lane only where a row would need more than
+// ten waves (16383 x 4097 bf16: 9 waves of one piece 95 us the gradient, 5 of two, with 134 registers, 147; 8192 x 4096 fp32: 16 of one 90, 8 of two 78.5)
+struct Share {
+    int TPR, PC, waves;
+};
+Share share_of(int C, int dtype)
+{
+    const int VE = dtype == MXC_BF16 ? 8 : 4, most = dtype == MXC_BF16 ? 2 : 4;
+    const int P = (C + VE - 1) / VE;
+    for (int lanes = 4; lanes <= 64; lanes *= 2)
+        if (P <= lanes) return {lanes, 1, 1};
+    for (int pc = 1; pc <= most; pc *= 2) {
+        const int waves = (P + 64 * pc - 1) / (64 * pc);
+        if (waves <= 10 || (pc == most && waves <= 16)) return {0, pc, waves};
+    }
+    return {0, 0, 0};
+}
+
+template <class T, class F>
+int with_share(const Share &h, F &&f)
+{
+    switch (h.TPR) {
+    case 4: return f(std::integral_constant<int, 4>{}, std::integral_constant<int, 1>{});
+    case 8: return f(std::integral_constant<int, 8>{}, std::integral_constant<int, 1>{});
+    case 16: return f(std::integral_constant<int, 16>{}, std::integral_constant<int, 1>{});
+    case 32: return f(std::integral_constant<int, 32>{}, std::integral_constant<int, 1>{});
+    case 64: return f(std::integral_constant<int, 64>{}, std::integral_constant<int, 1>{});
+    default: break;
+    }
+    if (h.PC == 1) return f(std::integral_constant<int, 0>{}, std::integral_constant<int, 1>{});
+    if (h.PC == 2) return f(std::integral_constant<int, 0>{}, std::integral_constant<int, 2>{});
+    if constexpr (sizeof(T) == 4) return f(std::integral_constant<int, 0>{}, std::integral_constant<int, 4>{});
+    return MXC_ERR_LAUNCH;
+}
+
 struct BwdPlan {
-    int rows, ranges, pitch;
+    Share h;
+    int workgroups;                     // of rows in registers
+    int rows, ranges, pitch;            // ranges: shares of dgamma and dbeta
     size_t part_bytes, sums_bytes;
 };
 BwdPlan bwd_plan(int N, int C, int dtype)
 {
-    BwdPlan q;
-    const int VE = dtype == MXC_BF16 ? 8 : 4;
-    const long long columns = (C + 256ll * VE - 1) / (256ll * VE);
-    const long long want = columns >= 1024 ? 1 : 1024 / columns;          // ranges of rows, for about four workgroups a compute unit
-    q.rows = (int)((N + want - 1) / want);
-    q.ranges = (N + q.rows - 1) / q.rows;
+    BwdPlan q = {};
+    q.h = share_of(C, dtype);
     q.pitch = (int)align_up(C, 4);
+    if (q.h.PC) {
+        // 18 waves a compute unit (8: 105 us at 16384 x 4096 bf16, 16: 79.5; of rows that a wave shares 24 are no better), and few workgroups where there are few rows, for
+        // each leaves a share that is read again: 512 x 4096 with 512 workgroups 12.8, with 256 11.0
+        const int G = q.h.TPR ? ROW_NT / q.h.TPR : 1, waves = q.h.TPR ? ROW_NT / 64 : q.h.waves;
+        const long long need = ((long long)N + G - 1) / G, most = 256ll * (waves > 18 || need <= 1024 ? 1 : 18 / waves);
+        q.ranges = q.workgroups = (int)(need < most ? need : most);
+    } else {
+        const int VE = dtype == MXC_BF16 ? 8 : 4;
+        const long long columns = (C + 256ll * VE - 1) / (256ll * VE);
+        const long long want = columns >= 1024 ? 1 : 1024 / columns;          // ranges of rows, for about four workgroups a compute unit
+        q.rows = (int)((N + want - 1) / want);
+        q.ranges = (N + q.rows - 1) / q.rows;
+        q.sums_bytes = align_up((size_t)N * 8, 256);
+    }
     q.part_bytes = align_up((size_t)q.ranges * 2 * q.pitch * 4, 256);
-    q.sums_bytes = align_up((size_t)N * 8, 256);
     return q;
+}
+
+template <class T>
+int fwd(int N, int C, int dtype, const T *x, const float *gamma, const float *beta, float eps, T *y, float *stats, hipStream_t st)
+{
+    const Share h = share_of(C, dtype);
+    if (h.PC == 0) {
+        hipLaunchKernelGGL(fwd_long_kernel<T>, dim3(N < 1 << 20 ? N : 1 << 20), dim3(LONG_NT), 0, st, N, C, x, gamma, beta, eps, y, stats);
+        return launched();
+    }
+    return with_share<T>(h, [&](auto tpr, auto pc) {
+        constexpr int TPR = decltype(tpr)::value, PC = decltype(pc)::value;
+        const int G = TPR ? ROW_NT / (TPR ? TPR : 1) : 1, waves = TPR ? ROW_NT / 64 : h.waves;
+        const long long need = ((long long)N + G - 1) / G, per_cu = (PC == 1 ? 32 : 24) / waves, most = 256 * (per_cu < 1 ? 1 : per_cu);
+        const auto kernel = past_caches(N, C, 2, dtype) ? fwd_rows_kernel<T, TPR, PC, true> : fwd_rows_kernel<T, TPR, PC, false>;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)(need < most ? need : most)), dim3(64 * waves), 0, st, N, C, x, gamma, beta, eps, y, stats);
+        return launched();
+    });
+}
+
+template <class T>
+int bwd(int N, int C, int dtype, const T *x, const float *gamma, const float *stats, const T *dy, T *dx, float *dgamma, float *dbeta, char *ws, hipStream_t st)
+{
+    const BwdPlan q = bwd_plan(N, C, dtype);
+    float *part = (float *)ws;
+    if (q.h.PC) {
+        const int rc = with_share<T>(q.h, [&](auto tpr, auto pc) {
+            constexpr int TPR = decltype(tpr)::value, PC = decltype(pc)::value;
+            const bool past = past_caches(N, C, 3, dtype);
+            const auto kernel = TPR || PC == 1 || q.h.waves <= 8 ? (past ? bwd_rows_kernel<T, TPR, PC, true, true> : bwd_rows_kernel<T, TPR, PC, true, false>)
+                                                      : (past ? bwd_rows_kernel<T, 0, PC, false, true> : bwd_rows_kernel<T, 0, PC, false, false>);
+            hipLaunchKernelGGL(kernel, dim3(q.workgroups), dim3(TPR ? ROW_NT : 64 * q.h.waves), 0, st, N, C, x, gamma, stats, dy, dx, part, q.pitch);
+            return launched();
+        });
+        if (rc != MXC_OK) return rc;
+    } else {
+        float2 *sums = (float2 *)(ws + q.part_bytes);
+        hipLaunchKernelGGL(bwd_sums_kernel<T>, dim3(N < 1 << 20 ? N : 1 << 20), dim3(LONG_NT), 0, st, N, C, x, gamma, stats, dy, sums);
+        if (launched() != MXC_OK) return MXC_ERR_LAUNCH;
+        hipLaunchKernelGGL(bwd_columns_kernel<T>, dim3((unsigned)((C + 256ll * Piece<T>::VE - 1) / (256ll * Piece<T>::VE)), q.ranges), dim3(256), 0, st, N, C, q.rows, x, gamma, stats,
+                           dy, sums, dx, part, q.pitch);
+        if (launched() != MXC_OK) return MXC_ERR_LAUNCH;
+    }
+    if (!dgamma && !dbeta) return MXC_OK;
+    const bool few = q.ranges <= 64;
+    hipLaunchKernelGGL(few ? bwd_join_kernel<8> : bwd_join_kernel<32>, dim3((C + 31) / 32, 2), dim3(few ? 256 : 1024), 0, st, C, q.ranges, part, q.pitch, dgamma, dbeta);
+    return launched();
 }
 
 }  // namespace
 
 int layernorm_fwd(int N, int C, int dtype, const void *x, const float *gamma, const float *beta, float eps, void *y, float *stats, hipStream_t st)
 {
-    if (dtype == MXC_BF16)
-        hipLaunchKernelGGL(fwd_long_kernel<bf16_t>, dim3(N < 1 << 20 ? N : 1 << 20), dim3(LONG_NT), 0, st, N, C, (const bf16_t *)x, gamma, beta, eps, (bf16_t *)y, stats);
-    else
-        hipLaunchKernelGGL(fwd_long_kernel<float>, dim3(N < 1 << 20 ? N : 1 << 20), dim3(LONG_NT), 0, st, N, C, (const float *)x, gamma, beta, eps, (float *)y, stats);
-    return hipGetLastError() == hipSuccess ? MXC_OK : MXC_ERR_LAUNCH;
+    if (dtype == MXC_BF16) return fwd(N, C, dtype, (const bf16_t *)x, gamma, beta, eps, (bf16_t *)y, stats, st);
+    return fwd(N, C, dtype, (const float *)x, gamma, beta, eps, (float *)y, stats, st);
 }
 
 size_t layernorm_workspace(int N, int C, int dtype)
 {
     const BwdPlan q = bwd_plan(N, C, dtype);
     return q.part_bytes + q.sums_bytes;
-}
-
-template <class T>
-static int bwd(int N, int C, int dtype, const T *x, const float *gamma, const float *stats, const T *dy, T *dx, float *dgamma, float *dbeta, char *ws, hipStream_t st)
-{
-    const BwdPlan q = bwd_plan(N, C, dtype);
-    float *part = (float *)ws;
-    float2 *sums = (float2 *)(ws + q.part_bytes);
-    hipLaunchKernelGGL(bwd_sums_kernel<T>, dim3(N < 1 << 20 ? N : 1 << 20), dim3(LONG_NT), 0, st, N, C, x, gamma, stats, dy, sums);
-    if (hipGetLastError() != hipSuccess) return MXC_ERR_LAUNCH;
-    hipLaunchKernelGGL(bwd_columns_kernel<T>, dim3((unsigned)((C + 256ll * Piece<T>::VE - 1) / (256ll * Piece<T>::VE)), q.ranges), dim3(256), 0, st, N, C, q.rows, x, gamma, stats, dy,
-                       sums, dx, part, q.pitch);
-    if (hipGetLastError() != hipSuccess) return MXC_ERR_LAUNCH;
-    if (!dgamma && !dbeta) return MXC_OK;
-    hipLaunchKernelGGL(bwd_join_kernel, dim3((C + 63) / 64, 2), dim3(1024), 0, st, C, q.ranges, part, q.pitch, dgamma, dbeta);
-    return hipGetLastError() == hipSuccess ? MXC_OK : MXC_ERR_LAUNCH;
 }
 
 int layernorm_bwd(int N, int C, int dtype, const void *x, const float *gamma, const float *stats, const void *dy, void *dx, float *dgamma, float *dbeta, void *ws, hipStream_t st)

@@ -5,7 +5,10 @@
 
 namespace mxc {
 
-struct __attribute__((packed, aligned(2))) Bytes16 { unsigned x, y, z, w; };
+typedef unsigned Bytes16 __attribute__((ext_vector_type(4), aligned(2)));       // 16 bytes at any element
+
+// Keeps a value where it is in registers: what is made of it before is not kept for after, in more of them.
+__device__ __forceinline__ void held(uint4 &v) { asm volatile("" : "+v"(v.x), "+v"(v.y), "+v"(v.z), "+v"(v.w)); }
 
 template <class T> struct Piece;
 template <> struct Piece<float> {
@@ -30,32 +33,81 @@ template <> struct Piece<bf16_t> {
     static __device__ __forceinline__ bf16_t rounded(float v) { return (bf16_t)pack_bf16x2(v, 0.f); }
 };
 
-// elements [at, at + VE) of a row of `len`: zeros past its end
-template <class T>
-__device__ __forceinline__ Piece<T> load_piece(const T *row, int at, int len)
+// Elements [at, at + VE) of a row of `len`, zeros past its end, in two steps, so that loads stay under way: the load, which for a piece that the row ends in brings the
+// row's last VE elements (of rows of fewer, one by one), and settle_piece, which moves these down.  (Loads in the branch of a short piece would wait there
+// for all before them: a gradient of 40000 x 1000 bf16, 125 pieces by 128 lanes, took 100 us where 65536 x 512 took 51.)
+template <bool PAST = false, class T>
+__device__ __forceinline__ Piece<T> begin_piece(const T *row, int at, int len)
 {
+    constexpr int VE = Piece<T>::VE;
     Piece<T> p;
-    if (at + Piece<T>::VE <= len) {
-        const Bytes16 b = *reinterpret_cast<const Bytes16 *>(row + at);
+    if (len >= VE) {
+        const Bytes16 *from = reinterpret_cast<const Bytes16 *>(row + (at + VE <= len ? at : len - VE));
+        const Bytes16 b = PAST ? __builtin_nontemporal_load(from) : *from;
         p.raw = make_uint4(b.x, b.y, b.z, b.w);
     } else {
-        float v[Piece<T>::VE];
+        float v[VE];
 #pragma unroll
-        for (int i = 0; i < Piece<T>::VE; ++i) v[i] = at + i < len ? load_f32(row + at + i) : 0.f;
+        for (int i = 0; i < VE; ++i) v[i] = at + i < len ? load_f32(row + at + i) : 0.f;
         p.set(v);
     }
     return p;
 }
 template <class T>
+__device__ __forceinline__ void settle_piece(Piece<T> &p, int at, int len)
+{
+    constexpr int VE = Piece<T>::VE;
+    if (at + VE > len && len >= VE) {
+        const int bits = (at + VE - len) * (int)sizeof(T) * 8;
+        unsigned long long lo = p.raw.x | (unsigned long long)p.raw.y << 32, hi = p.raw.z | (unsigned long long)p.raw.w << 32;
+        if (bits >= 64) {
+            lo = bits >= 128 ? 0 : hi >> (bits - 64);
+            hi = 0;
+        } else {
+            lo = lo >> bits | hi << (64 - bits);
+            hi >>= bits;
+        }
+        p.raw = make_uint4((unsigned)lo, (unsigned)(lo >> 32), (unsigned)hi, (unsigned)(hi >> 32));
+    }
+}
+template <class T>
+__device__ __forceinline__ Piece<T> load_piece(const T *row, int at, int len)
+{
+    Piece<T> p = begin_piece(row, at, len);
+    settle_piece(p, at, len);
+    return p;
+}
+template <bool PAST = false, class T>
 __device__ __forceinline__ void store_piece(T *row, int at, int len, const Piece<T> &p)
 {
     if (at + Piece<T>::VE <= len) {
-        *reinterpret_cast<Bytes16 *>(row + at) = Bytes16{p.raw.x, p.raw.y, p.raw.z, p.raw.w};
+        const Bytes16 b = {p.raw.x, p.raw.y, p.raw.z, p.raw.w};
+        if (PAST) __builtin_nontemporal_store(b, reinterpret_cast<Bytes16 *>(row + at));
+        else *reinterpret_cast<Bytes16 *>(row + at) = b;
     } else {
 #pragma unroll
         for (int i = 0; i < Piece<T>::VE; ++i)
             if (at + i < len) row[at + i] = Piece<T>::rounded(p.get(i));
     }
+}
+
+// Sum over aligned groups of G lanes (a power of two), the same in each of them.  Exchanges within 16 lanes are part of an instruction; the four sixteens of a wave
+// meet as scalars.
+template <int CONTROL>
+__device__ __forceinline__ float lane_exchanged(float x) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CONTROL, 0xF, 0xF, true)); }
+template <int G>
+__device__ __forceinline__ float lane_sum(float x)
+{
+    if constexpr (G >= 2) x += lane_exchanged<0xB1>(x);        // lanes 1 0 3 2
+    if constexpr (G >= 4) x += lane_exchanged<0x4E>(x);        // lanes 2 3 0 1
+    if constexpr (G >= 8) x += lane_exchanged<0x141>(x);       // the other half of eight
+    if constexpr (G >= 16) x += lane_exchanged<0x140>(x);      // the other half of sixteen
+    if constexpr (G == 32) x += __shfl_xor(x, 16);
+    if constexpr (G == 64) {
+        auto of = [&](int lane) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), lane)); };
+        x = (of(0) + of(16)) + (of(32) + of(48));
+    }
+    return x;
 }
 
 }  // namespace mxc
