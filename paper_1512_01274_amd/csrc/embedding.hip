@@ -1,7 +1,8 @@
 // Embedding: y[n] = scale * w[tokens[n]], and the gradient of the table, dw[v] = scale * sum of dy[n] over the places n where tokens[n] == v, in
 // the order of n.  Memory bounds both: forward reads and writes each row once; the gradient reads dy once and writes a row of dw for every
-// token of the vocabulary.  The gradient of more than a few places goes by the tokens' order: one launch sorts the places by their token,
-// one adds each token's rows, with the many places of a common token cut into parts, and one joins these parts.
+// token of the vocabulary.  The gradient of more than a few places goes by the tokens' order, in three launches: the places are sorted by their token, each token's rows added, in
+// parts, and the parts of a token that has several joined.  16384 rows of 4096 bf16 41.6 us, 6.5 TB/s (64 rows 3.9, a launch); gradient of 32768 places on 50257 x 2048, bf16,
+// 144 us; of 500 places on 1000 x 512 fp32, in one launch, 8.4.
 #include "pieces.h"
 
 namespace mxc {
@@ -46,49 +47,47 @@ __global__ __launch_bounds__(NT) void fwd_kernel(int N, int V, int C, int log_la
 
 // ---- gradient -----------------------------------------------------------------------------------------------------------------
 
-// to[0, VE) = scale * s, or to it added
-template <int VE>
-__device__ __forceinline__ void put(float *row, int c, int C, const float *s, float scale, bool add)
+// four results: row[c, c + 4) = scale * s, or that added
+template <bool PAST>
+__device__ __forceinline__ void put(float *row, int c, int C, const float (&s)[4], float scale, bool add)
 {
+    Piece<float> p;
+    float v[4];
+    if (add) {
+        p = load_piece(row, c, C);
 #pragma unroll
-    for (int k = 0; k < VE; k += 4) {
-        if (c + k >= C) break;
-        Piece<float> p;
-        float v[4];
-        if (add) {
-            p = load_piece(row, c + k, C);
+        for (int i = 0; i < 4; ++i) v[i] = p.get(i) + s[i] * scale;
+    } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = p.get(i) + s[k + i] * scale;
-        } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = s[k + i] * scale;
-        }
-        p.set(v);
-        store_piece(row, c + k, C, p);
+        for (int i = 0; i < 4; ++i) v[i] = s[i] * scale;
     }
+    p.set(v);
+    store_piece<PAST>(row, c, C, p);
 }
 
-// s[0, VE) = the sum of the pieces at column c of rows places[0, count), in their order
+// s += columns [c, c + 4) of rows places[0, count), in their order; the places of the next rows are under way while rows are
 template <class T>
-__device__ __forceinline__ void add_rows(const T *dy, int c, int C, const int *places, int count, float *s)
+__device__ __forceinline__ void add_rows(const T *dy, int c, int C, const int *places, int count, float (&s)[4])
 {
-    constexpr int VE = Piece<T>::VE, AHEAD = 4;
+    constexpr int AHEAD = 8;
+    if (count <= 0) return;
+    int at[AHEAD];
 #pragma unroll
-    for (int i = 0; i < VE; ++i) s[i] = 0.f;
-    int k = 0;
-    for (; k + AHEAD <= count; k += AHEAD) {
-        Piece<T> p[AHEAD];
-#pragma unroll
-        for (int j = 0; j < AHEAD; ++j) p[j] = load_piece(dy + (size_t)places[k + j] * C, c, C);
+    for (int j = 0; j < AHEAD; ++j) at[j] = places[min(j, count - 1)];
+    for (int k = 0; k < count; k += AHEAD) {
+        decltype(load_quad(dy, 0, 0)) p[AHEAD];
 #pragma unroll
         for (int j = 0; j < AHEAD; ++j)
+            if (k + j < count) p[j] = load_quad(dy + (size_t)at[j] * C, c, C);
+        if (k + AHEAD < count) {
 #pragma unroll
-            for (int i = 0; i < VE; ++i) s[i] += p[j].get(i);
-    }
-    for (; k < count; ++k) {
-        const Piece<T> p = load_piece(dy + (size_t)places[k] * C, c, C);
+            for (int j = 0; j < AHEAD; ++j) at[j] = places[min(k + AHEAD + j, count - 1)];
+        }
 #pragma unroll
-        for (int i = 0; i < VE; ++i) s[i] += p.get(i);
+        for (int j = 0; j < AHEAD; ++j)
+            if (k + j < count)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[i] += p[j].get(i);
     }
 }
 
@@ -98,10 +97,10 @@ constexpr int FEW = 1024, ZERO_ROWS = 64;
 template <class T>
 __global__ __launch_bounds__(NT) void few_kernel(int N, int V, int C, const int *tokens, const T *dy, float scale, int add, float *dw)
 {
-    constexpr int VE = Piece<T>::VE;
     __shared__ int places[FEW];
-    __shared__ int wave_count[NT / 64];
-    const int nt = blockDim.x, waves = nt / 64, lane = threadIdx.x & 63, wave = threadIdx.x / 64;
+    constexpr int TURNS = FEW / NT, nt = NT;
+    __shared__ int wave_count[TURNS * (NT / 64)];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
     if ((int)blockIdx.x >= N) {
         int *found = places;
         const long long v0 = (long long)(blockIdx.x - N) * ZERO_ROWS;
@@ -116,68 +115,116 @@ __global__ __launch_bounds__(NT) void few_kernel(int N, int V, int C, const int 
         const float zeros[4] = {0.f, 0.f, 0.f, 0.f};
         for (int r = 0; r < rows; ++r)
             if (!found[r])
-                for (int c = ((int)blockIdx.y * nt + threadIdx.x) * 4; c < C; c += nt * 4 * gridDim.y) put<4>(dw + (size_t)(v0 + r) * C, c, C, zeros, 1.f, false);
+                for (int c = ((int)blockIdx.y * nt + threadIdx.x) * 4; c < C; c += nt * 4 * gridDim.y) put<false>(dw + (size_t)(v0 + r) * C, c, C, zeros, 1.f, false);
         return;
     }
-    const int me = blockIdx.x, t = tokens[me];
+    const int me = blockIdx.x;
+    int other[TURNS];
+#pragma unroll
+    for (int j = 0; j < TURNS; ++j) {
+        const int n = j * NT + threadIdx.x;
+        other[j] = n < N ? tokens[n] : -1;
+    }
+    const int t = tokens[me];
     if ((unsigned)t >= (unsigned)V) return;
+    bool earlier = false;
+    unsigned long long same[TURNS];
+#pragma unroll
+    for (int j = 0; j < TURNS; ++j) {
+        same[j] = __ballot(other[j] == t);
+        earlier |= other[j] == t && j * NT + (int)threadIdx.x < me;
+        if (lane == 0) wave_count[j * (NT / 64) + wave] = __popcll(same[j]);
+    }
+    if (__syncthreads_or(earlier)) return;
     int count = 0;
-    for (int base = 0; base < N; base += nt) {
-        const int n = base + threadIdx.x;
-        const bool same = n < N && tokens[n] == t;
-        if (__syncthreads_or(same && n < me)) return;
-        const unsigned long long b = __ballot(same);
-        if (lane == 0) wave_count[wave] = __popcll(b);
-        __syncthreads();
+#pragma unroll
+    for (int j = 0; j < TURNS; ++j) {
         int at = count;
-        for (int k = 0; k < waves; ++k) {
-            at += k < wave ? wave_count[k] : 0;
-            count += wave_count[k];
+        for (int k = 0; k < NT / 64; ++k) {
+            at += k < wave ? wave_count[j * (NT / 64) + k] : 0;
+            count += wave_count[j * (NT / 64) + k];
         }
-        if (same) places[at + __popcll(b & ((1ull << lane) - 1))] = n;
+        if (other[j] == t) places[at + __popcll(same[j] & ((1ull << lane) - 1))] = j * NT + threadIdx.x;
     }
     __syncthreads();
-    for (int c = ((int)blockIdx.y * nt + threadIdx.x) * VE; c < C; c += nt * VE * gridDim.y) {
-        float s[VE];
+    for (int c = ((int)blockIdx.y * nt + threadIdx.x) * 4; c < C; c += nt * 4 * gridDim.y) {
+        float s[4] = {0.f, 0.f, 0.f, 0.f};
         add_rows(dy, c, C, places, count, s);
-        put<VE>(dw + (size_t)t * C, c, C, s, scale, add);
+        put<false>(dw + (size_t)t * C, c, C, s, scale, add);
     }
 }
 
-// The places in the order of their tokens (of equal tokens in their own), and where each token's begin: a workgroup for `R` tokens reads all places
-// twice, first to count.  Each of its waves has a range of the places and a counter for each token, so that no wave waits for another on the way.
-constexpr int ORDER_NT = 1024, ORDER_WAVES = ORDER_NT / 64, ORDER_MOST = 768;
-static_assert(ORDER_MOST <= ORDER_NT && ORDER_WAVES * ORDER_MOST * 4 <= 48 << 10, "a thread a token; LDS that any launch may ask for");
-__global__ __launch_bounds__(ORDER_NT) void order_kernel(int N, int V, int R, const int *tokens, int *order, int *start)
+// The places in the order of their tokens (of equal tokens in their own), and where each token's begin.  Workgroup (x, y) puts the places of segment y
+// whose token is among the R tokens of range x; for where they go it counts all places first.  Each of its waves has a share of the segment and a counter of its own for each
+// token, so that no wave waits for another on the way; lanes of one token find each other by the ballots of its bits.  LDS bounds it, where the common tokens are: 32768 places of 50257
+// tokens 15.6 us, of which the range of the 786 most common ones takes all and another 8.
+constexpr int ORDER_NT = 1024, ORDER_WAVES = ORDER_NT / 64, ORDER_MOST = 2048, BATCH = 16, OTHERS = 24;
+template <int MOST>
+__global__ __launch_bounds__(ORDER_NT) void order_kernel(int N, int V, int R, int segment, const int *tokens, int *order, int *start)
 {
-    extern __shared__ int counts[];                 // [ORDER_WAVES][R]
+    __shared__ int counts[(ORDER_WAVES + 2) * MOST];         // [ORDER_WAVES][R] of this segment, [R] of earlier ones, [R] of later ones
     __shared__ int wave_sum[ORDER_WAVES], wave_before[ORDER_WAVES];
     const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
-    const long long lo = (long long)blockIdx.x * R;
-    const int here = (int)min((long long)R, V - lo);
-    for (int i = threadIdx.x; i < ORDER_WAVES * R; i += ORDER_NT) counts[i] = 0;
+    const int lo = blockIdx.x * R, here = min(R, V - lo);
+    for (int i = threadIdx.x; i < (ORDER_WAVES + 2) * R; i += ORDER_NT) counts[i] = 0;
     __syncthreads();
     int *own = counts + wave * R;
-    const int share = (N + ORDER_NT - 1) / ORDER_NT * 64;              // places of a wave
-    const long long n0 = (long long)wave * share, n1 = min((long long)N, n0 + share);
+    // places of a wave in its segment: a multiple of 64
+    const int share = (segment + ORDER_NT - 1) / ORDER_NT * 64;
+    const long long seg0 = (long long)blockIdx.y * segment, seg1 = min((long long)N, seg0 + segment);
+    const long long n0 = min(seg1, seg0 + (long long)wave * share), n1 = min(seg1, n0 + share);
     int before = 0;
-    for (long long n = n0 + lane; n < n1; n += 64) {
-        const int t = tokens[n];
-        before += t >= 0 && t < lo;
-        if (t >= lo && t < lo + here) atomicAdd(own + (t - lo), 1);
+    auto count = [&](int t, int *into) __attribute__((always_inline)) {
+        before += __popcll(__ballot((unsigned)t < (unsigned)lo));
+        const unsigned d = (unsigned)t - (unsigned)lo;              // (a negative token is past every range: V - lo < 2^24)
+        if (d < (unsigned)here) atomicAdd(into + d, 1);
+    };
+    // this wave's first places, which stay in registers, are on their way while those of the other segments are counted
+    int mine[BATCH];
+    auto load_mine = [&](long long m) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < BATCH; ++j) {
+            const long long n = m + 64 * j + lane;
+            mine[j] = n < n1 ? tokens[n] : -1;
+        }
+    };
+    load_mine(n0);
+    const long long others = N - (seg1 - seg0);
+    for (long long m0 = 0; m0 < others; m0 += (long long)ORDER_NT * OTHERS) {
+        const long long m = m0 + threadIdx.x;
+        int t[OTHERS];
+#pragma unroll
+        for (int j = 0; j < OTHERS; ++j) {
+            const long long i = m + (long long)ORDER_NT * j;
+            t[j] = i < others ? tokens[i < seg0 ? i : i + (seg1 - seg0)] : -1;
+        }
+#pragma unroll
+        for (int j = 0; j < OTHERS; ++j) count(t[j], counts + (ORDER_WAVES + (m + (long long)ORDER_NT * j < seg0 ? 0 : 1)) * R);
     }
 #pragma unroll
-    for (int d = 32; d; d >>= 1) before += __shfl_xor(before, d);
+    for (int j = 0; j < BATCH; ++j) count(mine[j], own);
+    for (long long m = n0 + 64 * BATCH; m < n1; m += 64 * BATCH) {
+        load_mine(m);
+#pragma unroll
+        for (int j = 0; j < BATCH; ++j) count(mine[j], own);
+    }
     if (lane == 0) wave_before[wave] = before;
     __syncthreads();
     int base = 0;
     for (int k = 0; k < ORDER_WAVES; ++k) base += wave_before[k];
-    // from counts to where a wave's places of a token go: a token a thread
-    const int t0 = threadIdx.x;
-    int total = 0;
-    if (t0 < here)
-        for (int k = 0; k < ORDER_WAVES; ++k) total += counts[k * R + t0];
-    int up = total;
+    // from counts to where a wave's places of a token go: OF tokens a thread
+    constexpr int OF = MOST > ORDER_NT ? MOST / ORDER_NT : 1;
+    const int t0 = threadIdx.x * OF;
+    int total[OF], sum = 0;
+#pragma unroll
+    for (int j = 0; j < OF; ++j) {
+        total[j] = 0;
+        if (t0 + j < here)
+#pragma unroll
+            for (int k = 0; k < ORDER_WAVES + 2; ++k) total[j] += counts[k * R + t0 + j];
+        sum += total[j];
+    }
+    int up = sum;
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) {
         const int v = __shfl_up(up, d);
@@ -186,120 +233,177 @@ __global__ __launch_bounds__(ORDER_NT) void order_kernel(int N, int V, int R, co
     if (lane == 63) wave_sum[wave] = up;
     __syncthreads();
     for (int k = 0; k < wave; ++k) base += wave_sum[k];
-    int at = base + up - total;
-    if (t0 < here) {
-        start[lo + t0] = at;
+    base += up - sum;
+#pragma unroll
+    for (int j = 0; j < OF; ++j) {
+        if (t0 + j >= here) break;
+        if (blockIdx.y == 0) {
+            start[lo + t0 + j] = base;
+            if (lo + t0 + j == V - 1) start[V] = base + total[j];
+        }
+        int at = base + counts[ORDER_WAVES * R + t0 + j];
+#pragma unroll
         for (int k = 0; k < ORDER_WAVES; ++k) {
-            const int c = counts[k * R + t0];
-            counts[k * R + t0] = at;
+            const int c = counts[k * R + t0 + j];
+            counts[k * R + t0 + j] = at;
             at += c;
         }
-        if (lo + t0 == V - 1) start[V] = at;
+        base += total[j];
     }
     __syncthreads();
-    for (long long m = n0; m < n1; m += 64) {
-        const long long n = m + lane;
-        const int t = n < n1 ? tokens[n] : -1;
-        const int d = t >= lo && t < lo + here ? (int)(t - lo) : -1;
-        unsigned long long left = __ballot(d >= 0);
-        while (left) {
-            const int first = __ffsll(left) - 1, what = __shfl(d, first);
-            const unsigned long long same = __ballot(d == what);
-            const int to = own[what];
-            if (d == what) order[to + __popcll(same & ((1ull << lane) - 1))] = (int)n;
-            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-            __builtin_amdgcn_wave_barrier();
-            if (lane == first) own[what] = to + __popcll(same);
+    const int bits = 32 - __clz(R);
+    for (long long m = n0; m < n1; m += 64 * BATCH) {
+        if (n1 - n0 > 64 * BATCH) load_mine(m);
+#pragma unroll
+        for (int j = 0; j < BATCH; ++j) {
+            const unsigned d = (unsigned)mine[j] - (unsigned)lo;
+            const bool in = d < (unsigned)here;
+            unsigned long long same = __ballot(in);
+            if (same == 0) continue;
+            // the lanes that have the same token: those that agree in every bit
+            for (int b = 0; b < bits; ++b) {
+                const bool one = d >> b & 1;
+                const unsigned long long ones = __ballot(one);
+                same &= one ? ones : ~ones;
+            }
+            if (in) {
+                const int to = own[d], rank = __popcll(same & ((1ull << lane) - 1));
+                order[to + rank] = (int)(m + 64 * j) + lane;
+                __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+                if (rank == 0) own[d] = to + __popcll(same);
+            }
             __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
             __builtin_amdgcn_wave_barrier();
             __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-            left &= ~same;
         }
     }
 }
 
-// A token of more than HEAVY places is added in parts: part p is what it has among the places PART * p ... of the order.  Such a token is longer than
-// a part, so that a part meets two of them at most: slot 0 is for one that holds the part's first place, slot 1 for one that begins within it.
-constexpr int HEAVY = 128, PART = 64;
-template <class T>
-__global__ __launch_bounds__(NT) void rows_kernel(int N, int V, int C, int log_lanes, int row_groups, const int *tokens, const int *order, const int *start, const T *dy, float scale,
-                                                 int add, float *dw, float *parts)
+// Sums of each token's rows: a wave for PART (16 to 64) places of the order and 256 columns.  Its lanes hold the places and their tokens, so that all control is the wave's; it loads the
+// rows of 16 places at once and adds them one after the other, and where the token changes the sum is the token's row of dw, or, of a token that has places in other
+// parts too, this part's share: slot 0 for the token of the part's first place, slot 1 for one that begins within it.  Workgroups behind the parts' clear the rows of
+// tokens that stand nowhere (between the parts', 4 % slower).  32768 places on 50257 x 2048 from memory, bf16: 117 us of the gradient's 144, 4.7 TB/s.
+constexpr int BLOCK = 256;
+template <class T, bool PAST>
+__global__ __launch_bounds__(NT) void rows_kernel(int V, int C, int PART, long long part_waves, unsigned part_groups, int empty_rows, const int *tokens,
+                                                 const int *order, const int *start, const T *dy, float scale, int add, float *dw, float *parts)
 {
-    constexpr int VE = Piece<T>::VE;
-    const int L = 1 << log_lanes, lane = threadIdx.x & (L - 1), G = NT >> log_lanes, group = threadIdx.x >> log_lanes;
-    if ((int)blockIdx.x < row_groups) {
-        const long long v = (long long)blockIdx.x * G + group;
-        if (v >= V) return;
-        const int s0 = start[v], count = start[v + 1] - s0;
-        if (count > HEAVY || (add && count == 0)) return;
-        for (int c = lane * VE; c < C; c += L * VE) {
-            float s[VE];
-            add_rows(dy, c, C, order + s0, count, s);
-            put<VE>(dw + (size_t)v * C, c, C, s, scale, add);
+    constexpr int AHEAD = 16;
+    const int lane = threadIdx.x & 63;
+    if (blockIdx.x >= part_groups) {
+        const int v0 = (int)(blockIdx.x - part_groups) * empty_rows, rows = min(empty_rows, V - v0);
+        const unsigned long long empty = __ballot(lane < rows && start[v0 + min(lane, rows - 1)] == start[v0 + min(lane, rows - 1) + 1]);
+        const float zeros[4] = {0.f, 0.f, 0.f, 0.f};
+        if (C > 256) {
+            for (int r = 0; r < rows; ++r)
+                if (empty >> r & 1)
+                    for (int c = threadIdx.x * 4; c < C; c += NT * 4) put<PAST>(dw + (size_t)(v0 + r) * C, c, C, zeros, 1.f, false);
+        } else {
+            const unsigned quads = (unsigned)(C + 3) / 4;
+            for (unsigned i = threadIdx.x; i < rows * quads; i += NT) {
+                const unsigned r = i / quads;
+                if (empty >> r & 1) put<PAST>(dw + (size_t)(v0 + (int)r) * C, (int)(i - r * quads) * 4, C, zeros, 1.f, false);
+            }
         }
         return;
     }
-    const long long p = (long long)(blockIdx.x - row_groups) * G + group;
-    const int all = start[V];
-    if (p * PART >= all) return;
-    const int p0 = (int)p * PART, p1 = min(all, p0 + PART);
-    int t = tokens[order[p0]];
-    for (int slot = 0; slot < 2; ++slot) {
-        const int s0 = start[t], s1 = start[t + 1];
-        if (s1 - s0 > HEAVY) {
-            const int a = max(s0, p0), b = min(s1, p1);
-            float *to = parts + (size_t)(2 * p + slot) * C;
-            for (int c = lane * VE; c < C; c += L * VE) {
-                float s[VE];
-                add_rows(dy, c, C, order + a, b - a, s);
-                put<VE>(to, c, C, s, 1.f, false);
+    const long long w = (long long)blockIdx.x * (NT / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (w >= part_waves) return;
+    const int blocks = (C + BLOCK - 1) / BLOCK, part = (int)(w / blocks), c = ((int)(w - (long long)part * blocks) * 64 + lane) * 4;
+    const int all = __builtin_amdgcn_readfirstlane(start[V]), p0 = part * PART, count = min(PART, all - p0);
+    if (count <= 0) return;
+    // past the last place: the last one's row again, under a token of its own
+    const int o = order[p0 + min(lane, count - 1)], t = lane < count ? tokens[o] : -1;
+    const int ahead = p0 > 0 ? tokens[order[p0 - 1]] : -1, behind = p0 + count < all ? tokens[order[p0 + count]] : -1;
+    const bool has = c < C;
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+    int now = __builtin_amdgcn_readlane(t, 0), slot = 0;
+    bool whole = __builtin_amdgcn_readfirstlane(ahead) != now;          // the token's places begin in this part
+    for (int k = 0; k < count; k += AHEAD) {
+        decltype(load_quad(dy, 0, 0)) p[AHEAD];
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) p[j] = load_quad(dy + (size_t)__builtin_amdgcn_readlane(o, k + j) * C, has ? c : 0, C);
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+            const int next = __builtin_amdgcn_readlane(t, k + j);
+            if (next != now) {
+                if (now >= 0 && has) {
+                    if (whole) put<PAST>(dw + (size_t)now * C, c, C, s, scale, add);
+                    else put<false>(parts + (size_t)(2 * part) * C, c, C, s, 1.f, false);
+                }
+                now = next;
+                slot = 1;
+                whole = true;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[i] = 0.f;
             }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[i] += p[j].get(i);
         }
-        const int last = tokens[order[p1 - 1]];
-        if (last == t) break;
-        t = last;
+    }
+    if (now >= 0 && has) {          // (a part of fewer places has ended its last token above)
+        if (whole && __builtin_amdgcn_readfirstlane(behind) != now) put<PAST>(dw + (size_t)now * C, c, C, s, scale, add);
+        else put<false>(parts + (size_t)(2 * part + slot) * C, c, C, s, 1.f, false);
     }
 }
 
-// A part in which a heavy token begins adds up that token's parts.
-__global__ __launch_bounds__(NT) void join_kernel(int V, int C, int log_lanes, const int *tokens, const int *order, const int *start, const float *parts, float scale, int add, float *dw)
+// A part in which a token begins that ends in another adds up that token's shares: a workgroup for 256 columns, whose waves take a quarter of the shares each.
+__global__ __launch_bounds__(NT) void join_kernel(int V, int C, int PART, const int *tokens, const int *order, const int *start, const float *parts, float scale, int add, float *dw)
 {
-    const int L = 1 << log_lanes, lane = threadIdx.x & (L - 1), G = NT >> log_lanes, group = threadIdx.x >> log_lanes;
-    const long long p = (long long)blockIdx.x * G + group;
-    const int all = start[V];
-    if (p * PART >= all) return;
-    const int p0 = (int)p * PART, p1 = min(all, p0 + PART);
-    int t = tokens[order[p0]];
-    if (start[t] != p0) t = tokens[order[p1 - 1]];           // the one that can begin here
-    const int s0 = start[t], s1 = start[t + 1];
-    if (s0 < p0 || s1 - s0 <= HEAVY) return;
-    const int q1 = (s1 - 1) / PART;
-    for (int c = lane * 4; c < C; c += L * 4) {
-        float s[4];
-        Piece<float> f = load_piece(parts + (size_t)(2 * p + (s0 == p0 ? 0 : 1)) * C, c, C);
+    constexpr int AHEAD = 16;
+    __shared__ float4 sum[NT];
+    const int all = start[V], part = blockIdx.x, p0 = part * PART, p1 = p0 + PART;
+    if (p1 >= all) return;
+    const int t = tokens[order[p1 - 1]], s0 = start[t], s1 = start[t + 1];
+    if (s0 < p0 || s1 <= p1) return;
+    const int shares = (s1 - 1) / PART - part + 1, wave = threadIdx.x >> 6, quarter = (shares + NT / 64 - 1) / (NT / 64), c = ((int)blockIdx.y * 64 + (threadIdx.x & 63)) * 4;
+    const int q0 = wave * quarter, q1 = min(shares, q0 + quarter), at = c < C ? c : 0;
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int q = q0; q < q1; q += AHEAD) {
+        Piece<float> g[AHEAD];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[i] = f.get(i);
-        for (int q = (int)p + 1; q <= q1; ++q) {
-            f = load_piece(parts + (size_t)(2 * (long long)q) * C, c, C);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) s[i] += f.get(i);
+        for (int j = 0; j < AHEAD; ++j) {
+            const int k = min(q + j, q1 - 1);
+            g[j] = load_piece(parts + (size_t)(2 * ((long long)part + k) + (k == 0 && s0 != p0 ? 1 : 0)) * C, at, C);
         }
-        put<4>(dw + (size_t)t * C, c, C, s, scale, add);
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[i] += q + j < q1 ? g[j].get(i) : 0.f;
     }
+    sum[threadIdx.x] = make_float4(s[0], s[1], s[2], s[3]);
+    __syncthreads();
+    if (wave || c >= C) return;
+#pragma unroll
+    for (int k = 1; k < NT / 64; ++k) {
+        const float4 o = sum[k * 64 + threadIdx.x];
+        s[0] += o.x; s[1] += o.y; s[2] += o.z; s[3] += o.w;
+    }
+    put<false>(dw + (size_t)t * C, c, C, s, scale, add);
 }
 
 struct OrderPlan {
-    int R, workgroups;
+    int R, ranges, segment, segments, part;
     long long part_count;
     size_t order_bytes, start_bytes, part_bytes;
 };
 OrderPlan order_plan(int N, int V, int C)
 {
     OrderPlan q = {};
-    q.R = (V + 255) / 256;
+    // some 256 workgroups, one a compute unit: 64 ranges of tokens where there are as many, by segments of the places
+    q.ranges = V < 16 * 64 ? (V + 15) / 16 : 64;
+    q.R = (V + q.ranges - 1) / q.ranges;
     if (q.R > ORDER_MOST) q.R = ORDER_MOST;
-    q.workgroups = (V + q.R - 1) / q.R;
-    q.part_count = N > HEAVY ? ((long long)N + PART - 1) / PART : 0;
+    q.ranges = (V + q.R - 1) / q.R;
+    int segments = 256 / q.ranges;
+    segments = segments < 1 ? 1 : segments > 16 ? 16 : segments;
+    q.segment = (N + segments - 1) / segments;
+    q.segments = (N + q.segment - 1) / q.segment;
+    const int blocks = (C + BLOCK - 1) / BLOCK;
+    // places of a part: as many as leave 2048 waves (65536 places of 256 columns: 64 places 81 us, 32 83, 16 93, for each part may leave shares that are read again)
+    q.part = 64;
+    while (q.part > 16 && (long long)N * blocks / q.part < 2048) q.part /= 2;
+    q.part_count = ((long long)N + q.part - 1) / q.part;
     q.order_bytes = align_up((size_t)N * 4, 256);
     q.start_bytes = align_up(((size_t)V + 1) * 4, 256);
     q.part_bytes = align_up((size_t)q.part_count * 2 * C * 4, 256);
@@ -326,25 +430,24 @@ int fwd(int N, int V, int C, const int *tokens, const T *w, float scale, T *y, h
 template <class T>
 int bwd(int N, int V, int C, const int *tokens, const T *dy, float scale, int add, float *dw, char *ws, hipStream_t st)
 {
-    constexpr int VE = Piece<T>::VE;
     if (N <= FEW) {
-        const int L = row_lanes(C, VE), nt = L < 64 ? 64 : L;
-        const unsigned grid = (unsigned)(N + (add ? 0 : ((long long)V + ZERO_ROWS - 1) / ZERO_ROWS)), columns = (unsigned)(((long long)C + nt * VE - 1) / (nt * VE));
-        hipLaunchKernelGGL(few_kernel<T>, dim3(grid, columns), dim3(nt), 0, st, N, V, C, tokens, dy, scale, add, dw);
+        const unsigned grid = (unsigned)(N + (add ? 0 : ((long long)V + ZERO_ROWS - 1) / ZERO_ROWS)), columns = (unsigned)((C + NT * 4 - 1) / (NT * 4));
+        hipLaunchKernelGGL(few_kernel<T>, dim3(grid, columns), dim3(NT), 0, st, N, V, C, tokens, dy, scale, add, dw);
         return launched();
     }
     const OrderPlan q = order_plan(N, V, C);
     int *order = (int *)ws, *start = (int *)(ws + q.order_bytes);
     float *parts = (float *)(ws + q.order_bytes + q.start_bytes);
-    hipLaunchKernelGGL(order_kernel, dim3(q.workgroups), dim3(ORDER_NT), (size_t)ORDER_WAVES * q.R * 4, st, N, V, q.R, tokens, order, start);
+    hipLaunchKernelGGL(q.R <= 512 ? order_kernel<512> : q.R <= 1024 ? order_kernel<1024> : order_kernel<2048>, dim3(q.ranges, q.segments), dim3(ORDER_NT), 0, st, N, V, q.R, q.segment, tokens, order, start);
     if (launched() != MXC_OK) return MXC_ERR_LAUNCH;
-    const int L = row_lanes(C, VE), G = NT / L;
-    const int row_groups = (int)(((long long)V + G - 1) / G);
-    hipLaunchKernelGGL(rows_kernel<T>, dim3((unsigned)(row_groups + (q.part_count + G - 1) / G)), dim3(NT), 0, st, N, V, C, log2_of(L), row_groups, tokens, order, start, dy, scale, add, dw,
-                       parts);
+    const long long part_waves = q.part_count * ((C + BLOCK - 1) / BLOCK);
+    const int empty_rows = C <= 256 ? 64 : 16;
+    const unsigned part_groups = (unsigned)((part_waves + NT / 64 - 1) / (NT / 64)), empty_groups = add ? 0 : (unsigned)((V + empty_rows - 1) / empty_rows);
+    const bool past = !add && (unsigned long long)V * C * 4 >= 256ull << 20;
+    hipLaunchKernelGGL(past ? (rows_kernel<T, true>) : (rows_kernel<T, false>), dim3(part_groups + empty_groups), dim3(NT), 0, st, V, C, q.part, part_waves, part_groups, empty_rows,
+                       tokens, order, start, dy, scale, add, dw, parts);
     if (launched() != MXC_OK) return MXC_ERR_LAUNCH;
-    const int LJ = row_lanes(C, 4), GJ = NT / LJ;
-    hipLaunchKernelGGL(join_kernel, dim3((unsigned)((q.part_count + GJ - 1) / GJ)), dim3(NT), 0, st, V, C, log2_of(LJ), tokens, order, start, parts, scale, add, dw);
+    hipLaunchKernelGGL(join_kernel, dim3((unsigned)q.part_count, (C + BLOCK - 1) / BLOCK), dim3(NT), 0, st, V, C, q.part, tokens, order, start, parts, scale, add, dw);
     return launched();
 }
 
