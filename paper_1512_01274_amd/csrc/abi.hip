@@ -1288,8 +1288,7 @@ int mxc_orthogonalize_workspace_bytes(int count, const int *rows, const int *col
 {
     if (!out_bytes) return MXC_ERR_NULL;
     MXC_TRY(matrices_check(count, rows, cols));
-    *out_bytes = muon_workspace(count, rows, cols);
-    return MXC_OK;
+    return muon_workspace(count, rows, cols, out_bytes);
 }
 
 int mxc_orthogonalize(int count, const int *rows, const int *cols, const void *const *x, int dtype, int steps, void *const *y, void *workspace, size_t workspace_bytes,
@@ -1300,10 +1299,9 @@ int mxc_orthogonalize(int count, const int *rows, const int *cols, const void *c
     const void *const *const tensors[] = {x, y};
     MXC_TRY(pointers_check(count, tensors, 2));
     if (misaligned(workspace)) return MXC_ERR_ALIGN;
-    if (!workspace || workspace_bytes < muon_workspace(count, rows, cols)) return MXC_ERR_WORKSPACE;
     MuonArgs a = {};
     a.count = count; a.rows = rows; a.cols = cols; a.u = x; a.dtype = dtype; a.y = y; a.steps = steps;
-    return muon_run(a, workspace, (hipStream_t)hip_stream);
+    return muon_run(a, workspace, workspace_bytes, (hipStream_t)hip_stream);
 }
 
 int mxc_muon_update(int count, const int *rows, const int *cols, float *const *w, const void *const *g, int grad_dtype, float *const *m, void *const *w_bf16,
@@ -1318,11 +1316,10 @@ int mxc_muon_update(int count, const int *rows, const int *cols, float *const *w
     const void *const *const tensors[] = {(const void *const *)w, g, (const void *const *)m, (const void *const *)w_bf16};
     MXC_TRY(pointers_check(count, tensors, w_bf16 ? 4 : 3));
     if (misaligned(workspace)) return MXC_ERR_ALIGN;
-    if (!workspace || workspace_bytes < muon_workspace(count, rows, cols)) return MXC_ERR_WORKSPACE;
     MuonArgs a = {};
     a.count = count; a.rows = rows; a.cols = cols; a.u = g; a.dtype = grad_dtype; a.w = w; a.m = m; a.w_bf16 = w_bf16;
     a.steps = steps; a.nesterov = nesterov; a.momentum = (float)momentum; a.grad_scale = (float)grad_scale; a.keep = (float)(1.0 - lr * wd); a.lr = lr; a.rms = rms;
-    return muon_run(a, workspace, (hipStream_t)hip_stream);
+    return muon_run(a, workspace, workspace_bytes, (hipStream_t)hip_stream);
 }
 
 int mxc_conv2d_workspace_bytes(int pass, int N, int C, int H, int W, int K, int R, int S, int stride, int pad,

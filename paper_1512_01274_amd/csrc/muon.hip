@@ -12,10 +12,13 @@
 // of rank 4, whose rounding errors the first steps would blow up by a^5, 6e-4, 7e-2 and 0.6.
 #include <math.h>
 
+#include <algorithm>
+#include <new>
 #include <type_traits>
 #include <utility>
+#include <vector>
 
-#include "mxc_internal.h"
+#include "pieces.h"
 
 namespace mxc {
 namespace {
@@ -29,7 +32,7 @@ constexpr float NS_A = 3.4445f, NS_B = -4.7750f, NS_C = 2.0315f;
 constexpr float X_UP = 32768.f, X_DOWN = 1.f / 32768.f, LO_UP = 2048.f, LO_DOWN = 1.f / 2048.f, S_UP = 16384.f, S_DOWN = 1.f / 16384.f;
 
 constexpr int BK = 64;                      // reduction of a stage, and what sides are padded to
-constexpr int NORM_MOST = 256, NORM_CHUNK = 8192;
+constexpr int NORM_MOST = 1024, NORM_CHUNK = 8192;
 
 // One matrix of a call.  Z is ping-ponged where the third product reads it (tall), its transpose where it does not (wide); the other pair of pointers is one buffer.
 struct Entry {
@@ -43,9 +46,15 @@ struct Entry {
     f16_t *z[2], *zt[2], *lo, *O, *P;
     float *d, *e;
     double *norm;
-    unsigned sym_first, prod_first, prep_first, sym_count, prod_count, prep_count;      // tiles of the three kinds of launches
+    unsigned prep_first, prep_count;        // tiles of prepare_kernel
+    struct Items {                          // of the launches of each product
+        unsigned first, count;              // work items: tiles, the last of them in `split` ranges of the reduction each
+        unsigned whole, split;              // tiles that are not split
+        unsigned part_first, finish_first, finish_count;        // of the split ones: the first one's first partial sums; workgroups that add them
+        int shape;                          // of the tiles: a launch each
+    } items[3];
 };
-constexpr int GROUP = 20;
+constexpr int GROUP = 14;
 struct Group {
     Entry t[GROUP];
     unsigned first[GROUP + 1];
@@ -55,33 +64,85 @@ struct Common {
     float momentum, grad_scale, keep;
     int nesterov, muon, bf16;
 };
-static_assert(sizeof(Group) + sizeof(Common) + 64 <= 4096, "kernel arguments");
 
-__device__ __forceinline__ float value_of(const void *p, size_t i, int bf16) { return bf16 ? bf16_to_f32(((const bf16_t *)p)[i]) : ((const float *)p)[i]; }
+// whether the momentum is still to be made of the gradient, and where it goes
+struct ToMake {
+    static constexpr bool fresh = true;
+    float *m;
+    int c, len;
+    __device__ __forceinline__ void store(const Piece<float> &p) const { store_piece(m, c, len, p); }
+};
+struct Made {
+    static constexpr bool fresh = false;
+    __device__ __forceinline__ void store(const Piece<float> &) const {}
+};
+
+// four values of the matrix that is made orthogonal, from column c of row r: x, or the momentum's part (m: as it is after norm_kernel)
+template <bool BF16, class M>
+__device__ __forceinline__ void values_at(const Entry &t, const Common &f, const void *u, const float *m, int c, int len, float (&v)[4], M &&made)
+{
+    if (!f.muon || f.nesterov || made.fresh) {
+        if constexpr (BF16) {
+            const Quad q = load_quad((const bf16_t *)u, c, len);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = q.get(i);
+        } else {
+            const Piece<float> q = load_piece((const float *)u, c, len);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = q.get(i);
+        }
+    }
+    if (f.muon) {
+        Piece<float> q = load_piece(m, c, len);
+        float n[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float g = v[i] * f.grad_scale;
+            n[i] = made.fresh ? q.get(i) * f.momentum + g : q.get(i);
+            v[i] = f.nesterov ? g + n[i] * f.momentum : n[i];
+        }
+        if (made.fresh) {
+            q.set(n);
+            made.store(q);
+        }
+    }
+}
 
 // ---- sums of squares, the momentum, and the table of the call's matrices ---------------------------------------------------------------------
 
-__global__ __launch_bounds__(256) void norm_kernel(Group q, Common f, Entry *table, unsigned *sym_map, unsigned *prod_map, unsigned *prep_map)
+// which matrix each workgroup of a launch belongs to
+struct Maps {
+    unsigned *prep, *items[3][4], *finish[3][4];        // [product][shape]
+};
+static_assert(sizeof(Group) + sizeof(Common) + sizeof(Maps) + 32 <= 4096, "kernel arguments");
+__device__ __forceinline__ void fill(unsigned *map, unsigned first, unsigned count, unsigned value, unsigned at, unsigned step)
+{
+    for (unsigned k = at; k < count; k += step) map[first + k] = value;
+}
+
+template <bool BF16>
+__global__ __launch_bounds__(256) void norm_kernel(Group q, Common f, Entry *table, Maps maps)
 {
     int i = 0;
     while (i + 1 < q.count && blockIdx.x >= q.first[i + 1]) ++i;
     const Entry &t = q.t[i];
-    const unsigned part = blockIdx.x - q.first[i];
-    if (part == 0 && threadIdx.x == 0) table[q.base + i] = t;
-    for (unsigned k = part * 256 + threadIdx.x; k < t.sym_count; k += t.norm_count * 256) sym_map[t.sym_first + k] = q.base + i;
-    for (unsigned k = part * 256 + threadIdx.x; k < t.prod_count; k += t.norm_count * 256) prod_map[t.prod_first + k] = q.base + i;
-    for (unsigned k = part * 256 + threadIdx.x; k < t.prep_count; k += t.norm_count * 256) prep_map[t.prep_first + k] = q.base + i;
-    const size_t n = (size_t)t.R * t.C;
+    const unsigned part = blockIdx.x - q.first[i], at = part * 256 + threadIdx.x, step = t.norm_count * 256, me = q.base + i;
+    if (at == 0) table[me] = t;
+    fill(maps.prep, t.prep_first, t.prep_count, me, at, step);
+    for (int k = 0; k < 3; ++k) {
+        fill(maps.items[k][t.items[k].shape], t.items[k].first, t.items[k].count, me, at, step);
+        fill(maps.finish[k][t.items[k].shape], t.items[k].finish_first, t.items[k].finish_count, me, at, step);
+    }
+    const int n = t.R * t.C;                // (below 2^30 + 2^15)
+    const void *u = t.u;
+    float *m = t.m;
     double s = 0.0;
-    for (size_t k = (size_t)part * 256 + threadIdx.x; k < n; k += (size_t)t.norm_count * 256) {
-        float u = value_of(t.u, k, f.bf16);
-        if (f.muon) {
-            u *= f.grad_scale;
-            const float m = t.m[k] * f.momentum + u;
-            t.m[k] = m;
-            u = f.nesterov ? u + m * f.momentum : m;
-        }
-        s += (double)u * (double)u;
+#pragma unroll 4
+    for (long long k = (long long)(part * 256 + threadIdx.x) * 4; k < n; k += (long long)t.norm_count * 1024) {
+        float v[4];
+        values_at<BF16>(t, f, u, m, (int)k, n, v, ToMake{m, (int)k, n});
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s += k + j < n ? (double)v[j] * (double)v[j] : 0.0;
     }
     __shared__ double wave_sum[4];
 #pragma unroll
@@ -93,46 +154,56 @@ __global__ __launch_bounds__(256) void norm_kernel(Group q, Common f, Entry *tab
 
 // ---- X over its norm, in both orientations: a workgroup for 64 x 64 values -----------------------------------------------------------------------
 
+template <bool BF16>
 __global__ __launch_bounds__(256) void prepare_kernel(Common f, const Entry *table, const unsigned *map)
 {
+    typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
     const Entry &t = table[map[blockIdx.x]];
     const unsigned tile = blockIdx.x - t.prep_first, across = t.Cp / 64;
     const int r0 = tile / across * 64, c0 = tile % across * 64;
-    __shared__ f16_t turned[64][66];
+    __shared__ f16_t turned[64][68];
     __shared__ double wave_sum[4];
-    double s = (int)threadIdx.x < t.norm_count ? t.norm[threadIdx.x] : 0.0;
+    const int c = threadIdx.x % 16 * 4, row = threadIdx.x / 16;
+    float v[4][4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int r = r0 + k * 16 + row;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[k][i] = 0.f;
+        if (r < t.R && c0 + c < t.C) {
+            const size_t at = (size_t)r * t.C;
+            values_at<BF16>(t, f, BF16 ? (const void *)((const bf16_t *)t.u + at) : (const void *)((const float *)t.u + at), t.m + at, c0 + c, t.C, v[k], Made{});
+        }
+    }
+    double s = 0.0;
+    for (int k = threadIdx.x; k < t.norm_count; k += 256) s += t.norm[k];
 #pragma unroll
     for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
     if ((threadIdx.x & 63) == 0) wave_sum[threadIdx.x >> 6] = s;
     __syncthreads();
     s = wave_sum[0] + wave_sum[1] + wave_sum[2] + wave_sum[3];
-    // a value that is not finite makes NaN of the whole matrix; zeros stay zeros
-    const double by = !(s < 1e300) ? __builtin_nan("") : s > 0.0 ? (double)X_UP / sqrt(s) : 0.0;
-    const int c = c0 + (threadIdx.x & 63);
-    for (int k = threadIdx.x >> 6; k < 64; k += 4) {
-        const int r = r0 + k;
-        double x = 0.0;
-        if (r < t.R && c < t.C) {
-            const size_t at = (size_t)r * t.C + c;
-            float u;
-            if (f.muon && !f.nesterov) u = t.m[at];
-            else {
-                u = value_of(t.u, at, f.bf16);
-                if (f.muon) {
-                    u *= f.grad_scale;
-                    u += t.m[at] * f.momentum;
-                }
-            }
-            x = (double)u * by;
+    // 1 / norm as a power of two and a factor of ordinary size.  A value that is not finite makes NaN of the whole matrix; zeros stay zeros
+    int up = 0;
+    const double norm = frexp(sqrt(s), &up);
+    const float by = !(s < 1e300) ? __builtin_nanf("") : s > 0.0 ? (float)((double)X_UP / norm) : 0.f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        f16x4 hi, lo;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const bool in = r0 + k * 16 + row < t.R && c0 + c + i < t.C;
+            const float x = in ? ldexpf(v[k][i], -up) * by : 0.f;
+            hi[i] = (f16_t)x;
+            lo[i] = (f16_t)((x - (float)hi[i]) * LO_UP);
+            turned[c + i][k * 16 + row] = hi[i];
         }
-        const f16_t hi = (f16_t)(float)x, lo = (f16_t)(float)((x - (double)(float)hi) * (double)LO_UP);
-        const size_t to = (size_t)r * t.Cp + c;
-        t.z[0][to] = hi;
-        t.lo[to] = lo;
-        turned[threadIdx.x & 63][k] = hi;
+        const size_t to = (size_t)(r0 + k * 16 + row) * t.Cp + c0 + c;
+        *reinterpret_cast<f16x4 *>(t.z[0] + to) = hi;
+        *reinterpret_cast<f16x4 *>(t.lo + to) = lo;
     }
     __syncthreads();
-    for (int k = threadIdx.x >> 6; k < 64; k += 4) t.zt[0][(size_t)(c0 + k) * t.Rp + r0 + (threadIdx.x & 63)] = turned[k][threadIdx.x & 63];
+#pragma unroll
+    for (int k = 0; k < 64; k += 16) *reinterpret_cast<f16x4 *>(t.zt[0] + (size_t)(c0 + k + row) * t.Rp + r0 + c) = *reinterpret_cast<const f16x4 *>(&turned[k + row][c]);
 }
 
 // ---- products -----------------------------------------------------------------------------------------------------------------------------------
@@ -166,54 +237,221 @@ __device__ __forceinline__ void triangle(unsigned t, unsigned T, unsigned &i, un
     j = k + t - start(k);
 }
 
+// where tile `tile` of a matrix lies: its first row and column
+template <int BM, int BN, int MODE>
+__device__ __forceinline__ void place(const Entry &t, unsigned tile, int &m0, int &n0)
+{
+    unsigned ti, tj;
+    if (MODE == THIRD) {
+        // in bands of 8 rows of tiles, column by column
+        const unsigned across = (t.Cp + BN - 1) / BN, down = (t.Rp + BM - 1) / BM;
+        const unsigned band = tile / (8 * across), rows = min(8u, down - band * 8), in = tile - band * 8 * across;
+        ti = band * 8 + in % rows;
+        tj = in / rows;
+    } else {
+        static_assert(MODE == THIRD || BM == BN, "a symmetric result has square tiles");
+        triangle(tile, (t.mp + BM - 1) / BM, ti, tj);
+    }
+    m0 = ti * BM;
+    n0 = tj * BN;
+}
+
+// What becomes of the sums of 32 rows by NI * 32 columns, a wave's: through LDS, as fp32, in rows and then, for the other orientation, in columns.
+template <int MODE, int NI>
+struct Results {
+    static constexpr int WN = NI * 32, PITCH = WN + 4, CPR = WN / 8, ROWS = 64 / CPR, KI = 32 / ROWS;      // chunks of 8 columns in a row; rows that 64 lanes cover; turns
+    static constexpr int WITH = MODE == THIRD ? 2 : MODE == SQUARE_A ? 1 : 0, BYTES = 32 * PITCH * 4;
+    // what results are made with besides the sums: X, or O, and a value of the diagonal for each row
+    struct With {
+        f16x8 v[KI][WITH ? WITH : 1];
+        float of_row[KI];
+    };
+    const Entry &t;
+    const Common &f;
+    const int cur, last, rows, cols, mp, lane, my_row, my_col, col0, col;
+    const bool tall, turned;                // turned: the other orientation is stored too
+    const float *const diagonal;
+    float *const stage;
+    float of_col[8];                        // the diagonal at this lane's columns
+
+    __device__ __forceinline__ Results(const Entry &t_, const Common &f_, int cur_, int last_, int m0, int n0, int col0_, float *stage_)
+        : t(t_), f(f_), cur(cur_), last(last_), rows(MODE == THIRD ? t.Rp : t.mp), cols(MODE == THIRD ? t.Cp : t.mp), mp(t.mp), lane(threadIdx.x & 63), my_row(lane / CPR),
+          my_col(lane % CPR * 8), col0(col0_), col(col0 + my_col), tall(t.tall != 0), turned(MODE == THIRD ? !last_ : m0 != n0), diagonal(MODE == THIRD ? t.e : t.d), stage(stage_)
+    {
+        if constexpr (WITH != 0)
+#pragma unroll
+            for (int q = 0; q < 8; q += 4) {
+                const float4 f4 = *reinterpret_cast<const float4 *>(diagonal + min(col, mp - 8) + q);
+                of_col[q] = f4.x; of_col[q + 1] = f4.y; of_col[q + 2] = f4.z; of_col[q + 3] = f4.w;
+            }
+    }
+    __device__ __forceinline__ void fetch(With &w, int row0) const
+    {
+        if constexpr (WITH != 0) {
+#pragma unroll
+            for (int k = 0; k < KI; ++k) {
+                const int row = row0 + k * ROWS + my_row;
+                const size_t at = (size_t)min(row, rows - 1) * cols + min(col, cols - 8);
+                w.v[k][0] = *reinterpret_cast<const f16x8 *>((MODE == THIRD ? t.z[cur] : t.O) + at);
+                if constexpr (WITH == 2) w.v[k][WITH - 1] = *reinterpret_cast<const f16x8 *>(t.lo + at);
+                w.of_row[k] = diagonal[min(row, mp - 1)];
+            }
+        }
+    }
+    __device__ __forceinline__ void put(const f32x16 (&acc)[NI], const With &with, int row0) const
+    {
+        const int frag_row = lane & 31, frag_k = lane >> 5;
+#pragma unroll
+        for (int j = 0; j < NI; ++j)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                *reinterpret_cast<float4 *>(stage + frag_row * PITCH + j * 32 + 8 * g + 4 * frag_k) =
+                    make_float4(acc[j][4 * g], acc[j][4 * g + 1], acc[j][4 * g + 2], acc[j][4 * g + 3]);
+        wave_sync();
+#pragma unroll
+        for (int turn = 0; turn < KI; ++turn) {
+            const int r = turn * ROWS + my_row, c = my_col, row = row0 + r;
+            float v[8];
+            *reinterpret_cast<float4 *>(v) = *reinterpret_cast<const float4 *>(stage + r * PITCH + c);
+            *reinterpret_cast<float4 *>(v + 4) = *reinterpret_cast<const float4 *>(stage + r * PITCH + c + 4);
+            f16x8 out;
+            if (row < rows && col < cols) {
+                if constexpr (MODE == SQUARE_X) {
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) {
+                        v[q] *= X_DOWN * X_DOWN;
+                        if (col + q == row) {
+                            t.d[row] = v[q];
+                            v[q] = 0.f;
+                        }
+                        out[q] = (f16_t)(v[q] * S_UP);
+                    }
+                    *reinterpret_cast<f16x8 *>(t.O + (size_t)row * mp + col) = out;
+                } else if constexpr (MODE == SQUARE_A) {
+                    const f16x8 o = with.v[turn][0];
+                    const float di = with.of_row[turn];
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) {
+                        const float s = v[q] * (S_DOWN * S_DOWN), dj = of_col[q], oq = (float)o[q] * S_DOWN;
+                        v[q] = NS_B * oq + NS_C * ((di + dj) * oq + s);
+                        if (col + q == row) {
+                            t.e[row] = NS_B * di + NS_C * (di * di + s);
+                            v[q] = 0.f;
+                        }
+                        out[q] = (f16_t)(v[q] * S_UP);
+                    }
+                    *reinterpret_cast<f16x8 *>(t.P + (size_t)row * mp + col) = out;
+                } else {
+                    const size_t at = (size_t)row * t.Cp + col;
+                    const f16x8 hi = with.v[turn][0], lo = with.v[turn][WITH ? WITH - 1 : 0];
+                    const float er = with.of_row[turn];
+                    f16x8 low;
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) {
+                        const float e = tall ? of_col[q] : er;
+                        v[q] = (NS_A + e) * ((float)hi[q] + (float)lo[q] * LO_DOWN) + v[q] * S_DOWN;       // at 2^15, as X is
+                        out[q] = (f16_t)v[q];
+                        low[q] = (f16_t)((v[q] - (float)out[q]) * LO_UP);
+                    }
+                    if (!last) {
+                        *reinterpret_cast<f16x8 *>(t.z[cur ^ 1] + at) = out;
+                        *reinterpret_cast<f16x8 *>(t.lo + at) = low;
+                    } else if (row < t.R && col < t.C) {
+                        Piece<bf16_t> copy;
+                        if (f.muon) {
+                            float *w = t.w + (size_t)row * t.C;
+#pragma unroll
+                            for (int h = 0; h < 8; h += 4) {
+                                if (col + h >= t.C) break;
+                                Piece<float> p = load_piece(w, col + h, t.C);
+                                float n[4];
+#pragma unroll
+                                for (int q = 0; q < 4; ++q) n[q] = v[h + q] = p.get(q) * f.keep - t.step * (v[h + q] * X_DOWN);
+                                p.set(n);
+                                store_piece(w, col + h, t.C, p);
+                            }
+                        } else {
+#pragma unroll
+                            for (int q = 0; q < 8; ++q) v[q] *= X_DOWN;
+                        }
+                        copy.set(v);
+                        if (t.y) store_piece(t.y + (size_t)row * t.C, col, t.C, copy);
+                    }
+                }
+                if (turned) {               // the values as stored
+                    *reinterpret_cast<float4 *>(stage + r * PITCH + c) = make_float4((float)out[0], (float)out[1], (float)out[2], (float)out[3]);
+                    *reinterpret_cast<float4 *>(stage + r * PITCH + c + 4) = make_float4((float)out[4], (float)out[5], (float)out[6], (float)out[7]);
+                }
+            }
+        }
+        wave_sync();
+        if (turned) {
+            f16_t *to = MODE == THIRD ? t.zt[cur ^ 1] : MODE == SQUARE_X ? t.O : t.P;
+#pragma unroll
+            for (int k = 0; k < WN; k += 16) {
+                const int c = k + lane / 4, r = lane % 4 * 8;
+                f16x8 out;
+#pragma unroll
+                for (int q = 0; q < 8; ++q) out[q] = (f16_t)stage[(r + q) * PITCH + c];
+                if (row0 + r < rows && col0 + c < cols) *reinterpret_cast<f16x8 *>(to + (size_t)(col0 + c) * rows + row0 + r) = out;
+            }
+            wave_sync();
+        }
+    }
+};
+
 // Tiles of BM x BN by WR x WC waves.  The reduction runs through a ring of NS stages of 64 values in LDS, filled by loads that go there directly and are issued
-// NS stages ahead; 16-byte chunk k of a row lies at chunk k ^ (row / 2 % 8), which spreads the operand fetches over the banks.
+// NS stages ahead; 16-byte chunk k of a row lies at chunk k ^ (row / 2 % 8), which spreads the operand fetches over the banks. 
+// A tile that is split leaves its sums, in the order of the registers, for finish_kernel.
 template <int BM, int BN, int NS, int WR, int WC, int MODE>
-__global__ __launch_bounds__(64 * WR * WC) void product_kernel(const Entry *table, const unsigned *map, int cur, int last, Common f)
+__global__ __launch_bounds__(64 * WR * WC) void product_kernel(const Entry *table, const unsigned *map, int cur, int last, Common f, float *partial)
 {
     constexpr int NW = WR * WC, WM = BM / WR, WN = BN / WC, MI = WM / 32, NI = WN / 32, NMF = MI * NI;
     constexpr int RPL = 8, A_LD = BM / RPL / NW, B_LD = BN / RPL / NW, L = A_LD + B_LD, KS = BK / 16;
-    constexpr int STAGE = (BM + BN) * BK * 2, PITCH = WN + 4, STAGING = NW * 32 * PITCH * 4;
+    constexpr int STAGE = (BM + BN) * BK * 2, STAGING = NW * Results<MODE, NI>::BYTES;
     static_assert(BM % (RPL * NW) == 0 && BN % (RPL * NW) == 0 && KS % 2 == 0 && L * (NS - 1) < 64, "tile");
     constexpr int LDS = STAGE * NS > STAGING ? STAGE * NS : STAGING;
     __shared__ __attribute__((aligned(1024))) unsigned char lds[LDS];
 
     const Entry &t = table[map[blockIdx.x]];
+    const Entry::Items &items = t.items[MODE];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wave_m = wave / WC * WM, wave_n = wave % WC * WN;
     const bool tall = t.tall != 0;
     const int mp = t.mp;
+    // workgroups go to the XCDs in turn: each XCD has items of the matrix that follow each other, so that its L2 serves several with what one reads
+    auto spread = [](unsigned at, unsigned count) { return at % 8 * (count / 8) + min(at % 8, count % 8) + at / 8; };
+    const unsigned at = blockIdx.x - items.first;
+    const bool whole = at < items.whole;
+    const unsigned item = whole ? spread(at, items.whole) : items.whole + spread(at - items.whole, items.count - items.whole);
+    const unsigned tile = whole ? item : items.whole + (item - items.whole) / items.split, piece = whole ? 0 : (item - items.whole) % items.split;
+    int m0, n0;
+    place<BM, BN, MODE>(t, tile, m0, n0);
 
     const f16_t *a, *b;
     int K, a_rows, b_rows;
-    unsigned ti, tj;
     if (MODE == THIRD) {
-        const unsigned tile = blockIdx.x - t.prod_first, across = (t.Cp + BN - 1) / BN;
-        ti = tile / across;
-        tj = tile % across;
         a = tall ? t.z[cur] : t.P;
         b = tall ? t.P : t.zt[cur];
         K = mp;
         a_rows = t.Rp;
         b_rows = t.Cp;
     } else {
-        static_assert(MODE == THIRD || BM == BN, "a symmetric result has square tiles");
-        triangle(blockIdx.x - t.sym_first, (mp + BM - 1) / BM, ti, tj);
         a = MODE == SQUARE_A ? t.O : tall ? t.zt[cur] : t.z[cur];
         b = a;
         K = MODE == SQUARE_A ? mp : tall ? t.Rp : t.Cp;
         a_rows = b_rows = mp;
     }
-    const int m0 = ti * BM, n0 = tj * BN;
+    const int per = whole ? K / BK : (K / BK + (int)items.split - 1) / (int)items.split, k0 = (int)piece * per, stages = max(0, min(per, K / BK - k0));
 
     // rows past the operand's lie past the resource's end: their loads give zeros
     const buf_rsrc_t rs_a = make_buf_rsrc(a, (unsigned)a_rows * (unsigned)K * 2u), rs_b = make_buf_rsrc(b, (unsigned)b_rows * (unsigned)K * 2u);
     const int ld_row = lane / 8, ld_chunk = (lane % 8) ^ ((4 * wave + ld_row / 2) % 8);
     unsigned va[A_LD], vb[B_LD];
 #pragma unroll
-    for (int i = 0; i < A_LD; ++i) va[i] = (unsigned)(m0 + RPL * (wave + NW * i) + ld_row) * (unsigned)K * 2u + ld_chunk * 16;
+    for (int i = 0; i < A_LD; ++i) va[i] = (unsigned)(m0 + RPL * (wave + NW * i) + ld_row) * (unsigned)K * 2u + ld_chunk * 16 + k0 * (BK * 2);
 #pragma unroll
-    for (int i = 0; i < B_LD; ++i) vb[i] = (unsigned)(n0 + RPL * (wave + NW * i) + ld_row) * (unsigned)K * 2u + ld_chunk * 16;
+    for (int i = 0; i < B_LD; ++i) vb[i] = (unsigned)(n0 + RPL * (wave + NW * i) + ld_row) * (unsigned)K * 2u + ld_chunk * 16 + k0 * (BK * 2);
     static_assert(NW % 2 == 0, "the chunk a lane loads is the same for all of its loads");
     auto load_task = [&](auto k, unsigned char *stage) __attribute__((always_inline)) {
         constexpr int Tk = decltype(k)::value;
@@ -284,116 +522,73 @@ __global__ __launch_bounds__(64 * WR * WC) void product_kernel(const Entry *tabl
             else load_task(IC<Tk - N_READ>{}, here);
         });
     };
-    const int stages = K / BK;
     int kt = 0;
     for (; kt + NS <= stages; kt += NS) static_for<NS>([&](auto s) __attribute__((always_inline)) { run_stage(s); });
     const int rest = stages - kt;
     if (rest >= 1) run_stage(IC<0>{});
     if constexpr (NS > 2) if (rest >= 2) run_stage(IC<1>{});
     if constexpr (NS > 3) if (rest >= 3) run_stage(IC<2>{});
+
     wait_vmcnt<0>();                        // loads past the end: nothing is under way any more
     wait_lgkmcnt0();
-    __syncthreads();
-
-    // ---- results: 32 rows of the wave's tile at a time through LDS, as fp32, in rows and then in columns ------------------------------------------------
-    float *stage = reinterpret_cast<float *>(lds) + wave * 32 * PITCH;
-    constexpr int CPR = WN / 8, ROWS = 64 / CPR;           // chunks of 8 columns in a row; rows that 64 lanes cover
+    if (!whole) {
+        float4 *to = reinterpret_cast<float4 *>(partial + (size_t)(items.part_first + (item - items.whole)) * BM * BN);
 #pragma unroll
-    for (int i = 0; i < MI; ++i) {
-        const int row0 = m0 + wave_m + i * 32, col0 = n0 + wave_n;
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int j = 0; j < NI; ++j)
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+                    to[(((wave * MI + i) * NI + j) * 4 + g) * 64 + lane] = make_float4(acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]);
+        return;
+    }
+    typedef Results<MODE, NI> Out;
+    const Out out(t, f, cur, last, m0, n0, n0 + wave_n, reinterpret_cast<float *>(lds + wave * Out::BYTES));
+    typename Out::With with[2];
+    out.fetch(with[0], m0 + wave_m);
+    ring_barrier();                         // every wave is done with the operands: their LDS is free
+    static_for<MI>([&](auto block) __attribute__((always_inline)) {
+        constexpr int i = decltype(block)::value;
+        if constexpr (i + 1 < MI) out.fetch(with[(i + 1) % 2], m0 + wave_m + (i + 1) * 32);
+        out.put(acc[i], with[i % 2], m0 + wave_m + i * 32);
+    });
+}
+
+// The sums of split tiles, their pieces added in order: a wave for 32 rows of what was a wave's tile.
+constexpr int FINISH = 2;                   // waves of a workgroup
+template <int BM, int BN, int WR, int WC, int MODE>
+__global__ __launch_bounds__(64 * FINISH) void finish_kernel(const Entry *table, const unsigned *map, int cur, int last, Common f, const float *partial)
+{
+    constexpr int NW = WR * WC, WM = BM / WR, WN = BN / WC, MI = WM / 32, NI = WN / 32;
+    typedef Results<MODE, NI> Out;
+    __shared__ __attribute__((aligned(16))) unsigned char lds[FINISH * Out::BYTES];
+    const Entry &t = table[map[blockIdx.x]];
+    const Entry::Items &items = t.items[MODE];
+    const int lane = threadIdx.x & 63, half = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const unsigned unit = (blockIdx.x - items.finish_first) * FINISH + half, wave = unit / MI % NW, i = unit % MI, q = unit / (MI * NW);
+    static_assert(NW * MI % FINISH == 0, "a tile's waves fill workgroups");
+    int m0, n0;
+    place<BM, BN, MODE>(t, items.whole + q, m0, n0);
+    const int row0 = m0 + (int)(wave / WC) * WM + (int)i * 32, col0 = n0 + (int)(wave % WC) * WN;
+    const Out out(t, f, cur, last, m0, n0, col0, reinterpret_cast<float *>(lds + half * Out::BYTES));
+    typename Out::With with;
+    out.fetch(with, row0);
+    f32x16 acc[NI];
+#pragma unroll
+    for (int j = 0; j < NI; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[j][e] = 0.f;
+    const float4 *from = reinterpret_cast<const float4 *>(partial + (size_t)(items.part_first + q * items.split) * BM * BN) + (wave * MI + i) * NI * 256 + lane;
+    for (unsigned p = 0; p < items.split; ++p, from += BM * BN / 4) {
 #pragma unroll
         for (int j = 0; j < NI; ++j)
 #pragma unroll
-            for (int g = 0; g < 4; ++g)
-                *reinterpret_cast<float4 *>(stage + frag_row * PITCH + j * 32 + 8 * g + 4 * frag_k) =
-                    make_float4(acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]);
-        wave_sync();
-#pragma unroll
-        for (int k = 0; k < 32; k += ROWS) {
-            const int r = k + lane / CPR, c = lane % CPR * 8, row = row0 + r, col = col0 + c;
-            float v[8];
-            *reinterpret_cast<float4 *>(v) = *reinterpret_cast<const float4 *>(stage + r * PITCH + c);
-            *reinterpret_cast<float4 *>(v + 4) = *reinterpret_cast<const float4 *>(stage + r * PITCH + c + 4);
-            const bool in = MODE == THIRD ? row < t.Rp && col < t.Cp : row < mp && col < mp;
-            f16x8 out;
-            if (in) {
-                if constexpr (MODE == SQUARE_X) {
-#pragma unroll
-                    for (int q = 0; q < 8; ++q) {
-                        v[q] *= X_DOWN * X_DOWN;
-                        if (col + q == row) {
-                            t.d[row] = v[q];
-                            v[q] = 0.f;
-                        }
-                        out[q] = (f16_t)(v[q] * S_UP);
-                    }
-                    *reinterpret_cast<f16x8 *>(t.O + (size_t)row * mp + col) = out;
-                } else if constexpr (MODE == SQUARE_A) {
-                    const f16x8 o = *reinterpret_cast<const f16x8 *>(t.O + (size_t)row * mp + col);
-                    const float di = t.d[row];
-#pragma unroll
-                    for (int q = 0; q < 8; ++q) {
-                        const float s = v[q] * (S_DOWN * S_DOWN), dj = t.d[col + q], oq = (float)o[q] * S_DOWN;
-                        v[q] = NS_B * oq + NS_C * ((di + dj) * oq + s);
-                        if (col + q == row) {
-                            t.e[row] = NS_B * di + NS_C * (di * di + s);
-                            v[q] = 0.f;
-                        }
-                        out[q] = (f16_t)(v[q] * S_UP);
-                    }
-                    *reinterpret_cast<f16x8 *>(t.P + (size_t)row * mp + col) = out;
-                } else {
-                    const size_t at = (size_t)row * t.Cp + col;
-                    const f16x8 hi = *reinterpret_cast<const f16x8 *>(t.z[cur] + at), lo = *reinterpret_cast<const f16x8 *>(t.lo + at);
-                    const float er = tall ? 0.f : t.e[row];
-                    f16x8 low;
-#pragma unroll
-                    for (int q = 0; q < 8; ++q) {
-                        const float e = tall ? t.e[col + q] : er;
-                        v[q] = (NS_A + e) * ((float)hi[q] + (float)lo[q] * LO_DOWN) + v[q] * S_DOWN;       // at 2^15, as X is
-                        out[q] = (f16_t)v[q];
-                        low[q] = (f16_t)((v[q] - (float)out[q]) * LO_UP);
-                    }
-                    if (!last) {
-                        *reinterpret_cast<f16x8 *>(t.z[cur ^ 1] + at) = out;
-                        *reinterpret_cast<f16x8 *>(t.lo + at) = low;
-                    } else if (row < t.R) {
-#pragma unroll
-                        for (int q = 0; q < 8; ++q) {
-                            if (col + q >= t.C) break;
-                            const size_t to = (size_t)row * t.C + col + q;
-                            if (f.muon) {
-                                const float w = t.w[to] * f.keep - t.step * (v[q] * X_DOWN);
-                                t.w[to] = w;
-                                if (t.y) t.y[to] = (bf16_t)pack_bf16x2(w, 0.f);
-                            } else {
-                                t.y[to] = (bf16_t)pack_bf16x2(v[q] * X_DOWN, 0.f);
-                            }
-                        }
-                    }
-                }
-                // the values as stored, for the other orientation
-                if (MODE == THIRD ? !last : ti != tj) {
-                    *reinterpret_cast<float4 *>(stage + r * PITCH + c) = make_float4((float)out[0], (float)out[1], (float)out[2], (float)out[3]);
-                    *reinterpret_cast<float4 *>(stage + r * PITCH + c + 4) = make_float4((float)out[4], (float)out[5], (float)out[6], (float)out[7]);
-                }
+            for (int g = 0; g < 4; ++g) {
+                const float4 v = from[(j * 4 + g) * 64];
+                acc[j][4 * g] += v.x; acc[j][4 * g + 1] += v.y; acc[j][4 * g + 2] += v.z; acc[j][4 * g + 3] += v.w;
             }
-        }
-        wave_sync();
-        if (MODE == THIRD ? !last : ti != tj) {
-            f16_t *to = MODE == THIRD ? t.zt[cur ^ 1] : MODE == SQUARE_X ? t.O : t.P;
-            const int pitch = MODE == THIRD ? t.Rp : mp, rows = MODE == THIRD ? t.Rp : mp, cols = MODE == THIRD ? t.Cp : mp;
-#pragma unroll
-            for (int k = 0; k < WN; k += 16) {
-                const int c = k + lane / 4, r = lane % 4 * 8;
-                f16x8 out;
-#pragma unroll
-                for (int q = 0; q < 8; ++q) out[q] = (f16_t)stage[(r + q) * PITCH + c];
-                if (row0 + r < rows && col0 + c < cols) *reinterpret_cast<f16x8 *>(to + (size_t)(col0 + c) * pitch + row0 + r) = out;
-            }
-            wave_sync();
-        }
     }
+    out.put(acc, with, row0);
 }
 
 // ---- a call -------------------------------------------------------------------------------------------------------------------------------------
@@ -401,10 +596,9 @@ __global__ __launch_bounds__(64 * WR * WC) void product_kernel(const Entry *tabl
 struct Sizes {
     int Rp, Cp, mp, norm_count;
     size_t mat, sq;                         // bytes of one orientation of X, of A
-    unsigned sym, prod, prep;
+    unsigned prep;
     size_t bytes;
 };
-constexpr int TILE = 128;
 Sizes sizes_of(int R, int C)
 {
     Sizes s;
@@ -415,45 +609,204 @@ Sizes sizes_of(int R, int C)
     s.norm_count = chunks < NORM_MOST ? (int)chunks : NORM_MOST;
     s.mat = align_up((size_t)s.Rp * s.Cp * 2, 256);
     s.sq = align_up((size_t)s.mp * s.mp * 2, 256);
-    const unsigned T = (s.mp + TILE - 1) / TILE;
-    s.sym = T * (T + 1) / 2;
-    s.prod = (unsigned)((s.Rp + TILE - 1) / TILE) * ((s.Cp + TILE - 1) / TILE);
     s.prep = (unsigned)(s.Rp / 64) * (s.Cp / 64);
-    s.bytes = 4 * s.mat + 2 * s.sq + 2 * align_up((size_t)s.mp * 4, 256) + NORM_MOST * 8;
+    s.bytes = 4 * s.mat + 2 * s.sq + 2 * align_up((size_t)s.mp * 4, 256) + align_up(s.norm_count * 8, 256);
     return s;
+}
+
+// A shape of tiles
+typedef void (*Product)(const Entry *, const unsigned *, int, int, Common, float *);
+typedef void (*Finish)(const Entry *, const unsigned *, int, int, Common, const float *);
+struct Shape {
+    int bm, bn, threads, per_cu;
+    double stage, alone, begin, store;      // us: a stage where all compute units are full, and where each has one workgroup at most; a tile's begin and end; what third ones store besides
+    Product product[3];
+    Finish finish[3];
+    unsigned tiles(const Sizes &s, int kind) const
+    {
+        if (kind == THIRD) return (unsigned)((s.Rp + bm - 1) / bm) * ((s.Cp + bn - 1) / bn);
+        const unsigned T = (s.mp + bm - 1) / bm;
+        return T * (T + 1) / 2;
+    }
+    unsigned finish_groups() const { return (unsigned)(bm / 32) * (bn / wn()) / FINISH; }
+    int wn() const { return bn == 64 ? 32 : 64; }
+};
+#define TILES(BM, BN, NS, WR, WC, PER_CU, ...)                                                                                                                       \
+    {BM, BN, 64 * WR * WC, PER_CU, __VA_ARGS__,                                                                                                                        \
+     {product_kernel<BM, BN, NS, WR, WC, SQUARE_X>, product_kernel<BM, BN, NS, WR, WC, SQUARE_A>, product_kernel<BM, BN, NS, WR, WC, THIRD>}, \
+     {finish_kernel<BM, BN, WR, WC, SQUARE_X>, finish_kernel<BM, BN, WR, WC, SQUARE_A>, finish_kernel<BM, BN, WR, WC, THIRD>}}
+// (times measured on 512 x 512 to 8192 x 8192; the model is within a tenth of most launches, S of a quarter)
+constexpr int KINDS = 3, SHAPE_COUNT = 4;
+const Shape SHAPES[SHAPE_COUNT] = {TILES(64, 64, 4, 2, 2, 2, 0.38, 0.26, 4.5, 2), TILES(128, 128, 2, 2, 2, 2, 1.0, 0.66, 10, 14), TILES(192, 192, 2, 2, 3, 1, 1.13, 1.13, 14, 18),
+                                   TILES(256, 256, 2, 2, 4, 1, 1.35, 1.35, 18, 33)};
+
+// tiles and stages of a reduction
+struct Load {
+    unsigned tiles;
+    int stages;
+};
+int stages_of(const Sizes &s, int kind) { return (kind == SQUARE_X && s.Rp != s.mp ? s.Rp : kind == SQUARE_X ? s.Cp : s.mp) / BK; }
+// Time of a launch of these loads, longest first, each going to the workgroup slots that are free first.  `busy` is for slots and the time they are free at, earliest first.
+struct Busy {
+    double us;
+    unsigned slots;
+};
+double time_of(const Shape &h, int kind, const Load *loads, int count, std::vector<Busy> &busy)
+{
+    const unsigned slots = 256 * h.per_cu;
+    unsigned total = 0;
+    for (int k = 0; k < count; ++k) total += loads[k].tiles;
+    const double fill = total < slots ? (double)total / slots : 1.0;
+    busy.assign(1, Busy{0.0, slots});
+    double last = 0.0;
+    for (int k = 0; k < count;) {
+        const int stages = loads[k].stages;
+        unsigned tiles = 0;
+        for (; k < count && loads[k].stages == stages; ++k) tiles += loads[k].tiles;
+        while (tiles) {
+            const Busy b = busy.front();
+            const unsigned n = std::min(tiles, b.slots);
+            const double us = b.us + stages * (total > 256 && (b.us == 0.0 || tiles > 256) ? h.stage : h.alone) + h.begin + (kind == THIRD ? h.store * fill : 0.0);
+            if (n == b.slots) busy.erase(busy.begin());
+            else busy.front().slots -= n;
+            size_t at = 0;
+            while (at < busy.size() && busy[at].us < us) ++at;
+            busy.insert(busy.begin() + at, Busy{us, n});
+            last = std::max(last, us);
+            tiles -= n;
+        }
+    }
+    return last;
+}
+// The tiles that a matrix's launch leaves for a last round, or all of few, may be split over the reduction.  This goes by the matrix alone, for it decides the order of sums: a call's
+// results do not depend on its other matrices.  8192 x 8192: 528 tiles of 256 on 256 compute units, 620 us; the last 16 of them in 16 pieces each 505.
+struct Split {
+    int shape;                              // or -1
+    unsigned whole, by;
+};
+Split split_of(const Sizes &s, int kind, std::vector<Busy> &busy)
+{
+    Split best = {-1, 0, 1};
+    double least = 1e30, unsplit = 1e30;
+    const int stages = stages_of(s, kind);
+    for (int i = 0; i < SHAPE_COUNT; ++i) {
+        const Shape &h = SHAPES[i];
+        const Load all = {h.tiles(s, kind), stages};
+        const unsigned slots = 256 * h.per_cu, rest = all.tiles % slots;
+        unsplit = std::min(unsplit, time_of(h, kind, &all, 1, busy));
+        unsigned by = rest ? std::min(slots / rest, 16u) : 1;
+        by = std::min(by, (unsigned)stages / 8);
+        if (by < 2) continue;
+        const Load rounds = {all.tiles - rest, stages}, pieces = {rest * by, (int)((stages + by - 1) / by)};
+        // the pieces' sums are written and read at some 5 TB/s
+        const double us = (rounds.tiles ? time_of(h, kind, &rounds, 1, busy) : 0.0) + time_of(h, 0, &pieces, 1, busy) + 6.0 + pieces.tiles * (h.bm * h.bn * 8.0 / 5e6) + (kind == THIRD ? h.store * rest / slots : 0.0);
+        if (us < least) {
+            least = us;
+            best = {i, all.tiles - rest, by};
+        }
+    }
+    if (unsplit - least < 10.0) best.shape = -1;
+    return best;
+}
+
+// What a call of these matrices launches
+struct Plan {
+    std::vector<Entry::Items> items[KINDS];
+    unsigned count[KINDS][SHAPE_COUNT], finish[KINDS][SHAPE_COUNT], prep;
+    size_t parts, bytes;                    // bytes of partial sums; of the workspace
+};
+Plan plan_of(int count, const int *rows, const int *cols)
+{
+    Plan p = {};
+    std::vector<Sizes> sizes(count);
+    std::vector<Split> split(count);
+    std::vector<int> order(count);
+    std::vector<Load> loads(count);
+    std::vector<Busy> busy;
+    p.bytes = align_up((size_t)count * sizeof(Entry), 256);
+    for (int i = 0; i < count; ++i) {
+        sizes[i] = sizes_of(rows[i], cols[i]);
+        p.bytes += sizes[i].bytes;
+        p.prep += sizes[i].prep;
+    }
+    p.bytes += align_up((size_t)p.prep * 4, 256);
+    for (int kind = 0; kind < KINDS; ++kind) {
+        // longest reductions first
+        for (int i = 0; i < count; ++i) order[i] = i;
+        std::stable_sort(order.begin(), order.end(), [&](int a, int b) { return stages_of(sizes[a], kind) > stages_of(sizes[b], kind); });
+        for (int i = 0; i < count; ++i) split[i] = split_of(sizes[i], kind, busy);
+        // the others have one shape, that of the least time
+        int shape = 0;
+        double least = 1e30;
+        for (int i = 0; i < SHAPE_COUNT; ++i) {
+            int n = 0;
+            for (int k = 0; k < count; ++k)
+                if (split[order[k]].shape < 0) loads[n++] = {SHAPES[i].tiles(sizes[order[k]], kind), stages_of(sizes[order[k]], kind)};
+            const double us = n ? time_of(SHAPES[i], kind, loads.data(), n, busy) : 0.0;
+            if (us < least) {
+                least = us;
+                shape = i;
+            }
+        }
+        p.items[kind].resize(count);
+        size_t parts[SHAPE_COUNT] = {};
+        for (int k = 0; k < count; ++k) {
+            const int i = order[k], at = split[i].shape < 0 ? shape : split[i].shape;
+            const Shape &h = SHAPES[at];
+            Entry::Items &t = p.items[kind][i];
+            const unsigned tiles = h.tiles(sizes[i], kind);
+            t.first = p.count[kind][at];
+            t.whole = split[i].shape < 0 ? tiles : split[i].whole;
+            t.split = split[i].by;
+            t.count = t.whole + (tiles - t.whole) * t.split;
+            t.part_first = (unsigned)parts[at];
+            t.finish_first = p.finish[kind][at];
+            t.finish_count = (tiles - t.whole) * h.finish_groups();
+            t.shape = at;
+            parts[at] += (tiles - t.whole) * t.split;
+            p.finish[kind][at] += t.finish_count;
+            p.count[kind][at] += t.count;
+        }
+        for (int i = 0; i < SHAPE_COUNT; ++i) {
+            p.parts = std::max(p.parts, align_up(parts[i] * SHAPES[i].bm * SHAPES[i].bn * 4, 256));
+            p.bytes += align_up((size_t)p.count[kind][i] * 4, 256) + align_up((size_t)p.finish[kind][i] * 4, 256);
+        }
+    }
+    p.bytes += p.parts;
+    return p;
 }
 int launched() { return hipGetLastError() == hipSuccess ? MXC_OK : MXC_ERR_LAUNCH; }
 
 }  // namespace
 
-size_t muon_workspace(int count, const int *rows, const int *cols)
+// (the plan's lists are the library's only memory of its own; a call that has none is refused)
+int muon_workspace(int count, const int *rows, const int *cols, size_t *bytes)
 {
-    size_t bytes = align_up((size_t)count * sizeof(Entry), 256), sym = 0, prod = 0, prep = 0;
-    for (int i = 0; i < count; ++i) {
-        const Sizes s = sizes_of(rows[i], cols[i]);
-        bytes += s.bytes;
-        sym += s.sym;
-        prod += s.prod;
-        prep += s.prep;
+    try {
+        *bytes = plan_of(count, rows, cols).bytes;
+        return MXC_OK;
+    } catch (const std::bad_alloc &) {
+        return MXC_ERR_LAUNCH;
     }
-    return bytes + align_up(sym * 4, 256) + align_up(prod * 4, 256) + align_up(prep * 4, 256);
 }
 
-int muon_run(const MuonArgs &q, void *ws, hipStream_t st)
+static int run(const MuonArgs &q, void *ws, size_t ws_bytes, hipStream_t st)
 {
+    const Plan p = plan_of(q.count, q.rows, q.cols);
+    if (!ws || ws_bytes < p.bytes) return MXC_ERR_WORKSPACE;
     char *at = (char *)ws;
-    auto take = [&](size_t bytes) { char *p = at; at += align_up(bytes, 256); return p; };
-    size_t sym = 0, prod = 0, prep = 0;
-    for (int i = 0; i < q.count; ++i) {
-        const Sizes s = sizes_of(q.rows[i], q.cols[i]);
-        sym += s.sym;
-        prod += s.prod;
-        prep += s.prep;
-    }
+    auto take = [&](size_t bytes) { char *to = at; at += align_up(bytes, 256); return to; };
     Entry *table = (Entry *)take((size_t)q.count * sizeof(Entry));
-    unsigned *sym_map = (unsigned *)take(sym * 4), *prod_map = (unsigned *)take(prod * 4), *prep_map = (unsigned *)take(prep * 4);
+    Maps maps;
+    maps.prep = (unsigned *)take((size_t)p.prep * 4);
+    for (int kind = 0; kind < KINDS; ++kind)
+        for (int i = 0; i < SHAPE_COUNT; ++i) {
+            maps.items[kind][i] = (unsigned *)take((size_t)p.count[kind][i] * 4);
+            maps.finish[kind][i] = (unsigned *)take((size_t)p.finish[kind][i] * 4);
+        }
+    float *partial = (float *)take(p.parts);
     const Common f = {q.momentum, q.grad_scale, q.keep, q.nesterov, q.w != nullptr, q.dtype == MXC_BF16};
-    unsigned sym_at = 0, prod_at = 0, prep_at = 0;
+    unsigned prep_at = 0;
     for (int base = 0; base < q.count; base += GROUP) {
         Group g;
         g.base = base;
@@ -479,29 +832,44 @@ int muon_run(const MuonArgs &q, void *ws, hipStream_t st)
             t.P = (f16_t *)take(s.sq);
             t.d = (float *)take((size_t)s.mp * 4);
             t.e = (float *)take((size_t)s.mp * 4);
-            t.norm = (double *)take(NORM_MOST * 8);
-            t.sym_first = sym_at; t.prod_first = prod_at; t.prep_first = prep_at;
-            t.sym_count = s.sym; t.prod_count = s.prod; t.prep_count = s.prep;
-            sym_at += s.sym; prod_at += s.prod; prep_at += s.prep;
+            t.norm = (double *)take((size_t)s.norm_count * 8);
+            t.prep_first = prep_at;
+            t.prep_count = s.prep;
+            prep_at += s.prep;
+            for (int kind = 0; kind < KINDS; ++kind) t.items[kind] = p.items[kind][i];
             g.first[k] = blocks;
             blocks += s.norm_count;
         }
         g.first[g.count] = blocks;
-        hipLaunchKernelGGL(norm_kernel, dim3(blocks), dim3(256), 0, st, g, f, table, sym_map, prod_map, prep_map);
+        hipLaunchKernelGGL(f.bf16 ? norm_kernel<true> : norm_kernel<false>, dim3(blocks), dim3(256), 0, st, g, f, table, maps);
         if (launched() != MXC_OK) return MXC_ERR_LAUNCH;
     }
-    hipLaunchKernelGGL(prepare_kernel, dim3(prep_at), dim3(256), 0, st, f, table, prep_map);
+    hipLaunchKernelGGL(f.bf16 ? prepare_kernel<true> : prepare_kernel<false>, dim3(prep_at), dim3(256), 0, st, f, table, maps.prep);
     if (launched() != MXC_OK) return MXC_ERR_LAUNCH;
     for (int k = 0; k < q.steps; ++k) {
         const int cur = k & 1, last = k == q.steps - 1;
-        hipLaunchKernelGGL((product_kernel<TILE, TILE, 2, 2, 2, SQUARE_X>), dim3(sym_at), dim3(256), 0, st, table, sym_map, cur, last, f);
-        if (launched() != MXC_OK) return MXC_ERR_LAUNCH;
-        hipLaunchKernelGGL((product_kernel<TILE, TILE, 2, 2, 2, SQUARE_A>), dim3(sym_at), dim3(256), 0, st, table, sym_map, cur, last, f);
-        if (launched() != MXC_OK) return MXC_ERR_LAUNCH;
-        hipLaunchKernelGGL((product_kernel<TILE, TILE, 2, 2, 2, THIRD>), dim3(prod_at), dim3(256), 0, st, table, prod_map, cur, last, f);
-        if (launched() != MXC_OK) return MXC_ERR_LAUNCH;
+        for (int mode = SQUARE_X; mode <= THIRD; ++mode) {
+            for (int i = 0; i < SHAPE_COUNT; ++i) {
+                if (!p.count[mode][i]) continue;
+                const Shape &h = SHAPES[i];
+                hipLaunchKernelGGL(h.product[mode], dim3(p.count[mode][i]), dim3(h.threads), 0, st, table, maps.items[mode][i], cur, last, f, partial);
+                if (launched() != MXC_OK) return MXC_ERR_LAUNCH;
+                if (!p.finish[mode][i]) continue;
+                hipLaunchKernelGGL(h.finish[mode], dim3(p.finish[mode][i]), dim3(64 * FINISH), 0, st, table, maps.finish[mode][i], cur, last, f, partial);
+                if (launched() != MXC_OK) return MXC_ERR_LAUNCH;
+            }
+        }
     }
     return MXC_OK;
+}
+
+int muon_run(const MuonArgs &q, void *ws, size_t ws_bytes, hipStream_t st)
+{
+    try {
+        return run(q, ws, ws_bytes, st);
+    } catch (const std::bad_alloc &) {
+        return MXC_ERR_LAUNCH;
+    }
 }
 
 }  // namespace mxc

@@ -335,8 +335,8 @@ struct MuonArgs {
     float momentum, grad_scale, keep;
     double lr, rms;
 };
-size_t muon_workspace(int count, const int *rows, const int *cols);
-int muon_run(const MuonArgs &a, void *ws, hipStream_t st);
+int muon_workspace(int count, const int *rows, const int *cols, size_t *bytes);
+int muon_run(const MuonArgs &a, void *ws, size_t ws_bytes, hipStream_t st);     // MXC_ERR_WORKSPACE, before anything is launched
 
 // ---- logprob.hip: log probabilities, entropies, top tokens and their gradient -------------
 size_t logprob_workspace(int N, int K, int dtype, int top);
