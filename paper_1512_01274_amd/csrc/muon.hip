@@ -25,6 +25,7 @@ namespace {
 
 typedef _Float16 f16_t;
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr float NS_A = 3.4445f, NS_B = -4.7750f, NS_C = 2.0315f;
@@ -32,7 +33,7 @@ constexpr float NS_A = 3.4445f, NS_B = -4.7750f, NS_C = 2.0315f;
 constexpr float X_UP = 32768.f, X_DOWN = 1.f / 32768.f, LO_UP = 2048.f, LO_DOWN = 1.f / 2048.f, S_UP = 16384.f, S_DOWN = 1.f / 16384.f;
 
 constexpr int BK = 64;                      // reduction of a stage, and what sides are padded to
-constexpr int NORM_MOST = 1024, NORM_CHUNK = 8192;
+constexpr int NORM_MOST = 1024, NORM_CHUNK = 2048;
 
 // One matrix of a call.  Z is ping-ponged where the third product reads it (tall), its transpose where it does not (wide); the other pair of pointers is one buffer.
 struct Entry {
@@ -65,6 +66,19 @@ struct Common {
     int nesterov, muon, bf16;
 };
 
+// The arithmetic of each value, the same wherever it is done: a product and a sum that the compiler may or may not join, or a sum that it may round to 16 bits without
+// rounding to 32 first, would differ from kernel to kernel.
+__device__ __forceinline__ float in_32_bits(float x)
+{
+    asm("" : "+v"(x));
+    return x;
+}
+__device__ __forceinline__ float b_of(float o, float di, float dj, float sum) { return in_32_bits(__builtin_fmaf(NS_C, __builtin_fmaf(di + dj, o, sum), NS_B * o)); }        // off the diagonal
+__device__ __forceinline__ float e_of(float d, float sum) { return __builtin_fmaf(NS_C, __builtin_fmaf(d, d, sum), NS_B * d); }                                  // on it
+__device__ __forceinline__ float x_of(float e, f16_t hi, f16_t lo, float sum) { return in_32_bits(__builtin_fmaf(NS_A + e, __builtin_fmaf((float)lo, LO_DOWN, (float)hi), sum * S_DOWN)); }
+__device__ __forceinline__ f16_t rest_of(float x, f16_t hi) { return (f16_t)((x - (float)hi) * LO_UP); }
+__device__ __forceinline__ float w_of(float w, float x, float keep, float step) { return __builtin_fmaf(-step, x * X_DOWN, w * keep); }
+
 // whether the momentum is still to be made of the gradient, and where it goes
 struct ToMake {
     static constexpr bool fresh = true;
@@ -79,7 +93,7 @@ struct Made {
 
 // four values of the matrix that is made orthogonal, from column c of row r: x, or the momentum's part (m: as it is after norm_kernel)
 template <bool BF16, class M>
-__device__ __forceinline__ void values_at(const Entry &t, const Common &f, const void *u, const float *m, int c, int len, float (&v)[4], M &&made)
+__device__ __forceinline__ void values_at(const Common &f, const void *u, const float *m, int c, int len, float (&v)[4], M &&made)
 {
     if (!f.muon || f.nesterov || made.fresh) {
         if constexpr (BF16) {
@@ -98,8 +112,8 @@ __device__ __forceinline__ void values_at(const Entry &t, const Common &f, const
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const float g = v[i] * f.grad_scale;
-            n[i] = made.fresh ? q.get(i) * f.momentum + g : q.get(i);
-            v[i] = f.nesterov ? g + n[i] * f.momentum : n[i];
+            n[i] = made.fresh ? __builtin_fmaf(q.get(i), f.momentum, g) : q.get(i);
+            v[i] = f.nesterov ? __builtin_fmaf(n[i], f.momentum, g) : n[i];
         }
         if (made.fresh) {
             q.set(n);
@@ -140,9 +154,9 @@ __global__ __launch_bounds__(256) void norm_kernel(Group q, Common f, Entry *tab
 #pragma unroll 4
     for (long long k = (long long)(part * 256 + threadIdx.x) * 4; k < n; k += (long long)t.norm_count * 1024) {
         float v[4];
-        values_at<BF16>(t, f, u, m, (int)k, n, v, ToMake{m, (int)k, n});
+        values_at<BF16>(f, u, m, (int)k, n, v, ToMake{m, (int)k, n});
 #pragma unroll
-        for (int j = 0; j < 4; ++j) s += k + j < n ? (double)v[j] * (double)v[j] : 0.0;
+        for (int j = 0; j < 4; ++j) s = k + j < n ? __builtin_fma((double)v[j], (double)v[j], s) : s;
     }
     __shared__ double wave_sum[4];
 #pragma unroll
@@ -152,12 +166,19 @@ __global__ __launch_bounds__(256) void norm_kernel(Group q, Common f, Entry *tab
     if (threadIdx.x == 0) t.norm[part] = wave_sum[0] + wave_sum[1] + wave_sum[2] + wave_sum[3];
 }
 
+// 1 / norm, at X's power of two, as a power of two and a factor of ordinary size.  A value that is not finite makes NaN of the whole matrix; zeros stay zeros
+__device__ __forceinline__ float over_norm(double squares, int &up)
+{
+    up = 0;
+    const double norm = frexp(sqrt(squares), &up);
+    return !(squares < 1e300) ? __builtin_nanf("") : squares > 0.0 ? (float)((double)X_UP / norm) : 0.f;
+}
+
 // ---- X over its norm, in both orientations: a workgroup for 64 x 64 values -----------------------------------------------------------------------
 
 template <bool BF16>
 __global__ __launch_bounds__(256) void prepare_kernel(Common f, const Entry *table, const unsigned *map)
 {
-    typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
     const Entry &t = table[map[blockIdx.x]];
     const unsigned tile = blockIdx.x - t.prep_first, across = t.Cp / 64;
     const int r0 = tile / across * 64, c0 = tile % across * 64;
@@ -172,7 +193,7 @@ __global__ __launch_bounds__(256) void prepare_kernel(Common f, const Entry *tab
         for (int i = 0; i < 4; ++i) v[k][i] = 0.f;
         if (r < t.R && c0 + c < t.C) {
             const size_t at = (size_t)r * t.C;
-            values_at<BF16>(t, f, BF16 ? (const void *)((const bf16_t *)t.u + at) : (const void *)((const float *)t.u + at), t.m + at, c0 + c, t.C, v[k], Made{});
+            values_at<BF16>(f, BF16 ? (const void *)((const bf16_t *)t.u + at) : (const void *)((const float *)t.u + at), t.m + at, c0 + c, t.C, v[k], Made{});
         }
     }
     double s = 0.0;
@@ -182,19 +203,17 @@ __global__ __launch_bounds__(256) void prepare_kernel(Common f, const Entry *tab
     if ((threadIdx.x & 63) == 0) wave_sum[threadIdx.x >> 6] = s;
     __syncthreads();
     s = wave_sum[0] + wave_sum[1] + wave_sum[2] + wave_sum[3];
-    // 1 / norm as a power of two and a factor of ordinary size.  A value that is not finite makes NaN of the whole matrix; zeros stay zeros
-    int up = 0;
-    const double norm = frexp(sqrt(s), &up);
-    const float by = !(s < 1e300) ? __builtin_nanf("") : s > 0.0 ? (float)((double)X_UP / norm) : 0.f;
+    int up;
+    const float by = over_norm(s, up);
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         f16x4 hi, lo;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const bool in = r0 + k * 16 + row < t.R && c0 + c + i < t.C;
-            const float x = in ? ldexpf(v[k][i], -up) * by : 0.f;
+            const float x = in ? in_32_bits(ldexpf(v[k][i], -up) * by) : 0.f;
             hi[i] = (f16_t)x;
-            lo[i] = (f16_t)((x - (float)hi[i]) * LO_UP);
+            lo[i] = rest_of(x, hi[i]);
             turned[c + i][k * 16 + row] = hi[i];
         }
         const size_t to = (size_t)(r0 + k * 16 + row) * t.Cp + c0 + c;
@@ -332,10 +351,10 @@ struct Results {
                     const float di = with.of_row[turn];
 #pragma unroll
                     for (int q = 0; q < 8; ++q) {
-                        const float s = v[q] * (S_DOWN * S_DOWN), dj = of_col[q], oq = (float)o[q] * S_DOWN;
-                        v[q] = NS_B * oq + NS_C * ((di + dj) * oq + s);
+                        const float s = v[q] * (S_DOWN * S_DOWN);
+                        v[q] = b_of((float)o[q] * S_DOWN, di, of_col[q], s);
                         if (col + q == row) {
-                            t.e[row] = NS_B * di + NS_C * (di * di + s);
+                            t.e[row] = e_of(di, s);
                             v[q] = 0.f;
                         }
                         out[q] = (f16_t)(v[q] * S_UP);
@@ -349,9 +368,9 @@ struct Results {
 #pragma unroll
                     for (int q = 0; q < 8; ++q) {
                         const float e = tall ? of_col[q] : er;
-                        v[q] = (NS_A + e) * ((float)hi[q] + (float)lo[q] * LO_DOWN) + v[q] * S_DOWN;       // at 2^15, as X is
+                        v[q] = x_of(e, hi[q], lo[q], v[q]);       // at 2^15, as X is
                         out[q] = (f16_t)v[q];
-                        low[q] = (f16_t)((v[q] - (float)out[q]) * LO_UP);
+                        low[q] = rest_of(v[q], out[q]);
                     }
                     if (!last) {
                         *reinterpret_cast<f16x8 *>(t.z[cur ^ 1] + at) = out;
@@ -366,7 +385,7 @@ struct Results {
                                 Piece<float> p = load_piece(w, col + h, t.C);
                                 float n[4];
 #pragma unroll
-                                for (int q = 0; q < 4; ++q) n[q] = v[h + q] = p.get(q) * f.keep - t.step * (v[h + q] * X_DOWN);
+                                for (int q = 0; q < 4; ++q) n[q] = v[h + q] = w_of(p.get(q), v[h + q], f.keep, t.step);
                                 p.set(n);
                                 store_piece(w, col + h, t.C, p);
                             }
@@ -591,6 +610,227 @@ __global__ __launch_bounds__(64 * FINISH) void finish_kernel(const Entry *table,
     out.put(acc, with, row0);
 }
 
+// ---- matrices that a compute unit holds -----------------------------------------------------------------------------------------------------------
+//
+// All steps in one launch, a workgroup for a matrix of up to 64 by 576 (either way): X's first parts lie in LDS in both orientations, its second ones in the registers of
+// the waves that form them; 16-byte chunks of a row are exchanged so that 16 rows of a fetch fall into different banks.  The same operations in the same order as in the
+// kernels above, with the same bits.  One 64 x 363 matrix: 95 us of 17 launches before.
+
+constexpr int SMALL_M = 64, SMALL_N = 576, SMALL_NT = 1024, SMALL_GROUP = 72, SMALL_PARTS = (SMALL_M * SMALL_N + NORM_CHUNK - 1) / NORM_CHUNK;
+struct SmallEntry {
+    int R, C;
+    float step;
+    const void *u;
+    bf16_t *y;
+    float *w, *m;
+};
+struct SmallGroup {
+    SmallEntry t[SMALL_GROUP];
+};
+static_assert(sizeof(SmallGroup) + sizeof(Common) + 16 <= 4096, "kernel arguments");
+template <bool BF16>
+__global__ __launch_bounds__(SMALL_NT) void small_kernel(SmallGroup q, Common f, int steps)
+{
+    constexpr int MOST = (SMALL_N / 32 * 2 + 15) / 16;         // 32 x 32 blocks of X of a wave
+    __shared__ __attribute__((aligned(256))) unsigned char lds[SMALL_M * SMALL_N * 4 + 8192];
+    __shared__ float diagonal[2][SMALL_M];                     // d, e
+    __shared__ double part_sum[SMALL_PARTS][4];
+    __shared__ double all_squares;
+    const SmallEntry &t = q.t[blockIdx.x];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int l32 = lane & 31, half = lane >> 5;
+    const bool tall = t.R > t.C;
+    const int m = tall ? t.C : t.R, n = tall ? t.R : t.C, np = (n + BK - 1) / BK * BK;
+    const void *const u = t.u;
+    float *const mom = t.m;
+
+    // the squares, and the momentum: as norm_kernel's workgroups of 256, four at a time
+    const int values = t.R * t.C, parts = (values + NORM_CHUNK - 1) / NORM_CHUNK, tid = threadIdx.x & 255;
+    for (int part = threadIdx.x >> 8; part < parts; part += 4) {
+        double s = 0.0;
+        for (int k = (part * 256 + tid) * 4; k < values; k += parts * 1024) {
+            float v[4];
+            values_at<BF16>(f, u, mom, k, values, v, ToMake{mom, k, values});
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s = k + j < values ? __builtin_fma((double)v[j], (double)v[j], s) : s;
+        }
+#pragma unroll
+        for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
+        if (lane == 0) part_sum[part][wave & 3] = s;
+    }
+    __syncthreads();
+    if (wave == 0) {
+        double s = lane < parts ? part_sum[lane][0] + part_sum[lane][1] + part_sum[lane][2] + part_sum[lane][3] : 0.0;
+#pragma unroll
+        for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
+        if (lane == 0) all_squares = s + 0.0 + 0.0 + 0.0;
+    }
+    __syncthreads();
+    int up;
+    const float by = over_norm(all_squares, up);
+
+    // where 16-byte chunk c of a row lies: X [64][np], its transpose [np][64], A and B [64][64]
+    unsigned char *const z = lds, *const zt = lds + SMALL_M * 2 * np, *const sq = lds + SMALL_M * 4 * np;
+    const bool odd = np / 64 % 2 != 0;
+    auto z_at = [&](int r, int c) __attribute__((always_inline)) { return z + r * np * 2 + ((c ^ (odd ? r >> 1 & 7 : r & 15)) << 4); };
+    auto narrow_at = [](unsigned char *base, int r, int c) __attribute__((always_inline)) { return base + r * 128 + ((c ^ (r >> 1 & 7)) << 4); };
+
+    // this wave's blocks of X: rows 32 * (b % 2), columns 32 * (b / 2) of block b; a lane has row l32 and of the columns 8 g + 4 half + 0 .. 3
+    const int blocks = np / 32 * 2;
+    f16x4 hi[MOST][4], lo[MOST][4];
+    auto put_x = [&](int b, int g, const f16x4 &x) __attribute__((always_inline)) {
+        const int r = b % 2 * 32 + l32, c = b / 2 * 32 + 8 * g + 4 * half;
+        *reinterpret_cast<f16x4 *>(z_at(r, c / 8) + half * 8) = x;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) *reinterpret_cast<f16_t *>(narrow_at(zt, c + i, r / 8) + r % 8 * 2) = x[i];
+    };
+#pragma unroll
+    for (int k = 0; k < MOST; ++k) {
+        const int b = wave + 16 * k, r = b % 2 * 32 + l32;
+        if (b >= blocks) break;
+        float v[4][4];
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int c = b / 2 * 32 + 8 * g + 4 * half;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[g][i] = 0.f;
+            if (r >= m || c >= n) continue;
+            if (!tall) {
+                const int at = r * n;
+                values_at<BF16>(f, BF16 ? (const void *)((const bf16_t *)u + at) : (const void *)((const float *)u + at), mom + at, c, n, v[g], Made{});
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (c + i >= n) break;
+                    const int at = (c + i) * m + r;
+                    float one = 0.f;
+                    if (!f.muon || f.nesterov) one = BF16 ? bf16_to_f32(((const bf16_t *)u)[at]) : ((const float *)u)[at];
+                    if (f.muon) one = f.nesterov ? __builtin_fmaf(mom[at], f.momentum, one * f.grad_scale) : mom[at];
+                    v[g][i] = one;
+                }
+            }
+        }
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int c = b / 2 * 32 + 8 * g + 4 * half;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float x = r < m && c + i < n ? in_32_bits(ldexpf(v[g][i], -up) * by) : 0.f;
+                hi[k][g][i] = (f16_t)x;
+                lo[k][g][i] = rest_of(x, hi[k][g][i]);
+            }
+            put_x(b, g, hi[k][g]);
+        }
+        asm volatile("" ::: "memory");      // a block after the other: their values together are more than the registers
+    }
+    __syncthreads();
+
+    for (int step = 0; step < steps; ++step) {
+        // addresses are worked out in each step: all of them at once are more than the registers
+        asm volatile("" : "+v"(l32), "+v"(half));
+        const bool last = step == steps - 1;
+        const int ti = wave >> 1, tj = wave & 1, row = ti * 32 + l32;
+        f16x4 out[4];
+        if (wave < 4) {
+            f32x16 acc;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[e] = 0.f;
+#pragma unroll 4
+            for (int c = half; c < np / 8; c += 2) {
+                const f16x8 a = *reinterpret_cast<const f16x8 *>(z_at(row, c)), b = *reinterpret_cast<const f16x8 *>(z_at(tj * 32 + l32, c));
+                acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(b, a, acc, 0, 0, 0);
+            }
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int c = tj * 32 + 8 * g + 4 * half;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float x = acc[4 * g + i] * (X_DOWN * X_DOWN);
+                    if (c + i == row) {
+                        diagonal[0][row] = x;
+                        x = 0.f;
+                    }
+                    out[g][i] = (f16_t)(x * S_UP);
+                }
+                *reinterpret_cast<f16x4 *>(narrow_at(sq, row, c / 8) + half * 8) = out[g];
+            }
+        }
+        __syncthreads();
+        if (wave < 4) {
+            f32x16 acc;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[e] = 0.f;
+#pragma unroll
+            for (int c = 0; c < 8; c += 2) {
+                const f16x8 a = *reinterpret_cast<const f16x8 *>(narrow_at(sq, row, c + half)), b = *reinterpret_cast<const f16x8 *>(narrow_at(sq, tj * 32 + l32, c + half));
+                acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(b, a, acc, 0, 0, 0);
+            }
+            const float di = diagonal[0][row];
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int c = tj * 32 + 8 * g + 4 * half;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float s = acc[4 * g + i] * (S_DOWN * S_DOWN);
+                    float x = b_of((float)out[g][i] * S_DOWN, di, diagonal[0][c + i], s);
+                    if (c + i == row) {
+                        diagonal[1][row] = e_of(di, s);
+                        x = 0.f;
+                    }
+                    out[g][i] = (f16_t)(x * S_UP);
+                }
+            }
+        }
+        __syncthreads();                    // O has been read
+        if (wave < 4)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) *reinterpret_cast<f16x4 *>(narrow_at(sq, row, tj * 4 + g) + half * 8) = out[g];
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < MOST; ++k) {
+            const int b = wave + 16 * k, r = b % 2 * 32 + l32;
+            if (b >= blocks) continue;
+            f32x16 acc;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[e] = 0.f;
+#pragma unroll
+            for (int c = 0; c < 8; c += 2) {
+                const f16x8 x = *reinterpret_cast<const f16x8 *>(narrow_at(sq, r, c + half)), y = *reinterpret_cast<const f16x8 *>(narrow_at(zt, b / 2 * 32 + l32, c + half));
+                acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(y, x, acc, 0, 0, 0);
+            }
+            const float e = diagonal[1][r];
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                float x[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    x[i] = x_of(e, hi[k][g][i], lo[k][g][i], acc[4 * g + i]);
+                    hi[k][g][i] = (f16_t)x[i];
+                    lo[k][g][i] = rest_of(x[i], hi[k][g][i]);
+                }
+                if (!last) continue;
+                const int c = b / 2 * 32 + 8 * g + 4 * half;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (r >= m || c + i >= n) continue;
+                    const int at = tall ? (c + i) * m + r : r * n + c + i;
+                    float o = x[i] * X_DOWN;
+                    if (f.muon) t.w[at] = o = w_of(t.w[at], x[i], f.keep, t.step);
+                    if (t.y) t.y[at] = Piece<bf16_t>::rounded(o);
+                }
+            }
+        }
+        if (last) break;
+        __syncthreads();                    // X and B have been read
+#pragma unroll
+        for (int k = 0; k < MOST; ++k)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                if (wave + 16 * k < blocks) put_x(wave + 16 * k, g, hi[k][g]);
+        __syncthreads();
+    }
+}
+
 // ---- a call -------------------------------------------------------------------------------------------------------------------------------------
 
 struct Sizes {
@@ -775,6 +1015,15 @@ Plan plan_of(int count, const int *rows, const int *cols)
     p.bytes += p.parts;
     return p;
 }
+// whether every matrix of a call fits a compute unit: then the call is one launch for SMALL_GROUP of them, without a workspace.  (Beside larger ones they are
+// less than a round of the tiles' launches.)
+bool all_small(int count, const int *rows, const int *cols)
+{
+    for (int i = 0; i < count; ++i)
+        if (std::min(rows[i], cols[i]) > SMALL_M || std::max(rows[i], cols[i]) > SMALL_N) return false;
+    return true;
+}
+float step_of(const MuonArgs &q, int R, int C) { return (float)(q.lr * (q.rms > 0.0 ? q.rms * sqrt((double)std::max(R, C)) : R > C ? sqrt((double)R / C) : 1.0)); }
 int launched() { return hipGetLastError() == hipSuccess ? MXC_OK : MXC_ERR_LAUNCH; }
 
 }  // namespace
@@ -783,15 +1032,33 @@ int launched() { return hipGetLastError() == hipSuccess ? MXC_OK : MXC_ERR_LAUNC
 int muon_workspace(int count, const int *rows, const int *cols, size_t *bytes)
 {
     try {
-        *bytes = plan_of(count, rows, cols).bytes;
+        *bytes = all_small(count, rows, cols) ? 0 : plan_of(count, rows, cols).bytes;
         return MXC_OK;
     } catch (const std::bad_alloc &) {
         return MXC_ERR_LAUNCH;
     }
 }
 
+static int run_small(const MuonArgs &q, hipStream_t st)
+{
+    const Common f = {q.momentum, q.grad_scale, q.keep, q.nesterov, q.w != nullptr, q.dtype == MXC_BF16};
+    for (int base = 0; base < q.count; base += SMALL_GROUP) {
+        SmallGroup g;
+        const int count = std::min(SMALL_GROUP, q.count - base);
+        for (int k = 0; k < count; ++k) {
+            const int i = base + k;
+            g.t[k] = SmallEntry{q.rows[i], q.cols[i], step_of(q, q.rows[i], q.cols[i]), q.u[i], (bf16_t *)(q.w ? (q.w_bf16 ? q.w_bf16[i] : nullptr) : q.y[i]), q.w ? q.w[i] : nullptr,
+                                q.w ? q.m[i] : nullptr};
+        }
+        hipLaunchKernelGGL(f.bf16 ? small_kernel<true> : small_kernel<false>, dim3(count), dim3(SMALL_NT), 0, st, g, f, q.steps);
+        if (launched() != MXC_OK) return MXC_ERR_LAUNCH;
+    }
+    return MXC_OK;
+}
+
 static int run(const MuonArgs &q, void *ws, size_t ws_bytes, hipStream_t st)
 {
+    if (all_small(q.count, q.rows, q.cols)) return run_small(q, st);
     const Plan p = plan_of(q.count, q.rows, q.cols);
     if (!ws || ws_bytes < p.bytes) return MXC_ERR_WORKSPACE;
     char *at = (char *)ws;
@@ -817,7 +1084,7 @@ static int run(const MuonArgs &q, void *ws, size_t ws_bytes, hipStream_t st)
             const Sizes s = sizes_of(R, C);
             Entry &t = g.t[k];
             t.R = R; t.C = C; t.Rp = s.Rp; t.Cp = s.Cp; t.mp = s.mp; t.tall = R > C; t.norm_count = s.norm_count;
-            t.step = (float)(q.lr * (q.rms > 0.0 ? q.rms * sqrt((double)(R > C ? R : C)) : R > C ? sqrt((double)R / C) : 1.0));
+            t.step = step_of(q, R, C);
             t.u = q.u[i];
             t.y = (bf16_t *)(q.w ? (q.w_bf16 ? q.w_bf16[i] : nullptr) : q.y[i]);
             t.w = q.w ? q.w[i] : nullptr;

@@ -116,7 +116,7 @@ def check(got, x, steps, rounded=True):
     assert float(off.norm()) <= tol, (tuple(x.shape), float(off.norm()), tol, float(want.norm()))
 
 
-SHAPES = [(1, 1), (1, 7), (9, 1), (2, 3), (5, 5), (16, 33), (33, 16), (63, 64), (64, 64), (65, 64), (64, 363), (363, 64), (100, 1000), (128, 129), (200, 200), (257, 255), (130, 700), (700, 130),
+SHAPES = [(1, 1), (1, 7), (9, 1), (2, 3), (5, 5), (16, 33), (33, 16), (63, 64), (64, 64), (65, 64), (64, 363), (363, 64), (64, 576), (576, 61), (64, 577), (40, 449), (31, 500), (100, 1000), (128, 129), (200, 200), (257, 255), (130, 700), (700, 130),
           (512, 640), (1025, 513)]
 
 
@@ -133,6 +133,11 @@ def test_orthogonalize(mxc, dtype, r, c):
         ws.fill_(255)           # whatever the workspace held
         mxc.mxc_orthogonalize([x], steps, [y], ws)
         assert torch.equal(first, y) and intact(whole, y) and intact(ws_whole, ws, 5)
+        # beside one that no compute unit holds: by other kernels, with the same bits
+        beside = matrix(65, 600, "random", 9).to(dtype)
+        y.zero_()
+        mxc.mxc_orthogonalize([x, beside], steps, [y, torch.empty(65, 600, dtype=torch.bfloat16, device="cuda")], workspace(mxc, [(r, c), (65, 600)])[1])
+        assert torch.equal(first, y)
 
 
 @pytest.mark.parametrize("kind", ["one", "ones", "rank1", "outlier", "few"])
@@ -257,6 +262,30 @@ def test_update(mxc, dtype, nesterov, copy):
             assert torch.equal(now["wb"][i], now["w"][i].bfloat16() if copy else torch.zeros_like(now["wb"][i]))
             assert torch.equal(now["g"][i], was["g"][i])
         assert all(intact(whole, part) for v in held.values() for whole, part in v) and intact(ws_whole, ws, 5)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("nesterov", [False, True])
+def test_update_of_small_matrices(mxc, dtype, nesterov):
+    """One launch for 72 of them, without a workspace: the bits of a call that has a larger one too."""
+    shapes = [(1 + 17 * i % 64, 1 + 131 * i % 576) if i % 2 else (1 + 131 * i % 576, 1 + 17 * i % 64) for i in range(75)]
+    assert mxc.mxc_orthogonalize_workspace_bytes([r for r, _ in shapes], [c for _, c in shapes]) == 0
+    def state(more):
+        all_shapes = shapes + more
+        return [[guarded(s, t) for s in all_shapes] for t in (torch.float32, dtype, torch.float32, torch.bfloat16)]
+    results = []
+    for more in ([], [(70, 600)]):
+        held = state(more)
+        for k, (kind, size) in enumerate((("random", 0.1), ("few", 1e-3), ("few", 1e-2))):
+            for i, (_, part) in enumerate(held[k]):
+                part.copy_(matrix(*part.shape, kind, i + k) * size)
+        now = [[p for _, p in v] for v in held]
+        ws = workspace(mxc, shapes + more)[1] if more else None
+        for _ in range(2):
+            mxc.mxc_muon_update(now[0], now[1], now[2], now[3], 1e-2, 0.9, nesterov, 0.1, 0.2, 0.5, 5, ws)
+        assert all(intact(whole, part) for v in held for whole, part in v)
+        results.append([t.clone() for v in (now[0], now[2], now[3]) for t in v[:len(shapes)]])
+    assert all(torch.equal(a, b) for a, b in zip(*results))
 
 
 def test_streams_and_graphs(mxc):

@@ -83,10 +83,10 @@ def test_muon_refusals(mxc):
     lib = mxc.raw()
     two, most = (ctypes.c_int * 2), mxc.MXC_ORTHOGONALIZE_MAX_SIDE
 
-    def orth(count=2, rows=two(3, 5), cols=two(4, 6), w=arrays(A, B), dtype=1, steps=5, y=arrays(C_, D), ws=H, wn=1 << 40):
+    def orth(count=2, rows=two(3, 600), cols=two(4, 700), w=arrays(A, B), dtype=1, steps=5, y=arrays(C_, D), ws=H, wn=1 << 40):
         return lib.mxc_orthogonalize(count, rows, cols, w, dtype, steps, y, ws, wn, None)
 
-    def muon(count=2, rows=two(3, 5), cols=two(4, 6), w=arrays(A, B), g=arrays(C_, D), dtype=1, m=arrays(E, F_), wb=None, lr=1e-3, mu=0.9, nesterov=1, wd=0.1, rms=0.2, gs=1.0, steps=5,
+    def muon(count=2, rows=two(3, 600), cols=two(4, 700), w=arrays(A, B), g=arrays(C_, D), dtype=1, m=arrays(E, F_), wb=None, lr=1e-3, mu=0.9, nesterov=1, wd=0.1, rms=0.2, gs=1.0, steps=5,
              ws=H, wn=1 << 40):
         return lib.mxc_muon_update(count, rows, cols, w, g, dtype, m, wb, lr, mu, nesterov, wd, rms, gs, steps, ws, wn, None)
 
@@ -99,8 +99,8 @@ def test_muon_refusals(mxc):
         for bad in (dict(rows=None), dict(cols=None), dict(w=None), dict(w=arrays(A, None))):
             assert call(**bad) == mxc.MXC_ERR_NULL, bad
         assert call(w=arrays(A, B + 4)) == mxc.MXC_ERR_ALIGN and call(ws=H + 8) == mxc.MXC_ERR_ALIGN
-        need = mxc.mxc_orthogonalize_workspace_bytes([3, 5], [4, 6])
-        assert need % 256 == 0 and call(wn=need - 1) == mxc.MXC_ERR_WORKSPACE and call(ws=None) == mxc.MXC_ERR_WORKSPACE
+        need = mxc.mxc_orthogonalize_workspace_bytes([3, 600], [4, 700])
+        assert need and need % 256 == 0 and call(wn=need - 1) == mxc.MXC_ERR_WORKSPACE and call(ws=None) == mxc.MXC_ERR_WORKSPACE
     assert orth(y=None) == mxc.MXC_ERR_NULL and orth(y=arrays(None, A)) == mxc.MXC_ERR_NULL and orth(y=arrays(A + 2, B)) == mxc.MXC_ERR_ALIGN
     for bad in (dict(mu=1.0), dict(mu=-0.1), dict(mu=NAN), dict(nesterov=2), dict(rms=-1.0), dict(rms=NAN), dict(rms=INF), dict(lr=NAN), dict(lr=INF), dict(lr=1e37), dict(wd=NAN), dict(gs=INF)):
         assert muon(**bad) == mxc.MXC_ERR_UNSUPPORTED, bad
@@ -108,6 +108,9 @@ def test_muon_refusals(mxc):
         assert muon(**bad) == mxc.MXC_ERR_NULL, bad
     for bad in (dict(g=arrays(A + 2, B)), dict(m=arrays(A, B + 8)), dict(wb=arrays(A + 2, B))):
         assert muon(**bad) == mxc.MXC_ERR_ALIGN, bad
+    # matrices that a compute unit holds need none
+    assert mxc.mxc_orthogonalize_workspace_bytes([64, 1, 576], [576, 1, 64]) == 0
+    assert mxc.mxc_orthogonalize_workspace_bytes([64], [577]) > 0 and mxc.mxc_orthogonalize_workspace_bytes([65], [65]) > 0
     n = ctypes.c_size_t()
     assert lib.mxc_orthogonalize_workspace_bytes(2, two(3, 5), two(4, 6), None) == mxc.MXC_ERR_NULL
     assert lib.mxc_orthogonalize_workspace_bytes(2, None, two(4, 6), ctypes.byref(n)) == mxc.MXC_ERR_NULL
