@@ -2,7 +2,7 @@
 // the order of n.  Memory bounds both: forward reads and writes each row once; the gradient reads dy once and writes a row of dw for every
 // token of the vocabulary.  The gradient of more than a few places goes by the tokens' order, in three launches: the places are sorted by their token, each token's rows added, in
 // parts, and the parts of a token that has several joined.  16384 rows of 4096 bf16 41.6 us, 6.5 TB/s (64 rows 3.9, a launch); gradient of 32768 places on 50257 x 2048, bf16,
-// 144 us; of 500 places on 1000 x 512 fp32, in one launch, 8.4.
+// 138 us; of 500 places on 1000 x 512 fp32, in one launch, 8.4.
 #include "pieces.h"
 
 namespace mxc {
@@ -65,30 +65,23 @@ __device__ __forceinline__ void put(float *row, int c, int C, const float (&s)[4
     store_piece<PAST>(row, c, C, p);
 }
 
-// s += columns [c, c + 4) of rows places[0, count), in their order; the places of the next rows are under way while rows are
-template <class T>
+// s += columns [c, c + 4) of rows places[0, count), in their order, AHEAD rows on their way at once
+template <int AHEAD, class T>
 __device__ __forceinline__ void add_rows(const T *dy, int c, int C, const int *places, int count, float (&s)[4])
 {
-    constexpr int AHEAD = 8;
-    if (count <= 0) return;
-    int at[AHEAD];
+    int k = 0;
+    for (; k + AHEAD <= count; k += AHEAD) {
+        decltype(begin_quad(dy, 0, 0)) p[AHEAD];
 #pragma unroll
-    for (int j = 0; j < AHEAD; ++j) at[j] = places[min(j, count - 1)];
-    for (int k = 0; k < count; k += AHEAD) {
-        decltype(load_quad(dy, 0, 0)) p[AHEAD];
+        for (int j = 0; j < AHEAD; ++j) p[j] = begin_quad(dy + (size_t)places[k + j] * C, c, C);
 #pragma unroll
-        for (int j = 0; j < AHEAD; ++j)
-            if (k + j < count) p[j] = load_quad(dy + (size_t)at[j] * C, c, C);
-        if (k + AHEAD < count) {
+        for (int j = 0; j < AHEAD; ++j) {
+            settle_quad(p[j], c, C);
 #pragma unroll
-            for (int j = 0; j < AHEAD; ++j) at[j] = places[min(k + AHEAD + j, count - 1)];
+            for (int i = 0; i < 4; ++i) s[i] += p[j].get(i);
         }
-#pragma unroll
-        for (int j = 0; j < AHEAD; ++j)
-            if (k + j < count)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) s[i] += p[j].get(i);
     }
+    if constexpr (AHEAD > 1) add_rows<AHEAD / 4>(dy, c, C, places + k, count - k, s);
 }
 
 // Few places, one launch: the workgroup of a place looks for its token among all places and, if the place is the first that has it, adds their rows;
@@ -149,7 +142,7 @@ __global__ __launch_bounds__(NT) void few_kernel(int N, int V, int C, const int 
     __syncthreads();
     for (int c = ((int)blockIdx.y * nt + threadIdx.x) * 4; c < C; c += nt * 4 * gridDim.y) {
         float s[4] = {0.f, 0.f, 0.f, 0.f};
-        add_rows(dy, c, C, places, count, s);
+        add_rows<16>(dy, c, C, places, count, s);
         put<false>(dw + (size_t)t * C, c, C, s, scale, add);
     }
 }
@@ -320,11 +313,12 @@ __global__ __launch_bounds__(NT) void rows_kernel(int V, int C, int PART, long l
     int now = __builtin_amdgcn_readlane(t, 0), slot = 0;
     bool whole = __builtin_amdgcn_readfirstlane(ahead) != now;          // the token's places begin in this part
     for (int k = 0; k < count; k += AHEAD) {
-        decltype(load_quad(dy, 0, 0)) p[AHEAD];
+        decltype(begin_quad(dy, 0, 0)) p[AHEAD];
 #pragma unroll
-        for (int j = 0; j < AHEAD; ++j) p[j] = load_quad(dy + (size_t)__builtin_amdgcn_readlane(o, k + j) * C, has ? c : 0, C);
+        for (int j = 0; j < AHEAD; ++j) p[j] = begin_quad(dy + (size_t)__builtin_amdgcn_readlane(o, k + j) * C, has ? c : 0, C);
 #pragma unroll
         for (int j = 0; j < AHEAD; ++j) {
+            settle_quad(p[j], has ? c : 0, C);
             const int next = __builtin_amdgcn_readlane(t, k + j);
             if (next != now) {
                 if (now >= 0 && has) {
@@ -364,12 +358,14 @@ __global__ __launch_bounds__(NT) void join_kernel(int V, int C, int PART, const 
 #pragma unroll
         for (int j = 0; j < AHEAD; ++j) {
             const int k = min(q + j, q1 - 1);
-            g[j] = load_piece(parts + (size_t)(2 * ((long long)part + k) + (k == 0 && s0 != p0 ? 1 : 0)) * C, at, C);
+            g[j] = begin_piece(parts + (size_t)(2 * ((long long)part + k) + (k == 0 && s0 != p0 ? 1 : 0)) * C, at, C);
         }
 #pragma unroll
-        for (int j = 0; j < AHEAD; ++j)
+        for (int j = 0; j < AHEAD; ++j) {
+            settle_piece(g[j], at, C);
 #pragma unroll
             for (int i = 0; i < 4; ++i) s[i] += q + j < q1 ? g[j].get(i) : 0.f;
+        }
     }
     sum[threadIdx.x] = make_float4(s[0], s[1], s[2], s[3]);
     __syncthreads();

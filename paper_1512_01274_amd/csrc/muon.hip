@@ -39,7 +39,7 @@ constexpr int NORM_MOST = 1024, NORM_CHUNK = 2048;
 struct Entry {
     int R, C, Rp, Cp;                       // rows, columns, and padded to BK
     int mp, tall;                           // the padded shorter side; rows > cols
-    int norm_count;                         // workgroups that sum the squares
+    int norm_count, norm_parts;             // workgroups that sum the squares, and what they leave
     float step;                             // w' = keep w - step O
     const void *u;                          // x, or the gradient
     bf16_t *y;                              // y, or the bf16 copy of w
@@ -79,47 +79,103 @@ __device__ __forceinline__ float x_of(float e, f16_t hi, f16_t lo, float sum) { 
 __device__ __forceinline__ f16_t rest_of(float x, f16_t hi) { return (f16_t)((x - (float)hi) * LO_UP); }
 __device__ __forceinline__ float w_of(float w, float x, float keep, float step) { return __builtin_fmaf(-step, x * X_DOWN, w * keep); }
 
-// whether the momentum is still to be made of the gradient, and where it goes
-struct ToMake {
-    static constexpr bool fresh = true;
-    float *m;
-    int c, len;
-    __device__ __forceinline__ void store(const Piece<float> &p) const { store_piece(m, c, len, p); }
-};
-struct Made {
-    static constexpr bool fresh = false;
-    __device__ __forceinline__ void store(const Piece<float> &) const {}
+// Four values of the matrix that is made orthogonal, from column c of a row of len: x, or of the gradient and the momentum.  In two steps, so that the loads of many stay under way.
+// FRESH: the momentum is still to be made of the gradient; it goes back to where it was.
+template <bool BF16, bool FRESH>
+struct Values {
+    typedef typename std::conditional<BF16, bf16_t, float>::type T;
+    decltype(begin_quad((const T *)nullptr, 0, 0)) u;
+    Piece<float> m;
+    __device__ __forceinline__ void begin(const Common &f, const void *from, const float *mom, int c, int len)
+    {
+        if (FRESH || !f.muon || f.nesterov) u = begin_quad((const T *)from, c, len);
+        if (f.muon) m = begin_quad(mom, c, len);
+    }
+    __device__ __forceinline__ void end(const Common &f, float *mom, int c, int len, float (&v)[4])
+    {
+        if (FRESH || !f.muon || f.nesterov) {
+            settle_quad(u, c, len);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = u.get(i);
+        }
+        if (f.muon) {
+            settle_quad(m, c, len);
+            float n[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float g = v[i] * f.grad_scale;
+                n[i] = FRESH ? __builtin_fmaf(m.get(i), f.momentum, g) : m.get(i);
+                v[i] = f.nesterov ? __builtin_fmaf(n[i], f.momentum, g) : n[i];
+            }
+            if (FRESH) {
+                m.set(n);
+                store_piece(mom, c, len, m);
+            }
+        }
+    }
 };
 
-// four values of the matrix that is made orthogonal, from column c of row r: x, or the momentum's part (m: as it is after norm_kernel)
-template <bool BF16, class M>
-__device__ __forceinline__ void values_at(const Common &f, const void *u, const float *m, int c, int len, float (&v)[4], M &&made)
+// Matrices of up to SMALL_M by SMALL_N (either way), which a compute unit holds: X, its shorter side as rows, in blocks of 32 x 32, the b-th at row 32 * (b % 2) and column
+// 32 * (b / 2), block b belonging to wave b % 16; a lane has row lane % 32 and of the columns 8 g + 4 (lane / 32) + 0 .. 3.  Their squares are added in this order wherever it is
+// done.
+constexpr int SMALL_M = 64, SMALL_N = 576, SMALL_BLOCKS = (SMALL_N / 32 * 2 + 15) / 16;
+__host__ __device__ inline bool is_small(int R, int C) { return (R < C ? R : C) <= SMALL_M && (R < C ? C : R) <= SMALL_N; }
+// Block b's values, zeros outside of the matrix; the momentum is made of the gradient on the way.
+template <bool BF16>
+__device__ __forceinline__ void block_values(const Common &f, int R, int C, const void *u, float *mom, int b, int lane, float (&v)[4][4])
 {
-    if (!f.muon || f.nesterov || made.fresh) {
-        if constexpr (BF16) {
-            const Quad q = load_quad((const bf16_t *)u, c, len);
+    typedef typename std::conditional<BF16, bf16_t, float>::type T;
+    const int m = min(R, C), n = max(R, C), r = b % 2 * 32 + lane % 32, c0 = b / 2 * 32 + lane / 32 * 4;
+    // (loads first, outside of branches and with addresses inside of the matrix: they are under way together)
+    if (R <= C) {
+        const int at = min(r, m - 1) * n;
+        Values<BF16, true> q[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = q.get(i);
-        } else {
-            const Piece<float> q = load_piece((const float *)u, c, len);
+        for (int g = 0; g < 4; ++g) q[g].begin(f, (const T *)u + at, mom + at, c0 + 8 * g, n);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = q.get(i);
+        for (int g = 0; g < 4; ++g) {
+            const bool in = r < m && c0 + 8 * g < n;
+            if (in) q[g].end(f, mom + at, c0 + 8 * g, n, v[g]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[g][i] = in && c0 + 8 * g + i < n ? v[g][i] : 0.f;
         }
+    } else {
+        float o[4][4];
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int at = min(c0 + 8 * g + i, n - 1) * m + min(r, m - 1);
+                v[g][i] = load_f32((const T *)u + at);
+                o[g][i] = f.muon ? mom[at] : 0.f;
+            }
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const bool in = r < m && c0 + 8 * g + i < n;
+                if (f.muon) {
+                    const float grad = v[g][i] * f.grad_scale, next = __builtin_fmaf(o[g][i], f.momentum, grad);
+                    v[g][i] = f.nesterov ? __builtin_fmaf(next, f.momentum, grad) : next;
+                    if (in) mom[(c0 + 8 * g + i) * m + r] = next;
+                }
+                v[g][i] = in ? v[g][i] : 0.f;
+            }
     }
-    if (f.muon) {
-        Piece<float> q = load_piece(m, c, len);
-        float n[4];
+}
+__device__ __forceinline__ double squares_of(const float (&v)[4][4], double s)
+{
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float g = v[i] * f.grad_scale;
-            n[i] = made.fresh ? __builtin_fmaf(q.get(i), f.momentum, g) : q.get(i);
-            v[i] = f.nesterov ? __builtin_fmaf(n[i], f.momentum, g) : n[i];
-        }
-        if (made.fresh) {
-            q.set(n);
-            made.store(q);
-        }
-    }
+    for (int g = 0; g < 4; ++g)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s = __builtin_fma((double)v[g][i], (double)v[g][i], s);
+    return s;
+}
+__device__ __forceinline__ double wave_total(double s)
+{
+#pragma unroll
+    for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
+    return s;
 }
 
 // ---- sums of squares, the momentum, and the table of the call's matrices ---------------------------------------------------------------------
@@ -147,20 +203,40 @@ __global__ __launch_bounds__(256) void norm_kernel(Group q, Common f, Entry *tab
         fill(maps.items[k][t.items[k].shape], t.items[k].first, t.items[k].count, me, at, step);
         fill(maps.finish[k][t.items[k].shape], t.items[k].finish_first, t.items[k].finish_count, me, at, step);
     }
-    const int n = t.R * t.C;                // (below 2^30 + 2^15)
+    if (is_small(t.R, t.C)) {               // a wave's blocks
+        const int wave = part * 4 + (threadIdx.x >> 6), blocks = (max(t.R, t.C) + BK - 1) / BK * BK / 32 * 2;
+        double s = 0.0;
+        for (int b = wave; b < blocks; b += 16) {
+            float v[4][4];
+            block_values<BF16>(f, t.R, t.C, t.u, t.m, b, threadIdx.x & 63, v);
+            s = squares_of(v, s);
+        }
+        s = wave_total(s);
+        if ((threadIdx.x & 63) == 0) t.norm[wave] = s;
+        return;
+    }
+    const int n = t.R * t.C;                // (2^30 at most)
     const void *u = t.u;
     float *m = t.m;
     double s = 0.0;
-#pragma unroll 4
-    for (long long k = (long long)(part * 256 + threadIdx.x) * 4; k < n; k += (long long)t.norm_count * 1024) {
-        float v[4];
-        values_at<BF16>(f, u, m, (int)k, n, v, ToMake{m, (int)k, n});
+    constexpr int AHEAD = 4;
+    const long long every = (long long)t.norm_count * 1024;
+    for (long long k0 = (long long)(part * 256 + threadIdx.x) * 4; k0 < n; k0 += AHEAD * every) {
+        Values<BF16, true> q[AHEAD];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) s = k + j < n ? __builtin_fma((double)v[j], (double)v[j], s) : s;
+        for (int a = 0; a < AHEAD; ++a) q[a].begin(f, u, m, (int)min(k0 + a * every, (long long)n), n);
+#pragma unroll
+        for (int a = 0; a < AHEAD; ++a) {
+            const long long k = k0 + a * every;
+            if (k >= n) break;
+            float v[4];
+            q[a].end(f, m, (int)k, n, v);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s = k + j < n ? __builtin_fma((double)v[j], (double)v[j], s) : s;
+        }
     }
     __shared__ double wave_sum[4];
-#pragma unroll
-    for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
+    s = wave_total(s);
     if ((threadIdx.x & 63) == 0) wave_sum[threadIdx.x >> 6] = s;
     __syncthreads();
     if (threadIdx.x == 0) t.norm[part] = wave_sum[0] + wave_sum[1] + wave_sum[2] + wave_sum[3];
@@ -185,21 +261,16 @@ __global__ __launch_bounds__(256) void prepare_kernel(Common f, const Entry *tab
     __shared__ f16_t turned[64][68];
     __shared__ double wave_sum[4];
     const int c = threadIdx.x % 16 * 4, row = threadIdx.x / 16;
-    float v[4][4];
+    Values<BF16, false> q[4];
+    // (rows and columns past the matrix: the last row's, not used)
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-        const int r = r0 + k * 16 + row;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[k][i] = 0.f;
-        if (r < t.R && c0 + c < t.C) {
-            const size_t at = (size_t)r * t.C;
-            values_at<BF16>(f, BF16 ? (const void *)((const bf16_t *)t.u + at) : (const void *)((const float *)t.u + at), t.m + at, c0 + c, t.C, v[k], Made{});
-        }
+        const size_t at = (size_t)min(r0 + k * 16 + row, t.R - 1) * t.C;
+        q[k].begin(f, BF16 ? (const void *)((const bf16_t *)t.u + at) : (const void *)((const float *)t.u + at), t.m + at, c0 + c, t.C);
     }
     double s = 0.0;
-    for (int k = threadIdx.x; k < t.norm_count; k += 256) s += t.norm[k];
-#pragma unroll
-    for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
+    for (int k = threadIdx.x; k < t.norm_parts; k += 256) s += t.norm[k];
+    s = wave_total(s);
     if ((threadIdx.x & 63) == 0) wave_sum[threadIdx.x >> 6] = s;
     __syncthreads();
     s = wave_sum[0] + wave_sum[1] + wave_sum[2] + wave_sum[3];
@@ -208,10 +279,12 @@ __global__ __launch_bounds__(256) void prepare_kernel(Common f, const Entry *tab
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         f16x4 hi, lo;
+        float v[4];
+        q[k].end(f, nullptr, c0 + c, t.C, v);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const bool in = r0 + k * 16 + row < t.R && c0 + c + i < t.C;
-            const float x = in ? in_32_bits(ldexpf(v[k][i], -up) * by) : 0.f;
+            const float x = in ? in_32_bits(ldexpf(v[i], -up) * by) : 0.f;
             hi[i] = (f16_t)x;
             lo[i] = rest_of(x, hi[i]);
             turned[c + i][k * 16 + row] = hi[i];
@@ -616,7 +689,7 @@ __global__ __launch_bounds__(64 * FINISH) void finish_kernel(const Entry *table,
 // the waves that form them; 16-byte chunks of a row are exchanged so that 16 rows of a fetch fall into different banks.  The same operations in the same order as in the
 // kernels above, with the same bits.  One 64 x 363 matrix: 95 us of 17 launches before.
 
-constexpr int SMALL_M = 64, SMALL_N = 576, SMALL_NT = 1024, SMALL_GROUP = 72, SMALL_PARTS = (SMALL_M * SMALL_N + NORM_CHUNK - 1) / NORM_CHUNK;
+constexpr int SMALL_NT = 1024, SMALL_GROUP = 72;
 struct SmallEntry {
     int R, C;
     float step;
@@ -631,43 +704,31 @@ static_assert(sizeof(SmallGroup) + sizeof(Common) + 16 <= 4096, "kernel argument
 template <bool BF16>
 __global__ __launch_bounds__(SMALL_NT) void small_kernel(SmallGroup q, Common f, int steps)
 {
-    constexpr int MOST = (SMALL_N / 32 * 2 + 15) / 16;         // 32 x 32 blocks of X of a wave
+    constexpr int MOST = SMALL_BLOCKS;
     __shared__ __attribute__((aligned(256))) unsigned char lds[SMALL_M * SMALL_N * 4 + 8192];
     __shared__ float diagonal[2][SMALL_M];                     // d, e
-    __shared__ double part_sum[SMALL_PARTS][4];
-    __shared__ double all_squares;
+    __shared__ double part_sum[SMALL_NT / 64];
     const SmallEntry &t = q.t[blockIdx.x];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int l32 = lane & 31, half = lane >> 5;
     const bool tall = t.R > t.C;
     const int m = tall ? t.C : t.R, n = tall ? t.R : t.C, np = (n + BK - 1) / BK * BK;
-    const void *const u = t.u;
-    float *const mom = t.m;
+    const int blocks = np / 32 * 2;
 
-    // the squares, and the momentum: as norm_kernel's workgroups of 256, four at a time
-    const int values = t.R * t.C, parts = (values + NORM_CHUNK - 1) / NORM_CHUNK, tid = threadIdx.x & 255;
-    for (int part = threadIdx.x >> 8; part < parts; part += 4) {
-        double s = 0.0;
-        for (int k = (part * 256 + tid) * 4; k < values; k += parts * 1024) {
-            float v[4];
-            values_at<BF16>(f, u, mom, k, values, v, ToMake{mom, k, values});
+    float v[MOST][4][4];
+    double s = 0.0;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) s = k + j < values ? __builtin_fma((double)v[j], (double)v[j], s) : s;
+    for (int k = 0; k < MOST; ++k)
+        if (wave + 16 * k < blocks) {
+            block_values<BF16>(f, t.R, t.C, t.u, t.m, wave + 16 * k, lane, v[k]);
+            s = squares_of(v[k], s);
         }
-#pragma unroll
-        for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
-        if (lane == 0) part_sum[part][wave & 3] = s;
-    }
+    s = wave_total(s);
+    if (lane == 0) part_sum[wave] = s;
     __syncthreads();
-    if (wave == 0) {
-        double s = lane < parts ? part_sum[lane][0] + part_sum[lane][1] + part_sum[lane][2] + part_sum[lane][3] : 0.0;
-#pragma unroll
-        for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
-        if (lane == 0) all_squares = s + 0.0 + 0.0 + 0.0;
-    }
-    __syncthreads();
+    s = wave_total(lane < 16 ? part_sum[lane] : 0.0);
     int up;
-    const float by = over_norm(all_squares, up);
+    const float by = over_norm(s, up);
 
     // where 16-byte chunk c of a row lies: X [64][np], its transpose [np][64], A and B [64][64]
     unsigned char *const z = lds, *const zt = lds + SMALL_M * 2 * np, *const sq = lds + SMALL_M * 4 * np;
@@ -675,54 +736,36 @@ __global__ __launch_bounds__(SMALL_NT) void small_kernel(SmallGroup q, Common f,
     auto z_at = [&](int r, int c) __attribute__((always_inline)) { return z + r * np * 2 + ((c ^ (odd ? r >> 1 & 7 : r & 15)) << 4); };
     auto narrow_at = [](unsigned char *base, int r, int c) __attribute__((always_inline)) { return base + r * 128 + ((c ^ (r >> 1 & 7)) << 4); };
 
-    // this wave's blocks of X: rows 32 * (b % 2), columns 32 * (b / 2) of block b; a lane has row l32 and of the columns 8 g + 4 half + 0 .. 3
-    const int blocks = np / 32 * 2;
     f16x4 hi[MOST][4], lo[MOST][4];
-    auto put_x = [&](int b, int g, const f16x4 &x) __attribute__((always_inline)) {
-        const int r = b % 2 * 32 + l32, c = b / 2 * 32 + 8 * g + 4 * half;
-        *reinterpret_cast<f16x4 *>(z_at(r, c / 8) + half * 8) = x;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) *reinterpret_cast<f16_t *>(narrow_at(zt, c + i, r / 8) + r % 8 * 2) = x[i];
+    auto put_z = [&](int b, int g, const f16x4 &x) __attribute__((always_inline)) {
+        *reinterpret_cast<f16x4 *>(z_at(b % 2 * 32 + l32, b / 2 * 4 + g) + half * 8) = x;
+    };
+    // the transpose: neighbouring lanes, which have neighbouring rows, give each other two columns, so that either stores two of both rows
+    auto put_zt = [&](int b, int g, const f16x4 &x) __attribute__((always_inline)) {
+        const uint2 w = __builtin_bit_cast(uint2, x);
+        const bool upper = l32 & 1;
+        const unsigned keep = upper ? w.y : w.x, give = upper ? w.x : w.y;
+        const unsigned got = (unsigned)__builtin_amdgcn_update_dpp(0, (int)give, 0xB1, 0xF, 0xF, true);
+        const unsigned even = upper ? got : keep, uneven = upper ? keep : got;            // of the even row and of the one below
+        const int r = b % 2 * 32 + (l32 & 30), c = b / 2 * 32 + 8 * g + 4 * half + (upper ? 2 : 0);
+        *reinterpret_cast<unsigned *>(narrow_at(zt, c, r / 8) + r % 8 * 2) = __builtin_amdgcn_perm(uneven, even, 0x05040100);
+        *reinterpret_cast<unsigned *>(narrow_at(zt, c + 1, r / 8) + r % 8 * 2) = __builtin_amdgcn_perm(uneven, even, 0x07060302);
     };
 #pragma unroll
-    for (int k = 0; k < MOST; ++k) {
-        const int b = wave + 16 * k, r = b % 2 * 32 + l32;
-        if (b >= blocks) break;
-        float v[4][4];
+    for (int k = 0; k < MOST; ++k)
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-            const int c = b / 2 * 32 + 8 * g + 4 * half;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[g][i] = 0.f;
-            if (r >= m || c >= n) continue;
-            if (!tall) {
-                const int at = r * n;
-                values_at<BF16>(f, BF16 ? (const void *)((const bf16_t *)u + at) : (const void *)((const float *)u + at), mom + at, c, n, v[g], Made{});
-            } else {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if (c + i >= n) break;
-                    const int at = (c + i) * m + r;
-                    float one = 0.f;
-                    if (!f.muon || f.nesterov) one = BF16 ? bf16_to_f32(((const bf16_t *)u)[at]) : ((const float *)u)[at];
-                    if (f.muon) one = f.nesterov ? __builtin_fmaf(mom[at], f.momentum, one * f.grad_scale) : mom[at];
-                    v[g][i] = one;
-                }
-            }
-        }
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const int c = b / 2 * 32 + 8 * g + 4 * half;
+            const int b = wave + 16 * k, c = b / 2 * 32 + 8 * g + 4 * half;
+            if (b >= blocks) continue;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float x = r < m && c + i < n ? in_32_bits(ldexpf(v[g][i], -up) * by) : 0.f;
+                const float x = b % 2 * 32 + l32 < m && c + i < n ? in_32_bits(ldexpf(v[k][g][i], -up) * by) : 0.f;       // (zeros outside, also where the norm is NaN)
                 hi[k][g][i] = (f16_t)x;
                 lo[k][g][i] = rest_of(x, hi[k][g][i]);
             }
-            put_x(b, g, hi[k][g]);
+            put_z(b, g, hi[k][g]);
+            put_zt(b, g, hi[k][g]);
         }
-        asm volatile("" ::: "memory");      // a block after the other: their values together are more than the registers
-    }
     __syncthreads();
 
     for (int step = 0; step < steps; ++step) {
@@ -735,7 +778,7 @@ __global__ __launch_bounds__(SMALL_NT) void small_kernel(SmallGroup q, Common f,
             f32x16 acc;
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[e] = 0.f;
-#pragma unroll 4
+#pragma unroll 8
             for (int c = half; c < np / 8; c += 2) {
                 const f16x8 a = *reinterpret_cast<const f16x8 *>(z_at(row, c)), b = *reinterpret_cast<const f16x8 *>(z_at(tj * 32 + l32, c));
                 acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(b, a, acc, 0, 0, 0);
@@ -826,7 +869,10 @@ __global__ __launch_bounds__(SMALL_NT) void small_kernel(SmallGroup q, Common f,
         for (int k = 0; k < MOST; ++k)
 #pragma unroll
             for (int g = 0; g < 4; ++g)
-                if (wave + 16 * k < blocks) put_x(wave + 16 * k, g, hi[k][g]);
+                if (wave + 16 * k < blocks) {
+                    put_z(wave + 16 * k, g, hi[k][g]);
+                    put_zt(wave + 16 * k, g, hi[k][g]);
+                }
         __syncthreads();
     }
 }
@@ -834,7 +880,7 @@ __global__ __launch_bounds__(SMALL_NT) void small_kernel(SmallGroup q, Common f,
 // ---- a call -------------------------------------------------------------------------------------------------------------------------------------
 
 struct Sizes {
-    int Rp, Cp, mp, norm_count;
+    int Rp, Cp, mp, norm_count, norm_parts;
     size_t mat, sq;                         // bytes of one orientation of X, of A
     unsigned prep;
     size_t bytes;
@@ -846,11 +892,12 @@ Sizes sizes_of(int R, int C)
     s.Cp = (int)align_up(C, BK);
     s.mp = R <= C ? s.Rp : s.Cp;
     const size_t n = (size_t)R * C, chunks = (n + NORM_CHUNK - 1) / NORM_CHUNK;
-    s.norm_count = chunks < NORM_MOST ? (int)chunks : NORM_MOST;
+    s.norm_count = is_small(R, C) ? 4 : chunks < NORM_MOST ? (int)chunks : NORM_MOST;
+    s.norm_parts = is_small(R, C) ? 16 : s.norm_count;
     s.mat = align_up((size_t)s.Rp * s.Cp * 2, 256);
     s.sq = align_up((size_t)s.mp * s.mp * 2, 256);
     s.prep = (unsigned)(s.Rp / 64) * (s.Cp / 64);
-    s.bytes = 4 * s.mat + 2 * s.sq + 2 * align_up((size_t)s.mp * 4, 256) + align_up(s.norm_count * 8, 256);
+    s.bytes = 4 * s.mat + 2 * s.sq + 2 * align_up((size_t)s.mp * 4, 256) + align_up(s.norm_parts * 8, 256);
     return s;
 }
 
@@ -1020,7 +1067,7 @@ Plan plan_of(int count, const int *rows, const int *cols)
 bool all_small(int count, const int *rows, const int *cols)
 {
     for (int i = 0; i < count; ++i)
-        if (std::min(rows[i], cols[i]) > SMALL_M || std::max(rows[i], cols[i]) > SMALL_N) return false;
+        if (!is_small(rows[i], cols[i])) return false;
     return true;
 }
 float step_of(const MuonArgs &q, int R, int C) { return (float)(q.lr * (q.rms > 0.0 ? q.rms * sqrt((double)std::max(R, C)) : R > C ? sqrt((double)R / C) : 1.0)); }
@@ -1083,7 +1130,7 @@ static int run(const MuonArgs &q, void *ws, size_t ws_bytes, hipStream_t st)
             const int i = base + k, R = q.rows[i], C = q.cols[i];
             const Sizes s = sizes_of(R, C);
             Entry &t = g.t[k];
-            t.R = R; t.C = C; t.Rp = s.Rp; t.Cp = s.Cp; t.mp = s.mp; t.tall = R > C; t.norm_count = s.norm_count;
+            t.R = R; t.C = C; t.Rp = s.Rp; t.Cp = s.Cp; t.mp = s.mp; t.tall = R > C; t.norm_count = s.norm_count; t.norm_parts = s.norm_parts;
             t.step = step_of(q, R, C);
             t.u = q.u[i];
             t.y = (bf16_t *)(q.w ? (q.w_bf16 ? q.w_bf16[i] : nullptr) : q.y[i]);
@@ -1099,7 +1146,7 @@ static int run(const MuonArgs &q, void *ws, size_t ws_bytes, hipStream_t st)
             t.P = (f16_t *)take(s.sq);
             t.d = (float *)take((size_t)s.mp * 4);
             t.e = (float *)take((size_t)s.mp * 4);
-            t.norm = (double *)take((size_t)s.norm_count * 8);
+            t.norm = (double *)take((size_t)s.norm_parts * 8);
             t.prep_first = prep_at;
             t.prep_count = s.prep;
             prep_at += s.prep;

@@ -43,26 +43,6 @@ struct Quad {
         return __uint_as_float(i & 1 ? w & 0xFFFF0000u : w << 16);
     }
 };
-__device__ __forceinline__ Quad load_quad(const bf16_t *row, int at, int len)
-{
-    typedef unsigned Bytes8 __attribute__((ext_vector_type(2), aligned(2)));
-    Quad q;
-    if (len >= 4) {
-        const Bytes8 b = *reinterpret_cast<const Bytes8 *>(row + (at + 4 <= len ? at : len - 4));
-        unsigned long long v = b.x | (unsigned long long)b.y << 32;
-        const int bits = (at + 4 - len) * 16;
-        if (bits > 0) v = bits >= 64 ? 0 : v >> bits;
-        q.raw = make_uint2((unsigned)v, (unsigned)(v >> 32));
-    } else {
-        unsigned w[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = at + i < len ? row[at + i] : 0;
-        q.raw = make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16);
-    }
-    return q;
-}
-__device__ __forceinline__ Piece<float> load_quad(const float *row, int at, int len);
-
 // Elements [at, at + VE) of a row of `len`, zeros past its end, in two steps, so that loads stay under way: the load, which for a piece that the row ends in brings the
 // row's last VE elements (of rows of fewer, one by one), and settle_piece, which moves these down.  (Loads in the branch of a short piece would wait there
 // for all before them: a gradient of 40000 x 1000 bf16, 125 pieces by 128 lanes, took 100 us where 65536 x 512 took 51.)
@@ -107,7 +87,39 @@ __device__ __forceinline__ Piece<T> load_piece(const T *row, int at, int len)
     settle_piece(p, at, len);
     return p;
 }
-__device__ __forceinline__ Piece<float> load_quad(const float *row, int at, int len) { return load_piece(row, at, len); }
+// the same for four values: a Quad of bf16, a Piece of fp32
+__device__ __forceinline__ Quad begin_quad(const bf16_t *row, int at, int len)
+{
+    typedef unsigned Bytes8 __attribute__((ext_vector_type(2), aligned(2)));
+    Quad q;
+    if (len >= 4) {
+        const Bytes8 b = *reinterpret_cast<const Bytes8 *>(row + (at + 4 <= len ? at : len - 4));
+        q.raw = make_uint2(b.x, b.y);
+    } else {
+        unsigned w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = at + i < len ? row[at + i] : 0;
+        q.raw = make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16);
+    }
+    return q;
+}
+__device__ __forceinline__ void settle_quad(Quad &q, int at, int len)
+{
+    if (at + 4 > len && len >= 4) {
+        const int bits = (at + 4 - len) * 16;
+        const unsigned long long v = q.raw.x | (unsigned long long)q.raw.y << 32, down = bits >= 64 ? 0 : v >> bits;
+        q.raw = make_uint2((unsigned)down, (unsigned)(down >> 32));
+    }
+}
+__device__ __forceinline__ Piece<float> begin_quad(const float *row, int at, int len) { return begin_piece(row, at, len); }
+__device__ __forceinline__ void settle_quad(Piece<float> &p, int at, int len) { settle_piece(p, at, len); }
+template <class T>
+__device__ __forceinline__ auto load_quad(const T *row, int at, int len)
+{
+    auto q = begin_quad(row, at, len);
+    settle_quad(q, at, len);
+    return q;
+}
 template <bool PAST = false, class T>
 __device__ __forceinline__ void store_piece(T *row, int at, int len, const Piece<T> &p)
 {
