@@ -34,6 +34,7 @@ constexpr float X_UP = 32768.f, X_DOWN = 1.f / 32768.f, LO_UP = 2048.f, LO_DOWN 
 
 constexpr int BK = 64;                      // reduction of a stage, and what sides are padded to
 constexpr int NORM_MOST = 1024, NORM_CHUNK = 2048;
+constexpr int KINDS = 3, SHAPE_COUNT = 5;   // products of a step, shapes of their tiles
 
 // One matrix of a call.  Z is ping-ponged where the third product reads it (tall), its transpose where it does not (wide); the other pair of pointers is one buffer.
 struct Entry {
@@ -53,7 +54,7 @@ struct Entry {
         unsigned whole, split;              // tiles that are not split
         unsigned part_first, finish_first, finish_count;        // of the split ones: the first one's first partial sums; workgroups that add them
         int shape;                          // of the tiles: a launch each
-    } items[3];
+    } items[KINDS];
 };
 constexpr int GROUP = 14;
 struct Group {
@@ -182,7 +183,7 @@ __device__ __forceinline__ double wave_total(double s)
 
 // which matrix each workgroup of a launch belongs to
 struct Maps {
-    unsigned *prep, *items[3][4], *finish[3][4];        // [product][shape]
+    unsigned *prep, *items[KINDS][SHAPE_COUNT], *finish[KINDS][SHAPE_COUNT];
 };
 static_assert(sizeof(Group) + sizeof(Common) + sizeof(Maps) + 32 <= 4096, "kernel arguments");
 __device__ __forceinline__ void fill(unsigned *map, unsigned first, unsigned count, unsigned value, unsigned at, unsigned step)
@@ -199,7 +200,7 @@ __global__ __launch_bounds__(256) void norm_kernel(Group q, Common f, Entry *tab
     const unsigned part = blockIdx.x - q.first[i], at = part * 256 + threadIdx.x, step = t.norm_count * 256, me = q.base + i;
     if (at == 0) table[me] = t;
     fill(maps.prep, t.prep_first, t.prep_count, me, at, step);
-    for (int k = 0; k < 3; ++k) {
+    for (int k = 0; k < KINDS; ++k) {
         fill(maps.items[k][t.items[k].shape], t.items[k].first, t.items[k].count, me, at, step);
         fill(maps.finish[k][t.items[k].shape], t.items[k].finish_first, t.items[k].finish_count, me, at, step);
     }
@@ -907,8 +908,8 @@ typedef void (*Finish)(const Entry *, const unsigned *, int, int, Common, const 
 struct Shape {
     int bm, bn, threads, per_cu;
     double stage, alone, begin, store;      // us: a stage where all compute units are full, and where each has one workgroup at most; a tile's begin and end; what third ones store besides
-    Product product[3];
-    Finish finish[3];
+    Product product[KINDS];
+    Finish finish[KINDS];
     unsigned tiles(const Sizes &s, int kind) const
     {
         if (kind == THIRD) return (unsigned)((s.Rp + bm - 1) / bm) * ((s.Cp + bn - 1) / bn);
@@ -922,10 +923,10 @@ struct Shape {
     {BM, BN, 64 * WR * WC, PER_CU, __VA_ARGS__,                                                                                                                        \
      {product_kernel<BM, BN, NS, WR, WC, SQUARE_X>, product_kernel<BM, BN, NS, WR, WC, SQUARE_A>, product_kernel<BM, BN, NS, WR, WC, THIRD>}, \
      {finish_kernel<BM, BN, WR, WC, SQUARE_X>, finish_kernel<BM, BN, WR, WC, SQUARE_A>, finish_kernel<BM, BN, WR, WC, THIRD>}}
-// (times measured on 512 x 512 to 8192 x 8192; the model is within a tenth of most launches, S of a quarter)
-constexpr int KINDS = 3, SHAPE_COUNT = 4;
-const Shape SHAPES[SHAPE_COUNT] = {TILES(64, 64, 4, 2, 2, 2, 0.38, 0.26, 4.5, 2), TILES(128, 128, 2, 2, 2, 2, 1.0, 0.66, 10, 14), TILES(192, 192, 2, 2, 3, 1, 1.13, 1.13, 14, 18),
-                                   TILES(256, 256, 2, 2, 4, 1, 1.35, 1.35, 18, 33)};
+// (times measured on 512 x 512 to 8192 x 8192; the model is within a tenth of most launches, those of small tiles a quarter.  64 x 64 twice: four stages in LDS for few tiles, which
+// wait for their loads, or two and twice the workgroups for many short ones.  42 filters of up to 512: 93 tiles of squares 9.6 and 13 us, 615 of thirds 14.8 and 10.8)
+const Shape SHAPES[SHAPE_COUNT] = {TILES(64, 64, 4, 2, 2, 2, 0.38, 0.26, 4.5, 2), TILES(64, 64, 2, 2, 2, 4, 0.76, 0.45, 4.5, 2), TILES(128, 128, 2, 2, 2, 2, 1.0, 0.66, 10, 14),
+                                   TILES(192, 192, 2, 2, 3, 1, 1.13, 1.13, 14, 18), TILES(256, 256, 2, 2, 4, 1, 1.35, 1.35, 18, 33)};
 
 // tiles and stages of a reduction
 struct Load {
@@ -1162,7 +1163,7 @@ static int run(const MuonArgs &q, void *ws, size_t ws_bytes, hipStream_t st)
     if (launched() != MXC_OK) return MXC_ERR_LAUNCH;
     for (int k = 0; k < q.steps; ++k) {
         const int cur = k & 1, last = k == q.steps - 1;
-        for (int mode = SQUARE_X; mode <= THIRD; ++mode) {
+        for (int mode = SQUARE_X; mode < KINDS; ++mode) {
             for (int i = 0; i < SHAPE_COUNT; ++i) {
                 if (!p.count[mode][i]) continue;
                 const Shape &h = SHAPES[i];
