@@ -180,3 +180,20 @@ def test_binding_sizes_past_32_bits(mxc):
                         call(*args[:i], big, *args[i + 1:])
         with pytest.raises(OverflowError):
             mxc.mxc_orthogonalize_workspace_bytes([big], [5])
+
+
+def test_model_refuses_other_rows():
+    """Rows of another length, type or layout than the window's are refused before anything runs; what a step works with lies where the weights do."""
+    import torch
+    from paper_1512_01274_amd.tokens import Model, text
+    model = Model(17, 12, 20, 3, device="cpu")
+    assert all(t is None or t.device.type == "cpu" for t in model._of_batch(5).values())
+    labels = torch.zeros(4, dtype=torch.int32)
+    for rows in (torch.zeros(4, 2, dtype=torch.int32), torch.zeros(4, 3, dtype=torch.int64), torch.zeros(12, dtype=torch.int32), torch.zeros(3, 4, dtype=torch.int32).t()):
+        with pytest.raises(ValueError, match="rows"):
+            model.train_step(rows, labels)
+        with pytest.raises(ValueError, match="rows"):
+            model.predict(rows)
+    assert model.step == 0
+    rows, labels = text(17, 3, device="cpu")(70)
+    assert rows.shape == (70, 3) and labels.shape == (70,) and bool((rows[0] == -1).all()) and torch.equal(rows[1:64, -1], labels[:63])
