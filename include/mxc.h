@@ -450,9 +450,9 @@ int mxc_layernorm_bwd(int N, int C, int dtype, const void *x, const float *gamma
  * bounded) with fp32 sums; the diagonals of A and of b A + c A A are kept apart in fp32, and X is carried with 22 bits.  O's error is about 1e-3 of its
  * norm after 5 steps, in directions of any singular value.  |x| is summed in 64 bits.  Results are bit-identical from run to run and do not depend on the
  * other matrices of a call.  No tensor may overlap another of the call.
- * Workspace: mxc_orthogonalize_workspace_bytes, for both.  Errors, found before anything is launched: MXC_ERR_SHAPE (non-positive count or sides, more
+ * Workspace: mxc_orthogonalize_workspace_bytes, for both; none where every matrix has at most 64 by 576 values, either way.  Errors, found before anything is launched: MXC_ERR_SHAPE (non-positive count or sides, more
  * than MXC_ORTHOGONALIZE_MAX_COUNT matrices, sides above MXC_ORTHOGONALIZE_MAX_SIDE), MXC_ERR_UNSUPPORTED (dtype; steps outside 1..MXC_ORTHOGONALIZE_MAX_STEPS, past which the
- * rounding of small directions grows; momentum outside [0, 1), negative rms, nesterov, factors that are not finite), MXC_ERR_NULL, MXC_ERR_ALIGN (16 bytes),
+ * rounding of small directions grows; momentum outside [0, 1), negative rms, nesterov, factors that are not finite; a matrix twice in y, w, m or w_bf16), MXC_ERR_NULL, MXC_ERR_ALIGN (16 bytes),
  * MXC_ERR_WORKSPACE, MXC_ERR_LAUNCH.
  */
 enum { MXC_ORTHOGONALIZE_MAX_SIDE = 32768, MXC_ORTHOGONALIZE_MAX_STEPS = 6, MXC_ORTHOGONALIZE_MAX_COUNT = 4096 };

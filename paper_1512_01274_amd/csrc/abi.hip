@@ -2,6 +2,7 @@
 // and kernel selection.  See include/mxc.h for the contract of every call.
 #include <string.h>
 
+#include <algorithm>
 #include <cmath>
 #include <mutex>
 #include <string>
@@ -1284,6 +1285,15 @@ static int pointers_check(int count, const void *const *const *tensors, int kind
     return MXC_OK;
 }
 
+// a matrix twice among those that a call writes: its two updates would race
+static bool twice(int count, const void *const *tensors)
+{
+    const void *sorted[MXC_ORTHOGONALIZE_MAX_COUNT];
+    std::copy(tensors, tensors + count, sorted);
+    std::sort(sorted, sorted + count);
+    return std::adjacent_find(sorted, sorted + count) != sorted + count;
+}
+
 int mxc_orthogonalize_workspace_bytes(int count, const int *rows, const int *cols, size_t *out_bytes)
 {
     if (!out_bytes) return MXC_ERR_NULL;
@@ -1299,6 +1309,7 @@ int mxc_orthogonalize(int count, const int *rows, const int *cols, const void *c
     const void *const *const tensors[] = {x, y};
     MXC_TRY(pointers_check(count, tensors, 2));
     if (misaligned(workspace)) return MXC_ERR_ALIGN;
+    if (twice(count, y)) return MXC_ERR_UNSUPPORTED;
     MuonArgs a = {};
     a.count = count; a.rows = rows; a.cols = cols; a.u = x; a.dtype = dtype; a.y = y; a.steps = steps;
     return muon_run(a, workspace, workspace_bytes, (hipStream_t)hip_stream);
@@ -1316,6 +1327,7 @@ int mxc_muon_update(int count, const int *rows, const int *cols, float *const *w
     const void *const *const tensors[] = {(const void *const *)w, g, (const void *const *)m, (const void *const *)w_bf16};
     MXC_TRY(pointers_check(count, tensors, w_bf16 ? 4 : 3));
     if (misaligned(workspace)) return MXC_ERR_ALIGN;
+    if (twice(count, tensors[0]) || twice(count, tensors[2]) || (w_bf16 && twice(count, w_bf16))) return MXC_ERR_UNSUPPORTED;
     MuonArgs a = {};
     a.count = count; a.rows = rows; a.cols = cols; a.u = g; a.dtype = grad_dtype; a.w = w; a.m = m; a.w_bf16 = w_bf16;
     a.steps = steps; a.nesterov = nesterov; a.momentum = (float)momentum; a.grad_scale = (float)grad_scale; a.keep = (float)(1.0 - lr * wd); a.lr = lr; a.rms = rms;

@@ -439,7 +439,7 @@ BwdPlan bwd_plan(int N, int C, int dtype)
         const long long columns = (C + 256ll * VE - 1) / (256ll * VE);
         const long long want = columns >= 1024 ? 1 : 1024 / columns;          // ranges of rows, for about four workgroups a compute unit
         q.rows = (int)((N + want - 1) / want);
-        q.ranges = (N + q.rows - 1) / q.rows;
+        q.ranges = (int)(((long long)N + q.rows - 1) / q.rows);
         q.sums_bytes = align_up((size_t)N * 8, 256);
     }
     q.part_bytes = align_up((size_t)q.ranges * 2 * q.pitch * 4, 256);

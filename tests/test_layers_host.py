@@ -108,6 +108,11 @@ def test_muon_refusals(mxc):
         assert muon(**bad) == mxc.MXC_ERR_NULL, bad
     for bad in (dict(g=arrays(A + 2, B)), dict(m=arrays(A, B + 8)), dict(wb=arrays(A + 2, B))):
         assert muon(**bad) == mxc.MXC_ERR_ALIGN, bad
+    # a matrix twice among those that are written: small ones too, which need no workspace
+    for sides in (dict(), dict(rows=two(3, 3), cols=two(4, 4))):
+        assert orth(y=arrays(C_, C_), **sides) == mxc.MXC_ERR_UNSUPPORTED
+        for bad in (dict(w=arrays(A, A)), dict(m=arrays(E, E)), dict(wb=arrays(G, G))):
+            assert muon(**bad, **sides) == mxc.MXC_ERR_UNSUPPORTED, bad
     # matrices that a compute unit holds need none
     assert mxc.mxc_orthogonalize_workspace_bytes([64, 1, 576], [576, 1, 64]) == 0
     assert mxc.mxc_orthogonalize_workspace_bytes([64], [577]) > 0 and mxc.mxc_orthogonalize_workspace_bytes([65], [65]) > 0
@@ -197,3 +202,10 @@ def test_model_refuses_other_rows():
     assert model.step == 0
     rows, labels = text(17, 3, device="cpu")(70)
     assert rows.shape == (70, 3) and labels.shape == (70,) and bool((rows[0] == -1).all()) and torch.equal(rows[1:64, -1], labels[:63])
+
+
+def test_layernorm_workspace_of_the_longest(mxc):
+    """The most rows of rows that registers do not hold: two sums a row and a share of the weights' gradients, in sizes past 32 bits."""
+    for C in (40000, mxc.MXC_LAYERNORM_MAX_C):
+        need = [mxc.mxc_layernorm_workspace_bytes(N, C, 1) for N in (1 << 30, (1 << 31) - 4096, (1 << 31) - 1)]
+        assert need == sorted(need) and need[-1] >= 8 * ((1 << 31) - 1) + 8 * C
