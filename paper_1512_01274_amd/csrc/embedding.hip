@@ -1,8 +1,8 @@
-// Embedding: y[n] = scale * w[tokens[n]], and the gradient of the table, dw[v] = scale * sum of dy[n] over the places n where tokens[n] == v, in
-// the order of n.  Memory bounds both: forward reads and writes each row once; the gradient reads dy once and writes a row of dw for every
+// Embedding: y[n] = scale * w[tokens[n]], and the gradient of the table, dw[v] = scale * sum of dy[n] over the places n where tokens[n] == v.
+// Memory bounds both: forward reads and writes each row once; the gradient reads dy once and writes a row of dw for every
 // token of the vocabulary.  The gradient of more than a few places goes by the tokens' order, in three launches: the places are sorted by their token, each token's rows added, in
 // parts, and the parts of a token that has several joined.  16384 rows of 4096 bf16 41.6 us, 6.5 TB/s (64 rows 3.9, a launch); gradient of 32768 places on 50257 x 2048, bf16,
-// 138 us; of 500 places on 1000 x 512 fp32, in one launch, 8.4.
+// 137 us; of 500 places on 1000 x 512 fp32, added to it, in one launch, 5.2.
 #include "pieces.h"
 
 namespace mxc {
@@ -84,13 +84,46 @@ __device__ __forceinline__ void add_rows(const T *dy, int c, int C, const int *p
     if constexpr (AHEAD > 1) add_rows<AHEAD / 4>(dy, c, C, places + k, count - k, s);
 }
 
-// Few places, one launch: the workgroup of a place looks for its token among all places and, if the place is the first that has it, adds their rows;
-// workgroups behind them look which of ZERO_ROWS rows of dw have no place and clear these.
-constexpr int FEW = 1024, ZERO_ROWS = 64;
-template <class T>
-__global__ __launch_bounds__(NT) void few_kernel(int N, int V, int C, const int *tokens, const T *dy, float scale, int add, float *dw)
+// zeros for those of rows [v0, v0 + rows) of which clear() is true, by a workgroup: long rows one after the other, short ones together
+template <bool PAST, class F>
+__device__ __forceinline__ void clear_rows(float *dw, int v0, int rows, int C, F &&clear)
+{
+    const float zeros[4] = {0.f, 0.f, 0.f, 0.f};
+    if (C > 256) {
+        for (int r = 0; r < rows; ++r)
+            if (clear(r))
+                for (int c = threadIdx.x * 4; c < C; c += NT * 4) put<PAST>(dw + (size_t)(v0 + r) * C, c, C, zeros, 1.f, false);
+    } else {
+        const unsigned quads = (unsigned)(C + 3) / 4;
+        for (int i = threadIdx.x; i < rows * (int)quads; i += NT) {
+            const int r = (int)((unsigned)i / quads);
+            if (clear(r)) put<PAST>(dw + (size_t)(v0 + r) * C, (i - r * (int)quads) * 4, C, zeros, 1.f, false);
+        }
+    }
+}
+
+// Groups of L = 1 << log_lanes threads hold sums of the same 4 L columns; those of the first group become the sums of all.
+__device__ __forceinline__ void add_groups(float (&s)[4], float4 *room, int log_lanes)
+{
+    room[threadIdx.x] = make_float4(s[0], s[1], s[2], s[3]);
+    __syncthreads();
+    if (threadIdx.x >> log_lanes) return;
+    for (unsigned k = threadIdx.x + (1 << log_lanes); k < NT; k += 1 << log_lanes) {
+        const float4 o = room[k];
+        s[0] += o.x; s[1] += o.y; s[2] += o.z; s[3] += o.w;
+    }
+}
+// lanes of a group: 16 to 64, as the columns need
+int group_lanes(int C) { return C <= 64 ? 4 : C <= 128 ? 5 : 6; }
+
+// Few places, one launch: the workgroup of a place looks for its token among all places and, if the place is the first that has it, adds their rows,
+// of which each group of L threads takes a run; workgroups behind them look which of ZERO_ROWS rows of dw have no place and clear these.
+constexpr int FEW = 2048, ZERO_ROWS = 64;
+template <class T, bool PAST>
+__global__ __launch_bounds__(NT) void few_kernel(int N, int V, int C, int log_lanes, const int *tokens, const T *dy, float scale, int add, float *dw)
 {
     __shared__ int places[FEW];
+    __shared__ float4 room[NT];
     constexpr int TURNS = FEW / NT, nt = NT;
     __shared__ int wave_count[TURNS * (NT / 64)];
     const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
@@ -104,11 +137,8 @@ __global__ __launch_bounds__(NT) void few_kernel(int N, int V, int C, const int 
             if (d >= 0 && d < ZERO_ROWS) found[d] = 1;
         }
         __syncthreads();
-        const int rows = (int)min((long long)ZERO_ROWS, V - v0);
-        const float zeros[4] = {0.f, 0.f, 0.f, 0.f};
-        for (int r = 0; r < rows; ++r)
-            if (!found[r])
-                for (int c = ((int)blockIdx.y * nt + threadIdx.x) * 4; c < C; c += nt * 4 * gridDim.y) put<false>(dw + (size_t)(v0 + r) * C, c, C, zeros, 1.f, false);
+        const int of = (ZERO_ROWS + (int)gridDim.y - 1) / (int)gridDim.y, r0 = (int)blockIdx.y * of, rows = (int)min((long long)min(of, ZERO_ROWS - r0), V - v0 - r0);
+        clear_rows<PAST>(dw, (int)v0 + r0, rows, C, [&](int r) __attribute__((always_inline)) { return !found[r0 + r]; });
         return;
     }
     const int me = blockIdx.x;
@@ -140,11 +170,12 @@ __global__ __launch_bounds__(NT) void few_kernel(int N, int V, int C, const int 
         if (other[j] == t) places[at + __popcll(same[j] & ((1ull << lane) - 1))] = j * NT + threadIdx.x;
     }
     __syncthreads();
-    for (int c = ((int)blockIdx.y * nt + threadIdx.x) * 4; c < C; c += nt * 4 * gridDim.y) {
-        float s[4] = {0.f, 0.f, 0.f, 0.f};
-        add_rows<16>(dy, c, C, places, count, s);
-        put<false>(dw + (size_t)t * C, c, C, s, scale, add);
-    }
+    const int L = 1 << log_lanes, c = ((int)blockIdx.y * L + (threadIdx.x & (L - 1))) * 4, share = (count + (NT >> log_lanes) - 1) / (NT >> log_lanes);
+    const int k0 = min(count, (int)(threadIdx.x >> log_lanes) * share), k1 = min(count, k0 + share);
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+    add_rows<16>(dy, c < C ? c : 0, C, places + k0, k1 - k0, s);
+    if (count > 1) add_groups(s, room, log_lanes);
+    if (threadIdx.x < (unsigned)L && c < C) put<PAST>(dw + (size_t)t * C, c, C, s, scale, add);
 }
 
 // The places in the order of their tokens (of equal tokens in their own), and where each token's begin.  Workgroup (x, y) puts the places of segment y
@@ -275,7 +306,7 @@ __global__ __launch_bounds__(ORDER_NT) void order_kernel(int N, int V, int R, in
 // Sums of each token's rows: a wave for PART (16 to 64) places of the order and 256 columns.  Its lanes hold the places and their tokens, so that all control is the wave's; it loads the
 // rows of 16 places at once and adds them one after the other, and where the token changes the sum is the token's row of dw, or, of a token that has places in other
 // parts too, this part's share: slot 0 for the token of the part's first place, slot 1 for one that begins within it.  Workgroups behind the parts' clear the rows of
-// tokens that stand nowhere (between the parts', 4 % slower).  32768 places on 50257 x 2048 from memory, bf16: 117 us of the gradient's 144, 4.7 TB/s.
+// tokens that stand nowhere (between the parts', 4 % slower).  32768 places on 50257 x 2048 from memory, bf16: 117 us of the gradient's 137, 4.7 TB/s.
 constexpr int BLOCK = 256;
 template <class T, bool PAST>
 __global__ __launch_bounds__(NT) void rows_kernel(int V, int C, int PART, long long part_waves, unsigned part_groups, int empty_rows, const int *tokens,
@@ -286,18 +317,7 @@ __global__ __launch_bounds__(NT) void rows_kernel(int V, int C, int PART, long l
     if (blockIdx.x >= part_groups) {
         const int v0 = (int)(blockIdx.x - part_groups) * empty_rows, rows = min(empty_rows, V - v0);
         const unsigned long long empty = __ballot(lane < rows && start[v0 + min(lane, rows - 1)] == start[v0 + min(lane, rows - 1) + 1]);
-        const float zeros[4] = {0.f, 0.f, 0.f, 0.f};
-        if (C > 256) {
-            for (int r = 0; r < rows; ++r)
-                if (empty >> r & 1)
-                    for (int c = threadIdx.x * 4; c < C; c += NT * 4) put<PAST>(dw + (size_t)(v0 + r) * C, c, C, zeros, 1.f, false);
-        } else {
-            const unsigned quads = (unsigned)(C + 3) / 4;
-            for (unsigned i = threadIdx.x; i < rows * quads; i += NT) {
-                const unsigned r = i / quads;
-                if (empty >> r & 1) put<PAST>(dw + (size_t)(v0 + (int)r) * C, (int)(i - r * quads) * 4, C, zeros, 1.f, false);
-            }
-        }
+        clear_rows<PAST>(dw, v0, rows, C, [&](int r) __attribute__((always_inline)) { return (empty >> r & 1) != 0; });
         return;
     }
     const long long w = (long long)blockIdx.x * (NT / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -341,17 +361,18 @@ __global__ __launch_bounds__(NT) void rows_kernel(int V, int C, int PART, long l
     }
 }
 
-// A part in which a token begins that ends in another adds up that token's shares: a workgroup for 256 columns, whose waves take a quarter of the shares each.
-__global__ __launch_bounds__(NT) void join_kernel(int V, int C, int PART, const int *tokens, const int *order, const int *start, const float *parts, float scale, int add, float *dw)
+// A part in which a token begins that ends in another adds up that token's shares: a workgroup for 4 L columns, whose groups of L threads take a run of the shares each.
+__global__ __launch_bounds__(NT) void join_kernel(int V, int C, int PART, int log_lanes, const int *tokens, const int *order, const int *start, const float *parts, float scale, int add,
+                                                 float *dw)
 {
     constexpr int AHEAD = 16;
-    __shared__ float4 sum[NT];
+    __shared__ float4 room[NT];
     const int all = start[V], part = blockIdx.x, p0 = part * PART, p1 = p0 + PART;
     if (p1 >= all) return;
     const int t = tokens[order[p1 - 1]], s0 = start[t], s1 = start[t + 1];
     if (s0 < p0 || s1 <= p1) return;
-    const int shares = (s1 - 1) / PART - part + 1, wave = threadIdx.x >> 6, quarter = (shares + NT / 64 - 1) / (NT / 64), c = ((int)blockIdx.y * 64 + (threadIdx.x & 63)) * 4;
-    const int q0 = wave * quarter, q1 = min(shares, q0 + quarter), at = c < C ? c : 0;
+    const int L = 1 << log_lanes, groups = NT >> log_lanes, c = ((int)blockIdx.y * L + (threadIdx.x & (L - 1))) * 4, at = c < C ? c : 0;
+    const int shares = (s1 - 1) / PART - part + 1, run = (shares + groups - 1) / groups, q0 = (int)(threadIdx.x >> log_lanes) * run, q1 = min(shares, q0 + run);
     float s[4] = {0.f, 0.f, 0.f, 0.f};
     for (int q = q0; q < q1; q += AHEAD) {
         Piece<float> g[AHEAD];
@@ -367,15 +388,8 @@ __global__ __launch_bounds__(NT) void join_kernel(int V, int C, int PART, const 
             for (int i = 0; i < 4; ++i) s[i] += q + j < q1 ? g[j].get(i) : 0.f;
         }
     }
-    sum[threadIdx.x] = make_float4(s[0], s[1], s[2], s[3]);
-    __syncthreads();
-    if (wave || c >= C) return;
-#pragma unroll
-    for (int k = 1; k < NT / 64; ++k) {
-        const float4 o = sum[k * 64 + threadIdx.x];
-        s[0] += o.x; s[1] += o.y; s[2] += o.z; s[3] += o.w;
-    }
-    put<false>(dw + (size_t)t * C, c, C, s, scale, add);
+    add_groups(s, room, log_lanes);
+    if (threadIdx.x < (unsigned)L && c < C) put<false>(dw + (size_t)t * C, c, C, s, scale, add);
 }
 
 struct OrderPlan {
@@ -423,12 +437,20 @@ int fwd(int N, int V, int C, const int *tokens, const T *w, float scale, T *y, h
     return launched();
 }
 
+// groups of the whole workgroup where those of a wave would make too many workgroups, each of which looks at all places
+// One launch or three.  Up to 1024 places one; up to 2048 where the looking (each place among all, for each 256 columns) and the longest run of one workgroup cost less than two
+// launches: us, one and three: 2048 places on 50257 x 512 bf16 8.1, 21.6; x 2048 17.7, 27.4; on 5000 x 4096 fp32 53, 33.5; on 2 x 512 30.6, 20.3; 4096 places on 10000 x 300 31, 21
+bool is_few(int N, int V, int C) { return N <= 1024 || (N <= FEW && V >= 256 && (long long)N * C <= 1 << 22); }
+int few_lanes(int N, int C) { return (long long)N * ((C + 255) / 256) <= 4096 ? group_lanes(C) : 8; }
+
 template <class T>
 int bwd(int N, int V, int C, const int *tokens, const T *dy, float scale, int add, float *dw, char *ws, hipStream_t st)
 {
-    if (N <= FEW) {
-        const unsigned grid = (unsigned)(N + (add ? 0 : ((long long)V + ZERO_ROWS - 1) / ZERO_ROWS)), columns = (unsigned)((C + NT * 4 - 1) / (NT * 4));
-        hipLaunchKernelGGL(few_kernel<T>, dim3(grid, columns), dim3(NT), 0, st, N, V, C, tokens, dy, scale, add, dw);
+    const bool past = !add && (unsigned long long)V * C * 4 >= 256ull << 20;
+    if (is_few(N, V, C)) {
+        const int log_lanes = few_lanes(N, C), columns = 4 << log_lanes;
+        const unsigned grid = (unsigned)(N + (add ? 0 : ((long long)V + ZERO_ROWS - 1) / ZERO_ROWS));
+        hipLaunchKernelGGL(past ? (few_kernel<T, true>) : (few_kernel<T, false>), dim3(grid, (C + columns - 1) / columns), dim3(NT), 0, st, N, V, C, log_lanes, tokens, dy, scale, add, dw);
         return launched();
     }
     const OrderPlan q = order_plan(N, V, C);
@@ -439,11 +461,11 @@ int bwd(int N, int V, int C, const int *tokens, const T *dy, float scale, int ad
     const long long part_waves = q.part_count * ((C + BLOCK - 1) / BLOCK);
     const int empty_rows = C <= 256 ? 64 : 16;
     const unsigned part_groups = (unsigned)((part_waves + NT / 64 - 1) / (NT / 64)), empty_groups = add ? 0 : (unsigned)((V + empty_rows - 1) / empty_rows);
-    const bool past = !add && (unsigned long long)V * C * 4 >= 256ull << 20;
     hipLaunchKernelGGL(past ? (rows_kernel<T, true>) : (rows_kernel<T, false>), dim3(part_groups + empty_groups), dim3(NT), 0, st, V, C, q.part, part_waves, part_groups, empty_rows,
                        tokens, order, start, dy, scale, add, dw, parts);
     if (launched() != MXC_OK) return MXC_ERR_LAUNCH;
-    hipLaunchKernelGGL(join_kernel, dim3((unsigned)q.part_count, (C + BLOCK - 1) / BLOCK), dim3(NT), 0, st, V, C, q.part, tokens, order, start, parts, scale, add, dw);
+    const int log_lanes = group_lanes(C);
+    hipLaunchKernelGGL(join_kernel, dim3((unsigned)q.part_count, (C + (4 << log_lanes) - 1) / (4 << log_lanes)), dim3(NT), 0, st, V, C, q.part, log_lanes, tokens, order, start, parts, scale, add, dw);
     return launched();
 }
 
@@ -456,7 +478,7 @@ int embedding_fwd(int N, int V, int C, int dtype, const int *tokens, const void 
 
 size_t embedding_workspace(int N, int V, int C)
 {
-    if (N <= FEW) return 0;
+    if (is_few(N, V, C)) return 0;
     const OrderPlan q = order_plan(N, V, C);
     return q.order_bytes + q.start_bytes + q.part_bytes;
 }

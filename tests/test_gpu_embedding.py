@@ -93,7 +93,10 @@ def test_forward_values_that_are_not_finite(mxc):
 
 GRADS = [(1, 1, 1, "uniform"), (3, 7, 5, "uniform"), (500, 100, 64, "common"), (1000, 1000, 33, "uniform"), (1024, 3, 520, "one"), (1024, 70, 8, "none"),
          (1025, 3, 520, "one"), (1025, 70, 8, "none"), (1500, 64, 1, "common"), (3000, 1, 3, "uniform"), (5000, 257, 1031, "common"), (4096, 4000, 24, "runs129"),
-         (4100, 4000, 136, "runs128"), (9999, 2, 2056, "two"), (20000, 50257, 8, "common"), (2049, 300000, 4, "uniform"), (70001, 999, 16, "common")]
+         (4100, 4000, 136, "runs128"), (9999, 2, 2056, "two"), (20000, 50257, 8, "common"), (2049, 300000, 4, "uniform"), (70001, 999, 16, "common"),
+         # on either side of where one launch does it
+         (2048, 256, 40, "common"), (2049, 256, 40, "common"), (2048, 255, 33, "common"), (2048, 300, 2048, "common"), (2048, 300, 2049, "common"), (1500, 400, 2100, "one"),
+         (1100, 257, 65, "one"), (1024, 3, 129, "two")]
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
