@@ -35,32 +35,52 @@ constexpr float X_UP = 32768.f, X_DOWN = 1.f / 32768.f, LO_UP = 2048.f, LO_DOWN 
 constexpr int BK = 64;                      // reduction of a stage, and what sides are padded to
 constexpr int NORM_MOST = 1024, NORM_CHUNK = 2048;
 constexpr int KINDS = 3, SHAPE_COUNT = 5;   // products of a step, shapes of their tiles
+constexpr int SMALL_M = 64, SMALL_N = 576;
+__host__ __device__ inline bool is_small(int R, int C) { return (R < C ? R : C) <= SMALL_M && (R < C ? C : R) <= SMALL_N; }
 
-// One matrix of a call.  Z is ping-ponged where the third product reads it (tall), its transpose where it does not (wide); the other pair of pointers is one buffer.
-struct Entry {
-    int R, C, Rp, Cp;                       // rows, columns, and padded to BK
-    int mp, tall;                           // the padded shorter side; rows > cols
-    int norm_count, norm_parts;             // workgroups that sum the squares, and what they leave
-    float step;                             // w' = keep w - step O
+// The work items of a matrix in the launches of a product
+struct Items {
+    unsigned first, count;                  // tiles, the last of them in `split` ranges of the reduction each
+    unsigned whole, split;                  // tiles that are not split
+    unsigned part_first, finish_first, finish_count;            // of the split ones: the first one's first partial sums; workgroups that add them
+    unsigned short shape, side;             // of the tiles: a launch each
+};
+// One matrix of a call: what the host knows
+struct Given {
+    int R, C;
     const void *u;                          // x, or the gradient
     bf16_t *y;                              // y, or the bf16 copy of w
+    float *w, *m;
+    char *room;                             // its part of the workspace
+    float step;                             // w' = keep w - step O
+    unsigned prep_first;                    // among the tiles of prepare_kernel
+    Items items[KINDS];
+};
+constexpr int GROUP = 22;
+struct Group {
+    Given t[GROUP];
+    unsigned first[GROUP + 1];
+    int count, base;
+};
+struct Sizes {
+    int Rp, Cp, mp;                         // rows, columns and the shorter side, padded to BK
+    int norm_count, norm_parts;             // workgroups that sum the squares, and what they leave
+    size_t mat, sq, side;                   // bytes of one orientation of X, of A, of a diagonal
+    unsigned prep;                          // tiles of prepare_kernel
+    size_t bytes;
+};
+// and what the kernels read.  Z is ping-ponged where the third product reads it (tall), its transpose where it does not (wide); the other pair of pointers is one buffer.
+struct Entry {
+    int R, C, Rp, Cp, mp, tall, norm_parts;
+    float step;
+    const void *u;
+    bf16_t *y;
     float *w, *m;
     f16_t *z[2], *zt[2], *lo, *O, *P;
     float *d, *e;
     double *norm;
-    unsigned prep_first, prep_count;        // tiles of prepare_kernel
-    struct Items {                          // of the launches of each product
-        unsigned first, count;              // work items: tiles, the last of them in `split` ranges of the reduction each
-        unsigned whole, split;              // tiles that are not split
-        unsigned part_first, finish_first, finish_count;        // of the split ones: the first one's first partial sums; workgroups that add them
-        int shape;                          // of the tiles: a launch each
-    } items[KINDS];
-};
-constexpr int GROUP = 14;
-struct Group {
-    Entry t[GROUP];
-    unsigned first[GROUP + 1];
-    int count, base;
+    unsigned prep_first;
+    Items items[KINDS];
 };
 struct Common {
     float momentum, grad_scale, keep;
@@ -119,8 +139,7 @@ struct Values {
 // Matrices of up to SMALL_M by SMALL_N (either way), which a compute unit holds: X, its shorter side as rows, in blocks of 32 x 32, the b-th at row 32 * (b % 2) and column
 // 32 * (b / 2), block b belonging to wave b % 16; a lane has row lane % 32 and of the columns 8 g + 4 (lane / 32) + 0 .. 3.  Their squares are added in this order wherever it is
 // done.
-constexpr int SMALL_M = 64, SMALL_N = 576, SMALL_BLOCKS = (SMALL_N / 32 * 2 + 15) / 16;
-__host__ __device__ inline bool is_small(int R, int C) { return (R < C ? R : C) <= SMALL_M && (R < C ? C : R) <= SMALL_N; }
+constexpr int SMALL_BLOCKS = (SMALL_N / 32 * 2 + 15) / 16;
 // Block b's values, zeros outside of the matrix; the momentum is made of the gradient on the way.
 template <bool BF16>
 __device__ __forceinline__ void block_values(const Common &f, int R, int C, const void *u, float *mom, int b, int lane, float (&v)[4][4])
@@ -181,9 +200,88 @@ __device__ __forceinline__ double wave_total(double s)
 
 // ---- sums of squares, the momentum, and the table of the call's matrices ---------------------------------------------------------------------
 
-// which matrix each workgroup of a launch belongs to
+enum { SQUARE_X, SQUARE_A, THIRD };         // A, then P and e, then the next X
+
+// (i, j), i <= j, of the t-th tile of the upper triangle of T x T, row by row
+__device__ __forceinline__ void triangle(unsigned t, unsigned T, unsigned &i, unsigned &j)
+{
+    const float b = 2.f * T + 1.f;
+    unsigned k = (unsigned)fmaxf(0.f, (b - sqrtf(b * b - 8.f * (float)t)) * 0.5f);
+    auto start = [&](unsigned r) { return r * T - r * (r - 1) / 2; };       // (for r = 0: 0 - 0)
+    while (k > 0 && start(k) > t) --k;
+    while (start(k + 1) <= t) ++k;
+    i = k;
+    j = k + t - start(k);
+}
+
+// where tile `tile` of a matrix lies, of side x side: its first row and column
+__device__ __forceinline__ void place(int Rp, int Cp, int mp, int kind, unsigned side, unsigned tile, int &m0, int &n0)
+{
+    unsigned ti, tj;
+    if (kind == THIRD) {
+        // in bands of 8 rows of tiles, column by column
+        const unsigned across = (Cp + side - 1) / side, down = (Rp + side - 1) / side;
+        const unsigned band = tile / (8 * across), rows = min(8u, down - band * 8), in = tile - band * 8 * across;
+        ti = band * 8 + in % rows;
+        tj = in / rows;
+    } else {
+        triangle(tile, (mp + side - 1) / side, ti, tj);
+    }
+    m0 = ti * side;
+    n0 = tj * side;
+}
+
+// What a workgroup of a product's launch does
+struct Work {
+    unsigned matrix;
+    int m0, n0;                             // its tile
+    int part;                               // which of the matrix's partial sums, or -1: a whole tile
+};
+__host__ __device__ inline Sizes sizes_of(int R, int C)
+{
+    auto up = [](size_t bytes, size_t to) { return (bytes + to - 1) / to * to; };
+    Sizes s;
+    s.Rp = (int)up(R, BK);
+    s.Cp = (int)up(C, BK);
+    s.mp = R <= C ? s.Rp : s.Cp;
+    const unsigned chunks = ((unsigned)R * (unsigned)C + NORM_CHUNK - 1) / NORM_CHUNK;
+    s.norm_count = is_small(R, C) ? 4 : chunks < NORM_MOST ? (int)chunks : NORM_MOST;
+    s.norm_parts = is_small(R, C) ? 16 : s.norm_count;
+    s.mat = up((size_t)s.Rp * s.Cp * 2, 256);
+    s.sq = up((size_t)s.mp * s.mp * 2, 256);
+    s.side = up((size_t)s.mp * 4, 256);
+    s.prep = (unsigned)(s.Rp / BK) * (s.Cp / BK);
+    s.bytes = 4 * s.mat + 2 * s.sq + 2 * s.side + up((size_t)s.norm_parts * 8, 256);
+    return s;
+}
+__device__ __forceinline__ Entry entry_of(const Given &g, const Sizes &s)
+{
+    Entry t;
+    t.R = g.R; t.C = g.C; t.Rp = s.Rp; t.Cp = s.Cp; t.mp = s.mp; t.tall = g.R > g.C; t.norm_parts = s.norm_parts; t.step = g.step;
+    t.u = g.u; t.y = g.y; t.w = g.w; t.m = g.m;
+    char *at = g.room;
+    auto take = [&](size_t bytes) { char *to = at; at += bytes; return to; };
+    t.norm = (double *)at;                  // (first: norm_kernel finds it there)
+    take(s.bytes - 4 * s.mat - 2 * s.sq - 2 * s.side);
+    t.z[0] = (f16_t *)take(s.mat);
+    t.zt[0] = (f16_t *)take(s.mat);
+    f16_t *second = (f16_t *)take(s.mat);
+    t.z[1] = t.tall ? second : t.z[0];
+    t.zt[1] = t.tall ? t.zt[0] : second;
+    t.lo = (f16_t *)take(s.mat);
+    t.O = (f16_t *)take(s.sq);
+    t.P = (f16_t *)take(s.sq);
+    t.d = (float *)take(s.side);
+    t.e = (float *)take(s.side);
+    t.prep_first = g.prep_first;
+#pragma unroll
+    for (int k = 0; k < KINDS; ++k) t.items[k] = g.items[k];
+    return t;
+}
+// which matrix each workgroup of the other launches belongs to
 struct Maps {
-    unsigned *prep, *items[KINDS][SHAPE_COUNT], *finish[KINDS][SHAPE_COUNT];
+    unsigned *prep, *finish[KINDS][SHAPE_COUNT];
+    Work *items[KINDS][SHAPE_COUNT];
 };
 static_assert(sizeof(Group) + sizeof(Common) + sizeof(Maps) + 32 <= 4096, "kernel arguments");
 __device__ __forceinline__ void fill(unsigned *map, unsigned first, unsigned count, unsigned value, unsigned at, unsigned step)
@@ -194,15 +292,26 @@ __device__ __forceinline__ void fill(unsigned *map, unsigned first, unsigned cou
 template <bool BF16>
 __global__ __launch_bounds__(256) void norm_kernel(Group q, Common f, Entry *table, Maps maps)
 {
-    int i = 0;
-    while (i + 1 < q.count && blockIdx.x >= q.first[i + 1]) ++i;
-    const Entry &t = q.t[i];
-    const unsigned part = blockIdx.x - q.first[i], at = part * 256 + threadIdx.x, step = t.norm_count * 256, me = q.base + i;
-    if (at == 0) table[me] = t;
-    fill(maps.prep, t.prep_first, t.prep_count, me, at, step);
+    // (its lanes look at all matrices at once)
+    const int looked = min((int)(threadIdx.x & 63), q.count - 1), i = __builtin_amdgcn_readfirstlane(63 - __clzll(__ballot(blockIdx.x >= q.first[looked] && (int)(threadIdx.x & 63) < q.count)));
+    const Given &t = q.t[i];
+    const Sizes z = sizes_of(t.R, t.C);
+    double *const norm = (double *)t.room;
+    const unsigned part = blockIdx.x - q.first[i], at = part * 256 + threadIdx.x, step = z.norm_count * 256, me = q.base + i;
+    if (at == 0) table[me] = entry_of(t, z);
+    fill(maps.prep, t.prep_first, z.prep, me, at, step);
     for (int k = 0; k < KINDS; ++k) {
-        fill(maps.items[k][t.items[k].shape], t.items[k].first, t.items[k].count, me, at, step);
-        fill(maps.finish[k][t.items[k].shape], t.items[k].finish_first, t.items[k].finish_count, me, at, step);
+        const Items &items = t.items[k];
+        // workgroups go to the XCDs in turn: each XCD has items of the matrix that follow each other, so that its L2 serves several with what one reads
+        auto spread = [](unsigned i, unsigned count) { return i % 8 * (count / 8) + min(i % 8, count % 8) + i / 8; };
+        for (unsigned i = at; i < items.count; i += step) {
+            const bool whole = i < items.whole;
+            const unsigned piece = whole ? 0 : spread(i - items.whole, items.count - items.whole);
+            Work w = {me, 0, 0, whole ? -1 : (int)piece};
+            place(z.Rp, z.Cp, z.mp, k, items.side, whole ? spread(i, items.whole) : items.whole + piece / items.split, w.m0, w.n0);
+            maps.items[k][items.shape][items.first + i] = w;
+        }
+        fill(maps.finish[k][items.shape], items.finish_first, items.finish_count, me, at, step);
     }
     if (is_small(t.R, t.C)) {               // a wave's blocks
         const int wave = part * 4 + (threadIdx.x >> 6), blocks = (max(t.R, t.C) + BK - 1) / BK * BK / 32 * 2;
@@ -213,7 +322,7 @@ __global__ __launch_bounds__(256) void norm_kernel(Group q, Common f, Entry *tab
             s = squares_of(v, s);
         }
         s = wave_total(s);
-        if ((threadIdx.x & 63) == 0) t.norm[wave] = s;
+        if ((threadIdx.x & 63) == 0) norm[wave] = s;
         return;
     }
     const int n = t.R * t.C;                // (2^30 at most)
@@ -221,7 +330,7 @@ __global__ __launch_bounds__(256) void norm_kernel(Group q, Common f, Entry *tab
     float *m = t.m;
     double s = 0.0;
     constexpr int AHEAD = 4;
-    const long long every = (long long)t.norm_count * 1024;
+    const long long every = (long long)z.norm_count * 1024;
     for (long long k0 = (long long)(part * 256 + threadIdx.x) * 4; k0 < n; k0 += AHEAD * every) {
         Values<BF16, true> q[AHEAD];
 #pragma unroll
@@ -240,7 +349,7 @@ __global__ __launch_bounds__(256) void norm_kernel(Group q, Common f, Entry *tab
     s = wave_total(s);
     if ((threadIdx.x & 63) == 0) wave_sum[threadIdx.x >> 6] = s;
     __syncthreads();
-    if (threadIdx.x == 0) t.norm[part] = wave_sum[0] + wave_sum[1] + wave_sum[2] + wave_sum[3];
+    if (threadIdx.x == 0) norm[part] = wave_sum[0] + wave_sum[1] + wave_sum[2] + wave_sum[3];
 }
 
 // 1 / norm, at X's power of two, as a power of two and a factor of ordinary size.  A value that is not finite makes NaN of the whole matrix; zeros stay zeros
@@ -314,39 +423,6 @@ __device__ __forceinline__ void wave_sync()
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-}
-
-enum { SQUARE_X, SQUARE_A, THIRD };         // A, then P and e, then the next X
-
-// (i, j), i <= j, of the t-th tile of the upper triangle of T x T, row by row
-__device__ __forceinline__ void triangle(unsigned t, unsigned T, unsigned &i, unsigned &j)
-{
-    const float b = 2.f * T + 1.f;
-    unsigned k = (unsigned)fmaxf(0.f, (b - sqrtf(b * b - 8.f * (float)t)) * 0.5f);
-    auto start = [&](unsigned r) { return r * T - r * (r - 1) / 2; };       // (for r = 0: 0 - 0)
-    while (k > 0 && start(k) > t) --k;
-    while (start(k + 1) <= t) ++k;
-    i = k;
-    j = k + t - start(k);
-}
-
-// where tile `tile` of a matrix lies: its first row and column
-template <int BM, int BN, int MODE>
-__device__ __forceinline__ void place(const Entry &t, unsigned tile, int &m0, int &n0)
-{
-    unsigned ti, tj;
-    if (MODE == THIRD) {
-        // in bands of 8 rows of tiles, column by column
-        const unsigned across = (t.Cp + BN - 1) / BN, down = (t.Rp + BM - 1) / BM;
-        const unsigned band = tile / (8 * across), rows = min(8u, down - band * 8), in = tile - band * 8 * across;
-        ti = band * 8 + in % rows;
-        tj = in / rows;
-    } else {
-        static_assert(MODE == THIRD || BM == BN, "a symmetric result has square tiles");
-        triangle(tile, (t.mp + BM - 1) / BM, ti, tj);
-    }
-    m0 = ti * BM;
-    n0 = tj * BN;
 }
 
 // What becomes of the sums of 32 rows by NI * 32 columns, a wave's: through LDS, as fp32, in rows and then, for the other orientation, in columns.
@@ -497,29 +573,21 @@ struct Results {
 // NS stages ahead; 16-byte chunk k of a row lies at chunk k ^ (row / 2 % 8), which spreads the operand fetches over the banks. 
 // A tile that is split leaves its sums, in the order of the registers, for finish_kernel.
 template <int BM, int BN, int NS, int WR, int WC, int MODE>
-__global__ __launch_bounds__(64 * WR * WC) void product_kernel(const Entry *table, const unsigned *map, int cur, int last, Common f, float *partial)
+__global__ __launch_bounds__(64 * WR * WC) void product_kernel(const Entry *table, const Work *map, int cur, int last, Common f, float *partial)
 {
     constexpr int NW = WR * WC, WM = BM / WR, WN = BN / WC, MI = WM / 32, NI = WN / 32, NMF = MI * NI;
     constexpr int RPL = 8, A_LD = BM / RPL / NW, B_LD = BN / RPL / NW, L = A_LD + B_LD, KS = BK / 16;
     constexpr int STAGE = (BM + BN) * BK * 2, STAGING = NW * Results<MODE, NI>::BYTES;
-    static_assert(BM % (RPL * NW) == 0 && BN % (RPL * NW) == 0 && KS % 2 == 0 && L * (NS - 1) < 64, "tile");
+    static_assert(BM == BN && BM % (RPL * NW) == 0 && BN % (RPL * NW) == 0 && KS % 2 == 0 && L * (NS - 1) < 64, "tile");
     constexpr int LDS = STAGE * NS > STAGING ? STAGE * NS : STAGING;
     __shared__ __attribute__((aligned(1024))) unsigned char lds[LDS];
 
-    const Entry &t = table[map[blockIdx.x]];
-    const Entry::Items &items = t.items[MODE];
+    const Work me = map[blockIdx.x];
+    const Entry &t = table[me.matrix];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wave_m = wave / WC * WM, wave_n = wave % WC * WN;
-    const bool tall = t.tall != 0;
-    const int mp = t.mp;
-    // workgroups go to the XCDs in turn: each XCD has items of the matrix that follow each other, so that its L2 serves several with what one reads
-    auto spread = [](unsigned at, unsigned count) { return at % 8 * (count / 8) + min(at % 8, count % 8) + at / 8; };
-    const unsigned at = blockIdx.x - items.first;
-    const bool whole = at < items.whole;
-    const unsigned item = whole ? spread(at, items.whole) : items.whole + spread(at - items.whole, items.count - items.whole);
-    const unsigned tile = whole ? item : items.whole + (item - items.whole) / items.split, piece = whole ? 0 : (item - items.whole) % items.split;
-    int m0, n0;
-    place<BM, BN, MODE>(t, tile, m0, n0);
+    const bool tall = t.tall != 0, whole = me.part < 0;
+    const int mp = t.mp, m0 = me.m0, n0 = me.n0;
 
     const f16_t *a, *b;
     int K, a_rows, b_rows;
@@ -535,7 +603,12 @@ __global__ __launch_bounds__(64 * WR * WC) void product_kernel(const Entry *tabl
         K = MODE == SQUARE_A ? mp : tall ? t.Rp : t.Cp;
         a_rows = b_rows = mp;
     }
-    const int per = whole ? K / BK : (K / BK + (int)items.split - 1) / (int)items.split, k0 = (int)piece * per, stages = max(0, min(per, K / BK - k0));
+    int k0 = 0, stages = K / BK;
+    if (!whole) {
+        const int split = (int)t.items[MODE].split, per = (stages + split - 1) / split;
+        k0 = me.part % split * per;
+        stages = max(0, min(per, stages - k0));
+    }
 
     // rows past the operand's lie past the resource's end: their loads give zeros
     const buf_rsrc_t rs_a = make_buf_rsrc(a, (unsigned)a_rows * (unsigned)K * 2u), rs_b = make_buf_rsrc(b, (unsigned)b_rows * (unsigned)K * 2u);
@@ -625,7 +698,7 @@ __global__ __launch_bounds__(64 * WR * WC) void product_kernel(const Entry *tabl
     wait_vmcnt<0>();                        // loads past the end: nothing is under way any more
     wait_lgkmcnt0();
     if (!whole) {
-        float4 *to = reinterpret_cast<float4 *>(partial + (size_t)(items.part_first + (item - items.whole)) * BM * BN);
+        float4 *to = reinterpret_cast<float4 *>(partial + (size_t)(t.items[MODE].part_first + (unsigned)me.part) * BM * BN);
 #pragma unroll
         for (int i = 0; i < MI; ++i)
 #pragma unroll
@@ -656,12 +729,12 @@ __global__ __launch_bounds__(64 * FINISH) void finish_kernel(const Entry *table,
     typedef Results<MODE, NI> Out;
     __shared__ __attribute__((aligned(16))) unsigned char lds[FINISH * Out::BYTES];
     const Entry &t = table[map[blockIdx.x]];
-    const Entry::Items &items = t.items[MODE];
+    const Items &items = t.items[MODE];
     const int lane = threadIdx.x & 63, half = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const unsigned unit = (blockIdx.x - items.finish_first) * FINISH + half, wave = unit / MI % NW, i = unit % MI, q = unit / (MI * NW);
     static_assert(NW * MI % FINISH == 0, "a tile's waves fill workgroups");
     int m0, n0;
-    place<BM, BN, MODE>(t, items.whole + q, m0, n0);
+    place(t.Rp, t.Cp, t.mp, MODE, BM, items.whole + q, m0, n0);
     const int row0 = m0 + (int)(wave / WC) * WM + (int)i * 32, col0 = n0 + (int)(wave % WC) * WN;
     const Out out(t, f, cur, last, m0, n0, col0, reinterpret_cast<float *>(lds + half * Out::BYTES));
     typename Out::With with;
@@ -880,30 +953,8 @@ __global__ __launch_bounds__(SMALL_NT) void small_kernel(SmallGroup q, Common f,
 
 // ---- a call -------------------------------------------------------------------------------------------------------------------------------------
 
-struct Sizes {
-    int Rp, Cp, mp, norm_count, norm_parts;
-    size_t mat, sq;                         // bytes of one orientation of X, of A
-    unsigned prep;
-    size_t bytes;
-};
-Sizes sizes_of(int R, int C)
-{
-    Sizes s;
-    s.Rp = (int)align_up(R, BK);
-    s.Cp = (int)align_up(C, BK);
-    s.mp = R <= C ? s.Rp : s.Cp;
-    const size_t n = (size_t)R * C, chunks = (n + NORM_CHUNK - 1) / NORM_CHUNK;
-    s.norm_count = is_small(R, C) ? 4 : chunks < NORM_MOST ? (int)chunks : NORM_MOST;
-    s.norm_parts = is_small(R, C) ? 16 : s.norm_count;
-    s.mat = align_up((size_t)s.Rp * s.Cp * 2, 256);
-    s.sq = align_up((size_t)s.mp * s.mp * 2, 256);
-    s.prep = (unsigned)(s.Rp / 64) * (s.Cp / 64);
-    s.bytes = 4 * s.mat + 2 * s.sq + 2 * align_up((size_t)s.mp * 4, 256) + align_up(s.norm_parts * 8, 256);
-    return s;
-}
-
 // A shape of tiles
-typedef void (*Product)(const Entry *, const unsigned *, int, int, Common, float *);
+typedef void (*Product)(const Entry *, const Work *, int, int, Common, float *);
 typedef void (*Finish)(const Entry *, const unsigned *, int, int, Common, const float *);
 struct Shape {
     int bm, bn, threads, per_cu;
@@ -999,7 +1050,7 @@ Split split_of(const Sizes &s, int kind, std::vector<Busy> &busy)
 
 // What a call of these matrices launches
 struct Plan {
-    std::vector<Entry::Items> items[KINDS];
+    std::vector<Items> items[KINDS];
     unsigned count[KINDS][SHAPE_COUNT], finish[KINDS][SHAPE_COUNT], prep;
     size_t parts, bytes;                    // bytes of partial sums; of the workspace
 };
@@ -1041,7 +1092,7 @@ Plan plan_of(int count, const int *rows, const int *cols)
         for (int k = 0; k < count; ++k) {
             const int i = order[k], at = split[i].shape < 0 ? shape : split[i].shape;
             const Shape &h = SHAPES[at];
-            Entry::Items &t = p.items[kind][i];
+            Items &t = p.items[kind][i];
             const unsigned tiles = h.tiles(sizes[i], kind);
             t.first = p.count[kind][at];
             t.whole = split[i].shape < 0 ? tiles : split[i].whole;
@@ -1050,14 +1101,15 @@ Plan plan_of(int count, const int *rows, const int *cols)
             t.part_first = (unsigned)parts[at];
             t.finish_first = p.finish[kind][at];
             t.finish_count = (tiles - t.whole) * h.finish_groups();
-            t.shape = at;
+            t.shape = (unsigned short)at;
+            t.side = (unsigned short)h.bm;
             parts[at] += (tiles - t.whole) * t.split;
             p.finish[kind][at] += t.finish_count;
             p.count[kind][at] += t.count;
         }
         for (int i = 0; i < SHAPE_COUNT; ++i) {
             p.parts = std::max(p.parts, align_up(parts[i] * SHAPES[i].bm * SHAPES[i].bn * 4, 256));
-            p.bytes += align_up((size_t)p.count[kind][i] * 4, 256) + align_up((size_t)p.finish[kind][i] * 4, 256);
+            p.bytes += align_up((size_t)p.count[kind][i] * sizeof(Work), 256) + align_up((size_t)p.finish[kind][i] * 4, 256);
         }
     }
     p.bytes += p.parts;
@@ -1116,7 +1168,7 @@ static int run(const MuonArgs &q, void *ws, size_t ws_bytes, hipStream_t st)
     maps.prep = (unsigned *)take((size_t)p.prep * 4);
     for (int kind = 0; kind < KINDS; ++kind)
         for (int i = 0; i < SHAPE_COUNT; ++i) {
-            maps.items[kind][i] = (unsigned *)take((size_t)p.count[kind][i] * 4);
+            maps.items[kind][i] = (Work *)take((size_t)p.count[kind][i] * sizeof(Work));
             maps.finish[kind][i] = (unsigned *)take((size_t)p.finish[kind][i] * 4);
         }
     float *partial = (float *)take(p.parts);
@@ -1130,26 +1182,15 @@ static int run(const MuonArgs &q, void *ws, size_t ws_bytes, hipStream_t st)
         for (int k = 0; k < g.count; ++k) {
             const int i = base + k, R = q.rows[i], C = q.cols[i];
             const Sizes s = sizes_of(R, C);
-            Entry &t = g.t[k];
-            t.R = R; t.C = C; t.Rp = s.Rp; t.Cp = s.Cp; t.mp = s.mp; t.tall = R > C; t.norm_count = s.norm_count; t.norm_parts = s.norm_parts;
+            Given &t = g.t[k];
+            t.R = R; t.C = C;
             t.step = step_of(q, R, C);
             t.u = q.u[i];
             t.y = (bf16_t *)(q.w ? (q.w_bf16 ? q.w_bf16[i] : nullptr) : q.y[i]);
             t.w = q.w ? q.w[i] : nullptr;
             t.m = q.w ? q.m[i] : nullptr;
-            t.z[0] = (f16_t *)take(s.mat);
-            t.zt[0] = (f16_t *)take(s.mat);
-            f16_t *second = (f16_t *)take(s.mat);
-            t.z[1] = t.tall ? second : t.z[0];
-            t.zt[1] = t.tall ? t.zt[0] : second;
-            t.lo = (f16_t *)take(s.mat);
-            t.O = (f16_t *)take(s.sq);
-            t.P = (f16_t *)take(s.sq);
-            t.d = (float *)take((size_t)s.mp * 4);
-            t.e = (float *)take((size_t)s.mp * 4);
-            t.norm = (double *)take((size_t)s.norm_parts * 8);
+            t.room = take(s.bytes);
             t.prep_first = prep_at;
-            t.prep_count = s.prep;
             prep_at += s.prep;
             for (int kind = 0; kind < KINDS; ++kind) t.items[kind] = p.items[kind][i];
             g.first[k] = blocks;
