@@ -312,7 +312,7 @@ __global__ __launch_bounds__(ORDER_NT) void order_kernel(int N, int V, Ranges ra
             const bool in = d < (unsigned)R;
             const unsigned long long all = __ballot(in);
             if (all == 0) continue;
-            // the lanes that have the same token: of few one token after the other, of many those that agree in every bit
+            // the lanes that have the same token: of few one token after the other, of many those that agree in every bit (always the latter: 60000 places on 100000 x 16 28.9 us for 24.5)
             unsigned long long same = all;
             if (__popcll(all) <= 6) {
                 for (unsigned long long left = all; left;) {
