@@ -191,11 +191,21 @@ __device__ __forceinline__ double squares_of(const float (&v)[4][4], double s)
         for (int i = 0; i < 4; ++i) s = __builtin_fma((double)v[g][i], (double)v[g][i], s);
     return s;
 }
+// s + that of the lane that DPP control CONTROL names
+template <int CONTROL>
+__device__ __forceinline__ double with_lane(double s)
+{
+    const long long bits = __double_as_longlong(s);
+    const unsigned lo = (unsigned)__builtin_amdgcn_update_dpp(0, (int)bits, CONTROL, 0xF, 0xF, true), hi = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(bits >> 32), CONTROL, 0xF, 0xF, true);
+    return s + __longlong_as_double((long long)((unsigned long long)hi << 32 | lo));
+}
+// sums over 16 lanes: pairs, fours, and the other half of eight and of sixteen, whose lanes have the same
+__device__ __forceinline__ double sixteen_total(double s) { return with_lane<0x140>(with_lane<0x141>(with_lane<0x4E>(with_lane<0xB1>(s)))); }
 __device__ __forceinline__ double wave_total(double s)
 {
-#pragma unroll
-    for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
-    return s;
+    s = sixteen_total(s);
+    s += __shfl_xor(s, 16);
+    return s + __shfl_xor(s, 32);
 }
 
 // ---- sums of squares, the momentum, and the table of the call's matrices ---------------------------------------------------------------------
@@ -787,7 +797,7 @@ __global__ __launch_bounds__(SMALL_NT) void small_kernel(SmallGroup q, Common f,
 {
     constexpr int MOST = SMALL_BLOCKS;
     __shared__ __attribute__((aligned(256))) unsigned char lds[SMALL_M * SMALL_N * 4 + 8192];
-    __shared__ float diagonal[2][SMALL_M];                     // d, e
+    __shared__ __attribute__((aligned(16))) float diagonal[2][SMALL_M];       // d, e
     __shared__ double part_sum[SMALL_NT / 64];
     const SmallEntry &t = q.t[blockIdx.x];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -807,31 +817,36 @@ __global__ __launch_bounds__(SMALL_NT) void small_kernel(SmallGroup q, Common f,
     s = wave_total(s);
     if (lane == 0) part_sum[wave] = s;
     __syncthreads();
-    s = wave_total(lane < 16 ? part_sum[lane] : 0.0);
+    s = sixteen_total(part_sum[lane & 15]);
     int up;
     const float by = over_norm(s, up);
 
-    // where 16-byte chunk c of a row lies: X [64][np], its transpose [np][64], A and B [64][64]
+    // X [64][np], its transpose [np][64], A and B [64][64], in 16-byte chunks: chunk c of row r lies at chunk c ^ (r / 2 % 8), in X, where np / 64 is even, at c ^ r % 16.  A lane's addresses
+    // of a block of 32 x 32 are a few sums and exclusive ors away from these:
     unsigned char *const z = lds, *const zt = lds + SMALL_M * 2 * np, *const sq = lds + SMALL_M * 4 * np;
-    const bool odd = np / 64 % 2 != 0;
-    auto z_at = [&](int r, int c) __attribute__((always_inline)) { return z + r * np * 2 + ((c ^ (odd ? r >> 1 & 7 : r & 15)) << 4); };
+    const bool odd = np / 64 % 2 != 0, upper = l32 & 1;
+    int of_row = l32 * np * 2 + half * 8, swap = odd ? l32 >> 1 & 7 : l32 & 15;                        // X: its row, and what the chunks are exchanged by
+    int operand = l32 * 128 + ((half ^ (l32 >> 1 & 7)) << 4);                                          // rows of 64: its chunk of the first 16 values; the others' differ in bits 5 and 6
+    int turned = (4 * half + 2 * upper) * 128 + l32 % 8 / 2 * 4 + ((l32 / 8 ^ (2 * half + upper)) << 4);    // transpose: its row and column; bit 6 is that of the block's half and of g
+    unsigned first = upper ? 0x01000504u : 0x05040100u, second = upper ? 0x03020706u : 0x07060302u;   // of its own two values and those of the lane beside: the lower row's first
     auto narrow_at = [](unsigned char *base, int r, int c) __attribute__((always_inline)) { return base + r * 128 + ((c ^ (r >> 1 & 7)) << 4); };
-
     f16x4 hi[MOST][4], lo[MOST][4];
+    // 32 rows (upper ones, or the lower) by 8 columns, of which the lane has four of its row
     auto put_z = [&](int b, int g, const f16x4 &x) __attribute__((always_inline)) {
-        *reinterpret_cast<f16x4 *>(z_at(b % 2 * 32 + l32, b / 2 * 4 + g) + half * 8) = x;
+        *reinterpret_cast<f16x4 *>(z + ((of_row + b % 2 * (np * 64) + (((b / 2 * 4) ^ swap) << 4)) ^ (g << 4))) = x;
     };
-    // the transpose: neighbouring lanes, which have neighbouring rows, give each other two columns, so that either stores two of both rows
-    auto put_zt = [&](int b, int g, const f16x4 &x) __attribute__((always_inline)) {
+    // the same turned, into rows of 64 at `to`, the first of them column 0: neighbouring lanes, which have neighbouring rows, give each other two columns, so that either stores two
+    // of both rows
+    auto put_turned = [&](unsigned char *to, int low, int g, const f16x4 &x) __attribute__((always_inline)) {
         const uint2 w = __builtin_bit_cast(uint2, x);
-        const bool upper = l32 & 1;
         const unsigned keep = upper ? w.y : w.x, give = upper ? w.x : w.y;
         const unsigned got = (unsigned)__builtin_amdgcn_update_dpp(0, (int)give, 0xB1, 0xF, 0xF, true);
-        const unsigned even = upper ? got : keep, uneven = upper ? keep : got;            // of the even row and of the one below
-        const int r = b % 2 * 32 + (l32 & 30), c = b / 2 * 32 + 8 * g + 4 * half + (upper ? 2 : 0);
-        *reinterpret_cast<unsigned *>(narrow_at(zt, c, r / 8) + r % 8 * 2) = __builtin_amdgcn_perm(uneven, even, 0x05040100);
-        *reinterpret_cast<unsigned *>(narrow_at(zt, c + 1, r / 8) + r % 8 * 2) = __builtin_amdgcn_perm(uneven, even, 0x07060302);
+        unsigned char *const at = to + (turned ^ ((low ^ (g & 1)) << 6)) + g * 1024;
+        *reinterpret_cast<unsigned *>(at) = __builtin_amdgcn_perm(got, keep, first);
+        *reinterpret_cast<unsigned *>(at + 128) = __builtin_amdgcn_perm(got, keep, second);
     };
+    auto put_zt = [&](int b, int g, const f16x4 &x) __attribute__((always_inline)) { put_turned(zt + b / 2 * 4096, b % 2, g, x); };
+    auto operand_at = [&](const unsigned char *rows, int c) __attribute__((always_inline)) { return *reinterpret_cast<const f16x8 *>(rows + (operand ^ (c << 4))); };
 #pragma unroll
     for (int k = 0; k < MOST; ++k)
 #pragma unroll
@@ -850,23 +865,47 @@ __global__ __launch_bounds__(SMALL_NT) void small_kernel(SmallGroup q, Common f,
     __syncthreads();
 
     for (int step = 0; step < steps; ++step) {
-        // addresses are worked out in each step: all of them at once are more than the registers
-        asm volatile("" : "+v"(l32), "+v"(half));
+        // addresses are worked out of these in each step: all of them at once are more than the registers
+        asm volatile("" : "+v"(l32), "+v"(half), "+v"(of_row), "+v"(swap), "+v"(operand), "+v"(turned));
         const bool last = step == steps - 1;
-        const int ti = wave >> 1, tj = wave & 1, row = ti * 32 + l32;
-        f16x4 out[4];
-        if (wave < 4) {
+        // A, of which the lower left quarter is the upper right turned: a quarter a wave
+        if (wave < 3) {
+            const int ti = wave >> 1, tj = (wave + 1) >> 1, row = ti * 32 + l32, pairs = np / 32;
             f32x16 acc;
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[e] = 0.f;
-#pragma unroll 8
-            for (int c = half; c < np / 8; c += 2) {
-                const f16x8 a = *reinterpret_cast<const f16x8 *>(z_at(row, c)), b = *reinterpret_cast<const f16x8 *>(z_at(tj * 32 + l32, c));
-                acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(b, a, acc, 0, 0, 0);
-            }
+            // the operands of 32 values of the reduction are fetched while those before are multiplied
+            f16x8 a[2][2], b[2][2];
+            auto quarter = [&](auto off_diagonal) __attribute__((always_inline)) {
+                constexpr bool OFF = decltype(off_diagonal)::value;
+                auto fetch = [&](auto into, int pair) __attribute__((always_inline)) {
+                    constexpr int I = decltype(into)::value;
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const unsigned char *const at = z + (of_row - half * 8) + ti * (np * 64) + (((pair * 4 + 2 * j + half) ^ swap) << 4);
+                        a[I][j] = *reinterpret_cast<const f16x8 *>(at);
+                        if (OFF) b[I][j] = *reinterpret_cast<const f16x8 *>(at + np * 64);
+                    }
+                };
+                auto multiply = [&](auto from) __attribute__((always_inline)) {
+                    constexpr int I = decltype(from)::value;
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(OFF ? b[I][j] : a[I][j], a[I][j], acc, 0, 0, 0);
+                };
+                fetch(IC<0>{}, 0);
+                for (int pair = 0; pair < pairs; pair += 2) {          // (an even number of them)
+                    fetch(IC<1>{}, pair + 1);
+                    multiply(IC<0>{});
+                    if (pair + 2 < pairs) fetch(IC<0>{}, pair + 2);
+                    multiply(IC<1>{});
+                }
+            };
+            if (wave == 1) quarter(std::integral_constant<bool, true>{});
+            else quarter(std::integral_constant<bool, false>{});
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 const int c = tj * 32 + 8 * g + 4 * half;
+                f16x4 o;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     float x = acc[4 * g + i] * (X_DOWN * X_DOWN);
@@ -874,41 +913,52 @@ __global__ __launch_bounds__(SMALL_NT) void small_kernel(SmallGroup q, Common f,
                         diagonal[0][row] = x;
                         x = 0.f;
                     }
-                    out[g][i] = (f16_t)(x * S_UP);
+                    o[i] = (f16_t)(x * S_UP);
                 }
-                *reinterpret_cast<f16x4 *>(narrow_at(sq, row, c / 8) + half * 8) = out[g];
+                *reinterpret_cast<f16x4 *>(narrow_at(sq, row, tj * 4 + g) + half * 8) = o;
+                if (wave == 1) put_turned(sq + 32 * 128, 0, g, o);
             }
         }
         __syncthreads();
-        if (wave < 4) {
+        // B likewise: two waves for each of the three quarters, who multiply the same and finish half of the rows' values each
+        const int part = wave & 1, ti = wave >> 2, tj = (wave / 2 + 1) >> 1, row = ti * 32 + l32;
+        f16x4 out[2];
+        if (wave < 6) {
             f32x16 acc;
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[e] = 0.f;
 #pragma unroll
-            for (int c = 0; c < 8; c += 2) {
-                const f16x8 a = *reinterpret_cast<const f16x8 *>(narrow_at(sq, row, c + half)), b = *reinterpret_cast<const f16x8 *>(narrow_at(sq, tj * 32 + l32, c + half));
-                acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(b, a, acc, 0, 0, 0);
-            }
+            for (int c = 0; c < 8; c += 2) acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(operand_at(sq + tj * 4096, c), operand_at(sq + ti * 4096, c), acc, 0, 0, 0);
             const float di = diagonal[0][row];
+            auto finish = [&](auto from) __attribute__((always_inline)) {
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int c = tj * 32 + 8 * g + 4 * half;
+                for (int q = 0; q < 2; ++q) {
+                    constexpr int G = decltype(from)::value;
+                    const int g = G + q, c = tj * 32 + 8 * g + 4 * half;
+                    const f16x4 o = *reinterpret_cast<const f16x4 *>(narrow_at(sq, row, tj * 4 + g) + half * 8);
+                    const float4 dj = *reinterpret_cast<const float4 *>(&diagonal[0][c]);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float s = acc[4 * g + i] * (S_DOWN * S_DOWN);
-                    float x = b_of((float)out[g][i] * S_DOWN, di, diagonal[0][c + i], s);
-                    if (c + i == row) {
-                        diagonal[1][row] = e_of(di, s);
-                        x = 0.f;
+                    for (int i = 0; i < 4; ++i) {
+                        const float s = acc[4 * g + i] * (S_DOWN * S_DOWN);
+                        float x = b_of((float)o[i] * S_DOWN, di, i == 0 ? dj.x : i == 1 ? dj.y : i == 2 ? dj.z : dj.w, s);
+                        if (c + i == row) {
+                            diagonal[1][row] = e_of(di, s);
+                            x = 0.f;
+                        }
+                        out[q][i] = (f16_t)(x * S_UP);
                     }
-                    out[g][i] = (f16_t)(x * S_UP);
                 }
-            }
+            };
+            if (part) finish(IC<2>{});
+            else finish(IC<0>{});
         }
         __syncthreads();                    // O has been read
-        if (wave < 4)
+        if (wave < 6)
 #pragma unroll
-            for (int g = 0; g < 4; ++g) *reinterpret_cast<f16x4 *>(narrow_at(sq, row, tj * 4 + g) + half * 8) = out[g];
+            for (int q = 0; q < 2; ++q) {
+                *reinterpret_cast<f16x4 *>(narrow_at(sq, row, tj * 4 + part * 2 + q) + half * 8) = out[q];
+                if (ti != tj) put_turned(sq + 32 * 128 + part * 2048, 0, q, out[q]);
+            }
         __syncthreads();
 #pragma unroll
         for (int k = 0; k < MOST; ++k) {
@@ -919,8 +969,7 @@ __global__ __launch_bounds__(SMALL_NT) void small_kernel(SmallGroup q, Common f,
             for (int e = 0; e < 16; ++e) acc[e] = 0.f;
 #pragma unroll
             for (int c = 0; c < 8; c += 2) {
-                const f16x8 x = *reinterpret_cast<const f16x8 *>(narrow_at(sq, r, c + half)), y = *reinterpret_cast<const f16x8 *>(narrow_at(zt, b / 2 * 32 + l32, c + half));
-                acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(y, x, acc, 0, 0, 0);
+                acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(operand_at(zt + b / 2 * 4096, c), operand_at(sq + b % 2 * 4096, c), acc, 0, 0, 0);
             }
             const float e = diagonal[1][r];
 #pragma unroll
