@@ -778,7 +778,8 @@ __global__ __launch_bounds__(64 * FINISH) void finish_kernel(const Entry *table,
 //
 // All steps in one launch, a workgroup for a matrix of up to 64 by 576 (either way): X's first parts lie in LDS in both orientations, its second ones in the registers of
 // the waves that form them; 16-byte chunks of a row are exchanged so that 16 rows of a fetch fall into different banks.  The same operations in the same order as in the
-// kernels above, with the same bits.  One 64 x 363 matrix 37.5 us (95 by 17 launches of those), 5.3 a step and 11 to begin and end: latency of one unit's LDS, barriers and instructions.
+// kernels above, with the same bits.  One 64 x 363 matrix 31 us (95 by 17 launches of those), 4.2 a step and 10 to begin and end: latency of one unit's LDS,
+// barriers and instructions, of which the third product and its results take half.
 
 constexpr int SMALL_NT = 1024, SMALL_GROUP = 72;
 struct SmallEntry {
@@ -806,12 +807,57 @@ __global__ __launch_bounds__(SMALL_NT) void small_kernel(SmallGroup q, Common f,
     const int m = tall ? t.C : t.R, n = tall ? t.R : t.C, np = (n + BK - 1) / BK * BK;
     const int blocks = np / 32 * 2;
 
+    // the matrix's values, in the order of memory, to rows of X in LDS, fp32, 16-byte chunks exchanged so that both 16 rows and 16 fours of rows differ in their banks; and from there a wave's blocks (straight from and to memory, a lane a
+    // row: 64 x 363 2 us more, 64 x 576 13)
+    typedef typename std::conditional<BF16, bf16_t, float>::type T;
+    auto at_x = [&](int r, int c) __attribute__((always_inline)) { return reinterpret_cast<float *>(lds + r * np * 4 + ((c / 4 ^ ((r >> 2 ^ r << 2) & 15)) << 4)) + c % 4; };
+    if (!tall) {
+        constexpr int PIECES = (SMALL_N + 255) / 256;
+        for (int r = wave; r < m; r += 16) {
+            Values<BF16, true> q[PIECES];
+#pragma unroll
+            for (int j = 0; j < PIECES; ++j) q[j].begin(f, (const T *)t.u + r * n, t.m + r * n, lane * 4 + 256 * j, n);
+#pragma unroll
+            for (int j = 0; j < PIECES; ++j) {
+                const int c = lane * 4 + 256 * j;
+                float x[4];
+                if (c >= n) continue;
+                q[j].end(f, t.m + r * n, c, n, x);
+                *reinterpret_cast<float4 *>(at_x(r, c)) = make_float4(x[0], x[1], x[2], x[3]);
+            }
+        }
+    } else {
+        const int r = lane % 16 * 4;
+        constexpr int AHEAD = 3;
+        for (int c0 = wave * 4 + lane / 16; c0 < n; c0 += 64 * AHEAD) {
+            Values<BF16, true> q[AHEAD];
+#pragma unroll
+            for (int j = 0; j < AHEAD; ++j) q[j].begin(f, (const T *)t.u + min(c0 + 64 * j, n - 1) * m, t.m + min(c0 + 64 * j, n - 1) * m, r, m);
+#pragma unroll
+            for (int j = 0; j < AHEAD; ++j) {
+                const int c = c0 + 64 * j;
+                float x[4];
+                if (c >= n || r >= m) continue;
+                q[j].end(f, t.m + c * m, r, m, x);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) *at_x(r + i, c) = x[i];
+            }
+        }
+    }
+    __syncthreads();
     float v[MOST][4][4];
     double s = 0.0;
 #pragma unroll
     for (int k = 0; k < MOST; ++k)
         if (wave + 16 * k < blocks) {
-            block_values<BF16>(f, t.R, t.C, t.u, t.m, wave + 16 * k, lane, v[k]);
+            const int b = wave + 16 * k, r = b % 2 * 32 + l32;
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int c = b / 2 * 32 + 8 * g + 4 * half;
+                const float4 x = *reinterpret_cast<const float4 *>(at_x(r, c));
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[k][g][i] = r < m && c + i < n ? (i == 0 ? x.x : i == 1 ? x.y : i == 2 ? x.z : x.w) : 0.f;
+            }
             s = squares_of(v[k], s);
         }
     s = wave_total(s);
@@ -976,25 +1022,21 @@ __global__ __launch_bounds__(SMALL_NT) void small_kernel(SmallGroup q, Common f,
             for (int g = 0; g < 4; ++g) {
                 float x[4];
 #pragma unroll
+                for (int i = 0; i < 4; ++i) x[i] = x_of(e, hi[k][g][i], lo[k][g][i], acc[4 * g + i]);
+                if (last) {                 // the result stays as it is, in the registers of both parts
+                    hi[k][g] = __builtin_bit_cast(f16x4, make_float2(x[0], x[1]));
+                    lo[k][g] = __builtin_bit_cast(f16x4, make_float2(x[2], x[3]));
+                    continue;
+                }
+#pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    x[i] = x_of(e, hi[k][g][i], lo[k][g][i], acc[4 * g + i]);
                     hi[k][g][i] = (f16_t)x[i];
                     lo[k][g][i] = rest_of(x[i], hi[k][g][i]);
                 }
-                if (!last) continue;
-                const int c = b / 2 * 32 + 8 * g + 4 * half;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if (r >= m || c + i >= n) continue;
-                    const int at = tall ? (c + i) * m + r : r * n + c + i;
-                    float o = x[i] * X_DOWN;
-                    if (f.muon) t.w[at] = o = w_of(t.w[at], x[i], f.keep, t.step);
-                    if (t.y) t.y[at] = Piece<bf16_t>::rounded(o);
-                }
             }
         }
-        if (last) break;
         __syncthreads();                    // X and B have been read
+        if (last) break;
 #pragma unroll
         for (int k = 0; k < MOST; ++k)
 #pragma unroll
@@ -1004,6 +1046,42 @@ __global__ __launch_bounds__(SMALL_NT) void small_kernel(SmallGroup q, Common f,
                     put_zt(wave + 16 * k, g, hi[k][g]);
                 }
         __syncthreads();
+    }
+
+    // results back to the order of memory
+#pragma unroll
+    for (int k = 0; k < MOST; ++k)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int b = wave + 16 * k;
+            const float2 x = __builtin_bit_cast(float2, hi[k][g]), y = __builtin_bit_cast(float2, lo[k][g]);
+            if (b < blocks) *reinterpret_cast<float4 *>(at_x(b % 2 * 32 + l32, b / 2 * 32 + 8 * g + 4 * half)) = make_float4(x.x, x.y, y.x, y.y);
+        }
+    __syncthreads();
+    // four results of a row of len values
+    auto put_results = [&](const float (&x)[4], int row, int at, int len) __attribute__((always_inline)) {
+        float o[4];
+        if (f.muon) {
+            Piece<float> w = load_piece(t.w + row * len, at, len);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[i] = w_of(w.get(i), x[i], f.keep, t.step);
+            w.set(o);
+            store_piece(t.w + row * len, at, len, w);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[i] = x[i] * X_DOWN;
+        }
+        if (t.y) store_quad(t.y + row * len, at, len, o);
+    };
+    if (!tall) {
+        for (int r = wave; r < m; r += 16)
+            for (int c = lane * 4; c < n; c += 256) {
+                const float4 x = *reinterpret_cast<const float4 *>(at_x(r, c));
+                put_results({x.x, x.y, x.z, x.w}, r, c, n);
+            }
+    } else if (lane % 16 * 4 < m) {
+        const int r = lane % 16 * 4;
+        for (int c = wave * 4 + lane / 16; c < n; c += 64) put_results({*at_x(r, c), *at_x(r + 1, c), *at_x(r + 2, c), *at_x(r + 3, c)}, c, r, m);
     }
 }
 

@@ -134,6 +134,19 @@ __device__ __forceinline__ void store_piece(T *row, int at, int len, const Piece
     }
 }
 
+// four values rounded to bf16
+__device__ __forceinline__ void store_quad(bf16_t *row, int at, int len, const float (&v)[4])
+{
+    typedef unsigned Bytes8 __attribute__((ext_vector_type(2), aligned(2)));
+    if (at + 4 <= len) {
+        *reinterpret_cast<Bytes8 *>(row + at) = Bytes8{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (at + i < len) row[at + i] = Piece<bf16_t>::rounded(v[i]);
+    }
+}
+
 // Sum over aligned groups of G lanes (a power of two), the same in each of them.  Exchanges within 16 lanes are part of an instruction; the four sixteens of a wave
 // meet as scalars.
 template <int CONTROL>
