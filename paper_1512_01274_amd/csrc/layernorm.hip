@@ -3,8 +3,8 @@
 //     dx = rstd * (g - sum(g) / C - z * sum(g * z) / C),   dgamma[c] = sum_n dy * z,   dbeta[c] = sum_n dy.
 // Memory bounds both: a row is read once (x, and dy), held in registers over its sums, and written once; rows that registers do not hold are read again.
 // Sums are fp32: a thread's values one after the other, then lanes and waves as a tree; squares are of differences from the mean.  16384 x 4096 bf16: forward 50 us,
-// 5.4 TB/s, gradient 78, 5.2 TB/s with the shares of dgamma and dbeta; rows of 4097 values, which begin at any element, 64.5 and 95.7; 128 x 1000 fp32 4.4 and 7.5, one launch
-// and two.
+// 5.4 TB/s, gradient 78, 5.2 TB/s with the shares of dgamma and dbeta; rows of 4097 values, which begin at any element, 64.5 and 95.7; 128 x 1000 fp32 4.4 and 4.8, a launch
+// each.
 #include <type_traits>
 
 #include "pieces.h"
@@ -277,10 +277,58 @@ __global__ __launch_bounds__(TPR ? ROW_NT : 1024) void fwd_rows_kernel(int N, in
     }
 }
 
-// AHEAD: with the next row's loads under way; rows of more than 8 waves have no registers for it
-template <class T, int TPR, int PC, bool AHEAD, bool PAST>
-__global__ __launch_bounds__(TPR ? ROW_NT : AHEAD && PC > 1 ? 512 : 1024) void bwd_rows_kernel(int N, int C, const T *x, const float *gamma, const float *stats, const T *dy, T *dx, float *parts, int pitch)
+// dgamma and dbeta of COLUMNS columns over all rows, from the stats alone: by 8 lanes of four columns, the others sharing the rows
+constexpr int COLUMNS = 32;
+template <class T>
+__device__ __forceinline__ void columns_of(int N, int C, int c0, const T *x, const float *stats, const T *dy, float *dgamma, float *dbeta, float *room)
 {
+    constexpr int AHEAD = 4;
+    const int share = threadIdx.x / 8, shares = blockDim.x / 8, c = c0 + threadIdx.x % 8 * 4, at = c < C ? c : c0;
+    float ag[4] = {0.f, 0.f, 0.f, 0.f}, ab[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int n0 = share; n0 < N; n0 += AHEAD * shares) {
+        decltype(begin_quad(x, 0, 0)) p[AHEAD], q[AHEAD];
+        Two st[AHEAD];
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+            const size_t n = (size_t)min(n0 + j * shares, N - 1);
+            p[j] = begin_quad(x + n * C, at, C);
+            q[j] = begin_quad(dy + n * C, at, C);
+            st[j] = *reinterpret_cast<const Two *>(stats + 2 * n);
+        }
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+            if (n0 + j * shares >= N) break;
+            settle_quad(p[j], at, C);
+            settle_quad(q[j], at, C);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float d = q[j].get(i);
+                ag[i] += d * ((p[j].get(i) - st[j].x) * st[j].y);
+                ab[i] += d;
+            }
+        }
+    }
+    float4 *const to = reinterpret_cast<float4 *>(room + share * 2 * COLUMNS);
+    to[threadIdx.x % 8] = make_float4(ag[0], ag[1], ag[2], ag[3]);
+    to[8 + threadIdx.x % 8] = make_float4(ab[0], ab[1], ab[2], ab[3]);
+    __syncthreads();
+    if (threadIdx.x >= 2 * COLUMNS) return;
+    float s = 0.f;
+#pragma unroll 8
+    for (int k = 0; k < shares; ++k) s += room[k * 2 * COLUMNS + threadIdx.x];
+    float *const out = threadIdx.x < COLUMNS ? dgamma : dbeta;
+    if (out && c0 + (int)threadIdx.x % COLUMNS < C) out[c0 + threadIdx.x % COLUMNS] = s;
+}
+
+// FEW rows: workgroups behind those of the rows make dgamma and dbeta in the same launch, reading the rows again.  AHEAD: with the next row's loads under way; rows of more than 8 waves have no registers for it
+template <class T, int TPR, int PC, bool AHEAD, bool PAST, bool FEW>
+__global__ __launch_bounds__(TPR ? ROW_NT : AHEAD && PC > 1 ? 512 : 1024) void bwd_rows_kernel(int N, int C, const T *x, const float *gamma, const float *stats, const T *dy, T *dx, float *parts, int pitch,
+                                                                                                int row_groups, float *dgamma, float *dbeta)
+{
+    if constexpr (FEW) {
+        extern __shared__ __attribute__((aligned(16))) float room[];
+        if ((int)blockIdx.x >= row_groups) return columns_of(N, C, ((int)blockIdx.x - row_groups) * COLUMNS, x, stats, dy, dgamma, dbeta, room);
+    }
     constexpr int VE = Piece<T>::VE, V = PC * VE;
     __shared__ float part[2][2][16];
     __shared__ float4 meet[TPR ? ROW_NT : 1];
@@ -292,7 +340,7 @@ __global__ __launch_bounds__(TPR ? ROW_NT : AHEAD && PC > 1 ? 512 : 1024) void b
     for (int i = 0; i < V; ++i) ag[i] = ab[i] = 0.f;
     const float by = 1.f / (float)C;
     long long n = (long long)blockIdx.x * G + l.group;
-    const long long step = (long long)gridDim.x * G, turns = (N - (long long)blockIdx.x * G + step - 1) / step;
+    const long long step = (long long)(FEW ? row_groups : (int)gridDim.x) * G, turns = (N - (long long)blockIdx.x * G + step - 1) / step;
     Piece<T> p[PC], q[PC], p1[PC], q1[PC];
     auto fetch = [&](Piece<T> (&a)[PC], Piece<T> (&b)[PC], long long row) __attribute__((always_inline)) {
         l.load(a, x + (size_t)row * C, C);
@@ -356,6 +404,7 @@ __global__ __launch_bounds__(TPR ? ROW_NT : AHEAD && PC > 1 ? 512 : 1024) void b
             st = *reinterpret_cast<const Two *>(stats + 2 * m);
         }
     }
+    if constexpr (FEW) return;
     float *to = parts + (size_t)blockIdx.x * 2 * pitch;
 #pragma unroll
     for (int half = 0; half < 2; ++half)
@@ -464,21 +513,37 @@ int fwd(int N, int C, int dtype, const T *x, const float *gamma, const float *be
     });
 }
 
+// rows for which one launch makes dx and the weights' gradients; us, two launches and one: 128 x 1000 fp32 8.1, 4.8; 256 x 4096 bf16 10.1, 5.0; 512 x 4096 11.2, 7.5; 1024 x 64 fp32 8.1,
+// 9.5; 1024 x 1000 bf16 10.6, 19.9
+bool is_few(int N) { return N <= 512; }
+
 template <class T>
 int bwd(int N, int C, int dtype, const T *x, const float *gamma, const float *stats, const T *dy, T *dx, float *dgamma, float *dbeta, char *ws, hipStream_t st)
 {
     const BwdPlan q = bwd_plan(N, C, dtype);
     float *part = (float *)ws;
     if (q.h.PC) {
+        const bool few = is_few(N);
         const int rc = with_share<T>(q.h, [&](auto tpr, auto pc) {
             constexpr int TPR = decltype(tpr)::value, PC = decltype(pc)::value;
-            const bool past = past_caches(N, C, 3, dtype);
-            const auto kernel = TPR || PC == 1 || q.h.waves <= 8 ? (past ? bwd_rows_kernel<T, TPR, PC, true, true> : bwd_rows_kernel<T, TPR, PC, true, false>)
-                                                      : (past ? bwd_rows_kernel<T, 0, PC, false, true> : bwd_rows_kernel<T, 0, PC, false, false>);
-            hipLaunchKernelGGL(kernel, dim3(q.workgroups), dim3(TPR ? ROW_NT : 64 * q.h.waves), 0, st, N, C, x, gamma, stats, dy, dx, part, q.pitch);
-            return launched();
+            const int threads = TPR ? ROW_NT : 64 * q.h.waves;
+            auto launch = [&](auto kernel, int groups, int columns) {
+                hipLaunchKernelGGL(kernel, dim3(groups + columns), dim3(threads), few ? threads / 8 * 2 * COLUMNS * 4 : 0, st, N, C, x, gamma, stats, dy, dx, part, q.pitch, groups, dgamma, dbeta);
+                return launched();
+            };
+            const bool ahead = TPR || PC == 1 || q.h.waves <= 8;
+            if (few) {
+                const auto kernel = ahead ? bwd_rows_kernel<T, TPR, PC, true, false, true> : bwd_rows_kernel<T, 0, PC, false, false, true>;
+                const int columns = dgamma || dbeta ? (C + COLUMNS - 1) / COLUMNS : 0;
+                // in place: what the columns read is overwritten only after them
+                const bool apart = columns && ((const void *)dx == x || (const void *)dx == dy);
+                if (apart && launch(kernel, 0, columns) != MXC_OK) return (int)MXC_ERR_LAUNCH;
+                return launch(kernel, q.workgroups, apart ? 0 : columns);
+            }
+            if (past_caches(N, C, 3, dtype)) return launch(ahead ? bwd_rows_kernel<T, TPR, PC, true, true, false> : bwd_rows_kernel<T, 0, PC, false, true, false>, q.workgroups, 0);
+            return launch(ahead ? bwd_rows_kernel<T, TPR, PC, true, false, false> : bwd_rows_kernel<T, 0, PC, false, false, false>, q.workgroups, 0);
         });
-        if (rc != MXC_OK) return rc;
+        if (rc != MXC_OK || few) return rc;
     } else {
         float2 *sums = (float2 *)(ws + q.part_bytes);
         hipLaunchKernelGGL(bwd_sums_kernel<T>, dim3(N < 1 << 20 ? N : 1 << 20), dim3(LONG_NT), 0, st, N, C, x, gamma, stats, dy, sums);

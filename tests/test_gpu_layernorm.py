@@ -62,7 +62,9 @@ def forward_tolerance(x, gamma, beta, eps, dtype):
 
 
 SIZES = [(1, 1), (3, 2), (5, 3), (2, 7), (9, 8), (130, 64), (65, 100), (4, 127), (33, 256), (1, 1000), (128, 1000), (17, 1025), (3, 4096), (300, 4097), (2, 8200), (3, 16384), (2, 16385),
-         (2, 32771), (1, 100003), (5000, 16), (70000, 3)]
+         (2, 32771), (1, 100003), (5000, 16), (70000, 3),
+         # on either side of where one launch makes the whole gradient
+         (511, 1000), (512, 200), (513, 200), (512, 4097), (513, 4097), (300, 31), (512, 3)]
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
