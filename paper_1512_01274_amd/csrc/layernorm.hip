@@ -3,7 +3,7 @@
 //     dx = rstd * (g - sum(g) / C - z * sum(g * z) / C),   dgamma[c] = sum_n dy * z,   dbeta[c] = sum_n dy.
 // Memory bounds both: a row is read once (x, and dy), held in registers over its sums, and written once; rows that registers do not hold are read again.
 // Sums are fp32: a thread's values one after the other, then lanes and waves as a tree; squares are of differences from the mean.  16384 x 4096 bf16: forward 50 us,
-// 5.4 TB/s, gradient 78, 5.2 TB/s with the shares of dgamma and dbeta; rows of 4097 values, which begin at any element, 64.5 and 95.7; 128 x 1000 fp32 4.4 and 4.8, a launch
+// 5.4 TB/s, gradient 78, 5.2 TB/s with the shares of dgamma and dbeta; rows of 4097 values, which begin at any element, 62.5 and 95.6; 128 x 1000 fp32 4.4 and 4.8, a launch
 // each.
 #include <type_traits>
 
@@ -250,12 +250,21 @@ __global__ __launch_bounds__(TPR ? ROW_NT : 1024) void fwd_rows_kernel(int N, in
         const float mean = s[0] * by;
         s[0] = 0.f;
 #pragma unroll
-        for (int k = 0; k < PC; ++k)
+        for (int k = 0; k < PC; ++k) {
+            if (l.at(k) + VE <= C) {
 #pragma unroll
-            for (int i = 0; i < VE; ++i) {
-                const float d = p[k].get(i) - mean;
-                s[0] += l.at(k) + i < C ? d * d : 0.f;
+                for (int i = 0; i < VE; ++i) {
+                    const float d = p[k].get(i) - mean;
+                    s[0] = __builtin_fmaf(d, d, s[0]);
+                }
+            } else {                        // the row ends in this piece, or before it
+#pragma unroll
+                for (int i = 0; i < VE; ++i) {
+                    const float d = l.at(k) + i < C ? p[k].get(i) - mean : 0.f;
+                    s[0] = __builtin_fmaf(d, d, s[0]);
+                }
             }
+        }
         row_sums<TPR>(s, part[1]);
         const float rstd = 1.f / sqrtf(s[0] * by + eps);
 #pragma unroll
