@@ -38,6 +38,9 @@ constexpr int KINDS = 3, SHAPE_COUNT = 5;   // products of a step, shapes of the
 constexpr int SMALL_M = 64, SMALL_N = 576;
 __host__ __device__ inline bool is_small(int R, int C) { return (R < C ? R : C) <= SMALL_M && (R < C ? C : R) <= SMALL_N; }
 
+// Longer matrices whose shorter side is one tile of 64: A is split over the reduction, and what adds its parts makes B at once
+__host__ __device__ inline bool is_flat(int R, int C) { return (R < C ? R : C) <= BK && !is_small(R, C); }
+
 // The work items of a matrix in the launches of a product
 struct Items {
     unsigned first, count;                  // tiles, the last of them in `split` ranges of the reduction each
@@ -67,6 +70,7 @@ struct Sizes {
     int norm_count, norm_parts;             // workgroups that sum the squares, and what they leave
     size_t mat, sq, side;                   // bytes of one orientation of X, of A, of a diagonal
     unsigned prep;                          // tiles of prepare_kernel
+    bool flat;
     size_t bytes;
 };
 // and what the kernels read.  Z is ping-ponged where the third product reads it (tall), its transpose where it does not (wide); the other pair of pointers is one buffer.
@@ -264,6 +268,7 @@ __host__ __device__ inline Sizes sizes_of(int R, int C)
     s.sq = up((size_t)s.mp * s.mp * 2, 256);
     s.side = up((size_t)s.mp * 4, 256);
     s.prep = (unsigned)(s.Rp / BK) * (s.Cp / BK);
+    s.flat = is_flat(R, C);
     s.bytes = 4 * s.mat + 2 * s.sq + 2 * s.side + up((size_t)s.norm_parts * 8, 256);
     return s;
 }
@@ -293,7 +298,7 @@ __device__ __forceinline__ Entry entry_of(const Given &g, const Sizes &s)
 }
 // which matrix each workgroup of the other launches belongs to
 struct Maps {
-    unsigned *prep, *finish[KINDS][SHAPE_COUNT];
+    unsigned *prep, *flat, *finish[KINDS][SHAPE_COUNT];
     Work *items[KINDS][SHAPE_COUNT];
 };
 static_assert(sizeof(Group) + sizeof(Common) + sizeof(Maps) + 32 <= 4096, "kernel arguments");
@@ -313,6 +318,7 @@ __global__ __launch_bounds__(256) void norm_kernel(Group q, Common f, Entry *tab
     const unsigned part = blockIdx.x - q.first[i], at = part * 256 + threadIdx.x, step = z.norm_count * 256, me = q.base + i;
     if (at == 0) table[me] = entry_of(t, z);
     fill(maps.prep, t.prep_first, z.prep, me, at, step);
+    if (at == 0 && is_flat(t.R, t.C)) maps.flat[t.items[SQUARE_A].first] = me;
     for (int k = 0; k < KINDS; ++k) {
         const Items &items = t.items[k];
         // workgroups go to the XCDs in turn: each XCD has items of the matrix that follow each other, so that its L2 serves several with what one reads
@@ -774,6 +780,77 @@ __global__ __launch_bounds__(64 * FINISH) void finish_kernel(const Entry *table,
     out.put(acc, with, row0);
 }
 
+// Flat matrices: the parts of A, of four stages or more, added in order, and B = b A + c A A and its diagonal of them, a wave for each quarter.  Latency of a launch bounds it.  In place of
+// A's sum by one workgroup, or of parts and their addition, and B's launch: 64 x 640 94 -> 81 us, 64 x 4096 137 -> 103, nine of up to 64 x 2304 122 -> 100.
+__global__ __launch_bounds__(256) void flat_kernel(const Entry *table, const unsigned *map, const float *partial)
+{
+    __shared__ __attribute__((aligned(16))) unsigned char sq[8192];
+    __shared__ __attribute__((aligned(16))) float diagonal[BK];
+    const Entry &t = table[map[blockIdx.x]];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, half = lane >> 5, ti = wave >> 1, tj = wave & 1, row = ti * 32 + l32;
+    auto at = [&](int r, int c) __attribute__((always_inline)) { return sq + r * 128 + ((c ^ (r >> 1 & 7)) << 4); };
+    f32x16 acc;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[e] = 0.f;
+    const int parts = (int)t.items[SQUARE_X].split;
+    const float4 *from = reinterpret_cast<const float4 *>(partial + (size_t)t.items[SQUARE_X].part_first * BK * BK) + wave * 256 + lane;
+    constexpr int AHEAD = 4;
+    for (int p0 = 0; p0 < parts; p0 += AHEAD) {
+        float4 v[AHEAD][4];
+#pragma unroll
+        for (int p = 0; p < AHEAD; ++p)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) v[p][g] = from[(size_t)min(p0 + p, parts - 1) * (BK * BK / 4) + g * 64];
+#pragma unroll
+        for (int p = 0; p < AHEAD; ++p) {
+            if (p0 + p >= parts) break;
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                acc[4 * g] += v[p][g].x; acc[4 * g + 1] += v[p][g].y; acc[4 * g + 2] += v[p][g].z; acc[4 * g + 3] += v[p][g].w;
+            }
+        }
+    }
+    f16x4 o[4];
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        const int c = tj * 32 + 8 * g + 4 * half;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float x = acc[4 * g + i] * (X_DOWN * X_DOWN);
+            if (c + i == row) {
+                diagonal[row] = x;
+                x = 0.f;
+            }
+            o[g][i] = (f16_t)(x * S_UP);
+        }
+        *reinterpret_cast<f16x4 *>(at(row, c / 8) + half * 8) = o[g];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[e] = 0.f;
+#pragma unroll
+    for (int c = 0; c < 8; c += 2) {
+        const f16x8 a = *reinterpret_cast<const f16x8 *>(at(row, c + half)), b = *reinterpret_cast<const f16x8 *>(at(tj * 32 + l32, c + half));
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(b, a, acc, 0, 0, 0);
+    }
+    const float di = diagonal[row];
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        const int c = tj * 32 + 8 * g + 4 * half;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float s = acc[4 * g + i] * (S_DOWN * S_DOWN);
+            float x = b_of((float)o[g][i] * S_DOWN, di, diagonal[c + i], s);
+            if (c + i == row) {
+                t.e[row] = e_of(di, s);
+                x = 0.f;
+            }
+            o[g][i] = (f16_t)(x * S_UP);
+        }
+        *reinterpret_cast<f16x4 *>(t.P + row * BK + c) = o[g];
+    }
+}
+
 // ---- matrices that a compute unit holds -----------------------------------------------------------------------------------------------------------
 //
 // All steps in one launch, a workgroup for a matrix of up to 64 by 576 (either way): X's first parts lie in LDS in both orientations, its second ones in the registers of
@@ -1162,6 +1239,8 @@ Split split_of(const Sizes &s, int kind, std::vector<Busy> &busy)
     Split best = {-1, 0, 1};
     double least = 1e30, unsplit = 1e30;
     const int stages = stages_of(s, kind);
+    if (s.flat && kind == SQUARE_X) return {0, 0, (unsigned)std::min(16, std::max(1, stages / 4))};
+    if (s.flat && kind == SQUARE_A) return {0, 1, 1};
     for (int i = 0; i < SHAPE_COUNT; ++i) {
         const Shape &h = SHAPES[i];
         const Load all = {h.tiles(s, kind), stages};
@@ -1185,7 +1264,7 @@ Split split_of(const Sizes &s, int kind, std::vector<Busy> &busy)
 // What a call of these matrices launches
 struct Plan {
     std::vector<Items> items[KINDS];
-    unsigned count[KINDS][SHAPE_COUNT], finish[KINDS][SHAPE_COUNT], prep;
+    unsigned count[KINDS][SHAPE_COUNT], finish[KINDS][SHAPE_COUNT], prep, flat;
     size_t parts, bytes;                    // bytes of partial sums; of the workspace
 };
 Plan plan_of(int count, const int *rows, const int *cols)
@@ -1227,6 +1306,11 @@ Plan plan_of(int count, const int *rows, const int *cols)
             const int i = order[k], at = split[i].shape < 0 ? shape : split[i].shape;
             const Shape &h = SHAPES[at];
             Items &t = p.items[kind][i];
+            t = Items{};
+            if (sizes[i].flat && kind == SQUARE_A) {        // flat_kernel does it
+                t.first = p.flat++;
+                continue;
+            }
             const unsigned tiles = h.tiles(sizes[i], kind);
             t.first = p.count[kind][at];
             t.whole = split[i].shape < 0 ? tiles : split[i].whole;
@@ -1234,7 +1318,7 @@ Plan plan_of(int count, const int *rows, const int *cols)
             t.count = t.whole + (tiles - t.whole) * t.split;
             t.part_first = (unsigned)parts[at];
             t.finish_first = p.finish[kind][at];
-            t.finish_count = (tiles - t.whole) * h.finish_groups();
+            t.finish_count = sizes[i].flat && kind == SQUARE_X ? 0 : (tiles - t.whole) * h.finish_groups();
             t.shape = (unsigned short)at;
             t.side = (unsigned short)h.bm;
             parts[at] += (tiles - t.whole) * t.split;
@@ -1246,7 +1330,7 @@ Plan plan_of(int count, const int *rows, const int *cols)
             p.bytes += align_up((size_t)p.count[kind][i] * sizeof(Work), 256) + align_up((size_t)p.finish[kind][i] * 4, 256);
         }
     }
-    p.bytes += p.parts;
+    p.bytes += p.parts + align_up((size_t)p.flat * 4, 256);
     return p;
 }
 // whether every matrix of a call fits a compute unit: then the call is one launch for SMALL_GROUP of them, without a workspace.  (Beside larger ones they are
@@ -1300,6 +1384,7 @@ static int run(const MuonArgs &q, void *ws, size_t ws_bytes, hipStream_t st)
     Entry *table = (Entry *)take((size_t)q.count * sizeof(Entry));
     Maps maps;
     maps.prep = (unsigned *)take((size_t)p.prep * 4);
+    maps.flat = (unsigned *)take((size_t)p.flat * 4);
     for (int kind = 0; kind < KINDS; ++kind)
         for (int i = 0; i < SHAPE_COUNT; ++i) {
             maps.items[kind][i] = (Work *)take((size_t)p.count[kind][i] * sizeof(Work));
@@ -1344,6 +1429,10 @@ static int run(const MuonArgs &q, void *ws, size_t ws_bytes, hipStream_t st)
                 const Shape &h = SHAPES[i];
                 hipLaunchKernelGGL(h.product[mode], dim3(p.count[mode][i]), dim3(h.threads), 0, st, table, maps.items[mode][i], cur, last, f, partial);
                 if (launched() != MXC_OK) return MXC_ERR_LAUNCH;
+                if (mode == SQUARE_X && i == 0 && p.flat) {
+                    hipLaunchKernelGGL(flat_kernel, dim3(p.flat), dim3(256), 0, st, table, maps.flat, partial);
+                    if (launched() != MXC_OK) return MXC_ERR_LAUNCH;
+                }
                 if (!p.finish[mode][i]) continue;
                 hipLaunchKernelGGL(h.finish[mode], dim3(p.finish[mode][i]), dim3(64 * FINISH), 0, st, table, maps.finish[mode][i], cur, last, f, partial);
                 if (launched() != MXC_OK) return MXC_ERR_LAUNCH;

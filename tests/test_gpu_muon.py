@@ -117,7 +117,7 @@ def check(got, x, steps, rounded=True):
 
 
 SHAPES = [(1, 1), (1, 7), (9, 1), (2, 3), (5, 5), (16, 33), (33, 16), (63, 64), (64, 64), (65, 64), (64, 363), (363, 64), (64, 576), (576, 61), (64, 577), (40, 449), (31, 500), (100, 1000), (128, 129), (200, 200), (257, 255), (130, 700), (700, 130),
-          (512, 640), (1025, 513)]
+          (512, 640), (1025, 513), (577, 64), (640, 33), (1, 5000), (7000, 17), (50, 4100)]
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
@@ -196,13 +196,13 @@ def test_zeros_and_values_that_are_not_finite(mxc):
 
 def test_many_matrices_are_each_as_alone(mxc):
     """One call for many of different shapes, more than travel in one launch's arguments: the bits of calls of their own."""
-    shapes = [(1 + 37 * i % 150, 1 + 53 * i % 260) for i in range(75)] + [(520, 300), (300, 520), (64, 1000)]
+    shapes = [(1 + 37 * i % 150, 1 + 53 * i % 260) for i in range(75)] + [(520, 300), (300, 520), (64, 1000), (33, 3000), (2000, 64), (64, 577)]
     xs = [matrix(r, c, "few", i) for i, (r, c) in enumerate(shapes)]
     ys = [torch.empty(s, dtype=torch.bfloat16, device="cuda") for s in shapes]
     whole, ws = workspace(mxc, shapes)
     mxc.mxc_orthogonalize(xs, 5, ys, ws)
     assert intact(whole, ws, 5)
-    for i in (0, 1, 5, 19, 20, 21, 39, 40, 62, 74, 75, 76, 77):
+    for i in (0, 1, 5, 19, 20, 21, 39, 40, 62, 74, 75, 76, 77, 78, 79, 80):
         alone = torch.empty_like(ys[i])
         mxc.mxc_orthogonalize([xs[i]], 5, [alone], workspace(mxc, [shapes[i]])[1])
         assert torch.equal(alone, ys[i]), shapes[i]
