@@ -195,6 +195,27 @@ def test_gradient_is_that_of_differences(mxc, N, C):
         assert abs(float((got.double() * direction).sum()) - change) <= tol
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("exponent,eps,C", [(120, 1e-5, 4), (120, 1e-5, 24), (120, 1e-5, 100), (110, 1e-12, 1000), (66, 1.2e-38, 4), (66, 1.2e-38, 24), (66, 1.2e-38, 1000), (66, 1.2e-38, 4097),
+                                           (66, 1.2e-38, 12000), (66, 1.2e-38, 17001)])
+def test_gradient_where_the_mean_over_the_deviation_is_past_all_numbers(mxc, dtype, exponent, eps, C):
+    """Rows of one value, a power of two, beside others: z is zero at every place though |mean| rstd passes the largest number."""
+    code = mxc.dtype_code(dtype)
+    eps = float(torch.tensor(eps, dtype=torch.float32))
+    for N in (5, 513):
+        x, dy, gamma, _ = data(N, C, dtype, N + C)
+        x[::2] = 2.0 ** exponent
+        _, mean, rstd, _, _ = forward64(x, gamma.double(), gamma.double(), eps)
+        stats = torch.cat([mean, rstd], 1).float()
+        stats[::2, 0], stats[::2, 1] = 2.0 ** exponent, eps ** -0.5
+        assert math.log2(float(stats[0, 0])) + math.log2(float(stats[0, 1])) > 128
+        want, wg, wb, parts = backward64(x, gamma.double(), stats, dy)
+        dx, dgamma, dbeta = torch.empty_like(x), torch.empty(C, device="cuda"), torch.empty(C, device="cuda")
+        mxc.mxc_layernorm_bwd(N, C, code, x, gamma, stats, dy, dx, dgamma, dbeta, mxc.alloc_workspace(mxc.mxc_layernorm_workspace_bytes(N, C, code)))
+        for got, exact, tol in zip((dx, dgamma, dbeta), (want, wg, wb), backward_tolerance(parts, want, dtype)):
+            assert bool(((got.double() - exact).abs() <= tol).all()), (N, tuple(got.shape))
+
+
 def test_rows_that_are_not_finite(mxc):
     """They make NaN of themselves and of what they enter, and leave other rows alone."""
     for C in (24, 5000, 20000):
