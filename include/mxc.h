@@ -423,7 +423,8 @@ int mxc_embedding_bwd(int N, int V, int C, int dtype, const int *tokens, const v
  *   mxc_layernorm_bwd:  from x and the stats of the forward call, with g = dy * gamma:
  *                       dx = rstd * (g - sum_c g / C - z * sum_c g * z / C),  dgamma[c] = sum_n dy * z,  dbeta[c] = sum_n dy
  *                       gamma (ones), dgamma and dbeta may each be NULL; dx may be dy or x
- * Arithmetic, stats, dgamma and dbeta are fp32 (the squares are those of the differences from the mean: a large mean costs no digits), y and dx are rounded
+ * Arithmetic, stats, dgamma and dbeta are fp32 (the squares are those of the differences from the mean, and where the mean is more than 16 deviations, sqrt(var + eps), from zero
+ * its rounding is taken out of z and the variance too: a large mean costs no digits; the gradient's z has the mean as stats hold it), y and dx are rounded
  * once to `dtype`; an infinity or a NaN makes NaN of its row's results and of the gradients that it enters.  dgamma and dbeta are added in a fixed order.
  * Workspace: mxc_layernorm_workspace_bytes, for the gradient.  Errors: MXC_ERR_SHAPE (non-positive sizes, C above MXC_LAYERNORM_MAX_C), MXC_ERR_UNSUPPORTED
  * (dtype; eps that is not a normal positive number), MXC_ERR_NULL, MXC_ERR_ALIGN (16 bytes, 4 for stats), MXC_ERR_WORKSPACE, MXC_ERR_LAUNCH.

@@ -29,6 +29,10 @@ __device__ __forceinline__ float workgroup_sum(float v, float *part)
     return v;
 }
 
+// Whether a row's values lie close together far from zero, where the rounding of the mean, some ulps of it, counts beside them (2^20 in 49 places had z = 1 or -1): then `rest`, the mean of
+// the differences from the rounded mean, is taken from these before they are squared, and from z.  Other rows go without: both for every row 16384 x 4096 bf16 52.6 us for 48.7.
+__device__ __forceinline__ bool is_near(float mean, float var, float eps) { return mean * mean > 256.f * (var + eps); }
+
 template <class T>
 __global__ __launch_bounds__(LONG_NT) void fwd_long_kernel(int N, int C, const T *x, const float *gamma, const float *beta, float eps, T *y, float *stats)
 {
@@ -42,17 +46,23 @@ __global__ __launch_bounds__(LONG_NT) void fwd_long_kernel(int N, int C, const T
             for (int i = 0; i < VE; ++i) s += p.get(i);
         }
         const float mean = workgroup_sum(s, part) / (float)C;
-        s = 0.f;
-        for (int c = threadIdx.x * VE; c < C; c += LONG_NT * VE) {
-            const Piece<T> p = load_piece(x + at, c, C);
-            for (int i = 0; i < VE; ++i) {
-                const float d = p.get(i) - mean;
-                s += c + i < C ? d * d : 0.f;
+        // sum over the row of f(x - mean)
+        auto sum_of = [&](auto f) {
+            float v = 0.f;
+            for (int c = threadIdx.x * VE; c < C; c += LONG_NT * VE) {
+                const Piece<T> p = load_piece(x + at, c, C);
+                for (int i = 0; i < VE; ++i) v += c + i < C ? f(p.get(i) - mean) : 0.f;
             }
+            return workgroup_sum(v, part);
+        };
+        float rest = 0.f, var = sum_of([](float d) { return d * d; }) / (float)C;
+        if (is_near(mean, var, eps)) {
+            rest = sum_of([](float d) { return d; }) / (float)C;
+            var = sum_of([&](float d) { return (d - rest) * (d - rest); }) / (float)C;
         }
-        const float rstd = 1.f / sqrtf(workgroup_sum(s, part) / (float)C + eps);
+        const float rstd = 1.f / sqrtf(var + eps), off = -rest * rstd;
         if (stats && threadIdx.x == 0) {
-            stats[2 * (size_t)n] = mean;
+            stats[2 * (size_t)n] = mean + rest;
             stats[2 * (size_t)n + 1] = rstd;
         }
         for (int c = threadIdx.x * VE; c < C; c += LONG_NT * VE) {
@@ -60,7 +70,7 @@ __global__ __launch_bounds__(LONG_NT) void fwd_long_kernel(int N, int C, const T
             float v[VE];
             for (int i = 0; i < VE; ++i) {
                 const bool in = c + i < C;
-                v[i] = (p.get(i) - mean) * rstd * (gamma && in ? gamma[c + i] : 1.f) + (beta && in ? beta[c + i] : 0.f);
+                v[i] = __builtin_fmaf(p.get(i) - mean, rstd, off) * (gamma && in ? gamma[c + i] : 1.f) + (beta && in ? beta[c + i] : 0.f);
             }
             p.set(v);
             store_piece(y + at, c, C, p);
@@ -226,7 +236,7 @@ template <class T, int TPR, int PC, bool PAST>
 __global__ __launch_bounds__(TPR ? ROW_NT : 1024) void fwd_rows_kernel(int N, int C, const T *x, const float *gamma, const float *beta, float eps, T *y, float *stats)
 {
     constexpr int VE = Piece<T>::VE, V = PC * VE;
-    __shared__ float part[2][1][16];
+    __shared__ float part[4][1][16];
     const Lane<T, TPR, PC, PAST> l;
     const int G = groups<TPR>();
     float gm[V], bt[V];
@@ -247,7 +257,7 @@ __global__ __launch_bounds__(TPR ? ROW_NT : 1024) void fwd_rows_kernel(int N, in
 #pragma unroll
             for (int i = 0; i < VE; ++i) s[0] += p[k].get(i);       // (zeros past the row)
         row_sums<TPR>(s, part[0]);
-        const float mean = s[0] * by;
+        const float mean = in_32_bits(s[0] * by);
         s[0] = 0.f;
 #pragma unroll
         for (int k = 0; k < PC; ++k) {
@@ -266,16 +276,35 @@ __global__ __launch_bounds__(TPR ? ROW_NT : 1024) void fwd_rows_kernel(int N, in
             }
         }
         row_sums<TPR>(s, part[1]);
-        const float rstd = 1.f / sqrtf(s[0] * by + eps);
+        float rest = 0.f, var = s[0] * by;
+        const bool near = is_near(mean, var, eps);
+        if (TPR ? __any(near) : near) {
+            // sum over the row of f(x - mean)
+            auto sum_of = [&](auto f, float (*room)[16]) __attribute__((always_inline)) {
+                s[0] = 0.f;
+#pragma unroll
+                for (int k = 0; k < PC; ++k) {
+                    held(p[k].raw);
+#pragma unroll
+                    for (int i = 0; i < VE; ++i) s[0] += l.at(k) + i < C ? f(p[k].get(i) - mean) : 0.f;
+                }
+                row_sums<TPR>(s, room);
+                return in_32_bits(s[0] * by);
+            };
+            const float r = sum_of([](float d) { return d; }, part[2]), v = sum_of([&](float d) { return (d - r) * (d - r); }, part[3]);
+            rest = near ? r : 0.f;
+            var = near ? v : var;
+        }
+        const float rstd = 1.f / sqrtf(var + eps), off = -rest * rstd;
 #pragma unroll
         for (int k = 0; k < PC; ++k) held(p[k].raw);
         if (in) {
-            if (stats && l.first == 0) *reinterpret_cast<Two *>(stats + 2 * n) = Two{mean, rstd};
+            if (stats && l.first == 0) *reinterpret_cast<Two *>(stats + 2 * n) = Two{mean + rest, rstd};
 #pragma unroll
             for (int k = 0; k < PC; ++k) {
                 float v[VE];
 #pragma unroll
-                for (int i = 0; i < VE; ++i) v[i] = (p[k].get(i) - mean) * rstd * gm[k * VE + i] + bt[k * VE + i];
+                for (int i = 0; i < VE; ++i) v[i] = __builtin_fmaf(p[k].get(i) - mean, rstd, off) * gm[k * VE + i] + bt[k * VE + i];
                 Piece<T> r;
                 r.set(v);
                 store_piece<PAST>(y + (size_t)n * C, l.at(k), C, r);

@@ -93,11 +93,6 @@ struct Common {
 
 // The arithmetic of each value, the same wherever it is done: a product and a sum that the compiler may or may not join, or a sum that it may round to 16 bits without
 // rounding to 32 first, would differ from kernel to kernel.
-__device__ __forceinline__ float in_32_bits(float x)
-{
-    asm("" : "+v"(x));
-    return x;
-}
 __device__ __forceinline__ float b_of(float o, float di, float dj, float sum) { return in_32_bits(__builtin_fmaf(NS_C, __builtin_fmaf(di + dj, o, sum), NS_B * o)); }        // off the diagonal
 __device__ __forceinline__ float e_of(float d, float sum) { return __builtin_fmaf(NS_C, __builtin_fmaf(d, d, sum), NS_B * d); }                                  // on it
 __device__ __forceinline__ float x_of(float e, f16_t hi, f16_t lo, float sum) { return in_32_bits(__builtin_fmaf(NS_A + e, __builtin_fmaf((float)lo, LO_DOWN, (float)hi), sum * S_DOWN)); }

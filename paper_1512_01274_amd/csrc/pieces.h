@@ -10,6 +10,13 @@ typedef unsigned Bytes16 __attribute__((ext_vector_type(4), aligned(2)));       
 // Keeps a value where it is in registers: what is made of it before is not kept for after, in more of them.
 __device__ __forceinline__ void held(uint4 &v) { asm volatile("" : "+v"(v.x), "+v"(v.y), "+v"(v.z), "+v"(v.w)); }
 
+// x rounded to 32 bits: the compiler does not join what made it with what it goes into.
+__device__ __forceinline__ float in_32_bits(float x)
+{
+    asm("" : "+v"(x));
+    return x;
+}
+
 template <class T> struct Piece;
 template <> struct Piece<float> {
     static constexpr int VE = 4;

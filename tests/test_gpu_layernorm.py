@@ -216,6 +216,42 @@ def test_gradient_where_the_mean_over_the_deviation_is_past_all_numbers(mxc, dty
             assert bool(((got.double() - exact).abs() <= tol).all()), (N, tuple(got.shape))
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("C", [3, 24, 49, 100, 1000, 4097, 5000, 12000, 20001])
+def test_rows_whose_values_hardly_differ(mxc, dtype, C):
+    """Rows of one value have a variance of 0 whatever the value, and rows of two neighbouring numbers that of half their distance: a rounding of the mean, which is of the
+    distance's size, may not enter."""
+    code, N = mxc.dtype_code(dtype), 130
+    x, _, gamma, beta = data(N, C, dtype, C)
+    g = torch.Generator(device="cuda").manual_seed(C)
+    value = (torch.exp2(torch.arange(N, device="cuda") % 22 + 3.0) * (1.0 + torch.rand(N, generator=g, device="cuda"))).to(dtype)
+    x[:] = value[:, None]
+    step = torch.exp2(torch.floor(torch.log2(value.float())) - (23 if dtype == torch.float32 else 7))
+    x[1::2, 1::2] = (value.float() + step).to(dtype)[1::2, None]
+    assert bool((x[1::2, 1] != x[1::2, 0]).all())
+    y, stats = torch.empty_like(x), torch.empty(N, 2, device="cuda")
+    mxc.mxc_layernorm_fwd(N, C, code, x, gamma, beta, 1e-5, y, stats)
+    eps = float(torch.tensor(1e-5, dtype=torch.float32))
+    want, mean, rstd, d, var = forward64(x, gamma.double(), beta.double(), eps)
+    k = chain(C)
+    # The mean's first rounding is off by `delta` at most; the differences from it are exact (numbers within a factor of two of each other).  Their sum is exact too where they are
+    # some hundred units of a last place, so that their mean is off by two roundings of at most delta; where they are a step of bf16 the chain's roundings of them count.
+    delta = 1.01 * (k + 2) * U * mean.abs()
+    e_c = 1.01 * (k + 2) * U * d.abs().amax(1, keepdim=True) + 2.1 * U * delta
+    # (all rows here are ones that the kernels take so: their mean is 16 deviations and more away from zero)
+    V = var + eps
+    assert bool((mean.abs() > 17 * V.sqrt()).all())
+    e_var = (k + 5) * U * var + 2 * var.sqrt() * e_c + 1.1 * e_c * e_c
+    e_rstd = rstd * (e_var / (2 * V) * 1.1 + 4 * U)
+    assert bool(((stats[:, :1].double() - mean).abs() <= 1.01 * (U * mean.abs() + e_c)).all())
+    assert bool(((stats[:, 1:].double() - rstd).abs() <= 1.01 * e_rstd).all())
+    z = d * rstd
+    e_z = 1.01 * rstd * (e_c + U * delta) + d.abs() * e_rstd + 1.01 * U * z.abs()
+    e_y = e_z * gamma.abs() + U * (z * gamma).abs() + U * (want.abs() + beta.abs())
+    bad = ~((y.double() - want).abs() <= 1.01 * (e_y + HALF[dtype] * (want.abs() + e_y)))
+    assert not bool(bad.any()), (int(bad.sum()), bad.nonzero()[:3])
+
+
 def test_rows_that_are_not_finite(mxc):
     """They make NaN of themselves and of what they enter, and leave other rows alone."""
     for C in (24, 5000, 20000):
