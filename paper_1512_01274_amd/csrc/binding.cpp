@@ -354,34 +354,41 @@ WRAP(mxc_layernorm_bwd, 10, N_("N", "C", "dtype", "x", "gamma", "stats", "dy", "
      PTR_IN(dx, 7, d[2], count(d[0], d[1])); PTR_OF(dgamma, 8, Float, count(d[1])); PTR_OF(dbeta, 9, Float, count(d[1])); BUF(ws, 10); STREAM(11);
      RUN(mxc_layernorm_bwd(d[0], d[1], d[2], x, (const float *)gamma, (const float *)stats, dy, dx, (float *)dgamma, (float *)dbeta, ws, ws_n, st));)
 
-// rows and columns of the matrices in argument 0: a tensor of more dimensions is the matrix of its first by the rest (a filter's outputs by its taps)
-bool to_sides(PyObject *o, std::vector<int> *rows, std::vector<int> *cols)
+// Rows and columns of a list's matrices: a tensor of more dimensions is the matrix of its first by the rest (a filter's outputs by its taps).  first: of the list that says what they
+// are; those of the others have to be the same (a matrix and its transpose have as many values), but for values without rows, of one dimension.
+bool to_sides(PyObject *o, const char *name, bool first, std::vector<int> *rows, std::vector<int> *cols)
 {
     const Py_ssize_t n = o && (PyList_Check(o) || PyTuple_Check(o)) ? PySequence_Fast_GET_SIZE(o) : 0;
     for (Py_ssize_t i = 0; i < n; ++i) {
-        const at::Tensor &t = THPVariable_Unpack(PySequence_Fast_GET_ITEM(o, i));        // (to_ptrs has seen that it is one)
+        const at::Tensor &t = THPVariable_Unpack(PySequence_Fast_GET_ITEM(o, i));        // (to_ptrs has seen that it is one, and how many values it has)
+        if (!first && t.dim() == 1) continue;
         if (t.dim() < 2) {
-            PyErr_Format(PyExc_ValueError, "[%zd]: a matrix has two dimensions or more, got %d", i, (int)t.dim());
+            PyErr_Format(PyExc_ValueError, "%s[%zd]: a matrix has two dimensions or more, got %d", name, i, (int)t.dim());
             return false;
         }
         long long r = t.size(0), c = 1;
         for (int64_t k = 1; k < t.dim(); ++k) c *= t.size(k);
         if (r > INT_MAX || c > INT_MAX) {
-            PyErr_Format(PyExc_OverflowError, "[%zd]: %lld x %lld does not fit an int", i, r, c);
+            PyErr_Format(PyExc_OverflowError, "%s[%zd]: %lld x %lld does not fit an int", name, i, r, c);
             return false;
         }
-        rows->push_back((int)r);
-        cols->push_back((int)c);
+        if (first) {
+            rows->push_back((int)r);
+            cols->push_back((int)c);
+        } else if (r != (*rows)[(size_t)i] || c != (*cols)[(size_t)i]) {
+            PyErr_Format(PyExc_ValueError, "%s[%zd]: a matrix of %lld x %lld, expected %d x %d", name, i, r, c, (*rows)[(size_t)i], (*cols)[(size_t)i]);
+            return false;
+        }
     }
     return true;
 }
-#define SIDES std::vector<int> rows, cols; if (!to_sides(a.v[0], &rows, &cols)) return nullptr
+#define SIDES(AT) if (!to_sides(a.v[AT], names[AT], (AT) == 0, &rows, &cols)) return nullptr
 WRAP(mxc_orthogonalize, 3, N_("x", "steps", "y", "workspace", "stream"),
-     std::vector<size_t> numel; PTRS(g, 0, Undefined); SIDES; INT(steps, 1); PTRS(y, 2, BFloat16); GRAD_TYPE; BUF(ws, 3); STREAM(4);
+     std::vector<size_t> numel; std::vector<int> rows, cols; PTRS(g, 0, Undefined); SIDES(0); INT(steps, 1); PTRS(y, 2, BFloat16); SIDES(2); GRAD_TYPE; BUF(ws, 3); STREAM(4);
      RUN(mxc_orthogonalize((int)rows.size(), rows.data(), cols.data(), LIST(g), gt, steps, LIST(y), ws, ws_n, st));)
 WRAP(mxc_muon_update, 11, N_("w", "g", "m", "w_bf16", "lr", "momentum", "nesterov", "wd", "rms", "grad_scale", "steps", "workspace", "stream"),
-     std::vector<size_t> numel; PTRS(w, 0, Float); SIDES; PTRS(g, 1, Undefined); PTRS(m, 2, Float); PTRS(wb, 3, BFloat16); GRAD_TYPE;
-     FLOAT(lr, 4); FLOAT(mom, 5); BOOL(nesterov, 6); FLOAT(wd, 7); FLOAT(rms, 8); FLOAT(gs, 9); INT(steps, 10); BUF(ws, 11); STREAM(12);
+     std::vector<size_t> numel; std::vector<int> rows, cols; PTRS(w, 0, Float); SIDES(0); PTRS(g, 1, Undefined); SIDES(1); PTRS(m, 2, Float); SIDES(2); PTRS(wb, 3, BFloat16); SIDES(3);
+     GRAD_TYPE; FLOAT(lr, 4); FLOAT(mom, 5); BOOL(nesterov, 6); FLOAT(wd, 7); FLOAT(rms, 8); FLOAT(gs, 9); INT(steps, 10); BUF(ws, 11); STREAM(12);
      RUN(mxc_muon_update((int)rows.size(), rows.data(), cols.data(), (float *const *)LIST(w), LIST(g), gt, (float *const *)LIST(m), LIST(wb), lr, mom, nesterov, wd, rms, gs, steps,
                          ws, ws_n, st));)
 WRAP(mxc_layout_convert, 9, N_("n", "c", "h", "w", "dtype", "src_layout", "dst_layout", "src", "dst", "stream"),

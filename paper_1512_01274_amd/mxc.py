@@ -186,7 +186,8 @@ def _stream(stream):
 
 # The entry points, with these arguments (workspace and stream may be left out; tensors may be None where the header
 # allows it).  They are built-in functions of the extension module (csrc/binding.cpp) and raise MxcError on a status.  The
-# log-probability, 4-bit, AdamW, embedding, layer norm, orthogonalise and Muon calls raise TypeError or ValueError for tensors of another element type or too few elements.
+# log-probability, 4-bit, AdamW, embedding, layer norm, orthogonalise and Muon calls raise TypeError or ValueError for tensors of another element type or too few elements,
+# the last two also for matrices of other sides than the first list's (a tensor of one dimension there has its values).
 #
 #   mxc_conv2d_workspace_bytes(op, N, C, H, W, K, R, S, stride, pad, dtype, layout) -> int
 #   mxc_conv2d_fwd(N, C, H, W, K, R, S, stride, pad, dtype, layout, x, w, y, workspace=None, stream=None)

@@ -175,6 +175,36 @@ def test_binding_types_and_sizes(mxc):
             mxc.mxc_orthogonalize_workspace_bytes(bad, bad)
 
 
+def test_binding_compares_sides(mxc):
+    """Every list's matrices have the sides of the first list's: as many values in other rows are refused, more dimensions than two are the first by the rest."""
+    import torch
+    from torch._subclasses.fake_tensor import FakeTensorMode
+    f32, bf = torch.float32, torch.bfloat16
+    args = (1e-3, 0.9, True, 0.1, 0.2, 1.0, 5, None, 0)
+    with FakeTensorMode():
+        new = lambda *s, dtype=f32: torch.empty(*s, dtype=dtype, device="cuda")  # noqa: E731
+        right = dict(w=[new(4, 6), new(8, 3, 5)], g=[new(4, 6), new(8, 15)], m=[new(4, 2, 3), new(8, 5, 3)], w_bf16=[new(4, 6, dtype=bf), new(8, 15, 1, dtype=bf)])
+        with pytest.raises(mxc.MxcError) as e:          # (fake tensors: null pointers)
+            mxc.mxc_muon_update(*right.values(), *args)
+        assert e.value.status == mxc.MXC_ERR_NULL
+        for name in ("g", "m", "w_bf16"):
+            for i, others in ((0, [(6, 4), (2, 12), (3, 2, 4), (24, 1)]), (1, [(15, 8), (24, 5), (3, 8, 5)])):
+                for other in others:
+                    wrong = list(right[name])
+                    wrong[i] = new(*other, dtype=right[name][i].dtype)
+                    with pytest.raises(ValueError, match=name + r"\[%d\]: a matrix of" % i):
+                        mxc.mxc_muon_update(*{**right, name: wrong}.values(), *args)
+            with pytest.raises(mxc.MxcError) as e:      # values without rows: those of the first list's
+                mxc.mxc_muon_update(*{**right, name: [new(24, dtype=right[name][0].dtype), right[name][1]]}.values(), *args)
+            assert e.value.status == mxc.MXC_ERR_NULL
+        for x, y in ((new(4, 6), new(6, 4, dtype=bf)), (new(3, 4, 5, dtype=bf), new(12, 5, dtype=bf)), (new(4, 6), new(1, 24, dtype=bf))):
+            with pytest.raises(ValueError, match=r"y\[0\]"):
+                mxc.mxc_orthogonalize([x], 5, [y], None, 0)
+        with pytest.raises(mxc.MxcError) as e:
+            mxc.mxc_orthogonalize([new(4, 6), new(3, 4, 5)], 5, [new(4, 2, 3, dtype=bf), new(3, 20, dtype=bf)], None, 0)
+        assert e.value.status == mxc.MXC_ERR_NULL
+
+
 def test_binding_sizes_past_32_bits(mxc):
     for big in (1 << 32, (1 << 32) + 5, 1 << 31, -(1 << 31) - 1):
         for call, args in ((mxc.mxc_embedding_workspace_bytes, [5, 7, 9, 1]), (mxc.mxc_layernorm_workspace_bytes, [5, 9, 1]),
