@@ -30,28 +30,35 @@ class Model:
                   for i, s in enumerate(shapes)]
         self.copy = [w.bfloat16() for w in self.w]
         self.grad, self.m, self.v = ([torch.zeros_like(w) for w in self.w] for _ in range(3))
-        self.step, self._buffers = 0, {}
+        self.step, self._buffers, self._workspaces, self._need = 0, {}, {}, {}
         self._update = mxc.alloc_workspace(mxc.mxc_orthogonalize_workspace_bytes(*zip(*(shapes[i] for i in FILTERS))), device=device)
 
     def _of_batch(self, N):
-        """Activations, gradients and workspace for batches of N, made once."""
-        if N not in self._buffers:
-            V, C, H, T = self.dims
-            device = self.w[0].device
-            new = lambda *s, dtype=torch.bfloat16: torch.empty(*s, dtype=dtype, device=device)  # noqa: E731
+        """Activations, gradients and workspace for batches of N.  Rows of a buffer and bytes of a workspace are a power of two, each made once and kept, for a captured step goes on using
+        them: all together are less than twice the largest of each."""
+        V, C, H, T = self.dims
+        device, rows = self.w[0].device, 1 << (N - 1).bit_length()
+        if N not in self._need:
             need = [mxc.mxc_conv2d_workspace_bytes(op, N, c, 1, 1, k, 1, 1, 1, 0, BF16, mxc.MXC_NHWC) for c, k in ((T * C, H), (H, C), (C, V))
                     for op in (mxc.MXC_FWD, mxc.MXC_BWD_DATA, mxc.MXC_BWD_DATA_RELU, mxc.MXC_BWD_WEIGHT, mxc.MXC_BIAS_GRAD)]
             need += [mxc.mxc_logprob_workspace_bytes(N, V, BF16, top) for top in (0, min(V, 5))]
             need += [mxc.mxc_embedding_workspace_bytes(N * T, V, C, BF16), mxc.mxc_layernorm_workspace_bytes(N * T, C, BF16), mxc.mxc_layernorm_workspace_bytes(N, C, BF16)]
-            self._buffers[N] = {"e": new(N * T, C), "a": new(N * T, C), "s0": new(N * T, 2, dtype=torch.float32), "h": new(N, H), "u": new(N, C), "o": new(N, C),
-                                "s1": new(N, 2, dtype=torch.float32), "z": new(N, V), "da": new(N * T, C), "dh": new(N, H), "du": new(N, C),
-                                "weight": torch.full((N,), -1.0 / N, device=device), "workspace": mxc.alloc_workspace(max(need), device=device)}
-        return self._buffers[N]
+            self._need[N] = 1 << max(max(need) - 1, 0).bit_length()
+        if rows not in self._buffers:
+            new = lambda *s, dtype=torch.bfloat16: torch.empty(*s, dtype=dtype, device=device)  # noqa: E731
+            self._buffers[rows] = {"e": new(rows * T, C), "a": new(rows * T, C), "s0": new(rows * T, 2, dtype=torch.float32), "h": new(rows, H), "u": new(rows, C), "o": new(rows, C),
+                                   "s1": new(rows, 2, dtype=torch.float32), "z": new(rows, V), "da": new(rows * T, C), "dh": new(rows, H), "du": new(rows, C),
+                                   "weight": new(rows, dtype=torch.float32)}
+        if self._need[N] not in self._workspaces:
+            self._workspaces[self._need[N]] = mxc.alloc_workspace(self._need[N], device=device)
+        return {**self._buffers[rows], "workspace": self._workspaces[self._need[N]]}
 
     def _rows(self, tokens):
         V, C, H, T = self.dims
         if tokens.dim() != 2 or tokens.shape[1] != T or tokens.dtype != torch.int32 or not tokens.is_contiguous():
             raise ValueError(f"expected dense int32 rows of {T} tokens, got {tokens.dtype} of shape {tuple(tokens.shape)}")
+        if tokens.shape[0] == 0:
+            raise ValueError("expected rows of tokens, got none")
         return tokens.shape[0]
 
     def _forward(self, N, tokens, b):
@@ -71,6 +78,7 @@ class Model:
         b = self._of_batch(N)
         copy, grad, ws = self.copy, self.grad, b["workspace"]
         self._forward(N, tokens, b)
+        b["weight"].fill_(-1.0 / N)         # (batches of other sizes have the same buffers)
         mxc.mxc_logprob_fwd_bwd(N, V, V, BF16, b["z"], labels, 1.0, b["weight"], None, logp, None, b["z"], ws)
         mxc.mxc_fc_bwd_weight(N, C, V, BF16, b["o"], b["z"], grad[TABLE], ws)
         mxc.mxc_fc_bwd_data(N, C, V, BF16, b["z"], copy[TABLE], None, b["du"], ws)

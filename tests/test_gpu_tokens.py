@@ -194,6 +194,29 @@ def test_captured(tokens):
         assert all(torch.equal(a, b) for a, b in zip(model.grad + model.w + [logp], want))
 
 
+def test_captured_among_other_batch_sizes(tokens):
+    """A captured batch's gradients keep their bits when eager batches of more and of fewer rows come between."""
+    V, C, H, T = 300, 72, 100, 3
+    model, batch = tokens.Model(V, C, H, T), tokens.text(V, T)
+    rows, labels = batch(100)
+    logp = torch.empty(100, device="cuda")
+    model.gradients(rows, labels, logp)
+    want = [t.clone() for t in model.grad + [logp]]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        model.gradients(rows, labels, logp)
+    for N in (120, 65, 7, 400, 100):
+        other = torch.empty(N, device="cuda")
+        model.gradients(*batch(N), other)
+        model.predict(batch(N)[0])
+        for t in model.grad + [logp]:
+            t.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(model.grad + [logp], want)), N
+
+
 def test_on_another_stream(tokens):
     """The same model's steps on a stream of their own have the bits of the first stream's."""
     runs = []

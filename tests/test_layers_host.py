@@ -234,6 +234,30 @@ def test_model_refuses_other_rows():
     assert rows.shape == (70, 3) and labels.shape == (70,) and bool((rows[0] == -1).all()) and torch.equal(rows[1:64, -1], labels[:63])
 
 
+def test_model_of_many_batch_sizes_holds_twice_the_largest(mxc):
+    """What is kept for batches of all sizes is less than twice the largest's buffers and twice the largest workspace (sums of powers of two), and stays where it is; a batch of no rows is
+    refused."""
+    import torch
+    from paper_1512_01274_amd.tokens import Model
+    model = Model(17, 12, 20, 3, device="cpu")
+    with pytest.raises(ValueError, match="rows"):
+        model.predict(torch.zeros(0, 3, dtype=torch.int32))
+    with pytest.raises(ValueError, match="rows"):
+        model.train_step(torch.zeros(0, 3, dtype=torch.int32), torch.zeros(0, dtype=torch.int32))
+    buffers, workspaces = {}, {}
+    for N in [1, 300, *range(2, 513, 7), 300, 512, 5]:
+        b = model._of_batch(N)
+        for name, rows in (("e", 3 * N), ("da", 3 * N), ("s0", 3 * N), ("h", N), ("z", N), ("weight", N), ("s1", N)):
+            assert b[name].shape[0] >= rows and b[name].is_contiguous()
+        ws = b.pop("workspace")
+        assert ws is None or ws.nbytes >= mxc.mxc_layernorm_workspace_bytes(3 * N, 12, 1)
+        workspaces[0 if ws is None else ws.data_ptr()] = 0 if ws is None else ws.nbytes
+        buffers.setdefault(tuple(t.data_ptr() for t in b.values()), sum(t.nbytes for t in b.values()))
+        again = model._of_batch(N)
+        assert again["workspace"] is ws and all(again[k] is t for k, t in b.items())
+    assert sum(buffers.values()) < 2 * max(buffers.values()) and sum(workspaces.values()) < 2 * max(workspaces.values())
+
+
 def test_layernorm_workspace_of_the_longest(mxc):
     """The most rows of rows that registers do not hold: two sums a row and a share of the weights' gradients, in sizes past 32 bits."""
     for C in (40000, mxc.MXC_LAYERNORM_MAX_C):
