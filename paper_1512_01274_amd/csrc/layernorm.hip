@@ -507,8 +507,13 @@ int with_share(const Share &h, F &&f)
     return MXC_ERR_LAUNCH;
 }
 
+// rows for which one launch makes dx and the weights' gradients; us, two launches and one: 128 x 1000 fp32 8.1, 4.8; 256 x 4096 bf16 10.1, 5.0; 512 x 4096 11.2, 7.5; 1024 x 64 fp32 8.1,
+// 9.5; 1024 x 1000 bf16 10.6, 19.9
+bool is_few(int N) { return N <= 512; }
+
 struct BwdPlan {
     Share h;
+    bool few;                           // one launch, which leaves nothing for another
     int workgroups;                     // of rows in registers
     int rows, ranges, pitch;            // ranges: shares of dgamma and dbeta
     size_t part_bytes, sums_bytes;
@@ -517,6 +522,7 @@ BwdPlan bwd_plan(int N, int C, int dtype)
 {
     BwdPlan q = {};
     q.h = share_of(C, dtype);
+    q.few = q.h.PC && is_few(N);
     q.pitch = (int)align_up(C, 4);
     if (q.h.PC) {
         // 18 waves a compute unit (8: 105 us at 16384 x 4096 bf16, 16: 79.5; of rows that a wave shares 24 are no better), and few workgroups where there are few rows, for
@@ -532,7 +538,7 @@ BwdPlan bwd_plan(int N, int C, int dtype)
         q.ranges = (int)(((long long)N + q.rows - 1) / q.rows);
         q.sums_bytes = align_up((size_t)N * 8, 256);
     }
-    q.part_bytes = align_up((size_t)q.ranges * 2 * q.pitch * 4, 256);
+    q.part_bytes = q.few ? 0 : align_up((size_t)q.ranges * 2 * q.pitch * 4, 256);
     return q;
 }
 
@@ -554,17 +560,13 @@ int fwd(int N, int C, int dtype, const T *x, const float *gamma, const float *be
     });
 }
 
-// rows for which one launch makes dx and the weights' gradients; us, two launches and one: 128 x 1000 fp32 8.1, 4.8; 256 x 4096 bf16 10.1, 5.0; 512 x 4096 11.2, 7.5; 1024 x 64 fp32 8.1,
-// 9.5; 1024 x 1000 bf16 10.6, 19.9
-bool is_few(int N) { return N <= 512; }
-
 template <class T>
 int bwd(int N, int C, int dtype, const T *x, const float *gamma, const float *stats, const T *dy, T *dx, float *dgamma, float *dbeta, char *ws, hipStream_t st)
 {
     const BwdPlan q = bwd_plan(N, C, dtype);
     float *part = (float *)ws;
     if (q.h.PC) {
-        const bool few = is_few(N);
+        const bool few = q.few;
         const int rc = with_share<T>(q.h, [&](auto tpr, auto pc) {
             constexpr int TPR = decltype(tpr)::value, PC = decltype(pc)::value;
             const int threads = TPR ? ROW_NT : 64 * q.h.waves;

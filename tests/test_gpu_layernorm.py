@@ -324,3 +324,17 @@ def test_streams_and_graphs(mxc):
         assert all(torch.equal(a, b) for a, b in zip(got, outs))
         if turn == 0:
             assert all(torch.equal(a, b) for a, b in zip(got, first))
+
+
+@pytest.mark.parametrize("N,C", [(512, 200), (512, 4097), (3, 12000), (1, 1)])
+def test_gradient_of_few_rows_needs_no_workspace(mxc, N, C):
+    for dtype in (torch.float32, torch.bfloat16):
+        x, dy, gamma, beta = data(N, C, dtype, 5)
+        stats, code = torch.empty(N, 2, device="cuda"), mxc.dtype_code(dtype)
+        mxc.mxc_layernorm_fwd(N, C, code, x, gamma, beta, 1e-3, torch.empty_like(x), stats)
+        want, wg, wb, parts = backward64(x, gamma.double(), stats, dy)
+        for in_place in (False, True):
+            dx, dgamma, dbeta = dy.clone() if in_place else torch.empty_like(x), torch.empty(C, device="cuda"), torch.empty(C, device="cuda")
+            mxc.mxc_layernorm_bwd(N, C, code, x, gamma, stats, dx if in_place else dy, dx, dgamma, dbeta)
+            for got, exact, tol in zip((dx, dgamma, dbeta), (want, wg, wb), backward_tolerance(parts, want, dtype)):
+                assert bool(((got.double() - exact).abs() <= tol + 1e-42).all())

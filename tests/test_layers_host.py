@@ -263,3 +263,12 @@ def test_layernorm_workspace_of_the_longest(mxc):
     for C in (40000, mxc.MXC_LAYERNORM_MAX_C):
         need = [mxc.mxc_layernorm_workspace_bytes(N, C, 1) for N in (1 << 30, (1 << 31) - 4096, (1 << 31) - 1)]
         assert need == sorted(need) and need[-1] >= 8 * ((1 << 31) - 1) + 8 * C
+
+
+def test_layernorm_workspace_is_of_what_a_second_launch_adds(mxc):
+    """The gradient of up to 512 rows that registers hold is one launch, which leaves nothing for another."""
+    for dtype in (0, 1):
+        for C in (1, 100, 4097, 16384):
+            assert [mxc.mxc_layernorm_workspace_bytes(N, C, dtype) for N in (1, 100, 512)] == [0, 0, 0]
+            assert mxc.mxc_layernorm_workspace_bytes(513, C, dtype) > 0
+        assert mxc.mxc_layernorm_workspace_bytes(1, 16385, dtype) > 0
