@@ -406,7 +406,7 @@ int mxc_adamw8_update(int count, const size_t *sizes, void *const *w, const void
  *   mxc_embedding_bwd:  dw[v,c] = scale * sum over n with tokens[n] == v of dy[n,c], zeros for a token that stands nowhere; with accumulate == 1 this
  *                       is added to the dw that is there, and rows of tokens that stand nowhere are neither read nor written (a table whose product
  *                       with the last layer's input has left its gradient there)
- * Sums in fp32 in an order that depends on the tokens alone (bit-identical from run to run).  Workspace: mxc_embedding_workspace_bytes, for the
+ * Sums in fp32 in an order that depends on N, V, C and the tokens alone (bit-identical from run to run).  Workspace: mxc_embedding_workspace_bytes, for the
  * gradient.  Errors: MXC_ERR_SHAPE (non-positive sizes, N, V or C above the limits below), MXC_ERR_UNSUPPORTED (dtype, scale that is not finite,
  * accumulate), MXC_ERR_NULL, MXC_ERR_ALIGN (16 bytes, 4 for tokens), MXC_ERR_WORKSPACE, MXC_ERR_LAUNCH.
  */
@@ -425,7 +425,9 @@ int mxc_embedding_bwd(int N, int V, int C, int dtype, const int *tokens, const v
  *                       gamma (ones), dgamma and dbeta may each be NULL; dx may be dy or x
  * Arithmetic, stats, dgamma and dbeta are fp32 (the squares are those of the differences from the mean, and where the mean is more than 16 deviations, sqrt(var + eps), from zero
  * its rounding is taken out of z and the variance too: a large mean costs no digits; the gradient's z has the mean as stats hold it), y and dx are rounded
- * once to `dtype`; an infinity or a NaN makes NaN of its row's results and of the gradients that it enters.  dgamma and dbeta are added in a fixed order.
+ * once to `dtype`.  An infinity or a NaN in x makes NaN of its row's y and dx and of all of dgamma, and its row's stats are not finite; one in dy makes values that are not
+ * finite of its row's dx and of its column's dgamma and dbeta.  Other rows and columns are left alone.  A row whose sum passes the
+ * largest fp32 number has NaN for y; one whose sum of squared differences does has rstd 0 and beta for y.  dgamma and dbeta are added in a fixed order.
  * Workspace: mxc_layernorm_workspace_bytes, for the gradient.  Errors: MXC_ERR_SHAPE (non-positive sizes, C above MXC_LAYERNORM_MAX_C), MXC_ERR_UNSUPPORTED
  * (dtype; eps that is not a normal positive number), MXC_ERR_NULL, MXC_ERR_ALIGN (16 bytes, 4 for stats), MXC_ERR_WORKSPACE, MXC_ERR_LAUNCH.
  */

@@ -267,6 +267,47 @@ def test_rows_that_are_not_finite(mxc):
         assert bool(dgamma.isnan().all()) and bool(dbeta.isfinite().all())
 
 
+@pytest.mark.parametrize("N", [6, 600])
+def test_gradients_that_are_not_finite(mxc, N):
+    """An infinity or a NaN in dy enters its row's dx and its column's sums, one in x its row's dx and all of dgamma; the rest is as without them."""
+    for C in (24, 5000, 20000):
+        for dtype in (torch.float32, torch.bfloat16):
+            x, dy, gamma, beta = data(N, C, dtype, C)
+            code, stats, ws = mxc.dtype_code(dtype), torch.empty(N, 2, device="cuda"), mxc.alloc_workspace(mxc.mxc_layernorm_workspace_bytes(N, C, mxc.dtype_code(dtype)))
+
+            def grads():
+                mxc.mxc_layernorm_fwd(N, C, code, x, gamma, beta, 1e-5, torch.empty_like(x), stats)
+                dx, dgamma, dbeta = torch.empty_like(x), torch.empty(C, device="cuda"), torch.empty(C, device="cuda")
+                mxc.mxc_layernorm_bwd(N, C, code, x, gamma, stats, dy, dx, dgamma, dbeta, ws)
+                return dx, dgamma, dbeta
+
+            clean = grads()
+            dy[1, 3], dy[4, C - 1], dy[5, 3] = math.inf, math.nan, -math.inf
+            rows, columns = torch.zeros(N, dtype=torch.bool, device="cuda"), torch.zeros(C, dtype=torch.bool, device="cuda")
+            rows[[1, 4, 5]], columns[[3, C - 1]] = True, True
+            dx, dgamma, dbeta = grads()
+            assert not bool(dx[rows].isfinite().any()) and torch.equal(dx[~rows], clean[0][~rows])
+            for got, was in ((dgamma, clean[1]), (dbeta, clean[2])):
+                assert not bool(got[columns].isfinite().any()) and torch.equal(got[~columns], was[~columns])
+            x[2, 0] = -math.inf
+            rows[2] = True
+            dx, dgamma, dbeta = grads()
+            assert bool(dx[2].isnan().all()) and torch.equal(dx[~rows], clean[0][~rows])
+            assert bool(dgamma.isnan().all()) and torch.equal(dbeta[~columns], clean[2][~columns]) and not bool(stats[2].isfinite().any())
+
+
+@pytest.mark.parametrize("C", [100, 5000, 20000])
+def test_rows_whose_sums_pass_the_largest_number(mxc, C):
+    x, _, gamma, beta = data(4, C, torch.float32, C)
+    x[1], x[2] = 2.0 ** 125, 2.0 ** 70 * (torch.arange(C, device="cuda") % 2 * 2.0 - 1.0)
+    y, stats = torch.empty_like(x), torch.empty(4, 2, device="cuda")
+    mxc.mxc_layernorm_fwd(4, C, 0, x, gamma, beta, 1e-5, y, stats)
+    assert bool(y[1].isnan().all()) and torch.equal(y[2], beta) and float(stats[2, 1]) == 0.0
+    alone, few = torch.empty(2, C, device="cuda"), torch.empty(2, 2, device="cuda")
+    mxc.mxc_layernorm_fwd(2, C, 0, x[::3].contiguous(), gamma, beta, 1e-5, alone, few)
+    assert torch.equal(y[::3], alone) and torch.equal(stats[::3], few)
+
+
 def test_offsets_past_32_bits(mxc):
     """More than 2^31 values: the last rows as those of a small call."""
     N, C = 66000, 32768
