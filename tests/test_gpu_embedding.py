@@ -130,6 +130,16 @@ def test_gradient(mxc, dtype, add, N, V, C, kind):
     assert intact(whole, dw) and intact(ws_whole, ws, 5)
 
 
+# More places of a segment than a wave holds in registers (over 16384 a segment), up to a million; tables of 256 MB and more, whose rows go past the caches, with more places than one
+# launch takes
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("add", [False, True])
+@pytest.mark.parametrize("N,V,C,kind", [(100000, 50257, 8, "common"), (20000, 300000, 4, "uniform"), (99999, 1000, 3, "runs129"), (300000, 7, 4, "one"), (1000001, 50257, 4, "common"),
+                                        (3000, 33000, 2048, "common"), (5000, 70000, 1001, "uniform")])
+def test_gradient_of_many_places_and_rows(mxc, dtype, add, N, V, C, kind):
+    test_gradient(mxc, dtype, add, N, V, C, kind)
+
+
 def test_gradient_is_that_of_differences(mxc):
     """Along a direction of the table: the change of a weighted sum of the forward formula, which is linear in it."""
     g = gen(3)

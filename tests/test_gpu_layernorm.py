@@ -166,6 +166,14 @@ def test_gradient(mxc, dtype, N, C):
     assert torch.equal(dx, results[0][0])
 
 
+# Rows of two and four pieces a lane over more rows than workgroups, with the next row's loads under way (6000) and without (12000), and of 256 MB and more, which go past the caches
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("N,C", [(600, 6000), (600, 12000), (700, 16383), (4000, 12000), (8000, 6001)])
+def test_many_rows_of_several_pieces(mxc, dtype, N, C):
+    test_forward(mxc, dtype, N, C)
+    test_gradient(mxc, dtype, N, C)
+
+
 @pytest.mark.parametrize("N,C", [(4, 9), (3, 300), (2, 17000)])
 def test_gradient_is_that_of_differences(mxc, N, C):
     """Central differences of the forward formula in 64 bits along random directions of x, gamma and beta."""

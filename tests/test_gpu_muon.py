@@ -218,6 +218,61 @@ def test_large(mxc, r, c):
         check(y, x, 5)
 
 
+# Sides at which products have tiles of 128, 192 and 256, whole ones, ones that are split over the reduction, and both beside each other (the tiles of the three products, and into how
+# many parts the last ones are split): 128 128 192; 256/5 256/5 256/4; 64/16 64 256; 128/3 64 192; 128/14 64 256; 192 192 256/2; 256 256 256/3; either way round
+TILED = [(3000, 2900), (5990, 6010), (6010, 5990), (2048, 8192), (8190, 2050), (1024, 32768), (4100, 9200), (9200, 4100), (4500, 4500)]
+
+
+@pytest.mark.parametrize("r,c", TILED)
+def test_tiles(mxc, r, c):
+    x = matrix(r, c, "few", 6).bfloat16()
+    whole, y = guarded((r, c), torch.bfloat16)
+    ws_whole, ws = workspace(mxc, [(r, c)])
+    mxc.mxc_orthogonalize([x], 5, [y], ws)
+    check(y, x, 5)
+    # No value by itself is far off, as one of a wrong row or block would be: besides the result's own rounding a value's error is the sum of many roundings, of which none of 2^26 passes
+    # six deviations where all have the norm's, and 16 where some rows have more of it.
+    want = orthogonal64(x, 5)
+    assert bool(((y.double() - want).abs() <= 2.0 ** -8 * want.abs() + 16 * tolerance(x, 5, want) / math.sqrt(r * c)).all())
+    del want
+    assert intact(whole, y) and intact(ws_whole, ws, 5)
+    # twice, and beside others, with the same bits
+    first = y.clone()
+    ws.fill_(255)
+    mxc.mxc_orthogonalize([x], 5, [y], ws)
+    assert torch.equal(first, y)
+    shapes = [(130, 70), (r, c), (1100, 2300), (64, 1000)]
+    xs = [x if s == (r, c) else matrix(*s, "random", 7).bfloat16() for s in shapes]
+    ys = [torch.empty(s, dtype=torch.bfloat16, device="cuda") for s in shapes]
+    mxc.mxc_orthogonalize(xs, 5, ys, workspace(mxc, shapes)[1])
+    assert torch.equal(first, ys[1])
+
+
+@pytest.mark.parametrize("r,c", [(4100, 9200), (9200, 4100)])
+def test_update_by_split_tiles(mxc, r, c):
+    """The last step's third product, whose split tiles write the weights when their parts are added."""
+    for nesterov, dtype in ((True, torch.float32), (False, torch.bfloat16)):
+        lr, momentum, wd, rms = 3e-2, 0.95, 0.1, 0.2
+        w, g, m = matrix(r, c, "random", 1) * 0.1, (matrix(r, c, "few", 2) * 1e-3).to(dtype), matrix(r, c, "few", 3) * 1e-2
+        whole, wb = guarded((r, c), torch.bfloat16)
+        w_whole, now = guarded((r, c), torch.float32)
+        now.copy_(w)
+        was = m.clone()
+        mxc.mxc_muon_update([now], [g], [m], [wb], lr, momentum, nesterov, wd, rms, 0.5, 5, workspace(mxc, [(r, c)])[1])
+        mu = float(torch.tensor(momentum, dtype=torch.float32))
+        m1 = mu * was.double() + 0.5 * g.double()
+        assert bool(((m.double() - m1).abs() <= 2 * U * (mu * was.abs().double() + m1.abs()) + 1e-42).all())
+        u = (0.5 * g.double() + mu * m.double() if nesterov else m).float()
+        del m1, was
+        o = orthogonal64(u, 5)
+        step = lr * rms * math.sqrt(max(r, c))
+        off = now.double() - ((1.0 - lr * wd) * w.double() - step * o)
+        tol = step * tolerance(u, 5, o) + 4 * U * float((w.abs() + step * o.abs()).norm())
+        assert float(off.norm()) <= tol, (float(off.norm()), tol)
+        assert float(off.abs().max()) <= 16 * tol / math.sqrt(r * c)        # a value by itself, as in test_tiles
+        assert torch.equal(wb, now.bfloat16()) and intact(whole, wb) and intact(w_whole, now)
+
+
 def test_longest_sides(mxc):
     for r, c in ((32768, 3), (70, 32768)):
         x = matrix(r, c, "random", 4)

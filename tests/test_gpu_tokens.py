@@ -126,6 +126,27 @@ def test_gradient_is_the_difference(tokens):
     assert abs(got - (losses[0] - losses[1]) / (2 * h)) <= 2.0 ** -4.6 * norm * size
 
 
+@pytest.mark.parametrize("which", range(9))
+def test_gradient_of_each_tensor_is_the_difference(tokens, which):
+    """The loss's change along one tensor's own gradient g, by differences of the network in 64 bits, against |g|: a gradient that is missing is off by all of it, one of the other sign by
+    twice that.  A rounding to bf16 is off by 2^-9.8 of a tensor's norm (a half step of 2^-8, evenly spread over values between two powers of two); ten of them between the
+    calls make 2^-8.1, eight times that where terms cancel (2^-5.1), and 2^-3 leaves four times that."""
+    model, _, rows, labels = trained(tokens, SIZES[0], 2)
+    logp = torch.empty(rows.shape[0], device="cuda")
+    model.gradients(rows, labels, logp)
+    g = model.grad[which].double().cpu()
+    size = float(g.norm())
+    assert size > 0
+    copies, weights, losses, h = model.copy, model.w, [], 1e-5
+    for sign in (1, -1):
+        model.w, model.copy = [w.double().cpu() for w in weights], [c.double().cpu() for c in copies]
+        for tensors in (model.w, model.copy):
+            tensors[which] = tensors[which] + sign * h * g / size
+        losses.append(-float(plain(tokens, model, rows, labels)[0].mean()))
+    change = (losses[0] - losses[1]) / (2 * h)
+    assert abs(change - size) <= 2.0 ** -3 * size
+
+
 @pytest.mark.parametrize("sizes", SIZES[:3])
 def test_updates(tokens, sizes):
     """What a step changes, by the gradients that it leaves.  Filters: the momentum is fp32 arithmetic of two operations; the step has singular values of 0.68 to 1.21
