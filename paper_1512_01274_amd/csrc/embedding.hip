@@ -482,10 +482,10 @@ int fwd(int N, int V, int C, const int *tokens, const T *w, float scale, T *y, h
     return launched();
 }
 
-// groups of the whole workgroup where those of a wave would make too many workgroups, each of which looks at all places
 // One launch or three.  Up to 1024 places one; up to 2048 where the looking (each place among all, for each 256 columns) and the longest run of one workgroup cost less than two
 // launches: us, one and three: 2048 places on 50257 x 512 bf16 8.1, 18.9; x 2048 17.7, 23.7; on 5000 x 4096 fp32 53, 27.7; on 2 x 512 30.6, 17.9; 4096 places on 10000 x 300 31, 19.2
 bool is_few(int N, int V, int C) { return N <= 1024 || (N <= FEW && V >= 256 && (long long)N * C <= 1 << 22); }
+// groups of the whole workgroup where those of a wave would make too many workgroups, each of which looks at all places
 int few_lanes(int N, int C) { return (long long)N * ((C + 255) / 256) <= 4096 ? group_lanes(C) : 8; }
 
 template <class T>

@@ -13,6 +13,8 @@ namespace mxc {
 namespace {
 
 // ---- any length: a row's values are read again for each sum -------------------------------------------------------------------
+//
+// 2048 x 20000 bf16: forward 170 us, where a row's three passes follow one another, gradient 151 in two launches: 1.0 and 1.6 TB/s of what has to be read and written.
 
 constexpr int LONG_NT = 1024;
 // sum over a workgroup of LONG_NT threads; `part` is free again after the next call's first barrier
@@ -358,7 +360,8 @@ __device__ __forceinline__ void columns_of(int N, int C, int c0, const T *x, con
     if (out && c0 + (int)threadIdx.x % COLUMNS < C) out[c0 + threadIdx.x % COLUMNS] = s;
 }
 
-// FEW rows: workgroups behind those of the rows make dgamma and dbeta in the same launch, reading the rows again.  AHEAD: with the next row's loads under way; rows of more than 8 waves have no registers for it
+// FEW rows: workgroups behind those of the rows make dgamma and dbeta in the same launch, reading the rows again.  AHEAD: with the next row's loads under way; rows of
+// more than 8 waves of several pieces have no registers for it (fp32 rows of four pieces keep 16 in scratch as it is): 4096 x 12000 bf16 84 us, 2048 x 12000 fp32 82, 3.5 TB/s
 template <class T, int TPR, int PC, bool AHEAD, bool PAST, bool FEW>
 __global__ __launch_bounds__(TPR ? ROW_NT : AHEAD && PC > 1 ? 512 : 1024) void bwd_rows_kernel(int N, int C, const T *x, const float *gamma, const float *stats, const T *dy, T *dx, float *parts, int pitch,
                                                                                                 int row_groups, float *dgamma, float *dbeta)
@@ -526,7 +529,7 @@ BwdPlan bwd_plan(int N, int C, int dtype)
     q.pitch = (int)align_up(C, 4);
     if (q.h.PC) {
         // 18 waves a compute unit (8: 105 us at 16384 x 4096 bf16, 16: 79.5; of rows that a wave shares 24 are no better), and few workgroups where there are few rows, for
-        // each leaves a share that is read again: 512 x 4096 with 512 workgroups 12.8, with 256 11.0
+        // each leaves a share that is read again: 1024 x 4096 bf16 with 512 workgroups 17.9, with 256 15.0, x 2048 16.1 and 11.5 (but fp32 x 4096 18.2 and 20.5)
         const int G = q.h.TPR ? ROW_NT / q.h.TPR : 1, waves = q.h.TPR ? ROW_NT / 64 : q.h.waves;
         const long long need = ((long long)N + G - 1) / G, most = 256ll * (waves > 18 || need <= 1024 ? 1 : 18 / waves);
         q.ranges = q.workgroups = (int)(need < most ? need : most);
@@ -574,17 +577,24 @@ int bwd(int N, int C, int dtype, const T *x, const float *gamma, const float *st
                 hipLaunchKernelGGL(kernel, dim3(groups + columns), dim3(threads), few ? threads / 8 * 2 * COLUMNS * 4 : 0, st, N, C, x, gamma, stats, dy, dx, part, q.pitch, groups, dgamma, dbeta);
                 return launched();
             };
-            const bool ahead = TPR || PC == 1 || q.h.waves <= 8;
+            // the kernel with the next row's loads under way, or of rows of more than 8 waves of several pieces without
+            auto kernel_of = [&](auto past, auto one) {
+                constexpr bool PAST = decltype(past)::value, FEW = decltype(one)::value;
+                if constexpr (TPR == 0 && PC > 1)
+                    if (q.h.waves > 8) return bwd_rows_kernel<T, 0, PC, false, PAST, FEW>;
+                return bwd_rows_kernel<T, TPR, PC, true, PAST, FEW>;
+            };
+            constexpr std::true_type yes{};
+            constexpr std::false_type no{};
             if (few) {
-                const auto kernel = ahead ? bwd_rows_kernel<T, TPR, PC, true, false, true> : bwd_rows_kernel<T, 0, PC, false, false, true>;
+                const auto kernel = kernel_of(no, yes);
                 const int columns = dgamma || dbeta ? (C + COLUMNS - 1) / COLUMNS : 0;
                 // in place: what the columns read is overwritten only after them
                 const bool apart = columns && ((const void *)dx == x || (const void *)dx == dy);
                 if (apart && launch(kernel, 0, columns) != MXC_OK) return (int)MXC_ERR_LAUNCH;
                 return launch(kernel, q.workgroups, apart ? 0 : columns);
             }
-            if (past_caches(N, C, 3, dtype)) return launch(ahead ? bwd_rows_kernel<T, TPR, PC, true, true, false> : bwd_rows_kernel<T, 0, PC, false, true, false>, q.workgroups, 0);
-            return launch(ahead ? bwd_rows_kernel<T, TPR, PC, true, false, false> : bwd_rows_kernel<T, 0, PC, false, false, false>, q.workgroups, 0);
+            return launch(past_caches(N, C, 3, dtype) ? kernel_of(yes, no) : kernel_of(no, no), q.workgroups, 0);
         });
         if (rc != MXC_OK || few) return rc;
     } else {

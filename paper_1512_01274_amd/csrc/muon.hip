@@ -1176,14 +1176,18 @@ struct Shape {
     unsigned finish_groups() const { return (unsigned)(bm / 32) * (bn / wn()) / FINISH; }
     int wn() const { return bn == 64 ? 32 : 64; }
 };
-#define TILES(BM, BN, NS, WR, WC, PER_CU, ...)                                                                                                                       \
+// Products whose tiles may be split, so that their parts are added.  The model splits those of X's square at every shape, of A's at 256 alone and thirds at 256 and, for six of all
+// pairs of sides in steps of 64, at 128.
+template <int...> constexpr Finish no_finish = nullptr;
+#define TILES(BM, BN, NS, WR, WC, PER_CU, FINISH_A, FINISH_THIRD, ...)                                                                                               \
     {BM, BN, 64 * WR * WC, PER_CU, __VA_ARGS__,                                                                                                                        \
      {product_kernel<BM, BN, NS, WR, WC, SQUARE_X>, product_kernel<BM, BN, NS, WR, WC, SQUARE_A>, product_kernel<BM, BN, NS, WR, WC, THIRD>}, \
-     {finish_kernel<BM, BN, WR, WC, SQUARE_X>, finish_kernel<BM, BN, WR, WC, SQUARE_A>, finish_kernel<BM, BN, WR, WC, THIRD>}}
+     {finish_kernel<BM, BN, WR, WC, SQUARE_X>, FINISH_A<BM, BN, WR, WC, SQUARE_A>, FINISH_THIRD<BM, BN, WR, WC, THIRD>}}
 // (times measured on 512 x 512 to 8192 x 8192; the model is within a tenth of most launches, those of small tiles a quarter.  64 x 64 twice: four stages in LDS for few tiles, which
 // wait for their loads, or two and twice the workgroups for many short ones.  42 filters of up to 512: 93 tiles of squares 9.6 and 13 us, 615 of thirds 14.8 and 10.8)
-const Shape SHAPES[SHAPE_COUNT] = {TILES(64, 64, 4, 2, 2, 2, 0.38, 0.26, 4.5, 2), TILES(64, 64, 2, 2, 2, 4, 0.76, 0.45, 4.5, 2), TILES(128, 128, 2, 2, 2, 2, 1.0, 0.66, 10, 14),
-                                   TILES(192, 192, 2, 2, 3, 1, 1.13, 1.13, 14, 18), TILES(256, 256, 2, 2, 4, 1, 1.35, 1.35, 18, 33)};
+const Shape SHAPES[SHAPE_COUNT] = {TILES(64, 64, 4, 2, 2, 2, no_finish, no_finish, 0.38, 0.26, 4.5, 2), TILES(64, 64, 2, 2, 2, 4, no_finish, no_finish, 0.76, 0.45, 4.5, 2),
+                                   TILES(128, 128, 2, 2, 2, 2, no_finish, finish_kernel, 1.0, 0.66, 10, 14), TILES(192, 192, 2, 2, 3, 1, no_finish, no_finish, 1.13, 1.13, 14, 18),
+                                   TILES(256, 256, 2, 2, 4, 1, finish_kernel, finish_kernel, 1.35, 1.35, 18, 33)};
 
 // tiles and stages of a reduction
 struct Load {
@@ -1243,7 +1247,7 @@ Split split_of(const Sizes &s, int kind, std::vector<Busy> &busy)
         unsplit = std::min(unsplit, time_of(h, kind, &all, 1, busy));
         unsigned by = rest ? std::min(slots / rest, 16u) : 1;
         by = std::min(by, (unsigned)stages / 8);
-        if (by < 2) continue;
+        if (by < 2 || !h.finish[kind]) continue;
         const Load rounds = {all.tiles - rest, stages}, pieces = {rest * by, (int)((stages + by - 1) / by)};
         // the pieces' sums are written and read at some 5 TB/s
         const double us = (rounds.tiles ? time_of(h, kind, &rounds, 1, busy) : 0.0) + time_of(h, 0, &pieces, 1, busy) + 6.0 + pieces.tiles * (h.bm * h.bn * 8.0 / 5e6) + (kind == THIRD ? h.store * rest / slots : 0.0);

@@ -120,13 +120,6 @@ __device__ __forceinline__ void settle_quad(Quad &q, int at, int len)
 }
 __device__ __forceinline__ Piece<float> begin_quad(const float *row, int at, int len) { return begin_piece(row, at, len); }
 __device__ __forceinline__ void settle_quad(Piece<float> &p, int at, int len) { settle_piece(p, at, len); }
-template <class T>
-__device__ __forceinline__ auto load_quad(const T *row, int at, int len)
-{
-    auto q = begin_quad(row, at, len);
-    settle_quad(q, at, len);
-    return q;
-}
 template <bool PAST = false, class T>
 __device__ __forceinline__ void store_piece(T *row, int at, int len, const Piece<T> &p)
 {

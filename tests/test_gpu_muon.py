@@ -219,8 +219,10 @@ def test_large(mxc, r, c):
 
 
 # Sides at which products have tiles of 128, 192 and 256, whole ones, ones that are split over the reduction, and both beside each other (the tiles of the three products, and into how
-# many parts the last ones are split): 128 128 192; 256/5 256/5 256/4; 64/16 64 256; 128/3 64 192; 128/14 64 256; 192 192 256/2; 256 256 256/3; either way round
-TILED = [(3000, 2900), (5990, 6010), (6010, 5990), (2048, 8192), (8190, 2050), (1024, 32768), (4100, 9200), (9200, 4100), (4500, 4500)]
+# many parts the last ones are split): 128 128 192; 256/5 256/5 256/4; 64/16 64 256; 128/3 64 192; 128/14 64 256; 192 192 256/2; 256 256 256/3; either way round; and first products
+# 64/9 of the other kind, 192/9, 256/12, 128/16 and 192/12 beside whole ones, a third 128/4
+TILED = [(3000, 2900), (5990, 6010), (6010, 5990), (2048, 8192), (8190, 2050), (1024, 32768), (4100, 9200), (9200, 4100), (4500, 4500),
+         (890, 22300), (22900, 1340), (1472, 26560), (4032, 20990), (4416, 23680), (2430, 7550)]
 
 
 @pytest.mark.parametrize("r,c", TILED)
