@@ -2,8 +2,8 @@
 // and g = dy * gamma,
 //     dx = rstd * (g - sum(g) / C - z * sum(g * z) / C),   dgamma[c] = sum_n dy * z,   dbeta[c] = sum_n dy.
 // Memory bounds both: a row is read once (x, and dy), held in registers over its sums, and written once; rows that registers do not hold are read again.
-// Sums are fp32: a thread's values one after the other, then lanes and waves as a tree; squares are of differences from the mean.  16384 x 4096 bf16: forward 50 us,
-// 5.4 TB/s, gradient 78, 5.2 TB/s with the shares of dgamma and dbeta; rows of 4097 values, which begin at any element, 62.5 and 95.6; 128 x 1000 fp32 4.4 and 4.8, a launch
+// Sums are fp32: a thread's values one after the other, then lanes and waves as a tree; squares are of differences from the mean.  16384 x 4096 bf16: forward 48 us,
+// 5.6 TB/s, gradient 78, 5.2 TB/s with the shares of dgamma and dbeta; rows of 4097 values, which begin at any element, 62 and 96; 128 x 1000 fp32 4.4 and 4.7, a launch
 // each.
 #include <type_traits>
 
